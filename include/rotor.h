@@ -405,6 +405,160 @@ ROTOR_API int32_t rotor_even_budgets(int64_t top, int32_t n, int64_t *budgets);
 ROTOR_API int32_t rotor_sequence_cost(const int64_t *h_params, int32_t L, const rotor_op *h_ops, int64_t n_ops,
                                       int64_t *time, int64_t *peak);
 
+/* ---- operators of a language-model chain's stages ------------------------
+ *
+ * What a chain of language-model stages needs around its blocks' own products
+ * when its forwards may run again: every result, gradients included, is the
+ * same bit for bit whenever the same call is made (no floating-point atomics,
+ * no generator state), and what a stage keeps for its backward is small: no
+ * mask, 16 bytes per row of a norm, 4 bytes per token of the loss, never a
+ * logit.
+ *
+ * Types.  `type` is the element type of the floating-point tensors of a call
+ * (ROTOR_F32, ROTOR_BF16 or ROTOR_F16); sums, statistics and losses are
+ * computed and kept in 32 bits, and every result is rounded once.
+ * Tensors.  A matrix of `rows` x `cols` elements starts at its pointer, with
+ * `pitch` (>= cols) elements from one row to the next and adjacent columns
+ * adjacent.  Any pitch and any element-aligned pointer is accepted; 16-byte
+ * aligned rows are the fast case.  Outputs may not overlap inputs unless
+ * stated.  Streams, errors and ownership are as above: nothing is allocated,
+ * every call only enqueues, and a call without elements returns ROTOR_OK
+ * after writing what it still has to (gradients of nothing are 0). */
+#define ROTOR_F32 0
+#define ROTOR_BF16 1
+#define ROTOR_F16 2
+
+/* Dropout whose mask is drawn from a counter and never stored:
+ *   y = residual + (keep(i) ? x * 65536 / (65536 - t) : 0),  t = round(65536 p)
+ * element by element; residual may be NULL (0).  i is the element's index in
+ * row-major order (row * cols + col, whatever the pitches).  keep(i) takes
+ * 16 bits of Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random
+ * numbers: as easy as 1, 2, 3", 2011): key = `seed` (low word first), counter
+ * = (i / 8, `step`), each as two 32-bit words, low first; of the four output
+ * words element i takes word (i % 8) / 2, the low half if i is even; it is
+ * kept if those bits are >= t.  So the same (seed, step) gives the same mask
+ * in every call, and the gradient of x is this function on the gradient of y
+ * (residual NULL); that of the residual is the gradient of y itself.
+ * A dropped element of x is never used: it may be infinite or NaN.
+ *   p       0 <= p <= 1 (p = 1 drops everything).
+ *   d_step  DEVICE, one int64 added to `step`, or NULL: for a captured graph,
+ *           whose replays then draw masks of their own.
+ *   d_y     may be d_x or d_residual (with the same pitch).
+ * Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_dropout(int32_t type, int64_t rows, int64_t cols, const void *d_x, int64_t x_pitch,
+                                const void *d_residual, int64_t residual_pitch, void *d_y, int64_t y_pitch,
+                                double p, uint64_t seed, uint64_t step, const int64_t *d_step, void *stream);
+
+/* Embedding lookup with scaling: y[i] = scale * table[tokens[i]].
+ *   d_tokens  DEVICE, n_tokens indices of token_bytes (4 or 8) bytes each,
+ *             signed.  A token outside [0, n_rows) reads nothing and gives a
+ *             row of NaN.
+ *   d_table   DEVICE [n_rows][cols];  d_y DEVICE, written [n_tokens][cols].
+ * n_tokens < 2^31, 1 <= n_rows < 2^31.  Returns ROTOR_OK, ROTOR_EINVAL or
+ * ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_embedding(int32_t type, int64_t n_tokens, int64_t n_rows, int64_t cols, const void *d_tokens,
+                                  int32_t token_bytes, const void *d_table, int64_t table_pitch, double scale,
+                                  void *d_y, int64_t y_pitch, void *stream);
+
+/* Device workspace of rotor_embedding_backward for these sizes: the tokens
+ * in sorted order, twice, and two rows of sums per 32 tokens.  Host only.
+ * Returns ROTOR_OK or ROTOR_EINVAL. */
+ROTOR_API int32_t rotor_embedding_workspace_bytes(int64_t n_tokens, int64_t n_rows, int64_t cols, uint64_t *bytes);
+
+/* Gradient of the table: dtable[v] = scale * sum over i with tokens[i] = v of
+ * dy[i], every row of it written (0 where no token is v).  The tokens are
+ * sorted on the device, stably, and each row's terms are added in an order
+ * that depends on the tokens alone.
+ *   d_dy       DEVICE [n_tokens][cols], the gradient of y.
+ *   padding    a token without a gradient (its row of dtable is 0), or -1.
+ *   d_dtable   DEVICE, written: [n_rows][cols], of the same type.
+ *   d_work     DEVICE scratch of rotor_embedding_workspace_bytes, 16-byte
+ *              aligned (NULL if that is 0).
+ * Tokens outside [0, n_rows) add nothing, nor do NaN or infinities at tokens
+ * that are padding or outside.  Returns ROTOR_OK, ROTOR_EINVAL or
+ * ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows, int64_t cols,
+                                           const void *d_tokens, int32_t token_bytes, const void *d_dy,
+                                           int64_t dy_pitch, double scale, int64_t padding, void *d_dtable,
+                                           int64_t dtable_pitch, void *d_work, uint64_t work_bytes, void *stream);
+
+/* The seam between two blocks of a chain: the norm after a block, its gate
+ * and the scale of the residual stream, and the norm before the next block,
+ * in one pass:
+ *   y = residual_scale * x + gate * post(z),   h = pre(y)
+ * with x the residual stream, z the block's output, both [rows][cols], and
+ * per row u of z (post) or y (pre), n its normed row:
+ *   ROTOR_NORM_NONE   the norm is left out: post(z) = z; without pre there is
+ *                     no h
+ *   ROTOR_NORM_RMS    n = u / sqrt(mean(u^2) + eps)
+ *   ROTOR_NORM_LAYER  n = (u - mean(u)) / sqrt(mean((u - mean(u))^2) + eps)
+ * and the norm's output n * weight + bias ([cols] each, of the call's type;
+ * NULL: 1, and 0).  pre(y) takes y before it is rounded. */
+#define ROTOR_NORM_NONE 0
+#define ROTOR_NORM_RMS 1
+#define ROTOR_NORM_LAYER 2
+#define ROTOR_NORM_MAX_COLS 16384
+
+typedef struct {
+    int32_t type, post, pre;
+    int32_t reserved;       /* 0 */
+    int64_t rows, cols;     /* rows >= 0, 1 <= cols <= ROTOR_NORM_MAX_COLS */
+    int64_t gate_rows;      /* rows of gate: row r takes row r / (rows / gate_rows); must
+                               divide rows (1: one gate for all; 0: no gate, a factor 1) */
+    int64_t gate_pitch;
+    double residual_scale, eps; /* eps >= 0 */
+    const void *post_weight, *post_bias; /* DEVICE [cols] or NULL; NULL without post */
+    const void *gate;                    /* DEVICE [gate_rows][cols], NULL if gate_rows is 0 */
+    const void *pre_weight, *pre_bias;   /* DEVICE [cols] or NULL; NULL without pre */
+} rotor_norm;
+
+/* y and h as above.
+ *   d_z      DEVICE or NULL: no block, y = residual_scale * x (post must be
+ *            ROTOR_NORM_NONE, gate_rows 0).
+ *   d_y      DEVICE, written; NULL if d_z is NULL and residual_scale is 1 (y
+ *            is x).
+ *   d_h      DEVICE, written; NULL if and only if pre is ROTOR_NORM_NONE.
+ *   d_stats  DEVICE, written: [rows][4] floats, mean and 1 / deviation of the
+ *            row's post norm, then of its pre norm (0 and 1 where there is
+ *            none; of y as rounded where that rounding is large against the
+ *            row's deviation); 16-byte aligned.  NULL: not kept (no backward
+ *            follows).
+ * Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_residual_norm(const rotor_norm *how, const void *d_x, int64_t x_pitch, const void *d_z,
+                                      int64_t z_pitch, void *d_y, int64_t y_pitch, void *d_h, int64_t h_pitch,
+                                      float *d_stats, void *stream);
+
+/* Device workspace of rotor_residual_norm_backward for these sizes (`how`'s
+ * pointers are not used): sums over strips of rows.  Host only.  Returns
+ * ROTOR_OK or ROTOR_EINVAL. */
+ROTOR_API int32_t rotor_residual_norm_workspace_bytes(const rotor_norm *how, uint64_t *bytes);
+
+/* Gradients of the parameters, DEVICE, written, of the call's type, with the
+ * shapes of the parameters; NULL: not wanted. */
+typedef struct {
+    void *post_weight, *post_bias, *gate, *pre_weight, *pre_bias;
+    int64_t gate_pitch;
+} rotor_norm_grads;
+
+/* Gradients of everything rotor_residual_norm takes, from those of y and h.
+ *   how      as given to rotor_residual_norm.
+ *   d_dy     DEVICE or NULL (0);  d_dh  DEVICE; NULL if and only if pre is
+ *            ROTOR_NORM_NONE (then d_dy is required).
+ *   d_y, d_z, d_stats  what rotor_residual_norm wrote and read (d_y is not
+ *            used, and may be NULL, without pre; d_z NULL as there).
+ *   d_dx     DEVICE, written;  d_dz  DEVICE, written; NULL if d_z is.
+ *   grads    HOST, the parameters' gradients.
+ *   d_work   DEVICE scratch of rotor_residual_norm_workspace_bytes, 16-byte
+ *            aligned.
+ * Sums over rows are taken in an order that depends on the sizes alone.
+ * Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_residual_norm_backward(const rotor_norm *how, const void *d_dy, int64_t dy_pitch,
+                                               const void *d_dh, int64_t dh_pitch, const void *d_y, int64_t y_pitch,
+                                               const void *d_z, int64_t z_pitch, const float *d_stats, void *d_dx,
+                                               int64_t dx_pitch, void *d_dz, int64_t dz_pitch,
+                                               const rotor_norm_grads *grads, void *d_work, uint64_t work_bytes,
+                                               void *stream);
+
 #ifdef __cplusplus
 }
 #endif

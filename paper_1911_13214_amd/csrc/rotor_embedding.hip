@@ -1,0 +1,501 @@
+// rotor_embedding: rows of a table by token, scaled; and the table's gradient
+// by sorted tokens.
+//
+// Backward: a stable radix sort of (token, position), one launch per digit of
+// up to 9 bits; then one launch in which groups of lanes take 32 sorted
+// positions each, add the rows of one token in registers and write each token
+// that lies within their positions, while the remaining workgroups clear the
+// rows of tokens that do not occur; then one launch that joins the tokens
+// that cross the 32-position cuts.  No atomics on the sums: their order
+// depends on the tokens alone.
+#include "rotor_ops.h"
+
+namespace rotor {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kVec = 8;        // adjacent elements of a lane, V below (1 in rows of fewer)
+constexpr int kChunk = 32;     // sorted positions of a group
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kPart = 2048;    // keys that one workgroup of the sort moves
+constexpr int kDigits = 512;
+
+// First column of piece k of a row, V columns each.  The last piece is moved
+// back to end with the row: what it shares with the one before is computed
+// and written twice, with the same bits.
+template <int V> __device__ inline int64_t column(int64_t k, int64_t cols)
+{
+    return k * V < cols - V ? k * V : cols - V;
+}
+
+__device__ inline int64_t token_at(const void *tokens, int bytes, int64_t i)
+{
+    return bytes == 8 ? ((const int64_t *)tokens)[i] : ((const int32_t *)tokens)[i];
+}
+
+// ---- forward ------------------------------------------------------------------
+
+// A wave per token (several for few tokens); lanes read V adjacent elements
+// each, so 16-bit rows move in pieces of 1 KiB.
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void lookup_kernel(const void *tokens, int token_bytes, int64_t n, int64_t rows,
+                                                          int64_t cols, const T *table, int64_t pitch, float scale,
+                                                          T *y, int64_t y_pitch)
+{
+    const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    if (i >= n)
+        return;
+    const int64_t t = token_at(tokens, token_bytes, i);
+    const bool in = t >= 0 && t < rows;
+    const T *src = table + (in ? t : 0) * pitch;
+    T *dst = y + i * y_pitch;
+    const int64_t pieces = (cols + V - 1) / V;
+    for (int64_t k = threadIdx.x % 64 + 64 * blockIdx.y; k < pieces; k += 64 * gridDim.y) {
+        const int64_t c = column<V>(k, cols);
+        float v[V];
+        load_vec(src + c, v);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            v[j] = in ? v[j] * scale : __builtin_nanf("");
+        store_vec(dst + c, v);
+    }
+}
+
+// ---- sort -----------------------------------------------------------------------
+
+// One pass of a stable radix sort over the digit key >> shift, `bits` wide
+// (<= 9).  The first pass reads the tokens and leaves out those without a
+// gradient; later ones read the pass before.  Every workgroup counts all keys
+// (the digits of the keys before its own part and of all), so no pass needs a
+// launch for its counts: 4 bytes a key from the L2, against the 2 cols bytes
+// of its row that the sums read later.
+struct SortArgs {
+    const void *tokens;
+    int token_bytes;
+    int64_t n, rows, padding;
+    const uint32_t *key_in, *pos_in;
+    uint32_t *key_out, *pos_out;
+    int32_t *count;  // keys that are sorted: written by the first pass, read by the others
+    int shift, bits;
+};
+
+template <bool FIRST> __device__ inline bool sort_key(const SortArgs &a, int64_t i, uint32_t &key)
+{
+    if (FIRST) {
+        const int64_t t = token_at(a.tokens, a.token_bytes, i);
+        key = (uint32_t)t;
+        return t >= 0 && t < a.rows && t != a.padding;
+    }
+    key = a.key_in[i];
+    return true;
+}
+
+// Orders LDS accesses of the lanes of one wave, which runs in step.
+__device__ inline void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs a)
+{
+    __shared__ uint32_t before[kDigits], from[kDigits];
+    __shared__ uint32_t at[kSortWaves][kDigits];
+    __shared__ uint32_t wave_total[kSortWaves];
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const uint32_t mask = (1u << a.bits) - 1;
+    const int64_t n = FIRST ? a.n : (int64_t)*a.count;
+    const int64_t part = (int64_t)blockIdx.x * kPart;
+    for (int d = tid; d < kDigits; d += kSortThreads) {
+        before[d] = 0;
+        from[d] = 0;
+        for (int w = 0; w < kSortWaves; ++w)
+            at[w][d] = 0;
+    }
+    __syncthreads();
+    if (part >= n && !(FIRST && blockIdx.x == 0))
+        return;  // the whole workgroup
+    // digits of the keys before the part, and of the rest
+    for (int64_t i = tid; i < n; i += kSortThreads) {
+        uint32_t key;
+        if (sort_key<FIRST>(a, i, key))
+            atomicAdd(&(i < part ? before : from)[key >> a.shift & mask], 1u);
+    }
+    // digits of each wave's own keys: kPart / kSortWaves adjacent ones
+    constexpr int kOwn = kPart / kSortWaves;
+    const int64_t own = part + (int64_t)wave * kOwn;
+    for (int k = lane; k < kOwn; k += 64) {
+        uint32_t key;
+        if (own + k < n && sort_key<FIRST>(a, own + k, key))
+            atomicAdd(&at[wave][key >> a.shift & mask], 1u);
+    }
+    __syncthreads();
+    // first place of each digit (threads 0..511, one digit each), then of
+    // each wave's first key of that digit
+    const uint32_t all = tid < kDigits ? before[tid] + from[tid] : 0;
+    uint32_t upto = all;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        const uint32_t u = __shfl_up(upto, off);
+        if (lane >= off)
+            upto += u;
+    }
+    if (lane == 63)
+        wave_total[wave] = upto;
+    __syncthreads();
+    if (tid < kDigits) {
+        uint32_t base = upto - all;
+        for (int w = 0; w < wave; ++w)
+            base += wave_total[w];
+        base += before[tid];
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = at[w][tid];
+            at[w][tid] = base;
+            base += c;
+        }
+    }
+    if (FIRST && blockIdx.x == 0 && tid == 0) {
+        uint32_t total = 0;
+        for (int w = 0; w < kDigits / 64; ++w)
+            total += wave_total[w];
+        *a.count = (int32_t)total;
+    }
+    __syncthreads();
+    // 64 keys at a time, in order: a key's place is its digit's next one plus
+    // the lanes before it that hold the same digit
+    for (int k = 0; k < kOwn; k += 64) {
+        const int64_t i = own + k + lane;
+        uint32_t key = 0;
+        const bool have = i < n && sort_key<FIRST>(a, i, key);
+        const uint32_t d = key >> a.shift & mask;
+        uint64_t same = __ballot(have);
+        for (int b = 0; b < a.bits; ++b) {
+            const uint64_t set = __ballot(have && (d >> b & 1));
+            same &= d >> b & 1 ? set : ~set;
+        }
+        if (have) {
+            const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
+            const uint32_t place = at[wave][d] + rank;
+            a.key_out[place] = key;
+            a.pos_out[place] = FIRST ? (uint32_t)i : a.pos_in[i];
+        }
+        wave_sync();
+        if (have && (same >> lane) == 1)  // the last lane of its digit
+            at[wave][d] += __popcll(same);
+        wave_sync();
+    }
+}
+
+// ---- sums -----------------------------------------------------------------------
+
+struct SumArgs {
+    int64_t rows, cols, dy_pitch, out_pitch;
+    const uint32_t *key, *pos;
+    const int32_t *count;
+    float *part;        // [chunks][2][part_pitch]: sums of the token that enters, and of the one that leaves
+    int64_t part_pitch;
+    float scale;
+    int lanes;          // lanes of a group: a power of two, 64 at least
+    uint32_t slices;    // workgroups side by side over a row's columns
+    uint32_t sum_blocks;  // the rest of the grid clears rows
+};
+
+// 64 rows a wave: a lane looks for its row's token, then the wave clears the
+// rows of those that do not occur.
+template <typename T, int V> __device__ void clear_rows(T *out, const SumArgs &a, int64_t n, int64_t r0)
+{
+    const int lane = threadIdx.x % 64;
+    const int64_t r = r0 + lane;
+    int64_t lo = 0, hi = r < a.rows ? n : 0;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (a.key[mid] < (uint32_t)r)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    uint64_t absent = __ballot(r < a.rows && !(lo < n && a.key[lo] == (uint32_t)r));
+    const int64_t pieces = (a.cols + V - 1) / V;
+    const float zero[V] = {};
+    while (absent) {
+        const int k = __builtin_ctzll(absent);
+        absent &= absent - 1;
+        T *dst = out + (r0 + k) * a.out_pitch;
+        for (int64_t q = lane; q < pieces; q += 64)
+            store_vec(dst + column<V>(q, a.cols), zero);
+    }
+}
+
+template <typename T, int V> __global__ __launch_bounds__(kThreads) void sum_kernel(const T *dy, T *out, SumArgs a)
+{
+    const int64_t n = *a.count;
+    if (blockIdx.x >= a.sum_blocks) {
+        clear_rows<T, V>(out, a, n,
+                         ((int64_t)(blockIdx.x - a.sum_blocks) * (kThreads / 64) + threadIdx.x / 64) * 64);
+        return;
+    }
+    const int64_t chunk = (int64_t)(blockIdx.x / a.slices) * (kThreads / a.lanes) + threadIdx.x / a.lanes;
+    const int64_t begin = chunk * kChunk;
+    if (begin >= n)
+        return;
+    const int64_t end = begin + kChunk < n ? begin + kChunk : n;
+    const int64_t piece = (int64_t)(blockIdx.x % a.slices) * a.lanes + threadIdx.x % a.lanes;
+    if (piece * V >= a.cols)
+        return;
+    const int64_t c = column<V>(piece, a.cols);
+    const bool enters = begin > 0 && a.key[begin - 1] == a.key[begin];
+    const bool leaves = end < n && a.key[end] == a.key[end - 1];
+    float sum[V] = {};
+    bool whole = !enters;  // the present token starts here
+    constexpr int kAhead = 8;
+    for (int64_t i = begin; i < end; i += kAhead) {
+        float v[kAhead][V];
+        uint32_t key[kAhead + 1];
+        // past the end the last position again, which is not added
+#pragma unroll
+        for (int k = 0; k <= kAhead; ++k)
+            key[k] = a.key[i + k < n ? i + k : n - 1];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            load_vec(dy + (int64_t)a.pos[i + k < end ? i + k : end - 1] * a.dy_pitch + c, v[k]);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i + k >= end)
+                break;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                sum[j] += v[k][j];
+            const bool last = i + k + 1 == end;
+            if (!last && key[k + 1] == key[k])
+                continue;
+            if (whole && !(last && leaves)) {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    sum[j] *= a.scale;
+                store_vec(out + (int64_t)key[k] * a.out_pitch + c, sum);
+            } else {
+                // the first half for a token that enters (whether or not it
+                // also leaves), the second for one that starts here
+                store_vec(a.part + (chunk * 2 + (whole ? 1 : 0)) * a.part_pitch + c, sum);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                sum[j] = 0.f;
+            whole = true;
+        }
+    }
+}
+
+// Joins a token that starts in one chunk and leaves it: its sums of that
+// chunk and of all it enters, split over the four waves of a workgroup (64 *
+// V columns), each in order, the waves' sums then in order.
+template <typename T, int V> __global__ __launch_bounds__(kThreads) void join_kernel(T *out, SumArgs a)
+{
+    __shared__ float other[kThreads / 64 - 1][64][V + 1];
+    const int64_t n = *a.count;
+    const int64_t chunk = blockIdx.x;
+    const int64_t end = (chunk + 1) * kChunk;
+    if (end >= n)
+        return;
+    const uint32_t key = a.key[end - 1];
+    if (a.key[end] != key)
+        return;
+    const int64_t begin = chunk * kChunk;
+    if (begin > 0 && a.key[begin - 1] == key)
+        return;  // it started before (sorted: the chunk holds nothing else)
+    // one past the token's last position
+    int64_t lo = end + 1, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (a.key[mid] > key)
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    const int64_t last = (lo - 1) / kChunk;  // last chunk it enters
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t piece = (int64_t)blockIdx.y * 64 + lane;
+    const bool have = piece * V < a.cols;
+    const int64_t c = have ? column<V>(piece, a.cols) : 0;
+    const int64_t each = (last - chunk + kThreads / 64) / (kThreads / 64);
+    const int64_t from = chunk + wave * each, to = from + each < last + 1 ? from + each : last + 1;
+    float sum[V] = {};
+#pragma unroll 4
+    for (int64_t k = from; k < to; ++k) {
+        float v[V];
+        load_vec(a.part + (k * 2 + (k == chunk ? 1 : 0)) * a.part_pitch + c, v);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            sum[j] += v[j];
+    }
+    if (wave > 0)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            other[wave - 1][lane][j] = sum[j];
+    __syncthreads();
+    if (wave > 0 || !have)
+        return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        for (int w = 0; w < kThreads / 64 - 1; ++w)
+            sum[j] += other[w][lane][j];
+        sum[j] *= a.scale;
+    }
+    store_vec(out + (int64_t)key * a.out_pitch + c, sum);
+}
+
+// Workspace: key and position arrays of two passes, the count, the partial sums.
+struct EmbedLayout {
+    uint64_t key[2], pos[2], count, part, total;
+    int64_t part_pitch;
+};
+
+EmbedLayout embed_layout(int64_t n, int64_t cols)
+{
+    EmbedLayout l;
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t here = at;
+        at = round256(at + bytes);
+        return here;
+    };
+    for (int k = 0; k < 2; ++k) {
+        l.key[k] = take(4 * (uint64_t)n);
+        l.pos[k] = take(4 * (uint64_t)n);
+    }
+    l.count = take(4);
+    l.part_pitch = ceil_div(cols, kVec) * kVec;
+    l.part = take(8 * (uint64_t)ceil_div(n, kChunk) * (uint64_t)l.part_pitch);
+    l.total = at;
+    return l;
+}
+
+bool embed_sizes_ok(int64_t n, int64_t rows, int64_t cols)
+{
+    return n >= 0 && n < ((int64_t)1 << 31) && rows >= 1 && rows < ((int64_t)1 << 31) && cols >= 1 &&
+           cols < ((int64_t)1 << 31);
+}
+
+}  // namespace
+}  // namespace rotor
+
+using namespace rotor;
+
+extern "C" {
+
+int32_t rotor_embedding(int32_t type, int64_t n_tokens, int64_t n_rows, int64_t cols, const void *d_tokens,
+                        int32_t token_bytes, const void *d_table, int64_t table_pitch, double scale, void *d_y,
+                        int64_t y_pitch, void *stream)
+{
+    if (!type_ok(type) || !embed_sizes_ok(n_tokens, n_rows, cols) || (token_bytes != 4 && token_bytes != 8))
+        return ROTOR_EINVAL;
+    const int64_t es = elem_bytes(type);
+    if (!matrix_ok(d_table, n_rows, cols, table_pitch, es) || !matrix_ok(d_y, n_tokens, cols, y_pitch, es))
+        return ROTOR_EINVAL;
+    if (n_tokens == 0)
+        return ROTOR_OK;
+    if (!d_tokens || (uintptr_t)d_tokens % (uintptr_t)token_bytes)
+        return ROTOR_EINVAL;
+    (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
+    with_type(type, [&](auto e) {
+        typedef typename decltype(e)::T T;
+        // few tokens: a row's pieces over several waves
+        const int64_t pieces = ceil_div(cols, 64 * kVec);
+        const int64_t slices = n_tokens >= 1024 ? 1 : pieces < 64 ? pieces : 64;
+        const auto kernel = cols >= kVec ? lookup_kernel<T, kVec> : lookup_kernel<T, 1>;
+        kernel<<<dim3((uint32_t)ceil_div(n_tokens, kThreads / 64), (uint32_t)slices), kThreads, 0,
+                 (hipStream_t)stream>>>(d_tokens, token_bytes, n_tokens, n_rows, cols, (const T *)d_table,
+                                        table_pitch, (float)scale, (T *)d_y, y_pitch);
+    });
+    return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+}
+
+int32_t rotor_embedding_workspace_bytes(int64_t n_tokens, int64_t n_rows, int64_t cols, uint64_t *bytes)
+{
+    if (!bytes || !embed_sizes_ok(n_tokens, n_rows, cols))
+        return ROTOR_EINVAL;
+    *bytes = embed_layout(n_tokens, cols).total;
+    return ROTOR_OK;
+}
+
+int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows, int64_t cols, const void *d_tokens,
+                                 int32_t token_bytes, const void *d_dy, int64_t dy_pitch, double scale,
+                                 int64_t padding, void *d_dtable, int64_t dtable_pitch, void *d_work,
+                                 uint64_t work_bytes, void *stream)
+{
+    if (!type_ok(type) || !embed_sizes_ok(n_tokens, n_rows, cols) || (token_bytes != 4 && token_bytes != 8) ||
+        padding < -1 || padding >= n_rows)
+        return ROTOR_EINVAL;
+    const int64_t es = elem_bytes(type);
+    if (!matrix_ok(d_dy, n_tokens, cols, dy_pitch, es) || !matrix_ok(d_dtable, n_rows, cols, dtable_pitch, es))
+        return ROTOR_EINVAL;
+    if (n_tokens > 0 && (!d_tokens || (uintptr_t)d_tokens % (uintptr_t)token_bytes))
+        return ROTOR_EINVAL;
+    const EmbedLayout l = embed_layout(n_tokens, cols);
+    if (!d_work || (uintptr_t)d_work % 16 || work_bytes < l.total)
+        return ROTOR_EINVAL;
+    char *const w = (char *)d_work;
+    const hipStream_t s = (hipStream_t)stream;
+    (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
+
+    // as few passes as digits of 9 bits allow, of equal width
+    int bits = 0;
+    while (((int64_t)1 << bits) < n_rows)
+        ++bits;
+    const int passes = bits <= 9 ? 1 : (bits + 8) / 9;
+    const int width = bits == 0 ? 1 : (bits + passes - 1) / passes;
+    SortArgs a{};
+    a.tokens = d_tokens;
+    a.token_bytes = token_bytes;
+    a.n = n_tokens;
+    a.rows = n_rows;
+    a.padding = padding;
+    a.count = (int32_t *)(w + l.count);
+    a.bits = width;
+    const dim3 parts((uint32_t)(n_tokens > 0 ? ceil_div(n_tokens, kPart) : 1));
+    for (int p = 0; p < passes; ++p) {
+        a.key_in = (const uint32_t *)(w + l.key[(p + 1) % 2]);
+        a.pos_in = (const uint32_t *)(w + l.pos[(p + 1) % 2]);
+        a.key_out = (uint32_t *)(w + l.key[p % 2]);
+        a.pos_out = (uint32_t *)(w + l.pos[p % 2]);
+        a.shift = p * width;
+        if (p == 0)
+            sort_kernel<true><<<parts, kSortThreads, 0, s>>>(a);
+        else
+            sort_kernel<false><<<parts, kSortThreads, 0, s>>>(a);
+    }
+    SumArgs b;
+    b.rows = n_rows;
+    b.cols = cols;
+    b.dy_pitch = dy_pitch;
+    b.out_pitch = dtable_pitch;
+    b.key = (const uint32_t *)(w + l.key[(passes + 1) % 2]);
+    b.pos = (const uint32_t *)(w + l.pos[(passes + 1) % 2]);
+    b.count = a.count;
+    b.part = (float *)(w + l.part);
+    b.part_pitch = l.part_pitch;
+    b.scale = (float)scale;
+    b.lanes = 64;
+    while (b.lanes < kThreads && b.lanes * kVec < cols)
+        b.lanes *= 2;
+    const int64_t chunks = ceil_div(n_tokens, kChunk);
+    const int64_t clear = ceil_div(n_rows, kThreads);
+    b.slices = (uint32_t)ceil_div(cols, (int64_t)b.lanes * kVec);
+    const int64_t sum_blocks = ceil_div(chunks, kThreads / b.lanes) * b.slices;
+    const int64_t join_slices = ceil_div(cols, 64 * kVec);
+    if (join_slices > 65535 || sum_blocks + clear > 0x7FFFFFFF)
+        return ROTOR_EINVAL;
+    b.sum_blocks = (uint32_t)sum_blocks;
+    with_type(type, [&](auto e) {
+        typedef typename decltype(e)::T T;
+        const auto sum = cols >= kVec ? sum_kernel<T, kVec> : sum_kernel<T, 1>;
+        const auto join = cols >= kVec ? join_kernel<T, kVec> : join_kernel<T, 1>;
+        sum<<<dim3((uint32_t)(sum_blocks + clear)), kThreads, 0, s>>>((const T *)d_dy, (T *)d_dtable, b);
+        if (chunks > 1)
+            join<<<dim3((uint32_t)(chunks - 1), (uint32_t)join_slices), kThreads, 0, s>>>((T *)d_dtable, b);
+    });
+    return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+}
+
+}  // extern "C"

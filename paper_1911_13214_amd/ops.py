@@ -1,0 +1,294 @@
+"""Operators of a language-model chain's stages, on the C ABI in
+include/rotor.h: counter-based dropout, embedding lookup, the residual seam
+between two blocks (norms, gate, residual scale), and their gradients.
+
+Argument checks, allocation and marshalling only: every operator runs in the
+library's HIP kernels.  Tensors are CUDA tensors of one device and, where
+floating-point, of one type (float32, bfloat16 or float16); a matrix may have
+any row pitch, its last dimension is dense.  Calls enqueue on ``stream``
+(default: the current one) and return at once; a tensor that was made on
+another stream is the caller's to order, as is an output used on one (the
+scratch a call allocates is returned to torch's caching allocator on
+``stream``).  Results are allocated unless ``out`` is given.
+
+``stages`` wraps these in autograd functions and modules."""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import rotor
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+NORM_MAX_COLS = 16384
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("post", ctypes.c_int32), ("pre", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("gate_rows", ctypes.c_int64), ("gate_pitch", ctypes.c_int64), ("residual_scale", ctypes.c_double),
+                ("eps", ctypes.c_double), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p)]
+
+
+class _NormGrads(ctypes.Structure):
+    _fields_ = [("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p), ("gate_pitch", ctypes.c_int64)]
+
+
+# ---- checks --------------------------------------------------------------------
+
+def _cuda(t, what):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    return t
+
+
+def _typed(t, what):
+    """The C ABI's code of a floating-point tensor's type."""
+    code = TYPES.get(_cuda(t, what).dtype)
+    if code is None:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _like(t, other, what, shape=None):
+    """``t`` checked to have ``other``'s device and type, and a shape."""
+    _cuda(t, what)
+    if t.device != other.device or t.dtype != other.dtype:
+        raise ValueError(f"{what} must be {other.dtype} on {other.device}")
+    shape = other.shape if shape is None else shape
+    if t.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    return t
+
+
+def _matrix(t, what):
+    """(rows, cols, pitch) of a tensor whose leading dimensions are rows."""
+    if t.dim() == 0:
+        raise ValueError(f"{what} needs at least one dimension")
+    cols = t.shape[-1]
+    if cols == 0:
+        raise ValueError(f"{what} has no columns")
+    rows = t.numel() // cols
+    if t.is_contiguous():
+        return rows, cols, cols
+    if t.dim() == 1:
+        t = t.unsqueeze(0)
+    elif t.dim() > 2:
+        try:
+            t = t.view(rows, cols)
+        except RuntimeError:
+            raise ValueError(f"the leading dimensions of {what} must be one row pitch apart") from None
+    pitch = t.stride(0) if rows > 1 else cols
+    if (cols > 1 and t.stride(1) != 1) or pitch < cols:
+        raise ValueError(f"{what} must have a dense last dimension and rows that do not overlap")
+    return rows, cols, pitch
+
+
+def _out(out, like, what, shape=None):
+    if out is None:
+        return torch.empty(like.shape if shape is None else shape, dtype=like.dtype, device=like.device)
+    return _like(out, like, what, shape)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _call(name, device, stream, *args):
+    """One entry point of the library, on ``stream`` or the device's current
+    stream."""
+    fn = getattr(rotor.lib(), name)
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    if device.index == torch.cuda.current_device():
+        status = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, stream.cuda_stream)
+    if status != rotor.ROTOR_OK:
+        raise rotor.RotorError(status, name)
+
+
+def _scratch(nbytes, device, stream):
+    """Device scratch of a call, returned to the allocator on ``stream``."""
+    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    if stream is not None:
+        work.record_stream(stream)
+    return work
+
+
+# ---- dropout ---------------------------------------------------------------------
+
+def dropout(x, p, seed, step=0, residual=None, *, step_tensor=None, out=None, stream=None):
+    """residual + keep * x / (1 - q), q = round(65536 p) / 65536, the mask a
+    function of (seed, step) and the element's index alone: the same call on
+    the gradient of the result (without residual) is the gradient of ``x``.
+
+    ``seed``, ``step``: integers, taken modulo 2^64.  ``step_tensor``: an int64
+    device tensor of one element added to ``step`` (for captured graphs).
+    ``out`` may be ``x`` or ``residual``."""
+    code = _typed(x, "x")
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must lie in [0, 1], not {p}")
+    if step_tensor is not None and (not isinstance(step_tensor, torch.Tensor) or step_tensor.device != x.device or
+                                    step_tensor.dtype != torch.int64 or step_tensor.numel() != 1):
+        raise ValueError("step_tensor must be one int64 on the device of x")
+    y = _out(out, x, "out")
+    if residual is not None:
+        _like(residual, x, "residual")
+    if x.numel() == 0:
+        return y
+    rows, cols, xp = _matrix(x, "x")
+    _, _, yp = _matrix(y, "out")
+    rp = _matrix(residual, "residual")[2] if residual is not None else cols
+    _call("rotor_dropout", x.device, stream, code, rows, cols, x.data_ptr(), xp, _ptr(residual), rp, y.data_ptr(), yp,
+          p, seed & 0xFFFFFFFFFFFFFFFF, step & 0xFFFFFFFFFFFFFFFF, _ptr(step_tensor))
+    return y
+
+
+# ---- embedding -------------------------------------------------------------------
+
+def _tokens(tokens, device):
+    _cuda(tokens, "tokens")
+    if tokens.dtype not in (torch.int64, torch.int32) or tokens.device != device or not tokens.is_contiguous():
+        raise ValueError(f"tokens must be contiguous int64 or int32 on {device}")
+    return tokens.element_size()
+
+
+def embedding(tokens, table, scale=1.0, *, out=None, stream=None):
+    """scale * table[tokens], of shape [*tokens.shape, cols].  A token outside
+    the table gives a row of NaN."""
+    code = _typed(table, "table")
+    if table.dim() != 2:
+        raise ValueError("table must have two dimensions")
+    size = _tokens(tokens, table.device)
+    rows, cols, pitch = _matrix(table, "table")
+    y = _out(out, table, "out", tokens.shape + (cols,))
+    if tokens.numel() == 0:
+        return y
+    _call("rotor_embedding", table.device, stream, code, tokens.numel(), rows, cols, tokens.data_ptr(), size,
+          table.data_ptr(), pitch, scale, y.data_ptr(), _matrix(y, "out")[2])
+    return y
+
+
+def embedding_backward(tokens, grad, n_rows, scale=1.0, *, padding=None, out=None, stream=None):
+    """Gradient [n_rows, cols] of the table from the gradient of
+    ``embedding(tokens, table, scale)``: every row written, that of the token
+    ``padding`` 0.  Bit for bit the same on every call."""
+    code = _typed(grad, "grad")
+    size = _tokens(tokens, grad.device)
+    if grad.dim() < 1 or grad.shape[:-1] != tokens.shape:
+        raise ValueError(f"grad must have shape {tuple(tokens.shape)} + (cols,)")
+    n, (_, cols, pitch) = tokens.numel(), _matrix(grad, "grad")
+    out = _out(out, grad, "out", (n_rows, cols))
+    need = ctypes.c_uint64()
+    rotor._check(rotor.lib().rotor_embedding_workspace_bytes(n, n_rows, cols, ctypes.byref(need)),
+                 "rotor_embedding_workspace_bytes")
+    work = _scratch(need.value, grad.device, stream)
+    _call("rotor_embedding_backward", grad.device, stream, code, n, n_rows, cols, _ptr(tokens), size, _ptr(grad),
+          pitch, scale, -1 if padding is None else padding, out.data_ptr(), _matrix(out, "out")[2], work.data_ptr(),
+          work.numel())
+    return out
+
+
+# ---- residual norm ------------------------------------------------------------------
+
+def _norm(x, z, post, post_weight, post_bias, gate, residual_scale, pre, pre_weight, pre_bias, eps):
+    """The C ABI's description of a seam, checked against ``x``."""
+    code = _typed(x, "x")
+    if post not in NORMS or pre not in NORMS:
+        raise ValueError(f"post and pre must be one of {tuple(NORMS)}")
+    cols = x.shape[-1] if x.dim() else 0
+    if not 1 <= cols <= NORM_MAX_COLS:
+        raise ValueError(f"the last dimension must lie in [1, {NORM_MAX_COLS}]")
+    if not eps >= 0.0:
+        raise ValueError("eps must not be negative")
+    rows = x.numel() // cols
+    if z is None and (post != "none" or gate is not None):
+        raise ValueError("post and gate need z")
+    for name, q, kind in (("post_weight", post_weight, post), ("post_bias", post_bias, post),
+                          ("pre_weight", pre_weight, pre), ("pre_bias", pre_bias, pre)):
+        if q is None:
+            continue
+        if kind == "none":
+            raise ValueError(f"{name} without its norm")
+        if not _like(q, x, name, (cols,)).is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    n = _Norm(type=code, post=NORMS[post], pre=NORMS[pre], rows=rows, cols=cols, residual_scale=residual_scale,
+              eps=eps, post_weight=_ptr(post_weight), post_bias=_ptr(post_bias), pre_weight=_ptr(pre_weight),
+              pre_bias=_ptr(pre_bias))
+    if gate is not None:
+        g_rows, g_cols, n.gate_pitch = _matrix(_cuda(gate, "gate"), "gate")
+        if gate.dtype != x.dtype or gate.device != x.device or g_cols != cols or g_rows < 1 or rows % g_rows:
+            raise ValueError(f"gate must be {x.dtype} on {x.device}, [n, {cols}] with n dividing the {rows} rows")
+        n.gate_rows, n.gate = g_rows, gate.data_ptr()
+    return n
+
+
+def residual_norm(x, z=None, *, post="none", post_weight=None, post_bias=None, gate=None, residual_scale=1.0,
+                  pre="none", pre_weight=None, pre_bias=None, eps=1e-5, stats=True, stream=None):
+    """y = residual_scale * x + gate * post(z) and h = pre(y): returns
+    (y, h, stats), h None without ``pre``.
+
+    ``post``, ``pre``: "none", "rms" or "layer", each with an optional weight
+    and bias [cols]; ``gate``: [cols], or [..., cols] of n rows where n divides
+    the rows of x (one row of gates for each run of rows / n adjacent rows);
+    ``z`` None: no block, y = residual_scale * x.  ``stats``: keep what the
+    backward needs (16 bytes a row), or None is returned."""
+    n = _norm(x, z, post, post_weight, post_bias, gate, residual_scale, pre, pre_weight, pre_bias, eps)
+    xp = _matrix(x, "x")[2]
+    zp = _matrix(_like(z, x, "z"), "z")[2] if z is not None else n.cols
+    copy = z is not None or residual_scale != 1.0
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if copy else x
+    h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if pre != "none" else None
+    st = torch.empty((n.rows, 4), dtype=torch.float32, device=x.device) if stats else None
+    _call("rotor_residual_norm", x.device, stream, ctypes.byref(n), x.data_ptr(), xp, _ptr(z), zp,
+          y.data_ptr() if copy else None, n.cols, _ptr(h), n.cols, _ptr(st))
+    return y, h, st
+
+
+def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None, post_bias=None, gate=None,
+                           residual_scale=1.0, pre="none", pre_weight=None, pre_bias=None, eps=1e-5, stream=None):
+    """Gradients of residual_norm's arguments from those of y (``dy``, None:
+    0) and h (``dh``, None without ``pre``), as a dict: "x", "z" and the
+    parameters that are given."""
+    lead = dy if dy is not None else dh
+    if lead is None:
+        raise ValueError("dy or dh is needed")
+    n = _norm(lead, z, post, post_weight, post_bias, gate, residual_scale, pre, pre_weight, pre_bias, eps)
+    if (dh is not None) != (pre != "none"):
+        raise ValueError("dh goes with pre")
+    if dh is not None:
+        _like(dh, lead, "dh")
+        _like(y, lead, "y")
+    _cuda(stats, "stats")
+    if stats.shape != (n.rows, 4) or stats.dtype != torch.float32 or not stats.is_contiguous() or \
+            stats.device != lead.device:
+        raise ValueError("stats must be what residual_norm returned")
+
+    def matrix(t, what):
+        return (None, n.cols) if t is None else (t.data_ptr(), _matrix(_like(t, lead, what), what)[2])
+
+    def empty(t):
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+    g = {"x": empty(lead)}
+    if z is not None:
+        g["z"] = empty(lead)
+    for name, q in (("pre_weight", pre_weight), ("pre_bias", pre_bias), ("post_weight", post_weight),
+                    ("post_bias", post_bias), ("gate", gate)):
+        if q is not None:
+            g[name] = empty(q)
+    out = _NormGrads(gate_pitch=n.cols, **{k: g[k].data_ptr() for k in g if k not in ("x", "z")})
+    need = ctypes.c_uint64()
+    rotor._check(rotor.lib().rotor_residual_norm_workspace_bytes(ctypes.byref(n), ctypes.byref(need)),
+                 "rotor_residual_norm_workspace_bytes")
+    work = _scratch(need.value, lead.device, stream)
+    _call("rotor_residual_norm_backward", lead.device, stream, ctypes.byref(n), *matrix(dy, "dy"), *matrix(dh, "dh"),
+          *(matrix(y, "y") if dh is not None else (None, n.cols)), *matrix(z, "z"), stats.data_ptr(),
+          g["x"].data_ptr(), n.cols, _ptr(g.get("z")), n.cols, ctypes.byref(out), work.data_ptr(), work.numel())
+    return g

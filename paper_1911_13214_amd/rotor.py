@@ -29,7 +29,7 @@ MAX_L = 32767
 MAX_L_RECONSTRUCT = 8191
 
 # name -> (restype, argtypes) of every function include/rotor.h declares
-_i32, _i64, _u64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_void_p
+_i32, _i64, _u64, _vp, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_double
 _P = ctypes.POINTER
 SIGNATURES = {
     "rotor_version": (_i32, []),
@@ -48,6 +48,16 @@ SIGNATURES = {
     "rotor_store_all_peak": (_i32, [_vp, _i32, _P(_i64)]),
     "rotor_even_budgets": (_i32, [_i64, _i32, _vp]),
     "rotor_sequence_cost": (_i32, [_vp, _i32, _vp, _i64, _P(_i64), _P(_i64)]),
+    # operators of a chain's stages (ops.py)
+    "rotor_dropout": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _f64, _u64, _u64, _vp, _vp]),
+    "rotor_embedding": (_i32, [_i32, _i64, _i64, _i64, _vp, _i32, _vp, _i64, _f64, _vp, _i64, _vp]),
+    "rotor_embedding_workspace_bytes": (_i32, [_i64, _i64, _i64, _P(_u64)]),
+    "rotor_embedding_backward": (_i32, [_i32, _i64, _i64, _i64, _vp, _i32, _vp, _i64, _f64, _i64, _vp, _i64, _vp, _u64,
+                                        _vp]),
+    "rotor_residual_norm": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "rotor_residual_norm_workspace_bytes": (_i32, [_vp, _P(_u64)]),
+    "rotor_residual_norm_backward": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64,
+                                            _vp, _vp, _u64, _vp]),
 }
 
 KERNEL_CLASSES = ("leaf", "diag", "middle", "edge", "prep")

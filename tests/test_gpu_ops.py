@@ -1,0 +1,464 @@
+"""The operators of a chain's stages on the GPU against plain 64-bit
+implementations (ops_model.py).  Tolerances: one rounding of the result's type
+plus a bound on the 32-bit arithmetic before it, stated at each test."""
+import itertools
+
+import pytest
+import torch
+
+import ops_model as m
+from paper_1911_13214_amd import ops
+
+pytestmark = pytest.mark.gpu
+TYPES = ["f32", "bf16", "f16"]
+
+
+def gpu(t):
+    return None if t is None else t.cuda()
+
+
+# ---- dropout --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(1,), (7,), (8,), (9,), (3, 5), (64, 33), (2, 3, 40), (5, 1000)])
+def test_dropout(dtype, shape):
+    print("dropout", dtype, shape, flush=True)
+    g = torch.Generator().manual_seed(len(shape) + shape[-1])
+    x, r = m.normal(g, *shape, dtype=m.DTYPES[dtype]), m.normal(g, *shape, dtype=m.DTYPES[dtype])
+    for p, seed, step, res in [(0.1, 5, 0, None), (0.5, 2 ** 63 + 12345, 2 ** 40 + 7, r), (0.0, 1, 1, r), (1.0, 1, 1, r),
+                               (0.37, -1, -2, None)]:
+        out = ops.dropout(gpu(x), p, seed, step, residual=gpu(res))
+        ref = m.dropout(x, p, seed % 2 ** 64, step % 2 ** 64, res)
+        # the factor and the product are rounded once each, and the sum
+        slack = 4 * m.U32 * ((x.double() * 2.1).abs() + ref.abs())
+        m.close(out, ref, slack, (p, seed, step))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols,pitch", [(8, 16), (40, 48), (33, 40), (3, 5), (1, 4), (17, 17 + 8)])
+def test_dropout_of_strided_rows_has_the_mask_of_dense_ones(dtype, cols, pitch):
+    print("dropout strided", dtype, cols, pitch, flush=True)
+    g = torch.Generator().manual_seed(cols)
+    whole = m.normal(g, 21, pitch, dtype=m.DTYPES[dtype]).cuda()
+    x, r = whole[:, :cols], m.normal(g, 21, cols, dtype=m.DTYPES[dtype]).cuda()
+    dense = ops.dropout(x.contiguous(), 0.3, 9, 4, residual=r)
+    assert torch.equal(ops.dropout(x, 0.3, 9, 4, residual=r), dense)
+    out = torch.full((21, pitch + 3), 7.0, dtype=x.dtype, device="cuda")
+    ops.dropout(x, 0.3, 9, 4, residual=r, out=out[:, 1:1 + cols])
+    assert torch.equal(out[:, 1:1 + cols], dense)
+    assert (out[:, 0] == 7).all() and (out[:, 1 + cols:] == 7).all()
+    # in place, and from a pointer that is aligned to one element only
+    y = x.contiguous()
+    assert ops.dropout(y, 0.3, 9, 4, residual=r, out=y) is y and torch.equal(y, dense)
+    odd = torch.empty(21 * cols + 1, dtype=x.dtype, device="cuda")[1:].view(21, cols)
+    odd.copy_(x)
+    assert torch.equal(ops.dropout(odd, 0.3, 9, 4, residual=r), dense)
+
+
+def test_dropped_infinities_and_nans_vanish():
+    x = torch.full((4, 64), float("nan"))
+    keep = m.keep_mask(x.numel(), 0.5, 3, 8).view(4, 64)
+    x[keep] = 1.0
+    x[~keep & (torch.arange(64) % 2 == 0)] = float("inf")
+    out = ops.dropout(x.cuda(), 0.5, 3, 8).cpu()
+    assert torch.equal(out, torch.where(keep, 2.0, 0.0))
+
+
+def test_dropout_steps_from_the_device_and_in_a_graph():
+    x = torch.ones(3, 50, device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    out = torch.empty_like(x)
+    want = [ops.dropout(x, 0.4, 21, 100 + k) for k in range(4)]
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ops.dropout(x, 0.4, 21, 100, step_tensor=step, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.cuda.graph(graph):
+        ops.dropout(x, 0.4, 21, 100, step_tensor=step, out=out)
+    for k in range(4):
+        step.fill_(k)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[k]), k
+        assert torch.equal(ops.dropout(x, 0.4, 21, 100, step_tensor=step), want[k])
+    assert not torch.equal(want[0], want[1])
+
+
+def test_operators_without_elements():
+    x = torch.zeros(0, 5, device="cuda")
+    assert ops.dropout(x, 0.5, 1).shape == (0, 5)
+    none = torch.zeros(0, dtype=torch.int64, device="cuda")
+    assert ops.embedding(none, torch.ones(4, 5, device="cuda")).shape == (0, 5)
+    assert torch.equal(ops.embedding_backward(none, x, 4), torch.zeros(4, 5, device="cuda"))
+    w = torch.ones(5, device="cuda")
+    y, h, st = ops.residual_norm(x, x, post="rms", post_weight=w, gate=w, pre="layer", pre_weight=w, pre_bias=w)
+    g = ops.residual_norm_backward(x, x, y, x, st, post="rms", post_weight=w, gate=w, pre="layer", pre_weight=w,
+                                   pre_bias=w)
+    assert g["x"].shape == (0, 5)
+    for k in ("post_weight", "gate", "pre_weight", "pre_bias"):
+        assert torch.equal(g[k], torch.zeros(5, device="cuda")), k
+
+
+# ---- embedding --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [1, 7, 8, 9, 64, 515, 2056])
+def test_embedding(dtype, cols):
+    print("embedding", dtype, cols, flush=True)
+    g = torch.Generator().manual_seed(cols)
+    table = m.normal(g, 37, cols, dtype=m.DTYPES[dtype])
+    for n, scale, tt in [(1, 1.0, torch.int64), (5, 3.25, torch.int32), (1030, -0.7, torch.int64)]:
+        tokens = torch.randint(0, 37, (n,), generator=g)
+        if n == 5:
+            tokens[1], tokens[3] = -1, 37  # outside the table
+        out = ops.embedding(tokens.to(tt).cuda(), table.cuda(), scale).cpu()
+        ref = m.embedding(tokens, table, scale)
+        lost = ref.isnan()
+        assert torch.equal(out.isnan(), lost)
+        # the scale is rounded to 32 bits, and the product
+        m.close(torch.where(lost, 0.0, out), torch.where(lost, 0.0, ref),
+                2 * m.U32 * torch.where(lost, 0.0, ref).abs(), (n, scale))
+    # leading dimensions, a table and a result with other pitches
+    tokens = torch.randint(0, 37, (3, 4), generator=g).cuda()
+    wide = torch.zeros(37, cols + 5, dtype=table.dtype, device="cuda")
+    wide[:, 2:2 + cols] = table.cuda()
+    out = torch.full((3, 4, cols + 3), 7.0, dtype=table.dtype, device="cuda")
+    ops.embedding(tokens, wide[:, 2:2 + cols], 2.0, out=out[..., 1:1 + cols])
+    assert torch.equal(out[..., 1:1 + cols], ops.embedding(tokens, table.cuda(), 2.0))
+    assert (out[..., 0] == 7).all() and (out[..., 1 + cols:] == 7).all()
+
+
+def tokens_of(kind, n, rows, g):
+    if kind == "uniform":
+        return torch.randint(0, rows, (n,), generator=g)
+    if kind == "one":
+        return torch.full((n,), rows // 2)
+    if kind == "last":  # the table's ends
+        return torch.where(torch.rand(n, generator=g) < 0.5, 0, rows - 1)
+    t = (torch.rand(n, generator=g, dtype=torch.float64) ** 4 * rows).long()  # most tokens small
+    t[::7] = -3
+    t[5::11] = rows + 2
+    return t
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["uniform", "one", "last", "skewed"])
+@pytest.mark.parametrize("n,rows,cols", [(1, 5, 8), (31, 3, 5), (32, 700, 64), (33, 1, 12), (65, 600, 7),
+                                         (1000, 513, 129), (2049, 300000, 3), (5000, 4000, 70), (4097, 70000, 16)])
+def test_embedding_gradient(dtype, kind, n, rows, cols):
+    print("embedding gradient", dtype, kind, n, rows, cols, flush=True)
+    g = torch.Generator().manual_seed(n + rows + cols)
+    tokens = tokens_of(kind, n, rows, g)
+    dy = m.normal(g, n, cols, dtype=m.DTYPES[dtype])
+    for scale, padding in [(1.0, None), (-2.5, 0)]:
+        out = ops.embedding_backward(tokens.cuda(), dy.cuda(), rows, scale, padding=padding)
+        ref, mag = m.embedding_grad(tokens, dy, rows, scale, padding)
+        # n terms in 32 bits, each partial sum below mag
+        m.close(out, ref, (n + 4) * m.U32 * mag, (scale, padding))
+        assert torch.equal(out, ops.embedding_backward(tokens.int().cuda(), dy.cuda(), rows, scale, padding=padding))
+
+
+def test_embedding_gradient_ignores_what_has_none():
+    g = torch.Generator().manual_seed(4)
+    tokens = torch.randint(0, 50, (300,), generator=g)
+    dy = m.normal(g, 300, 24, dtype=torch.float32)
+    tokens[10:20], tokens[30:40] = 60, -1
+    dy[10:20], dy[30:40] = float("nan"), float("inf")
+    dy[tokens == 7] = float("nan")
+    ref, mag = m.embedding_grad(tokens, dy.nan_to_num(0, 0, 0), 50, 1.0, 7)
+    m.close(ops.embedding_backward(tokens.cuda(), dy.cuda(), 50, padding=7), ref, 304 * m.U32 * mag)
+    # strided gradients and results
+    wide = torch.randn(300, 40, device="cuda")
+    out = torch.full((50, 32), 7.0, device="cuda")
+    ops.embedding_backward(tokens.cuda(), wide[:, 3:27], 50, padding=7, out=out[:, 5:29])
+    assert torch.equal(out[:, 5:29], ops.embedding_backward(tokens.cuda(), wide[:, 3:27].contiguous(), 50, padding=7))
+    assert (out[:, :5] == 7).all() and (out[:, 29:] == 7).all()
+
+
+# ---- residual norm ------------------------------------------------------------------
+
+def seam(g, rows, cols, dtype, post, pre, gate, biases, weights=True, z=True):
+    t = m.DTYPES[dtype]
+    s = dict(x=m.normal(g, rows, cols, dtype=t, std=2.0),
+             z=m.normal(g, rows, cols, dtype=t, std=0.7, mean=0.3) if z else None)
+    how = dict(post=post, pre=pre, residual_scale=0.8, eps=1e-5,
+               post_weight=m.normal(g, cols, dtype=t, std=0.2, mean=1.0) if weights and post != "none" else None,
+               post_bias=m.normal(g, cols, dtype=t, std=0.2) if biases and post != "none" else None,
+               gate=m.normal(g, gate, cols, dtype=t, std=0.5) if gate else None,
+               pre_weight=m.normal(g, cols, dtype=t, std=0.2, mean=1.0) if weights and pre != "none" else None,
+               pre_bias=m.normal(g, cols, dtype=t, std=0.2) if biases and pre != "none" else None)
+    return s, how
+
+
+def wide(t):
+    return t.double() if torch.is_tensor(t) else t
+
+
+def forward_slack(s, how):
+    """Bounds on the 32-bit errors of y and h: every value is a few products
+    and sums of rounded terms; sums over a row are trees of at most 32 + 10
+    levels, so a mean and 1 / deviation are within 64 roundings."""
+    x, z = wide(s["x"]), wide(s["z"])
+    size = (how["residual_scale"] * x).abs()
+    if z is not None:
+        out, n, r = m.norm(how["post"], z, None, None, how["eps"])
+        b = n.abs() + r * z.abs().mean(1, keepdim=True) if how["post"] != "none" else n.abs()
+        if how["post_weight"] is not None:
+            b = b * wide(how["post_weight"]).abs()
+        if how["post_bias"] is not None:
+            b = b + wide(how["post_bias"]).abs()
+        if how["gate"] is not None:
+            gt = wide(how["gate"])
+            b = b * gt.abs().repeat_interleave(x.shape[0] // gt.shape[0], 0)
+        size = size + b
+    y_slack = 128 * m.U32 * size
+    if how["pre"] == "none":
+        return y_slack, None
+    y = m.residual_norm(x, z, **{k: wide(v) for k, v in how.items()})[0]
+    _, n, r = m.norm(how["pre"], y, None, None, how["eps"])
+    h = 128 * m.U32 * (n.abs() + r * y.abs().mean(1, keepdim=True)) + r * (y_slack + y_slack.mean(1, keepdim=True)) + \
+        n.abs() * (n.abs() * r * y_slack).mean(1, keepdim=True)
+    if how["pre_weight"] is not None:
+        h = h * wide(how["pre_weight"]).abs()
+    if how["pre_bias"] is not None:
+        h = h + 2 * m.U32 * wide(how["pre_bias"]).abs()
+    return y_slack, h
+
+
+def check_seam(s, how, dy, dh):
+    gs, gh = {k: gpu(v) for k, v in s.items()}, {k: gpu(v) if torch.is_tensor(v) else v for k, v in how.items()}
+    y, h, stats = ops.residual_norm(gs["x"], gs["z"], **gh)
+    leaves = {k: wide(v).requires_grad_() for k, v in {**s, **how}.items() if torch.is_tensor(v)}
+    ref_y, ref_h = m.residual_norm(leaves["x"], leaves.get("z"), **{k: leaves.get(k, v) for k, v in how.items()})
+    ys, hs = forward_slack(s, how)
+    m.close(y, ref_y.detach(), ys, "y")
+    if ref_h is not None:
+        m.close(h, ref_h.detach(), hs, "h")
+    else:
+        assert h is None
+    again = ops.residual_norm(gs["x"], gs["z"], **gh, stats=False)
+    assert torch.equal(again[0], y) and again[2] is None
+
+    g = ops.residual_norm_backward(gpu(dy), gpu(dh) if ref_h is not None else None, y, gs["z"], stats, **gh)
+    outs = [o for o, d in ((ref_y, dy), (ref_h, dh)) if o is not None and d is not None]
+    gouts = [wide(d) for o, d in ((ref_y, dy), (ref_h, dh)) if o is not None and d is not None]
+    names = [k for k in ("x", "z", "pre_weight", "pre_bias", "post_weight", "post_bias", "gate") if k in leaves]
+    ref = dict(zip(names, torch.autograd.grad(outs, [leaves[k] for k in names], gouts)))
+    assert set(g) == set(names)
+
+    # The backward takes n of the pre norm from y as it was rounded (one
+    # rounding of the type), everything else from 32-bit values.  Bounds: d*
+    # is the error of *, each sum of products bounded term by term.
+    x, z = wide(s["x"]), wide(s["z"])
+    u = m.UNIT[y.dtype]
+    yy = ref_y.detach()
+    e = 256 * m.U32
+    t = wide(dy).abs() if dy is not None else torch.zeros_like(x)
+    dt = e * t
+    if ref_h is not None:
+        _, n2, r2 = m.norm(how["pre"], yy, None, None, how["eps"])
+        c = wide(dh).abs() * (wide(how["pre_weight"]).abs() if how["pre_weight"] is not None else 1.0)
+        dn2 = r2 * (u * (yy.abs() + ys) + ys + ys.mean(1, keepdim=True)) + e * (n2.abs() + r2 * yy.abs().mean(1, True)) + \
+            n2.abs() * (n2.abs() * r2 * ys).mean(1, keepdim=True)
+        du = r2 * (c + c.mean(1, True) + n2.abs() * (c * n2.abs()).mean(1, True))
+        dt = dt + e * du + r2 * (dn2 * (c * n2.abs()).mean(1, True) + n2.abs() * (c * dn2).mean(1, True)) + \
+            du * (n2.abs() * r2 * ys).mean(1, True)
+        t = t + du
+        if "pre_weight" in g:
+            m.close(g["pre_weight"], ref["pre_weight"],
+                    (wide(dh).abs() * (dn2 + (2 * x.shape[0] + 64) * m.U32 * n2.abs())).sum(0), "pre_weight")
+        if "pre_bias" in g:
+            m.close(g["pre_bias"], ref["pre_bias"], (x.shape[0] + 64) * m.U32 * wide(dh).abs().sum(0), "pre_bias")
+    m.close(g["x"], ref["x"], how["residual_scale"] * dt + e * ref["x"].abs(), "x")
+    if z is None:
+        return
+    gt = wide(how["gate"]).abs().repeat_interleave(x.shape[0] // how["gate"].shape[0], 0) if how["gate"] is not None \
+        else torch.ones_like(x)
+    w1 = wide(how["post_weight"]).abs() if how["post_weight"] is not None else 1.0
+    b1 = wide(how["post_bias"]).abs() if how["post_bias"] is not None else 0.0
+    _, n1, r1 = m.norm(how["post"], z, None, None, how["eps"])
+    n1, dn1 = n1.abs(), e * (n1.abs() + (r1 * z.abs().mean(1, True) if how["post"] != "none" else 0.0))
+    db, ddb = gt * t, gt * (dt + e * t)
+    rows_e = (2 * x.shape[0] + 64) * m.U32
+    if how["post"] == "none":
+        dz_slack = ddb
+    else:
+        c, dc = db * w1, (ddb + e * db) * w1
+        dz_slack = r1 * (dc + dc.mean(1, True) + n1 * (dc * n1 + c * dn1).mean(1, True) +
+                         dn1 * (c * n1).mean(1, True)) + \
+            e * r1 * (c + c.mean(1, True) + n1 * (c * n1).mean(1, True))
+    m.close(g["z"], ref["z"], dz_slack, "z")
+    if "post_weight" in g:
+        m.close(g["post_weight"], ref["post_weight"], (ddb * n1 + db * dn1 + rows_e * db * n1).sum(0), "post_weight")
+    if "post_bias" in g:
+        m.close(g["post_bias"], ref["post_bias"], (ddb + rows_e * db).sum(0), "post_bias")
+    if "gate" in g:
+        b = n1 * w1 + b1
+        part = (dt * b + t * dn1 * w1 + rows_e * t * b).reshape(how["gate"].shape[0], -1, x.shape[1]).sum(1)
+        m.close(g["gate"], ref["gate"], part, "gate")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 5), (2, 8), (5, 63), (4, 512), (6, 515), (33, 1024), (4, 1025),
+                                       (8, 2048), (4, 2055), (2, 4099), (3, 8200), (2, 16384)])
+def test_residual_norm_sizes(dtype, rows, cols):
+    print("residual norm", dtype, rows, cols, flush=True)
+    g = torch.Generator().manual_seed(rows * cols)
+    s, how = seam(g, rows, cols, dtype, "rms", "layer", 1, True)
+    check_seam(s, how, m.normal(g, rows, cols, dtype=m.DTYPES[dtype]), m.normal(g, rows, cols, dtype=m.DTYPES[dtype]))
+
+
+@pytest.mark.parametrize("post,pre", list(itertools.product(["none", "rms", "layer"], repeat=2)))
+@pytest.mark.parametrize("gate,biases,weights", [(0, False, True), (1, True, True), (4, True, False), (24, False, True)])
+def test_residual_norm_forms(post, pre, gate, biases, weights):
+    print("residual norm", post, pre, gate, biases, weights, flush=True)
+    g = torch.Generator().manual_seed(7)
+    s, how = seam(g, 24, 100, "f32", post, pre, gate, biases, weights)
+    d = [m.normal(g, 24, 100, dtype=torch.float32) for _ in range(2)]
+    check_seam(s, how, d[0], d[1])
+    if pre != "none":
+        check_seam(s, how, None, d[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,gate", [(2100, 1), (2100, 3), (1400, 700), (3000, 0), (1536, 1536)])
+def test_residual_norm_sums_over_many_rows(dtype, rows, gate):
+    print("residual norm rows", dtype, rows, gate, flush=True)
+    g = torch.Generator().manual_seed(rows)
+    s, how = seam(g, rows, 72, dtype, "layer", "rms", gate, True)
+    check_seam(s, how, m.normal(g, rows, 72, dtype=m.DTYPES[dtype]), m.normal(g, rows, 72, dtype=m.DTYPES[dtype]))
+
+
+def test_residual_norm_without_a_block():
+    g = torch.Generator().manual_seed(3)
+    s, how = seam(g, 9, 70, "bf16", "none", "rms", 0, False, z=False)
+    how["residual_scale"] = 1.0
+    x = gpu(s["x"])
+    y, h, st = ops.residual_norm(x, pre="rms", pre_weight=gpu(how["pre_weight"]))
+    assert y is x
+    check_seam(s, how, None, m.normal(g, 9, 70, dtype=torch.bfloat16))
+    how["residual_scale"] = 0.5
+    check_seam(s, how, m.normal(g, 9, 70, dtype=torch.bfloat16), m.normal(g, 9, 70, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_layer_norm_gradient_of_rows_far_from_zero(dtype):
+    # y's rounding is larger than the rows' deviation: the gradient is that of
+    # the norm at y as rounded.  Deviations there are 0 or a few spacings, so
+    # sums over a row are exact up to 32-bit rounding of the mean (relative to
+    # the mean, 2^-24 * 64 * 300, against spacings of 0.25 and more).
+    g = torch.Generator().manual_seed(31)
+    x = m.normal(g, 40, 65, std=0.02, mean=300.0).to(m.DTYPES[dtype])
+    dh = m.normal(g, 40, 65, dtype=x.dtype)
+    # a scale that makes y need rounding again
+    how = dict(pre="layer", residual_scale=1.01, eps=1e-5)
+    y, _, st = ops.residual_norm(x.cuda(), **how)
+    leaf = y.cpu().double().requires_grad_()
+    out, n, r = m.norm("layer", leaf, None, None, 1e-5)
+    ref = torch.autograd.grad(out, leaf, dh.double())[0] * 1.01
+    got = ops.residual_norm_backward(None, dh.cuda(), y, None, st, **how)["x"]
+    n, r, c = n.detach().abs(), r.detach(), dh.double().abs()
+    dn = r * 64 * m.U32 * 310 + 256 * m.U32 * n
+    du = r * (c + c.mean(1, True) + n * (c * n).mean(1, True))
+    m.close(got, ref, 1.01 * (256 * m.U32 * du + du * (n * dn).mean(1, True) +
+                              r * (dn * (c * n).mean(1, True) + (n + dn) * (c * dn).mean(1, True))))
+
+
+def test_residual_norm_of_strided_rows():
+    g = torch.Generator().manual_seed(5)
+    for cols in (64, 100, 2050):
+        big = [m.normal(g, 12, cols + 9, dtype=torch.bfloat16).cuda()[:, 3:3 + cols] for _ in range(5)]
+        x, z, gate, dy, dh = big
+        gate = gate[:4]
+        w = m.normal(g, cols, dtype=torch.bfloat16).cuda()
+        how = dict(post="layer", post_weight=w, pre="rms", pre_weight=w)
+        a = ops.residual_norm(x, z, gate=gate, **how)
+        b = ops.residual_norm(x.contiguous(), z.contiguous(), gate=gate.contiguous(), **how)
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+        ga = ops.residual_norm_backward(dy, dh, a[0], z, a[2], gate=gate, **how)
+        gb = ops.residual_norm_backward(dy.contiguous(), dh.contiguous(), a[0], z.contiguous(), a[2],
+                                        gate=gate.contiguous(), **how)
+        assert set(ga) == set(gb) and all(torch.equal(ga[k], gb[k]) for k in ga)
+
+
+def test_residual_norm_gradient_against_differences():
+    # L = sum(c y) + sum(d h): central differences along a random direction of
+    # every argument at once.  Rounding of the values: 2^-24 of terms whose
+    # magnitudes sum to S, over a step of 2 * 2^-6; curvature: below 2^-12 of
+    # the third derivative's size, bounded with the 64-bit model's own
+    # difference.
+    g = torch.Generator().manual_seed(6)
+    rows, cols, step = 16, 96, 2.0 ** -6
+    s, how = seam(g, rows, cols, "f32", "layer", "rms", 4, True)
+    tensors = {k: v for k, v in {**s, **how}.items() if torch.is_tensor(v)}
+    fixed = {k: v for k, v in how.items() if not torch.is_tensor(v)}
+    along = {k: m.normal(g, *v.shape, dtype=torch.float32) for k, v in tensors.items()}
+    c, d = (m.normal(g, rows, cols, dtype=torch.float32) for _ in range(2))
+
+    def value(e, f):
+        t = {k: v + e * along[k] for k, v in tensors.items()}
+        x, z = t.pop("x"), t.pop("z")
+        y, h = f(x, z, t)
+        return float((c.double() * y.cpu().double()).sum() + (d.double() * h.cpu().double()).sum()), \
+            float((c.double() * y.cpu().double()).abs().sum() + (d.double() * h.cpu().double()).abs().sum())
+
+    def kernel(x, z, t):
+        return ops.residual_norm(x.cuda(), z.cuda(), **{k: v.cuda() for k, v in t.items()}, **fixed)[:2]
+
+    def model(x, z, t):
+        return m.residual_norm(x.double(), z.double(), **{k: v.double() for k, v in t.items()}, **fixed)
+
+    y, h, st = kernel_out = ops.residual_norm(s["x"].cuda(), s["z"].cuda(), **{k: gpu(v) if torch.is_tensor(v) else v
+                                                                               for k, v in how.items()})
+    grads = ops.residual_norm_backward(c.cuda(), d.cuda(), y, s["z"].cuda(), st,
+                                       **{k: gpu(v) if torch.is_tensor(v) else v for k, v in how.items()})
+    analytic = sum(float((grads[k].cpu().double() * along[k].double()).sum()) for k in tensors)
+    size = sum(float((grads[k].cpu().double() * along[k].double()).abs().sum()) for k in tensors)
+    (up, mag), (down, _) = value(step, kernel), value(-step, kernel)
+    numeric = (up - down) / (2 * step)
+    exact = (value(step, model)[0] - value(-step, model)[0]) / (2 * step)
+    tiny = (value(step / 64, model)[0] - value(-step / 64, model)[0]) / (2 * step / 64)
+    curvature = abs(exact - tiny)
+    assert abs(numeric - analytic) <= curvature * 1.1 + 256 * m.U32 * (mag / step + size)
+
+
+def test_operators_run_on_the_stream_they_are_given():
+    g = torch.Generator().manual_seed(8)
+    x = m.normal(g, 512, 1024, dtype=torch.float32).cuda()
+    tokens = torch.randint(0, 100, (512,), generator=g).cuda()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    a = ops.dropout(x, 0.2, 1, stream=side)
+    b = ops.embedding_backward(tokens, x, 100, stream=side)
+    c = ops.residual_norm(x, x, pre="rms", stream=side)[1]
+    with torch.cuda.stream(side):
+        d = ops.dropout(x, 0.2, 1)
+    side.synchronize()
+    assert torch.equal(a, ops.dropout(x, 0.2, 1)) and torch.equal(a, d)
+    assert torch.equal(b, ops.embedding_backward(tokens, x, 100))
+    assert torch.equal(c, ops.residual_norm(x, x, pre="rms")[1])
+
+
+def test_the_binding_refuses_mismatched_tensors():
+    x = torch.zeros(4, 8, device="cuda")
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    bad = [lambda: ops.dropout(x.double(), 0.1, 1), lambda: ops.dropout(x, 1.5, 1),
+           lambda: ops.dropout(x, 0.1, 1, residual=x[:2]), lambda: ops.dropout(x, 0.1, 1, residual=x.half()),
+           lambda: ops.dropout(x.t(), 0.1, 1), lambda: ops.dropout(x, 0.1, 1, out=x[:2]),
+           lambda: ops.dropout(x, 0.1, 1, step_tensor=t), lambda: ops.embedding(t.float(), x),
+           lambda: ops.embedding(t.cpu(), x), lambda: ops.embedding(t, x[0]),
+           lambda: ops.embedding_backward(t, x[:2], 4), lambda: ops.embedding_backward(t, x, 4, out=x[:, :4]),
+           lambda: ops.residual_norm(x, pre="batch"), lambda: ops.residual_norm(x, x[:2]),
+           lambda: ops.residual_norm(x, x, gate=x[:3]), lambda: ops.residual_norm(x, gate=x),
+           lambda: ops.residual_norm(x, x, post_weight=x[0]), lambda: ops.residual_norm(x, pre="rms", eps=-1.0),
+           lambda: ops.residual_norm(x, pre="rms", pre_weight=x[0].half()),
+           lambda: ops.residual_norm(torch.zeros(2, 16385, device="cuda"), pre="rms"),
+           lambda: ops.residual_norm_backward(x, None, x, x, x, pre="rms"),
+           lambda: ops.residual_norm_backward(x, x, x, x, x, pre="rms"),
+           lambda: ops.residual_norm_backward(None, None, x, x, x)]
+    for k, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            print("not refused:", k)

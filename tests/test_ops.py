@@ -1,0 +1,105 @@
+"""Refusals of the operators of a chain's stages (no GPU): the C entry points
+return ROTOR_EINVAL before any device work, the binding raises ValueError."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_1911_13214_amd import ops, rotor
+
+FAKE = 0x10000
+E = rotor.ROTOR_EINVAL
+
+
+def test_dropout_refuses_bad_arguments():
+    f = rotor.lib().rotor_dropout
+    good = [0, 4, 8, FAKE, 8, None, 0, FAKE, 8, 0.1, 1, 2, None, None]
+    for at, bad in [(0, 3), (0, -1), (1, -1), (2, 0), (3, None), (3, FAKE + 2), (4, 7), (5, FAKE), (7, None),
+                    (7, FAKE + 1), (8, 7), (9, -0.1), (9, 1.1), (9, float("nan")), (12, FAKE + 4), (1, 1 << 60)]:
+        a = list(good)
+        a[at] = bad
+        assert f(*a) == E, (at, bad)
+    a = list(good)
+    a[1] = 0  # no rows: nothing to do, whatever the pointers
+    a[3] = a[7] = None
+    assert f(*a) == rotor.ROTOR_OK
+
+
+def test_embedding_refuses_bad_arguments():
+    f = rotor.lib().rotor_embedding
+    good = [1, 4, 10, 8, FAKE, 8, FAKE, 8, 1.0, FAKE, 8, None]
+    for at, bad in [(0, 9), (1, -1), (1, 1 << 31), (2, 0), (2, 1 << 31), (3, 0), (4, None), (4, FAKE + 4), (5, 2),
+                    (6, None), (6, FAKE + 1), (7, 7), (9, None), (10, 7)]:
+        a = list(good)
+        a[at] = bad
+        assert f(*a) == E, (at, bad)
+    b = rotor.lib().rotor_embedding_backward
+    need = ctypes.c_uint64()
+    assert rotor.lib().rotor_embedding_workspace_bytes(4, 10, 8, ctypes.byref(need)) == rotor.ROTOR_OK
+    good = [1, 4, 10, 8, FAKE, 8, FAKE, 8, 1.0, -1, FAKE, 8, FAKE, need.value, None]
+    for at, bad in [(0, 9), (1, -1), (2, 0), (3, 0), (4, None), (5, 3), (6, None), (7, 7), (9, -2), (9, 10),
+                    (10, None), (11, 7), (12, None), (12, FAKE + 8), (13, need.value - 1)]:
+        a = list(good)
+        a[at] = bad
+        assert b(*a) == E, (at, bad)
+    w = rotor.lib().rotor_embedding_workspace_bytes
+    assert w(-1, 10, 8, ctypes.byref(need)) == E and w(4, 10, 8, None) == E
+
+
+def test_residual_norm_refuses_bad_arguments():
+    lib = rotor.lib()
+    base = dict(type=1, post=1, pre=2, rows=4, cols=8, gate_rows=2, gate_pitch=8, residual_scale=1.0, eps=1e-5,
+                gate=FAKE)
+    grads = ops._NormGrads(gate_pitch=8)
+    need = ctypes.c_uint64()
+
+    def fwd(how, x=FAKE, z=FAKE, y=FAKE, h=FAKE, stats=FAKE, zp=8):
+        n = ops._Norm(**{**base, **how})
+        return lib.rotor_residual_norm(ctypes.byref(n), x, 8, z, zp, y, 8, h, 8, stats, None)
+
+    def bwd(how, dy=FAKE, dh=FAKE, y=FAKE, z=FAKE, stats=FAKE, dx=FAKE, dz=FAKE, g=grads, work=FAKE, less=0):
+        n = ops._Norm(**{**base, **how})
+        lib.rotor_residual_norm_workspace_bytes(ctypes.byref(n), ctypes.byref(need))
+        return lib.rotor_residual_norm_backward(ctypes.byref(n), dy, 8, dh, 8, y, 8, z, 8, stats, dx, 8, dz, 8,
+                                                ctypes.byref(g), work, need.value - less, None)
+
+    for how in [dict(type=3), dict(post=3), dict(pre=-1), dict(rows=-1), dict(cols=0), dict(cols=16385),
+                dict(gate_rows=3), dict(gate_rows=-1), dict(gate=None), dict(gate_pitch=7), dict(eps=-1.0),
+                dict(post_weight=FAKE + 1), dict(post=0, post_weight=FAKE), dict(pre=0, pre_bias=FAKE)]:
+        assert fwd(how) == E, how
+        assert bwd(how) == E, how
+    for kw in [dict(x=None), dict(x=FAKE + 1), dict(z=None), dict(zp=7), dict(y=None), dict(h=None),
+               dict(stats=FAKE + 4)]:
+        assert fwd({}, **kw) == E, kw
+    assert fwd(dict(pre=0)) == E  # h without pre
+    assert fwd(dict(post=0, gate_rows=0, gate=None, residual_scale=0.5), z=None, y=None) == E
+    for kw in [dict(dh=None), dict(y=None), dict(z=None), dict(stats=None), dict(stats=FAKE + 8), dict(dx=None),
+               dict(dz=None), dict(work=None), dict(work=FAKE + 4), dict(less=1)]:
+        assert bwd({}, **kw) == E, kw
+    assert bwd(dict(pre=0), dy=None, dh=None) == E
+    assert bwd(dict(gate_rows=0, gate=None), g=ops._NormGrads(gate_pitch=8, gate=FAKE)) == E
+    assert bwd({}, g=ops._NormGrads(gate_pitch=7, gate=FAKE)) == E
+
+
+def test_the_binding_refuses_what_is_not_on_a_gpu():
+    x = torch.zeros(2, 4)
+    for call in (lambda: ops.dropout(x, 0.1, 1), lambda: ops.embedding(torch.zeros(2, dtype=torch.int64), x),
+                 lambda: ops.embedding_backward(torch.zeros(2, dtype=torch.int64), x, 3),
+                 lambda: ops.residual_norm(x, pre="rms"),
+                 lambda: ops.residual_norm_backward(x, None, None, None, x),
+                 lambda: ops.dropout([1.0], 0.1, 1)):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()
+
+
+def test_matrices_are_described_by_their_row_pitch():
+    x = torch.zeros(6, 10)
+    assert ops._matrix(x, "x") == (6, 10, 10)
+    assert ops._matrix(x[:, :7], "x") == (6, 7, 10)
+    assert ops._matrix(x[::2], "x") == (3, 10, 20)
+    assert ops._matrix(x.view(2, 3, 10)[:, :, 2:5], "x") == (6, 3, 10)
+    assert ops._matrix(x[0], "x") == (1, 10, 10)
+    assert ops._matrix(x[:1, :7], "x") == (1, 7, 7)
+    for bad in (x.t(), x[:, ::2], x.view(2, 3, 10)[:, :2], x[0].expand(6, 10), torch.zeros(()), torch.zeros(3, 0)):
+        with pytest.raises(ValueError):
+            ops._matrix(bad, "x")
