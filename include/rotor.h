@@ -559,6 +559,56 @@ ROTOR_API int32_t rotor_residual_norm_backward(const rotor_norm *how, const void
                                                const rotor_norm_grads *grads, void *d_work, uint64_t work_bytes,
                                                void *stream);
 
+/* Projection onto a vocabulary and softmax cross entropy, in pieces of the
+ * vocabulary, without keeping the logits:
+ *   logit[j][v] = h[j] . w[v],  lse[j] = log sum_v exp(logit[j][v]),
+ *   loss[j] = lse[j] - logit[j][targets[j]].
+ * Products of 16-bit tensors are exact and summed in 32 bits; 32-bit tensors
+ * are multiplied as three bf16 terms each, which keeps their 24 bits.
+ *   d_h, d_w    DEVICE [n_tokens][cols] and [n_rows][cols], of one type.
+ *   d_targets   DEVICE, n_tokens int64.  A token whose target is `ignore` has
+ *               loss 0 and no gradient, whatever its row of h holds; any
+ *               other target outside [0, n_rows) gives NaN (loss, its row of
+ *               dh, and dw).
+ *   d_loss, d_lse  DEVICE, written: n_tokens floats each.
+ *   aligned     1: every row of h and w starts 16-byte aligned and cols is a
+ *               multiple of 8 (refused where that does not hold); 0: any
+ *               rows, which are copied into the workspace piece by piece.
+ *               Without effect for 32-bit tensors.
+ *   d_work      DEVICE scratch of rotor_xent_workspace_bytes (same sizes,
+ *               `aligned` and direction), 16-byte aligned.
+ * 0 <= n_tokens <= ROTOR_XENT_MAX_TOKENS, 1 <= cols <= ROTOR_XENT_MAX_COLS,
+ * 1 <= n_rows < 2^28, pitches at most 2^22.  Return ROTOR_OK, ROTOR_EINVAL or
+ * ROTOR_EDEVICE. */
+#define ROTOR_XENT_MAX_TOKENS (1 << 20)
+#define ROTOR_XENT_MAX_COLS 65536
+
+/* Device workspace of rotor_xent (backward 0) or rotor_xent_backward (1).
+ * Forward: 8 bytes per token and 128 rows of w.  Backward: at most about
+ * 512 MB for a piece of the probabilities (more past 500 000 tokens), a copy
+ * of that piece of w and of h, 32-bit sums for dh.  Host only. */
+ROTOR_API int32_t rotor_xent_workspace_bytes(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
+                                             int32_t aligned, int32_t backward, uint64_t *bytes);
+
+ROTOR_API int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows, const void *d_h,
+                             int64_t h_pitch, const void *d_w, int64_t w_pitch, const int64_t *d_targets,
+                             int64_t ignore, float *d_loss, float *d_lse, int32_t aligned, void *d_work,
+                             uint64_t work_bytes, void *stream);
+
+/* Gradients of h and w, from those of the losses.
+ *   d_lse, d_grad_loss  DEVICE, n_tokens floats each: what rotor_xent wrote,
+ *                       and the gradient of each loss.
+ *   d_dh, d_dw          DEVICE, written, shaped and typed as h and w; either
+ *                       may be NULL (not wanted).
+ * The probabilities are rounded once to 16 bits (32-bit tensors: kept to 24)
+ * before they are multiplied with w and h; sums over the vocabulary and the
+ * tokens are taken in an order that depends on the sizes alone. */
+ROTOR_API int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows, const void *d_h,
+                                      int64_t h_pitch, const void *d_w, int64_t w_pitch, const int64_t *d_targets,
+                                      int64_t ignore, const float *d_lse, const float *d_grad_loss, void *d_dh,
+                                      int64_t dh_pitch, void *d_dw, int64_t dw_pitch, int32_t aligned, void *d_work,
+                                      uint64_t work_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

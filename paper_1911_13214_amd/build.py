@@ -13,7 +13,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librotor.so")
 SOURCES = ["rotor_host.cpp", "rotor_api.cpp", "rotor_plan.cpp", "rotor_fill.hip", "rotor_tile.hip", "rotor_rows_0.hip",
            "rotor_rows_1.hip", "rotor_rows_2.hip", "rotor_rows_3.hip", "rotor_reconstruct.hip", "rotor_noalloc.hip",
-           "rotor_dropout.hip", "rotor_embedding.hip", "rotor_norm.hip"]
+           "rotor_dropout.hip", "rotor_embedding.hip", "rotor_norm.hip", "rotor_xent.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

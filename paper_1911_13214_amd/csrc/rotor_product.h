@@ -1,0 +1,222 @@
+// Matrix products of the cross entropy: C[j][i] = sum over k of A[i][k] B[j][k],
+// both operands 16-bit with k adjacent, sums in 32 bits on the matrix units,
+// a tile's results handed to an epilogue while they are in registers.
+#pragma once
+
+#include "rotor_ops.h"
+
+namespace rotor {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Mfma;
+template <> struct Mfma<bf16> {
+    typedef bf16 Frag __attribute__((ext_vector_type(8)));
+    static __device__ f32x4 run(Frag a, Frag b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<f16> {
+    typedef f16 Frag __attribute__((ext_vector_type(8)));
+    static __device__ f32x4 run(Frag a, Frag b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+// An operand: `rows` rows, `pitch` elements apart, each row 16-byte aligned.
+// A 32-bit matrix is held as three bf16 terms whose sum has its 24 bits, the
+// terms of a row `seg` elements apart.
+template <typename T> struct Operand {
+    const T *p;
+    int64_t rows, pitch, seg;
+};
+
+// The products of terms (a, b) whose sum is the product of two 32-bit
+// matrices: all that are not below 2^-24 of the largest, the smallest first.
+// 16-bit operands take the last one alone.
+constexpr int kTerms = 3;
+constexpr int kTermProducts = 6;
+__device__ constexpr int term_a(int s) { return 0x124 >> (2 * s) & 3; }  // 0 1 2 0 1 0
+__device__ constexpr int term_b(int s) { return 0x046 >> (2 * s) & 3; }  // 2 1 0 1 0 0
+
+constexpr int kStep = 64;         // of k in one step
+constexpr int kRowBytes = 2 * kStep;
+
+struct ProductArgs {
+    int64_t k;        // a multiple of 8
+    int products;     // kTermProducts, or 1
+    int tiles_i, tiles_j;
+    int steps;        // of all products, ceil(k / kStep) each
+    int split_steps;  // of one part (grid y)
+};
+
+// The shape of a workgroup's tile: BI x BJ results, WI x WJ waves.
+template <int BI_, int BJ_, int WI_, int WJ_> struct Tile {
+    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
+    static constexpr int kWaves = WI * WJ, kThreads = kWaves * 64;
+    static constexpr int NI = BI / WI / 16, NJ = BJ / WJ / 16;  // 16 x 16 results of a wave
+    static constexpr int kBytes = (BI + BJ) * kRowBytes;
+    static constexpr int kLoadsA = BI / 8 / kWaves, kLoadsB = BJ / 8 / kWaves;  // of a wave in one step
+};
+
+// Where a lane's results lie: element r of acc[ii][jj] is
+// (i0 + 16 ii + r, j0 + 16 jj).
+template <typename S> struct Results {
+    f32x4 acc[S::NI][S::NJ];
+    int64_t tile_i, tile_j;  // tile indices
+    int64_t i0, j0;
+    int wave_i, wave_j, lane;
+    int part;
+};
+
+// Tile order: the eight XCDs (workgroups go to them in turn) take contiguous
+// runs, so that what neighbours share stays in one XCD's L2; in a run four
+// tiles of j for each tile of i.
+__device__ inline void tile_of(int id, int tiles_i, int tiles_j, int &ti, int &tj)
+{
+    const int n = tiles_i * tiles_j, xcd = id % 8, q = n / 8, r = n % 8;
+    id = xcd * q + (xcd < r ? xcd : r) + id / 8;
+    constexpr int kGroup = 4;
+    const int group = id / (kGroup * tiles_i), first = group * kGroup;
+    const int width = tiles_j - first < kGroup ? tiles_j - first : kGroup;
+    const int in = id - group * kGroup * tiles_i;
+    ti = in / width;
+    tj = first + in % width;
+}
+
+// Buffer descriptors exist in device code only: the host's pass sees a kernel
+// without a body.
+#if defined(__HIP_DEVICE_COMPILE__)
+template <typename T> __device__ inline __amdgpu_buffer_rsrc_t operand_rsrc(const Operand<T> &o, int64_t row0,
+                                                                              int64_t rows, int64_t k)
+{
+    const int64_t have = o.rows - row0 < rows ? o.rows - row0 : rows;
+    const int64_t bytes = ((have - 1) * o.pitch + o.seg * (kTerms - 1) + k) * (int64_t)sizeof(T);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(o.p + row0 * o.pitch), 0,
+                                             (int)(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF), 0x00020000);
+}
+
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+// One operand's rows of a step, global memory to LDS without registers.  A
+// wave's load moves 8 rows of 128 bytes; row r's 16-byte piece c lands in
+// place c ^ (r % 8), so that the 16 rows a fragment reads lie in different
+// banks.  Rows and pieces outside the operand come as 0 (the buffer's bound).
+template <typename T, int LOADS> struct Loader {
+    __amdgpu_buffer_rsrc_t rsrc;
+    uint32_t at[LOADS];
+    uint32_t limit;  // bytes of k before this lane's piece leaves the row
+    int first;       // LDS byte of this wave's first load
+    __device__ void init(const Operand<T> &o, int64_t row0, int64_t rows, int64_t k, int wave, int lane)
+    {
+        rsrc = operand_rsrc(o, row0, rows, k);
+        const int piece = (lane % 8) ^ (lane / 8);
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q)
+            at[q] = (uint32_t)((wave * LOADS + q) * 8 + lane / 8) * (uint32_t)(o.pitch * sizeof(T)) + piece * 16;
+        limit = (uint32_t)(k * sizeof(T)) - piece * 16;
+        first = wave * LOADS * 1024;
+    }
+    // `term`: byte of the term in a row; `kb`: byte of the step in the term
+    __device__ void load(char *lds, uint32_t term, uint32_t kb) const
+    {
+        const bool in = (int)kb < (int)limit;
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + q * 1024), 16,
+                                                     in ? at[q] + term + kb : 0x80000000u, 0, 0, 0);
+    }
+};
+
+#endif
+
+template <typename T, typename S, typename E>
+__global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Operand<T> b, ProductArgs p, E epilogue)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    // two steps: one is multiplied while the other arrives
+    __shared__ __attribute__((aligned(1024))) char even[S::kBytes];
+    __shared__ __attribute__((aligned(1024))) char odd[S::kBytes];
+    typedef typename Mfma<T>::Frag Frag;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    int ti, tj;
+    tile_of(blockIdx.x, p.tiles_i, p.tiles_j, ti, tj);
+    const int wi = wave / S::WJ, wj = wave % S::WJ;
+
+    Loader<T, S::kLoadsA> la;
+    Loader<T, S::kLoadsB> lb;
+    la.init(a, (int64_t)ti * S::BI, S::BI, p.k, wave, lane);
+    lb.init(b, (int64_t)tj * S::BJ, S::BJ, p.k, wave, lane);
+    const int per = (int)((p.k + kStep - 1) / kStep);
+    const int t0 = blockIdx.y * p.split_steps;
+    const int t1 = t0 + p.split_steps < p.steps ? t0 + p.split_steps : p.steps;
+    int s = kTermProducts - p.products + t0 / per, at = t0 % per;  // of the next load
+    auto load = [&](char *lds) {
+        la.load(lds, (uint32_t)(term_a(s) * a.seg * sizeof(T)), (uint32_t)at * kRowBytes);
+        lb.load(lds + S::BI * kRowBytes, (uint32_t)(term_b(s) * b.seg * sizeof(T)), (uint32_t)at * kRowBytes);
+        if (++at == per) {
+            at = 0;
+            ++s;
+        }
+    };
+
+    Results<S> res;
+#pragma unroll
+    for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+        for (int jj = 0; jj < S::NJ; ++jj)
+            res.acc[ii][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = lane % 16;
+    const int swz[2] = {((lane / 16) ^ (row & 7)) * 16, ((4 + lane / 16) ^ (row & 7)) * 16};
+    const int base_a = (wi * S::NI * 16 + row) * kRowBytes, base_b = (S::BI + wj * S::NJ * 16 + row) * kRowBytes;
+    auto multiply = [&](const char *lds) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Frag fa[S::NI], fb[S::NJ];
+#pragma unroll
+            for (int jj = 0; jj < S::NJ; ++jj)
+                fb[jj] = *(const Frag *)(lds + base_b + swz[h] + jj * 16 * kRowBytes);
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii)
+                fa[ii] = *(const Frag *)(lds + base_a + swz[h] + ii * 16 * kRowBytes);
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                for (int jj = 0; jj < S::NJ; ++jj)
+                    res.acc[ii][jj] = Mfma<T>::run(fa[ii], fb[jj], res.acc[ii][jj]);
+        }
+    };
+
+    if (t0 < t1)
+        load(even);
+    __syncthreads();
+    for (int t = t0; t < t1;) {
+        if (t + 1 < t1)
+            load(odd);
+        multiply(even);
+        __syncthreads();
+        if (++t >= t1)
+            break;
+        if (t + 1 < t1)
+            load(even);
+        multiply(odd);
+        __syncthreads();
+        ++t;
+    }
+    res.tile_i = ti;
+    res.tile_j = tj;
+    res.wave_i = wi;
+    res.wave_j = wj;
+    res.lane = lane;
+    res.i0 = (int64_t)ti * S::BI + wi * S::NI * 16 + lane / 16 * 4;
+    res.j0 = (int64_t)tj * S::BJ + wj * S::NJ * 16 + row;
+    res.part = blockIdx.y;
+    epilogue(res, even);
+#endif
+}
+
+}  // namespace
+}  // namespace rotor

@@ -1,0 +1,674 @@
+// rotor_xent: projection onto a vocabulary and softmax cross entropy, without
+// the logits.
+//
+// Forward: the product W H^T in tiles; a tile's logits stay in registers, and
+// each of its columns (a token) leaves a maximum and a sum of exponentials.
+// A second launch joins the tiles' pairs.
+// Backward, for pieces of the vocabulary: the same product again, whose
+// epilogue turns logits into P = (softmax - target) * gradient and writes
+// it in 16 bits, as it is and transposed; then dH += P W and dW = P^T H.  Each
+// product wants its summed index adjacent in both operands, so H once and W
+// piece by piece are transposed too.
+#include "rotor_product.h"
+
+namespace rotor {
+namespace {
+
+typedef Tile<256, 256, 2, 4> Large;
+typedef Tile<128, 128, 2, 2> Small;
+
+// ---- element conversions ---------------------------------------------------------
+
+// The three bf16 terms of a 32-bit value.  Infinities and NaN stay in the
+// first.
+__device__ inline void split(float v, bf16 (&t)[kTerms])
+{
+    t[0] = (bf16)v;
+    const float r = v - (float)t[0];
+    const bool finite = fabsf((float)t[0]) <= 3.3895314e38f;
+    t[1] = finite ? (bf16)r : (bf16)0.f;
+    t[2] = finite ? (bf16)(r - (float)t[1]) : (bf16)0.f;
+}
+
+// Element type of the products of a call: bf16 terms for 32-bit tensors.
+template <typename T> struct ProductOf {
+    typedef T P;
+    static constexpr int kParts = 1;
+};
+template <> struct ProductOf<float> {
+    typedef bf16 P;
+    static constexpr int kParts = kTerms;
+};
+
+// dst[c][r] = src[r][c] for rows and columns in range, 0 up to `rows_to` rows
+// of src (and for rows without a target, where targets is given).  64 x 64
+// elements a workgroup, through LDS.  TRANSPOSE false: dst[r][c], 0 up to
+// `cols_to` columns.
+template <typename T, bool TRANSPOSE>
+__global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t rows, int64_t cols, int64_t pitch,
+                                                   typename ProductOf<T>::P *dst, int64_t dst_pitch, int64_t dst_seg,
+                                                   int64_t rows_to, int64_t cols_to, const float *scale_row)
+{
+    typedef typename ProductOf<T>::P P;
+    constexpr int kParts = ProductOf<T>::kParts;
+    __shared__ float tile[64][65];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+    const int x = threadIdx.x % 64, y = threadIdx.x / 64;
+    for (int k = y; k < 64; k += 4) {
+        const int64_t r = r0 + k, c = c0 + x;
+        float v = 0.f;
+        if (r < rows && c < cols && !(scale_row && scale_row[r] == 0.f))
+            v = (float)src[r * pitch + c];
+        tile[k][x] = v;
+    }
+    __syncthreads();
+    for (int k = y; k < 64; k += 4) {
+        const int64_t r = TRANSPOSE ? r0 + x : r0 + k, c = TRANSPOSE ? c0 + k : c0 + x;
+        const float v = TRANSPOSE ? tile[x][k] : tile[k][x];
+        if (TRANSPOSE ? r >= rows_to || c >= cols : r >= rows || c >= cols_to)
+            continue;
+        P *at = dst + (TRANSPOSE ? c * dst_pitch + r : r * dst_pitch + c);
+        if constexpr (kParts == 1) {
+            *at = (P)v;
+        } else {
+            bf16 t[kTerms];
+            split(v, t);
+#pragma unroll
+            for (int q = 0; q < kTerms; ++q)
+                at[q * dst_seg] = t[q];
+        }
+    }
+}
+
+// ---- epilogues -------------------------------------------------------------------
+
+// A maximum and the sum of exponentials above it.
+struct Soft {
+    float top, sum;
+};
+__device__ inline float finite_or_0(float v) { return fabsf(v) <= 3.4028234e38f ? v : 0.f; }
+__device__ inline Soft join(Soft a, Soft b)
+{
+    const float top = fmaxf(a.top, b.top), m = finite_or_0(top);
+    return Soft{top, a.sum * __expf(a.top - m) + b.sum * __expf(b.top - m)};
+}
+
+// Maximum and sum of exponentials of each token over the tile's rows of W,
+// and the target's logit.
+struct StatsEpilogue {
+    float2 *part;  // [tiles_i][tokens]
+    float *target_logit;
+    const int64_t *targets;
+    int64_t v0, vocab, tokens;  // the first row of W, their number
+    template <typename S> __device__ void operator()(Results<S> &r, char *lds) const
+    {
+        Soft(*other)[S::BJ] = (Soft(*)[S::BJ])lds;
+        const bool tail = (r.tile_i + 1) * S::BI > vocab;
+#pragma unroll
+        for (int jj = 0; jj < S::NJ; ++jj) {
+            const int64_t j = r.j0 + 16 * jj;
+            const int64_t t = (j < tokens ? targets[j] : -1) - v0;
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t i = r.i0 + 16 * ii + e;
+                    if (tail && i >= vocab)
+                        r.acc[ii][jj][e] = -__builtin_inff();
+                    else if (i == t)
+                        target_logit[j] = r.acc[ii][jj][e];
+                    top = fmaxf(top, r.acc[ii][jj][e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m = finite_or_0(top);
+            float sum = 0.f;
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    sum += __expf(r.acc[ii][jj][e] - m);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (r.lane < 16)
+                other[r.wave_i][(r.wave_j * S::NJ + jj) * 16 + r.lane] = Soft{top, sum};
+        }
+        __syncthreads();
+        const int j = threadIdx.x;
+        if (j >= S::BJ || r.tile_j * S::BJ + j >= tokens)
+            return;
+        Soft s = other[0][j];
+#pragma unroll
+        for (int w = 1; w < S::WI; ++w)
+            s = join(s, other[w][j]);
+        part[r.tile_i * tokens + r.tile_j * S::BJ + j] = make_float2(s.top, s.sum);
+    }
+};
+
+// P[j][i] and its transpose, from the logits.
+template <typename T> struct ProbEpilogue {
+    typedef typename ProductOf<T>::P P;
+    P *p, *pt;
+    int64_t p_pitch, p_seg, pt_pitch, pt_seg;
+    const float *lse, *grad;  // grad: scaled gradient of each token's loss, 0 without a target
+    const int64_t *targets;
+    int64_t v0, rows, tokens, tokens_to;  // the piece's first row of W, its rows; tokens padded
+    template <typename S> __device__ void operator()(Results<S> &r, char *) const
+    {
+#pragma unroll
+        for (int jj = 0; jj < S::NJ; ++jj) {
+            const int64_t j = r.j0 + 16 * jj;
+            if (j >= tokens_to)
+                continue;
+            const float g = j < tokens ? grad[j] : 0.f, l = j < tokens ? lse[j] : 0.f;
+            const int64_t t = (j < tokens ? targets[j] : -1) - v0;
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii) {
+                const int64_t i = r.i0 + 16 * ii;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = __expf(r.acc[ii][jj][e] - l) - (i + e == t ? 1.f : 0.f);
+                    // selects: what a token without a target holds may be NaN
+                    v[e] = g != 0.f && i + e < rows ? v[e] * g : 0.f;
+                }
+                P t4[kTerms][4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (ProductOf<T>::kParts == 1) {
+                        t4[0][e] = (P)v[e];
+                    } else {
+                        bf16 s[kTerms];
+                        split(v[e], s);
+#pragma unroll
+                        for (int q = 0; q < kTerms; ++q)
+                            t4[q][e] = s[q];
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < ProductOf<T>::kParts; ++q) {
+                    // the piece is padded to whole tiles, and so is P's pitch
+                    if (j < tokens) {
+                        typename VecOf<P, 4>::V w;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = t4[q][e];
+                        *(typename VecOf<P, 4>::V *)(p + j * p_pitch + q * p_seg + i) = w;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < rows)
+                            pt[(i + e) * pt_pitch + q * pt_seg + j] = t4[q][e];
+                }
+            }
+        }
+    }
+};
+
+// C as 32-bit sums: one part of a split product, added to what is there or not.
+struct SumEpilogue {
+    float *c;
+    int64_t pitch, part, cols, rows;  // `part` elements between the parts
+    int add;
+    template <typename S> __device__ void operator()(Results<S> &r, char *) const
+    {
+        float *base = c + r.part * part;
+#pragma unroll
+        for (int jj = 0; jj < S::NJ; ++jj) {
+            const int64_t j = r.j0 + 16 * jj;
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii) {
+                const int64_t i = r.i0 + 16 * ii;  // pitch is a multiple of 4
+                if (j >= rows || i >= cols)
+                    continue;
+                f32x4 *at = (f32x4 *)(base + j * pitch + i);
+                *at = add ? *at + r.acc[ii][jj] : r.acc[ii][jj];
+            }
+        }
+    }
+};
+
+// C in the type of the result, times a scale from the device.
+template <typename T> struct OutEpilogue {
+    T *c;
+    int64_t pitch, cols, rows;
+    const float *scale;
+    template <typename S> __device__ void operator()(Results<S> &r, char *) const
+    {
+        const float f = *scale;
+#pragma unroll
+        for (int jj = 0; jj < S::NJ; ++jj) {
+            const int64_t j = r.j0 + 16 * jj;
+            if (j >= rows)
+                continue;
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii) {
+                const int64_t i = r.i0 + 16 * ii;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = r.acc[ii][jj][e] * f;
+                if (i < cols)
+                    store_some(c + j * pitch + i, cols - i < 4 ? (int)(cols - i) : 4, v);
+            }
+        }
+    }
+};
+
+// ---- small launches -----------------------------------------------------------------
+
+// Joins the tiles' maxima and sums: 16 tokens a workgroup, 16 lanes each.
+__global__ __launch_bounds__(256) void loss_kernel(const float2 *part, int64_t tiles, const float *target_logit,
+                                                   const int64_t *targets, int64_t ignore, int64_t vocab,
+                                                   int64_t tokens, float *loss, float *lse)
+{
+    __shared__ Soft other[16][17];
+    const int x = threadIdx.x % 16, y = threadIdx.x / 16;
+    const int64_t j = (int64_t)blockIdx.x * 16 + x;
+    Soft s{-__builtin_inff(), 0.f};
+    if (j < tokens)
+        for (int64_t t = y; t < tiles; t += 16) {
+            const float2 v = part[t * tokens + j];
+            s = join(s, Soft{v.x, v.y});
+        }
+    other[y][x] = s;
+    __syncthreads();
+    if (y > 0 || j >= tokens)
+        return;
+    for (int w = 1; w < 16; ++w)
+        s = join(s, other[w][x]);
+    const float l = finite_or_0(s.top) + logf(s.sum);
+    lse[j] = l;
+    const int64_t t = targets[j];
+    loss[j] = t == ignore ? 0.f : t >= 0 && t < vocab ? l - target_logit[j] : __builtin_nanf("");
+}
+
+// Gradients of the losses, 0 without a target, divided by a power of two near
+// the largest and multiplied by 2^12, so that P fits the range of 16-bit
+// floats whatever the loss was divided by; `scale` undoes it.
+__global__ __launch_bounds__(1024) void grad_kernel(const float *grad_loss, const int64_t *targets, int64_t ignore,
+                                                    int64_t vocab, int64_t tokens, float *grad, float *scale)
+{
+    __shared__ float top[16];
+    float m = 0.f;
+    for (int64_t j = threadIdx.x; j < tokens; j += 1024)
+        if (targets[j] != ignore) {
+            const float g = fabsf(grad_loss[j]);
+            m = fmaxf(m, g <= 3.4028234e38f ? g : 0.f);
+        }
+    for (int off = 32; off >= 1; off /= 2)
+        m = fmaxf(m, __shfl_xor(m, off));
+    if (threadIdx.x % 64 == 0)
+        top[threadIdx.x / 64] = m;
+    __syncthreads();
+    for (int w = 0; w < 16; ++w)
+        m = fmaxf(m, top[w]);
+    int e = 0;
+    if (m > 0.f)
+        (void)frexpf(m, &e);
+    e = (e < -100 ? -100 : e) - 12;
+    if (threadIdx.x == 0)
+        *scale = ldexpf(1.f, e);
+    for (int64_t j = threadIdx.x; j < tokens; j += 1024) {
+        const int64_t t = targets[j];
+        const float g = ldexpf(grad_loss[j], -e);
+        grad[j] = t == ignore ? 0.f : t >= 0 && t < vocab ? g : __builtin_nanf("");
+    }
+}
+
+// dH from its parts' sums.
+template <typename T>
+__global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t pitch, int64_t part, int parts,
+                                                     int64_t rows, int64_t cols, const float *scale, T *out,
+                                                     int64_t out_pitch)
+{
+    const int64_t quads = (cols + 3) / 4;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= rows * quads)
+        return;
+    const int64_t j = at / quads, i = at % quads * 4;
+    f32x4 s = *(const f32x4 *)(sum + j * pitch + i);
+    for (int q = 1; q < parts; ++q)
+        s += *(const f32x4 *)(sum + q * part + j * pitch + i);
+    const float f = *scale;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] = s[e] * f;
+    store_some(out + j * out_pitch + i, cols - i < 4 ? (int)(cols - i) : 4, v);
+}
+
+// Clears a matrix (gradients of nothing).
+template <typename T> __global__ __launch_bounds__(256) void clear_kernel(T *out, int64_t rows, int64_t cols,
+                                                                          int64_t pitch)
+{
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int64_t c = threadIdx.x; c < cols; c += 256)
+            out[r * pitch + c] = (T)0.f;
+}
+
+// ---- plans --------------------------------------------------------------------------
+
+constexpr int64_t kPad = 256;                     // rows and columns of P and its transpose in whole tiles
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of P and its transpose together
+
+int64_t pad(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
+
+struct Bump {
+    uint64_t at = 0;
+    uint64_t take(uint64_t bytes)
+    {
+        const uint64_t here = at;
+        at = round256(at + bytes);
+        return here;
+    }
+};
+
+bool xent_sizes_ok(int32_t type, int64_t n, int64_t d, int64_t v)
+{
+    return type_ok(type) && n >= 0 && n <= ROTOR_XENT_MAX_TOKENS && d >= 1 && d <= ROTOR_XENT_MAX_COLS && v >= 1 &&
+           v < ((int64_t)1 << 28);
+}
+
+// The largest pitch, in elements, with which 256 rows lie within 2^31 bytes.
+constexpr int64_t kMostPitch = (int64_t)1 << 22;
+
+// Whether the rows of a matrix can be read where they are.
+bool rows_aligned(const void *p, int64_t cols, int64_t pitch)
+{
+    return (uintptr_t)p % 16 == 0 && cols % 8 == 0 && pitch % 8 == 0;
+}
+
+struct ForwardLayout {
+    uint64_t part, target, h, w, total;
+    int64_t dk, piece;
+};
+
+// `pack`: H and W are copied as product operands, W piece by piece.
+ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool pack)
+{
+    ForwardLayout l;
+    Bump b;
+    const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
+    l.dk = pad(d, kStep);
+    l.part = b.take(8ull * (uint64_t)ceil_div(v, 128) * (uint64_t)n);
+    l.target = b.take(4ull * (uint64_t)n);
+    l.piece = v;
+    l.h = l.w = b.at;
+    if (pack) {
+        const int64_t most = (kPieceBytes / 2) / (2 * parts * l.dk) / kPad * kPad;  // at least kPad: see the limits
+        l.piece = v < most ? v : most;
+        l.h = b.take(2ull * (uint64_t)(parts * l.dk * n));
+        l.w = b.take(2ull * (uint64_t)(parts * l.dk * l.piece));
+    }
+    l.total = b.at;
+    return l;
+}
+
+struct BackwardLayout {
+    uint64_t grad, scale, h, w, ht, wt, p, pt, sum, total;
+    int64_t dk, piece, nk, pk, sum_pitch;
+    int split;
+};
+
+int64_t tiles(int64_t a, int64_t b, int64_t side) { return ceil_div(a, side) * ceil_div(b, side); }
+
+BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool pack)
+{
+    BackwardLayout l;
+    Bump b;
+    const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
+    l.dk = pad(d, kStep);
+    l.nk = pad(n, kPad);
+    l.piece = pad(v, kPad);
+    int64_t most = kPieceBytes / (4 * parts * l.nk) / kPad * kPad;
+    if (most < kPad)
+        most = kPad;
+    if (l.piece > most) {
+        // pieces of equal size
+        const int64_t count = ceil_div(l.piece, most);
+        l.piece = pad(ceil_div(l.piece, count), kPad);
+    }
+    l.grad = b.take(4ull * (uint64_t)n);
+    l.scale = b.take(4);
+    l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
+    l.w = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * l.piece) : 0);
+    l.ht = b.take(2ull * (uint64_t)(parts * l.nk * d));
+    l.wt = b.take(2ull * (uint64_t)(parts * l.piece * d));
+    l.p = b.take(2ull * (uint64_t)(parts * l.piece * n));
+    l.pt = b.take(2ull * (uint64_t)(parts * l.nk * l.piece));
+    // few tiles of dH: its summed index (the piece) in parts, for two
+    // workgroups on every CU
+    const int64_t t = tiles(d, n, 256) >= 128 ? tiles(d, n, 256) : tiles(d, n, 128);
+    int64_t split = t >= 256 ? 1 : 256 / t;
+    const int64_t steps = (type == ROTOR_F32 ? kTermProducts : 1) * (l.piece / kStep);
+    if (split > steps / 8)
+        split = steps / 8 > 0 ? steps / 8 : 1;
+    l.split = (int)split;
+    l.sum_pitch = pad(d, 4);
+    l.sum = b.take(4ull * (uint64_t)(l.split * n * l.sum_pitch));
+    l.total = b.at;
+    return l;
+}
+
+template <typename P, typename S, typename E>
+void run_tiles(const Operand<P> &a, const Operand<P> &b, int64_t k, int products, int split, E e, hipStream_t s)
+{
+    ProductArgs p;
+    p.k = k;
+    p.products = products;
+    p.tiles_i = (int)ceil_div(a.rows, S::BI);
+    p.tiles_j = (int)ceil_div(b.rows, S::BJ);
+    p.steps = products * (int)ceil_div(k, kStep);
+    p.split_steps = (int)ceil_div(p.steps, split);
+    product_kernel<P, S, E>
+        <<<dim3((uint32_t)((int64_t)p.tiles_i * p.tiles_j), (uint32_t)split), S::kThreads, 0, s>>>(a, b, p, e);
+}
+
+// Large tiles if they fill the 256 CUs, else small ones.
+bool large_tiles(int64_t a, int64_t b, int split) { return tiles(a, b, 256) * split >= 128; }
+
+template <typename P, typename E>
+void run_product(const Operand<P> &a, const Operand<P> &b, int64_t k, int products, int split, E e, hipStream_t s)
+{
+    if (large_tiles(a.rows, b.rows, split))
+        run_tiles<P, Large, E>(a, b, k, products, split, e, s);
+    else
+        run_tiles<P, Small, E>(a, b, k, products, split, e, s);
+}
+
+template <typename T, bool TRANSPOSE>
+void run_pack(const T *src, int64_t rows, int64_t cols, int64_t pitch, void *dst, int64_t dst_pitch, int64_t dst_seg,
+              int64_t rows_to, int64_t cols_to, const float *scale_row, hipStream_t s)
+{
+    pack_kernel<T, TRANSPOSE><<<dim3((uint32_t)ceil_div(TRANSPOSE ? rows_to : rows, 64),
+                                     (uint32_t)ceil_div(TRANSPOSE ? cols : cols_to, 64)),
+                                256, 0, s>>>(src, rows, cols, pitch, (typename ProductOf<T>::P *)dst, dst_pitch,
+                                             dst_seg, rows_to, cols_to, scale_row);
+}
+
+// H or rows of W as a product's operand, packed into `space` if need be.
+template <typename T>
+Operand<typename ProductOf<T>::P> operand(const T *src, int64_t rows, int64_t cols, int64_t pitch, bool pack,
+                                          void *space, int64_t dk, hipStream_t s)
+{
+    typedef typename ProductOf<T>::P P;
+    constexpr int64_t parts = ProductOf<T>::kParts;
+    if (!pack)
+        return Operand<P>{(const P *)src, rows, pitch, 0};
+    run_pack<T, false>(src, rows, cols, pitch, space, parts * dk, dk, rows, dk, nullptr, s);
+    return Operand<P>{(const P *)space, rows, parts * dk, parts > 1 ? dk : 0};
+}
+
+}  // namespace
+}  // namespace rotor
+
+using namespace rotor;
+
+extern "C" {
+
+int32_t rotor_xent_workspace_bytes(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows, int32_t aligned,
+                                   int32_t backward, uint64_t *bytes)
+{
+    if (!bytes || !xent_sizes_ok(type, n_tokens, cols, n_rows))
+        return ROTOR_EINVAL;
+    const bool pack = type == ROTOR_F32 || !aligned;
+    *bytes = backward ? backward_layout(type, n_tokens, cols, n_rows, pack).total
+                      : forward_layout(type, n_tokens, cols, n_rows, pack).total;
+    if (*bytes < 16)
+        *bytes = 16;
+    return ROTOR_OK;
+}
+
+int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows, const void *d_h, int64_t h_pitch,
+                   const void *d_w, int64_t w_pitch, const int64_t *d_targets, int64_t ignore, float *d_loss,
+                   float *d_lse, int32_t aligned, void *d_work, uint64_t work_bytes, void *stream)
+{
+    if (!xent_sizes_ok(type, n_tokens, cols, n_rows))
+        return ROTOR_EINVAL;
+    const int64_t es = elem_bytes(type);
+    const bool pack = type == ROTOR_F32 || !aligned;
+    if (!matrix_ok(d_h, n_tokens, cols, h_pitch, es) || !matrix_ok(d_w, n_rows, cols, w_pitch, es) ||
+        h_pitch > kMostPitch || w_pitch > kMostPitch)
+        return ROTOR_EINVAL;
+    if (n_tokens == 0)
+        return ROTOR_OK;
+    if (!pack && (!rows_aligned(d_h, cols, h_pitch) || !rows_aligned(d_w, cols, w_pitch)))
+        return ROTOR_EINVAL;
+    const ForwardLayout l = forward_layout(type, n_tokens, cols, n_rows, pack);
+    if (!d_targets || (uintptr_t)d_targets % 8 || !d_loss || (uintptr_t)d_loss % 4 || !d_lse ||
+        (uintptr_t)d_lse % 4 || !d_work || (uintptr_t)d_work % 16 || work_bytes < l.total)
+        return ROTOR_EINVAL;
+    char *const work = (char *)d_work;
+    const hipStream_t s = (hipStream_t)stream;
+    (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
+    with_type(type, [&](auto e) {
+        typedef typename decltype(e)::T T;
+        typedef typename ProductOf<T>::P P;
+        const int products = ProductOf<T>::kParts == 1 ? 1 : kTermProducts;
+        const T *w = (const T *)d_w;
+        const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
+        float2 *part = (float2 *)(work + l.part);
+        int64_t tiles_done = 0;
+        for (int64_t v0 = 0; v0 < n_rows; v0 += l.piece) {
+            const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
+            const Operand<P> a = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
+            StatsEpilogue ep;
+            ep.part = part + tiles_done * n_tokens;
+            ep.target_logit = (float *)(work + l.target);
+            ep.targets = d_targets;
+            ep.vocab = rows;
+            ep.tokens = n_tokens;
+            ep.v0 = v0;
+            run_product<P>(a, b, pad(cols, 8), products, 1, ep, s);
+            tiles_done += ceil_div(rows, large_tiles(rows, n_tokens, 1) ? 256 : 128);
+        }
+        loss_kernel<<<dim3((uint32_t)ceil_div(n_tokens, 16)), 256, 0, s>>>(part, tiles_done,
+                                                                          (const float *)(work + l.target), d_targets,
+                                                                          ignore, n_rows, n_tokens, d_loss, d_lse);
+    });
+    return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+}
+
+int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows, const void *d_h,
+                            int64_t h_pitch, const void *d_w, int64_t w_pitch, const int64_t *d_targets,
+                            int64_t ignore, const float *d_lse, const float *d_grad_loss, void *d_dh,
+                            int64_t dh_pitch, void *d_dw, int64_t dw_pitch, int32_t aligned, void *d_work,
+                            uint64_t work_bytes, void *stream)
+{
+    if (!xent_sizes_ok(type, n_tokens, cols, n_rows) || (!d_dh && !d_dw))
+        return ROTOR_EINVAL;
+    const int64_t es = elem_bytes(type);
+    const bool pack = type == ROTOR_F32 || !aligned;
+    if (!matrix_ok(d_h, n_tokens, cols, h_pitch, es) || !matrix_ok(d_w, n_rows, cols, w_pitch, es) ||
+        h_pitch > kMostPitch || w_pitch > kMostPitch ||
+        (d_dh && !matrix_ok(d_dh, n_tokens, cols, dh_pitch, es)) ||
+        (d_dw && !matrix_ok(d_dw, n_rows, cols, dw_pitch, es)))
+        return ROTOR_EINVAL;
+    const hipStream_t s = (hipStream_t)stream;
+    if (n_tokens == 0) {
+        (void)hipGetLastError();
+        if (d_dw)
+            with_type(type, [&](auto e) {
+                typedef typename decltype(e)::T T;
+                clear_kernel<T><<<dim3((uint32_t)(n_rows < 4096 ? n_rows : 4096)), 256, 0, s>>>((T *)d_dw, n_rows,
+                                                                                               cols, dw_pitch);
+            });
+        return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+    }
+    const BackwardLayout l = backward_layout(type, n_tokens, cols, n_rows, pack);
+    if (!pack && (!rows_aligned(d_h, cols, h_pitch) || !rows_aligned(d_w, cols, w_pitch)))
+        return ROTOR_EINVAL;
+    if (!d_targets || (uintptr_t)d_targets % 8 || !d_lse || (uintptr_t)d_lse % 4 || !d_grad_loss ||
+        (uintptr_t)d_grad_loss % 4 || !d_work || (uintptr_t)d_work % 16 || work_bytes < l.total)
+        return ROTOR_EINVAL;
+    char *const work = (char *)d_work;
+    (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
+    with_type(type, [&](auto e) {
+        typedef typename decltype(e)::T T;
+        typedef typename ProductOf<T>::P P;
+        constexpr int64_t parts = ProductOf<T>::kParts;
+        const int products = parts == 1 ? 1 : kTermProducts;
+        float *const grad = (float *)(work + l.grad), *const scale = (float *)(work + l.scale);
+        float *const sum = (float *)(work + l.sum);
+        const T *h = (const T *)d_h, *w = (const T *)d_w;
+        grad_kernel<<<1, 1024, 0, s>>>(d_grad_loss, d_targets, ignore, n_rows, n_tokens, grad, scale);
+        const Operand<P> hb = operand<T>(h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
+        if (d_dw)  // rows without a target as 0: they may hold NaN
+            run_pack<T, true>(h, n_tokens, cols, h_pitch, work + l.ht, parts * l.nk, l.nk, l.nk, cols, grad, s);
+        for (int64_t v0 = 0; v0 < n_rows; v0 += l.piece) {
+            const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
+            const Operand<P> wa = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
+            ProbEpilogue<T> ep;
+            ep.p = (P *)(work + l.p);
+            ep.pt = (P *)(work + l.pt);
+            ep.p_pitch = parts * l.piece;
+            ep.p_seg = l.piece;
+            ep.pt_pitch = parts * l.nk;
+            ep.pt_seg = l.nk;
+            ep.lse = d_lse;
+            ep.grad = grad;
+            ep.targets = d_targets;
+            ep.v0 = v0;
+            ep.rows = rows;
+            ep.tokens = n_tokens;
+            ep.tokens_to = l.nk;
+            run_product<P>(wa, hb, pad(cols, 8), products, 1, ep, s);
+            if (d_dh) {
+                const int64_t k = pad(rows, kStep);
+                run_pack<T, true>(w + v0 * w_pitch, rows, cols, w_pitch, work + l.wt, parts * l.piece, l.piece, k,
+                                  cols, nullptr, s);
+                SumEpilogue se;
+                se.c = sum;
+                se.pitch = l.sum_pitch;
+                se.part = n_tokens * l.sum_pitch;
+                se.cols = cols;
+                se.rows = n_tokens;
+                se.add = v0 > 0;
+                run_product<P>(Operand<P>{(const P *)(work + l.wt), cols, parts * l.piece, parts > 1 ? l.piece : 0},
+                               Operand<P>{(const P *)(work + l.p), n_tokens, parts * l.piece, parts > 1 ? l.piece : 0},
+                               k, products, l.split, se, s);
+            }
+            if (d_dw) {
+                OutEpilogue<T> oe;
+                oe.c = (T *)d_dw + v0 * dw_pitch;
+                oe.pitch = dw_pitch;
+                oe.cols = cols;
+                oe.rows = rows;
+                oe.scale = scale;
+                run_product<P>(Operand<P>{(const P *)(work + l.ht), cols, parts * l.nk, parts > 1 ? l.nk : 0},
+                               Operand<P>{(const P *)(work + l.pt), rows, parts * l.nk, parts > 1 ? l.nk : 0},
+                               pad(n_tokens, kStep), products, 1, oe, s);
+            }
+        }
+        if (d_dh) {
+            const int64_t quads = n_tokens * ceil_div(cols, 4);
+            finish_kernel<T><<<dim3((uint32_t)ceil_div(quads, 256)), 256, 0, s>>>(
+                sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, (T *)d_dh, dh_pitch);
+        }
+    });
+    return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+}
+
+}  // extern "C"

@@ -1,6 +1,7 @@
 """Operators of a language-model chain's stages, on the C ABI in
 include/rotor.h: counter-based dropout, embedding lookup, the residual seam
-between two blocks (norms, gate, residual scale), and their gradients.
+between two blocks (norms, gate, residual scale), the cross entropy over a
+vocabulary without its logits, and their gradients.
 
 Argument checks, allocation and marshalling only: every operator runs in the
 library's HIP kernels.  Tensors are CUDA tensors of one device and, where
@@ -292,3 +293,64 @@ def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None
           *(matrix(y, "y") if dh is not None else (None, n.cols)), *matrix(z, "z"), stats.data_ptr(),
           g["x"].data_ptr(), n.cols, _ptr(g.get("z")), n.cols, ctypes.byref(out), work.data_ptr(), work.numel())
     return g
+
+
+# ---- cross entropy ---------------------------------------------------------------------
+
+XENT_MAX_TOKENS, XENT_MAX_COLS = 1 << 20, 65536
+
+
+def _xent(h, w, targets, backward, stream):
+    """Checked sizes, pitches and workspace of a cross entropy."""
+    code = _typed(h, "h")
+    if h.dim() < 1 or w.dim() != 2 or h.shape[-1] != w.shape[1]:
+        raise ValueError("h and w must have the same columns, w two dimensions")
+    if _cuda(w, "w").dtype != h.dtype or w.device != h.device:
+        raise ValueError(f"w must be {h.dtype} on {h.device}")
+    if not isinstance(targets, torch.Tensor) or targets.dtype != torch.int64 or targets.device != h.device or \
+            targets.shape != h.shape[:-1] or not targets.is_contiguous():
+        raise ValueError(f"targets must be contiguous int64 on {h.device}, one for each row of h")
+    n, cols, hp = _matrix(h, "h")
+    rows, _, wp = _matrix(w, "w")
+    if rows < 1 or n > XENT_MAX_TOKENS or cols > XENT_MAX_COLS:
+        raise ValueError(f"at most {XENT_MAX_TOKENS} tokens and {XENT_MAX_COLS} columns, and at least one row of w")
+    aligned = int(not (cols % 8 or hp % 8 or wp % 8 or h.data_ptr() % 16 or w.data_ptr() % 16))
+    need = ctypes.c_uint64()
+    rotor._check(rotor.lib().rotor_xent_workspace_bytes(code, n, cols, rows, aligned, backward, ctypes.byref(need)),
+                 "rotor_xent_workspace_bytes")
+    return code, n, cols, rows, hp, wp, aligned, _scratch(need.value, h.device, stream)
+
+
+def _per_token(t, targets, what):
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.device != targets.device or \
+            t.shape != targets.shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous float32 on {targets.device}, shaped as targets")
+    return t.data_ptr()
+
+
+def linear_cross_entropy(h, w, targets, ignore=-100, *, stream=None):
+    """Loss and log-sum-exp of each token, float32, shaped as ``targets``: the
+    softmax cross entropy of the logits h w^T, which never exist whole.
+    Tokens with target ``ignore`` have loss 0; other targets outside the rows
+    of w give NaN."""
+    code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 0, stream)
+    loss, lse = (torch.empty(targets.shape, dtype=torch.float32, device=h.device) for _ in range(2))
+    _call("rotor_xent", h.device, stream, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp, targets.data_ptr(),
+          ignore, loss.data_ptr(), lse.data_ptr(), aligned, work.data_ptr(), work.numel())
+    return loss, lse
+
+
+def linear_cross_entropy_backward(h, w, targets, lse, grad_loss, ignore=-100, *, need_h=True, need_w=True,
+                                  stream=None):
+    """Gradients of h and w from those of the losses (float32, shaped as
+    ``targets``) and the log-sum-exps of the forward; None where not needed."""
+    if not (need_h or need_w):
+        return None, None
+    code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 1, stream)
+    lse, grad_loss = _per_token(lse, targets, "lse"), _per_token(grad_loss, targets, "grad_loss")
+    dh = torch.empty(h.shape, dtype=h.dtype, device=h.device) if need_h else None
+    dw = torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None
+    _call("rotor_xent_backward", h.device, stream, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp,
+          targets.data_ptr(), ignore, lse, grad_loss, _ptr(dh), cols, _ptr(dw), cols, aligned, work.data_ptr(),
+          work.numel())
+    return dh, dw

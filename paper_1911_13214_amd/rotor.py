@@ -58,6 +58,10 @@ SIGNATURES = {
     "rotor_residual_norm_workspace_bytes": (_i32, [_vp, _P(_u64)]),
     "rotor_residual_norm_backward": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64,
                                             _vp, _vp, _u64, _vp]),
+    "rotor_xent_workspace_bytes": (_i32, [_i32, _i64, _i64, _i64, _i32, _i32, _P(_u64)]),
+    "rotor_xent": (_i32, [_i32, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _u64, _vp]),
+    "rotor_xent_backward": (_i32, [_i32, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp,
+                                   _i64, _i32, _vp, _u64, _vp]),
 }
 
 KERNEL_CLASSES = ("leaf", "diag", "middle", "edge", "prep")
