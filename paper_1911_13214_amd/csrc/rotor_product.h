@@ -62,15 +62,22 @@ template <int BI_, int BJ_, int WI_, int WJ_> struct Tile {
     static constexpr int kLoadsA = BI / 8 / kWaves, kLoadsB = BJ / 8 / kWaves;  // of a wave in one step
 };
 
-// Where a lane's results lie: element r of acc[ii][jj] is
-// (i0 + 16 ii + r, j0 + 16 jj).
+// A wave's results: element r of acc[ii][jj] of a lane is row (of A)
+// i + 16 ii + r and row (of B) j + 16 jj of the tile that starts at
+// (tile_i * BI, tile_j * BJ).
 template <typename S> struct Results {
     f32x4 acc[S::NI][S::NJ];
-    int64_t tile_i, tile_j;  // tile indices
-    int64_t i0, j0;
+    int tile_i, tile_j;
+    int i, j;
     int wave_i, wave_j, lane;
     int part;
+    char *lds;  // the wave's own share of LDS: 16 BI BJ / waves bits at least
 };
+
+// Hides where a value comes from, so that what is computed from it stays
+// where it is written: the epilogues' addresses would otherwise be computed
+// before the product's loop and spilled.
+__device__ inline void opaque(int &v) { asm volatile("" : "+v"(v)); }
 
 // Tile order: the eight XCDs (workgroups go to them in turn) take contiguous
 // runs, so that what neighbours share stays in one XCD's L2; in a run four
@@ -154,9 +161,10 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     const int t0 = blockIdx.y * p.split_steps;
     const int t1 = t0 + p.split_steps < p.steps ? t0 + p.split_steps : p.steps;
     int s = kTermProducts - p.products + t0 / per, at = t0 % per;  // of the next load
-    auto load = [&](char *lds) {
-        la.load(lds, (uint32_t)(term_a(s) * a.seg * sizeof(T)), (uint32_t)at * kRowBytes);
-        lb.load(lds + S::BI * kRowBytes, (uint32_t)(term_b(s) * b.seg * sizeof(T)), (uint32_t)at * kRowBytes);
+    auto load = [&](char *lds, bool live) {
+        const uint32_t kb = live ? (uint32_t)at * kRowBytes : 0x7FFFFF00u;
+        la.load(lds, (uint32_t)(term_a(s) * a.seg * sizeof(T)), kb);
+        lb.load(lds + S::BI * kRowBytes, (uint32_t)(term_b(s) * b.seg * sizeof(T)), kb);
         if (++at == per) {
             at = 0;
             ++s;
@@ -190,30 +198,32 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
         }
     };
 
+    // an odd number of steps is followed by one of zeros: one way out of the
+    // loop, so that the sums stay where they are
     if (t0 < t1)
-        load(even);
+        load(even, true);
     __syncthreads();
-    for (int t = t0; t < t1;) {
-        if (t + 1 < t1)
-            load(odd);
+    for (int t = t0; t < t1; t += 2) {
+        load(odd, t + 1 < t1);
         multiply(even);
         __syncthreads();
-        if (++t >= t1)
-            break;
-        if (t + 1 < t1)
-            load(even);
+        if (t + 2 < t1)
+            load(even, true);
         multiply(odd);
         __syncthreads();
-        ++t;
     }
     res.tile_i = ti;
     res.tile_j = tj;
     res.wave_i = wi;
     res.wave_j = wj;
     res.lane = lane;
-    res.i0 = (int64_t)ti * S::BI + wi * S::NI * 16 + lane / 16 * 4;
-    res.j0 = (int64_t)tj * S::BJ + wj * S::NJ * 16 + row;
+    res.i = wi * S::NI * 16 + lane / 16 * 4;
+    res.j = wj * S::NJ * 16 + row;
     res.part = blockIdx.y;
+    constexpr int kShare = 2 * S::kBytes / S::kWaves;
+    res.lds = wave < S::kWaves / 2 ? even + wave * kShare : odd + (wave - S::kWaves / 2) * kShare;
+    opaque(res.i);
+    opaque(res.j);
     epilogue(res, even);
 #endif
 }

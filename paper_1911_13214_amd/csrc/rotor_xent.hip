@@ -99,24 +99,35 @@ struct StatsEpilogue {
     float2 *part;  // [tiles_i][tokens]
     float *target_logit;
     const int64_t *targets;
-    int64_t v0, vocab, tokens;  // the first row of W, their number
+    int64_t v0;         // the first row of W
+    int vocab, tokens;  // rows, tokens
     template <typename S> __device__ void operator()(Results<S> &r, char *lds) const
     {
         Soft(*other)[S::BJ] = (Soft(*)[S::BJ])lds;
-        const bool tail = (r.tile_i + 1) * S::BI > vocab;
+        const int have = vocab - r.tile_i * S::BI;  // rows of W in the tile
+        const int j0 = r.tile_j * S::BJ;
+        if (have < S::BI) {
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (r.i + 16 * ii + e >= have)
+#pragma unroll
+                        for (int jj = 0; jj < S::NJ; ++jj)
+                            r.acc[ii][jj][e] = -__builtin_inff();
+        }
 #pragma unroll
         for (int jj = 0; jj < S::NJ; ++jj) {
-            const int64_t j = r.j0 + 16 * jj;
-            const int64_t t = (j < tokens ? targets[j] : -1) - v0;
+            const int j = j0 + r.j + 16 * jj;
+            // the target's place among this lane's rows, if it is there
+            const int64_t t64 = (j < tokens ? targets[j] : -1) - v0 - r.tile_i * S::BI;
+            const int t = t64 >= 0 && t64 < S::BI && t64 < have ? (int)t64 - r.i : -1;
             float top = -__builtin_inff();
 #pragma unroll
             for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int64_t i = r.i0 + 16 * ii + e;
-                    if (tail && i >= vocab)
-                        r.acc[ii][jj][e] = -__builtin_inff();
-                    else if (i == t)
+                    if (t == 16 * ii + e)
                         target_logit[j] = r.acc[ii][jj][e];
                     top = fmaxf(top, r.acc[ii][jj][e]);
                 }
@@ -136,71 +147,109 @@ struct StatsEpilogue {
         }
         __syncthreads();
         const int j = threadIdx.x;
-        if (j >= S::BJ || r.tile_j * S::BJ + j >= tokens)
+        if (j >= S::BJ || j0 + j >= tokens)
             return;
         Soft s = other[0][j];
 #pragma unroll
         for (int w = 1; w < S::WI; ++w)
             s = join(s, other[w][j]);
-        part[r.tile_i * tokens + r.tile_j * S::BJ + j] = make_float2(s.top, s.sum);
+        part[(int64_t)r.tile_i * tokens + j0 + j] = make_float2(s.top, s.sum);
     }
 };
 
 // P[j][i] and its transpose, from the logits.
 template <typename T> struct ProbEpilogue {
     typedef typename ProductOf<T>::P P;
+    static constexpr int kParts = ProductOf<T>::kParts;
     P *p, *pt;
-    int64_t p_pitch, p_seg, pt_pitch, pt_seg;
+    int p_pitch, p_seg, pt_pitch, pt_seg;
     const float *lse, *grad;  // grad: scaled gradient of each token's loss, 0 without a target
     const int64_t *targets;
-    int64_t v0, rows, tokens, tokens_to;  // the piece's first row of W, its rows; tokens padded
+    int64_t v0;                   // the piece's first row of W
+    int rows, tokens, tokens_to;  // its rows; tokens, and padded
     template <typename S> __device__ void operator()(Results<S> &r, char *) const
     {
+        typedef typename VecOf<P, 4>::V V4;
+        typedef P V8 __attribute__((ext_vector_type(8)));
+        const int have = rows - r.tile_i * S::BI;
+        const int j0 = r.tile_j * S::BJ;
 #pragma unroll
         for (int jj = 0; jj < S::NJ; ++jj) {
-            const int64_t j = r.j0 + 16 * jj;
-            if (j >= tokens_to)
-                continue;
-            const float g = j < tokens ? grad[j] : 0.f, l = j < tokens ? lse[j] : 0.f;
-            const int64_t t = (j < tokens ? targets[j] : -1) - v0;
+            const int j = j0 + r.j + 16 * jj;
+            const bool in = j < tokens;
+            const float g = in ? grad[j] : 0.f, l = in ? lse[j] : 0.f;
+            const int64_t t64 = (in ? targets[j] : -1) - v0 - r.tile_i * S::BI;
+            const int t = t64 >= 0 && t64 < S::BI ? (int)t64 - r.i : -1;
 #pragma unroll
-            for (int ii = 0; ii < S::NI; ++ii) {
-                const int64_t i = r.i0 + 16 * ii;
-                float v[4];
+            for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = __expf(r.acc[ii][jj][e] - l) - (i + e == t ? 1.f : 0.f);
-                    // selects: what a token without a target holds may be NaN
-                    v[e] = g != 0.f && i + e < rows ? v[e] * g : 0.f;
+                    const float v = __expf(r.acc[ii][jj][e] - l) - (t == 16 * ii + e ? 1.f : 0.f);
+                    // a select: what a token without a target holds may be NaN
+                    r.acc[ii][jj][e] = g != 0.f && r.i + 16 * ii + e < have ? v * g : 0.f;
                 }
-                P t4[kTerms][4];
+        }
+        __syncthreads();  // all waves have left the LDS the transposition uses
+#pragma unroll 1
+        for (int q = 0; q < kParts; ++q) {
+            // the piece is padded to whole tiles, and so is P's pitch
+            P *const tile = p + (int64_t)j0 * p_pitch + q * p_seg + r.tile_i * S::BI;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (ProductOf<T>::kParts == 1) {
-                        t4[0][e] = (P)v[e];
-                    } else {
-                        bf16 s[kTerms];
-                        split(v[e], s);
+            for (int jj = 0; jj < S::NJ; ++jj) {
+                int row = r.j + 16 * jj;
+                opaque(row);
+                if (j0 + row < tokens) {
 #pragma unroll
-                        for (int q = 0; q < kTerms; ++q)
-                            t4[q][e] = s[q];
-                    }
-                }
-#pragma unroll
-                for (int q = 0; q < ProductOf<T>::kParts; ++q) {
-                    // the piece is padded to whole tiles, and so is P's pitch
-                    if (j < tokens) {
-                        typename VecOf<P, 4>::V w;
+                    for (int ii = 0; ii < S::NI; ++ii) {
+                        V4 w;
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            w[e] = t4[q][e];
-                        *(typename VecOf<P, 4>::V *)(p + j * p_pitch + q * p_seg + i) = w;
+                            w[e] = (P)r.acc[ii][jj][e];
+                        *(V4 *)(tile + (uint32_t)(row * p_pitch + r.i + 16 * ii)) = w;
                     }
+                }
+            }
+            // the wave's own results transposed through its share of LDS, a
+            // row of i adjacent, so that rows are stored 2 NJ * 16 bytes at a
+            // time; the four lanes groups' rows go to different banks
+            constexpr int kRow = S::NJ * 32;  // bytes
+            static_assert(kRow == 128, "the banks' pattern");
+#pragma unroll
+            for (int jj = 0; jj < S::NJ; ++jj)
+#pragma unroll
+                for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (i + e < rows)
-                            pt[(i + e) * pt_pitch + q * pt_seg + j] = t4[q][e];
+                        *(P *)(r.lds + (16 * ii + r.lane / 16 * 4 + e) * kRow +
+                               (((16 * jj + r.lane % 16) * 2) ^ (r.lane / 16 * 32))) = (P)r.acc[ii][jj][e];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            int i = r.lane / 8;  // 8 lanes a row
+            opaque(i);
+            const int jt = r.wave_j * S::NJ * 16 + r.lane % 8 * 8;
+            P *const tile_t = pt + (int64_t)r.tile_i * S::BI * pt_pitch + q * pt_seg + j0;
+            if (j0 + jt < tokens_to) {
+#pragma unroll
+                for (int k = 0; k < S::NI * 2; ++k) {
+                    const int row = i + 8 * k, it = r.wave_i * S::NI * 16 + row;
+                    const V8 w = *(const V8 *)(r.lds + row * kRow + ((r.lane % 8 * 16) ^ (row / 4 % 4 * 32)));
+                    if (it < have)
+                        *(V8 *)(tile_t + (uint32_t)(it * pt_pitch + jt)) = w;
                 }
+            }
+            if (kParts > 1) {
+                // what the next term has to hold
+#pragma unroll
+                for (int jj = 0; jj < S::NJ; ++jj)
+#pragma unroll
+                    for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float t = (float)(P)r.acc[ii][jj][e];
+                            r.acc[ii][jj][e] = finite_or_0(r.acc[ii][jj][e] - t);
+                        }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
             }
         }
     }
@@ -209,20 +258,24 @@ template <typename T> struct ProbEpilogue {
 // C as 32-bit sums: one part of a split product, added to what is there or not.
 struct SumEpilogue {
     float *c;
-    int64_t pitch, part, cols, rows;  // `part` elements between the parts
-    int add;
+    int64_t part;  // elements between the parts
+    int pitch, cols, rows, add;
     template <typename S> __device__ void operator()(Results<S> &r, char *) const
     {
-        float *base = c + r.part * part;
+        float *const tile = c + r.part * part + (int64_t)r.tile_j * S::BJ * pitch + r.tile_i * S::BI;
+        const int cols_in = cols - r.tile_i * S::BI, rows_in = rows - r.tile_j * S::BJ;
 #pragma unroll
         for (int jj = 0; jj < S::NJ; ++jj) {
-            const int64_t j = r.j0 + 16 * jj;
+            int j = r.j + 16 * jj;
+            opaque(j);
+            if (j >= rows_in)
+                continue;
 #pragma unroll
             for (int ii = 0; ii < S::NI; ++ii) {
-                const int64_t i = r.i0 + 16 * ii;  // pitch is a multiple of 4
-                if (j >= rows || i >= cols)
+                const int i = r.i + 16 * ii;  // pitch is a multiple of 4
+                if (i >= cols_in)
                     continue;
-                f32x4 *at = (f32x4 *)(base + j * pitch + i);
+                f32x4 *at = (f32x4 *)(tile + (uint32_t)(j * pitch + i));
                 *at = add ? *at + r.acc[ii][jj] : r.acc[ii][jj];
             }
         }
@@ -232,25 +285,36 @@ struct SumEpilogue {
 // C in the type of the result, times a scale from the device.
 template <typename T> struct OutEpilogue {
     T *c;
-    int64_t pitch, cols, rows;
     const float *scale;
+    int pitch, cols, rows;
     template <typename S> __device__ void operator()(Results<S> &r, char *) const
     {
+        typedef typename VecOf<T, 4>::V V4;
         const float f = *scale;
+        T *const tile = c + (int64_t)r.tile_j * S::BJ * pitch + r.tile_i * S::BI;
+        const int cols_in = cols - r.tile_i * S::BI, rows_in = rows - r.tile_j * S::BJ;
 #pragma unroll
         for (int jj = 0; jj < S::NJ; ++jj) {
-            const int64_t j = r.j0 + 16 * jj;
-            if (j >= rows)
+            int j = r.j + 16 * jj;
+            opaque(j);
+            if (j >= rows_in)
                 continue;
 #pragma unroll
             for (int ii = 0; ii < S::NI; ++ii) {
-                const int64_t i = r.i0 + 16 * ii;
-                float v[4];
+                const int i = r.i + 16 * ii;
+                T *const at = tile + (uint32_t)(j * pitch + i);
+                if (i + 4 <= cols_in) {
+                    V4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = r.acc[ii][jj][e] * f;
-                if (i < cols)
-                    store_some(c + j * pitch + i, cols - i < 4 ? (int)(cols - i) : 4, v);
+                    for (int e = 0; e < 4; ++e)
+                        v[e] = (T)(r.acc[ii][jj][e] * f);
+                    *(V4 *)at = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (i + e < cols_in)
+                            at[e] = (T)(r.acc[ii][jj][e] * f);
+                }
             }
         }
     }
@@ -558,8 +622,8 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
             ep.part = part + tiles_done * n_tokens;
             ep.target_logit = (float *)(work + l.target);
             ep.targets = d_targets;
-            ep.vocab = rows;
-            ep.tokens = n_tokens;
+            ep.vocab = (int)rows;
+            ep.tokens = (int)n_tokens;
             ep.v0 = v0;
             run_product<P>(a, b, pad(cols, 8), products, 1, ep, s);
             tiles_done += ceil_div(rows, large_tiles(rows, n_tokens, 1) ? 256 : 128);
@@ -582,7 +646,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
     const int64_t es = elem_bytes(type);
     const bool pack = type == ROTOR_F32 || !aligned;
     if (!matrix_ok(d_h, n_tokens, cols, h_pitch, es) || !matrix_ok(d_w, n_rows, cols, w_pitch, es) ||
-        h_pitch > kMostPitch || w_pitch > kMostPitch ||
+        h_pitch > kMostPitch || w_pitch > kMostPitch || (d_dw && dw_pitch > kMostPitch) ||
         (d_dh && !matrix_ok(d_dh, n_tokens, cols, dh_pitch, es)) ||
         (d_dw && !matrix_ok(d_dw, n_rows, cols, dw_pitch, es)))
         return ROTOR_EINVAL;
@@ -623,17 +687,17 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             ProbEpilogue<T> ep;
             ep.p = (P *)(work + l.p);
             ep.pt = (P *)(work + l.pt);
-            ep.p_pitch = parts * l.piece;
-            ep.p_seg = l.piece;
-            ep.pt_pitch = parts * l.nk;
-            ep.pt_seg = l.nk;
+            ep.p_pitch = (int)(parts * l.piece);
+            ep.p_seg = (int)l.piece;
+            ep.pt_pitch = (int)(parts * l.nk);
+            ep.pt_seg = (int)l.nk;
             ep.lse = d_lse;
             ep.grad = grad;
             ep.targets = d_targets;
             ep.v0 = v0;
-            ep.rows = rows;
-            ep.tokens = n_tokens;
-            ep.tokens_to = l.nk;
+            ep.rows = (int)rows;
+            ep.tokens = (int)n_tokens;
+            ep.tokens_to = (int)l.nk;
             run_product<P>(wa, hb, pad(cols, 8), products, 1, ep, s);
             if (d_dh) {
                 const int64_t k = pad(rows, kStep);
@@ -641,10 +705,10 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                                   cols, nullptr, s);
                 SumEpilogue se;
                 se.c = sum;
-                se.pitch = l.sum_pitch;
+                se.pitch = (int)l.sum_pitch;
                 se.part = n_tokens * l.sum_pitch;
-                se.cols = cols;
-                se.rows = n_tokens;
+                se.cols = (int)cols;
+                se.rows = (int)n_tokens;
                 se.add = v0 > 0;
                 run_product<P>(Operand<P>{(const P *)(work + l.wt), cols, parts * l.piece, parts > 1 ? l.piece : 0},
                                Operand<P>{(const P *)(work + l.p), n_tokens, parts * l.piece, parts > 1 ? l.piece : 0},
@@ -653,9 +717,9 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             if (d_dw) {
                 OutEpilogue<T> oe;
                 oe.c = (T *)d_dw + v0 * dw_pitch;
-                oe.pitch = dw_pitch;
-                oe.cols = cols;
-                oe.rows = rows;
+                oe.pitch = (int)dw_pitch;
+                oe.cols = (int)cols;
+                oe.rows = (int)rows;
                 oe.scale = scale;
                 run_product<P>(Operand<P>{(const P *)(work + l.ht), cols, parts * l.nk, parts > 1 ? l.nk : 0},
                                Operand<P>{(const P *)(work + l.pt), rows, parts * l.nk, parts > 1 ? l.nk : 0},
