@@ -578,10 +578,9 @@ int32_t rotor_xent_workspace_bytes(int32_t type, int64_t n_tokens, int64_t cols,
     if (!bytes || !xent_sizes_ok(type, n_tokens, cols, n_rows))
         return ROTOR_EINVAL;
     const bool pack = type == ROTOR_F32 || !aligned;
-    *bytes = backward ? backward_layout(type, n_tokens, cols, n_rows, pack).total
-                      : forward_layout(type, n_tokens, cols, n_rows, pack).total;
-    if (*bytes < 16)
-        *bytes = 16;
+    *bytes = n_tokens == 0 ? 0
+             : backward    ? backward_layout(type, n_tokens, cols, n_rows, pack).total
+                           : forward_layout(type, n_tokens, cols, n_rows, pack).total;
     return ROTOR_OK;
 }
 

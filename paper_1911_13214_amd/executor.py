@@ -33,10 +33,18 @@ import numpy as np
 F_CK, F_NONE, F_ALL, B = 0, 1, 2, 3
 
 
+def _leaf(t):
+    """A leaf that shares ``t``'s storage; integers (token ids) have no
+    gradient."""
+    t = t.detach()
+    return t.requires_grad_() if t.is_floating_point() or t.is_complex() else t
+
+
 def run_sequence(stages, x, dy, ops):
     """Execute ``ops`` ((kind, stage) pairs, stages 1..L) on the chain for
     input ``x`` and output gradient ``dy``.  Returns the gradient with respect
-    to ``x``.  Raises ValueError if an operation's input is missing."""
+    to ``x`` (None for an ``x`` of integers).  Raises ValueError if an
+    operation's input is missing."""
     import torch
 
     L = len(stages)
@@ -64,7 +72,7 @@ def run_sequence(stages, x, dy, ops):
         else:
             raise ValueError(f"forward {l} without its input")
         if kind == F_ALL:
-            leaf = inp.detach().requires_grad_()
+            leaf = _leaf(inp)
             with torch.enable_grad():
                 abar[l] = (leaf, stages[l - 1](leaf))
         else:
@@ -116,7 +124,7 @@ def estimate(stages, x, repeats=3, batch_runs=4):
     for l, f in enumerate(stages):
         of = ob = wab = 0
         for _ in range(2):  # the second pass finds the parameter gradients allocated
-            leaf = inp.detach().requires_grad_()
+            leaf = _leaf(inp)
             _sync(dev)
             base = torch.cuda.memory_allocated(dev)
             torch.cuda.reset_peak_memory_stats(dev)
@@ -147,7 +155,7 @@ def estimate(stages, x, repeats=3, batch_runs=4):
         for _ in range(repeats):
             with torch.no_grad():
                 tf.append(device_us(lambda: [f(inp) for _ in range(batch_runs)]))
-            leaves = [inp.detach().requires_grad_() for _ in range(batch_runs)]
+            leaves = [_leaf(inp) for _ in range(batch_runs)]
             with torch.enable_grad():
                 outs = [f(q) for q in leaves]
             _sync(dev)
@@ -213,9 +221,11 @@ def synthetic_chain(L, seed, width=1024, device="cpu", dtype=None):
     return stages, dims
 
 
-def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repeats=3):
+def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repeats=3, chain="mlp", rows=32000):
     """The paper's check of the model (Sections 5.3-5.4) on a synthetic chain
-    on cuda:0: estimate the parameters, fill the table with the library at
+    on cuda:0 (``chain`` "mlp": synthetic_chain in 32 bits; "language": token
+    lookup, L - 2 residual blocks with dropout and the loss over ``rows``
+    tokens, stages.language_chain, in bf16): estimate the parameters, fill the table with the library at
     ``slots`` slots of the store-everything memory, rebuild the sequences of
     ``n_budgets`` equally spaced budgets in one call, run each, and compare
     the measured time and peak memory with what the model predicts for that
@@ -229,9 +239,21 @@ def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repe
 
     dev = torch.device("cuda:0")
     torch.manual_seed(seed)
-    stages, dims = synthetic_chain(L, seed, width=width, device=dev)
-    x = torch.randn(batch, dims[0], device=dev)
-    dy = torch.randn(batch, dims[-1], device=dev)
+    if chain == "language":
+        from . import stages as lm
+        if L < 2:
+            raise ValueError("a language chain has a lookup and a loss: L >= 2")
+        stages, dims = lm.language_chain(L - 2, seed, rows=rows, width=width, device=dev), [width] * (L + 1)
+        lm.set_step(stages, seed)
+        tokens = torch.randint(0, rows, (batch + 1,), device=dev)
+        x, stages[-1].targets = tokens[:-1].contiguous(), tokens[1:].contiguous()
+        dy = torch.ones((), device=dev)
+    elif chain == "mlp":
+        stages, dims = synthetic_chain(L, seed, width=width, device=dev)
+        x = torch.randn(batch, dims[0], device=dev)
+        dy = torch.randn(batch, dims[-1], device=dev)
+    else:
+        raise ValueError(f"unknown chain {chain!r}")
     # a few passes of the whole chain first, so that the estimate does not
     # time a GPU still raising its clocks (the first work of a process)
     for _ in range(3):
@@ -256,13 +278,13 @@ def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repe
             for q in f.parameters():
                 q.grad = None
         g = run_sequence(stages, x, dy, seq)
-        grads = [g] + [q.grad.clone() for f in stages for q in f.parameters()]
+        grads = ([] if g is None else [g]) + [q.grad.clone() for f in stages for q in f.parameters()]
         if ref is None:
             for f in stages:
                 for q in f.parameters():
                     q.grad = None
             g0 = run_sequence(stages, x, dy, store_all_sequence(L))
-            ref = [g0] + [q.grad.clone() for f in stages for q in f.parameters()]
+            ref = ([] if g0 is None else [g0]) + [q.grad.clone() for f in stages for q in f.parameters()]
         same = all(torch.equal(u, v) for u, v in zip(grads, ref))
         rows.append({"budget_slots": b, "budget_bytes": top * b // slots, "feasible": True, "ops": len(seq),
                      "recomputed_forwards": sum(1 for k, _ in seq if k != B) - L,
@@ -270,7 +292,7 @@ def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repe
                      "measured_bytes": m, "gradients_equal": same})
     ok = [r for r in rows if r["feasible"]]
     mape = lambda key_p, key_m: float(np.mean([abs(r[key_m] - r[key_p]) / r[key_m] for r in ok])) if ok else None
-    return {"chain": {"L": L, "seed": seed, "width": width, "batch": batch, "dims": dims},
+    return {"chain": {"kind": chain, "L": L, "seed": seed, "width": width, "batch": batch, "dims": dims},
             "store_all_bytes": top, "slots": slots, "rows": rows,
             "mape_time": mape("predicted_us", "measured_us"), "mape_memory": mape("predicted_bytes", "measured_bytes"),
             "all_gradients_equal": all(r["gradients_equal"] for r in ok)}
@@ -287,5 +309,7 @@ if __name__ == "__main__":
     ap.add_argument("--batch", type=int, default=4096)
     ap.add_argument("--slots", type=int, default=500)
     ap.add_argument("--budgets", type=int, default=10)
+    ap.add_argument("--chain", choices=("mlp", "language"), default="mlp")
+    ap.add_argument("--rows", type=int, default=32000, help="tokens of a language chain")
     a = ap.parse_args()
-    print(json.dumps(validate(a.L, a.seed, a.width, a.batch, a.slots, a.budgets)))
+    print(json.dumps(validate(a.L, a.seed, a.width, a.batch, a.slots, a.budgets, chain=a.chain, rows=a.rows)))

@@ -104,3 +104,26 @@ def residual_norm(x, z, post, post_weight, post_bias, gate, residual_scale, pre,
             b = b * gate.reshape(-1, x.shape[1]).repeat_interleave(x.shape[0] // (gate.numel() // x.shape[1]), 0)
         y = y + b
     return y, norm(pre, y, pre_weight, pre_bias, eps)[0] if pre != "none" else None
+
+
+# ---- cross entropy ---------------------------------------------------------------------
+
+def cross_entropy(h, w, targets, ignore):
+    """Loss and log-sum-exp of each token, NaN for targets outside w."""
+    logits = h.double() @ w.double().t()
+    lse = torch.logsumexp(logits, 1)
+    some = targets != ignore
+    bad = some & ((targets < 0) | (targets >= w.shape[0]))
+    at = torch.where(some & ~bad, targets, 0)
+    loss = torch.where(some, lse - logits.gather(1, at.unsqueeze(1)).squeeze(1), 0.0)
+    return torch.where(bad, float("nan"), loss), lse
+
+
+def cross_entropy_grad(h, w, targets, grad_loss, ignore):
+    """P, the gradient of the logits, by the formula: (softmax - target) times
+    each loss's gradient, 0 for tokens without a target; the sums of the
+    magnitudes follow from it."""
+    p = torch.softmax(h.double() @ w.double().t(), 1)
+    some = targets != ignore
+    p[some, targets[some]] -= 1.0
+    return p * torch.where(some, grad_loss.double(), 0.0).unsqueeze(1)

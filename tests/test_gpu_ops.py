@@ -462,3 +462,187 @@ def test_the_binding_refuses_mismatched_tensors():
         with pytest.raises(ValueError):
             call()
             print("not refused:", k)
+
+
+# ---- cross entropy ---------------------------------------------------------------------
+
+def xent_case(n, rows, cols, dtype, seed=0, scale=1.0, ignored=0.3):
+    g = torch.Generator().manual_seed(seed + n + rows + cols)
+    h = m.normal(g, n, cols, dtype=m.DTYPES[dtype])
+    w = m.normal(g, rows, cols, dtype=m.DTYPES[dtype], std=scale / cols ** 0.5)
+    t = torch.randint(0, rows, (n,), generator=g)
+    t[torch.rand(n, generator=g) < ignored] = -100
+    return h, w, t, m.normal(g, n, dtype=torch.float32)
+
+
+def check_xent(h, w, t, gl, ignore=-100):
+    """Bounds.  A logit is a sum of `cols` products: 32-bit sums of exact
+    products (three-term products of 32-bit tensors are within 2^-22 of each
+    product), so it is within s = (cols + 32) 2^-24 of the sum of its terms'
+    magnitudes A, plus 2^-22 A for 32-bit tensors.  lse and loss are within
+    that of the largest A plus the exponentials' and logarithm's few
+    roundings.  P is within its relative error (the logit's and lse's absolute
+    ones, and one rounding to 16 bits, or 2^-23) of |softmax| + |target|
+    times the gradient; dh and dw sum such terms in 32 bits."""
+    gh, gw, gt, ggl = (x.cuda() for x in (h, w, t, gl))
+    loss, lse = ops.linear_cross_entropy(gh, gw, gt, ignore)
+    ref_loss, ref_lse = m.cross_entropy(h, w, t, ignore)
+    n, cols = h.shape
+    rows = w.shape[0]
+    a = h.double().abs() @ w.double().abs().t()
+    s = ((cols + 32) * m.U32 + (2.0 ** -22 if h.dtype == torch.float32 else 0.0)) * a
+    top = s.max(1).values
+    slack = top + 32 * m.U32 * (1 + ref_lse.abs())
+    m.close(lse, ref_lse, slack, "lse")
+    m.close(loss, ref_loss, slack + top + 4 * m.U32 * a.max(1).values, "loss")
+    dh, dw = ops.linear_cross_entropy_backward(gh, gw, gt, lse, ggl, ignore)
+    p = m.cross_entropy_grad(h, w, t, gl, ignore)
+    soft = torch.softmax(h.double() @ w.double().t(), 1)
+    some = (t != ignore).double().unsqueeze(1)
+    size = gl.double().abs().unsqueeze(1) * some
+    unit = 2.0 ** -23 if h.dtype == torch.float32 else m.UNIT[h.dtype]
+    dp = size * soft * (2 * s + 2 * slack.unsqueeze(1) + 64 * m.U32) * 1.1 + p.abs() * (unit + 8 * m.U32)
+    if h.dtype == torch.float16:
+        # P is scaled to a largest gradient of 2^11 at least: half a
+        # subnormal's spacing below
+        dp = dp + size.max() * 2.0 ** -36 * some
+    pa = p.abs() + dp
+    aw, ah = w.double().abs(), h.double().abs()
+    three = 2.0 ** -22 if h.dtype == torch.float32 else 0.0
+    m.close(dh, p @ w.double(), dp @ aw + ((rows + 64) * m.U32 + three) * (pa @ aw), "dh")
+    m.close(dw, p.t() @ h.double(), dp.t() @ ah + ((n + 64) * m.U32 + three) * (pa.t() @ ah), "dw")
+    return loss, lse, dh, dw
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,cols", [(1, 1, 1), (1, 300, 64), (2, 3, 7), (5, 129, 8), (16, 1000, 40), (17, 255, 72),
+                                         (33, 257, 65), (64, 513, 128), (65, 700, 136), (127, 128, 200),
+                                         (130, 1025, 63), (257, 300, 264), (300, 2000, 512), (700, 600, 96)])
+def test_cross_entropy(dtype, n, rows, cols):
+    print("cross entropy", dtype, n, rows, cols, flush=True)
+    check_xent(*xent_case(n, rows, cols, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_cross_entropy_of_large_logits_and_certain_tokens(dtype):
+    # logits of up to about 40: some softmaxes are one target, others ties
+    h, w, t, gl = xent_case(96, 500, 64, dtype, scale=10.0)
+    w[7] = w[9]
+    check_xent(h, w, t, gl)
+    t[:] = (h.double() @ w.double().t()).argmax(1)
+    check_xent(h, w, t, gl)
+    check_xent(h * 0, w, t, gl)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_cross_entropy_without_targets(dtype):
+    h, w, t, gl = xent_case(70, 300, 72, dtype, ignored=1.0)
+    loss, _, dh, dw = check_xent(h, w, t, gl)
+    assert not loss.any() and not dh.any() and not dw.any()
+    # what such tokens hold does not matter, nor does the gradient of their loss
+    h, w, t, gl = xent_case(70, 300, 72, dtype, ignored=0.4)
+    some = t != -100
+    h2, gl2 = h.clone(), gl.clone()
+    bad = torch.nonzero(~some).squeeze(1)
+    h2[bad[::2]], h2[bad[1::2]], gl2[bad] = float("nan"), float("inf"), float("nan")
+    ref = check_xent(h, w, t, gl)
+    out = ops.linear_cross_entropy(h2.cuda(), w.cuda(), t.cuda())
+    assert torch.equal(out[0], ref[0])
+    g2 = ops.linear_cross_entropy_backward(h2.cuda(), w.cuda(), t.cuda(), out[1], gl2.cuda())
+    assert torch.equal(g2[0], ref[2]) and torch.equal(g2[1], ref[3])
+    # another value may stand for "no target", one of the rows among them
+    t3 = torch.where(some, t, 5)
+    ref3 = check_xent(h, w, t3, gl, ignore=5)
+    assert not ref3[0][(t3 == 5).cuda()].any()
+
+
+def test_cross_entropy_of_targets_outside_the_vocabulary_is_nan():
+    h, w, t, gl = xent_case(20, 50, 16, "f32", ignored=0.0)
+    t[3], t[8] = 50, -7
+    loss, lse = ops.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    assert loss.cpu().isnan().nonzero().squeeze(1).tolist() == [3, 8]
+    dh, dw = ops.linear_cross_entropy_backward(h.cuda(), w.cuda(), t.cuda(), lse, gl.cuda())
+    assert dh.cpu().isnan().all(1).nonzero().squeeze(1).tolist() == [3, 8] and dw.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_cross_entropy_of_strided_and_unaligned_rows(dtype):
+    for cols, off, pitch in [(64, 0, 72), (64, 1, 80), (56, 3, 61), (33, 0, 33)]:
+        print("cross entropy strides", dtype, cols, off, pitch, flush=True)
+        h, w, t, gl = xent_case(40, 290, cols, dtype, seed=off)
+        ref = check_xent(h, w, t, gl)
+        gh, gw = torch.zeros(40, pitch, dtype=h.dtype), torch.zeros(290, pitch, dtype=h.dtype)
+        gh[:, off:off + cols], gw[:, off:off + cols] = h, w
+        gh, gw = gh.cuda()[:, off:off + cols], gw.cuda()[:, off:off + cols]
+        loss, lse = ops.linear_cross_entropy(gh, gw, t.cuda())
+        dh, dw = ops.linear_cross_entropy_backward(gh, gw, t.cuda(), lse, gl.cuda())
+        for a, b in zip((loss, lse, dh, dw), ref):
+            assert torch.equal(a, b)
+        only = ops.linear_cross_entropy_backward(gh, gw, t.cuda(), lse, gl.cuda(), need_w=False)
+        assert only[1] is None and torch.equal(only[0], ref[2])
+        only = ops.linear_cross_entropy_backward(gh, gw, t.cuda(), lse, gl.cuda(), need_h=False)
+        assert only[0] is None and torch.equal(only[1], ref[3])
+
+
+def test_cross_entropy_leading_dimensions_and_no_tokens():
+    h, w, t, gl = xent_case(24, 100, 32, "bf16")
+    a = ops.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    b = ops.linear_cross_entropy(h.view(4, 6, 32).cuda(), w.cuda(), t.view(4, 6).cuda())
+    assert b[0].shape == (4, 6) and torch.equal(a[0], b[0].view(-1))
+    none = torch.zeros(0, dtype=torch.int64, device="cuda")
+    loss, lse = ops.linear_cross_entropy(h[:0].cuda(), w.cuda(), none)
+    dh, dw = ops.linear_cross_entropy_backward(h[:0].cuda(), w.cuda(), none, lse, loss)
+    assert loss.shape == (0,) and dh.shape == (0, 32) and torch.equal(dw, torch.zeros_like(w).cuda())
+
+
+def test_cross_entropy_gradient_against_differences():
+    # sum of c * loss along a random direction of h and w: central difference
+    # of the 32-bit losses (rounding 2^-24 of the sum's terms over the step),
+    # its curvature taken from the 64-bit model
+    h, w, t, c = xent_case(48, 333, 40, "f32")
+    g = torch.Generator().manual_seed(12)
+    vh, vw = m.normal(g, *h.shape, dtype=torch.float32), m.normal(g, *w.shape, dtype=torch.float32, std=0.1)
+    step = 2.0 ** -7
+
+    def value(e, f):
+        loss = f(h + e * vh, w + e * vw)
+        return float((c.double() * loss.cpu().double()).sum()), float((c.double() * loss.cpu().double()).abs().sum())
+
+    def kernel(h, w):
+        return ops.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())[0]
+
+    def model(h, w):
+        return m.cross_entropy(h, w, t, -100)[0]
+
+    lse = ops.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())[1]
+    dh, dw = (x.cpu().double() for x in ops.linear_cross_entropy_backward(h.cuda(), w.cuda(), t.cuda(), lse, c.cuda()))
+    analytic = float((dh * vh).sum() + (dw * vw).sum())
+    size = float((dh * vh).abs().sum() + (dw * vw).abs().sum())
+    (up, mag), (down, _) = value(step, kernel), value(-step, kernel)
+    exact = (value(step, model)[0] - value(-step, model)[0]) / (2 * step)
+    tiny = (value(step / 64, model)[0] - value(-step / 64, model)[0]) / (2 * step / 64)
+    numeric = (up - down) / (2 * step)
+    assert abs(numeric - analytic) <= 1.1 * abs(exact - tiny) + 256 * m.U32 * (mag / step + size)
+
+
+def test_the_cross_entropy_binding_refuses_mismatched_tensors():
+    h, w = torch.zeros(4, 8, device="cuda"), torch.zeros(5, 8, device="cuda")
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    x = torch.zeros(4, device="cuda")
+    f, b = ops.linear_cross_entropy, ops.linear_cross_entropy_backward
+    for call in (lambda: f(h, w[:, :4], t), lambda: f(h, w.half(), t), lambda: f(h, w, t.int()),
+                 lambda: f(h, w, t[:3]), lambda: f(h, w, t.cpu()), lambda: f(h.t(), w, t),
+                 lambda: b(h, w, t, x.half(), x), lambda: b(h, w, t, x, x[:3]), lambda: b(h, w, t, x, x.cpu())):
+        with pytest.raises(ValueError):
+            call()
+    assert b(h, w, t, x, x, need_h=False, need_w=False) == (None, None)
+
+
+@pytest.mark.parametrize("dtype,n,rows,cols", [("f32", 3, 700000, 8), ("bf16", 2, 2200000, 7), ("f16", 3, 1100000, 8)])
+def test_cross_entropy_over_pieces_of_the_vocabulary(dtype, n, rows, cols):
+    # few tokens and many rows: several pieces in the backward and, where
+    # operands are copied, in the forward
+    print("cross entropy pieces", dtype, n, rows, cols, flush=True)
+    h, w, t, gl = xent_case(n, rows, cols, dtype, ignored=0.0)
+    t[0], t[1] = rows - 1, 0
+    check_xent(h, w, t, gl)

@@ -103,3 +103,48 @@ def test_matrices_are_described_by_their_row_pitch():
     for bad in (x.t(), x[:, ::2], x.view(2, 3, 10)[:, :2], x[0].expand(6, 10), torch.zeros(()), torch.zeros(3, 0)):
         with pytest.raises(ValueError):
             ops._matrix(bad, "x")
+
+
+def test_cross_entropy_refuses_bad_arguments():
+    lib = rotor.lib()
+    need = ctypes.c_uint64()
+
+    def bytes_of(*a):
+        return lib.rotor_xent_workspace_bytes(*a, ctypes.byref(need))
+
+    for bad in [(5, 4, 8, 10, 1, 0), (1, -1, 8, 10, 1, 0), (1, (1 << 20) + 1, 8, 10, 1, 0), (1, 4, 0, 10, 1, 0),
+                (1, 4, 65537, 10, 1, 1), (1, 4, 8, 0, 1, 1), (1, 4, 8, 1 << 28, 1, 1)]:
+        assert bytes_of(*bad) == E, bad
+    assert lib.rotor_xent_workspace_bytes(1, 4, 8, 10, 1, 0, None) == E
+    assert bytes_of(1, 0, 8, 10, 1, 1) == rotor.ROTOR_OK and need.value == 0  # no tokens
+    assert bytes_of(1, 4, 8, 10, 1, 0) == rotor.ROTOR_OK
+    good = [1, 4, 8, 10, FAKE, 8, FAKE, 8, FAKE, -100, FAKE, FAKE, 1, FAKE, need.value, None]
+    for at, bad in [(0, 5), (1, -1), (2, 0), (3, 0), (4, None), (4, FAKE + 8), (5, 7), (5, 12), (6, None), (6, FAKE + 2),
+                    (7, 7), (7, (1 << 22) + 8), (8, None), (8, FAKE + 4), (10, None), (10, FAKE + 2), (11, None),
+                    (13, None), (13, FAKE + 8), (14, need.value - 1)]:
+        a = list(good)
+        a[at] = bad
+        assert lib.rotor_xent(*a) == E, (at, bad)
+    assert bytes_of(1, 4, 8, 10, 1, 1) == rotor.ROTOR_OK
+    good = [1, 4, 8, 10, FAKE, 8, FAKE, 8, FAKE, -100, FAKE, FAKE, FAKE, 8, FAKE, 8, 1, FAKE, need.value, None]
+    for at, bad in [(0, 5), (1, -1), (2, 0), (3, 0), (4, None), (5, 7), (5, 12), (6, FAKE + 8), (7, 7), (8, None),
+                    (10, None), (11, None), (12, FAKE + 1), (13, 7), (14, FAKE + 1), (15, 7), (15, (1 << 22) + 8),
+                    (17, None), (18, need.value - 1)]:
+        a = list(good)
+        a[at] = bad
+        assert lib.rotor_xent_backward(*a) == E, (at, bad)
+    a = list(good)
+    a[12] = a[14] = None  # no gradient wanted
+    assert lib.rotor_xent_backward(*a) == E
+    x = torch.zeros(2, 4)
+    with pytest.raises(ValueError, match="CUDA"):
+        ops.linear_cross_entropy(x, x, torch.zeros(2, dtype=torch.int64))
+
+
+def test_cross_entropy_workspace_does_not_grow_with_the_logits():
+    need = ctypes.c_uint64()
+    # 2^20 tokens of 262144 rows would be 512 GiB of 16-bit logits
+    for n, v in [(8192, 128000), (8192, 1 << 20), (65536, 262144), (1 << 20, 262144)]:
+        assert rotor.lib().rotor_xent_workspace_bytes(1, n, 1024, v, 1, 1, ctypes.byref(need)) == rotor.ROTOR_OK
+        piece = max(512 << 20, 4 * 256 * n)
+        assert need.value < piece * 2 + 16 * n * 1024, (n, v, need.value)

@@ -47,3 +47,16 @@ def test_norm_gradients_against_differences():
 
     args = [t.requires_grad_() for t in (x, z, *w, gate)]
     assert torch.autograd.gradcheck(f, args, eps=1e-6, atol=1e-7, rtol=1e-5)
+
+
+def test_cross_entropy_gradients_against_differences():
+    g = torch.Generator().manual_seed(3)
+    h, w = m.normal(g, 5, 4).requires_grad_(), m.normal(g, 7, 4).requires_grad_()
+    targets = torch.tensor([0, 6, -100, 3, 3])
+    assert torch.autograd.gradcheck(lambda h, w: m.cross_entropy(h, w, targets, -100)[0], (h, w), eps=1e-6, atol=1e-8,
+                                    rtol=1e-6)
+    gl = m.normal(g, 5)
+    dh, dw = torch.autograd.grad(m.cross_entropy(h, w, targets, -100)[0], (h, w), gl)
+    p = m.cross_entropy_grad(h.detach(), w.detach(), targets, gl, -100)
+    assert torch.allclose(p @ w.detach(), dh, rtol=1e-12, atol=1e-13)
+    assert torch.allclose(p.t() @ h.detach(), dw, rtol=1e-12, atol=1e-13)
