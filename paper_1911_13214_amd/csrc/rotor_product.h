@@ -138,6 +138,21 @@ template <typename T, int LOADS> struct Loader {
     }
 };
 
+
+// A barrier that waits only for what it names: a workgroup barrier of the
+// language would also wait for the loads that the next phases hide.
+enum { kWaitNone, kWaitLds, kWaitAll };
+template <int WAIT> __device__ inline void phase_barrier()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    if (WAIT == kWaitAll)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if (WAIT == kWaitLds)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else
+        asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 #endif
 
 template <typename T, typename S, typename E>
@@ -180,37 +195,85 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     const int row = lane % 16;
     const int swz[2] = {((lane / 16) ^ (row & 7)) * 16, ((4 + lane / 16) ^ (row & 7)) * 16};
     const int base_a = (wi * S::NI * 16 + row) * kRowBytes, base_b = (S::BI + wj * S::NJ * 16 + row) * kRowBytes;
-    auto multiply = [&](const char *lds) {
+    Frag fa[S::NI], fb[S::NJ];
+    auto read = [&](const char *lds, int h) {  // half h of a step: 32 of k
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Frag fa[S::NI], fb[S::NJ];
+        for (int jj = 0; jj < S::NJ; ++jj)
+            fb[jj] = *(const Frag *)(lds + base_b + swz[h] + jj * 16 * kRowBytes);
+#pragma unroll
+        for (int ii = 0; ii < S::NI; ++ii)
+            fa[ii] = *(const Frag *)(lds + base_a + swz[h] + ii * 16 * kRowBytes);
+    };
+    auto multiply = [&]() {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
             for (int jj = 0; jj < S::NJ; ++jj)
-                fb[jj] = *(const Frag *)(lds + base_b + swz[h] + jj * 16 * kRowBytes);
-#pragma unroll
-            for (int ii = 0; ii < S::NI; ++ii)
-                fa[ii] = *(const Frag *)(lds + base_a + swz[h] + ii * 16 * kRowBytes);
-#pragma unroll
-            for (int ii = 0; ii < S::NI; ++ii)
-#pragma unroll
-                for (int jj = 0; jj < S::NJ; ++jj)
-                    res.acc[ii][jj] = Mfma<T>::run(fa[ii], fb[jj], res.acc[ii][jj]);
-        }
+                res.acc[ii][jj] = Mfma<T>::run(fa[ii], fb[jj], res.acc[ii][jj]);
+        __builtin_amdgcn_s_setprio(0);
     };
 
     // an odd number of steps is followed by one of zeros: one way out of the
     // loop, so that the sums stay where they are
-    if (t0 < t1)
-        load(even, true);
-    __syncthreads();
-    for (int t = t0; t < t1; t += 2) {
-        load(odd, t + 1 < t1);
-        multiply(even);
-        __syncthreads();
-        if (t + 2 < t1)
+    if constexpr (S::kWaves == 8) {
+        // Two groups of four waves, one on each SIMD, half a phase apart:
+        // while one multiplies what it holds (32 of k), the other reads its
+        // next operands from LDS.  Every phase has two barriers; the second
+        // group starts one barrier later and ends one earlier.  A step's
+        // place in LDS is written again one barrier after the other group's
+        // last read of it, and the loads into it are waited for three phases
+        // later, one barrier before its first read.
+        const bool late = wave >= 4;
+        auto phase = [&](const char *lds, int h, char *next, bool live) {
+            read(lds, h);
+            __builtin_amdgcn_sched_barrier(0);
+            if (next)
+                load(next, live);
+            if (h == 1 && late)
+                phase_barrier<kWaitAll>();
+            else
+                phase_barrier<kWaitLds>();
+            multiply();
+            if (h == 1 && !late)
+                phase_barrier<kWaitAll>();
+            else
+                phase_barrier<kWaitNone>();
+        };
+        if (t0 < t1)
             load(even, true);
-        multiply(odd);
+        phase_barrier<kWaitAll>();
+        if (late)
+            phase_barrier<kWaitNone>();
+        for (int t = t0; t < t1; t += 2) {
+            phase(even, 0, odd, t + 1 < t1);
+            phase(even, 1, nullptr, false);
+            phase(odd, 0, even, t + 2 < t1);
+            phase(odd, 1, nullptr, false);
+        }
+        if (!late)
+            phase_barrier<kWaitNone>();
         __syncthreads();
+    } else {
+        if (t0 < t1)
+            load(even, true);
+        __syncthreads();
+        auto step = [&](const char *lds) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                read(lds, h);
+                multiply();
+            }
+        };
+        for (int t = t0; t < t1; t += 2) {
+            load(odd, t + 1 < t1);
+            step(even);
+            __syncthreads();
+            if (t + 2 < t1)
+                load(even, true);
+            step(odd);
+            __syncthreads();
+        }
     }
     res.tile_i = ti;
     res.tile_j = tj;
