@@ -2,10 +2,10 @@
 // by sorted tokens.
 //
 // Backward: a stable radix sort of (token, position), one launch per digit of
-// up to 9 bits; then one launch in which groups of lanes take 32 sorted
+// up to 9 bits, whose few workgroups share the device with others that clear
+// the gradient; then one launch in which groups of lanes take 32 sorted
 // positions each, add the rows of one token in registers and write each token
-// that lies within their positions, while the remaining workgroups clear the
-// rows of tokens that do not occur; then one launch that joins the tokens
+// that lies within their positions; then one launch that joins the tokens
 // that cross the 32-position cuts.  No atomics on the sums: their order
 // depends on the tokens alone.
 #include "rotor_ops.h"
@@ -51,14 +51,26 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const void *tokens, in
     const T *src = table + (in ? t : 0) * pitch;
     T *dst = y + i * y_pitch;
     const int64_t pieces = (cols + V - 1) / V;
-    for (int64_t k = threadIdx.x % 64 + 64 * blockIdx.y; k < pieces; k += 64 * gridDim.y) {
-        const int64_t c = column<V>(k, cols);
-        float v[V];
-        load_vec(src + c, v);
+    constexpr int kAhead = 4;  // loads in flight
+    for (int64_t k0 = threadIdx.x % 64 + 64 * blockIdx.y; k0 < pieces; k0 += 64 * kAhead * gridDim.y) {
+        float v[kAhead][V];
+        int64_t c[kAhead];
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            v[j] = in ? v[j] * scale : __builtin_nanf("");
-        store_vec(dst + c, v);
+        for (int q = 0; q < kAhead; ++q) {
+            // past the end the first piece again, which is not written twice
+            const int64_t k = k0 + q * 64 * gridDim.y;
+            c[q] = column<V>(k < pieces ? k : k0, cols);
+            load_vec(src + c[q], v[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            if (q > 0 && k0 + q * 64 * gridDim.y >= pieces)
+                break;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                v[q][j] = in ? v[q][j] * scale : __builtin_nanf("");
+            store_vec(dst + c[q], v[q]);
+        }
     }
 }
 
@@ -78,11 +90,28 @@ struct SortArgs {
     uint32_t *key_out, *pos_out;
     int32_t *count;  // keys that are sorted: written by the first pass, read by the others
     int shift, bits;
+    uint32_t parts;  // workgroups that sort; the others clear rows [clear_from, clear_to) of out
+    int64_t clear_from, clear_to, cols, out_pitch;
 };
+
+// A workgroup's share of the rows to clear.
+template <typename T, int V> __device__ void clear_rows(T *out, const SortArgs &a)
+{
+    const int64_t blocks = gridDim.x - a.parts, rows = a.clear_to - a.clear_from;
+    const int64_t pieces = (a.cols + V - 1) / V;
+    const float zero[V] = {};
+    // whole waves take rows, adjacent waves adjacent ones
+    const int64_t wave = (int64_t)(blockIdx.x - a.parts) * kSortWaves + threadIdx.x / 64;
+    for (int64_t r = wave; r < rows; r += blocks * kSortWaves) {
+        T *dst = out + (a.clear_from + r) * a.out_pitch;
+        for (int64_t k = threadIdx.x % 64; k < pieces; k += 64)
+            store_vec(dst + column<V>(k, a.cols), zero);
+    }
+}
 
 template <bool FIRST> __device__ inline bool sort_key(const SortArgs &a, int64_t i, uint32_t &key)
 {
-    if (FIRST) {
+    if constexpr (FIRST) {
         const int64_t t = token_at(a.tokens, a.token_bytes, i);
         key = (uint32_t)t;
         return t >= 0 && t < a.rows && t != a.padding;
@@ -98,18 +127,27 @@ __device__ inline void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs a)
+template <typename T, int V, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs a, T *out)
 {
-    __shared__ uint32_t before[kDigits], from[kDigits];
+    // eight counters a digit, by lane: tokens repeat, and lanes that count at
+    // one address wait for each other
+    constexpr int kCopies = 8;
+    __shared__ uint32_t before[kDigits][kCopies], from[kDigits][kCopies];
     __shared__ uint32_t at[kSortWaves][kDigits];
     __shared__ uint32_t wave_total[kSortWaves];
+    if (blockIdx.x >= a.parts) {
+        clear_rows<T, V>(out, a);
+        return;
+    }
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const uint32_t mask = (1u << a.bits) - 1;
     const int64_t n = FIRST ? a.n : (int64_t)*a.count;
     const int64_t part = (int64_t)blockIdx.x * kPart;
     for (int d = tid; d < kDigits; d += kSortThreads) {
-        before[d] = 0;
-        from[d] = 0;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c)
+            before[d][c] = from[d][c] = 0;
         for (int w = 0; w < kSortWaves; ++w)
             at[w][d] = 0;
     }
@@ -117,23 +155,52 @@ template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void sort_kerne
     if (part >= n && !(FIRST && blockIdx.x == 0))
         return;  // the whole workgroup
     // digits of the keys before the part, and of the rest
-    for (int64_t i = tid; i < n; i += kSortThreads) {
-        uint32_t key;
-        if (sort_key<FIRST>(a, i, key))
-            atomicAdd(&(i < part ? before : from)[key >> a.shift & mask], 1u);
+    // (loads in batches: one at a time would take its latency for each)
+    constexpr int kAhead = 8;
+    for (int64_t i0 = tid; i0 < n; i0 += kSortThreads * kAhead) {
+        uint32_t key[kAhead];
+        bool have[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int64_t i = i0 + q * kSortThreads;
+            have[q] = sort_key<FIRST>(a, i < n ? i : i0, key[q]) && i < n;
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            if (have[q])
+                atomicAdd(&(i0 + q * kSortThreads < part ? before : from)[key[q] >> a.shift & mask][lane % kCopies],
+                          1u);
     }
-    // digits of each wave's own keys: kPart / kSortWaves adjacent ones
-    constexpr int kOwn = kPart / kSortWaves;
-    const int64_t own = part + (int64_t)wave * kOwn;
-    for (int k = lane; k < kOwn; k += 64) {
-        uint32_t key;
-        if (own + k < n && sort_key<FIRST>(a, own + k, key))
-            atomicAdd(&at[wave][key >> a.shift & mask], 1u);
+    // each wave's own keys, kPart / kSortWaves adjacent ones, and their digits
+    constexpr int kOwn = kPart / kSortWaves / 64;
+    const int64_t own = part + (int64_t)wave * kOwn * 64 + lane;
+    uint32_t key[kOwn], pos[kOwn];
+    bool have[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        const int64_t i = own + k * 64;
+        have[k] = i < n;
+        key[k] = pos[k] = 0;
+        if (have[k]) {
+            have[k] = sort_key<FIRST>(a, i, key[k]);
+            pos[k] = FIRST ? (uint32_t)i : a.pos_in[i];
+        }
     }
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+        if (have[k])
+            atomicAdd(&at[wave][key[k] >> a.shift & mask], 1u);
     __syncthreads();
     // first place of each digit (threads 0..511, one digit each), then of
     // each wave's first key of that digit
-    const uint32_t all = tid < kDigits ? before[tid] + from[tid] : 0;
+    uint32_t all = 0, earlier = 0;
+    if (tid < kDigits)
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+            earlier += before[tid][c];
+            all += from[tid][c];
+        }
+    all += earlier;
     uint32_t upto = all;
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) {
@@ -148,7 +215,7 @@ template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void sort_kerne
         uint32_t base = upto - all;
         for (int w = 0; w < wave; ++w)
             base += wave_total[w];
-        base += before[tid];
+        base += earlier;
         for (int w = 0; w < kSortWaves; ++w) {
             const uint32_t c = at[w][tid];
             at[w][tid] = base;
@@ -164,24 +231,21 @@ template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void sort_kerne
     __syncthreads();
     // 64 keys at a time, in order: a key's place is its digit's next one plus
     // the lanes before it that hold the same digit
-    for (int k = 0; k < kOwn; k += 64) {
-        const int64_t i = own + k + lane;
-        uint32_t key = 0;
-        const bool have = i < n && sort_key<FIRST>(a, i, key);
-        const uint32_t d = key >> a.shift & mask;
-        uint64_t same = __ballot(have);
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        const uint32_t d = key[k] >> a.shift & mask;
+        uint64_t same = __ballot(have[k]);
         for (int b = 0; b < a.bits; ++b) {
-            const uint64_t set = __ballot(have && (d >> b & 1));
+            const uint64_t set = __ballot(have[k] && (d >> b & 1));
             same &= d >> b & 1 ? set : ~set;
         }
-        if (have) {
-            const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
-            const uint32_t place = at[wave][d] + rank;
-            a.key_out[place] = key;
-            a.pos_out[place] = FIRST ? (uint32_t)i : a.pos_in[i];
+        if (have[k]) {
+            const uint32_t place = at[wave][d] + __popcll(same & ((1ull << lane) - 1));
+            a.key_out[place] = key[k];
+            a.pos_out[place] = pos[k];
         }
         wave_sync();
-        if (have && (same >> lane) == 1)  // the last lane of its digit
+        if (have[k] && (same >> lane) == 1)  // the last lane of its digit
             at[wave][d] += __popcll(same);
         wave_sync();
     }
@@ -190,7 +254,7 @@ template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void sort_kerne
 // ---- sums -----------------------------------------------------------------------
 
 struct SumArgs {
-    int64_t rows, cols, dy_pitch, out_pitch;
+    int64_t cols, dy_pitch, out_pitch;
     const uint32_t *key, *pos;
     const int32_t *count;
     float *part;        // [chunks][2][part_pitch]: sums of the token that enters, and of the one that leaves
@@ -198,43 +262,11 @@ struct SumArgs {
     float scale;
     int lanes;          // lanes of a group: a power of two, 64 at least
     uint32_t slices;    // workgroups side by side over a row's columns
-    uint32_t sum_blocks;  // the rest of the grid clears rows
 };
-
-// 64 rows a wave: a lane looks for its row's token, then the wave clears the
-// rows of those that do not occur.
-template <typename T, int V> __device__ void clear_rows(T *out, const SumArgs &a, int64_t n, int64_t r0)
-{
-    const int lane = threadIdx.x % 64;
-    const int64_t r = r0 + lane;
-    int64_t lo = 0, hi = r < a.rows ? n : 0;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (a.key[mid] < (uint32_t)r)
-            lo = mid + 1;
-        else
-            hi = mid;
-    }
-    uint64_t absent = __ballot(r < a.rows && !(lo < n && a.key[lo] == (uint32_t)r));
-    const int64_t pieces = (a.cols + V - 1) / V;
-    const float zero[V] = {};
-    while (absent) {
-        const int k = __builtin_ctzll(absent);
-        absent &= absent - 1;
-        T *dst = out + (r0 + k) * a.out_pitch;
-        for (int64_t q = lane; q < pieces; q += 64)
-            store_vec(dst + column<V>(q, a.cols), zero);
-    }
-}
 
 template <typename T, int V> __global__ __launch_bounds__(kThreads) void sum_kernel(const T *dy, T *out, SumArgs a)
 {
     const int64_t n = *a.count;
-    if (blockIdx.x >= a.sum_blocks) {
-        clear_rows<T, V>(out, a, n,
-                         ((int64_t)(blockIdx.x - a.sum_blocks) * (kThreads / 64) + threadIdx.x / 64) * 64);
-        return;
-    }
     const int64_t chunk = (int64_t)(blockIdx.x / a.slices) * (kThreads / a.lanes) + threadIdx.x / a.lanes;
     const int64_t begin = chunk * kChunk;
     if (begin >= n)
@@ -304,17 +336,14 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void join_ke
     const int64_t begin = chunk * kChunk;
     if (begin > 0 && a.key[begin - 1] == key)
         return;  // it started before (sorted: the chunk holds nothing else)
-    // one past the token's last position
-    int64_t lo = end + 1, hi = n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (a.key[mid] > key)
-            hi = mid;
-        else
-            lo = mid + 1;
-    }
-    const int64_t last = (lo - 1) / kChunk;  // last chunk it enters
+    // the last chunk it enters, 64 chunks a look
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    int64_t last = chunk;
+    for (uint64_t all = ~0ull; all == ~0ull;) {
+        const int64_t first = (last + 1 + lane) * kChunk;
+        all = __ballot(first < n && a.key[first] == key);
+        last += all == ~0ull ? 64 : __builtin_ctzll(~all);
+    }
     const int64_t piece = (int64_t)blockIdx.y * 64 + lane;
     const bool have = piece * V < a.cols;
     const int64_t c = have ? column<V>(piece, a.cols) : 0;
@@ -453,20 +482,10 @@ int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows,
     a.padding = padding;
     a.count = (int32_t *)(w + l.count);
     a.bits = width;
-    const dim3 parts((uint32_t)(n_tokens > 0 ? ceil_div(n_tokens, kPart) : 1));
-    for (int p = 0; p < passes; ++p) {
-        a.key_in = (const uint32_t *)(w + l.key[(p + 1) % 2]);
-        a.pos_in = (const uint32_t *)(w + l.pos[(p + 1) % 2]);
-        a.key_out = (uint32_t *)(w + l.key[p % 2]);
-        a.pos_out = (uint32_t *)(w + l.pos[p % 2]);
-        a.shift = p * width;
-        if (p == 0)
-            sort_kernel<true><<<parts, kSortThreads, 0, s>>>(a);
-        else
-            sort_kernel<false><<<parts, kSortThreads, 0, s>>>(a);
-    }
+    a.parts = (uint32_t)(n_tokens > 0 ? ceil_div(n_tokens, kPart) : 1);
+    a.cols = cols;
+    a.out_pitch = dtable_pitch;
     SumArgs b;
-    b.rows = n_rows;
     b.cols = cols;
     b.dy_pitch = dy_pitch;
     b.out_pitch = dtable_pitch;
@@ -480,20 +499,35 @@ int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows,
     while (b.lanes < kThreads && b.lanes * kVec < cols)
         b.lanes *= 2;
     const int64_t chunks = ceil_div(n_tokens, kChunk);
-    const int64_t clear = ceil_div(n_rows, kThreads);
     b.slices = (uint32_t)ceil_div(cols, (int64_t)b.lanes * kVec);
     const int64_t sum_blocks = ceil_div(chunks, kThreads / b.lanes) * b.slices;
     const int64_t join_slices = ceil_div(cols, 64 * kVec);
-    if (join_slices > 65535 || sum_blocks + clear > 0x7FFFFFFF)
+    if (join_slices > 65535 || sum_blocks > 0x7FFFFFFF)
         return ROTOR_EINVAL;
-    b.sum_blocks = (uint32_t)sum_blocks;
     with_type(type, [&](auto e) {
         typedef typename decltype(e)::T T;
+        T *const out = (T *)d_dtable;
+        for (int p = 0; p < passes; ++p) {
+            a.key_in = (const uint32_t *)(w + l.key[(p + 1) % 2]);
+            a.pos_in = (const uint32_t *)(w + l.pos[(p + 1) % 2]);
+            a.key_out = (uint32_t *)(w + l.key[p % 2]);
+            a.pos_out = (uint32_t *)(w + l.pos[p % 2]);
+            a.shift = p * width;
+            a.clear_from = n_rows * p / passes;
+            a.clear_to = n_rows * (p + 1) / passes;
+            // a row a wave, up to four workgroups on every CU
+            const int64_t clear = ceil_div(a.clear_to - a.clear_from, kSortWaves);
+            const dim3 grid(a.parts + (uint32_t)(clear < 1024 ? clear : 1024));
+            const auto sort = cols >= kVec ? (p == 0 ? sort_kernel<T, kVec, true> : sort_kernel<T, kVec, false>)
+                                           : (p == 0 ? sort_kernel<T, 1, true> : sort_kernel<T, 1, false>);
+            sort<<<grid, kSortThreads, 0, s>>>(a, out);
+        }
         const auto sum = cols >= kVec ? sum_kernel<T, kVec> : sum_kernel<T, 1>;
         const auto join = cols >= kVec ? join_kernel<T, kVec> : join_kernel<T, 1>;
-        sum<<<dim3((uint32_t)(sum_blocks + clear)), kThreads, 0, s>>>((const T *)d_dy, (T *)d_dtable, b);
+        if (chunks > 0)
+            sum<<<dim3((uint32_t)sum_blocks), kThreads, 0, s>>>((const T *)d_dy, out, b);
         if (chunks > 1)
-            join<<<dim3((uint32_t)(chunks - 1), (uint32_t)join_slices), kThreads, 0, s>>>((T *)d_dtable, b);
+            join<<<dim3((uint32_t)(chunks - 1), (uint32_t)join_slices), kThreads, 0, s>>>(out, b);
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
 }

@@ -1,8 +1,8 @@
 // rotor_residual_norm: y = a x + gate * post(z), h = pre(y), and the
 // gradients of all it takes.
 //
-// A row is held in the registers of its threads (64 to 1024 of them, 8 or 16
-// elements each), so each tensor is read once and written once in either
+// A row is held in the registers of its threads (64 to 1024 of them, 8
+// elements each, 16 past 4096 columns), so each tensor is read once and written once in either
 // direction.  Backward, a workgroup walks a strip of rows and keeps the sums
 // over rows (weights, biases, gate) in registers; the strips' sums are added
 // by a second launch.
@@ -24,9 +24,10 @@ struct NormArgs {
     float *stats;
 };
 
-// The threads of one row: TH of them, RP rows side by side in a workgroup.
+// The threads of one row: TH of them; rows of one wave four side by side in a
+// workgroup.
 template <int TH> struct Team {
-    static constexpr int kRows = TH >= 256 ? 1 : 256 / TH;
+    static constexpr int kRows = TH > 64 ? 1 : 4;
     static constexpr int kBlock = TH * kRows;
 };
 
@@ -79,7 +80,6 @@ template <int TH, int V, int N> struct Pieces {
 };
 
 template <typename T, int V, int N> struct Row {
-    typedef typename VecOf<T, V>::V Vec;
     float f[N][V];
     template <typename P> __device__ void load(const P &p, const T *src)
     {
@@ -101,7 +101,7 @@ template <typename T, int V, int N> struct Row {
     }
 };
 
-// A parameter row ([cols], storage type), or a constant where there is none.
+// A row as it is stored, or a constant where there is none (src is NULL).
 template <typename T, int V, int N> struct Param {
     typedef typename VecOf<T, V>::V Vec;
     Vec v[N];
@@ -263,6 +263,16 @@ __global__ __launch_bounds__(Team<TH>::kBlock) void back_kernel(const T *dy, con
     b1.load(p, (const T *)a.post_b, 0.f);
     w2.load(p, (const T *)a.pre_w, 1.f);
     float s_post_w[N][V] = {}, s_post_b[N][V] = {}, s_pre_w[N][V] = {}, s_pre_b[N][V] = {}, s_gate[N][V] = {};
+    // a row is loaded, as it is stored, while the one before is worked on
+    Param<T, V, N> next_d, next_u, next_q, next_v;
+    float4 next_st;
+    auto fetch = [&](int64_t r) {
+        next_d.load(p, dh ? dh + r * a.dh_pitch : nullptr, 0.f);
+        next_u.load(p, dh ? y + r * a.y_pitch : nullptr, 0.f);
+        next_q.load(p, dy ? dy + r * a.dy_pitch : nullptr, 0.f);
+        next_v.load(p, z ? z + r * a.z_pitch : nullptr, 0.f);
+        next_st = *(const float4 *)(a.stats + 4 * r);
+    };
     const int64_t s0 = (int64_t)blockIdx.x * a.plan.per_block;
     const int64_t s1 = s0 + a.plan.per_block < a.plan.strips ? s0 + a.plan.per_block : a.plan.strips;
     for (int64_t s = s0; s < s1; ++s) {
@@ -271,20 +281,21 @@ __global__ __launch_bounds__(Team<TH>::kBlock) void back_kernel(const T *dy, con
         const int64_t r0 = group * a.plan.group + in_group;
         const int64_t n = in_group + a.plan.strip < a.plan.group ? a.plan.strip : a.plan.group - in_group;
         g.load(p, a.gate ? (const T *)a.gate + group * a.gate_pitch : nullptr, 1.f);
+        if (row < n)
+            fetch(r0 + row);
         for (int64_t i = row; i < n; i += R) {
             const int64_t r = r0 + i;
             Row<T, V, N> d, u, q, v;
-            if (dh) {
-                d.load(p, dh + r * a.dh_pitch);
-                u.load(p, y + r * a.y_pitch);
+            FOR_ELEMENTS
+            {
+                d.f[k][j] = next_d.at(k, j);
+                u.f[k][j] = next_u.at(k, j);
+                q.f[k][j] = next_q.at(k, j);
+                v.f[k][j] = next_v.at(k, j);
             }
-            if (dy)
-                q.load(p, dy + r * a.dy_pitch);
-            if (z)
-                v.load(p, z + r * a.z_pitch);
-            const float4 st = *(const float4 *)(a.stats + 4 * r);
-            if (!dy)
-                FOR_ELEMENTS q.f[k][j] = 0.f;
+            const float4 st = next_st;
+            if (i + R < n)
+                fetch(r + R);
             if (dh) {
                 float c1 = 0.f, c2 = 0.f;
                 FOR_ELEMENTS
@@ -353,8 +364,8 @@ __global__ __launch_bounds__(Team<TH>::kBlock) void back_kernel(const T *dy, con
         put_sums<TH, V, N>(s_pre_b, p, a.part[kPreB] + at, sums_buf);
 }
 
-// Adds the strips' sums: 64 columns of one output row a workgroup, its four
-// waves a quarter of the strips each, the quarters then in order.
+// Adds the strips' sums: 64 columns of one output row a workgroup, its 16
+// waves a part of the strips each, the parts then in order.
 struct AddArgs {
     const float *part[kSums];
     void *out[kSums];
@@ -364,16 +375,17 @@ struct AddArgs {
     int64_t cols;
 };
 
-template <typename T> __global__ __launch_bounds__(256) void add_kernel(AddArgs a)
+constexpr int kAddWaves = 16;
+template <typename T> __global__ __launch_bounds__(kAddWaves * 64) void add_kernel(AddArgs a)
 {
-    __shared__ float other[3][64];
+    __shared__ float other[kAddWaves - 1][64];
     int task = 0;
     while (task + 1 < kSums && (int64_t)blockIdx.y >= a.first[task + 1])
         ++task;
     const int64_t out_row = (int64_t)blockIdx.y - a.first[task];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    const int64_t n = a.count[task], each = (n + 3) / 4;
+    const int64_t n = a.count[task], each = (n + kAddWaves - 1) / kAddWaves;
     const int64_t from = wave * each, to = from + each < n ? from + each : n;
     float s = 0.f;
     if (c < a.cols) {
@@ -387,21 +399,41 @@ template <typename T> __global__ __launch_bounds__(256) void add_kernel(AddArgs 
     __syncthreads();
     if (wave > 0 || c >= a.cols)
         return;
-    s += other[0][lane];
-    s += other[1][lane];
-    s += other[2][lane];
+#pragma unroll
+    for (int w = 0; w < kAddWaves - 1; ++w)
+        s += other[w][lane];
     ((T *)a.out[task])[out_row * a.out_pitch[task] + c] = (T)s;
 }
 
-// Strips for about `kBlocks` workgroups: two on every one of the 256 CUs.
-constexpr int64_t kBlocks = 512;
-
-StripPlan strip_plan(int64_t rows, int64_t gate_rows)
+// Calls f(team, V, N) with the smallest shape that holds a row.
+template <int V> struct IntV { static constexpr int v = V; };
+template <typename F> void with_shape(int64_t cols, F f)
 {
+    if (cols < kVec)
+        f(IntV<64>{}, IntV<1>{}, IntV<1>{});
+    else if (cols <= 64 * 8)
+        f(IntV<64>{}, IntV<8>{}, IntV<1>{});
+    else if (cols <= 128 * 8)
+        f(IntV<128>{}, IntV<8>{}, IntV<1>{});
+    else if (cols <= 256 * 8)
+        f(IntV<256>{}, IntV<8>{}, IntV<1>{});
+    else if (cols <= 512 * 8)
+        f(IntV<512>{}, IntV<8>{}, IntV<1>{});
+    else if (cols <= 512 * 16)
+        f(IntV<512>{}, IntV<8>{}, IntV<2>{});
+    else
+        f(IntV<1024>{}, IntV<8>{}, IntV<2>{});
+}
+
+// Strips for as many workgroups as the 256 CUs hold at once: 8 waves each.
+StripPlan strip_plan(int64_t rows, int64_t cols, int64_t gate_rows)
+{
+    int64_t blocks_at_once = 0;
+    with_shape(cols, [&](auto th, auto, auto) { blocks_at_once = 256 * 8 * 64 / Team<decltype(th)::v>::kBlock; });
     StripPlan s;
     s.groups = gate_rows > 0 ? gate_rows : 1;
     s.group = rows / s.groups;
-    int64_t per = kBlocks / s.groups;
+    int64_t per = blocks_at_once / s.groups;
     if (per < 1)
         per = 1;
     s.strip = ceil_div(s.group, per);
@@ -409,7 +441,7 @@ StripPlan strip_plan(int64_t rows, int64_t gate_rows)
         s.strip = 1;
     s.per_group = s.group > 0 ? ceil_div(s.group, s.strip) : 1;  // no rows: one empty strip
     s.strips = s.groups * s.per_group;
-    s.per_block = ceil_div(s.strips, kBlocks);
+    s.per_block = ceil_div(s.strips, blocks_at_once);
     s.blocks = ceil_div(s.strips, s.per_block);
     return s;
 }
@@ -432,26 +464,6 @@ bool norm_params_ok(const rotor_norm *n)
         (n->pre == ROTOR_NORM_NONE && (n->pre_weight || n->pre_bias)))
         return false;
     return n->gate_rows > 0 ? matrix_ok(n->gate, n->gate_rows, n->cols, n->gate_pitch, es) : !n->gate;
-}
-
-// Calls f(team, V, N) with the smallest shape that holds a row.
-template <int V> struct IntV { static constexpr int v = V; };
-template <typename F> void with_shape(int64_t cols, F f)
-{
-    if (cols < kVec)
-        f(IntV<64>{}, IntV<1>{}, IntV<1>{});
-    else if (cols <= 64 * 8)
-        f(IntV<64>{}, IntV<8>{}, IntV<1>{});
-    else if (cols <= 64 * 16)
-        f(IntV<64>{}, IntV<8>{}, IntV<2>{});
-    else if (cols <= 256 * 8)
-        f(IntV<256>{}, IntV<8>{}, IntV<1>{});
-    else if (cols <= 256 * 16)
-        f(IntV<256>{}, IntV<8>{}, IntV<2>{});
-    else if (cols <= 512 * 16)
-        f(IntV<512>{}, IntV<8>{}, IntV<2>{});
-    else
-        f(IntV<1024>{}, IntV<8>{}, IntV<2>{});
 }
 
 }  // namespace
@@ -515,7 +527,7 @@ int32_t rotor_residual_norm_workspace_bytes(const rotor_norm *how, uint64_t *byt
 {
     if (!bytes || !norm_sizes_ok(how))
         return ROTOR_EINVAL;
-    const StripPlan s = strip_plan(how->rows, how->gate_rows);
+    const StripPlan s = strip_plan(how->rows, how->cols, how->gate_rows);
     *bytes = 4ull * (uint64_t)how->cols * (uint64_t)((kSums - 1) * s.blocks + (s.per_group > 1 ? s.strips : 0));
     if (*bytes < 16)
         *bytes = 16;
@@ -547,7 +559,7 @@ int32_t rotor_residual_norm_backward(const rotor_norm *how, const void *d_dy, in
     for (const void *q : {grads->post_weight, grads->post_bias, grads->gate, grads->pre_weight, grads->pre_bias})
         if ((uintptr_t)q % (uintptr_t)es)
             return ROTOR_EINVAL;
-    const StripPlan plan = strip_plan(rows, how->gate_rows);
+    const StripPlan plan = strip_plan(rows, cols, how->gate_rows);
     void *const out[kSums] = {grads->post_weight, grads->post_bias, grads->pre_weight, grads->pre_bias, grads->gate};
     const bool gate_here = grads->gate && plan.per_group == 1;
     BackArgs a;
@@ -604,7 +616,8 @@ int32_t rotor_residual_norm_backward(const rotor_norm *how, const void *d_dy, in
                     (const T *)d_dy, (const T *)d_dh, (const T *)d_y, (const T *)d_z, (T *)d_dx, (T *)d_dz, a);
         });
         if (last >= 0)
-            add_kernel<T><<<dim3((uint32_t)ceil_div(cols, 64), (uint32_t)tasks), 256, 0, (hipStream_t)stream>>>(add);
+            add_kernel<T><<<dim3((uint32_t)ceil_div(cols, 64), (uint32_t)tasks), kAddWaves * 64, 0,
+                            (hipStream_t)stream>>>(add);
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
 }

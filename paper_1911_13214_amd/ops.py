@@ -68,9 +68,10 @@ def _like(t, other, what, shape=None):
 
 def _matrix(t, what):
     """(rows, cols, pitch) of a tensor whose leading dimensions are rows."""
-    if t.dim() == 0:
+    shape = t.shape
+    if not shape:
         raise ValueError(f"{what} needs at least one dimension")
-    cols = t.shape[-1]
+    cols = shape[-1]
     if cols == 0:
         raise ValueError(f"{what} has no columns")
     rows = t.numel() // cols
@@ -89,9 +90,14 @@ def _matrix(t, what):
     return rows, cols, pitch
 
 
+def _empty(like):
+    """A dense tensor of another's shape, type and device."""
+    return torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
 def _out(out, like, what, shape=None):
     if out is None:
-        return torch.empty(like.shape if shape is None else shape, dtype=like.dtype, device=like.device)
+        return _empty(like) if shape is None else like.new_empty(shape)
     return _like(out, like, what, shape)
 
 
@@ -103,13 +109,13 @@ def _call(name, device, stream, *args):
     """One entry point of the library, on ``stream`` or the device's current
     stream."""
     fn = getattr(rotor.lib(), name)
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    if device.index == torch.cuda.current_device():
-        status = fn(*args, stream.cuda_stream)
+    index = device.index
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if index == torch._C._cuda_getDevice():
+        status = fn(*args, raw)
     else:
         with torch.cuda.device(device):
-            status = fn(*args, stream.cuda_stream)
+            status = fn(*args, raw)
     if status != rotor.ROTOR_OK:
         raise rotor.RotorError(status, name)
 
@@ -211,17 +217,18 @@ def _norm(x, z, post, post_weight, post_bias, gate, residual_scale, pre, pre_wei
     rows = x.numel() // cols
     if z is None and (post != "none" or gate is not None):
         raise ValueError("post and gate need z")
+    at = []
     for name, q, kind in (("post_weight", post_weight, post), ("post_bias", post_bias, post),
                           ("pre_weight", pre_weight, pre), ("pre_bias", pre_bias, pre)):
         if q is None:
+            at.append(None)
             continue
         if kind == "none":
             raise ValueError(f"{name} without its norm")
         if not _like(q, x, name, (cols,)).is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-    n = _Norm(type=code, post=NORMS[post], pre=NORMS[pre], rows=rows, cols=cols, residual_scale=residual_scale,
-              eps=eps, post_weight=_ptr(post_weight), post_bias=_ptr(post_bias), pre_weight=_ptr(pre_weight),
-              pre_bias=_ptr(pre_bias))
+        at.append(q.data_ptr())
+    n = _Norm(code, NORMS[post], NORMS[pre], 0, rows, cols, 0, 0, residual_scale, eps, at[0], at[1], None, at[2], at[3])
     if gate is not None:
         g_rows, g_cols, n.gate_pitch = _matrix(_cuda(gate, "gate"), "gate")
         if gate.dtype != x.dtype or gate.device != x.device or g_cols != cols or g_rows < 1 or rows % g_rows:
@@ -244,8 +251,8 @@ def residual_norm(x, z=None, *, post="none", post_weight=None, post_bias=None, g
     xp = _matrix(x, "x")[2]
     zp = _matrix(_like(z, x, "z"), "z")[2] if z is not None else n.cols
     copy = z is not None or residual_scale != 1.0
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if copy else x
-    h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if pre != "none" else None
+    y = _empty(x) if copy else x
+    h = _empty(x) if pre != "none" else None
     st = torch.empty((n.rows, 4), dtype=torch.float32, device=x.device) if stats else None
     _call("rotor_residual_norm", x.device, stream, ctypes.byref(n), x.data_ptr(), xp, _ptr(z), zp,
           y.data_ptr() if copy else None, n.cols, _ptr(h), n.cols, _ptr(st))
@@ -274,16 +281,13 @@ def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None
     def matrix(t, what):
         return (None, n.cols) if t is None else (t.data_ptr(), _matrix(_like(t, lead, what), what)[2])
 
-    def empty(t):
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
-
-    g = {"x": empty(lead)}
+    g = {"x": _empty(lead)}
     if z is not None:
-        g["z"] = empty(lead)
+        g["z"] = _empty(lead)
     for name, q in (("pre_weight", pre_weight), ("pre_bias", pre_bias), ("post_weight", post_weight),
                     ("post_bias", post_bias), ("gate", gate)):
         if q is not None:
-            g[name] = empty(q)
+            g[name] = _empty(q)
     out = _NormGrads(gate_pitch=n.cols, **{k: g[k].data_ptr() for k in g if k not in ("x", "z")})
     need = ctypes.c_uint64()
     rotor._check(rotor.lib().rotor_residual_norm_workspace_bytes(ctypes.byref(n), ctypes.byref(need)),
@@ -334,7 +338,7 @@ def linear_cross_entropy(h, w, targets, ignore=-100, *, stream=None):
     Tokens with target ``ignore`` have loss 0; other targets outside the rows
     of w give NaN."""
     code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 0, stream)
-    loss, lse = (torch.empty(targets.shape, dtype=torch.float32, device=h.device) for _ in range(2))
+    loss, lse = (torch.empty_like(targets, dtype=torch.float32) for _ in range(2))
     _call("rotor_xent", h.device, stream, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp, targets.data_ptr(),
           ignore, loss.data_ptr(), lse.data_ptr(), aligned, work.data_ptr(), work.numel())
     return loss, lse
@@ -348,8 +352,8 @@ def linear_cross_entropy_backward(h, w, targets, lse, grad_loss, ignore=-100, *,
         return None, None
     code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 1, stream)
     lse, grad_loss = _per_token(lse, targets, "lse"), _per_token(grad_loss, targets, "grad_loss")
-    dh = torch.empty(h.shape, dtype=h.dtype, device=h.device) if need_h else None
-    dw = torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None
+    dh = _empty(h) if need_h else None
+    dw = _empty(w) if need_w else None
     _call("rotor_xent_backward", h.device, stream, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp,
           targets.data_ptr(), ignore, lse, grad_loss, _ptr(dh), cols, _ptr(dw), cols, aligned, work.data_ptr(),
           work.numel())
