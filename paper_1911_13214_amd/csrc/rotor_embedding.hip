@@ -267,45 +267,54 @@ struct SumArgs {
 template <typename T, int V> __global__ __launch_bounds__(kThreads) void sum_kernel(const T *dy, T *out, SumArgs a)
 {
     const int64_t n = *a.count;
-    const int64_t chunk = (int64_t)(blockIdx.x / a.slices) * (kThreads / a.lanes) + threadIdx.x / a.lanes;
+    const int64_t chunk = (int64_t)(blockIdx.x / a.slices) * (kThreads / a.lanes) +
+                          __builtin_amdgcn_readfirstlane(threadIdx.x / a.lanes);
     const int64_t begin = chunk * kChunk;
     if (begin >= n)
         return;
     const int64_t end = begin + kChunk < n ? begin + kChunk : n;
     const int64_t piece = (int64_t)(blockIdx.x % a.slices) * a.lanes + threadIdx.x % a.lanes;
-    if (piece * V >= a.cols)
-        return;
+    if ((piece - threadIdx.x % 64) * V >= a.cols)
+        return;  // the whole wave
+    // lanes past the row's end repeat its last piece
     const int64_t c = column<V>(piece, a.cols);
-    const bool enters = begin > 0 && a.key[begin - 1] == a.key[begin];
-    const bool leaves = end < n && a.key[end] == a.key[end - 1];
+    // A wave lies within one group, so the chunk's keys and positions, and
+    // with them what happens at each of them, are the same in all its lanes:
+    // lane k holds those of entry k (63: the entry before the chunk), and the
+    // loop reads them as scalars.
+    const int lane = threadIdx.x % 64, count = (int)(end - begin);
+    const int64_t mine = lane == 63 ? (begin > 0 ? begin - 1 : begin) : begin + lane < n ? begin + lane : n - 1;
+    const int keys = (int)a.key[mine], places = (int)a.pos[mine];
+    const bool enters = begin > 0 && __builtin_amdgcn_readlane(keys, 63) == __builtin_amdgcn_readlane(keys, 0);
+    const bool leaves = end < n && __builtin_amdgcn_readlane(keys, kChunk) ==
+                                       __builtin_amdgcn_readlane(keys, kChunk - 1);
     float sum[V] = {};
     bool whole = !enters;  // the present token starts here
     constexpr int kAhead = 8;
-    for (int64_t i = begin; i < end; i += kAhead) {
+    for (int i = 0; i < count; i += kAhead) {
         float v[kAhead][V];
-        uint32_t key[kAhead + 1];
         // past the end the last position again, which is not added
 #pragma unroll
-        for (int k = 0; k <= kAhead; ++k)
-            key[k] = a.key[i + k < n ? i + k : n - 1];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            load_vec(dy + (int64_t)a.pos[i + k < end ? i + k : end - 1] * a.dy_pitch + c, v[k]);
+        for (int k = 0; k < kAhead; ++k) {
+            const uint32_t row = __builtin_amdgcn_readlane(places, i + k < count ? i + k : count - 1);
+            load_vec(dy + (int64_t)row * a.dy_pitch + c, v[k]);
+        }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (i + k >= end)
+            if (i + k >= count)
                 break;
 #pragma unroll
             for (int j = 0; j < V; ++j)
                 sum[j] += v[k][j];
-            const bool last = i + k + 1 == end;
-            if (!last && key[k + 1] == key[k])
+            const bool last = i + k + 1 == count;
+            const int key = __builtin_amdgcn_readlane(keys, i + k);
+            if (!last && __builtin_amdgcn_readlane(keys, i + k + 1) == key)
                 continue;
             if (whole && !(last && leaves)) {
 #pragma unroll
                 for (int j = 0; j < V; ++j)
                     sum[j] *= a.scale;
-                store_vec(out + (int64_t)key[k] * a.out_pitch + c, sum);
+                store_vec(out + (int64_t)(uint32_t)key * a.out_pitch + c, sum);
             } else {
                 // the first half for a token that enters (whether or not it
                 // also leaves), the second for one that starts here
