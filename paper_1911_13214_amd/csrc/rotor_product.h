@@ -42,6 +42,38 @@ constexpr int kTermProducts = 6;
 __device__ constexpr int term_a(int s) { return 0x124 >> (2 * s) & 3; }  // 0 1 2 0 1 0
 __device__ constexpr int term_b(int s) { return 0x046 >> (2 * s) & 3; }  // 2 1 0 1 0 0
 
+// The three bf16 terms of a 32-bit value.  Infinities and NaN stay in the
+// first.
+__device__ inline void split(float v, bf16 (&t)[kTerms])
+{
+    t[0] = (bf16)v;
+    const float r = v - (float)t[0];
+    const bool finite = fabsf((float)t[0]) <= 3.3895314e38f;
+    t[1] = finite ? (bf16)r : (bf16)0.f;
+    t[2] = finite ? (bf16)(r - (float)t[1]) : (bf16)0.f;
+}
+
+// Element type of the products of a call: bf16 terms for 32-bit tensors.
+template <typename T> struct ProductOf {
+    typedef T P;
+    static constexpr int kParts = 1;
+};
+template <> struct ProductOf<float> {
+    typedef bf16 P;
+    static constexpr int kParts = kTerms;
+};
+
+// A maximum and the sum of exponentials above it.
+struct Soft {
+    float top, sum;
+};
+__device__ inline float finite_or_0(float v) { return fabsf(v) <= 3.4028234e38f ? v : 0.f; }
+__device__ inline Soft join(Soft a, Soft b)
+{
+    const float top = fmaxf(a.top, b.top), m = finite_or_0(top);
+    return Soft{top, a.sum * __expf(a.top - m) + b.sum * __expf(b.top - m)};
+}
+
 constexpr int kStep = 64;         // of k in one step
 constexpr int kRowBytes = 2 * kStep;
 

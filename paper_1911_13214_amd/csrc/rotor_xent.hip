@@ -9,6 +9,7 @@
 // it in 16 bits, as it is and transposed; then dH += P W and dW = P^T H.  Each
 // product wants its summed index adjacent in both operands, so H once and W
 // piece by piece are transposed too.
+#include "rotor_few.h"
 #include "rotor_product.h"
 
 namespace rotor {
@@ -16,29 +17,6 @@ namespace {
 
 typedef Tile<256, 256, 2, 4> Large;
 typedef Tile<128, 128, 2, 2> Small;
-
-// ---- element conversions ---------------------------------------------------------
-
-// The three bf16 terms of a 32-bit value.  Infinities and NaN stay in the
-// first.
-__device__ inline void split(float v, bf16 (&t)[kTerms])
-{
-    t[0] = (bf16)v;
-    const float r = v - (float)t[0];
-    const bool finite = fabsf((float)t[0]) <= 3.3895314e38f;
-    t[1] = finite ? (bf16)r : (bf16)0.f;
-    t[2] = finite ? (bf16)(r - (float)t[1]) : (bf16)0.f;
-}
-
-// Element type of the products of a call: bf16 terms for 32-bit tensors.
-template <typename T> struct ProductOf {
-    typedef T P;
-    static constexpr int kParts = 1;
-};
-template <> struct ProductOf<float> {
-    typedef bf16 P;
-    static constexpr int kParts = kTerms;
-};
 
 // dst[c][r] = src[r][c] for rows and columns in range, 0 up to `rows_to` rows
 // of src (and for rows without a target, where targets is given).  64 x 64
@@ -81,17 +59,6 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t rows, i
 }
 
 // ---- epilogues -------------------------------------------------------------------
-
-// A maximum and the sum of exponentials above it.
-struct Soft {
-    float top, sum;
-};
-__device__ inline float finite_or_0(float v) { return fabsf(v) <= 3.4028234e38f ? v : 0.f; }
-__device__ inline Soft join(Soft a, Soft b)
-{
-    const float top = fmaxf(a.top, b.top), m = finite_or_0(top);
-    return Soft{top, a.sum * __expf(a.top - m) + b.sum * __expf(b.top - m)};
-}
 
 // Maximum and sum of exponentials of each token over the tile's rows of W,
 // and the target's logit.
@@ -322,26 +289,33 @@ template <typename T> struct OutEpilogue {
 
 // ---- small launches -----------------------------------------------------------------
 
-// Joins the tiles' maxima and sums: 16 tokens a workgroup, 16 lanes each.
+// Joins the tiles' maxima and sums: X tokens a workgroup, 256 / X lanes each.
+template <int X>
 __global__ __launch_bounds__(256) void loss_kernel(const float2 *part, int64_t tiles, const float *target_logit,
                                                    const int64_t *targets, int64_t ignore, int64_t vocab,
                                                    int64_t tokens, float *loss, float *lse)
 {
-    __shared__ Soft other[16][17];
-    const int x = threadIdx.x % 16, y = threadIdx.x / 16;
-    const int64_t j = (int64_t)blockIdx.x * 16 + x;
+    constexpr int Y = 256 / X;
+    __shared__ Soft other[Y][X + 1];
+    const int x = threadIdx.x % X, y = threadIdx.x / X;
+    const int64_t j = (int64_t)blockIdx.x * X + x;
     Soft s{-__builtin_inff(), 0.f};
-    if (j < tokens)
-        for (int64_t t = y; t < tiles; t += 16) {
+    if (j < tokens) {
+#pragma unroll 4
+        for (int64_t t = y; t < tiles; t += Y) {
             const float2 v = part[t * tokens + j];
             s = join(s, Soft{v.x, v.y});
         }
+    }
     other[y][x] = s;
-    __syncthreads();
+    for (int half = Y / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        if (y < half)
+            other[y][x] = join(other[y][x], other[y + half][x]);
+    }
     if (y > 0 || j >= tokens)
         return;
-    for (int w = 1; w < 16; ++w)
-        s = join(s, other[w][x]);
+    s = other[0][x];
     const float l = finite_or_0(s.top) + logf(s.sum);
     lse[j] = l;
     const int64_t t = targets[j];
@@ -456,11 +430,13 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
     Bump b;
     const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
     l.dk = pad(d, kStep);
-    l.part = b.take(8ull * (uint64_t)ceil_div(v, 128) * (uint64_t)n);
+    l.part = b.take(8ull * (uint64_t)ceil_div(v, n <= kFew ? kFewRows : 128) * (uint64_t)n);
     l.target = b.take(4ull * (uint64_t)n);
     l.piece = v;
     l.h = l.w = b.at;
-    if (pack) {
+    if (n <= kFew) {
+        l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
+    } else if (pack) {
         const int64_t most = (kPieceBytes / 2) / (2 * parts * l.dk) / kPad * kPad;  // at least kPad: see the limits
         l.piece = v < most ? v : most;
         l.h = b.take(2ull * (uint64_t)(parts * l.dk * n));
@@ -484,6 +460,25 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     Bump b;
     const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
     l.dk = pad(d, kStep);
+    l.sum_pitch = pad(d, 4);
+    l.grad = b.take(4ull * (uint64_t)n);
+    l.scale = b.take(4);
+    if (n <= kFew) {
+        l.nk = n <= 32 ? 32 : 64;
+        l.piece = pad(v, kFewRows);
+        l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
+        l.ht = b.take(2ull * (uint64_t)(parts * l.nk * d));
+        l.p = b.take(2ull * (uint64_t)(parts * l.piece * n));
+        // parts of the vocabulary for two workgroups on every CU, of four
+        // tiles at least
+        const int64_t t = l.piece / kFewRows, most = ceil_div(t, 4);
+        const int64_t want = ceil_div(512, ceil_div(d, kFewCols));
+        l.split = (int)(want < most ? want : most);
+        l.sum = b.take(4ull * (uint64_t)(l.split * n * l.sum_pitch));
+        l.w = l.wt = l.pt = 0;
+        l.total = b.at;
+        return l;
+    }
     l.nk = pad(n, kPad);
     l.piece = pad(v, kPad);
     int64_t most = kPieceBytes / (4 * parts * l.nk) / kPad * kPad;
@@ -494,8 +489,6 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
         const int64_t count = ceil_div(l.piece, most);
         l.piece = pad(ceil_div(l.piece, count), kPad);
     }
-    l.grad = b.take(4ull * (uint64_t)n);
-    l.scale = b.take(4);
     l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
     l.w = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * l.piece) : 0);
     l.ht = b.take(2ull * (uint64_t)(parts * l.nk * d));
@@ -510,7 +503,6 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     if (split > steps / 8)
         split = steps / 8 > 0 ? steps / 8 : 1;
     l.split = (int)split;
-    l.sum_pitch = pad(d, 4);
     l.sum = b.take(4ull * (uint64_t)(l.split * n * l.sum_pitch));
     l.total = b.at;
     return l;
@@ -565,6 +557,30 @@ Operand<typename ProductOf<T>::P> operand(const T *src, int64_t rows, int64_t co
     return Operand<P>{(const P *)space, rows, parts * dk, parts > 1 ? dk : 0};
 }
 
+// Calls f with the number of 16-token tiles that few tokens take.
+template <int V> struct IntV { static constexpr int v = V; };
+template <typename F> void with_few(int64_t tokens, F f)
+{
+    if (tokens <= 16)
+        f(IntV<1>{});
+    else if (tokens <= 32)
+        f(IntV<2>{});
+    else
+        f(IntV<4>{});
+}
+
+void run_loss(const float2 *part, int64_t tiles, const float *target_logit, const int64_t *targets, int64_t ignore,
+              int64_t vocab, int64_t tokens, float *loss, float *lse, hipStream_t s)
+{
+    // a workgroup a token until those fill the device
+    if (tokens <= 1024)
+        loss_kernel<1><<<dim3((uint32_t)tokens), 256, 0, s>>>(part, tiles, target_logit, targets, ignore, vocab,
+                                                              tokens, loss, lse);
+    else
+        loss_kernel<16><<<dim3((uint32_t)ceil_div(tokens, 16)), 256, 0, s>>>(part, tiles, target_logit, targets,
+                                                                             ignore, vocab, tokens, loss, lse);
+}
+
 }  // namespace
 }  // namespace rotor
 
@@ -613,13 +629,32 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
         const T *w = (const T *)d_w;
         const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
         float2 *part = (float2 *)(work + l.part);
+        float *target = (float *)(work + l.target);
+        if (n_tokens <= kFew) {
+            FewArgs<T> f{};
+            f.w = w;
+            f.w_pitch = w_pitch;
+            f.rows = n_rows;
+            f.cols = cols;
+            f.h = b;
+            f.tokens = (int)n_tokens;
+            f.targets = d_targets;
+            f.part = part;
+            f.target_logit = target;
+            const int64_t blocks = ceil_div(n_rows, kFewRows);
+            with_few(n_tokens, [&](auto c) {
+                few_kernel<T, decltype(c)::v, false><<<dim3((uint32_t)blocks), kFewThreads, 0, s>>>(f);
+            });
+            run_loss(part, blocks, target, d_targets, ignore, n_rows, n_tokens, d_loss, d_lse, s);
+            return;
+        }
         int64_t tiles_done = 0;
         for (int64_t v0 = 0; v0 < n_rows; v0 += l.piece) {
             const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
             const Operand<P> a = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
             StatsEpilogue ep;
             ep.part = part + tiles_done * n_tokens;
-            ep.target_logit = (float *)(work + l.target);
+            ep.target_logit = target;
             ep.targets = d_targets;
             ep.vocab = (int)rows;
             ep.tokens = (int)n_tokens;
@@ -627,9 +662,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
             run_product<P>(a, b, pad(cols, 8), products, 1, ep, s);
             tiles_done += ceil_div(rows, large_tiles(rows, n_tokens, 1) ? 256 : 128);
         }
-        loss_kernel<<<dim3((uint32_t)ceil_div(n_tokens, 16)), 256, 0, s>>>(part, tiles_done,
-                                                                          (const float *)(work + l.target), d_targets,
-                                                                          ignore, n_rows, n_tokens, d_loss, d_lse);
+        run_loss(part, tiles_done, target, d_targets, ignore, n_rows, n_tokens, d_loss, d_lse, s);
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
 }
@@ -680,7 +713,44 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         const Operand<P> hb = operand<T>(h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
         if (d_dw)  // rows without a target as 0: they may hold NaN
             run_pack<T, true>(h, n_tokens, cols, h_pitch, work + l.ht, parts * l.nk, l.nk, l.nk, cols, grad, s);
-        for (int64_t v0 = 0; v0 < n_rows; v0 += l.piece) {
+        if (n_tokens <= kFew) {
+            FewArgs<T> f{};
+            f.w = w;
+            f.w_pitch = w_pitch;
+            f.rows = n_rows;
+            f.cols = cols;
+            f.h = hb;
+            f.tokens = (int)n_tokens;
+            f.targets = d_targets;
+            f.lse = d_lse;
+            f.grad = grad;
+            f.scale = scale;
+            f.p = d_dh ? (P *)(work + l.p) : nullptr;
+            f.p_seg = l.piece;
+            f.ht = (const P *)(work + l.ht);
+            f.dw = (T *)d_dw;
+            f.dw_pitch = dw_pitch;
+            with_few(n_tokens, [&](auto c) {
+                constexpr int C = decltype(c)::v;
+                few_kernel<T, C, true><<<dim3((uint32_t)ceil_div(n_rows, kFewRows)), kFewThreads, 0, s>>>(f);
+                if (!d_dh)
+                    return;
+                FewSumArgs<T> g;
+                g.w = w;
+                g.w_pitch = w_pitch;
+                g.rows = n_rows;
+                g.cols = cols;
+                g.p = f.p;
+                g.p_seg = l.piece;
+                g.tokens = (int)n_tokens;
+                g.sum = sum;
+                g.sum_pitch = l.sum_pitch;
+                g.tiles = ceil_div(ceil_div(n_rows, kFewRows), l.split);
+                few_sum_kernel<T, C><<<dim3((uint32_t)ceil_div(cols, kFewCols), (uint32_t)l.split), kFewThreads, 0, s>>>(
+                    g);
+            });
+        }
+        for (int64_t v0 = 0; v0 < n_rows && n_tokens > kFew; v0 += l.piece) {
             const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
             const Operand<P> wa = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
             ProbEpilogue<T> ep;
