@@ -1,6 +1,7 @@
-// Matrix products of the cross entropy: C[j][i] = sum over k of A[i][k] B[j][k],
-// both operands 16-bit with k adjacent, sums in 32 bits on the matrix units,
-// a tile's results handed to an epilogue while they are in registers.
+// Matrix products of the cross entropy: C[j][i] = sum over k of A(i, k) B(j, k),
+// operands 16-bit, each with k or with i (j) adjacent in memory, sums in 32
+// bits on the matrix units, a tile's results handed to an epilogue while they
+// are in registers.
 #pragma once
 
 #include "rotor_ops.h"
@@ -26,12 +27,24 @@ template <> struct Mfma<f16> {
     }
 };
 
-// An operand: `rows` rows, `pitch` elements apart, each row 16-byte aligned.
-// A 32-bit matrix is held as three bf16 terms whose sum has its 24 bits, the
-// terms of a row `seg` elements apart.
+#if defined(__HIP_DEVICE_COMPILE__)
+// The transposing read of four 16-bit elements: of the 16 lanes that address
+// four rows of 16 columns, lane i gets column i of the four rows.
+typedef short Turned __attribute__((ext_vector_type(4)));
+__device__ inline Turned turned(const char *lds)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Turned *)lds);
+}
+#endif
+
+// An operand: `rows` rows of `cols` elements, `pitch` elements apart, 16-byte
+// aligned, cols a multiple of 8.  The summed index k runs along the rows, or,
+// in a product's template with KA or KB set, over them.  A 32-bit matrix is
+// held as three bf16 terms whose sum has its 24 bits, the terms of a row
+// `seg` elements apart.
 template <typename T> struct Operand {
     const T *p;
-    int64_t rows, pitch, seg;
+    int64_t rows, cols, pitch, seg;
 };
 
 // The products of terms (a, b) whose sum is the product of two 32-bit
@@ -78,7 +91,7 @@ constexpr int kStep = 64;         // of k in one step
 constexpr int kRowBytes = 2 * kStep;
 
 struct ProductArgs {
-    int64_t k;        // a multiple of 8
+    int64_t k;
     int products;     // kTermProducts, or 1
     int tiles_i, tiles_j;
     int steps;        // of all products, ceil(k / kStep) each
@@ -103,7 +116,6 @@ template <typename S> struct Results {
     int i, j;
     int wave_i, wave_j, lane;
     int part;
-    char *lds;  // the wave's own share of LDS: 16 BI BJ / waves bits at least
 };
 
 // Hides where a value comes from, so that what is computed from it stays
@@ -129,47 +141,111 @@ __device__ inline void tile_of(int id, int tiles_i, int tiles_j, int &ti, int &t
 // Buffer descriptors exist in device code only: the host's pass sees a kernel
 // without a body.
 #if defined(__HIP_DEVICE_COMPILE__)
-template <typename T> __device__ inline __amdgpu_buffer_rsrc_t operand_rsrc(const Operand<T> &o, int64_t row0,
-                                                                              int64_t rows, int64_t k)
+template <typename T> __device__ inline __amdgpu_buffer_rsrc_t rsrc_of(const T *p, int64_t elements)
 {
-    const int64_t have = o.rows - row0 < rows ? o.rows - row0 : rows;
-    const int64_t bytes = ((have - 1) * o.pitch + o.seg * (kTerms - 1) + k) * (int64_t)sizeof(T);
-    return __builtin_amdgcn_make_buffer_rsrc((void *)(o.p + row0 * o.pitch), 0,
-                                             (int)(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF), 0x00020000);
+    const int64_t bytes = elements * (int64_t)sizeof(T);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF),
+                                             0x00020000);
 }
 
 typedef __attribute__((address_space(3))) void *lds_ptr;
 
-// One operand's rows of a step, global memory to LDS without registers.  A
-// wave's load moves 8 rows of 128 bytes; row r's 16-byte piece c lands in
-// place c ^ (r % 8), so that the 16 rows a fragment reads lie in different
-// banks.  Rows and pieces outside the operand come as 0 (the buffer's bound).
-template <typename T, int LOADS> struct Loader {
+// One operand's part of a step, global memory to LDS without registers, and
+// its fragments out of LDS.  SIDE: rows (columns) of the workgroup's tile;
+// LOADS: of a wave in one step; N: fragments of a wave.  What lies outside
+// the operand comes as 0 (the buffer's bound).
+template <typename T, int SIDE, int LOADS, int N, bool KROWS> struct Loader;
+
+// k along the rows.  A wave's load moves 8 rows of 128 bytes; row r's 16-byte
+// piece c lands in place c ^ (r % 8), so that the 16 rows a fragment reads lie
+// in different banks.
+template <typename T, int SIDE, int LOADS, int N> struct Loader<T, SIDE, LOADS, N, false> {
     __amdgpu_buffer_rsrc_t rsrc;
     uint32_t at[LOADS];
-    uint32_t limit;  // bytes of k before this lane's piece leaves the row
-    int first;       // LDS byte of this wave's first load
-    __device__ void init(const Operand<T> &o, int64_t row0, int64_t rows, int64_t k, int wave, int lane)
+    int limit;  // bytes of k before this lane's piece leaves the row
+    int first;  // LDS byte of this wave's first load
+    int base, swz[2];
+    __device__ void init(const Operand<T> &o, int64_t side0, int wave, int lane, int wave_side)
     {
-        rsrc = operand_rsrc(o, row0, rows, k);
+        const int64_t have = o.rows - side0 < SIDE ? o.rows - side0 : SIDE;
+        rsrc = rsrc_of(o.p + side0 * o.pitch, (have - 1) * o.pitch + o.seg * (kTerms - 1) + o.cols);
         const int piece = (lane % 8) ^ (lane / 8);
 #pragma unroll
         for (int q = 0; q < LOADS; ++q)
             at[q] = (uint32_t)((wave * LOADS + q) * 8 + lane / 8) * (uint32_t)(o.pitch * sizeof(T)) + piece * 16;
-        limit = (uint32_t)(k * sizeof(T)) - piece * 16;
+        limit = (int)(o.cols * sizeof(T)) - piece * 16;
         first = wave * LOADS * 1024;
+        const int row = lane % 16;
+        base = (wave_side * N * 16 + row) * kRowBytes;
+        swz[0] = ((lane / 16) ^ (row & 7)) * 16;
+        swz[1] = ((4 + lane / 16) ^ (row & 7)) * 16;
     }
-    // `term`: byte of the term in a row; `kb`: byte of the step in the term
-    __device__ void load(char *lds, uint32_t term, uint32_t kb) const
+    // `term`: elements from a row's start to its term; `step`: of k
+    __device__ void load(const Operand<T> &, char *lds, int64_t term, int step, bool live) const
     {
-        const bool in = (int)kb < (int)limit;
+        const int kb = live ? step * kRowBytes : 0x7FFFFF00;
+        const uint32_t off = (uint32_t)(term * sizeof(T)) + (uint32_t)kb;
+        const bool in = kb < limit;
 #pragma unroll
         for (int q = 0; q < LOADS; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + q * 1024), 16,
-                                                     in ? at[q] + term + kb : 0x80000000u, 0, 0, 0);
+                                                     in ? at[q] + off : 0x80000000u, 0, 0, 0);
+    }
+    __device__ void read(const char *lds, int h, typename Mfma<T>::Frag (&f)[N]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            f[n] = *(const typename Mfma<T>::Frag *)(lds + base + swz[h] + n * 16 * kRowBytes);
     }
 };
 
+// k over the rows: LDS holds 64 rows of SIDE elements, and the transposing
+// read hands four rows' elements of one column to a lane (its 16 lanes address
+// four rows of 16 columns).  The 16 rows that a read touches are spread over
+// the banks by the 32-byte slots' places, s ^ (r % 4 + 4 (r / 8 % 2)).
+template <typename T, int SIDE, int LOADS, int N> struct Loader<T, SIDE, LOADS, N, true> {
+    static constexpr int kRow = SIDE * 2, kLanes = kRow / 16;  // bytes of a row, and lanes that load it
+    const T *start;
+    int64_t cols;
+    uint32_t at[LOADS];
+    int first, base, sw, slot;
+    static __device__ int turn(int row) { return (row & 3) | (row >> 3 & 1) << 2; }
+    __device__ void init(const Operand<T> &o, int64_t side0, int wave, int lane, int wave_side)
+    {
+        start = o.p + side0;
+        cols = o.cols - side0 + o.seg * (kTerms - 1);
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q) {
+            const int row = (wave * LOADS + q) * (64 / kLanes) + lane / kLanes;
+            at[q] = (uint32_t)row * (uint32_t)(o.pitch * sizeof(T)) + ((lane % kLanes) ^ (turn(row) << 1)) * 16;
+        }
+        first = wave * LOADS * 1024;
+        const int g = lane / 16, i = lane % 16;
+        base = (g * 8 + i / 4) * kRow + i % 4 * 8;
+        sw = turn(g * 8 + i / 4);
+        slot = wave_side * N;
+    }
+    __device__ void load(const Operand<T> &o, char *lds, int64_t term, int step, bool live) const
+    {
+        const int64_t row0 = (int64_t)step * kStep, have = o.rows - row0 < kStep ? o.rows - row0 : kStep;
+        const auto rsrc = rsrc_of(start + row0 * o.pitch, live && have > 0 ? (have - 1) * o.pitch + cols : 0);
+        const uint32_t off = (uint32_t)(term * sizeof(T));
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + q * 1024), 16, at[q] + off, 0, 0,
+                                                     0);
+    }
+    __device__ void read(const char *lds, int h, typename Mfma<T>::Frag (&f)[N]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const char *p = lds + base + ((slot + n) ^ sw) * 32 + h * 32 * kRow;
+            f[n] = __builtin_bit_cast(typename Mfma<T>::Frag,
+                                      __builtin_shufflevector(turned(p), turned(p + 4 * kRow), 0, 1, 2, 3, 4, 5, 6,
+                                                              7));
+        }
+    }
+};
 
 // A barrier that waits only for what it names: a workgroup barrier of the
 // language would also wait for the loads that the next phases hide.
@@ -187,7 +263,7 @@ template <int WAIT> __device__ inline void phase_barrier()
 }
 #endif
 
-template <typename T, typename S, typename E>
+template <typename T, typename S, bool KA, bool KB, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Operand<T> b, ProductArgs p, E epilogue)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -200,18 +276,18 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     tile_of(blockIdx.x, p.tiles_i, p.tiles_j, ti, tj);
     const int wi = wave / S::WJ, wj = wave % S::WJ;
 
-    Loader<T, S::kLoadsA> la;
-    Loader<T, S::kLoadsB> lb;
-    la.init(a, (int64_t)ti * S::BI, S::BI, p.k, wave, lane);
-    lb.init(b, (int64_t)tj * S::BJ, S::BJ, p.k, wave, lane);
+    Loader<T, S::BI, S::kLoadsA, S::NI, KA> la;
+    Loader<T, S::BJ, S::kLoadsB, S::NJ, KB> lb;
+    la.init(a, (int64_t)ti * S::BI, wave, lane, wi);
+    lb.init(b, (int64_t)tj * S::BJ, wave, lane, wj);
+    constexpr int kB = S::BI * kRowBytes;  // LDS byte of B's part
     const int per = (int)((p.k + kStep - 1) / kStep);
     const int t0 = blockIdx.y * p.split_steps;
     const int t1 = t0 + p.split_steps < p.steps ? t0 + p.split_steps : p.steps;
     int s = kTermProducts - p.products + t0 / per, at = t0 % per;  // of the next load
     auto load = [&](char *lds, bool live) {
-        const uint32_t kb = live ? (uint32_t)at * kRowBytes : 0x7FFFFF00u;
-        la.load(lds, (uint32_t)(term_a(s) * a.seg * sizeof(T)), kb);
-        lb.load(lds + S::BI * kRowBytes, (uint32_t)(term_b(s) * b.seg * sizeof(T)), kb);
+        la.load(a, lds, term_a(s) * a.seg, at, live);
+        lb.load(b, lds + kB, term_b(s) * b.seg, at, live);
         if (++at == per) {
             at = 0;
             ++s;
@@ -224,17 +300,10 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
 #pragma unroll
         for (int jj = 0; jj < S::NJ; ++jj)
             res.acc[ii][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int row = lane % 16;
-    const int swz[2] = {((lane / 16) ^ (row & 7)) * 16, ((4 + lane / 16) ^ (row & 7)) * 16};
-    const int base_a = (wi * S::NI * 16 + row) * kRowBytes, base_b = (S::BI + wj * S::NJ * 16 + row) * kRowBytes;
     Frag fa[S::NI], fb[S::NJ];
     auto read = [&](const char *lds, int h) {  // half h of a step: 32 of k
-#pragma unroll
-        for (int jj = 0; jj < S::NJ; ++jj)
-            fb[jj] = *(const Frag *)(lds + base_b + swz[h] + jj * 16 * kRowBytes);
-#pragma unroll
-        for (int ii = 0; ii < S::NI; ++ii)
-            fa[ii] = *(const Frag *)(lds + base_a + swz[h] + ii * 16 * kRowBytes);
+        lb.read(lds + kB, h, fb);
+        la.read(lds, h, fa);
     };
     auto multiply = [&]() {
         __builtin_amdgcn_s_setprio(1);
@@ -313,10 +382,8 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     res.wave_j = wj;
     res.lane = lane;
     res.i = wi * S::NI * 16 + lane / 16 * 4;
-    res.j = wj * S::NJ * 16 + row;
+    res.j = wj * S::NJ * 16 + lane % 16;
     res.part = blockIdx.y;
-    constexpr int kShare = 2 * S::kBytes / S::kWaves;
-    res.lds = wave < S::kWaves / 2 ? even + wave * kShare : odd + (wave - S::kWaves / 2) * kShare;
     opaque(res.i);
     opaque(res.j);
     epilogue(res, even);

@@ -6,9 +6,8 @@
 // A second launch joins the tiles' pairs.
 // Backward, for pieces of the vocabulary: the same product again, whose
 // epilogue turns logits into P = (softmax - target) * gradient and writes
-// it in 16 bits, as it is and transposed; then dH += P W and dW = P^T H.  Each
-// product wants its summed index adjacent in both operands, so H once and W
-// piece by piece are transposed too.
+// it in 16 bits; then dH += P W and dW = P^T H, which read what they need
+// transposed on its way out of LDS.
 #include "rotor_few.h"
 #include "rotor_product.h"
 
@@ -124,99 +123,63 @@ struct StatsEpilogue {
     }
 };
 
-// P[j][i] and its transpose, from the logits.
+// P[j][i] from the logits.
 template <typename T> struct ProbEpilogue {
     typedef typename ProductOf<T>::P P;
     static constexpr int kParts = ProductOf<T>::kParts;
-    P *p, *pt;
-    int p_pitch, p_seg, pt_pitch, pt_seg;
+    P *p;
+    int pitch, seg;
     const float *lse, *grad;  // grad: scaled gradient of each token's loss, 0 without a target
     const int64_t *targets;
-    int64_t v0;                   // the piece's first row of W
-    int rows, tokens, tokens_to;  // its rows; tokens, and padded
+    int64_t v0;        // the piece's first row of W
+    int rows, tokens;  // its rows; tokens
     template <typename S> __device__ void operator()(Results<S> &r, char *) const
     {
         typedef typename VecOf<P, 4>::V V4;
-        typedef P V8 __attribute__((ext_vector_type(8)));
         const int have = rows - r.tile_i * S::BI;
         const int j0 = r.tile_j * S::BJ;
+        // the piece is padded to whole tiles, and so is P's pitch
+        P *const tile = p + (int64_t)j0 * pitch + r.tile_i * S::BI;
 #pragma unroll
         for (int jj = 0; jj < S::NJ; ++jj) {
-            const int j = j0 + r.j + 16 * jj;
-            const bool in = j < tokens;
-            const float g = in ? grad[j] : 0.f, l = in ? lse[j] : 0.f;
-            const int64_t t64 = (in ? targets[j] : -1) - v0 - r.tile_i * S::BI;
+            int row = r.j + 16 * jj;
+            opaque(row);
+            const int j = j0 + row;
+            if (j >= tokens)
+                continue;
+            const float g = grad[j], l = lse[j];
+            const int64_t t64 = targets[j] - v0 - r.tile_i * S::BI;
             const int t = t64 >= 0 && t64 < S::BI ? (int)t64 - r.i : -1;
 #pragma unroll
-            for (int ii = 0; ii < S::NI; ++ii)
+            for (int ii = 0; ii < S::NI; ++ii) {
+                float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = __expf(r.acc[ii][jj][e] - l) - (t == 16 * ii + e ? 1.f : 0.f);
+                    v[e] = __expf(r.acc[ii][jj][e] - l) - (t == 16 * ii + e ? 1.f : 0.f);
                     // a select: what a token without a target holds may be NaN
-                    r.acc[ii][jj][e] = g != 0.f && r.i + 16 * ii + e < have ? v * g : 0.f;
+                    v[e] = g != 0.f && r.i + 16 * ii + e < have ? v[e] * g : 0.f;
                 }
-        }
-        __syncthreads();  // all waves have left the LDS the transposition uses
-#pragma unroll 1
-        for (int q = 0; q < kParts; ++q) {
-            // the piece is padded to whole tiles, and so is P's pitch
-            P *const tile = p + (int64_t)j0 * p_pitch + q * p_seg + r.tile_i * S::BI;
-#pragma unroll
-            for (int jj = 0; jj < S::NJ; ++jj) {
-                int row = r.j + 16 * jj;
-                opaque(row);
-                if (j0 + row < tokens) {
-#pragma unroll
-                    for (int ii = 0; ii < S::NI; ++ii) {
-                        V4 w;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[e] = (P)r.acc[ii][jj][e];
-                        *(V4 *)(tile + (uint32_t)(row * p_pitch + r.i + 16 * ii)) = w;
-                    }
-                }
-            }
-            // the wave's own results transposed through its share of LDS, a
-            // row of i adjacent, so that rows are stored 2 NJ * 16 bytes at a
-            // time; the four lanes groups' rows go to different banks
-            constexpr int kRow = S::NJ * 32;  // bytes
-            static_assert(kRow == 128, "the banks' pattern");
-#pragma unroll
-            for (int jj = 0; jj < S::NJ; ++jj)
-#pragma unroll
-                for (int ii = 0; ii < S::NI; ++ii)
+                P *const at = tile + (uint32_t)(row * pitch + r.i + 16 * ii);
+                if constexpr (kParts == 1) {
+                    V4 w;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        *(P *)(r.lds + (16 * ii + r.lane / 16 * 4 + e) * kRow +
-                               (((16 * jj + r.lane % 16) * 2) ^ (r.lane / 16 * 32))) = (P)r.acc[ii][jj][e];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            int i = r.lane / 8;  // 8 lanes a row
-            opaque(i);
-            const int jt = r.wave_j * S::NJ * 16 + r.lane % 8 * 8;
-            P *const tile_t = pt + (int64_t)r.tile_i * S::BI * pt_pitch + q * pt_seg + j0;
-            if (j0 + jt < tokens_to) {
+                        w[e] = (P)v[e];
+                    *(V4 *)at = w;
+                } else {
+                    V4 w[kTerms];
 #pragma unroll
-                for (int k = 0; k < S::NI * 2; ++k) {
-                    const int row = i + 8 * k, it = r.wave_i * S::NI * 16 + row;
-                    const V8 w = *(const V8 *)(r.lds + row * kRow + ((r.lane % 8 * 16) ^ (row / 4 % 4 * 32)));
-                    if (it < have)
-                        *(V8 *)(tile_t + (uint32_t)(it * pt_pitch + jt)) = w;
+                    for (int e = 0; e < 4; ++e) {
+                        bf16 s[kTerms];
+                        split(v[e], s);
+#pragma unroll
+                        for (int q = 0; q < kTerms; ++q)
+                            w[q][e] = s[q];
+                    }
+#pragma unroll
+                    for (int q = 0; q < kTerms; ++q)
+                        *(V4 *)(at + q * seg) = w[q];
                 }
-            }
-            if (kParts > 1) {
-                // what the next term has to hold
-#pragma unroll
-                for (int jj = 0; jj < S::NJ; ++jj)
-#pragma unroll
-                    for (int ii = 0; ii < S::NI; ++ii)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float t = (float)(P)r.acc[ii][jj][e];
-                            r.acc[ii][jj][e] = finite_or_0(r.acc[ii][jj][e] - t);
-                        }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
             }
         }
     }
@@ -388,8 +351,8 @@ template <typename T> __global__ __launch_bounds__(256) void clear_kernel(T *out
 
 // ---- plans --------------------------------------------------------------------------
 
-constexpr int64_t kPad = 256;                     // rows and columns of P and its transpose in whole tiles
-constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of P and its transpose together
+constexpr int64_t kPad = 256;                        // columns of P in whole tiles
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;  // of P, or of a copied piece of W
 
 int64_t pad(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
 
@@ -437,7 +400,7 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
     if (n <= kFew) {
         l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
     } else if (pack) {
-        const int64_t most = (kPieceBytes / 2) / (2 * parts * l.dk) / kPad * kPad;  // at least kPad: see the limits
+        const int64_t most = kPieceBytes / (2 * parts * l.dk) / kPad * kPad;  // at least kPad: see the limits
         l.piece = v < most ? v : most;
         l.h = b.take(2ull * (uint64_t)(parts * l.dk * n));
         l.w = b.take(2ull * (uint64_t)(parts * l.dk * l.piece));
@@ -447,8 +410,8 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
 }
 
 struct BackwardLayout {
-    uint64_t grad, scale, h, w, ht, wt, p, pt, sum, total;
-    int64_t dk, piece, nk, pk, sum_pitch;
+    uint64_t grad, scale, h, w, ht, p, sum, total;
+    int64_t dk, piece, nk, sum_pitch;
     int split;
 };
 
@@ -475,13 +438,13 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
         const int64_t want = ceil_div(512, ceil_div(d, kFewCols));
         l.split = (int)(want < most ? want : most);
         l.sum = b.take(4ull * (uint64_t)(l.split * n * l.sum_pitch));
-        l.w = l.wt = l.pt = 0;
+        l.w = 0;
         l.total = b.at;
         return l;
     }
-    l.nk = pad(n, kPad);
+    l.nk = n;
     l.piece = pad(v, kPad);
-    int64_t most = kPieceBytes / (4 * parts * l.nk) / kPad * kPad;
+    int64_t most = kPieceBytes / (2 * parts * n) / kPad * kPad;
     if (most < kPad)
         most = kPad;
     if (l.piece > most) {
@@ -489,16 +452,13 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
         const int64_t count = ceil_div(l.piece, most);
         l.piece = pad(ceil_div(l.piece, count), kPad);
     }
-    l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
+    l.h = b.take(2ull * (uint64_t)(parts * l.dk * n));
     l.w = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * l.piece) : 0);
-    l.ht = b.take(2ull * (uint64_t)(parts * l.nk * d));
-    l.wt = b.take(2ull * (uint64_t)(parts * l.piece * d));
     l.p = b.take(2ull * (uint64_t)(parts * l.piece * n));
-    l.pt = b.take(2ull * (uint64_t)(parts * l.nk * l.piece));
-    // few tiles of dH: its summed index (the piece) in parts, for two
-    // workgroups on every CU
-    const int64_t t = tiles(d, n, 256) >= 128 ? tiles(d, n, 256) : tiles(d, n, 128);
-    int64_t split = t >= 256 ? 1 : 256 / t;
+    l.ht = 0;
+    // few tiles of dH: its summed index (the piece) in parts, for a large
+    // tile on every CU, of eight steps at least
+    int64_t split = ceil_div(256, tiles(d, n, 256));
     const int64_t steps = (type == ROTOR_F32 ? kTermProducts : 1) * (l.piece / kStep);
     if (split > steps / 8)
         split = steps / 8 > 0 ? steps / 8 : 1;
@@ -508,30 +468,36 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     return l;
 }
 
-template <typename P, typename S, typename E>
-void run_tiles(const Operand<P> &a, const Operand<P> &b, int64_t k, int products, int split, E e, hipStream_t s)
+// C of ni x nj results, the summed index in `split` parts.
+struct Extent {
+    int64_t ni, nj, k;
+    int split;
+};
+
+template <typename P, typename S, bool KA, bool KB, typename E>
+void run_tiles(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, hipStream_t s)
 {
     ProductArgs p;
-    p.k = k;
-    p.products = products;
-    p.tiles_i = (int)ceil_div(a.rows, S::BI);
-    p.tiles_j = (int)ceil_div(b.rows, S::BJ);
-    p.steps = products * (int)ceil_div(k, kStep);
-    p.split_steps = (int)ceil_div(p.steps, split);
-    product_kernel<P, S, E>
-        <<<dim3((uint32_t)((int64_t)p.tiles_i * p.tiles_j), (uint32_t)split), S::kThreads, 0, s>>>(a, b, p, e);
+    p.k = x.k;
+    p.products = a.seg ? kTermProducts : 1;
+    p.tiles_i = (int)ceil_div(x.ni, S::BI);
+    p.tiles_j = (int)ceil_div(x.nj, S::BJ);
+    p.steps = p.products * (int)ceil_div(x.k, kStep);
+    p.split_steps = (int)ceil_div(p.steps, x.split);
+    product_kernel<P, S, KA, KB, E><<<dim3((uint32_t)((int64_t)p.tiles_i * p.tiles_j), (uint32_t)x.split),
+                                      S::kThreads, 0, s>>>(a, b, p, e);
 }
 
-// Large tiles if they fill the 256 CUs, else small ones.
+// Large tiles if they fill half of the 256 CUs, else small ones.
 bool large_tiles(int64_t a, int64_t b, int split) { return tiles(a, b, 256) * split >= 128; }
 
-template <typename P, typename E>
-void run_product(const Operand<P> &a, const Operand<P> &b, int64_t k, int products, int split, E e, hipStream_t s)
+template <bool KA, bool KB, typename P, typename E>
+void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, hipStream_t s)
 {
-    if (large_tiles(a.rows, b.rows, split))
-        run_tiles<P, Large, E>(a, b, k, products, split, e, s);
+    if (large_tiles(x.ni, x.nj, x.split))
+        run_tiles<P, Large, KA, KB, E>(a, b, x, e, s);
     else
-        run_tiles<P, Small, E>(a, b, k, products, split, e, s);
+        run_tiles<P, Small, KA, KB, E>(a, b, x, e, s);
 }
 
 template <typename T, bool TRANSPOSE>
@@ -544,17 +510,18 @@ void run_pack(const T *src, int64_t rows, int64_t cols, int64_t pitch, void *dst
                                              dst_seg, rows_to, cols_to, scale_row);
 }
 
-// H or rows of W as a product's operand, packed into `space` if need be.
+// H or rows of W as a product's operand, copied into `space` if need be;
+// rows with scale_row 0 (if it is given) as 0.
 template <typename T>
 Operand<typename ProductOf<T>::P> operand(const T *src, int64_t rows, int64_t cols, int64_t pitch, bool pack,
-                                          void *space, int64_t dk, hipStream_t s)
+                                          void *space, int64_t dk, const float *scale_row, hipStream_t s)
 {
     typedef typename ProductOf<T>::P P;
     constexpr int64_t parts = ProductOf<T>::kParts;
     if (!pack)
-        return Operand<P>{(const P *)src, rows, pitch, 0};
-    run_pack<T, false>(src, rows, cols, pitch, space, parts * dk, dk, rows, dk, nullptr, s);
-    return Operand<P>{(const P *)space, rows, parts * dk, parts > 1 ? dk : 0};
+        return Operand<P>{(const P *)src, rows, cols, pitch, 0};
+    run_pack<T, false>(src, rows, cols, pitch, space, parts * dk, dk, rows, dk, scale_row, s);
+    return Operand<P>{(const P *)space, rows, pad(cols, 8), parts * dk, parts > 1 ? dk : 0};
 }
 
 // Calls f with the number of 16-token tiles that few tokens take.
@@ -625,9 +592,8 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
     with_type(type, [&](auto e) {
         typedef typename decltype(e)::T T;
         typedef typename ProductOf<T>::P P;
-        const int products = ProductOf<T>::kParts == 1 ? 1 : kTermProducts;
         const T *w = (const T *)d_w;
-        const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
+        const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, nullptr, s);
         float2 *part = (float2 *)(work + l.part);
         float *target = (float *)(work + l.target);
         if (n_tokens <= kFew) {
@@ -651,7 +617,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
         int64_t tiles_done = 0;
         for (int64_t v0 = 0; v0 < n_rows; v0 += l.piece) {
             const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
-            const Operand<P> a = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
+            const Operand<P> a = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, nullptr, s);
             StatsEpilogue ep;
             ep.part = part + tiles_done * n_tokens;
             ep.target_logit = target;
@@ -659,7 +625,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
             ep.vocab = (int)rows;
             ep.tokens = (int)n_tokens;
             ep.v0 = v0;
-            run_product<P>(a, b, pad(cols, 8), products, 1, ep, s);
+            run_product<false, false>(a, b, Extent{rows, n_tokens, cols, 1}, ep, s);
             tiles_done += ceil_div(rows, large_tiles(rows, n_tokens, 1) ? 256 : 128);
         }
         run_loss(part, tiles_done, target, d_targets, ignore, n_rows, n_tokens, d_loss, d_lse, s);
@@ -705,15 +671,17 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         typedef typename decltype(e)::T T;
         typedef typename ProductOf<T>::P P;
         constexpr int64_t parts = ProductOf<T>::kParts;
-        const int products = parts == 1 ? 1 : kTermProducts;
         float *const grad = (float *)(work + l.grad), *const scale = (float *)(work + l.scale);
         float *const sum = (float *)(work + l.sum);
         const T *h = (const T *)d_h, *w = (const T *)d_w;
         grad_kernel<<<1, 1024, 0, s>>>(d_grad_loss, d_targets, ignore, n_rows, n_tokens, grad, scale);
-        const Operand<P> hb = operand<T>(h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
-        if (d_dw)  // rows without a target as 0: they may hold NaN
+        // H with the rows without a target as 0 (they may hold NaN, which dW
+        // would take in)
+        const bool few = n_tokens <= kFew;
+        const Operand<P> hb = operand<T>(h, n_tokens, cols, h_pitch, pack || !few, work + l.h, l.dk, grad, s);
+        if (few && d_dw)
             run_pack<T, true>(h, n_tokens, cols, h_pitch, work + l.ht, parts * l.nk, l.nk, l.nk, cols, grad, s);
-        if (n_tokens <= kFew) {
+        if (few) {
             FewArgs<T> f{};
             f.w = w;
             f.w_pitch = w_pitch;
@@ -750,28 +718,23 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                     g);
             });
         }
-        for (int64_t v0 = 0; v0 < n_rows && n_tokens > kFew; v0 += l.piece) {
+        for (int64_t v0 = 0; v0 < n_rows && !few; v0 += l.piece) {
             const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
-            const Operand<P> wa = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
+            const Operand<P> wa = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, nullptr, s);
             ProbEpilogue<T> ep;
             ep.p = (P *)(work + l.p);
-            ep.pt = (P *)(work + l.pt);
-            ep.p_pitch = (int)(parts * l.piece);
-            ep.p_seg = (int)l.piece;
-            ep.pt_pitch = (int)(parts * l.nk);
-            ep.pt_seg = (int)l.nk;
+            ep.pitch = (int)(parts * l.piece);
+            ep.seg = (int)l.piece;
             ep.lse = d_lse;
             ep.grad = grad;
             ep.targets = d_targets;
             ep.v0 = v0;
             ep.rows = (int)rows;
             ep.tokens = (int)n_tokens;
-            ep.tokens_to = (int)l.nk;
-            run_product<P>(wa, hb, pad(cols, 8), products, 1, ep, s);
+            run_product<false, false>(wa, hb, Extent{rows, n_tokens, cols, 1}, ep, s);
+            const Operand<P> pb{(const P *)(work + l.p), n_tokens, pad(rows, 8), parts * l.piece,
+                                parts > 1 ? l.piece : 0};
             if (d_dh) {
-                const int64_t k = pad(rows, kStep);
-                run_pack<T, true>(w + v0 * w_pitch, rows, cols, w_pitch, work + l.wt, parts * l.piece, l.piece, k,
-                                  cols, nullptr, s);
                 SumEpilogue se;
                 se.c = sum;
                 se.pitch = (int)l.sum_pitch;
@@ -779,9 +742,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                 se.cols = (int)cols;
                 se.rows = (int)n_tokens;
                 se.add = v0 > 0;
-                run_product<P>(Operand<P>{(const P *)(work + l.wt), cols, parts * l.piece, parts > 1 ? l.piece : 0},
-                               Operand<P>{(const P *)(work + l.p), n_tokens, parts * l.piece, parts > 1 ? l.piece : 0},
-                               k, products, l.split, se, s);
+                run_product<true, false>(wa, pb, Extent{cols, n_tokens, rows, l.split}, se, s);
             }
             if (d_dw) {
                 OutEpilogue<T> oe;
@@ -790,9 +751,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                 oe.cols = (int)cols;
                 oe.rows = (int)rows;
                 oe.scale = scale;
-                run_product<P>(Operand<P>{(const P *)(work + l.ht), cols, parts * l.nk, parts > 1 ? l.nk : 0},
-                               Operand<P>{(const P *)(work + l.pt), rows, parts * l.nk, parts > 1 ? l.nk : 0},
-                               pad(n_tokens, kStep), products, 1, oe, s);
+                run_product<true, true>(hb, pb, Extent{cols, rows, n_tokens, 1}, oe, s);
             }
         }
         if (d_dh) {
