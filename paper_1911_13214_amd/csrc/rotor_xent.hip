@@ -17,39 +17,55 @@ namespace {
 typedef Tile<256, 256, 2, 4> Large;
 typedef Tile<128, 128, 2, 2> Small;
 
-// dst[c][r] = src[r][c] for rows and columns in range, 0 up to `rows_to` rows
-// of src (and for rows without a target, where targets is given).  64 x 64
-// elements a workgroup, through LDS.  TRANSPOSE false: dst[r][c], 0 up to
-// `cols_to` columns.
-template <typename T, bool TRANSPOSE>
+// dst[r][c] = src[r][c], 0 for columns up to `cols_to` (a multiple of 8) and
+// for rows whose scale is 0 (where scales are given): eight columns a thread.
+template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t rows, int64_t cols, int64_t pitch,
                                                    typename ProductOf<T>::P *dst, int64_t dst_pitch, int64_t dst_seg,
-                                                   int64_t rows_to, int64_t cols_to, const float *scale_row)
+                                                   int64_t cols_to, const float *scale_row)
+{
+    typedef typename ProductOf<T>::P P;
+    constexpr int kParts = ProductOf<T>::kParts;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, pieces = cols_to / 8;
+    const int64_t r = at / pieces, c = at % pieces * 8;
+    if (r >= rows)
+        return;
+    const bool none = scale_row && scale_row[r] == 0.f;
+    typename Mfma<P>::Frag t[kParts];
+    terms_of<T>(row_piece(src + r * pitch, c, none ? 0 : cols), t);
+#pragma unroll
+    for (int q = 0; q < kParts; ++q)
+        *(typename Mfma<P>::Frag *)(dst + r * dst_pitch + q * dst_seg + c) = t[q];
+}
+
+// dst[c][r] = src[r][c] for few tokens, 0 for rows up to `rows_to` and for
+// rows whose scale is 0.
+template <typename T>
+__global__ __launch_bounds__(256) void turn_kernel(const T *src, int64_t rows, int64_t cols, int64_t pitch,
+                                                   typename ProductOf<T>::P *dst, int64_t dst_pitch, int64_t dst_seg,
+                                                   int64_t rows_to, const float *scale_row)
 {
     typedef typename ProductOf<T>::P P;
     constexpr int kParts = ProductOf<T>::kParts;
     __shared__ float tile[64][65];
     const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
     const int x = threadIdx.x % 64, y = threadIdx.x / 64;
+#pragma unroll 4
     for (int k = y; k < 64; k += 4) {
         const int64_t r = r0 + k, c = c0 + x;
-        float v = 0.f;
-        if (r < rows && c < cols && !(scale_row && scale_row[r] == 0.f))
-            v = (float)src[r * pitch + c];
-        tile[k][x] = v;
+        tile[k][x] = r < rows && c < cols && scale_row[r] != 0.f ? (float)src[r * pitch + c] : 0.f;
     }
     __syncthreads();
-    for (int k = y; k < 64; k += 4) {
-        const int64_t r = TRANSPOSE ? r0 + x : r0 + k, c = TRANSPOSE ? c0 + k : c0 + x;
-        const float v = TRANSPOSE ? tile[x][k] : tile[k][x];
-        if (TRANSPOSE ? r >= rows_to || c >= cols : r >= rows || c >= cols_to)
-            continue;
-        P *at = dst + (TRANSPOSE ? c * dst_pitch + r : r * dst_pitch + c);
+    const int64_t r = r0 + x;
+    if (r >= rows_to)
+        return;
+    for (int k = y; k < 64 && c0 + k < cols; k += 4) {
+        P *at = dst + (c0 + k) * dst_pitch + r;
         if constexpr (kParts == 1) {
-            *at = (P)v;
+            *at = (P)tile[x][k];
         } else {
             bf16 t[kTerms];
-            split(v, t);
+            split(tile[x][k], t);
 #pragma unroll
             for (int q = 0; q < kTerms; ++q)
                 at[q * dst_seg] = t[q];
@@ -318,25 +334,38 @@ __global__ __launch_bounds__(1024) void grad_kernel(const float *grad_loss, cons
     }
 }
 
-// dH from its parts' sums.
-template <typename T>
+// dH from its parts' sums: four columns a thread, Y threads a share of the
+// parts each, the shares then in order.
+template <typename T, int Y>
 __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t pitch, int64_t part, int parts,
                                                      int64_t rows, int64_t cols, const float *scale, T *out,
                                                      int64_t out_pitch)
 {
+    constexpr int X = 256 / Y;
+    __shared__ f32x4 other[Y][X];
     const int64_t quads = (cols + 3) / 4;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= rows * quads)
-        return;
-    const int64_t j = at / quads, i = at % quads * 4;
-    f32x4 s = *(const f32x4 *)(sum + j * pitch + i);
-    for (int q = 1; q < parts; ++q)
+    const int x = threadIdx.x % X, y = threadIdx.x / X;
+    const int64_t at = (int64_t)blockIdx.x * X + x;
+    const bool in = at < rows * quads;
+    const int64_t j = in ? at / quads : 0, i = in ? at % quads * 4 : 0;
+    const int each = (parts + Y - 1) / Y, to = (y + 1) * each < parts ? (y + 1) * each : parts;
+    f32x4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int q = y * each; q < to; ++q)
         s += *(const f32x4 *)(sum + q * part + j * pitch + i);
-    const float f = *scale;
-    float v[4];
+    if (Y > 1) {
+        other[y][x] = s;
+        __syncthreads();
+        if (y > 0)
+            return;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        v[e] = s[e] * f;
+        for (int w = 1; w < Y; ++w)
+            s += other[w][x];
+    }
+    if (!in)
+        return;
+    const float f = *scale;
+    const float v[4] = {s[0] * f, s[1] * f, s[2] * f, s[3] * f};
     store_some(out + j * out_pitch + i, cols - i < 4 ? (int)(cols - i) : 4, v);
 }
 
@@ -393,7 +422,7 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
     Bump b;
     const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
     l.dk = pad(d, kStep);
-    l.part = b.take(8ull * (uint64_t)ceil_div(v, n <= kFew ? kFewRows : 128) * (uint64_t)n);
+    l.part = b.take(8ull * (uint64_t)ceil_div(v, n <= kFew ? few_rows(n, v) : 128) * (uint64_t)n);
     l.target = b.take(4ull * (uint64_t)n);
     l.piece = v;
     l.h = l.w = b.at;
@@ -410,7 +439,7 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
 }
 
 struct BackwardLayout {
-    uint64_t grad, scale, h, w, ht, p, sum, total;
+    uint64_t grad, scale, h, w, ht, p, pt, sum, total;
     int64_t dk, piece, nk, sum_pitch;
     int split;
 };
@@ -432,10 +461,11 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
         l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
         l.ht = b.take(2ull * (uint64_t)(parts * l.nk * d));
         l.p = b.take(2ull * (uint64_t)(parts * l.piece * n));
-        // parts of the vocabulary for two workgroups on every CU, of four
+        l.pt = b.take(2ull * (uint64_t)(parts * l.nk * v));
+        // parts of the vocabulary for three workgroups on every CU, of four
         // tiles at least
         const int64_t t = l.piece / kFewRows, most = ceil_div(t, 4);
-        const int64_t want = ceil_div(512, ceil_div(d, kFewCols));
+        const int64_t want = ceil_div(768, ceil_div(d, kFewCols));
         l.split = (int)(want < most ? want : most);
         l.sum = b.take(4ull * (uint64_t)(l.split * n * l.sum_pitch));
         l.w = 0;
@@ -455,7 +485,7 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     l.h = b.take(2ull * (uint64_t)(parts * l.dk * n));
     l.w = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * l.piece) : 0);
     l.p = b.take(2ull * (uint64_t)(parts * l.piece * n));
-    l.ht = 0;
+    l.ht = l.pt = 0;
     // few tiles of dH: its summed index (the piece) in parts, for a large
     // tile on every CU, of eight steps at least
     int64_t split = ceil_div(256, tiles(d, n, 256));
@@ -500,16 +530,6 @@ void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e,
         run_tiles<P, Small, KA, KB, E>(a, b, x, e, s);
 }
 
-template <typename T, bool TRANSPOSE>
-void run_pack(const T *src, int64_t rows, int64_t cols, int64_t pitch, void *dst, int64_t dst_pitch, int64_t dst_seg,
-              int64_t rows_to, int64_t cols_to, const float *scale_row, hipStream_t s)
-{
-    pack_kernel<T, TRANSPOSE><<<dim3((uint32_t)ceil_div(TRANSPOSE ? rows_to : rows, 64),
-                                     (uint32_t)ceil_div(TRANSPOSE ? cols : cols_to, 64)),
-                                256, 0, s>>>(src, rows, cols, pitch, (typename ProductOf<T>::P *)dst, dst_pitch,
-                                             dst_seg, rows_to, cols_to, scale_row);
-}
-
 // H or rows of W as a product's operand, copied into `space` if need be;
 // rows with scale_row 0 (if it is given) as 0.
 template <typename T>
@@ -520,20 +540,28 @@ Operand<typename ProductOf<T>::P> operand(const T *src, int64_t rows, int64_t co
     constexpr int64_t parts = ProductOf<T>::kParts;
     if (!pack)
         return Operand<P>{(const P *)src, rows, cols, pitch, 0};
-    run_pack<T, false>(src, rows, cols, pitch, space, parts * dk, dk, rows, dk, scale_row, s);
+    pack_kernel<T><<<dim3((uint32_t)ceil_div(rows * (dk / 8), 256)), 256, 0, s>>>(
+        src, rows, cols, pitch, (P *)space, parts * dk, dk, dk, scale_row);
     return Operand<P>{(const P *)space, rows, pad(cols, 8), parts * dk, parts > 1 ? dk : 0};
 }
 
-// Calls f with the number of 16-token tiles that few tokens take.
+// Calls f with the number of 16-token tiles that few tokens take and the
+// waves that share the workgroup's rows.
 template <int V> struct IntV { static constexpr int v = V; };
-template <typename F> void with_few(int64_t tokens, F f)
+template <typename F> void with_few(int64_t tokens, int rows, F f)
 {
-    if (tokens <= 16)
-        f(IntV<1>{});
-    else if (tokens <= 32)
-        f(IntV<2>{});
+    const auto split = [&](auto c) {
+        if (rows == 64 * few_row_tiles(decltype(c)::v))
+            f(c, IntV<1>{});
+        else
+            f(c, IntV<4>{});
+    };
+    if (few_tiles(tokens) == 1)
+        split(IntV<1>{});
+    else if (few_tiles(tokens) == 2)
+        split(IntV<2>{});
     else
-        f(IntV<4>{});
+        split(IntV<4>{});
 }
 
 void run_loss(const float2 *part, int64_t tiles, const float *target_logit, const int64_t *targets, int64_t ignore,
@@ -607,9 +635,10 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
             f.targets = d_targets;
             f.part = part;
             f.target_logit = target;
-            const int64_t blocks = ceil_div(n_rows, kFewRows);
-            with_few(n_tokens, [&](auto c) {
-                few_kernel<T, decltype(c)::v, false><<<dim3((uint32_t)blocks), kFewThreads, 0, s>>>(f);
+            const int rows = few_rows(n_tokens, n_rows);
+            const int64_t blocks = ceil_div(n_rows, rows);
+            with_few(n_tokens, rows, [&](auto c, auto kw) {
+                few_kernel<T, decltype(c)::v, decltype(kw)::v, false><<<dim3((uint32_t)blocks), kFewThreads, 0, s>>>(f);
             });
             run_loss(part, blocks, target, d_targets, ignore, n_rows, n_tokens, d_loss, d_lse, s);
             return;
@@ -680,7 +709,8 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         const bool few = n_tokens <= kFew;
         const Operand<P> hb = operand<T>(h, n_tokens, cols, h_pitch, pack || !few, work + l.h, l.dk, grad, s);
         if (few && d_dw)
-            run_pack<T, true>(h, n_tokens, cols, h_pitch, work + l.ht, parts * l.nk, l.nk, l.nk, cols, grad, s);
+            turn_kernel<T><<<dim3((uint32_t)ceil_div(l.nk, 64), (uint32_t)ceil_div(cols, 64)), 256, 0, s>>>(
+                h, n_tokens, cols, h_pitch, (P *)(work + l.ht), parts * l.nk, l.nk, l.nk, grad);
         if (few) {
             FewArgs<T> f{};
             f.w = w;
@@ -692,17 +722,33 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             f.targets = d_targets;
             f.lse = d_lse;
             f.grad = grad;
-            f.scale = scale;
             f.p = d_dh ? (P *)(work + l.p) : nullptr;
             f.p_seg = l.piece;
-            f.ht = (const P *)(work + l.ht);
-            f.dw = (T *)d_dw;
-            f.dw_pitch = dw_pitch;
-            with_few(n_tokens, [&](auto c) {
+            f.pt = d_dw ? (P *)(work + l.pt) : nullptr;
+            f.nk = (int)l.nk;
+            const int rows = few_rows(n_tokens, n_rows);
+            with_few(n_tokens, rows, [&](auto c, auto kw) {
                 constexpr int C = decltype(c)::v;
-                few_kernel<T, C, true><<<dim3((uint32_t)ceil_div(n_rows, kFewRows)), kFewThreads, 0, s>>>(f);
-                if (!d_dh)
-                    return;
+                // all of P, past the rows of W too: the sums take 64 at a time
+                few_kernel<T, C, decltype(kw)::v, true><<<dim3((uint32_t)ceil_div(l.piece, rows)), kFewThreads, 0, s>>>(
+                    f);
+            });
+            if (d_dw) {
+                FewWeightArgs<T> g;
+                g.pt = f.pt;
+                g.ht = (const P *)(work + l.ht);
+                g.scale = scale;
+                g.dw = (T *)d_dw;
+                g.pitch = dw_pitch;
+                g.rows = n_rows;
+                g.cols = cols;
+                // workgroups side by side over the columns until there are
+                // four for each CU
+                const int64_t x = ceil_div(n_rows, kFewRows), most = ceil_div(cols, 256), want = ceil_div(1024, x);
+                const auto kernel = l.nk == 32 ? few_weight_kernel<T, 1> : few_weight_kernel<T, 2>;
+                kernel<<<dim3((uint32_t)x, (uint32_t)(want < most ? want : most)), kFewThreads, 0, s>>>(g);
+            }
+            if (d_dh) {
                 FewSumArgs<T> g;
                 g.w = w;
                 g.w_pitch = w_pitch;
@@ -714,9 +760,11 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                 g.sum = sum;
                 g.sum_pitch = l.sum_pitch;
                 g.tiles = ceil_div(ceil_div(n_rows, kFewRows), l.split);
-                few_sum_kernel<T, C><<<dim3((uint32_t)ceil_div(cols, kFewCols), (uint32_t)l.split), kFewThreads, 0, s>>>(
-                    g);
-            });
+                const auto kernel = few_tiles(n_tokens) == 1   ? few_sum_kernel<T, 1>
+                                    : few_tiles(n_tokens) == 2 ? few_sum_kernel<T, 2>
+                                                               : few_sum_kernel<T, 4>;
+                kernel<<<dim3((uint32_t)ceil_div(cols, kFewCols), (uint32_t)l.split), kFewThreads, 0, s>>>(g);
+            }
         }
         for (int64_t v0 = 0; v0 < n_rows && !few; v0 += l.piece) {
             const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
@@ -756,7 +804,8 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         }
         if (d_dh) {
             const int64_t quads = n_tokens * ceil_div(cols, 4);
-            finish_kernel<T><<<dim3((uint32_t)ceil_div(quads, 256)), 256, 0, s>>>(
+            const auto finish = l.split >= 8 ? finish_kernel<T, 16> : finish_kernel<T, 1>;
+            finish<<<dim3((uint32_t)ceil_div(quads, l.split >= 8 ? 16 : 256)), 256, 0, s>>>(
                 sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, (T *)d_dh, dh_pitch);
         }
     });
