@@ -384,6 +384,7 @@ __global__ __launch_bounds__(kFewThreads) void few_sum_kernel(FewSumArgs<T> a)
     const int64_t t0 = (int64_t)blockIdx.y * a.tiles, t1 = t0 + a.tiles < all ? t0 + a.tiles : all;
     const int lr = threadIdx.x / 16, lc = threadIdx.x % 16 * 8;
     typename VecOf<T, 8>::V raw[4];
+    Frag next[2][C][kParts];  // of P
     auto load = [&](int64_t t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -391,6 +392,15 @@ __global__ __launch_bounds__(kFewThreads) void few_sum_kernel(FewSumArgs<T> a)
             const int64_t r = t * kFewRows + lr + 16 * i;
             raw[i] = row_piece(a.w + (r < a.rows ? r : a.rows - 1) * a.w_pitch, c0 + lc, r < a.rows ? a.cols : 0);
         }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int j = 16 * c + low < a.tokens ? 16 * c + low : a.tokens - 1;
+#pragma unroll
+                for (int q = 0; q < kParts; ++q)
+                    next[s][c][q] = *(const Frag *)(a.p + (j * kParts + q) * a.p_seg + t * kFewRows + 32 * s + 8 * high);
+            }
     };
     f32x4 acc[2][C];
 #pragma unroll
@@ -409,19 +419,19 @@ __global__ __launch_bounds__(kFewThreads) void few_sum_kernel(FewSumArgs<T> a)
             for (int q = 0; q < kParts; ++q)
                 *(Frag *)&tile[q][lr + 16 * i][lc] = s[q];
         }
+        Frag pb[2][C][kParts];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int q = 0; q < kParts; ++q)
+                    pb[s][c][q] = next[s][c][q];
         __syncthreads();
         if (t + 1 < t1)
             load(t + 1);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            Frag pb[C][kParts];
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int j = 16 * c + low < a.tokens ? 16 * c + low : a.tokens - 1;
-#pragma unroll
-                for (int q = 0; q < kParts; ++q)
-                    pb[c][q] = *(const Frag *)(a.p + (j * kParts + q) * a.p_seg + t * kFewRows + 32 * s + 8 * high);
-            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 Frag wa[kParts];
@@ -437,7 +447,7 @@ __global__ __launch_bounds__(kFewThreads) void few_sum_kernel(FewSumArgs<T> a)
 #endif
 #pragma unroll
                 for (int c = 0; c < C; ++c)
-                    acc[i][c] = multiply_terms<P, kParts>(wa, pb[c], acc[i][c]);
+                    acc[i][c] = multiply_terms<P, kParts>(wa, pb[s][c], acc[i][c]);
             }
         }
         __syncthreads();

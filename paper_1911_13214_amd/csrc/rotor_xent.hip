@@ -104,15 +104,20 @@ struct StatsEpilogue {
             // the target's place among this lane's rows, if it is there
             const int64_t t64 = (j < tokens ? targets[j] : -1) - v0 - r.tile_i * S::BI;
             const int t = t64 >= 0 && t64 < S::BI && t64 < have ? (int)t64 - r.i : -1;
+            if (__any(t >= 0 && t < 16 * S::NI)) {  // few tokens have their target in one tile
+#pragma unroll
+                for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (t == 16 * ii + e)
+                            target_logit[j] = r.acc[ii][jj][e];
+            }
             float top = -__builtin_inff();
 #pragma unroll
             for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (t == 16 * ii + e)
-                        target_logit[j] = r.acc[ii][jj][e];
+                for (int e = 0; e < 4; ++e)
                     top = fmaxf(top, r.acc[ii][jj][e]);
-                }
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float m = finite_or_0(top);
