@@ -116,12 +116,57 @@ template <typename S> struct Results {
     int i, j;
     int wave_i, wave_j, lane;
     int part;
+    char *lds;  // the wave's own share of LDS
 };
 
 // Hides where a value comes from, so that what is computed from it stays
 // where it is written: the epilogues' addresses would otherwise be computed
 // before the product's loop and spilled.
 __device__ inline void opaque(int &v) { asm volatile("" : "+v"(v)); }
+
+// Writes a wave's results, rounded to 16 bits, row by row of j: c is the
+// tile's first element, rows and cols what the matrix has from there.  They go
+// through the wave's share of LDS, so that a row's 32 NI bytes are written at
+// once (straight from the registers it would be 32 bytes a row and store);
+// a row's 16-byte pieces change places by the row, for the banks' sake.
+template <typename T, typename S>
+__device__ inline void put_rows(const Results<S> &r, T *c, int pitch, int rows, int cols)
+{
+    typedef T V4 __attribute__((ext_vector_type(4)));
+    typedef T V8 __attribute__((ext_vector_type(8)));
+    constexpr int kRow = S::NI * 32, kPieces = S::NI * 2, kAtOnce = 64 / kPieces;
+    const int low = r.lane % 16, high = r.lane / 16;
+#pragma unroll
+    for (int jj = 0; jj < S::NJ; ++jj)
+#pragma unroll
+        for (int ii = 0; ii < S::NI; ++ii) {
+            V4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = (T)r.acc[ii][jj][e];
+            *(V4 *)(r.lds + (16 * jj + low) * kRow + ((2 * ii + high / 2) ^ (low % kPieces)) * 16 + high % 2 * 8) = v;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    int line = r.lane / kPieces;
+    opaque(line);
+    const int piece = r.lane % kPieces, i = r.wave_i * S::NI * 16 + piece * 8;
+#pragma unroll
+    for (int k = 0; k < S::NJ * 16 / kAtOnce; ++k) {
+        const int row = line + k * kAtOnce, j = r.wave_j * S::NJ * 16 + row;
+        const V8 v = *(const V8 *)(r.lds + row * kRow + (piece ^ (row % 16 % kPieces)) * 16);
+        if (j < rows) {
+            T *const at = c + (uint32_t)(j * pitch + i);
+            if (i + 8 <= cols)
+                *(typename VecOf<T, 8>::V *)at = v;
+            else
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (i + e < cols)
+                        at[e] = v[e];
+        }
+    }
+}
 
 // Tile order: the eight XCDs (workgroups go to them in turn) take contiguous
 // runs, so that what neighbours share stays in one XCD's L2; in a run four
@@ -384,6 +429,8 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     res.i = wi * S::NI * 16 + lane / 16 * 4;
     res.j = wj * S::NJ * 16 + lane % 16;
     res.part = blockIdx.y;
+    constexpr int kShare = 2 * S::kBytes / S::kWaves;
+    res.lds = wave < S::kWaves / 2 ? even + wave * kShare : odd + (wave - S::kWaves / 2) * kShare;
     opaque(res.i);
     opaque(res.j);
     epilogue(res, even);

@@ -166,33 +166,29 @@ template <typename T> struct ProbEpilogue {
             int row = r.j + 16 * jj;
             opaque(row);
             const int j = j0 + row;
-            if (j >= tokens)
-                continue;
-            const float g = grad[j], l = lse[j];
-            const int64_t t64 = targets[j] - v0 - r.tile_i * S::BI;
+            const bool in = j < tokens;
+            const float g = in ? grad[j] : 0.f, l = in ? lse[j] : 0.f;
+            const int64_t t64 = (in ? targets[j] : -1) - v0 - r.tile_i * S::BI;
             const int t = t64 >= 0 && t64 < S::BI ? (int)t64 - r.i : -1;
 #pragma unroll
-            for (int ii = 0; ii < S::NI; ++ii) {
-                float v[4];
+            for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = __expf(r.acc[ii][jj][e] - l) - (t == 16 * ii + e ? 1.f : 0.f);
+                    const float v = __expf(r.acc[ii][jj][e] - l) - (t == 16 * ii + e ? 1.f : 0.f);
                     // a select: what a token without a target holds may be NaN
-                    v[e] = g != 0.f && r.i + 16 * ii + e < have ? v[e] * g : 0.f;
+                    r.acc[ii][jj][e] = g != 0.f && r.i + 16 * ii + e < have ? v * g : 0.f;
                 }
-                P *const at = tile + (uint32_t)(row * pitch + r.i + 16 * ii);
-                if constexpr (kParts == 1) {
-                    V4 w;
+            if constexpr (kParts > 1) {
+                if (!in)
+                    continue;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        w[e] = (P)v[e];
-                    *(V4 *)at = w;
-                } else {
+                for (int ii = 0; ii < S::NI; ++ii) {
+                    P *const at = tile + (uint32_t)(row * pitch + r.i + 16 * ii);
                     V4 w[kTerms];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         bf16 s[kTerms];
-                        split(v[e], s);
+                        split(r.acc[ii][jj][e], s);
 #pragma unroll
                         for (int q = 0; q < kTerms; ++q)
                             w[q][e] = s[q];
@@ -203,6 +199,8 @@ template <typename T> struct ProbEpilogue {
                 }
             }
         }
+        if constexpr (kParts == 1)
+            put_rows(r, tile, pitch, tokens - j0, S::BI);
     }
 };
 
@@ -240,31 +238,30 @@ template <typename T> struct OutEpilogue {
     int pitch, cols, rows;
     template <typename S> __device__ void operator()(Results<S> &r, char *) const
     {
-        typedef typename VecOf<T, 4>::V V4;
         const float f = *scale;
         T *const tile = c + (int64_t)r.tile_j * S::BJ * pitch + r.tile_i * S::BI;
         const int cols_in = cols - r.tile_i * S::BI, rows_in = rows - r.tile_j * S::BJ;
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int jj = 0; jj < S::NJ; ++jj) {
-            int j = r.j + 16 * jj;
-            opaque(j);
-            if (j >= rows_in)
-                continue;
+            for (int jj = 0; jj < S::NJ; ++jj)
 #pragma unroll
-            for (int ii = 0; ii < S::NI; ++ii) {
-                const int i = r.i + 16 * ii;
-                T *const at = tile + (uint32_t)(j * pitch + i);
-                if (i + 4 <= cols_in) {
-                    V4 v;
+                for (int ii = 0; ii < S::NI; ++ii)
+                    r.acc[ii][jj] *= f;
+            put_rows(r, tile, pitch, rows_in, cols_in);
+        } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[e] = (T)(r.acc[ii][jj][e] * f);
-                    *(V4 *)at = v;
-                } else {
+            for (int jj = 0; jj < S::NJ; ++jj) {
+                int j = r.j + 16 * jj;
+                opaque(j);
+                if (j >= rows_in)
+                    continue;
 #pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (i + e < cols_in)
-                            at[e] = (T)(r.acc[ii][jj][e] * f);
+                for (int ii = 0; ii < S::NI; ++ii) {
+                    const int i = r.i + 16 * ii, left = cols_in - i < 4 ? cols_in - i : 4;
+                    const float v[4] = {r.acc[ii][jj][0] * f, r.acc[ii][jj][1] * f, r.acc[ii][jj][2] * f,
+                                        r.acc[ii][jj][3] * f};
+                    if (left > 0)
+                        store_some(tile + (uint32_t)(j * pitch + i), left, v);
                 }
             }
         }
