@@ -253,7 +253,7 @@ template <typename T, int SIDE, int LOADS, int N> struct Loader<T, SIDE, LOADS, 
     const T *start;
     int64_t cols;
     uint32_t at[LOADS];
-    int first, base, sw, slot;
+    int first, base;
     static __device__ int turn(int row) { return (row & 3) | (row >> 3 & 1) << 2; }
     __device__ void init(const Operand<T> &o, int64_t side0, int wave, int lane, int wave_side)
     {
@@ -266,9 +266,10 @@ template <typename T, int SIDE, int LOADS, int N> struct Loader<T, SIDE, LOADS, 
         }
         first = wave * LOADS * 1024;
         const int g = lane / 16, i = lane % 16;
-        base = (g * 8 + i / 4) * kRow + i % 4 * 8;
-        sw = turn(g * 8 + i / 4);
-        slot = wave_side * N;
+        // bits 5 to 7 hold the place of the wave's first slot of 32 bytes: its
+        // n-th is at base ^ (32 n)
+        const int slot = wave_side * N;
+        base = (g * 8 + i / 4) * kRow + i % 4 * 8 + ((slot & ~7) | ((slot & 7) ^ turn(g * 8 + i / 4))) * 32;
     }
     __device__ void load(const Operand<T> &o, char *lds, int64_t term, int step, bool live) const
     {
@@ -284,7 +285,7 @@ template <typename T, int SIDE, int LOADS, int N> struct Loader<T, SIDE, LOADS, 
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const char *p = lds + base + ((slot + n) ^ sw) * 32 + h * 32 * kRow;
+            const char *p = lds + (base ^ (n * 32)) + h * 32 * kRow;
             f[n] = __builtin_bit_cast(typename Mfma<T>::Frag,
                                       __builtin_shufflevector(turned(p), turned(p + 4 * kRow), 0, 1, 2, 3, 4, 5, 6,
                                                               7));
