@@ -16,6 +16,7 @@ scratch a call allocates is returned to torch's caching allocator on
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -105,24 +106,36 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+@functools.lru_cache(maxsize=None)
+def _entry(name):
+    return getattr(rotor.lib(), name)
+
+
 def _call(name, device, stream, *args):
     """One entry point of the library, on ``stream`` or the device's current
     stream."""
-    fn = getattr(rotor.lib(), name)
     index = device.index
     raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
     if index == torch._C._cuda_getDevice():
-        status = fn(*args, raw)
+        status = _entry(name)(*args, raw)
     else:
         with torch.cuda.device(device):
-            status = fn(*args, raw)
+            status = _entry(name)(*args, raw)
     if status != rotor.ROTOR_OK:
         raise rotor.RotorError(status, name)
 
 
-def _scratch(nbytes, device, stream):
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(name, *sizes):
+    """Workspace of an entry point for these sizes (a function of them alone)."""
+    need = ctypes.c_uint64()
+    rotor._check(_entry(name)(*sizes, ctypes.byref(need)), name)
+    return need.value
+
+
+def _scratch(nbytes, like, stream):
     """Device scratch of a call, returned to the allocator on ``stream``."""
-    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    work = like.new_empty(max(nbytes, 16), dtype=torch.uint8)
     if stream is not None:
         work.record_stream(stream)
     return work
@@ -147,11 +160,15 @@ def dropout(x, p, seed, step=0, residual=None, *, step_tensor=None, out=None, st
     y = _out(out, x, "out")
     if residual is not None:
         _like(residual, x, "residual")
-    if x.numel() == 0:
+    n = x.numel()
+    if n == 0:
         return y
-    rows, cols, xp = _matrix(x, "x")
-    _, _, yp = _matrix(y, "out")
-    rp = _matrix(residual, "residual")[2] if residual is not None else cols
+    if x.is_contiguous() and y.is_contiguous() and (residual is None or residual.is_contiguous()):
+        rows, cols, xp, yp, rp = 1, n, n, n, n
+    else:
+        rows, cols, xp = _matrix(x, "x")
+        _, _, yp = _matrix(y, "out")
+        rp = _matrix(residual, "residual")[2] if residual is not None else cols
     _call("rotor_dropout", x.device, stream, code, rows, cols, x.data_ptr(), xp, _ptr(residual), rp, y.data_ptr(), yp,
           p, seed & 0xFFFFFFFFFFFFFFFF, step & 0xFFFFFFFFFFFFFFFF, _ptr(step_tensor))
     return y
@@ -192,10 +209,7 @@ def embedding_backward(tokens, grad, n_rows, scale=1.0, *, padding=None, out=Non
         raise ValueError(f"grad must have shape {tuple(tokens.shape)} + (cols,)")
     n, (_, cols, pitch) = tokens.numel(), _matrix(grad, "grad")
     out = _out(out, grad, "out", (n_rows, cols))
-    need = ctypes.c_uint64()
-    rotor._check(rotor.lib().rotor_embedding_workspace_bytes(n, n_rows, cols, ctypes.byref(need)),
-                 "rotor_embedding_workspace_bytes")
-    work = _scratch(need.value, grad.device, stream)
+    work = _scratch(_workspace_bytes("rotor_embedding_workspace_bytes", n, n_rows, cols), grad, stream)
     _call("rotor_embedding_backward", grad.device, stream, code, n, n_rows, cols, _ptr(tokens), size, _ptr(grad),
           pitch, scale, -1 if padding is None else padding, out.data_ptr(), _matrix(out, "out")[2], work.data_ptr(),
           work.numel())
@@ -253,7 +267,7 @@ def residual_norm(x, z=None, *, post="none", post_weight=None, post_bias=None, g
     copy = z is not None or residual_scale != 1.0
     y = _empty(x) if copy else x
     h = _empty(x) if pre != "none" else None
-    st = torch.empty((n.rows, 4), dtype=torch.float32, device=x.device) if stats else None
+    st = x.new_empty((n.rows, 4), dtype=torch.float32) if stats else None
     _call("rotor_residual_norm", x.device, stream, ctypes.byref(n), x.data_ptr(), xp, _ptr(z), zp,
           y.data_ptr() if copy else None, n.cols, _ptr(h), n.cols, _ptr(st))
     return y, h, st
@@ -290,9 +304,9 @@ def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None
             g[name] = _empty(q)
     out = _NormGrads(gate_pitch=n.cols, **{k: g[k].data_ptr() for k in g if k not in ("x", "z")})
     need = ctypes.c_uint64()
-    rotor._check(rotor.lib().rotor_residual_norm_workspace_bytes(ctypes.byref(n), ctypes.byref(need)),
+    rotor._check(_entry("rotor_residual_norm_workspace_bytes")(ctypes.byref(n), ctypes.byref(need)),
                  "rotor_residual_norm_workspace_bytes")
-    work = _scratch(need.value, lead.device, stream)
+    work = _scratch(need.value, lead, stream)
     _call("rotor_residual_norm_backward", lead.device, stream, ctypes.byref(n), *matrix(dy, "dy"), *matrix(dh, "dh"),
           *(matrix(y, "y") if dh is not None else (None, n.cols)), *matrix(z, "z"), stats.data_ptr(),
           g["x"].data_ptr(), n.cols, _ptr(g.get("z")), n.cols, ctypes.byref(out), work.data_ptr(), work.numel())
@@ -319,10 +333,8 @@ def _xent(h, w, targets, backward, stream):
     if rows < 1 or n > XENT_MAX_TOKENS or cols > XENT_MAX_COLS:
         raise ValueError(f"at most {XENT_MAX_TOKENS} tokens and {XENT_MAX_COLS} columns, and at least one row of w")
     aligned = int(not (cols % 8 or hp % 8 or wp % 8 or h.data_ptr() % 16 or w.data_ptr() % 16))
-    need = ctypes.c_uint64()
-    rotor._check(rotor.lib().rotor_xent_workspace_bytes(code, n, cols, rows, aligned, backward, ctypes.byref(need)),
-                 "rotor_xent_workspace_bytes")
-    return code, n, cols, rows, hp, wp, aligned, _scratch(need.value, h.device, stream)
+    need = _workspace_bytes("rotor_xent_workspace_bytes", code, n, cols, rows, aligned, backward)
+    return code, n, cols, rows, hp, wp, aligned, _scratch(need, h, stream)
 
 
 def _per_token(t, targets, what):
