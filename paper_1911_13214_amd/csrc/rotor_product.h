@@ -126,45 +126,53 @@ __device__ inline void opaque(int &v) { asm volatile("" : "+v"(v)); }
 
 // Writes a wave's results, rounded to 16 bits, row by row of j: c is the
 // tile's first element, rows and cols what the matrix has from there.  They go
-// through the wave's share of LDS, so that a row's 32 NI bytes are written at
-// once (straight from the registers it would be 32 bytes a row and store);
-// a row's 16-byte pieces change places by the row, for the banks' sake.
+// through the wave's share of LDS, half of them at a time, so that a row's 32
+// NI bytes are written at once (straight from the registers it would be 32
+// bytes a row and store); a row's 16-byte pieces change places by the row, for
+// the banks' sake.
 template <typename T, typename S>
 __device__ inline void put_rows(const Results<S> &r, T *c, int pitch, int rows, int cols)
 {
     typedef T V4 __attribute__((ext_vector_type(4)));
     typedef T V8 __attribute__((ext_vector_type(8)));
-    constexpr int kRow = S::NI * 32, kPieces = S::NI * 2, kAtOnce = 64 / kPieces;
+    constexpr int kRow = S::NI * 32, kPieces = S::NI * 2, kAtOnce = 64 / kPieces, kHalf = S::NJ / 2;
+    static_assert(kHalf * 16 * kRow <= S::kBytes / S::kWaves, "the wave's share of LDS");
     const int low = r.lane % 16, high = r.lane / 16;
-#pragma unroll
-    for (int jj = 0; jj < S::NJ; ++jj)
-#pragma unroll
-        for (int ii = 0; ii < S::NI; ++ii) {
-            V4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = (T)r.acc[ii][jj][e];
-            *(V4 *)(r.lds + (16 * jj + low) * kRow + ((2 * ii + high / 2) ^ (low % kPieces)) * 16 + high % 2 * 8) = v;
-        }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
     int line = r.lane / kPieces;
     opaque(line);
     const int piece = r.lane % kPieces, i = r.wave_i * S::NI * 16 + piece * 8;
 #pragma unroll
-    for (int k = 0; k < S::NJ * 16 / kAtOnce; ++k) {
-        const int row = line + k * kAtOnce, j = r.wave_j * S::NJ * 16 + row;
-        const V8 v = *(const V8 *)(r.lds + row * kRow + (piece ^ (row % 16 % kPieces)) * 16);
-        if (j < rows) {
-            T *const at = c + (uint32_t)(j * pitch + i);
-            if (i + 8 <= cols)
-                *(typename VecOf<T, 8>::V *)at = v;
-            else
+    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (i + e < cols)
-                        at[e] = v[e];
+        for (int jj = 0; jj < kHalf; ++jj)
+#pragma unroll
+            for (int ii = 0; ii < S::NI; ++ii) {
+                V4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = (T)r.acc[ii][half * kHalf + jj][e];
+                *(V4 *)(r.lds + (16 * jj + low) * kRow + ((2 * ii + high / 2) ^ (low % kPieces)) * 16 +
+                        high % 2 * 8) = v;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < kHalf * 16 / kAtOnce; ++k) {
+            const int row = line + k * kAtOnce, j = (r.wave_j * S::NJ + half * kHalf) * 16 + row;
+            const V8 v = *(const V8 *)(r.lds + row * kRow + (piece ^ (row % 16 % kPieces)) * 16);
+            if (j < rows) {
+                T *const at = c + (uint32_t)(j * pitch + i);
+                if (i + 8 <= cols)
+                    *(typename VecOf<T, 8>::V *)at = v;
+                else
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (i + e < cols)
+                            at[e] = v[e];
+            }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -318,19 +326,16 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     __shared__ __attribute__((aligned(1024))) char odd[S::kBytes];
     typedef typename Mfma<T>::Frag Frag;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    int ti, tj;
-    tile_of(blockIdx.x, p.tiles_i, p.tiles_j, ti, tj);
     const int wi = wave / S::WJ, wj = wave % S::WJ;
-
-    Loader<T, S::BI, S::kLoadsA, S::NI, KA> la;
-    Loader<T, S::BJ, S::kLoadsB, S::NJ, KB> lb;
-    la.init(a, (int64_t)ti * S::BI, wave, lane, wi);
-    lb.init(b, (int64_t)tj * S::BJ, wave, lane, wj);
     constexpr int kB = S::BI * kRowBytes;  // LDS byte of B's part
     const int per = (int)((p.k + kStep - 1) / kStep);
     const int t0 = blockIdx.y * p.split_steps;
     const int t1 = t0 + p.split_steps < p.steps ? t0 + p.split_steps : p.steps;
-    int s = kTermProducts - p.products + t0 / per, at = t0 % per;  // of the next load
+    const int tiles = p.tiles_i * p.tiles_j;
+
+    int ti, tj, s, at;  // the tile; product and step of the next load
+    Loader<T, S::BI, S::kLoadsA, S::NI, KA> la;
+    Loader<T, S::BJ, S::kLoadsB, S::NJ, KB> lb;
     auto load = [&](char *lds, bool live) {
         la.load(a, lds, term_a(s) * a.seg, at, live);
         lb.load(b, lds + kB, term_b(s) * b.seg, at, live);
@@ -339,13 +344,17 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
             ++s;
         }
     };
+    auto begin = [&](int id) {
+        tile_of(id, p.tiles_i, p.tiles_j, ti, tj);
+        la.init(a, (int64_t)ti * S::BI, wave, lane, wi);
+        lb.init(b, (int64_t)tj * S::BJ, wave, lane, wj);
+        s = kTermProducts - p.products + t0 / per;
+        at = t0 % per;
+        if (t0 < t1)
+            load(even, true);
+    };
 
     Results<S> res;
-#pragma unroll
-    for (int ii = 0; ii < S::NI; ++ii)
-#pragma unroll
-        for (int jj = 0; jj < S::NJ; ++jj)
-            res.acc[ii][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
     Frag fa[S::NI], fb[S::NJ];
     auto read = [&](const char *lds, int h) {  // half h of a step: 32 of k
         lb.read(lds + kB, h, fb);
@@ -361,80 +370,90 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
         __builtin_amdgcn_s_setprio(0);
     };
 
-    // an odd number of steps is followed by one of zeros: one way out of the
-    // loop, so that the sums stay where they are
-    if constexpr (S::kWaves == 8) {
-        // Two groups of four waves, one on each SIMD, half a phase apart:
-        // while one multiplies what it holds (32 of k), the other reads its
-        // next operands from LDS.  Every phase has two barriers; the second
-        // group starts one barrier later and ends one earlier.  A step's
-        // place in LDS is written again one barrier after the other group's
-        // last read of it, and the loads into it are waited for three phases
-        // later, one barrier before its first read.
-        const bool late = wave >= 4;
-        auto phase = [&](const char *lds, int h, char *next, bool live) {
-            read(lds, h);
-            __builtin_amdgcn_sched_barrier(0);
-            if (next)
-                load(next, live);
-            if (h == 1 && late)
-                phase_barrier<kWaitAll>();
-            else
-                phase_barrier<kWaitLds>();
-            multiply();
-            if (h == 1 && !late)
-                phase_barrier<kWaitAll>();
-            else
-                phase_barrier<kWaitNone>();
-        };
-        if (t0 < t1)
-            load(even, true);
-        phase_barrier<kWaitAll>();
-        if (late)
-            phase_barrier<kWaitNone>();
-        for (int t = t0; t < t1; t += 2) {
-            phase(even, 0, odd, t + 1 < t1);
-            phase(even, 1, nullptr, false);
-            phase(odd, 0, even, t + 2 < t1);
-            phase(odd, 1, nullptr, false);
-        }
-        if (!late)
-            phase_barrier<kWaitNone>();
-        __syncthreads();
-    } else {
-        if (t0 < t1)
-            load(even, true);
-        __syncthreads();
-        auto step = [&](const char *lds) {
+    // A workgroup takes every gridDim.x-th tile; the next one's first step is
+    // loaded while the epilogue works.
+    begin(blockIdx.x);
+    for (int id = blockIdx.x;;) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+        for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+            for (int jj = 0; jj < S::NJ; ++jj)
+                res.acc[ii][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // an odd number of steps is followed by one of zeros: one way out of
+        // the loop, so that the sums stay where they are
+        if constexpr (S::kWaves == 8) {
+            // Two groups of four waves, one on each SIMD, half a phase apart:
+            // while one multiplies what it holds (32 of k), the other reads
+            // its next operands from LDS.  Every phase has two barriers; the
+            // second group starts one barrier later and ends one earlier.  A
+            // step's place in LDS is written again one barrier after the
+            // other group's last read of it, and the loads into it are waited
+            // for three phases later, one barrier before its first read.
+            const bool late = wave >= 4;
+            auto phase = [&](const char *lds, int h, char *next, bool live) {
                 read(lds, h);
+                __builtin_amdgcn_sched_barrier(0);
+                if (next)
+                    load(next, live);
+                if (h == 1 && late)
+                    phase_barrier<kWaitAll>();
+                else
+                    phase_barrier<kWaitLds>();
                 multiply();
+                if (h == 1 && !late)
+                    phase_barrier<kWaitAll>();
+                else
+                    phase_barrier<kWaitNone>();
+            };
+            phase_barrier<kWaitAll>();
+            if (late)
+                phase_barrier<kWaitNone>();
+            for (int t = t0; t < t1; t += 2) {
+                phase(even, 0, odd, t + 1 < t1);
+                phase(even, 1, nullptr, false);
+                phase(odd, 0, even, t + 2 < t1);
+                phase(odd, 1, nullptr, false);
             }
-        };
-        for (int t = t0; t < t1; t += 2) {
-            load(odd, t + 1 < t1);
-            step(even);
+            if (!late)
+                phase_barrier<kWaitNone>();
             __syncthreads();
-            if (t + 2 < t1)
-                load(even, true);
-            step(odd);
+        } else {
+            auto step = [&](const char *lds) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    read(lds, h);
+                    multiply();
+                }
+            };
             __syncthreads();
+            for (int t = t0; t < t1; t += 2) {
+                load(odd, t + 1 < t1);
+                step(even);
+                __syncthreads();
+                if (t + 2 < t1)
+                    load(even, true);
+                step(odd);
+                __syncthreads();
+            }
         }
+        res.tile_i = ti;
+        res.tile_j = tj;
+        res.wave_i = wi;
+        res.wave_j = wj;
+        res.lane = lane;
+        res.i = wi * S::NI * 16 + lane / 16 * 4;
+        res.j = wj * S::NJ * 16 + lane % 16;
+        res.part = blockIdx.y;
+        res.lds = odd + wave * (S::kBytes / S::kWaves);
+        id += gridDim.x;
+        if (id < tiles)
+            begin(id);
+        opaque(res.i);
+        opaque(res.j);
+        epilogue(res, odd);
+        if (id >= tiles)
+            return;
     }
-    res.tile_i = ti;
-    res.tile_j = tj;
-    res.wave_i = wi;
-    res.wave_j = wj;
-    res.lane = lane;
-    res.i = wi * S::NI * 16 + lane / 16 * 4;
-    res.j = wj * S::NJ * 16 + lane % 16;
-    res.part = blockIdx.y;
-    constexpr int kShare = 2 * S::kBytes / S::kWaves;
-    res.lds = wave < S::kWaves / 2 ? even + wave * kShare : odd + (wave - S::kWaves / 2) * kShare;
-    opaque(res.i);
-    opaque(res.j);
-    epilogue(res, even);
 #endif
 }
 

@@ -516,8 +516,11 @@ void run_tiles(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, h
     p.tiles_j = (int)ceil_div(x.nj, S::BJ);
     p.steps = p.products * (int)ceil_div(x.k, kStep);
     p.split_steps = (int)ceil_div(p.steps, x.split);
-    product_kernel<P, S, KA, KB, E><<<dim3((uint32_t)((int64_t)p.tiles_i * p.tiles_j), (uint32_t)x.split),
-                                      S::kThreads, 0, s>>>(a, b, p, e);
+    // as many workgroups as the 256 CUs hold at once (by their LDS)
+    const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j, most = 256 * ((160 << 10) / (2 * S::kBytes)) / x.split;
+    product_kernel<P, S, KA, KB, E>
+        <<<dim3((uint32_t)(tiles < most || most < 8 ? tiles : most / 8 * 8), (uint32_t)x.split), S::kThreads, 0, s>>>(
+            a, b, p, e);
 }
 
 // Large tiles if they fill half of the 256 CUs, else small ones.
