@@ -578,15 +578,17 @@ ROTOR_API int32_t rotor_residual_norm_backward(const rotor_norm *how, const void
  *   d_work      DEVICE scratch of rotor_xent_workspace_bytes (same sizes,
  *               `aligned` and direction), 16-byte aligned.
  * 0 <= n_tokens <= ROTOR_XENT_MAX_TOKENS, 1 <= cols <= ROTOR_XENT_MAX_COLS,
- * 1 <= n_rows < 2^28, pitches at most 2^22.  Return ROTOR_OK, ROTOR_EINVAL or
+ * 1 <= n_rows <= ROTOR_XENT_MAX_ROWS, pitches at most 2^22.  Return ROTOR_OK, ROTOR_EINVAL or
  * ROTOR_EDEVICE. */
 #define ROTOR_XENT_MAX_TOKENS (1 << 20)
 #define ROTOR_XENT_MAX_COLS 65536
+#define ROTOR_XENT_MAX_ROWS (1 << 26)
 
 /* Device workspace of rotor_xent (backward 0) or rotor_xent_backward (1).
- * Forward: 8 bytes per token and 128 rows of w.  Backward: at most about
- * 512 MB for a piece of the probabilities (more past 500 000 tokens), a copy
- * of that piece of w and of h, 32-bit sums for dh.  Host only. */
+ * Forward: 8 bytes per token and 128 rows of w.  Backward: at most 128 MiB
+ * for a piece of the probabilities (256 rows of w at least; up to 64 tokens:
+ * 256 MiB), a copy of h, 32-bit sums for dh.  Where operands are copied, at
+ * most 128 MiB for a piece of w as well.  Host only. */
 ROTOR_API int32_t rotor_xent_workspace_bytes(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
                                              int32_t aligned, int32_t backward, uint64_t *bytes);
 

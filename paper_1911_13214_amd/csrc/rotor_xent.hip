@@ -383,7 +383,7 @@ template <typename T> __global__ __launch_bounds__(256) void clear_kernel(T *out
 // ---- plans --------------------------------------------------------------------------
 
 constexpr int64_t kPad = 256;                        // columns of P in whole tiles
-constexpr int64_t kPieceBytes = (int64_t)256 << 20;  // of P, or of a copied piece of W
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of P, or of a copied piece of W
 
 int64_t pad(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
 
@@ -400,7 +400,7 @@ struct Bump {
 bool xent_sizes_ok(int32_t type, int64_t n, int64_t d, int64_t v)
 {
     return type_ok(type) && n >= 0 && n <= ROTOR_XENT_MAX_TOKENS && d >= 1 && d <= ROTOR_XENT_MAX_COLS && v >= 1 &&
-           v < ((int64_t)1 << 28);
+           v <= ROTOR_XENT_MAX_ROWS;
 }
 
 // The largest pitch, in elements, with which 256 rows lie within 2^31 bytes.
@@ -410,6 +410,14 @@ constexpr int64_t kMostPitch = (int64_t)1 << 22;
 bool rows_aligned(const void *p, int64_t cols, int64_t pitch)
 {
     return (uintptr_t)p % 16 == 0 && cols % 8 == 0 && pitch % 8 == 0;
+}
+
+// Whether a call goes the way of few tokens: that of the probabilities as a
+// whole, in two layouts, if those are no larger than two pieces.
+bool few_tokens(int32_t type, int64_t n, int64_t v)
+{
+    const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
+    return n <= kFew && 2 * 2 * parts * kFew * v <= 2 * kPieceBytes;
 }
 
 struct ForwardLayout {
@@ -424,11 +432,11 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
     Bump b;
     const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
     l.dk = pad(d, kStep);
-    l.part = b.take(8ull * (uint64_t)ceil_div(v, n <= kFew ? few_rows(n, v) : 128) * (uint64_t)n);
+    l.part = b.take(8ull * (uint64_t)ceil_div(v, few_tokens(type, n, v) ? few_rows(n, v) : 128) * (uint64_t)n);
     l.target = b.take(4ull * (uint64_t)n);
     l.piece = v;
     l.h = l.w = b.at;
-    if (n <= kFew) {
+    if (few_tokens(type, n, v)) {
         l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
     } else if (pack) {
         const int64_t most = kPieceBytes / (2 * parts * l.dk) / kPad * kPad;  // at least kPad: see the limits
@@ -457,7 +465,7 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     l.sum_pitch = pad(d, 4);
     l.grad = b.take(4ull * (uint64_t)n);
     l.scale = b.take(4);
-    if (n <= kFew) {
+    if (few_tokens(type, n, v)) {
         l.nk = n <= 32 ? 32 : 64;
         l.piece = pad(v, kFewRows);
         l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
@@ -476,9 +484,10 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     }
     l.nk = n;
     l.piece = pad(v, kPad);
-    int64_t most = kPieceBytes / (2 * parts * n) / kPad * kPad;
-    if (most < kPad)
-        most = kPad;
+    int64_t most = kPieceBytes / (2 * parts * (pack && l.dk > n ? l.dk : n));
+    if (most > kMostPitch / parts)
+        most = kMostPitch / parts;
+    most = most < kPad ? kPad : most / kPad * kPad;
     if (l.piece > most) {
         // pieces of equal size
         const int64_t count = ceil_div(l.piece, most);
@@ -523,8 +532,16 @@ void run_tiles(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, h
             a, b, p, e);
 }
 
-// Large tiles if they fill half of the 256 CUs, else small ones.
-bool large_tiles(int64_t a, int64_t b, int split) { return tiles(a, b, 256) * split >= 128; }
+// Large tiles if they fill half of the 256 CUs and neither side fits a small
+// one.  Measured, forward and backward, large against small: 171 tokens x
+// 15156 x 1088 107 against 114 us at 120 large tiles, 2000 x 30000 x 64 205
+// against 178 us at under 100; 70 x 50000 x 2048 267 against 239 us, 4096 x
+// 50000 x 128 733 against 695 us, where half a large tile's work would go
+// unused.
+bool large_tiles(int64_t a, int64_t b, int split)
+{
+    return tiles(a, b, 256) * split >= 128 && a > 128 && b > 128;
+}
 
 template <bool KA, bool KB, typename P, typename E>
 void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, hipStream_t s)
@@ -629,7 +646,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
         const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, nullptr, s);
         float2 *part = (float2 *)(work + l.part);
         float *target = (float *)(work + l.target);
-        if (n_tokens <= kFew) {
+        if (few_tokens(type, n_tokens, n_rows)) {
             FewArgs<T> f{};
             f.w = w;
             f.w_pitch = w_pitch;
@@ -711,7 +728,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         grad_kernel<<<1, 1024, 0, s>>>(d_grad_loss, d_targets, ignore, n_rows, n_tokens, grad, scale);
         // H with the rows without a target as 0 (they may hold NaN, which dW
         // would take in)
-        const bool few = n_tokens <= kFew;
+        const bool few = few_tokens(type, n_tokens, n_rows);
         const Operand<P> hb = operand<T>(h, n_tokens, cols, h_pitch, pack || !few, work + l.h, l.dk, grad, s);
         if (few && d_dw)
             turn_kernel<T><<<dim3((uint32_t)ceil_div(l.nk, 64), (uint32_t)ceil_div(cols, 64)), 256, 0, s>>>(

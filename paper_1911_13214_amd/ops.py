@@ -315,7 +315,7 @@ def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None
 
 # ---- cross entropy ---------------------------------------------------------------------
 
-XENT_MAX_TOKENS, XENT_MAX_COLS = 1 << 20, 65536
+XENT_MAX_TOKENS, XENT_MAX_COLS, XENT_MAX_ROWS = 1 << 20, 65536, 1 << 26
 
 
 def _xent(h, w, targets, backward, stream):
@@ -330,8 +330,9 @@ def _xent(h, w, targets, backward, stream):
         raise ValueError(f"targets must be contiguous int64 on {h.device}, one for each row of h")
     n, cols, hp = _matrix(h, "h")
     rows, _, wp = _matrix(w, "w")
-    if rows < 1 or n > XENT_MAX_TOKENS or cols > XENT_MAX_COLS:
-        raise ValueError(f"at most {XENT_MAX_TOKENS} tokens and {XENT_MAX_COLS} columns, and at least one row of w")
+    if not 1 <= rows <= XENT_MAX_ROWS or n > XENT_MAX_TOKENS or cols > XENT_MAX_COLS:
+        raise ValueError(f"at most {XENT_MAX_TOKENS} tokens, {XENT_MAX_COLS} columns, {XENT_MAX_ROWS} rows of w, and "
+                         "at least one")
     aligned = int(not (cols % 8 or hp % 8 or wp % 8 or h.data_ptr() % 16 or w.data_ptr() % 16))
     need = _workspace_bytes("rotor_xent_workspace_bytes", code, n, cols, rows, aligned, backward)
     return code, n, cols, rows, hp, wp, aligned, _scratch(need, h, stream)

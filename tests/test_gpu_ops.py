@@ -646,3 +646,24 @@ def test_cross_entropy_over_pieces_of_the_vocabulary(dtype, n, rows, cols):
     h, w, t, gl = xent_case(n, rows, cols, dtype, ignored=0.0)
     t[0], t[1] = rows - 1, 0
     check_xent(h, w, t, gl)
+
+
+@pytest.mark.parametrize("dtype,n,rows,cols", [("bf16", 70, 70000, 1001), ("f32", 70, 25000, 1001),
+                                               ("f32", 70, 360000, 8), ("f16", 2100, 33000, 8)])
+def test_cross_entropy_of_many_tokens_over_pieces_of_the_vocabulary(dtype, n, rows, cols):
+    # two pieces each: of copied rows of w (forward and backward), of P
+    print("cross entropy pieces, many tokens", dtype, n, rows, cols, flush=True)
+    h, w, t, gl = xent_case(n, rows, cols, dtype)
+    t[0], t[1] = rows - 1, 0
+    check_xent(h, w, t, gl)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 16, 17, 32, 33, 64])
+def test_cross_entropy_of_few_tokens_over_many_rows(dtype, n):
+    # enough rows for the waves to take rows of their own (64 or 128 a
+    # workgroup, 512 workgroups), an odd number of them
+    rows = 32801 if n <= 16 else 65601
+    print("cross entropy few tokens", dtype, n, rows, flush=True)
+    h, w, t, gl = xent_case(n, rows, 40, dtype, ignored=0.2)
+    check_xent(h, w, t, gl)

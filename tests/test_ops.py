@@ -113,7 +113,7 @@ def test_cross_entropy_refuses_bad_arguments():
         return lib.rotor_xent_workspace_bytes(*a, ctypes.byref(need))
 
     for bad in [(5, 4, 8, 10, 1, 0), (1, -1, 8, 10, 1, 0), (1, (1 << 20) + 1, 8, 10, 1, 0), (1, 4, 0, 10, 1, 0),
-                (1, 4, 65537, 10, 1, 1), (1, 4, 8, 0, 1, 1), (1, 4, 8, 1 << 28, 1, 1)]:
+                (1, 4, 65537, 10, 1, 1), (1, 4, 8, 0, 1, 1), (1, 4, 8, (1 << 26) + 1, 1, 1)]:
         assert bytes_of(*bad) == E, bad
     assert lib.rotor_xent_workspace_bytes(1, 4, 8, 10, 1, 0, None) == E
     assert bytes_of(1, 0, 8, 10, 1, 1) == rotor.ROTOR_OK and need.value == 0  # no tokens
