@@ -76,6 +76,18 @@ template <> struct ProductOf<float> {
     static constexpr int kParts = kTerms;
 };
 
+// exp(x - m), m2 = m log2(e): one multiplication-addition and the hardware's
+// power of two.
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ inline float exp_over(float x, float m2)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -m2));
+#else
+    return 0.f * (x + m2);
+#endif
+}
+
 // A maximum and the sum of exponentials above it.
 struct Soft {
     float top, sum;

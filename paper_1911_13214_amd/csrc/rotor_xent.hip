@@ -120,13 +120,13 @@ struct StatsEpilogue {
                     top = fmaxf(top, r.acc[ii][jj][e]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float m = finite_or_0(top);
+            const float m2 = finite_or_0(top) * kLog2e;
             float sum = 0.f;
 #pragma unroll
             for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    sum += __expf(r.acc[ii][jj][e] - m);
+                    sum += exp_over(r.acc[ii][jj][e], m2);
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (r.lane < 16)
@@ -167,17 +167,32 @@ template <typename T> struct ProbEpilogue {
             opaque(row);
             const int j = j0 + row;
             const bool in = j < tokens;
-            const float g = in ? grad[j] : 0.f, l = in ? lse[j] : 0.f;
+            const float g = in ? grad[j] : 0.f, l2 = in ? lse[j] * kLog2e : 0.f;
             const int64_t t64 = (in ? targets[j] : -1) - v0 - r.tile_i * S::BI;
             const int t = t64 >= 0 && t64 < S::BI ? (int)t64 - r.i : -1;
+            // a select: what a token without a target holds may be NaN
+            const bool none = g == 0.f;
 #pragma unroll
             for (int ii = 0; ii < S::NI; ++ii)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = __expf(r.acc[ii][jj][e] - l) - (t == 16 * ii + e ? 1.f : 0.f);
-                    // a select: what a token without a target holds may be NaN
-                    r.acc[ii][jj][e] = g != 0.f && r.i + 16 * ii + e < have ? v * g : 0.f;
+                    const float v = exp_over(r.acc[ii][jj][e], l2) * g;
+                    r.acc[ii][jj][e] = none ? 0.f : v;
                 }
+            if (__any(t >= 0 && t < 16 * S::NI && !none)) {  // few tokens have their target in one tile
+#pragma unroll
+                for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        r.acc[ii][jj][e] -= t == 16 * ii + e && !none ? g : 0.f;
+            }
+            if (have < S::BI) {
+#pragma unroll
+                for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        r.acc[ii][jj][e] = r.i + 16 * ii + e < have ? r.acc[ii][jj][e] : 0.f;
+            }
             if constexpr (kParts > 1) {
                 if (!in)
                     continue;
