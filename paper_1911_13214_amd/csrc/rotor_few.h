@@ -99,7 +99,9 @@ template <typename T> struct FewArgs {
 };
 
 // C: tiles of 16 tokens.  KW: waves that share their rows and split the
-// columns.  Loads of W and H are batched U steps of 32 columns deep.
+// columns.  Loads of W and H are batched U steps of 32 columns deep.  Bound by
+// reading W: one token, 50021 x 2048 bf16, 41 us (205 MB, 5.0 TB/s); 64 tokens
+// 86 us, H then costs as many loads as W.
 template <typename T, int C, int KW, bool BACK>
 __global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
 {
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
 // dW = P^T H of few tokens: 64 rows a workgroup, P held in registers, H^T
 // streaming through from the L2.  What bounds it is writing dW: a wave's 16 x
 // 64 results of a 16-bit type go through LDS, so that a row's 128 bytes are
-// written at once.
+// written at once.  64 tokens, 50000 x 2048 bf16: 49 us (205 MB, 4.2 TB/s).
 template <typename T> struct FewWeightArgs {
     typedef typename ProductOf<T>::P P;
     const P *pt;  // [rows][terms][32 KS]
@@ -358,7 +360,8 @@ __global__ __launch_bounds__(kFewThreads) void few_weight_kernel(FewWeightArgs<T
 
 // Sums over a part of the vocabulary of P W, 128 columns a workgroup: 64 rows
 // of W at a time go through LDS and are read transposed out of it; the next 64
-// are loaded meanwhile.
+// are loaded meanwhile.  64 tokens, 50000 x 2048 bf16: 81 us (205 MB, 2.5
+// TB/s: each step waits for its loads and two barriers).
 template <typename T> struct FewSumArgs {
     typedef typename ProductOf<T>::P P;
     const T *w;

@@ -160,6 +160,20 @@ def test_embedding_gradient(dtype, kind, n, rows, cols):
         assert torch.equal(out, ops.embedding_backward(tokens.int().cuda(), dy.cuda(), rows, scale, padding=padding))
 
 
+@pytest.mark.parametrize("n", [3, 700, 2048, 2049])
+@pytest.mark.parametrize("rows", [2, 512, 513, 262144, 262145, 3000000])
+def test_embedding_gradient_by_table_size(n, rows):
+    # one, two and three digits of the sort, in one launch (up to 2048 tokens)
+    # and in one each
+    print("embedding gradient digits", n, rows, flush=True)
+    g = torch.Generator().manual_seed(n + rows)
+    tokens = tokens_of("uniform", n, rows, g)
+    tokens[-1], tokens[0] = rows - 1, 0
+    dy = m.normal(g, n, 9, dtype=torch.float32)
+    ref, mag = m.embedding_grad(tokens, dy, rows, 1.0)
+    m.close(ops.embedding_backward(tokens.cuda(), dy.cuda(), rows), ref, (n + 4) * m.U32 * mag)
+
+
 def test_embedding_gradient_ignores_what_has_none():
     g = torch.Generator().manual_seed(4)
     tokens = torch.randint(0, 50, (300,), generator=g)
