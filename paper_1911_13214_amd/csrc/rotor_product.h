@@ -1,5 +1,5 @@
 // Matrix products of the cross entropy: C[j][i] = sum over k of A(i, k) B(j, k),
-// operands 16-bit, each with k or with i (j) adjacent in memory, sums in 32
+// operands 16-bit, k adjacent in A's memory and k or j in B's, sums in 32
 // bits on the matrix units, a tile's results handed to an epilogue while they
 // are in registers.
 #pragma once
@@ -39,9 +39,9 @@ __device__ inline Turned turned(const char *lds)
 
 // An operand: `rows` rows of `cols` elements, `pitch` elements apart, 16-byte
 // aligned, cols a multiple of 8.  The summed index k runs along the rows, or,
-// in a product's template with KA or KB set, over them.  A 32-bit matrix is
-// held as three bf16 terms whose sum has its 24 bits, the terms of a row
-// `seg` elements apart.
+// for B in a product with KB set, over them.  A 32-bit matrix is held as three
+// bf16 terms whose sum has its 24 bits, the terms of a row `seg` elements
+// apart.
 template <typename T> struct Operand {
     const T *p;
     int64_t rows, cols, pitch, seg;
@@ -338,7 +338,7 @@ template <int WAIT> __device__ inline void phase_barrier()
 // buffers of 32 with counted waits 1066, 1183, 1247; two groups half a phase
 // apart (this one) 1101, 1267, 1372, and 1398, 1480, 1514 without the stores.
 // The library's product of 8192^3 reaches 1297 here, of 16384^3 1559.
-template <typename T, typename S, bool KA, bool KB, typename E>
+template <typename T, typename S, bool KB, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Operand<T> b, ProductArgs p, E epilogue)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     const int tiles = p.tiles_i * p.tiles_j;
 
     int ti, tj, s, at;  // the tile; product and step of the next load
-    Loader<T, S::BI, S::kLoadsA, S::NI, KA> la;
+    Loader<T, S::BI, S::kLoadsA, S::NI, false> la;
     Loader<T, S::BJ, S::kLoadsB, S::NJ, KB> lb;
     auto load = [&](char *lds, bool live) {
         la.load(a, lds, term_a(s) * a.seg, at, live);

@@ -6,8 +6,12 @@
 // A second launch joins the tiles' pairs.
 // Backward, for pieces of the vocabulary: the same product again, whose
 // epilogue turns logits into P = (softmax - target) * gradient and writes
-// it in 16 bits; then dH += P W and dW = P^T H, which read what they need
-// transposed on its way out of LDS.
+// it in 16 bits; then dH^T += W^T P^T and dW = P^T H.  Both read
+// their second operand with k over its rows and turn it on its way out of LDS,
+// the one of which a wave reads fewer fragments: that costs nothing, where the
+// first one turned would cost a tenth and both a third (8192 x 8192 results at
+// k = 8192, without stores: 1458 TF/s with none, 1467 and 1319 with one, 931
+// with both).  So dH is summed transposed, and H is transposed once for dW.
 #include "rotor_few.h"
 #include "rotor_product.h"
 
@@ -17,12 +21,12 @@ namespace {
 typedef Tile<256, 256, 2, 4> Large;
 typedef Tile<128, 128, 2, 2> Small;
 
-// dst[r][c] = src[r][c], 0 for columns up to `cols_to` (a multiple of 8) and
-// for rows whose scale is 0 (where scales are given): eight columns a thread.
+// dst[r][c] = src[r][c], 0 for columns up to `cols_to` (a multiple of 8): eight
+// columns a thread.
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t rows, int64_t cols, int64_t pitch,
                                                    typename ProductOf<T>::P *dst, int64_t dst_pitch, int64_t dst_seg,
-                                                   int64_t cols_to, const float *scale_row)
+                                                   int64_t cols_to)
 {
     typedef typename ProductOf<T>::P P;
     constexpr int kParts = ProductOf<T>::kParts;
@@ -30,12 +34,51 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t rows, i
     const int64_t r = at / pieces, c = at % pieces * 8;
     if (r >= rows)
         return;
-    const bool none = scale_row && scale_row[r] == 0.f;
     typename Mfma<P>::Frag t[kParts];
-    terms_of<T>(row_piece(src + r * pitch, c, none ? 0 : cols), t);
+    terms_of<T>(row_piece(src + r * pitch, c, cols), t);
 #pragma unroll
     for (int q = 0; q < kParts; ++q)
         *(typename Mfma<P>::Frag *)(dst + r * dst_pitch + q * dst_seg + c) = t[q];
+}
+
+// dst[c][r] = src[r][c], 0 for rows up to `rows_to` (a multiple of 8) and for
+// those whose scale is 0: 64 x 64 elements a workgroup through LDS, eight
+// adjacent ones a load and a store.
+template <typename T>
+__global__ __launch_bounds__(256) void turn_kernel(const T *src, int64_t rows, int64_t cols, int64_t pitch,
+                                                   typename ProductOf<T>::P *dst, int64_t dst_pitch, int64_t dst_seg,
+                                                   int64_t rows_to, const float *scale_row)
+{
+    typedef typename ProductOf<T>::P P;
+    constexpr int kParts = ProductOf<T>::kParts;
+    __shared__ float tile[64][65];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int row = threadIdx.x / 8 + 32 * k, col = threadIdx.x % 8 * 8;
+        const int64_t r = r0 + row;
+        const bool some = r < rows && scale_row[r] != 0.f;
+        const typename VecOf<T, 8>::V v = row_piece(src + (some ? r : 0) * pitch, c0 + col, some ? cols : 0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            tile[row][col + e] = (float)v[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int col = threadIdx.x / 8 + 32 * k, row = threadIdx.x % 8 * 8;
+        if (c0 + col >= cols || r0 + row >= rows_to)
+            continue;
+        typename VecOf<T, 8>::V v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = (T)tile[row + e][col];
+        typename Mfma<P>::Frag t[kParts];
+        terms_of<T>(v, t);
+#pragma unroll
+        for (int q = 0; q < kParts; ++q)
+            *(typename Mfma<P>::Frag *)(dst + (c0 + col) * dst_pitch + q * dst_seg + r0 + row) = t[q];
+    }
 }
 
 // ---- epilogues -------------------------------------------------------------------
@@ -115,7 +158,7 @@ struct StatsEpilogue {
 // P[j][i] from the logits, rounded once to 16 bits (what the two products
 // after it take; in bf16 an error of at most 2^-8 of each term, that of the
 // gradients' own rounding), or split into three terms.  8192 tokens x 8000 x
-// 4096 bf16: 440 us (1220 TF/s), with 131 MB of P written.
+// 4096 bf16: 445 us (1210 TF/s), with 131 MB of P written.
 template <typename T> struct ProbEpilogue {
     typedef typename ProductOf<T>::P P;
     static constexpr int kParts = ProductOf<T>::kParts;
@@ -190,8 +233,10 @@ template <typename T> struct ProbEpilogue {
     }
 };
 
-// dH: C as 32-bit sums, 475 us for 8192 x 4096 from 8000 rows (1130 TF/s with
-// 268 MB of sums read and written).  One part of a split product, added to what is there or not.
+// dH, transposed: C as 32-bit sums, one part of a split product, added to what
+// is there or not.  8192 x 4096 from 8000 rows bf16: 452 us (1190 TF/s with 268
+// MB of sums read and written; 475 us as C[token][column], for which more
+// fragments are read turned).
 struct SumEpilogue {
     float *c;
     int64_t part;  // elements between the parts
@@ -219,8 +264,7 @@ struct SumEpilogue {
 };
 
 // dW: C in the type of the result, times a scale from the device.  8000 x 4096
-// from 8192 tokens bf16: 465 us (1155 TF/s): both operands are read transposed,
-// twice as many LDS reads of half the size.
+// from 8192 tokens bf16: 437 us (1230 TF/s; 465 us with H not transposed before).
 template <typename T> struct OutEpilogue {
     T *c;
     const float *scale;
@@ -442,6 +486,46 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t p
     store_some(out + j * out_pitch + i, cols - i < 4 ? (int)(cols - i) : 4, v);
 }
 
+// The same from sums that lie transposed, [parts][cols][pitch]: D columns of 64
+// rows a workgroup, through LDS.  64 columns, or 16 where each has four parts
+// or more to add: more workgroups then read them (171 x 1088 of 29 parts 8 us,
+// with 64 columns 16 us; 512 x 1024 of 32 parts 11 and 14 us).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void turn_finish_kernel(const float *sum, int64_t pitch, int64_t part, int parts,
+                                                          int64_t rows, int64_t cols, const float *scale, T *out,
+                                                          int64_t out_pitch)
+{
+    __shared__ float tile[D][65];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * D;
+    const int x = threadIdx.x % 16 * 4, y = threadIdx.x / 16;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        const int64_t c = c0 + y + 16 * k;
+        f32x4 s{0.f, 0.f, 0.f, 0.f};
+        if (c < cols && r0 + x < rows) {  // pitch is a multiple of 4
+#pragma unroll 8
+            for (int q = 0; q < parts; ++q)
+                s += *(const f32x4 *)(sum + q * part + c * pitch + r0 + x);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            tile[y + 16 * k][x + e] = s[e];
+    }
+    __syncthreads();
+    const float f = *scale;
+    const int col = threadIdx.x % (D / 4) * 4, row0 = threadIdx.x / (D / 4);
+    const int64_t c = c0 + col;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        const int row = row0 + 1024 / D * k;
+        if (r0 + row >= rows || c >= cols)
+            continue;
+        const float v[4] = {tile[col][row] * f, tile[col + 1][row] * f, tile[col + 2][row] * f,
+                            tile[col + 3][row] * f};
+        store_some(out + (r0 + row) * out_pitch + c, cols - c < 4 ? (int)(cols - c) : 4, v);
+    }
+}
+
 // Clears a matrix (gradients of nothing).
 template <typename T> __global__ __launch_bounds__(256) void clear_kernel(T *out, int64_t rows, int64_t cols,
                                                                           int64_t pitch)
@@ -519,9 +603,16 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
     return l;
 }
 
+// Rows of the library's own operands start 512 bytes further on than their
+// lengths ask for: with a power of two between them, the rows of a tile lie in
+// few of the memory's channels (a product of 8192 x 8192 results at k = 2048
+// 1336 TF/s, 1463 with the 512 bytes).
+constexpr int64_t kSkew = 256;
+int64_t skewed(int64_t cols) { return cols + kSkew; }
+
 struct BackwardLayout {
     uint64_t grad, scale, h, w, ht, p, pt, sum, total;
-    int64_t dk, piece, nk, sum_pitch;
+    int64_t dk, piece, nk, p_pitch, sum_pitch;
     int split;
 };
 
@@ -553,21 +644,24 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
         l.total = b.at;
         return l;
     }
-    l.nk = n;
+    l.nk = skewed(pad(n, 8));
     l.piece = pad(v, kPad);
     int64_t most = kPieceBytes / (2 * parts * (pack && l.dk > n ? l.dk : n));
-    if (most > kMostPitch / parts)
-        most = kMostPitch / parts;
+    if (most > kMostPitch / parts - kSkew)
+        most = kMostPitch / parts - kSkew;
     most = most < kPad ? kPad : most / kPad * kPad;
     if (l.piece > most) {
         // pieces of equal size
         const int64_t count = ceil_div(l.piece, most);
         l.piece = pad(ceil_div(l.piece, count), kPad);
     }
-    l.h = b.take(2ull * (uint64_t)(parts * l.dk * n));
+    l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
     l.w = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * l.piece) : 0);
-    l.p = b.take(2ull * (uint64_t)(parts * l.piece * n));
-    l.ht = l.pt = 0;
+    l.p_pitch = skewed(l.piece);
+    l.sum_pitch = pad(n, 4);
+    l.p = b.take(2ull * (uint64_t)(parts * l.p_pitch * n));
+    l.ht = b.take(2ull * (uint64_t)(parts * l.nk * d));
+    l.pt = 0;
     // few tiles of dH: its summed index (the piece) in parts, for a large
     // tile on every CU, of eight steps at least
     int64_t split = ceil_div(256, tiles(d, n, 256));
@@ -575,7 +669,7 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     if (split > steps / 8)
         split = steps / 8 > 0 ? steps / 8 : 1;
     l.split = (int)split;
-    l.sum = b.take(4ull * (uint64_t)(l.split * n * l.sum_pitch));
+    l.sum = b.take(4ull * (uint64_t)(l.split * d * l.sum_pitch));
     l.total = b.at;
     return l;
 }
@@ -586,7 +680,7 @@ struct Extent {
     int split;
 };
 
-template <typename P, typename S, bool KA, bool KB, typename E>
+template <typename P, typename S, bool KB, typename E>
 void run_tiles(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, hipStream_t s)
 {
     ProductArgs p;
@@ -598,7 +692,7 @@ void run_tiles(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, h
     p.split_steps = (int)ceil_div(p.steps, x.split);
     // as many workgroups as the 256 CUs hold at once (by their LDS)
     const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j, most = 256 * ((160 << 10) / (2 * S::kBytes)) / x.split;
-    product_kernel<P, S, KA, KB, E>
+    product_kernel<P, S, KB, E>
         <<<dim3((uint32_t)(tiles < most || most < 8 ? tiles : most / 8 * 8), (uint32_t)x.split), S::kThreads, 0, s>>>(
             a, b, p, e);
 }
@@ -614,27 +708,26 @@ bool large_tiles(int64_t a, int64_t b, int split)
     return tiles(a, b, 256) * split >= 128 && a > 128 && b > 128;
 }
 
-template <bool KA, bool KB, typename P, typename E>
+template <bool KB, typename P, typename E>
 void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, hipStream_t s)
 {
     if (large_tiles(x.ni, x.nj, x.split))
-        run_tiles<P, Large, KA, KB, E>(a, b, x, e, s);
+        run_tiles<P, Large, KB, E>(a, b, x, e, s);
     else
-        run_tiles<P, Small, KA, KB, E>(a, b, x, e, s);
+        run_tiles<P, Small, KB, E>(a, b, x, e, s);
 }
 
-// H or rows of W as a product's operand, copied into `space` if need be;
-// rows with scale_row 0 (if it is given) as 0.
+// H or rows of W as a product's operand, copied into `space` if need be.
 template <typename T>
 Operand<typename ProductOf<T>::P> operand(const T *src, int64_t rows, int64_t cols, int64_t pitch, bool pack,
-                                          void *space, int64_t dk, const float *scale_row, hipStream_t s)
+                                          void *space, int64_t dk, hipStream_t s)
 {
     typedef typename ProductOf<T>::P P;
     constexpr int64_t parts = ProductOf<T>::kParts;
     if (!pack)
         return Operand<P>{(const P *)src, rows, cols, pitch, 0};
     pack_kernel<T><<<dim3((uint32_t)ceil_div(rows * (dk / 8), 256)), 256, 0, s>>>(
-        src, rows, cols, pitch, (P *)space, parts * dk, dk, dk, scale_row);
+        src, rows, cols, pitch, (P *)space, parts * dk, dk, dk);
     return Operand<P>{(const P *)space, rows, pad(cols, 8), parts * dk, parts > 1 ? dk : 0};
 }
 
@@ -714,7 +807,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
         typedef typename decltype(e)::T T;
         typedef typename ProductOf<T>::P P;
         const T *w = (const T *)d_w;
-        const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, nullptr, s);
+        const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
         float2 *part = (float2 *)(work + l.part);
         float *target = (float *)(work + l.target);
         if (few_tokens(type, n_tokens, n_rows)) {
@@ -739,7 +832,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
         int64_t tiles_done = 0;
         for (int64_t v0 = 0; v0 < n_rows; v0 += l.piece) {
             const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
-            const Operand<P> a = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, nullptr, s);
+            const Operand<P> a = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
             StatsEpilogue ep;
             ep.part = part + tiles_done * n_tokens;
             ep.target_logit = target;
@@ -747,7 +840,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
             ep.vocab = (int)rows;
             ep.tokens = (int)n_tokens;
             ep.v0 = v0;
-            run_product<false, false>(a, b, Extent{rows, n_tokens, cols, 1}, ep, s);
+            run_product<false>(a, b, Extent{rows, n_tokens, cols, 1}, ep, s);
             tiles_done += ceil_div(rows, large_tiles(rows, n_tokens, 1) ? 256 : 128);
         }
         run_loss(part, tiles_done, target, d_targets, ignore, n_rows, n_tokens, d_loss, d_lse, s);
@@ -798,8 +891,6 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         const T *h = (const T *)d_h, *w = (const T *)d_w;
         const GradArgs ga{d_grad_loss, d_targets, ignore, n_rows, n_tokens, grad, scale};
         const bool few = few_tokens(type, n_tokens, n_rows);
-        // H with the rows without a target as 0 (they may hold NaN, which dW
-        // would take in)
         Operand<P> hb{(const P *)d_h, n_tokens, cols, h_pitch, 0};
         if (few) {
             FewPrepareArgs<T> f;
@@ -816,7 +907,12 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                 hb = Operand<P>{f.packed, n_tokens, pad(cols, 8), parts * l.dk, parts > 1 ? l.dk : 0};
         } else {
             grad_kernel<<<1, 1024, 0, s>>>(ga);
-            hb = operand<T>(h, n_tokens, cols, h_pitch, true, work + l.h, l.dk, grad, s);
+            hb = operand<T>(h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
+            // H transposed for dW, the rows without a target as 0 (they may
+            // hold NaN, which dW would take in)
+            if (d_dw)
+                turn_kernel<T><<<dim3((uint32_t)ceil_div(n_tokens, 64), (uint32_t)ceil_div(cols, 64)), 256, 0, s>>>(
+                    h, n_tokens, cols, h_pitch, (P *)(work + l.ht), parts * l.nk, l.nk, pad(n_tokens, 8), grad);
         }
         if (few) {
             FewArgs<T> f{};
@@ -875,29 +971,29 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         }
         for (int64_t v0 = 0; v0 < n_rows && !few; v0 += l.piece) {
             const int64_t rows = n_rows - v0 < l.piece ? n_rows - v0 : l.piece;
-            const Operand<P> wa = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, nullptr, s);
+            const Operand<P> wa = operand<T>(w + v0 * w_pitch, rows, cols, w_pitch, pack, work + l.w, l.dk, s);
             ProbEpilogue<T> ep;
             ep.p = (P *)(work + l.p);
-            ep.pitch = (int)(parts * l.piece);
-            ep.seg = (int)l.piece;
+            ep.pitch = (int)(parts * l.p_pitch);
+            ep.seg = (int)l.p_pitch;
             ep.lse = d_lse;
             ep.grad = grad;
             ep.targets = d_targets;
             ep.v0 = v0;
             ep.rows = (int)rows;
             ep.tokens = (int)n_tokens;
-            run_product<false, false>(wa, hb, Extent{rows, n_tokens, cols, 1}, ep, s);
-            const Operand<P> pb{(const P *)(work + l.p), n_tokens, pad(rows, 8), parts * l.piece,
-                                parts > 1 ? l.piece : 0};
+            run_product<false>(wa, hb, Extent{rows, n_tokens, cols, 1}, ep, s);
+            const Operand<P> pb{(const P *)(work + l.p), n_tokens, pad(rows, 8), parts * l.p_pitch,
+                                parts > 1 ? l.p_pitch : 0};
             if (d_dh) {
                 SumEpilogue se;
                 se.c = sum;
                 se.pitch = (int)l.sum_pitch;
-                se.part = n_tokens * l.sum_pitch;
-                se.cols = (int)cols;
-                se.rows = (int)n_tokens;
+                se.part = cols * l.sum_pitch;
+                se.cols = (int)n_tokens;
+                se.rows = (int)cols;
                 se.add = v0 > 0;
-                run_product<true, false>(wa, pb, Extent{cols, n_tokens, rows, l.split}, se, s);
+                run_product<true>(pb, wa, Extent{n_tokens, cols, rows, l.split}, se, s);
             }
             if (d_dw) {
                 OutEpilogue<T> oe;
@@ -906,10 +1002,17 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                 oe.cols = (int)cols;
                 oe.rows = (int)rows;
                 oe.scale = scale;
-                run_product<true, true>(hb, pb, Extent{cols, rows, n_tokens, 1}, oe, s);
+                const Operand<P> ha{(const P *)(work + l.ht), cols, pad(n_tokens, 8), parts * l.nk,
+                                    parts > 1 ? l.nk : 0};
+                run_product<true>(ha, pb, Extent{cols, rows, n_tokens, 1}, oe, s);
             }
         }
-        if (d_dh) {
+        if (d_dh && !few) {
+            const int side = l.split >= 4 ? 16 : 64;
+            const auto finish = side == 16 ? turn_finish_kernel<T, 16> : turn_finish_kernel<T, 64>;
+            finish<<<dim3((uint32_t)ceil_div(n_tokens, 64), (uint32_t)ceil_div(cols, side)), 256, 0, s>>>(
+                sum, l.sum_pitch, cols * l.sum_pitch, l.split, n_tokens, cols, scale, (T *)d_dh, dh_pitch);
+        } else if (d_dh) {
             const int64_t quads = n_tokens * ceil_div(cols, 4);
             const auto finish = l.split >= 8 ? finish_kernel<T, 16> : finish_kernel<T, 1>;
             finish<<<dim3((uint32_t)ceil_div(quads, l.split >= 8 ? 16 : 256)), 256, 0, s>>>(
