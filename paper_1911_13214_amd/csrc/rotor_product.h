@@ -110,6 +110,11 @@ struct ProductArgs {
     int split_steps;  // of one part (grid y)
 };
 
+// Which of a product's extents is that of the tokens that count, whose number is
+// on the device (an epilogue's `live`): none of them (all tokens count), the
+// rows of A, those of B, or the summed index.
+enum Live { kLiveNone, kLiveA, kLiveB, kLiveK };
+
 // The shape of a workgroup's tile: BI x BJ results, WI x WJ waves.
 template <int BI_, int BJ_, int WI_, int WJ_> struct Tile {
     static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
@@ -342,6 +347,23 @@ template <typename T, typename S, bool KB, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Operand<T> b, ProductArgs p, E epilogue)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (E::kLive != kLiveNone) {
+        const int n = *epilogue.live;
+        if constexpr (E::kLive == kLiveA) {
+            a.rows = n;
+            p.tiles_i = (n + S::BI - 1) / S::BI;
+        } else if constexpr (E::kLive == kLiveB) {
+            b.rows = n;
+            p.tiles_j = (n + S::BJ - 1) / S::BJ;
+        } else {  // not split
+            a.cols = (n + 7) / 8 * 8;
+            b.rows = n;
+            p.k = n > 0 ? n : 1;  // for no tokens a step of zeros
+            p.steps = p.split_steps = p.products * (int)((p.k + kStep - 1) / kStep);
+        }
+        if ((int)blockIdx.x >= p.tiles_i * p.tiles_j)
+            return;
+    }
     // two steps: one is multiplied while the other arrives
     __shared__ __attribute__((aligned(1024))) char even[S::kBytes];
     __shared__ __attribute__((aligned(1024))) char odd[S::kBytes];

@@ -570,6 +570,30 @@ def test_cross_entropy_without_targets(dtype):
     assert not ref3[0][(t3 == 5).cuda()].any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,count", [(65, 1), (300, 8), (300, 64), (300, 256), (520, 257), (1100, 1025), (2100, 2048)])
+def test_cross_entropy_of_few_tokens_that_count(dtype, n, count):
+    # the backward works on those with a gradient alone: in one run, spread
+    # out, and among targets whose loss has no gradient
+    h, w, t, gl = xent_case(n, 270, 72, dtype, ignored=0.0)
+    for k, some in enumerate((torch.arange(n) >= n - count, torch.arange(n) < count,
+                              torch.argsort(torch.rand(n, generator=torch.Generator().manual_seed(n))) < count)):
+        print("cross entropy tokens that count", dtype, n, count, k, flush=True)
+        out = check_xent(h, w, torch.where(some, t, -100), gl)
+        assert not out[2][~some.cuda()].any()
+        again = ops.linear_cross_entropy_backward(h.cuda(), w.cuda(), t.cuda(), out[1], torch.where(some, gl, 0.0).cuda())
+        assert torch.equal(again[0], out[2]) and torch.equal(again[1], out[3])
+
+
+def test_cross_entropy_of_many_tokens_with_a_target_outside_the_vocabulary():
+    h, w, t, gl = xent_case(150, 290, 72, "bf16")
+    t[3], t[148] = 290, -7
+    loss, lse = ops.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    assert loss.cpu().isnan().nonzero().squeeze(1).tolist() == [3, 148]
+    dh, dw = ops.linear_cross_entropy_backward(h.cuda(), w.cuda(), t.cuda(), lse, gl.cuda())
+    assert dh.cpu().isnan().all(1).nonzero().squeeze(1).tolist() == [3, 148] and dw.isnan().all()
+
+
 def test_cross_entropy_of_targets_outside_the_vocabulary_is_nan():
     h, w, t, gl = xent_case(20, 50, 16, "f32", ignored=0.0)
     t[3], t[8] = 50, -7
