@@ -20,6 +20,16 @@ from torch import nn
 from . import ops
 
 
+def _rows(grad):
+    """A gradient as the operators take matrices: one that autograd hands on
+    broadcast or transposed is copied."""
+    try:
+        ops._matrix(grad, "grad")
+    except ValueError:
+        return grad.contiguous()
+    return grad
+
+
 class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed, step, step_tensor):
@@ -31,7 +41,7 @@ class _Dropout(torch.autograd.Function):
     def backward(ctx, dy):
         dx = None
         if ctx.needs_input_grad[0]:
-            dx = ops.dropout(dy, *ctx.draw, step_tensor=ctx.step_tensor)
+            dx = ops.dropout(_rows(dy), *ctx.draw, step_tensor=ctx.step_tensor)
         return dx, dy if ctx.needs_input_grad[1] else None, None, None, None, None
 
 
@@ -50,7 +60,7 @@ class _Embedding(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         rows, scale, padding = ctx.how
-        return None, ops.embedding_backward(ctx.saved_tensors[0], dy, rows, scale, padding=padding), None, None
+        return None, ops.embedding_backward(ctx.saved_tensors[0], _rows(dy), rows, scale, padding=padding), None, None
 
 
 def embedding(tokens, table, scale=1.0, padding=None):
@@ -75,7 +85,7 @@ class _ResidualNorm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *grads):
-        dy, dh = (None, grads[0]) if ctx.alone else grads
+        dy, dh = (None if g is None else _rows(g) for g in ((None, grads[0]) if ctx.alone else grads))
         y, z, stats, *params = ctx.saved_tensors
         how = dict(zip(_PARAMS, params))
         if dh is None and ctx.how["pre"] != "none":

@@ -115,3 +115,26 @@ def test_optimal_sequences_of_a_language_chain_run_within_their_budgets():
     for r in ok:
         # the allocator rounds blocks to 512 bytes
         assert r["measured_bytes"] <= r["budget_bytes"] * 1.02 + (8 << 20), r
+
+
+def test_gradients_that_arrive_broadcast_or_transposed():
+    # what autograd hands on for a sum (no strides) or through a transpose is
+    # the same gradient as a dense one, bit for bit
+    from paper_1911_13214_amd import stages as lm
+    g = torch.Generator().manual_seed(4)
+    x, z = (m.normal(g, 24, 40, dtype=torch.float32).cuda().requires_grad_() for _ in range(2))
+    table = m.normal(g, 30, 40, dtype=torch.float32).cuda().requires_grad_()
+    tokens = torch.randint(0, 30, (24,), generator=g).cuda()
+    w = m.normal(g, 40, dtype=torch.float32).cuda().requires_grad_()
+    calls = [(lambda: lm.dropout(x, 0.3, 7, 2, z), (x, z)), (lambda: lm.embedding(tokens, table, 2.0), (table,)),
+             (lambda: lm.residual_norm(x, z, post="rms", pre="layer", pre_weight=w)[0], (x, z)),
+             (lambda: lm.residual_norm(x, z, post="rms", pre="layer", pre_weight=w)[1], (x, z, w)),
+             (lambda: lm.residual_norm(x, pre="rms", pre_weight=w)[1], (x, w)),
+             (lambda: lm.linear_cross_entropy(x, table, tokens), (x, table))]
+    for k, (call, wrt) in enumerate(calls):
+        y = call()
+        for dy in (torch.ones(1, device="cuda").expand_as(y), torch.randn(y.shape[::-1], device="cuda").t()):
+            print("gradient layout", k, dy.stride(), flush=True)
+            a = torch.autograd.grad(y, wrt, dy, retain_graph=True)
+            b = torch.autograd.grad(y, wrt, dy.contiguous(), retain_graph=True)
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
