@@ -2,10 +2,12 @@
 // gradients of all it takes.
 //
 // A row is held in the registers of its threads (64 to 1024 of them, 8
-// elements each, 16 past 4096 columns), so each tensor is read once and written once in either
-// direction.  Backward, a workgroup walks a strip of rows and keeps the sums
-// over rows (weights, biases, gate) in registers; the strips' sums are added
-// by a second launch.
+// elements each, 16 past 4096 columns), so each tensor is read once and written
+// once in either direction.  Backward, a workgroup walks a strip of rows and
+// keeps the sums over rows (weights, biases, gate) in registers; the strips'
+// sums are added by a second launch.  Past 4096 columns the registers do not
+// hold both: the rows' gradients and the sums over rows are launches of their
+// own.
 #include "rotor_ops.h"
 
 #include <type_traits>
@@ -218,6 +220,7 @@ struct BackArgs {
     const float *stats;
     float *part[kSums];  // [blocks][cols], gate: [strips][cols]; NULL: not wanted
     void *dgate;         // written here if each group is one strip (part[kGate] is NULL then)
+    float2 *row_sums;    // of wide rows: means of d and d n of each row's pre norm
     StripPlan plan;
 };
 
@@ -251,8 +254,6 @@ __device__ inline void put_sums(const float (&s)[N][V], const Pieces<TH, V, N> &
 // Bound by memory: 16384 x 2048 bf16, two norms and a gate for each 2048 rows,
 // 86 us (403 MB, 4.7 TB/s; 162 us without the next row's loads under the
 // present one's work); 4096 x 1024 f32, LayerNorm, 20 us (101 MB, 5.0 TB/s).
-// Rows of more than 4096 columns hold 16 elements a thread and spill some of
-// the sums.
 template <typename T, int TH, int V, int N>
 __global__ __launch_bounds__(Team<TH>::kBlock) void back_kernel(const T *dy, const T *dh, const T *y, const T *z,
                                                                  T *dx, T *dz, BackArgs a)
@@ -372,6 +373,165 @@ __global__ __launch_bounds__(Team<TH>::kBlock) void back_kernel(const T *dy, con
         put_sums<TH, V, N>(s_pre_b, p, a.part[kPreB] + at, sums_buf);
 }
 
+// The gradients of wide rows, a workgroup a row.
+template <typename T, int TH, int V, int N>
+__global__ __launch_bounds__(TH) void wide_row_kernel(const T *dy, const T *dh, const T *y, const T *z, T *dx, T *dz,
+                                                      BackArgs a)
+{
+    __shared__ float red[2][16][2];
+    int half = 0;
+    const int64_t r = blockIdx.x;
+    const Pieces<TH, V, N> p(threadIdx.x, (int)a.cols);
+    const float inv = 1.f / (float)a.cols;
+    const float4 st = *(const float4 *)(a.stats + 4 * r);
+    Param<T, V, N> in_d, in_u, in_q, in_v;
+    in_d.load(p, dh ? dh + r * a.dh_pitch : nullptr, 0.f);
+    in_u.load(p, dh ? y + r * a.y_pitch : nullptr, 0.f);
+    in_q.load(p, dy ? dy + r * a.dy_pitch : nullptr, 0.f);
+    in_v.load(p, z ? z + r * a.z_pitch : nullptr, 0.f);
+    Row<T, V, N> d, q;
+    FOR_ELEMENTS q.f[k][j] = in_q.at(k, j);
+    if (dh) {
+        Param<T, V, N> w2;
+        w2.load(p, (const T *)a.pre_w, 1.f);
+        float c1 = 0.f, c2 = 0.f;
+        FOR_ELEMENTS
+        {
+            d.f[k][j] = in_d.at(k, j) * w2.at(k, j);
+            if (j >= p.dup[k]) {
+                c1 += d.f[k][j];
+                c2 += d.f[k][j] * ((in_u.at(k, j) - st.z) * st.w);
+            }
+        }
+        row_sum2<TH>(c1, c2, red, half);
+        c1 = a.pre == ROTOR_NORM_LAYER ? c1 * inv : 0.f;
+        c2 *= inv;
+        if (threadIdx.x == 0)
+            a.row_sums[r] = make_float2(c1, c2);
+        FOR_ELEMENTS q.f[k][j] += st.w * (d.f[k][j] - c1 - (in_u.at(k, j) - st.z) * st.w * c2);
+    }
+    if (z) {
+        Param<T, V, N> w1, g;
+        w1.load(p, (const T *)a.post_w, 1.f);
+        g.load(p, a.gate ? (const T *)a.gate + r / a.plan.group * a.gate_pitch : nullptr, 1.f);
+        float c1 = 0.f, c2 = 0.f;
+        FOR_ELEMENTS
+        {
+            d.f[k][j] = g.at(k, j) * q.f[k][j] * w1.at(k, j);
+            if (j >= p.dup[k]) {
+                c1 += d.f[k][j];
+                c2 += d.f[k][j] * ((in_v.at(k, j) - st.x) * st.y);
+            }
+        }
+        if (a.post != ROTOR_NORM_NONE) {
+            row_sum2<TH>(c1, c2, red, half);
+            c1 = a.post == ROTOR_NORM_LAYER ? c1 * inv : 0.f;
+            c2 *= inv;
+            FOR_ELEMENTS d.f[k][j] = st.y * (d.f[k][j] - c1 - (in_v.at(k, j) - st.x) * st.y * c2);
+        }
+        d.store(p, dz + r * a.dz_pitch);
+    }
+    FOR_ELEMENTS q.f[k][j] *= a.a;
+    q.store(p, dx + r * a.dx_pitch);
+}
+
+// The sums over the rows of wide ones, the gradient of y once more from the
+// row's means: eight columns a thread, a strip of rows a workgroup.
+template <typename T> __global__ __launch_bounds__(256) void wide_sum_kernel(const T *dy, const T *dh, const T *y,
+                                                                             const T *z, BackArgs a)
+{
+    constexpr int V = kVec;
+    typedef typename VecOf<T, V>::V Vec;
+    const int64_t at = ((int64_t)blockIdx.y * 256 + threadIdx.x) * V;
+    if (at >= a.cols)
+        return;
+    const int64_t c = at < a.cols - V ? at : a.cols - V;  // the last piece ends with the row
+    const bool gate_sums = a.part[kGate] || a.dgate, after = z && (gate_sums || a.part[kPostW] || a.part[kPostB]);
+    float w1[V], b1[V], w2[V], g[V];
+    float s_post_w[V] = {}, s_post_b[V] = {}, s_pre_w[V] = {}, s_pre_b[V] = {}, s_gate[V] = {};
+    auto param = [&](const void *src, float otherwise, float (&v)[V]) {
+        if (src)
+            load_vec((const T *)src + c, v);
+        else
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                v[j] = otherwise;
+    };
+    param(a.post_w, 1.f, w1);
+    param(a.post_b, 0.f, b1);
+    param(a.pre_w, 1.f, w2);
+    auto put = [&](const float (&v)[V], auto *dst) { store_vec(dst + c, v); };
+    const int64_t s0 = (int64_t)blockIdx.x * a.plan.per_block;
+    const int64_t s1 = s0 + a.plan.per_block < a.plan.strips ? s0 + a.plan.per_block : a.plan.strips;
+    for (int64_t s = s0; s < s1; ++s) {
+        const int64_t group = s / a.plan.per_group;
+        const int64_t in_group = (s - group * a.plan.per_group) * a.plan.strip;
+        const int64_t r0 = group * a.plan.group + in_group;
+        const int64_t n = in_group + a.plan.strip < a.plan.group ? a.plan.strip : a.plan.group - in_group;
+        param(a.gate ? (const T *)a.gate + group * a.gate_pitch : nullptr, 1.f, g);
+        constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;  // rows in flight
+        for (int64_t i = 0; i < n; i += kAhead) {
+            Vec d[kAhead] = {}, u[kAhead] = {}, q[kAhead] = {}, v[kAhead] = {};
+            float4 st[kAhead];
+            float2 m[kAhead];
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                const int64_t r = r0 + (i + e < n ? i + e : i);
+                st[e] = *(const float4 *)(a.stats + 4 * r);
+                m[e] = dh ? a.row_sums[r] : make_float2(0.f, 0.f);
+                if (dh) {
+                    d[e] = *(const Vec *)(dh + r * a.dh_pitch + c);
+                    u[e] = *(const Vec *)(y + r * a.y_pitch + c);
+                }
+                if (after) {
+                    if (dy)
+                        q[e] = *(const Vec *)(dy + r * a.dy_pitch + c);
+                    v[e] = *(const Vec *)(z + r * a.z_pitch + c);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                if (i + e >= n)
+                    break;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float t = (float)q[e][j];
+                    if (dh) {
+                        const float b = (float)d[e][j], k = ((float)u[e][j] - st[e].z) * st[e].w;
+                        s_pre_w[j] += b * k;
+                        s_pre_b[j] += b;
+                        t += st[e].w * (b * w2[j] - m[e].x - k * m[e].y);
+                    }
+                    if (after) {
+                        const float k = ((float)v[e][j] - st[e].x) * st[e].y, b = g[j] * t;
+                        s_gate[j] += t * (k * w1[j] + b1[j]);
+                        s_post_w[j] += b * k;
+                        s_post_b[j] += b;
+                    }
+                }
+            }
+        }
+        if (gate_sums) {
+            if (a.dgate)
+                put(s_gate, (T *)a.dgate + group * a.dgate_pitch);
+            else
+                put(s_gate, a.part[kGate] + s * a.cols);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                s_gate[j] = 0.f;
+        }
+    }
+    const int64_t row = (int64_t)blockIdx.x * a.cols;
+    if (a.part[kPostW])
+        put(s_post_w, a.part[kPostW] + row);
+    if (a.part[kPostB])
+        put(s_post_b, a.part[kPostB] + row);
+    if (a.part[kPreW])
+        put(s_pre_w, a.part[kPreW] + row);
+    if (a.part[kPreB])
+        put(s_pre_b, a.part[kPreB] + row);
+}
+
 // Adds the strips' sums: 64 columns of one output row a workgroup, its 16
 // waves a part of the strips each, the parts then in order (5 us for those of
 // 16384 x 2048).
@@ -432,6 +592,16 @@ template <typename F> void with_shape(int64_t cols, F f)
         f(IntV<512>{}, IntV<8>{}, IntV<2>{});
     else
         f(IntV<1024>{}, IntV<8>{}, IntV<2>{});
+}
+
+// Whether a thread has two pieces of a row (with_shape), and the backward goes
+// its way of wide rows.
+bool wide(int64_t cols) { return cols > 512 * 8; }
+
+// Bytes of the backward's workspace for the rows' means.
+uint64_t row_sums_bytes(const rotor_norm *n)
+{
+    return wide(n->cols) && n->pre != ROTOR_NORM_NONE ? (8ull * (uint64_t)n->rows + 15) / 16 * 16 : 0;
 }
 
 // Strips for as many workgroups as the 256 CUs hold at once: 8 waves each.
@@ -537,7 +707,7 @@ int32_t rotor_residual_norm_workspace_bytes(const rotor_norm *how, uint64_t *byt
     if (!bytes || !norm_sizes_ok(how))
         return ROTOR_EINVAL;
     const StripPlan s = strip_plan(how->rows, how->cols, how->gate_rows);
-    *bytes = 4ull * (uint64_t)how->cols * (uint64_t)((kSums - 1) * s.blocks + (s.per_group > 1 ? s.strips : 0));
+    *bytes = row_sums_bytes(how) + 4ull * (uint64_t)how->cols * (uint64_t)((kSums - 1) * s.blocks + (s.per_group > 1 ? s.strips : 0));
     if (*bytes < 16)
         *bytes = 16;
     return ROTOR_OK;
@@ -575,7 +745,8 @@ int32_t rotor_residual_norm_backward(const rotor_norm *how, const void *d_dy, in
     AddArgs add;
     int64_t tasks = 0;
     int last = -1;
-    float *w = (float *)d_work;
+    a.row_sums = (float2 *)d_work;
+    float *w = (float *)((char *)d_work + row_sums_bytes(how));
     for (int k = 0; k < kSums; ++k) {
         const bool wanted = out[k] && !(k == kGate && gate_here);
         a.part[k] = wanted ? w : nullptr;
@@ -619,10 +790,22 @@ int32_t rotor_residual_norm_backward(const rotor_norm *how, const void *d_dy, in
         typedef typename decltype(e)::T T;
         // without rows the strips are empty, and the sums 0
         with_shape(cols, [&](auto th, auto v, auto n) {
-            constexpr int TH = decltype(th)::v;
-            back_kernel<T, TH, decltype(v)::v, decltype(n)::v>
-                <<<dim3((uint32_t)plan.blocks), Team<TH>::kBlock, 0, (hipStream_t)stream>>>(
-                    (const T *)d_dy, (const T *)d_dh, (const T *)d_y, (const T *)d_z, (T *)d_dx, (T *)d_dz, a);
+            constexpr int TH = decltype(th)::v, V = decltype(v)::v, N = decltype(n)::v;
+            const hipStream_t st = (hipStream_t)stream;
+            const T *const dy = (const T *)d_dy, *const dh = (const T *)d_dh, *const y = (const T *)d_y,
+                    *const z = (const T *)d_z;
+            if constexpr (N == 1) {
+                back_kernel<T, TH, V, N>
+                    <<<dim3((uint32_t)plan.blocks), Team<TH>::kBlock, 0, st>>>(dy, dh, y, z, (T *)d_dx, (T *)d_dz, a);
+            } else {
+                if (rows > 0)
+                    wide_row_kernel<T, TH, V, N>
+                        <<<dim3((uint32_t)rows), TH, 0, st>>>(dy, dh, y, z, (T *)d_dx, (T *)d_dz, a);
+                if (last >= 0 || gate_here)
+                    wide_sum_kernel<T>
+                        <<<dim3((uint32_t)plan.blocks, (uint32_t)ceil_div(cols, 256 * kVec)), 256, 0, st>>>(dy, dh, y,
+                                                                                                         z, a);
+            }
         });
         if (last >= 0)
             add_kernel<T><<<dim3((uint32_t)ceil_div(cols, 64), (uint32_t)tasks), kAddWaves * 64, 0,

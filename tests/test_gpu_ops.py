@@ -345,6 +345,19 @@ def test_residual_norm_sums_over_many_rows(dtype, rows, gate):
     check_seam(s, how, m.normal(g, rows, 72, dtype=m.DTYPES[dtype]), m.normal(g, rows, 72, dtype=m.DTYPES[dtype]))
 
 
+@pytest.mark.parametrize("dtype,rows,cols,post,pre,gate", [
+    ("bf16", 1030, 4103, "rms", "layer", 0), ("f32", 600, 4104, "layer", "rms", 6), ("f16", 300, 8191, "none", "rms", 300),
+    ("bf16", 70, 16383, "layer", "layer", 1), ("f32", 33, 8208, "none", "none", 3), ("f16", 530, 5120, "rms", "none", 2)])
+def test_residual_norm_of_wide_rows(dtype, rows, cols, post, pre, gate):
+    print("residual norm wide", dtype, rows, cols, post, pre, gate, flush=True)
+    g = torch.Generator().manual_seed(rows + cols)
+    s, how = seam(g, rows, cols, dtype, post, pre, gate, post != "none")
+    dy, dh = (m.normal(g, rows, cols, dtype=m.DTYPES[dtype]) for _ in range(2))
+    check_seam(s, how, dy, dh)
+    if pre != "none":
+        check_seam(s, how, None, dh)
+
+
 def test_residual_norm_without_a_block():
     g = torch.Generator().manual_seed(3)
     s, how = seam(g, 9, 70, "bf16", "none", "rms", 0, False, z=False)
