@@ -529,9 +529,8 @@ ROTOR_API int32_t rotor_residual_norm(const rotor_norm *how, const void *d_x, in
                                       float *d_stats, void *stream);
 
 /* Device workspace of rotor_residual_norm_backward for these sizes (`how`'s
- * pointers are not used): sums over strips of rows and, past 4096
- * columns, 8 bytes a row.  Host only.  Returns
- * ROTOR_OK or ROTOR_EINVAL. */
+ * pointers are not used): sums over strips of rows and, past 4096 columns,
+ * 8 bytes a row.  Host only.  Returns ROTOR_OK or ROTOR_EINVAL. */
 ROTOR_API int32_t rotor_residual_norm_workspace_bytes(const rotor_norm *how, uint64_t *bytes);
 
 /* Gradients of the parameters, DEVICE, written, of the call's type, with the

@@ -2,7 +2,7 @@
 // gradients of all it takes.
 //
 // A row is held in the registers of its threads (64 to 1024 of them, 8
-// elements each, 16 past 4096 columns), so each tensor is read once and written
+// elements each, 16 past 8192 columns), so each tensor is read once and written
 // once in either direction.  Backward, a workgroup walks a strip of rows and
 // keeps the sums over rows (weights, biases, gate) in registers; the strips'
 // sums are added by a second launch.  Past 4096 columns the registers do not
@@ -373,7 +373,10 @@ __global__ __launch_bounds__(Team<TH>::kBlock) void back_kernel(const T *dy, con
         put_sums<TH, V, N>(s_pre_b, p, a.part[kPreB] + at, sums_buf);
 }
 
-// The gradients of wide rows, a workgroup a row.
+// The gradients of wide rows, a workgroup a row.  With the sums over rows
+// beside them in one launch, registers spilled: 8192 x 5120 bf16 450 us, 3000 x
+// 12288 2243 us; the two launches 177 and 172 us (ten tensors moved instead of
+// six, 4.3 to 4.7 TB/s).
 template <typename T, int TH, int V, int N>
 __global__ __launch_bounds__(TH) void wide_row_kernel(const T *dy, const T *dh, const T *y, const T *z, T *dx, T *dz,
                                                       BackArgs a)
@@ -574,7 +577,8 @@ template <typename T> __global__ __launch_bounds__(kAddWaves * 64) void add_kern
     ((T *)a.out[task])[out_row * a.out_pitch[task] + c] = (T)s;
 }
 
-// Calls f(team, V, N) with the smallest shape that holds a row.
+// Calls f(team, V, N) with the smallest shape that holds a row (forward, 8192 x
+// 5120 bf16: 640 threads of 8 elements 80 us, 1024 88, 512 of 16 102).
 template <int V> struct IntV { static constexpr int v = V; };
 template <typename F> void with_shape(int64_t cols, F f)
 {
@@ -588,15 +592,23 @@ template <typename F> void with_shape(int64_t cols, F f)
         f(IntV<256>{}, IntV<8>{}, IntV<1>{});
     else if (cols <= 512 * 8)
         f(IntV<512>{}, IntV<8>{}, IntV<1>{});
-    else if (cols <= 512 * 16)
-        f(IntV<512>{}, IntV<8>{}, IntV<2>{});
+    else if (cols <= 640 * 8)
+        f(IntV<640>{}, IntV<8>{}, IntV<1>{});
+    else if (cols <= 768 * 8)
+        f(IntV<768>{}, IntV<8>{}, IntV<1>{});
+    else if (cols <= 1024 * 8)
+        f(IntV<1024>{}, IntV<8>{}, IntV<1>{});
+    else if (cols <= 640 * 16)
+        f(IntV<640>{}, IntV<8>{}, IntV<2>{});
+    else if (cols <= 768 * 16)
+        f(IntV<768>{}, IntV<8>{}, IntV<2>{});
     else
         f(IntV<1024>{}, IntV<8>{}, IntV<2>{});
 }
 
-// Whether a thread has two pieces of a row (with_shape), and the backward goes
-// its way of wide rows.
-bool wide(int64_t cols) { return cols > 512 * 8; }
+// Columns past which the backward goes its way of wide rows.
+constexpr int kNarrow = 512 * kVec;
+bool wide(int64_t cols) { return cols > kNarrow; }
 
 // Bytes of the backward's workspace for the rows' means.
 uint64_t row_sums_bytes(const rotor_norm *n)
@@ -607,8 +619,9 @@ uint64_t row_sums_bytes(const rotor_norm *n)
 // Strips for as many workgroups as the 256 CUs hold at once: 8 waves each.
 StripPlan strip_plan(int64_t rows, int64_t cols, int64_t gate_rows)
 {
-    int64_t blocks_at_once = 0;
-    with_shape(cols, [&](auto th, auto, auto) { blocks_at_once = 256 * 8 * 64 / Team<decltype(th)::v>::kBlock; });
+    int64_t blocks_at_once = 256;  // of wide rows, times their slices of columns
+    if (!wide(cols))
+        with_shape(cols, [&](auto th, auto, auto) { blocks_at_once = 256 * 8 * 64 / Team<decltype(th)::v>::kBlock; });
     StripPlan s;
     s.groups = gate_rows > 0 ? gate_rows : 1;
     s.group = rows / s.groups;
@@ -794,7 +807,7 @@ int32_t rotor_residual_norm_backward(const rotor_norm *how, const void *d_dy, in
             const hipStream_t st = (hipStream_t)stream;
             const T *const dy = (const T *)d_dy, *const dh = (const T *)d_dh, *const y = (const T *)d_y,
                     *const z = (const T *)d_z;
-            if constexpr (N == 1) {
+            if constexpr (TH * V * N <= kNarrow) {
                 back_kernel<T, TH, V, N>
                     <<<dim3((uint32_t)plan.blocks), Team<TH>::kBlock, 0, st>>>(dy, dh, y, z, (T *)d_dx, (T *)d_dz, a);
             } else {
