@@ -355,11 +355,12 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
         } else if constexpr (E::kLive == kLiveB) {
             b.rows = n;
             p.tiles_j = (n + S::BJ - 1) / S::BJ;
-        } else {  // not split
+        } else {
             a.cols = (n + 7) / 8 * 8;
             b.rows = n;
             p.k = n > 0 ? n : 1;  // for no tokens a step of zeros
-            p.steps = p.split_steps = p.products * (int)((p.k + kStep - 1) / kStep);
+            p.steps = p.products * (int)((p.k + kStep - 1) / kStep);
+            p.split_steps = (p.steps + (int)gridDim.y - 1) / (int)gridDim.y;
         }
         if ((int)blockIdx.x >= p.tiles_i * p.tiles_j)
             return;

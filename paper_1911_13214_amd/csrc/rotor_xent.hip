@@ -249,20 +249,20 @@ template <typename T> struct ProbEpilogue {
     }
 };
 
-// dH, transposed: C as 32-bit sums, one part of a split product, added to what
-// is there or not.  8192 x 4096 from 8000 rows bf16: 452 us (1190 TF/s with 268
+// C as 32-bit sums, one part of a split product, added to what is there or not:
+// dH, transposed (L is kLiveA), and dW where it has few tiles (kLiveK).  8192 x 4096 from 8000 rows bf16: 452 us (1190 TF/s with 268
 // MB of sums read and written; 475 us as C[token][column], for which more
 // fragments are read turned).
-struct SumEpilogue {
-    [[maybe_unused]] static constexpr Live kLive = kLiveA;
-    const int *live;  // the results' columns
+template <Live L> struct SumEpilogue {
+    static constexpr Live kLive = L;
+    const int *live;
     float *c;
     int64_t part;  // elements between the parts
-    int pitch, rows, add;
+    int pitch, cols, rows, add;
     template <typename S> __device__ void operator()(Results<S> &r, char *) const
     {
         float *const tile = c + r.part * part + (int64_t)r.tile_j * S::BJ * pitch + r.tile_i * S::BI;
-        const int cols_in = *live - r.tile_i * S::BI, rows_in = rows - r.tile_j * S::BJ;
+        const int cols_in = (L == kLiveA ? *live : cols) - r.tile_i * S::BI, rows_in = rows - r.tile_j * S::BJ;
 #pragma unroll
         for (int jj = 0; jj < S::NJ; ++jj) {
             int j = r.j + 16 * jj;
@@ -407,6 +407,7 @@ __global__ __launch_bounds__(1024) void grad_kernel(TokenArgs a)
     __shared__ int count[2][16];
     const int tokens = (int)a.g.tokens, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     float m = 0.f;
+#pragma unroll 4
     for (int j = threadIdx.x; j < tokens; j += 1024)
         m = fmaxf(m, grad_size(a.g, j));
     m = wave_max(m);
@@ -417,27 +418,37 @@ __global__ __launch_bounds__(1024) void grad_kernel(TokenArgs a)
         m = fmaxf(m, top[w]);
     const float unit = grad_unit(m);
     int live = 0, even = 0;  // tokens that count, so far
-    for (int j0 = 0; j0 < tokens; j0 += 1024, even ^= 1) {
-        const int j = j0 + threadIdx.x;
-        const float g = j < tokens ? scaled_grad(a.g, j, unit) : 0.f;
-        const bool some = g != 0.f;
-        const uint64_t mask = __ballot(some);
+    constexpr int kEach = 4;  // adjacent tokens of a thread
+    for (int j0 = 0; j0 < tokens; j0 += 1024 * kEach, even ^= 1) {
+        const int j = j0 + (int)threadIdx.x * kEach;
+        float g[kEach];
+        int at = live, sum = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            g[k] = j + k < tokens ? scaled_grad(a.g, j + k, unit) : 0.f;
+            const uint64_t mask = __ballot(g[k] != 0.f);
+            at += __popcll(mask & (((uint64_t)1 << lane) - 1));
+            sum += __popcll(mask);
+        }
         if (lane == 0)
-            count[even][wave] = __popcll(mask);
+            count[even][wave] = sum;
         __syncthreads();
-        int at = live + __popcll(mask & (((uint64_t)1 << lane) - 1));
         for (int w = 0; w < 16; ++w) {
             at += w < wave ? count[even][w] : 0;
             live += count[even][w];
         }
-        if (some) {
-            const int64_t t = a.g.targets[j];
-            a.order[at] = j;
-            a.g.grad[at] = g;
-            a.live_lse[at] = a.lse[j];
-            a.live_target[at] = t >= 0 && t < a.g.vocab ? (int)t : -1;
-        } else if (j < tokens) {
-            a.order[tokens - 1 - (j - at)] = j;  // of the j before it, `at` count
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            if (g[k] != 0.f) {
+                const int64_t t = a.g.targets[j + k];
+                a.order[at] = j + k;
+                a.g.grad[at] = g[k];
+                a.live_lse[at] = a.lse[j + k];
+                a.live_target[at] = t >= 0 && t < a.g.vocab ? (int)t : -1;
+                ++at;
+            } else if (j + k < tokens) {
+                a.order[tokens - 1 - (j + k - at)] = j + k;  // of the tokens before it, `at` count
+            }
         }
     }
     if (threadIdx.x == 0) {
@@ -508,7 +519,7 @@ template <typename T> __global__ __launch_bounds__(256) void few_prepare_kernel(
         }
 }
 
-// dH from its parts' sums: four columns a thread, Y threads a share of the
+// A gradient from its parts' sums: four columns a thread, Y threads a share of the
 // parts each, the shares then in order.
 template <typename T, int Y>
 __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t pitch, int64_t part, int parts,
@@ -630,11 +641,20 @@ bool rows_aligned(const void *p, int64_t cols, int64_t pitch)
 }
 
 // Whether a call goes the way of few tokens: that of the probabilities as a
-// whole, in two layouts, if those are no larger than two pieces.
-bool few_tokens(int32_t type, int64_t n, int64_t v)
+// whole, in two layouts, if those are no larger than two pieces.  Operands that
+// would have to be copied always do: the small tiles read a copy of W, the few
+// tokens' kernels W itself (64 tokens x 32000 x 1024 f32 80 against 192 us forward,
+// 245 against 330 backward).  Others where W's rows do not give small tiles to
+// three quarters of the CUs (1 x 1000 x 4096 bf16 16 against 47 us), and up to
+// 32 tokens backward (1 x 50000 x 2048 139 against 174 us; 64 tokens 228
+// against 193); forward the small tiles read W faster (1 x 50021 x 2048 44
+// against 38 us, 64 x 128000 x 4096 402 against 180).
+bool few_tokens(int32_t type, int64_t n, int64_t v, bool pack, bool backward)
 {
     const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
-    return n <= kFew && 2 * 2 * parts * kFew * v <= 2 * kPieceBytes;
+    if (n > kFew || 2 * 2 * parts * kFew * v > 2 * kPieceBytes)
+        return false;
+    return pack || ceil_div(v, Small::BI) < 192 || (backward && n <= 32);
 }
 
 struct ForwardLayout {
@@ -649,11 +669,11 @@ ForwardLayout forward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bool
     Bump b;
     const int64_t parts = type == ROTOR_F32 ? kTerms : 1;
     l.dk = pad(d, kStep);
-    l.part = b.take(8ull * (uint64_t)ceil_div(v, few_tokens(type, n, v) ? few_rows(n, v) : 128) * (uint64_t)n);
+    l.part = b.take(8ull * (uint64_t)ceil_div(v, few_tokens(type, n, v, pack, false) ? few_rows(n, v) : 128) * (uint64_t)n);
     l.target = b.take(4ull * (uint64_t)n);
     l.piece = v;
     l.h = l.w = b.at;
-    if (few_tokens(type, n, v)) {
+    if (few_tokens(type, n, v, pack, false)) {
         l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
     } else if (pack) {
         const int64_t most = kPieceBytes / (2 * parts * l.dk) / kPad * kPad;  // at least kPad: see the limits
@@ -673,9 +693,9 @@ constexpr int64_t kSkew = 256;
 int64_t skewed(int64_t cols) { return cols + kSkew; }
 
 struct BackwardLayout {
-    uint64_t grad, scale, order, lse, target, live, h, w, ht, p, pt, sum, total;
-    int64_t dk, piece, nk, p_pitch, sum_pitch;
-    int split;
+    uint64_t grad, scale, order, lse, target, live, h, w, ht, p, pt, sum, w_sum, total;
+    int64_t dk, piece, nk, p_pitch, sum_pitch, w_pitch;
+    int split, w_split;
 };
 
 int64_t tiles(int64_t a, int64_t b, int64_t side) { return ceil_div(a, side) * ceil_div(b, side); }
@@ -689,7 +709,7 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     l.sum_pitch = pad(d, 4);
     l.grad = b.take(4ull * (uint64_t)n);
     l.scale = b.take(4);
-    if (few_tokens(type, n, v)) {
+    if (few_tokens(type, n, v, pack, true)) {
         l.nk = n <= 32 ? 32 : 64;
         l.piece = pad(v, kFewRows);
         l.h = b.take(pack ? 2ull * (uint64_t)(parts * l.dk * n) : 0);
@@ -702,7 +722,7 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
         const int64_t want = ceil_div(768, ceil_div(d, kFewCols));
         l.split = (int)(want < most ? want : most);
         l.sum = b.take(4ull * (uint64_t)(l.split * n * l.sum_pitch));
-        l.w = l.order = l.lse = l.target = l.live = 0;
+        l.w = l.w_sum = l.order = l.lse = l.target = l.live = 0;
         l.total = b.at;
         return l;
     }
@@ -736,6 +756,17 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
         split = steps / 8 > 0 ? steps / 8 : 1;
     l.split = (int)split;
     l.sum = b.take(4ull * (uint64_t)(l.split * d * l.sum_pitch));
+    // and few of dW: the tokens in parts, if there is a whole round of them
+    // (65536 tokens x 1000 x 512 bf16, backward, 1267 us without, 519 with; 2048 x 5000 x
+    // 1024, which has 80 tiles, 118 without, 135 with)
+    l.w_split = tiles(d, l.piece, 256) <= 64 ? (int)(256 / tiles(d, l.piece, 256)) : 1;
+    const int64_t w_steps = (type == ROTOR_F32 ? kTermProducts : 1) * ceil_div(n, kStep);
+    if (l.w_split > w_steps / 8)
+        l.w_split = (int)(w_steps / 8);
+    if (l.w_split < 2)
+        l.w_split = 1;
+    l.w_pitch = pad(d, 4);
+    l.w_sum = b.take(l.w_split > 1 ? 4ull * (uint64_t)(l.w_split * l.piece * l.w_pitch) : 0);
     l.total = b.at;
     return l;
 }
@@ -781,6 +812,17 @@ void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e,
         run_tiles<P, Large, KB, E>(a, b, x, e, s);
     else
         run_tiles<P, Small, KB, E>(a, b, x, e, s);
+}
+
+// The parts' sums joined, into a gradient.
+template <typename T>
+void finish_rows(const float *sum, int64_t pitch, int64_t part, int parts, int64_t rows, int64_t cols,
+                 const float *scale, T *out, int64_t out_pitch, hipStream_t s)
+{
+    const int share = parts >= 8 ? 16 : 1;
+    const auto finish = share > 1 ? finish_kernel<T, 16> : finish_kernel<T, 1>;
+    finish<<<dim3((uint32_t)ceil_div(rows * ceil_div(cols, 4), 256 / share)), 256, 0, s>>>(
+        sum, pitch, part, parts, rows, cols, scale, out, out_pitch);
 }
 
 // H or rows of W as a product's operand, copied into `space` if need be.
@@ -876,7 +918,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
         const Operand<P> b = operand<T>((const T *)d_h, n_tokens, cols, h_pitch, pack, work + l.h, l.dk, s);
         float2 *part = (float2 *)(work + l.part);
         float *target = (float *)(work + l.target);
-        if (few_tokens(type, n_tokens, n_rows)) {
+        if (few_tokens(type, n_tokens, n_rows, pack, false)) {
             FewArgs<T> f{};
             f.w = w;
             f.w_pitch = w_pitch;
@@ -957,7 +999,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         int *const order = (int *)(work + l.order), *const live = (int *)(work + l.live);
         const T *h = (const T *)d_h, *w = (const T *)d_w;
         const GradArgs ga{d_grad_loss, d_targets, ignore, n_rows, n_tokens, grad, scale};
-        const bool few = few_tokens(type, n_tokens, n_rows);
+        const bool few = few_tokens(type, n_tokens, n_rows, pack, true);
         Operand<P> hb{(const P *)d_h, n_tokens, cols, h_pitch, 0};
         if (few) {
             FewPrepareArgs<T> f;
@@ -1062,26 +1104,41 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             const Operand<P> pb{(const P *)(work + l.p), n_tokens, pad(rows, 8), parts * l.p_pitch,
                                 parts > 1 ? l.p_pitch : 0};
             if (d_dh) {
-                SumEpilogue se;
+                SumEpilogue<kLiveA> se;
                 se.c = sum;
                 se.pitch = (int)l.sum_pitch;
                 se.part = cols * l.sum_pitch;
                 se.live = live;
+                se.cols = (int)n_tokens;
                 se.rows = (int)cols;
                 se.add = v0 > 0;
                 run_product<true>(pb, wa, Extent{n_tokens, cols, rows, l.split}, se, s);
             }
             if (d_dw) {
-                OutEpilogue<T> oe;
-                oe.live = live;
-                oe.c = (T *)d_dw + v0 * dw_pitch;
-                oe.pitch = (int)dw_pitch;
-                oe.cols = (int)cols;
-                oe.rows = (int)rows;
-                oe.scale = scale;
                 const Operand<P> ha{(const P *)(work + l.ht), cols, pad(n_tokens, 8), parts * l.nk,
                                     parts > 1 ? l.nk : 0};
-                run_product<true>(ha, pb, Extent{cols, rows, n_tokens, 1}, oe, s);
+                if (l.w_split > 1) {
+                    SumEpilogue<kLiveK> we;
+                    we.live = live;
+                    we.c = (float *)(work + l.w_sum);
+                    we.part = rows * l.w_pitch;
+                    we.pitch = (int)l.w_pitch;
+                    we.cols = (int)cols;
+                    we.rows = (int)rows;
+                    we.add = 0;
+                    run_product<true>(ha, pb, Extent{cols, rows, n_tokens, l.w_split}, we, s);
+                    finish_rows(we.c, l.w_pitch, we.part, l.w_split, rows, cols, scale, (T *)d_dw + v0 * dw_pitch,
+                                dw_pitch, s);
+                } else {
+                    OutEpilogue<T> oe;
+                    oe.live = live;
+                    oe.c = (T *)d_dw + v0 * dw_pitch;
+                    oe.pitch = (int)dw_pitch;
+                    oe.cols = (int)cols;
+                    oe.rows = (int)rows;
+                    oe.scale = scale;
+                    run_product<true>(ha, pb, Extent{cols, rows, n_tokens, 1}, oe, s);
+                }
             }
         }
         if (d_dh && !few) {
@@ -1091,10 +1148,8 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                 sum, l.sum_pitch, cols * l.sum_pitch, l.split, n_tokens, cols, order, live, scale, (T *)d_dh,
                 dh_pitch);
         } else if (d_dh) {
-            const int64_t quads = n_tokens * ceil_div(cols, 4);
-            const auto finish = l.split >= 8 ? finish_kernel<T, 16> : finish_kernel<T, 1>;
-            finish<<<dim3((uint32_t)ceil_div(quads, l.split >= 8 ? 16 : 256)), 256, 0, s>>>(
-                sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, (T *)d_dh, dh_pitch);
+            finish_rows(sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, (T *)d_dh, dh_pitch,
+                        s);
         }
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;

@@ -551,6 +551,21 @@ def test_cross_entropy(dtype, n, rows, cols):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,cols", [(1, 24700, 64), (16, 25001, 72), (33, 24600, 136), (64, 26000, 24)])
+def test_cross_entropy_of_few_tokens_and_many_rows(dtype, n, rows, cols):
+    print("cross entropy", dtype, n, rows, cols, flush=True)
+    check_xent(*xent_case(n, rows, cols, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,cols,ignored", [(9000, 300, 70, 0.0), (3001, 130, 300, 0.1), (2500, 1000, 129, 0.9),
+                                                 (1100, 7, 8, 0.5)])
+def test_cross_entropy_of_many_tokens_and_few_rows(dtype, n, rows, cols, ignored):
+    print("cross entropy", dtype, n, rows, cols, ignored, flush=True)
+    check_xent(*xent_case(n, rows, cols, dtype, ignored=ignored))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_cross_entropy_of_large_logits_and_certain_tokens(dtype):
     # logits of up to about 40: some softmaxes are one target, others ties
     h, w, t, gl = xent_case(96, 500, 64, dtype, scale=10.0)
