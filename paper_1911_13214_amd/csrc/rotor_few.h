@@ -100,8 +100,8 @@ template <typename T> struct FewArgs {
 
 // C: tiles of 16 tokens.  KW: waves that share their rows and split the
 // columns.  Loads of W and H are batched U steps of 32 columns deep.  Bound by
-// reading W: one token, 50021 x 2048 bf16, 41 us (205 MB, 5.0 TB/s); 64 tokens
-// 86 us, H then costs as many loads as W.
+// reading W: backward, one token, 50021 x 2048 bf16, 41 us (205 MB, 5.0 TB/s);
+// 64 tokens 86 us, H then costs as many loads as W.
 template <typename T, int C, int KW, bool BACK>
 __global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
 {

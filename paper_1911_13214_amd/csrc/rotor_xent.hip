@@ -372,14 +372,16 @@ struct GradArgs {
 };
 __device__ inline float grad_size(const GradArgs &a, int64_t j)
 {
-    const float g = a.targets[j] == a.ignore ? 0.f : fabsf(a.grad_loss[j]);
-    return g <= 3.4028234e38f ? g : 0.f;
+    const int64_t t = a.targets[j];
+    const float g = fabsf(a.grad_loss[j]);
+    return t != a.ignore && g <= 3.4028234e38f ? g : 0.f;
 }
 __device__ inline float grad_unit(float most) { return fmaxf(most, 0x1p-100f); }
 __device__ inline float scaled_grad(const GradArgs &a, int64_t j, float unit)
 {
     const int64_t t = a.targets[j];
-    return t == a.ignore ? 0.f : t >= 0 && t < a.vocab ? a.grad_loss[j] / unit * 0x1p12f : __builtin_nanf("");
+    const float g = a.grad_loss[j] / unit * 0x1p12f;
+    return t == a.ignore ? 0.f : t >= 0 && t < a.vocab ? g : __builtin_nanf("");
 }
 __device__ inline float wave_max(float v)
 {
@@ -394,20 +396,24 @@ __device__ inline float wave_max(float v)
 // targets (-1: none of the rows) of a token that counts lie at its place among
 // them.  The others cost the backward's three products nothing: 4096 tokens x
 // 32768 x 2048 bf16, 30% of them without a target, forward and backward 1535 us,
-// 1855 with all of them in the products.  One workgroup: 4096 tokens 10 us.
+// 1855 with all of them in the products.  Every workgroup finds the largest
+// gradient, and how many tokens count before its own, for itself: 12 bytes a token
+// from the L2 (65536 tokens 36 us, 175 in one workgroup).
 struct TokenArgs {
     GradArgs g;
     const float *lse;
     float *live_lse;
     int *order, *live_target, *live;
 };
+constexpr int kEach = 4;                   // adjacent tokens of a thread
+constexpr int kGradTokens = 1024 * kEach;  // of a workgroup
 __global__ __launch_bounds__(1024) void grad_kernel(TokenArgs a)
 {
     __shared__ float top[16];
-    __shared__ int count[2][16];
+    __shared__ int before[16], count[16];
     const int tokens = (int)a.g.tokens, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     float m = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int j = threadIdx.x; j < tokens; j += 1024)
         m = fmaxf(m, grad_size(a.g, j));
     m = wave_max(m);
@@ -417,44 +423,50 @@ __global__ __launch_bounds__(1024) void grad_kernel(TokenArgs a)
     for (int w = 0; w < 16; ++w)
         m = fmaxf(m, top[w]);
     const float unit = grad_unit(m);
-    int live = 0, even = 0;  // tokens that count, so far
-    constexpr int kEach = 4;  // adjacent tokens of a thread
-    for (int j0 = 0; j0 < tokens; j0 += 1024 * kEach, even ^= 1) {
-        const int j = j0 + (int)threadIdx.x * kEach;
-        float g[kEach];
-        int at = live, sum = 0;
+    const int j0 = blockIdx.x * kGradTokens, j = j0 + (int)threadIdx.x * kEach;
+    int sum = 0;  // of the tokens before this workgroup's
+#pragma unroll 8
+    for (int i = threadIdx.x; i < j0; i += 1024)
+        sum += scaled_grad(a.g, i, unit) != 0.f;
+    for (int off = 32; off >= 1; off /= 2)
+        sum += __shfl_xor(sum, off);
+    if (lane == 0)
+        before[wave] = sum;
+    float g[kEach];
+    int at = 0;
+    sum = 0;
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            g[k] = j + k < tokens ? scaled_grad(a.g, j + k, unit) : 0.f;
-            const uint64_t mask = __ballot(g[k] != 0.f);
-            at += __popcll(mask & (((uint64_t)1 << lane) - 1));
-            sum += __popcll(mask);
-        }
-        if (lane == 0)
-            count[even][wave] = sum;
-        __syncthreads();
-        for (int w = 0; w < 16; ++w) {
-            at += w < wave ? count[even][w] : 0;
-            live += count[even][w];
-        }
+    for (int k = 0; k < kEach; ++k) {
+        g[k] = j + k < tokens ? scaled_grad(a.g, j + k, unit) : 0.f;
+        const uint64_t mask = __ballot(g[k] != 0.f);
+        at += __popcll(mask & (((uint64_t)1 << lane) - 1));
+        sum += __popcll(mask);
+    }
+    if (lane == 0)
+        count[wave] = sum;
+    __syncthreads();
+    int live = 0;  // tokens that count, up to the workgroup's last
+    for (int w = 0; w < 16; ++w) {
+        at += before[w] + (w < wave ? count[w] : 0);
+        live += before[w] + count[w];
+    }
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            if (g[k] != 0.f) {
-                const int64_t t = a.g.targets[j + k];
-                a.order[at] = j + k;
-                a.g.grad[at] = g[k];
-                a.live_lse[at] = a.lse[j + k];
-                a.live_target[at] = t >= 0 && t < a.g.vocab ? (int)t : -1;
-                ++at;
-            } else if (j + k < tokens) {
-                a.order[tokens - 1 - (j + k - at)] = j + k;  // of the tokens before it, `at` count
-            }
+    for (int k = 0; k < kEach; ++k) {
+        if (g[k] != 0.f) {
+            const int64_t t = a.g.targets[j + k];
+            a.order[at] = j + k;
+            a.g.grad[at] = g[k];
+            a.live_lse[at] = a.lse[j + k];
+            a.live_target[at] = t >= 0 && t < a.g.vocab ? (int)t : -1;
+            ++at;
+        } else if (j + k < tokens) {
+            a.order[tokens - 1 - (j + k - at)] = j + k;  // of the tokens before it, `at` count
         }
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && blockIdx.x == 0)
         *a.g.scale = unit * 0x1p-12f;
+    if (threadIdx.x == 0 && blockIdx.x == gridDim.x - 1)
         *a.live = live;
-    }
 }
 
 // The same for few tokens, H transposed (dst[c][r] = src[r][c], 0 for rows up
@@ -757,8 +769,8 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     l.split = (int)split;
     l.sum = b.take(4ull * (uint64_t)(l.split * d * l.sum_pitch));
     // and few of dW: the tokens in parts, if there is a whole round of them
-    // (65536 tokens x 1000 x 512 bf16, backward, 1267 us without, 519 with; 2048 x 5000 x
-    // 1024, which has 80 tiles, 118 without, 135 with)
+    // (65536 tokens x 1000 x 512 bf16, backward, 1267 us without, 519 with; 2048
+    // x 5000 x 1024, which has 80 tiles, 118 without, 135 with)
     l.w_split = tiles(d, l.piece, 256) <= 64 ? (int)(256 / tiles(d, l.piece, 256)) : 1;
     const int64_t w_steps = (type == ROTOR_F32 ? kTermProducts : 1) * ceil_div(n, kStep);
     if (l.w_split > w_steps / 8)
@@ -1015,8 +1027,8 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             if (pack)
                 hb = Operand<P>{f.packed, n_tokens, pad(cols, 8), parts * l.dk, parts > 1 ? l.dk : 0};
         } else {
-            grad_kernel<<<1, 1024, 0, s>>>(TokenArgs{ga, d_lse, (float *)(work + l.lse), order,
-                                                     (int *)(work + l.target), live});
+            const TokenArgs ta{ga, d_lse, (float *)(work + l.lse), order, (int *)(work + l.target), live};
+            grad_kernel<<<dim3((uint32_t)ceil_div(n_tokens, kGradTokens)), 1024, 0, s>>>(ta);
             TurnArgs<P> t;
             t.cols = cols;
             t.pitch = h_pitch;
