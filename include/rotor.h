@@ -587,8 +587,9 @@ ROTOR_API int32_t rotor_residual_norm_backward(const rotor_norm *how, const void
 /* Device workspace of rotor_xent (backward 0) or rotor_xent_backward (1).
  * Forward: 8 bytes per token and 128 rows of w.  Backward: at most 128 MiB
  * for a piece of the probabilities (256 rows of w at least; up to 64 tokens:
- * 256 MiB), two copies of h, 32-bit sums for dh.  Where
- * operands are copied, at most 128 MiB for a piece of w as well.  Host only. */
+ * 256 MiB), two copies of h, 32-bit sums for dh, and for dw where that has few
+ * tiles (64 MiB at most).  Where operands are copied, at most 128 MiB for a
+ * piece of w as well.  Host only. */
 ROTOR_API int32_t rotor_xent_workspace_bytes(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
                                              int32_t aligned, int32_t backward, uint64_t *bytes);
 

@@ -1,10 +1,10 @@
-// The cross entropy of few tokens (up to 64): W is read as it is, once
-// forward and twice backward, straight into the matrix units' operands; what
-// bounds it is that reading, and the writing of dW.
+// The cross entropy of few tokens (up to 64; which calls: few_tokens): W is
+// read as it is, once forward and twice backward, straight into the matrix
+// units' operands; what bounds it is that reading, and the writing of dW.
 //
-// A tile of 256 tokens would leave three quarters and more of its work
-// unused here, and copies of W (transposed, or split into terms) would cost
-// several times the reading.
+// Tiles would leave most of their work unused here, which only a forward over
+// many aligned rows hides, and copies of W (split into terms, or aligned) would
+// cost several times the reading.
 #pragma once
 
 #include "rotor_product.h"
@@ -100,8 +100,8 @@ template <typename T> struct FewArgs {
 
 // C: tiles of 16 tokens.  KW: waves that share their rows and split the
 // columns.  Loads of W and H are batched U steps of 32 columns deep.  Bound by
-// reading W: backward, one token, 50021 x 2048 bf16, 41 us (205 MB, 5.0 TB/s);
-// 64 tokens 86 us, H then costs as many loads as W.
+// reading W: backward, one token, 50000 x 2048 bf16, 40 us (205 MB, 5.1 TB/s);
+// 32 tokens 57 us, H then costs half as many loads as W.
 template <typename T, int C, int KW, bool BACK>
 __global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
 {
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
 // dW = P^T H of few tokens: 64 rows a workgroup, P held in registers, H^T
 // streaming through from the L2.  What bounds it is writing dW: a wave's 16 x
 // 64 results of a 16-bit type go through LDS, so that a row's 128 bytes are
-// written at once.  64 tokens, 50000 x 2048 bf16: 49 us (205 MB, 4.2 TB/s).
+// written at once.  32 tokens, 50000 x 2048 bf16: 37 us (205 MB, 5.5 TB/s).
 template <typename T> struct FewWeightArgs {
     typedef typename ProductOf<T>::P P;
     const P *pt;  // [rows][terms][32 KS]
@@ -360,8 +360,8 @@ __global__ __launch_bounds__(kFewThreads) void few_weight_kernel(FewWeightArgs<T
 
 // Sums over a part of the vocabulary of P W, 128 columns a workgroup: 64 rows
 // of W at a time go through LDS and are read transposed out of it; the next 64
-// are loaded meanwhile.  64 tokens, 50000 x 2048 bf16: 81 us (205 MB, 2.5
-// TB/s: each step waits for its loads and two barriers).
+// are loaded meanwhile.  50000 x 2048 bf16, one token 51 us, 32 tokens 66 us (205
+// MB, 3.1 TB/s: each step waits for its loads and two barriers).
 template <typename T> struct FewSumArgs {
     typedef typename ProductOf<T>::P P;
     const T *w;
