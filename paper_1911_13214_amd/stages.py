@@ -6,12 +6,14 @@ first time, and what it keeps for its backward (w_abar) is what the schedule
 budgets.  So the dropout here draws its mask from (seed, step) and keeps
 nothing, the residual seam keeps its block's output, its sum and 16 bytes a
 row, the loss keeps 4 bytes a token and no logits, and every gradient is the
-same bit for bit on every call.
+same bit for bit on every call.  Second derivatives exist for the dropout
+alone; the others raise where one is taken.
 
 ``language_chain`` builds a chain of them: token lookup, residual blocks and
 the loss over the vocabulary, ready for ``executor.run_sequence``."""
 from __future__ import annotations
 
+import functools
 import math
 
 import torch
@@ -30,6 +32,33 @@ def _rows(grad):
     return grad
 
 
+class _Refuse(torch.autograd.Function):
+    """Passes first derivatives on; raises where one is differentiated."""
+
+    @staticmethod
+    def forward(ctx, *grads):
+        return tuple(None if g is None else g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the kernels compute first derivatives only: a derivative of one has been asked for")
+
+
+def _first_order(backward):
+    """A backward whose results come from kernels, without a graph.  Under
+    create_graph they depend on what the forward kept as well as on the
+    gradients that arrive, so they are marked whether or not those require one:
+    a second derivative through them raises instead of leaving its terms out."""
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return out
+        return _Refuse.apply(*(None if g is None else g.detach().requires_grad_() for g in out))
+    return run
+
+
 class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed, step, step_tensor):
@@ -41,7 +70,8 @@ class _Dropout(torch.autograd.Function):
     def backward(ctx, dy):
         dx = None
         if ctx.needs_input_grad[0]:
-            dx = ops.dropout(_rows(dy), *ctx.draw, step_tensor=ctx.step_tensor)
+            # linear: the gradient is a dropout itself, with a gradient of its own
+            dx = _Dropout.apply(_rows(dy), None, *ctx.draw, ctx.step_tensor)
         return dx, dy if ctx.needs_input_grad[1] else None, None, None, None, None
 
 
@@ -58,6 +88,7 @@ class _Embedding(torch.autograd.Function):
         return ops.embedding(tokens, table, scale)
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy):
         rows, scale, padding = ctx.how
         return None, ops.embedding_backward(ctx.saved_tensors[0], _rows(dy), rows, scale, padding=padding), None, None
@@ -84,6 +115,7 @@ class _ResidualNorm(torch.autograd.Function):
         return h if alone else (y, h)
 
     @staticmethod
+    @_first_order
     def backward(ctx, *grads):
         dy, dh = (None if g is None else _rows(g) for g in ((None, grads[0]) if ctx.alone else grads))
         y, z, stats, *params = ctx.saved_tensors
@@ -112,6 +144,7 @@ class _CrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @_first_order
     def backward(ctx, grad_loss):
         h, w, targets, lse = ctx.saved_tensors
         return (*ops.linear_cross_entropy_backward(h, w, targets, lse, grad_loss.contiguous(), ctx.ignore,
