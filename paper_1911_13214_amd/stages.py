@@ -63,7 +63,8 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed, step, step_tensor):
         ctx.draw = (p, seed, step)
-        ctx.step_tensor = step_tensor
+        # saved, so that autograd notices a step that was advanced in between
+        ctx.save_for_backward(step_tensor)
         return ops.dropout(x, p, seed, step, residual, step_tensor=step_tensor)
 
     @staticmethod
@@ -71,12 +72,14 @@ class _Dropout(torch.autograd.Function):
         dx = None
         if ctx.needs_input_grad[0]:
             # linear: the gradient is a dropout itself, with a gradient of its own
-            dx = _Dropout.apply(_rows(dy), None, *ctx.draw, ctx.step_tensor)
+            dx = _Dropout.apply(_rows(dy), None, *ctx.draw, *ctx.saved_tensors)
         return dx, dy if ctx.needs_input_grad[1] else None, None, None, None, None
 
 
 def dropout(x, p, seed, step=0, residual=None, step_tensor=None):
-    """ops.dropout with a gradient; nothing is kept between the two."""
+    """ops.dropout with a gradient; nothing is kept between the two.
+    ``step_tensor`` must still hold the forward's value in the backward, which
+    raises otherwise."""
     return _Dropout.apply(x, residual, p, seed, step, step_tensor)
 
 

@@ -79,3 +79,14 @@ def test_second_derivatives_of_dropout(model_ops):
     assert torch.allclose(first, 2 * s ** 2 * k * x, rtol=2.0 ** -49, atol=0)
     second, = torch.autograd.grad(first.square().sum(), x)
     assert torch.allclose(second, 8 * s ** 4 * k * x, rtol=2.0 ** -49, atol=0)
+
+
+def test_a_step_advanced_before_the_backward_is_noticed(model_ops):
+    # the gradient would be drawn from another mask than the result
+    x, step = leaf(6, 8), torch.tensor([3])
+    y = lm.dropout(x, 0.3, 7, 2, step_tensor=step)
+    g, = torch.autograd.grad(y.sum(), x, retain_graph=True)
+    assert torch.equal(g, lm.ops.dropout(torch.ones(6, 8).double(), 0.3, 7, 5))
+    step += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
