@@ -8,9 +8,11 @@ library's HIP kernels.  Tensors are CUDA tensors of one device and, where
 floating-point, of one type (float32, bfloat16 or float16); a matrix may have
 any row pitch, its last dimension is dense.  Calls enqueue on ``stream``
 (default: the current one) and return at once; a tensor that was made on
-another stream is the caller's to order, as is an output used on one (the
-scratch a call allocates is returned to torch's caching allocator on
-``stream``).  Results are allocated unless ``out`` is given.
+another stream is the caller's to order and to keep (``record_stream``), and
+so is the order of a result's use on another one.  What a call allocates,
+results and scratch, comes from torch's caching allocator for the stream it
+runs on; results are recorded for the caller's current stream as well.  Results
+are allocated unless ``out`` is given.
 
 ``stages`` wraps these in autograd functions and modules."""
 from __future__ import annotations
@@ -111,11 +113,26 @@ def _entry(name):
     return getattr(rotor.lib(), name)
 
 
-def _call(name, device, stream, *args):
-    """One entry point of the library, on ``stream`` or the device's current
-    stream."""
+def _on(stream, f, *args, **kw):
+    """A call on the stream it is given: that stream is the current one while
+    it allocates and launches, since a block of another stream's pool may still
+    be in use there.  Results are free to be used, and freed, on the caller's."""
+    for t in args:
+        if isinstance(t, torch.Tensor) and t.device != stream.device:
+            raise ValueError(f"stream is one of {stream.device}, a tensor is on {t.device}")
+    here = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        out = f(*args, **kw)
+    for t in out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(here)
+    return out
+
+
+def _call(name, device, *args):
+    """One entry point of the library, on the device's current stream."""
     index = device.index
-    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    raw = torch._C._cuda_getCurrentRawStream(index)
     if index == torch._C._cuda_getDevice():
         status = _entry(name)(*args, raw)
     else:
@@ -133,12 +150,10 @@ def _workspace_bytes(name, *sizes):
     return need.value
 
 
-def _scratch(nbytes, like, stream):
-    """Device scratch of a call, returned to the allocator on ``stream``."""
-    work = like.new_empty(max(nbytes, 16), dtype=torch.uint8)
-    if stream is not None:
-        work.record_stream(stream)
-    return work
+def _scratch(nbytes, like):
+    """Device scratch of a call, returned to the allocator when it ends: what is
+    allocated there next is used after it, on the same stream."""
+    return like.new_empty(max(nbytes, 16), dtype=torch.uint8)
 
 
 # ---- dropout ---------------------------------------------------------------------
@@ -151,6 +166,8 @@ def dropout(x, p, seed, step=0, residual=None, *, step_tensor=None, out=None, st
     ``seed``, ``step``: integers, taken modulo 2^64.  ``step_tensor``: an int64
     device tensor of one element added to ``step`` (for captured graphs).
     ``out`` may be ``x`` or ``residual``."""
+    if stream is not None:
+        return _on(stream, dropout, x, p, seed, step, residual, step_tensor=step_tensor, out=out)
     code = _typed(x, "x")
     if not 0.0 <= p <= 1.0:
         raise ValueError(f"p must lie in [0, 1], not {p}")
@@ -169,7 +186,7 @@ def dropout(x, p, seed, step=0, residual=None, *, step_tensor=None, out=None, st
         rows, cols, xp = _matrix(x, "x")
         _, _, yp = _matrix(y, "out")
         rp = _matrix(residual, "residual")[2] if residual is not None else cols
-    _call("rotor_dropout", x.device, stream, code, rows, cols, x.data_ptr(), xp, _ptr(residual), rp, y.data_ptr(), yp,
+    _call("rotor_dropout", x.device, code, rows, cols, x.data_ptr(), xp, _ptr(residual), rp, y.data_ptr(), yp,
           p, seed & 0xFFFFFFFFFFFFFFFF, step & 0xFFFFFFFFFFFFFFFF, _ptr(step_tensor))
     return y
 
@@ -186,6 +203,8 @@ def _tokens(tokens, device):
 def embedding(tokens, table, scale=1.0, *, out=None, stream=None):
     """scale * table[tokens], of shape [*tokens.shape, cols].  A token outside
     the table gives a row of NaN."""
+    if stream is not None:
+        return _on(stream, embedding, tokens, table, scale, out=out)
     code = _typed(table, "table")
     if table.dim() != 2:
         raise ValueError("table must have two dimensions")
@@ -194,7 +213,7 @@ def embedding(tokens, table, scale=1.0, *, out=None, stream=None):
     y = _out(out, table, "out", tokens.shape + (cols,))
     if tokens.numel() == 0:
         return y
-    _call("rotor_embedding", table.device, stream, code, tokens.numel(), rows, cols, tokens.data_ptr(), size,
+    _call("rotor_embedding", table.device, code, tokens.numel(), rows, cols, tokens.data_ptr(), size,
           table.data_ptr(), pitch, scale, y.data_ptr(), _matrix(y, "out")[2])
     return y
 
@@ -203,14 +222,16 @@ def embedding_backward(tokens, grad, n_rows, scale=1.0, *, padding=None, out=Non
     """Gradient [n_rows, cols] of the table from the gradient of
     ``embedding(tokens, table, scale)``: every row written, that of the token
     ``padding`` 0.  Bit for bit the same on every call."""
+    if stream is not None:
+        return _on(stream, embedding_backward, tokens, grad, n_rows, scale, padding=padding, out=out)
     code = _typed(grad, "grad")
     size = _tokens(tokens, grad.device)
     if grad.dim() < 1 or grad.shape[:-1] != tokens.shape:
         raise ValueError(f"grad must have shape {tuple(tokens.shape)} + (cols,)")
     n, (_, cols, pitch) = tokens.numel(), _matrix(grad, "grad")
     out = _out(out, grad, "out", (n_rows, cols))
-    work = _scratch(_workspace_bytes("rotor_embedding_workspace_bytes", n, n_rows, cols), grad, stream)
-    _call("rotor_embedding_backward", grad.device, stream, code, n, n_rows, cols, _ptr(tokens), size, _ptr(grad),
+    work = _scratch(_workspace_bytes("rotor_embedding_workspace_bytes", n, n_rows, cols), grad)
+    _call("rotor_embedding_backward", grad.device, code, n, n_rows, cols, _ptr(tokens), size, _ptr(grad),
           pitch, scale, -1 if padding is None else padding, out.data_ptr(), _matrix(out, "out")[2], work.data_ptr(),
           work.numel())
     return out
@@ -261,6 +282,10 @@ def residual_norm(x, z=None, *, post="none", post_weight=None, post_bias=None, g
     the rows of x (one row of gates for each run of rows / n adjacent rows);
     ``z`` None: no block, y = residual_scale * x.  ``stats``: keep what the
     backward needs (16 bytes a row), or None is returned."""
+    if stream is not None:
+        return _on(stream, residual_norm, x, z, post=post, post_weight=post_weight, post_bias=post_bias, gate=gate,
+                   residual_scale=residual_scale, pre=pre, pre_weight=pre_weight, pre_bias=pre_bias, eps=eps,
+                   stats=stats)
     n = _norm(x, z, post, post_weight, post_bias, gate, residual_scale, pre, pre_weight, pre_bias, eps)
     xp = _matrix(x, "x")[2]
     zp = _matrix(_like(z, x, "z"), "z")[2] if z is not None else n.cols
@@ -268,7 +293,7 @@ def residual_norm(x, z=None, *, post="none", post_weight=None, post_bias=None, g
     y = _empty(x) if copy else x
     h = _empty(x) if pre != "none" else None
     st = x.new_empty((n.rows, 4), dtype=torch.float32) if stats else None
-    _call("rotor_residual_norm", x.device, stream, ctypes.byref(n), x.data_ptr(), xp, _ptr(z), zp,
+    _call("rotor_residual_norm", x.device, ctypes.byref(n), x.data_ptr(), xp, _ptr(z), zp,
           y.data_ptr() if copy else None, n.cols, _ptr(h), n.cols, _ptr(st))
     return y, h, st
 
@@ -278,6 +303,10 @@ def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None
     """Gradients of residual_norm's arguments from those of y (``dy``, None:
     0) and h (``dh``, None without ``pre``), as a dict: "x", "z" and the
     parameters that are given."""
+    if stream is not None:
+        return _on(stream, residual_norm_backward, dy, dh, y, z, stats, post=post, post_weight=post_weight,
+                   post_bias=post_bias, gate=gate, residual_scale=residual_scale, pre=pre, pre_weight=pre_weight,
+                   pre_bias=pre_bias, eps=eps)
     lead = dy if dy is not None else dh
     if lead is None:
         raise ValueError("dy or dh is needed")
@@ -306,8 +335,8 @@ def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None
     need = ctypes.c_uint64()
     rotor._check(_entry("rotor_residual_norm_workspace_bytes")(ctypes.byref(n), ctypes.byref(need)),
                  "rotor_residual_norm_workspace_bytes")
-    work = _scratch(need.value, lead, stream)
-    _call("rotor_residual_norm_backward", lead.device, stream, ctypes.byref(n), *matrix(dy, "dy"), *matrix(dh, "dh"),
+    work = _scratch(need.value, lead)
+    _call("rotor_residual_norm_backward", lead.device, ctypes.byref(n), *matrix(dy, "dy"), *matrix(dh, "dh"),
           *(matrix(y, "y") if dh is not None else (None, n.cols)), *matrix(z, "z"), stats.data_ptr(),
           g["x"].data_ptr(), n.cols, _ptr(g.get("z")), n.cols, ctypes.byref(out), work.data_ptr(), work.numel())
     return g
@@ -318,7 +347,7 @@ def residual_norm_backward(dy, dh, y, z, stats, *, post="none", post_weight=None
 XENT_MAX_TOKENS, XENT_MAX_COLS, XENT_MAX_ROWS = 1 << 20, 65536, 1 << 26
 
 
-def _xent(h, w, targets, backward, stream):
+def _xent(h, w, targets, backward):
     """Checked sizes, pitches and workspace of a cross entropy."""
     code = _typed(h, "h")
     if h.dim() < 1 or w.dim() != 2 or h.shape[-1] != w.shape[1]:
@@ -335,7 +364,7 @@ def _xent(h, w, targets, backward, stream):
                          "at least one")
     aligned = int(not (cols % 8 or hp % 8 or wp % 8 or h.data_ptr() % 16 or w.data_ptr() % 16))
     need = _workspace_bytes("rotor_xent_workspace_bytes", code, n, cols, rows, aligned, backward)
-    return code, n, cols, rows, hp, wp, aligned, _scratch(need, h, stream)
+    return code, n, cols, rows, hp, wp, aligned, _scratch(need, h)
 
 
 def _per_token(t, targets, what):
@@ -350,9 +379,11 @@ def linear_cross_entropy(h, w, targets, ignore=-100, *, stream=None):
     softmax cross entropy of the logits h w^T, which never exist whole.
     Tokens with target ``ignore`` have loss 0; other targets outside the rows
     of w give NaN."""
-    code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 0, stream)
+    if stream is not None:
+        return _on(stream, linear_cross_entropy, h, w, targets, ignore)
+    code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 0)
     loss, lse = (torch.empty_like(targets, dtype=torch.float32) for _ in range(2))
-    _call("rotor_xent", h.device, stream, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp, targets.data_ptr(),
+    _call("rotor_xent", h.device, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp, targets.data_ptr(),
           ignore, loss.data_ptr(), lse.data_ptr(), aligned, work.data_ptr(), work.numel())
     return loss, lse
 
@@ -361,13 +392,16 @@ def linear_cross_entropy_backward(h, w, targets, lse, grad_loss, ignore=-100, *,
                                   stream=None):
     """Gradients of h and w from those of the losses (float32, shaped as
     ``targets``) and the log-sum-exps of the forward; None where not needed."""
+    if stream is not None:
+        return _on(stream, linear_cross_entropy_backward, h, w, targets, lse, grad_loss, ignore, need_h=need_h,
+                   need_w=need_w)
     if not (need_h or need_w):
         return None, None
-    code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 1, stream)
+    code, n, cols, rows, hp, wp, aligned, work = _xent(h, w, targets, 1)
     lse, grad_loss = _per_token(lse, targets, "lse"), _per_token(grad_loss, targets, "grad_loss")
     dh = _empty(h) if need_h else None
     dw = _empty(w) if need_w else None
-    _call("rotor_xent_backward", h.device, stream, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp,
+    _call("rotor_xent_backward", h.device, code, n, cols, rows, h.data_ptr(), hp, w.data_ptr(), wp,
           targets.data_ptr(), ignore, lse, grad_loss, _ptr(dh), cols, _ptr(dw), cols, aligned, work.data_ptr(),
           work.numel())
     return dh, dw

@@ -1,6 +1,7 @@
 """The operators of a chain's stages on the GPU against plain 64-bit
 implementations (ops_model.py).  Tolerances: one rounding of the result's type
 plus a bound on the 32-bit arithmetic before it, stated at each test."""
+import ctypes
 import itertools
 
 import pytest
@@ -733,3 +734,45 @@ def test_cross_entropy_of_few_tokens_over_many_rows(dtype, n):
     print("cross entropy few tokens", dtype, n, rows, flush=True)
     h, w, t, gl = xent_case(n, rows, 40, dtype, ignored=0.2)
     check_xent(h, w, t, gl)
+
+
+def test_a_call_on_a_stream_keeps_off_blocks_that_another_one_still_uses():
+    # Blocks of the sizes that the call will ask for, written and read by work
+    # that waits on the current stream when they are freed: the call runs
+    # beside that work and may not be given them.
+    g = torch.Generator().manual_seed(9)
+    x, z = (m.normal(g, 768, 1024, dtype=torch.bfloat16).cuda() for _ in range(2))
+    w = m.normal(g, 1000, 1024, dtype=torch.bfloat16, std=0.03).cuda()
+    t = torch.randint(0, 1000, (768,), generator=g).cuda()
+    _, lse = ops.linear_cross_entropy(x, w, t)
+    y, _, stats = ops.residual_norm(x, z, pre="layer")
+    dl = torch.ones(768, device="cuda")
+    n = ops._norm(x, z, "none", None, None, None, 1.0, "layer", None, None, 1e-5)
+    need = ctypes.c_uint64()
+    ops.rotor.lib().rotor_residual_norm_workspace_bytes(ctypes.byref(n), ctypes.byref(need))
+    calls = [(lambda **kw: ops.dropout(x, 0.2, 1, **kw), 0),
+             (lambda **kw: ops.embedding_backward(t, x, 1000, **kw),
+              ops._workspace_bytes("rotor_embedding_workspace_bytes", 768, 1000, 1024)),
+             (lambda **kw: ops.residual_norm_backward(x, z, y, z, stats, pre="layer", **kw), need.value),
+             (lambda **kw: ops.linear_cross_entropy_backward(x, w, t, lse, dl, **kw),
+              ops._workspace_bytes("rotor_xent_workspace_bytes", 1, 768, 1024, 1000, 1, 1))]
+    side = torch.cuda.Stream()
+    for k, (call, scratch) in enumerate(calls):
+        print("streams", k, flush=True)
+        want = tensors_of(call())
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        torch.cuda._sleep(50_000_000)
+        busy = [torch.full((v.numel() * v.element_size(),), 3, dtype=torch.uint8, device="cuda") for v in want]
+        if scratch:
+            busy.append(torch.full((scratch,), 3, dtype=torch.uint8, device="cuda"))
+        kept = [b.clone() for b in busy]
+        del busy
+        out = tensors_of(call(stream=side))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert all((b == 3).all() for b in kept)
+
+
+def tensors_of(out):
+    return list(out.values()) if isinstance(out, dict) else list(out) if isinstance(out, tuple) else [out]

@@ -1,5 +1,6 @@
 """Refusals of the operators of a chain's stages (no GPU): the C entry points
 return ROTOR_EINVAL before any device work, the binding raises ValueError."""
+import contextlib
 import ctypes
 
 import pytest
@@ -148,3 +149,54 @@ def test_cross_entropy_workspace_does_not_grow_with_the_logits():
         assert rotor.lib().rotor_xent_workspace_bytes(1, n, 1024, v, 1, 1, ctypes.byref(need)) == rotor.ROTOR_OK
         piece = max(512 << 20, 4 * 256 * n)
         assert need.value < piece * 2 + 16 * n * 1024, (n, v, need.value)
+
+
+def test_a_call_allocates_on_the_stream_it_is_given(monkeypatch):
+    # Its results and scratch are written on that stream: blocks of another
+    # one's pool may still be in use there.  Allocations are watched, kernels
+    # and streams replaced.
+    class Stream:
+        device = torch.device("cpu")
+        cuda_stream = 7
+
+    now, seen, recorded = ["current"], [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, now[0] = now[0], stream
+        yield
+        now[0] = before
+
+    def watch(f):
+        def alloc(*args, **kw):
+            seen.append(now[0])
+            return f(*args, **kw)
+        return alloc
+
+    given = Stream()
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[0])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: recorded.append(stream))
+    monkeypatch.setattr(torch.Tensor, "new_empty", watch(torch.Tensor.new_empty))
+    monkeypatch.setattr(torch, "empty_like", watch(torch.empty_like))
+    monkeypatch.setattr(ops, "_cuda", lambda t, what: t)
+    monkeypatch.setattr(ops, "_call", lambda *args: None)
+    x, t = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+    stats, per = torch.zeros(4, 4), torch.zeros(4)
+    calls = [lambda **kw: ops.dropout(x, 0.1, 1, **kw), lambda **kw: ops.embedding(t, x, **kw),
+             lambda **kw: ops.embedding_backward(t, x, 9, **kw),
+             lambda **kw: ops.residual_norm(x, x, pre="rms", **kw),
+             lambda **kw: ops.residual_norm_backward(x, x, x, x, stats, pre="rms", **kw),
+             lambda **kw: ops.linear_cross_entropy(x, x, t, **kw),
+             lambda **kw: ops.linear_cross_entropy_backward(x, x, t, per, per, **kw)]
+    for k, call in enumerate(calls):
+        for kw, want in (({}, "current"), ({"stream": given}, given)):
+            seen.clear()
+            recorded.clear()
+            call(**kw)
+            assert seen and all(s is want for s in seen), (k, want, seen)
+            # what is returned may be used and freed where the caller works
+            assert ("current" in recorded) == bool(kw), (k, recorded)
+    with pytest.raises(ValueError, match="stream"):
+        given.device = torch.device("meta")
+        calls[0](stream=given)
