@@ -461,7 +461,8 @@ ROTOR_API int32_t rotor_embedding(int32_t type, int64_t n_tokens, int64_t n_rows
                                   void *d_y, int64_t y_pitch, void *stream);
 
 /* Device workspace of rotor_embedding_backward for these sizes: the tokens
- * in sorted order, twice, and two rows of sums per 32 tokens.  Host only.
+ * in sorted order, twice, two rows of sums per 32 tokens and, past 32768
+ * tokens, 512 KiB of counts.  Host only.
  * Returns ROTOR_OK or ROTOR_EINVAL. */
 ROTOR_API int32_t rotor_embedding_workspace_bytes(int64_t n_tokens, int64_t n_rows, int64_t cols, uint64_t *bytes);
 

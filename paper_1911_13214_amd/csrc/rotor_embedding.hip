@@ -2,11 +2,12 @@
 // by sorted tokens.
 //
 // Backward: a stable radix sort of (token, position), one launch per digit of
-// up to 9 bits (one in all for up to 2048 tokens), whose few workgroups share
-// the device with others that clear the gradient; then one launch in which groups of lanes take 32 sorted
-// positions each, add the rows of one token in registers and write each token
-// that lies within their positions; then one launch that joins the tokens
-// that cross the 32-position cuts.  No atomics on the sums: their order
+// up to 9 bits (one in all for up to 2048 tokens; past 32768 tokens one more per
+// digit, for its counts), whose few workgroups share the device with others
+// that clear the gradient; then one launch in which groups of lanes take 32
+// sorted positions each, add the rows of one token in registers and write each
+// token that lies within their positions; then one launch that joins the
+// tokens that cross the 32-position cuts.  No atomics on the sums: their order
 // depends on the tokens alone.
 #include "rotor_ops.h"
 
@@ -20,6 +21,8 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kPart = 2048;    // keys that one workgroup of the sort moves
 constexpr int kDigits = 512;
+constexpr int kFewParts = 16;   // parts whose workgroups count all keys
+constexpr int kMostSlabs = 256; // workgroups that sort more parts
 
 // First column of piece k of a row, V columns each.  The last piece is moved
 // back to end with the row: what it shares with the one before is computed
@@ -80,11 +83,16 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const void *tokens, in
 
 // One pass of a stable radix sort over the digit key >> shift, `bits` wide
 // (<= 9).  The first pass reads the tokens and leaves out those without a
-// gradient; later ones read the pass before.  Every workgroup counts all keys
-// (the digits of the keys before its own part and of all), so no pass needs a
-// launch for its counts: 4 bytes a key from the L2, against the 2 cols bytes
-// of its row that the sums read later.  The sort of 32768 tokens (two passes)
-// takes less than the clearing beside it (134 MB, 27 us a pass, 5.0 TB/s).
+// gradient; later ones read the pass before.  Up to kFewParts parts of 2048
+// keys, a workgroup takes one part and counts all keys (the digits of the keys
+// before its own part and of all), so no pass needs a launch for its counts:
+// parts times 4 or 8 bytes a key, from the L2.  The sort of 32768 tokens (16
+// parts, two passes) takes less than the clearing beside it (134 MB, 27 us a
+// pass, 5.0 TB/s).  That grows with the square of the tokens, so of more parts
+// the digits are counted once, in a launch of their own, by at most kMostSlabs
+// workgroups, which take several parts in turn and add each other's counts
+// (gradient of 65536 x 8 bf16, us without and with that launch: 16384 tokens 34
+// and 37, 32768 39 and 36, 65536 48 and 38, 2^20 640 and 142, 2^22 8070 and 388).
 struct SortArgs {
     const void *tokens;
     int token_bytes;
@@ -95,6 +103,8 @@ struct SortArgs {
     int shift, bits;
     int passes;      // of this launch: all of them if one workgroup sorts, else one
     uint32_t parts;  // workgroups that sort; the others clear rows [clear_from, clear_to) of out
+    int64_t slab;    // keys of one of them: a multiple of kPart
+    uint32_t *table; // [parts][kDigits] counts of their digits, or NULL: every one counts all keys
     int64_t clear_from, clear_to, cols, out_pitch;
 };
 
@@ -150,6 +160,41 @@ struct SortShared {
     uint32_t wave_total[kSortWaves];
 };
 
+// The digits of a workgroup's keys, for a sort of many parts.
+template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void count_kernel(SortArgs a)
+{
+    __shared__ uint32_t counts[kDigits][kCopies];
+    const int tid = threadIdx.x;
+    for (int d = tid; d < kDigits * kCopies; d += kSortThreads)
+        (&counts[0][0])[d] = 0;
+    __syncthreads();
+    const uint32_t mask = (1u << a.bits) - 1;
+    const int64_t n = FIRST ? a.n : (int64_t)*a.count;
+    const int64_t begin = (int64_t)blockIdx.x * a.slab, end = begin + a.slab < n ? begin + a.slab : n;
+    constexpr int kAhead = kPart / kSortThreads;
+    for (int64_t i0 = begin + tid; i0 < end; i0 += kPart) {
+        uint32_t key[kAhead];
+        bool have[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int64_t i = i0 + q * kSortThreads;
+            have[q] = sort_key<FIRST>(a, i < end ? i : i0, key[q]) && i < end;
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            if (have[q])
+                atomicAdd(&counts[key[q] >> a.shift & mask][tid % kCopies], 1u);
+    }
+    __syncthreads();
+    if (tid < kDigits) {
+        uint32_t all = 0;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c)
+            all += counts[tid][c];
+        a.table[(int64_t)blockIdx.x * kDigits + tid] = all;
+    }
+}
+
 template <bool FIRST> __device__ void sort_pass(const SortArgs &a, SortShared &sh)
 {
     auto &before = sh.before, &from = sh.from;
@@ -158,7 +203,7 @@ template <bool FIRST> __device__ void sort_pass(const SortArgs &a, SortShared &s
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const uint32_t mask = (1u << a.bits) - 1;
     const int64_t n = FIRST ? a.n : (int64_t)*a.count;
-    const int64_t part = (int64_t)blockIdx.x * kPart;
+    const int64_t begin = (int64_t)blockIdx.x * a.slab, end = begin + a.slab < n ? begin + a.slab : n;
     for (int d = tid; d < kDigits; d += kSortThreads) {
 #pragma unroll
         for (int c = 0; c < kCopies; ++c)
@@ -167,102 +212,130 @@ template <bool FIRST> __device__ void sort_pass(const SortArgs &a, SortShared &s
             at[w][d] = 0;
     }
     __syncthreads();
-    if (part >= n && !(FIRST && blockIdx.x == 0))
+    if (begin >= n && !(FIRST && blockIdx.x == 0))
         return;  // the whole workgroup
-    // digits of the keys before the part, and of the rest
-    // (loads in batches: one at a time would take its latency for each)
-    constexpr int kAhead = 8;
-    for (int64_t i0 = tid; i0 < n; i0 += kSortThreads * kAhead) {
-        uint32_t key[kAhead];
-        bool have[kAhead];
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            const int64_t i = i0 + q * kSortThreads;
-            have[q] = sort_key<FIRST>(a, i < n ? i : i0, key[q]) && i < n;
+    // digits of the keys before the workgroup's own, and of the rest
+    if (a.table) {
+        uint32_t b = 0, f = 0;
+        const int d = tid % kDigits, first = tid / kDigits;
+#pragma unroll 8
+        for (uint32_t p = first; p < a.parts; p += kSortThreads / kDigits) {
+            const uint32_t c = a.table[(int64_t)p * kDigits + d];
+            b += p < blockIdx.x ? c : 0;
+            f += p < blockIdx.x ? 0 : c;
         }
+        before[d][first] = b;
+        from[d][first] = f;
+    } else {
+        // (loads in batches: one at a time would take its latency for each)
+        constexpr int kAhead = 8;
+        for (int64_t i0 = tid; i0 < n; i0 += kSortThreads * kAhead) {
+            uint32_t key[kAhead];
+            bool have[kAhead];
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q)
-            if (have[q])
-                atomicAdd(&(i0 + q * kSortThreads < part ? before : from)[key[q] >> a.shift & mask][lane % kCopies],
-                          1u);
-    }
-    // each wave's own keys, kPart / kSortWaves adjacent ones, and their digits
-    constexpr int kOwn = kPart / kSortWaves / 64;
-    const int64_t own = part + (int64_t)wave * kOwn * 64 + lane;
-    uint32_t key[kOwn], pos[kOwn];
-    bool have[kOwn];
+            for (int q = 0; q < kAhead; ++q) {
+                const int64_t i = i0 + q * kSortThreads;
+                have[q] = sort_key<FIRST>(a, i < n ? i : i0, key[q]) && i < n;
+            }
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-        const int64_t i = own + k * 64;
-        have[k] = i < n;
-        key[k] = pos[k] = 0;
-        if (have[k]) {
-            have[k] = sort_key<FIRST>(a, i, key[k]);
-            pos[k] = FIRST ? (uint32_t)i : a.pos_in[i];
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < kOwn; ++k)
-        if (have[k])
-            atomicAdd(&at[wave][key[k] >> a.shift & mask], 1u);
-    __syncthreads();
-    // first place of each digit (threads 0..511, one digit each), then of
-    // each wave's first key of that digit
-    uint32_t all = 0, earlier = 0;
-    if (tid < kDigits)
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) {
-            earlier += before[tid][c];
-            all += from[tid][c];
-        }
-    all += earlier;
-    uint32_t upto = all;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const uint32_t u = __shfl_up(upto, off);
-        if (lane >= off)
-            upto += u;
-    }
-    if (lane == 63)
-        wave_total[wave] = upto;
-    __syncthreads();
-    if (tid < kDigits) {
-        uint32_t base = upto - all;
-        for (int w = 0; w < wave; ++w)
-            base += wave_total[w];
-        base += earlier;
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = at[w][tid];
-            at[w][tid] = base;
-            base += c;
+            for (int q = 0; q < kAhead; ++q)
+                if (have[q])
+                    atomicAdd(&(i0 + q * kSortThreads < begin ? before
+                                                              : from)[key[q] >> a.shift & mask][lane % kCopies],
+                              1u);
         }
     }
-    if (FIRST && blockIdx.x == 0 && tid == 0) {
-        uint32_t total = 0;
-        for (int w = 0; w < kDigits / 64; ++w)
-            total += wave_total[w];
-        *a.count = (int32_t)total;
-    }
-    __syncthreads();
-    // 64 keys at a time, in order: a key's place is its digit's next one plus
-    // the lanes before it that hold the same digit
+    uint32_t base = 0;  // place of the next key of digit `tid`
+    for (int64_t part = begin;; part += kPart) {
+        // each wave's keys of the part, kPart / kSortWaves adjacent ones, and
+        // their digits
+        constexpr int kOwn = kPart / kSortWaves / 64;
+        const int64_t own = part + (int64_t)wave * kOwn * 64 + lane;
+        uint32_t key[kOwn], pos[kOwn];
+        bool have[kOwn];
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-        const uint32_t d = key[k] >> a.shift & mask;
-        uint64_t same = __ballot(have[k]);
-        for (int b = 0; b < a.bits; ++b) {
-            const uint64_t set = __ballot(have[k] && (d >> b & 1));
-            same &= d >> b & 1 ? set : ~set;
+        for (int k = 0; k < kOwn; ++k) {
+            const int64_t i = own + k * 64;
+            have[k] = i < n;
+            key[k] = pos[k] = 0;
+            if (have[k]) {
+                have[k] = sort_key<FIRST>(a, i, key[k]);
+                pos[k] = FIRST ? (uint32_t)i : a.pos_in[i];
+            }
         }
-        if (have[k]) {
-            const uint32_t place = at[wave][d] + __popcll(same & ((1ull << lane) - 1));
-            a.key_out[place] = key[k];
-            a.pos_out[place] = pos[k];
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k)
+            if (have[k])
+                atomicAdd(&at[wave][key[k] >> a.shift & mask], 1u);
+        __syncthreads();
+        if (part == begin) {
+            // first place of each digit (threads 0..511, one digit each)
+            uint32_t all = 0, earlier = 0;
+            if (tid < kDigits)
+#pragma unroll
+                for (int c = 0; c < kCopies; ++c) {
+                    earlier += before[tid][c];
+                    all += from[tid][c];
+                }
+            all += earlier;
+            uint32_t upto = all;
+#pragma unroll
+            for (int off = 1; off < 64; off *= 2) {
+                const uint32_t u = __shfl_up(upto, off);
+                if (lane >= off)
+                    upto += u;
+            }
+            if (lane == 63)
+                wave_total[wave] = upto;
+            __syncthreads();
+            if (tid < kDigits) {
+                base = upto - all;
+                for (int w = 0; w < wave; ++w)
+                    base += wave_total[w];
+                base += earlier;
+            }
+            if (FIRST && blockIdx.x == 0 && tid == 0) {
+                uint32_t total = 0;
+                for (int w = 0; w < kDigits / 64; ++w)
+                    total += wave_total[w];
+                *a.count = (int32_t)total;
+            }
         }
-        wave_sync();
-        if (have[k] && (same >> lane) == 1)  // the last lane of its digit
-            at[wave][d] += __popcll(same);
-        wave_sync();
+        // then of each wave's first key of that digit
+        if (tid < kDigits)
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = at[w][tid];
+                at[w][tid] = base;
+                base += c;
+            }
+        __syncthreads();
+        // 64 keys at a time, in order: a key's place is its digit's next one
+        // plus the lanes before it that hold the same digit
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const uint32_t d = key[k] >> a.shift & mask;
+            uint64_t same = __ballot(have[k]);
+            for (int b = 0; b < a.bits; ++b) {
+                const uint64_t set = __ballot(have[k] && (d >> b & 1));
+                same &= d >> b & 1 ? set : ~set;
+            }
+            if (have[k]) {
+                const uint32_t place = at[wave][d] + __popcll(same & ((1ull << lane) - 1));
+                a.key_out[place] = key[k];
+                a.pos_out[place] = pos[k];
+            }
+            wave_sync();
+            if (have[k] && (same >> lane) == 1)  // the last lane of its digit
+                at[wave][d] += __popcll(same);
+            wave_sync();
+        }
+        if (part + kPart >= end)
+            break;  // the whole workgroup
+        __syncthreads();
+        for (int d = tid; d < kDigits; d += kSortThreads)
+            for (int w = 0; w < kSortWaves; ++w)
+                at[w][d] = 0;
+        __syncthreads();
     }
 }
 
@@ -429,9 +502,10 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void join_ke
     store_vec(out + (int64_t)key * a.out_pitch + c, sum);
 }
 
-// Workspace: key and position arrays of two passes, the count, the partial sums.
+// Workspace: key and position arrays of two passes, the count, the digits'
+// counts of many parts, the partial sums.
 struct EmbedLayout {
-    uint64_t key[2], pos[2], count, part, total;
+    uint64_t key[2], pos[2], count, table, part, total;
     int64_t part_pitch;
 };
 
@@ -449,6 +523,7 @@ EmbedLayout embed_layout(int64_t n, int64_t cols)
         l.pos[k] = take(4 * (uint64_t)n);
     }
     l.count = take(4);
+    l.table = take(ceil_div(n, kPart) > kFewParts ? 4ull * kMostSlabs * kDigits : 0);
     l.part_pitch = ceil_div(cols, kVec) * kVec;
     l.part = take(8 * (uint64_t)ceil_div(n, kChunk) * (uint64_t)l.part_pitch);
     l.total = at;
@@ -537,7 +612,11 @@ int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows,
     a.padding = padding;
     a.count = (int32_t *)(w + l.count);
     a.bits = width;
-    a.parts = (uint32_t)(n_tokens > 0 ? ceil_div(n_tokens, kPart) : 1);
+    const int64_t parts = n_tokens > 0 ? ceil_div(n_tokens, kPart) : 1;
+    const bool many = parts > kFewParts;
+    a.slab = kPart * ceil_div(parts, many ? kMostSlabs : parts);
+    a.parts = (uint32_t)(many ? ceil_div(n_tokens, a.slab) : parts);
+    a.table = many ? (uint32_t *)(w + l.table) : nullptr;
     a.cols = cols;
     a.out_pitch = dtable_pitch;
     SumArgs b;
@@ -580,6 +659,8 @@ int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows,
                 cols < kVec ? (p == 0 ? sort_kernel<T, 1, false, true> : sort_kernel<T, 1, false, false>)
                 : past      ? (p == 0 ? sort_kernel<T, kVec, true, true> : sort_kernel<T, kVec, true, false>)
                             : (p == 0 ? sort_kernel<T, kVec, false, true> : sort_kernel<T, kVec, false, false>);
+            if (many)
+                (p == 0 ? count_kernel<true> : count_kernel<false>)<<<dim3(a.parts), kSortThreads, 0, s>>>(a);
             sort<<<grid, kSortThreads, 0, s>>>(a, out);
         }
         const auto sum = cols >= kVec ? sum_kernel<T, kVec> : sum_kernel<T, 1>;

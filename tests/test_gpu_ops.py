@@ -175,6 +175,48 @@ def test_embedding_gradient_by_table_size(n, rows):
     m.close(ops.embedding_backward(tokens.cuda(), dy.cuda(), rows), ref, (n + 4) * m.U32 * mag)
 
 
+@pytest.mark.parametrize("n,rows", [(32768, 300), (32769, 70000), (140001, 300), (530000, 70000), (1100003, 3000000)])
+@pytest.mark.parametrize("kind", ["uniform", "one", "skewed"])
+def test_embedding_gradient_of_many_tokens(n, rows, kind):
+    # the largest sort whose workgroups count all keys, and some whose digits
+    # are counted beforehand: one, two and three of them, one to three parts a
+    # workgroup, the last one not whole
+    print("embedding gradient of many tokens", n, rows, kind, flush=True)
+    g = torch.Generator().manual_seed(n + rows)
+    tokens = tokens_of(kind, n, rows, g)
+    dy = m.normal(g, n, 3, dtype=torch.float32)
+    out = ops.embedding_backward(tokens.cuda(), dy.cuda(), rows, padding=1)
+    ref, mag = m.embedding_grad(tokens, dy, rows, 1.0, 1)
+    m.close(out, ref, (n + 4) * m.U32 * mag)
+    assert torch.equal(out, ops.embedding_backward(tokens.int().cuda(), dy.cuda(), rows, padding=1))
+    # exact in whole numbers: no token is lost or added twice
+    dy = torch.randint(-3, 4, (n, 3), generator=g).float()
+    ref, mag = m.embedding_grad(tokens, dy, rows, 1.0, 1)
+    if float(mag.max()) < 2.0 ** 24:
+        assert torch.equal(ops.embedding_backward(tokens.cuda(), dy.cuda(), rows, padding=1).cpu().double(), ref)
+
+
+def test_embedding_gradients_time_does_not_grow_with_the_square_of_the_tokens():
+    # four times the tokens: four times the time and, for the caches' sake, at
+    # most half as much again, where a cost that grows with their square gives
+    # sixteen times
+    ms = []
+    for n in (1 << 20, 1 << 22):
+        tokens = torch.randint(0, 500, (n,), device="cuda")
+        dy = torch.ones(n, 1, device="cuda")
+        ops.embedding_backward(tokens, dy, 500)
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        for _ in range(5):
+            out = ops.embedding_backward(tokens, dy, 500)
+        b.record()
+        b.synchronize()
+        assert int(out.sum()) == n
+        ms.append(a.elapsed_time(b))
+    print("embedding gradient, ms of five", ms, flush=True)
+    assert ms[1] < 6 * ms[0], ms
+
+
 def test_embedding_gradient_ignores_what_has_none():
     g = torch.Generator().manual_seed(4)
     tokens = torch.randint(0, 50, (300,), generator=g)
