@@ -454,8 +454,8 @@ ROTOR_API int32_t rotor_dropout(int32_t type, int64_t rows, int64_t cols, const 
  *             signed.  A token outside [0, n_rows) reads nothing and gives a
  *             row of NaN.
  *   d_table   DEVICE [n_rows][cols];  d_y DEVICE, written [n_tokens][cols].
- * n_tokens < 2^31, 1 <= n_rows < 2^31.  Returns ROTOR_OK, ROTOR_EINVAL or
- * ROTOR_EDEVICE. */
+ * n_tokens < 2^31, 1 <= n_rows < 2^31, cols < 2^31 (its gradient: cols <=
+ * 33553920).  Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
 ROTOR_API int32_t rotor_embedding(int32_t type, int64_t n_tokens, int64_t n_rows, int64_t cols, const void *d_tokens,
                                   int32_t token_bytes, const void *d_table, int64_t table_pitch, double scale,
                                   void *d_y, int64_t y_pitch, void *stream);

@@ -54,7 +54,7 @@ __device__ inline uint32_t bits_of(const uint32_t (&c)[4], int k)
 template <typename T, bool PACKED, bool RESIDUAL>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(const T *x, const T *res, T *y, DropArgs a)
 {
-    const uint64_t g = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+    const uint64_t g = (uint64_t)block_at() * kThreads + threadIdx.x;
     const uint64_t n = (uint64_t)a.rows * (uint64_t)a.cols;
     const uint64_t i0 = g * kGroup;
     if (i0 >= n)
@@ -112,8 +112,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const T *x, const T *
 
 template <typename T> void launch(const void *x, const void *res, void *y, const DropArgs &a, hipStream_t s)
 {
-    const int64_t groups = ceil_div(a.rows * a.cols, kGroup);
-    const dim3 grid((uint32_t)ceil_div(groups, kThreads));
+    const dim3 grid = grid_of(ceil_div(a.rows * a.cols, (int64_t)kThreads * kGroup));
     const bool packed = a.x_pitch == a.cols && a.y_pitch == a.cols && (!res || a.r_pitch == a.cols);
     if (packed && res)
         dropout_kernel<T, true, true><<<grid, kThreads, 0, s>>>((const T *)x, (const T *)res, (T *)y, a);
@@ -142,8 +141,7 @@ extern "C" int32_t rotor_dropout(int32_t type, int64_t rows, int64_t cols, const
         return ROTOR_EINVAL;
     if (rows == 0)
         return ROTOR_OK;
-    // one block of the grid holds kThreads * kGroup elements
-    if (ceil_div(rows * cols, (int64_t)kThreads * kGroup) > 0x7FFFFFFF)
+    if (!grid_ok(ceil_div(rows * cols, (int64_t)kThreads * kGroup)))
         return ROTOR_EINVAL;
     DropArgs a;
     a.rows = rows;

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const void *tokens, in
                                                           int64_t cols, const T *table, int64_t pitch, float scale,
                                                           T *y, int64_t y_pitch)
 {
-    const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    const int64_t i = block_at_xz() * (kThreads / 64) + threadIdx.x / 64;
     if (i >= n)
         return;
     const int64_t t = token_at(tokens, token_bytes, i);
@@ -385,13 +385,13 @@ struct SumArgs {
 template <typename T, int V> __global__ __launch_bounds__(kThreads) void sum_kernel(const T *dy, T *out, SumArgs a)
 {
     const int64_t n = *a.count;
-    const int64_t chunk = (int64_t)(blockIdx.x / a.slices) * (kThreads / a.lanes) +
-                          __builtin_amdgcn_readfirstlane(threadIdx.x / a.lanes);
+    const int64_t block = block_at(), strip = block / a.slices;
+    const int64_t chunk = strip * (kThreads / a.lanes) + __builtin_amdgcn_readfirstlane(threadIdx.x / a.lanes);
     const int64_t begin = chunk * kChunk;
     if (begin >= n)
         return;
     const int64_t end = begin + kChunk < n ? begin + kChunk : n;
-    const int64_t piece = (int64_t)(blockIdx.x % a.slices) * a.lanes + threadIdx.x % a.lanes;
+    const int64_t piece = (block - strip * a.slices) * a.lanes + threadIdx.x % a.lanes;
     if ((piece - threadIdx.x % 64) * V >= a.cols)
         return;  // the whole wave
     // lanes past the row's end repeat its last piece
@@ -454,7 +454,7 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void join_ke
 {
     __shared__ float other[kThreads / 64 - 1][64][V + 1];
     const int64_t n = *a.count;
-    const int64_t chunk = blockIdx.x;
+    const int64_t chunk = block_at_xz();
     const int64_t end = (chunk + 1) * kChunk;
     if (end >= n)
         return;
@@ -563,8 +563,7 @@ int32_t rotor_embedding(int32_t type, int64_t n_tokens, int64_t n_rows, int64_t 
         const int64_t pieces = ceil_div(cols, 64 * kVec);
         const int64_t slices = n_tokens >= 1024 ? 1 : pieces < 64 ? pieces : 64;
         const auto kernel = cols >= kVec ? lookup_kernel<T, kVec> : lookup_kernel<T, 1>;
-        kernel<<<dim3((uint32_t)ceil_div(n_tokens, kThreads / 64), (uint32_t)slices), kThreads, 0,
-                 (hipStream_t)stream>>>(d_tokens, token_bytes, n_tokens, n_rows, cols, (const T *)d_table,
+        kernel<<<grid_of(ceil_div(n_tokens, kThreads / 64), slices), kThreads, 0, (hipStream_t)stream>>>(d_tokens, token_bytes, n_tokens, n_rows, cols, (const T *)d_table,
                                         table_pitch, (float)scale, (T *)d_y, y_pitch);
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
@@ -636,7 +635,7 @@ int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows,
     b.slices = (uint32_t)ceil_div(cols, (int64_t)b.lanes * kVec);
     const int64_t sum_blocks = ceil_div(chunks, kThreads / b.lanes) * b.slices;
     const int64_t join_slices = ceil_div(cols, 64 * kVec);
-    if (join_slices > 65535 || sum_blocks > 0x7FFFFFFF)
+    if (join_slices > 65535 || !grid_ok(sum_blocks))
         return ROTOR_EINVAL;
     with_type(type, [&](auto e) {
         typedef typename decltype(e)::T T;
@@ -666,9 +665,9 @@ int32_t rotor_embedding_backward(int32_t type, int64_t n_tokens, int64_t n_rows,
         const auto sum = cols >= kVec ? sum_kernel<T, kVec> : sum_kernel<T, 1>;
         const auto join = cols >= kVec ? join_kernel<T, kVec> : join_kernel<T, 1>;
         if (chunks > 0)
-            sum<<<dim3((uint32_t)sum_blocks), kThreads, 0, s>>>((const T *)d_dy, out, b);
+            sum<<<grid_of(sum_blocks), kThreads, 0, s>>>((const T *)d_dy, out, b);
         if (chunks > 1)
-            join<<<dim3((uint32_t)(chunks - 1), (uint32_t)join_slices), kThreads, 0, s>>>(out, b);
+            join<<<grid_of(chunks - 1, join_slices), kThreads, 0, s>>>(out, b);
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
 }

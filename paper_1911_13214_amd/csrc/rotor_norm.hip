@@ -154,7 +154,7 @@ __global__ __launch_bounds__(Team<TH>::kBlock) void norm_kernel(const T *x, cons
     __shared__ float red[2][16][2];
     int half = 0;
     const int t = threadIdx.x % TH;
-    const int64_t r = (int64_t)blockIdx.x * Team<TH>::kRows + threadIdx.x / TH;
+    const int64_t r = block_at() * Team<TH>::kRows + threadIdx.x / TH;
     if (r >= a.rows)
         return;  // whole waves, and no barrier where a workgroup holds several rows
     const Pieces<TH, V, N> p(t, (int)a.cols);
@@ -383,7 +383,9 @@ __global__ __launch_bounds__(TH) void wide_row_kernel(const T *dy, const T *dh, 
 {
     __shared__ float red[2][16][2];
     int half = 0;
-    const int64_t r = blockIdx.x;
+    const int64_t r = block_at();
+    if (r >= a.rows)
+        return;  // the whole workgroup
     const Pieces<TH, V, N> p(threadIdx.x, (int)a.cols);
     const float inv = 1.f / (float)a.cols;
     const float4 st = *(const float4 *)(a.stats + 4 * r);
@@ -708,7 +710,7 @@ int32_t rotor_residual_norm(const rotor_norm *how, const void *d_x, int64_t x_pi
         with_shape(cols, [&](auto th, auto v, auto n) {
             constexpr int TH = decltype(th)::v;
             norm_kernel<T, TH, decltype(v)::v, decltype(n)::v>
-                <<<dim3((uint32_t)ceil_div(rows, Team<TH>::kRows)), Team<TH>::kBlock, 0, (hipStream_t)stream>>>(
+                <<<grid_of(ceil_div(rows, Team<TH>::kRows)), Team<TH>::kBlock, 0, (hipStream_t)stream>>>(
                     (const T *)d_x, (const T *)d_z, (T *)d_y, (T *)d_h, a);
         });
     });
@@ -813,7 +815,7 @@ int32_t rotor_residual_norm_backward(const rotor_norm *how, const void *d_dy, in
             } else {
                 if (rows > 0)
                     wide_row_kernel<T, TH, V, N>
-                        <<<dim3((uint32_t)rows), TH, 0, st>>>(dy, dh, y, z, (T *)d_dx, (T *)d_dz, a);
+                        <<<grid_of(rows), TH, 0, st>>>(dy, dh, y, z, (T *)d_dx, (T *)d_dz, a);
                 if (last >= 0 || gate_here)
                     wide_sum_kernel<T>
                         <<<dim3((uint32_t)plan.blocks, (uint32_t)ceil_div(cols, 256 * kVec)), 256, 0, st>>>(dy, dh, y,

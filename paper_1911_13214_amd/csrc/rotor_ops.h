@@ -93,6 +93,26 @@ template <typename F> inline void with_type(int32_t type, F f)
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A grid of `blocks` workgroups, of up to 1024 threads each.  Along one index it
+// holds fewer than 2^32 threads (more of them are not refused: the number
+// wraps, and the rest never runs), so workgroups past 2^20 go along a second
+// index; block_at is a workgroup's place, past `blocks` for some of the last.
+constexpr int64_t kGridX = (int64_t)1 << 20;
+inline bool grid_ok(int64_t blocks) { return blocks <= kGridX * 65535; }
+inline dim3 grid_of(int64_t blocks)
+{
+    return blocks <= kGridX ? dim3((uint32_t)blocks) : dim3((uint32_t)kGridX, (uint32_t)ceil_div(blocks, kGridX));
+}
+__device__ inline int64_t block_at() { return blockIdx.x + (int64_t)blockIdx.y * gridDim.x; }
+// The same where y is taken: the second index is z.
+inline dim3 grid_of(int64_t blocks, int64_t y)
+{
+    const dim3 g = grid_of(blocks);
+    return dim3(g.x, (uint32_t)y, g.y);
+}
+__device__ inline int64_t block_at_xz() { return blockIdx.x + (int64_t)blockIdx.z * gridDim.x; }
+
 inline uint64_t round256(uint64_t x) { return (x + 255) / 256 * 256; }
 
 // A matrix operand: pitch >= cols, pointer aligned to its elements, byte

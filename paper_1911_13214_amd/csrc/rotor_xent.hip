@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t rows, i
 {
     typedef typename ProductOf<T>::P P;
     constexpr int kParts = ProductOf<T>::kParts;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, pieces = cols_to / 8;
+    const int64_t at = block_at() * 256 + threadIdx.x, pieces = cols_to / 8;
     const int64_t r = at / pieces, c = at % pieces * 8;
     if (r >= rows)
         return;
@@ -847,7 +847,7 @@ Operand<typename ProductOf<T>::P> operand(const T *src, int64_t rows, int64_t co
     constexpr int64_t parts = ProductOf<T>::kParts;
     if (!pack)
         return Operand<P>{(const P *)src, rows, cols, pitch, 0};
-    pack_kernel<T><<<dim3((uint32_t)ceil_div(rows * (dk / 8), 256)), 256, 0, s>>>(
+    pack_kernel<T><<<grid_of(ceil_div(rows * (dk / 8), 256)), 256, 0, s>>>(
         src, rows, cols, pitch, (P *)space, parts * dk, dk, dk);
     return Operand<P>{(const P *)space, rows, pad(cols, 8), parts * dk, parts > 1 ? dk : 0};
 }

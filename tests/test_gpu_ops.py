@@ -818,3 +818,78 @@ def test_a_call_on_a_stream_keeps_off_blocks_that_another_one_still_uses():
 
 def tensors_of(out):
     return list(out.values()) if isinstance(out, dict) else list(out) if isinstance(out, tuple) else [out]
+
+
+# ---- more workgroups than a grid holds along one index -----------------------------
+
+def test_dropout_of_more_elements_than_one_grid_index_holds():
+    n = 2 ** 35 + 4099
+    if torch.cuda.mem_get_info()[0] < 2 * n + (8 << 30):
+        pytest.skip("needs 72 GiB")
+    print("dropout", n, flush=True)
+    x = torch.ones(n, dtype=torch.float16, device="cuda")
+    assert ops.dropout(x, 0.5, 2 ** 40 + 3, 8, out=x) is x
+    for first in (0, 2 ** 34 - 64, 2 ** 35 - 4096, n - n % 8 - 64):
+        have = x[first:first + 4096].cpu()
+        keep = [word >> (16 * half) & 0xFFFF
+                for g in range(first // 8, -(-(first + have.numel()) // 8))
+                for word in m.philox((g & 0xFFFFFFFF, g >> 32, 8, 0), (3, 2 ** 8)) for half in range(2)]
+        keep = torch.tensor(keep[:have.numel()]) >= 2 ** 15
+        assert torch.equal(have, torch.where(keep, 2.0, 0.0).half()), first
+    # every element was reached: none is left at 1
+    assert all(not (part == 1).any() for part in x.split(2 ** 31))
+
+
+def test_residual_norm_of_more_rows_than_one_grid_index_holds():
+    rows = 2 ** 26 + 5
+    print("residual norm", rows, flush=True)
+    x = torch.randn(rows, 2, device="cuda", dtype=torch.float16)
+    _, h, _ = ops.residual_norm(x, pre="rms", stats=False)
+    half = rows // 2
+    for a, b in ((0, half), (half, rows)):
+        assert torch.equal(h[a:b], ops.residual_norm(x[a:b], pre="rms", stats=False)[1])
+
+
+def test_embedding_of_more_tokens_than_one_grid_index_holds():
+    n = 2 ** 26 + 5
+    print("embedding", n, flush=True)
+    tokens = torch.randint(0, 50, (n,), device="cuda", dtype=torch.int32)
+    table = torch.randn(50, 2, device="cuda", dtype=torch.float16)
+    assert torch.equal(ops.embedding(tokens, table), table[tokens])
+
+
+def test_embedding_gradient_of_more_tokens_than_one_grid_index_holds():
+    n = 2 ** 29 + 77
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    print("embedding gradient", n, flush=True)
+    tokens = torch.randint(0, 500, (n,), device="cuda", dtype=torch.int32)
+    tokens[:1000] = 499
+    dy = torch.ones(n, 1, device="cuda")
+    out = ops.embedding_backward(tokens, dy, 500)
+    counts = sum(torch.bincount(part, minlength=500) for part in tokens.split(2 ** 27))
+    assert torch.equal(out[:, 0].long(), counts) and int(counts.max()) < 2 ** 24
+
+
+def test_cross_entropy_of_more_copies_than_one_grid_index_holds():
+    # rows of an odd pitch are copied, eight columns a thread: 2^32 threads.
+    # Seven kinds of rows; a logit is within 2^-24 a product of its terms'
+    # magnitudes' sum, lse and loss within that and a few roundings.
+    n, cols = 2 ** 19 + 9, 65535
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("needs 160 GiB")
+    print("cross entropy copies", n, cols, flush=True)
+    g = torch.Generator().manual_seed(2)
+    kinds = m.normal(g, 7, cols, dtype=torch.bfloat16)
+    w = m.normal(g, 3, cols, dtype=torch.bfloat16, std=2.0 ** -10)
+    h = torch.empty(n, cols, dtype=torch.bfloat16, device="cuda")
+    for k in range(7):
+        h[k::7] = kinds[k].cuda()
+    t = torch.arange(n, device="cuda") % 3
+    loss, lse = ops.linear_cross_entropy(h, w.cuda(), t)
+    ref_loss, ref_lse = m.cross_entropy(kinds.repeat(3, 1), w, torch.arange(21) % 3, -100)
+    slack = (cols + 32) * m.U32 * float((kinds.double().abs() @ w.double().abs().t()).max()) + 2.0 ** -18
+    for out, ref in ((lse, ref_lse), (loss, ref_loss)):
+        m.close(out[:21], ref, 2 * slack)
+        # the same row and target, the same bits
+        assert torch.equal(out, out[:21].repeat(n // 21 + 1)[:n])

@@ -200,3 +200,15 @@ def test_a_call_allocates_on_the_stream_it_is_given(monkeypatch):
     with pytest.raises(ValueError, match="stream"):
         given.device = torch.device("meta")
         calls[0](stream=given)
+
+
+def test_more_workgroups_than_a_grid_holds_are_refused():
+    # 2^20 along one index and 65535 along another
+    f = rotor.lib().rotor_dropout
+    per = 2048  # elements of a workgroup
+    rows = (1 << 20) * 65535 * per // 8 + 1
+    assert f(1, rows, 8, FAKE, 8, None, 0, FAKE, 8, 0.1, 1, 2, None, None) == E
+    need = ctypes.c_uint64()
+    assert rotor.lib().rotor_embedding_workspace_bytes(4, 10, 33553921, ctypes.byref(need)) == rotor.ROTOR_OK
+    assert rotor.lib().rotor_embedding_backward(1, 4, 10, 33553921, FAKE, 8, FAKE, 33553921, 1.0, -1, FAKE, 33553921,
+                                                FAKE, need.value, None) == E
