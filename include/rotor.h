@@ -568,8 +568,8 @@ ROTOR_API int32_t rotor_residual_norm_backward(const rotor_norm *how, const void
  * are multiplied as three bf16 terms each, which keeps their 24 bits.
  *   d_h, d_w    DEVICE [n_tokens][cols] and [n_rows][cols], of one type.
  *   d_targets   DEVICE, n_tokens int64.  A token whose target is `ignore` has
- *               loss 0 and no gradient, whatever its row of h holds; any
- *               other target outside [0, n_rows) gives NaN (loss, its row of
+ *               loss 0 and no gradient, whatever h and w hold; any other
+ *               target outside [0, n_rows) gives NaN (loss, its row of
  *               dh, and dw).
  *   d_loss, d_lse  DEVICE, written: n_tokens floats each.
  *   aligned     1: every row of h and w starts 16-byte aligned and cols is a

@@ -533,11 +533,13 @@ template <typename T> __global__ __launch_bounds__(256) void few_prepare_kernel(
 }
 
 // A gradient from its parts' sums: four columns a thread, Y threads a share of the
-// parts each, the shares then in order.
+// parts each, the shares then in order.  Where rows are tokens (grad is their
+// losses' gradients), those without a gradient are 0 whatever their sums hold: 0
+// times a row of W that is not finite is NaN.
 template <typename T, int Y>
 __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t pitch, int64_t part, int parts,
-                                                     int64_t rows, int64_t cols, const float *scale, T *out,
-                                                     int64_t out_pitch)
+                                                     int64_t rows, int64_t cols, const float *scale,
+                                                     const float *grad, T *out, int64_t out_pitch)
 {
     constexpr int X = 256 / Y;
     __shared__ f32x4 other[Y][X];
@@ -562,6 +564,8 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t p
     }
     if (!in)
         return;
+    if (grad && grad[j] == 0.f)
+        s = f32x4{0.f, 0.f, 0.f, 0.f};
     const float f = *scale;
     const float v[4] = {s[0] * f, s[1] * f, s[2] * f, s[3] * f};
     store_some(out + j * out_pitch + i, cols - i < 4 ? (int)(cols - i) : 4, v);
@@ -830,12 +834,12 @@ void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e,
 // The parts' sums joined, into a gradient.
 template <typename T>
 void finish_rows(const float *sum, int64_t pitch, int64_t part, int parts, int64_t rows, int64_t cols,
-                 const float *scale, T *out, int64_t out_pitch, hipStream_t s)
+                 const float *scale, const float *grad, T *out, int64_t out_pitch, hipStream_t s)
 {
     const int share = parts >= 8 ? 16 : 1;
     const auto finish = share > 1 ? finish_kernel<T, 16> : finish_kernel<T, 1>;
     finish<<<dim3((uint32_t)ceil_div(rows * ceil_div(cols, 4), 256 / share)), 256, 0, s>>>(
-        sum, pitch, part, parts, rows, cols, scale, out, out_pitch);
+        sum, pitch, part, parts, rows, cols, scale, grad, out, out_pitch);
 }
 
 // H or rows of W as a product's operand, copied into `space` if need be.
@@ -1140,8 +1144,8 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                     we.rows = (int)rows;
                     we.add = 0;
                     run_product<true>(ha, pb, Extent{cols, rows, n_tokens, l.w_split}, we, s);
-                    finish_rows(we.c, l.w_pitch, we.part, l.w_split, rows, cols, scale, (T *)d_dw + v0 * dw_pitch,
-                                dw_pitch, s);
+                    finish_rows(we.c, l.w_pitch, we.part, l.w_split, rows, cols, scale, nullptr,
+                                (T *)d_dw + v0 * dw_pitch, dw_pitch, s);
                 } else {
                     OutEpilogue<T> oe;
                     oe.live = live;
@@ -1161,8 +1165,8 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                 sum, l.sum_pitch, cols * l.sum_pitch, l.split, n_tokens, cols, order, live, scale, (T *)d_dh,
                 dh_pitch);
         } else if (d_dh) {
-            finish_rows(sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, (T *)d_dh, dh_pitch,
-                        s);
+            finish_rows(sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, grad, (T *)d_dh,
+                        dh_pitch, s);
         }
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;

@@ -893,3 +893,20 @@ def test_cross_entropy_of_more_copies_than_one_grid_index_holds():
         m.close(out[:21], ref, 2 * slack)
         # the same row and target, the same bits
         assert torch.equal(out, out[:21].repeat(n // 21 + 1)[:n])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,cols", [(3, 300, 64), (40, 700, 33), (64, 300, 64), (150, 700, 72), (150, 700, 71)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_cross_entropy_of_tokens_without_a_target_over_a_row_that_is_not_finite(dtype, n, rows, cols, value):
+    # what the others' gradients turn into does not reach a token without one
+    h, w, t, gl = xent_case(n, rows, cols, dtype, ignored=0.4)
+    t[0], t[1] = 5, -100
+    w[rows // 2, cols // 3] = value
+    gl[2] = 0.0
+    loss, lse = ops.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    dh, _ = ops.linear_cross_entropy_backward(h.cuda(), w.cuda(), t.cuda(), lse, gl.cuda())
+    none = (t == -100) | (gl == 0)
+    assert not loss[(t == -100).cuda()].any()
+    assert torch.equal(dh[none.cuda()], torch.zeros(int(none.sum()), cols, dtype=h.dtype, device="cuda"))
+    assert dh[0].isnan().any()
