@@ -6,7 +6,9 @@ first time, and what it keeps for its backward (w_abar) is what the schedule
 budgets.  So the dropout here draws its mask from (seed, step) and keeps
 nothing, the residual seam keeps its block's output, its sum and 16 bytes a
 row, the loss keeps 4 bytes a token and no logits, and every gradient is the
-same bit for bit on every call.  Second derivatives exist for the dropout
+same bit for bit on every call.  Inputs of any layout are taken, as in
+``linear_cross_entropy(x[:, :-1], w, tokens[:, 1:])``: those that the operators
+refuse are copied (and the copy is what is kept).  Second derivatives exist for the dropout
 alone; the others raise where one is taken.
 
 ``language_chain`` builds a chain of them: token lookup, residual blocks and
@@ -22,14 +24,17 @@ from torch import nn
 from . import ops
 
 
-def _rows(grad):
-    """A gradient as the operators take matrices: one that autograd hands on
-    broadcast or transposed is copied."""
+def _rows(t):
+    """A tensor as the operators take matrices: an input that is a slice of
+    several dimensions or transposed is copied, and a gradient that autograd
+    hands on so or broadcast."""
+    if t is None or t.is_contiguous():
+        return t
     try:
-        ops._matrix(grad, "grad")
+        ops._matrix(t, "t")
     except ValueError:
-        return grad.contiguous()
-    return grad
+        return t.contiguous()
+    return t
 
 
 class _Refuse(torch.autograd.Function):
@@ -65,7 +70,7 @@ class _Dropout(torch.autograd.Function):
         ctx.draw = (p, seed, step)
         # saved, so that autograd notices a step that was advanced in between
         ctx.save_for_backward(step_tensor)
-        return ops.dropout(x, p, seed, step, residual, step_tensor=step_tensor)
+        return ops.dropout(_rows(x), p, seed, step, _rows(residual), step_tensor=step_tensor)
 
     @staticmethod
     def backward(ctx, dy):
@@ -86,9 +91,10 @@ def dropout(x, p, seed, step=0, residual=None, step_tensor=None):
 class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, tokens, table, scale, padding):
+        tokens = tokens.contiguous()
         ctx.save_for_backward(tokens)
         ctx.how = (table.shape[0], scale, padding)
-        return ops.embedding(tokens, table, scale)
+        return ops.embedding(tokens, _rows(table), scale)
 
     @staticmethod
     @_first_order
@@ -108,6 +114,8 @@ _PARAMS = ("post_weight", "post_bias", "gate", "pre_weight", "pre_bias")
 class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, z, post, pre, residual_scale, eps, *params):
+        x, z = _rows(x), _rows(z)
+        params = [_rows(q) if name == "gate" or q is None else q.contiguous() for name, q in zip(_PARAMS, params)]
         ctx.how = dict(post=post, pre=pre, residual_scale=residual_scale, eps=eps)
         y, h, stats = ops.residual_norm(x, z, **ctx.how, **dict(zip(_PARAMS, params)))
         # without a block y is x itself: only h is a result
@@ -141,6 +149,8 @@ def residual_norm(x, z=None, *, post="none", post_weight=None, post_bias=None, g
 class _CrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, h, w, targets, ignore):
+        h, w = _rows(h), _rows(w)
+        targets = (targets.long() if targets.dtype == torch.int32 else targets).contiguous()
         loss, lse = ops.linear_cross_entropy(h, w, targets, ignore)
         ctx.save_for_backward(h, w, targets, lse)
         ctx.ignore = ignore
@@ -156,7 +166,8 @@ class _CrossEntropy(torch.autograd.Function):
 
 
 def linear_cross_entropy(h, w, targets, ignore=-100):
-    """ops.linear_cross_entropy with gradients: the loss of each token."""
+    """ops.linear_cross_entropy with gradients: the loss of each token.
+    ``targets`` may be int32 as well."""
     return _CrossEntropy.apply(h, w, targets, ignore)
 
 

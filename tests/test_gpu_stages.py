@@ -138,3 +138,40 @@ def test_gradients_that_arrive_broadcast_or_transposed():
             a = torch.autograd.grad(y, wrt, dy, retain_graph=True)
             b = torch.autograd.grad(y, wrt, dy.contiguous(), retain_graph=True)
             assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_inputs_that_are_slices_or_transposed():
+    # what the operators refuse (rows that are not one pitch apart, columns
+    # that are not adjacent, tokens that are not dense) is copied, and gives
+    # what the dense tensors give, bit for bit, gradients included
+    from paper_1911_13214_amd import stages as lm
+    g = torch.Generator().manual_seed(14)
+
+    def leaf(*shape):
+        return m.normal(g, *shape, dtype=torch.float32).cuda().requires_grad_()
+
+    x, z = leaf(3, 9, 40), leaf(3, 9, 40)
+    table, gate = leaf(40, 40), leaf(1, 40)
+    tokens = torch.randint(0, 40, (3, 9), generator=g).cuda()
+    before, after = (lambda t: t[:, :-1]), (lambda t: t[:, 1:])
+    turned = lambda t: t.transpose(0, 1)
+    calls = [
+        # the loss of the next token
+        lambda c: lm.linear_cross_entropy(c(before(x)), table, c(after(tokens))),
+        lambda c: lm.linear_cross_entropy(c(before(x)), c(table.t()), c(after(tokens).int())),
+        lambda c: lm.embedding(c(before(tokens)), c(table.t()), 2.0, 3),
+        lambda c: lm.embedding(c(turned(tokens)), table),
+        lambda c: lm.dropout(c(turned(x)), 0.3, 7, 2, c(turned(z))),
+        lambda c: lm.dropout(c(x.transpose(1, 2)), 0.3, 7, 2),
+        lambda c: lm.residual_norm(c(turned(x)), c(turned(z)), post="rms", pre="layer", gate=c(gate.expand(9, 40)),
+                                   pre_weight=c(table[:, 1]))[1],
+        lambda c: lm.residual_norm(c(x.transpose(1, 2)[:, :, ::3]), pre="rms")[1]]
+    for k, call in enumerate(calls):
+        print("input layout", k, flush=True)
+        out = []
+        for c in (lambda t: t, lambda t: t.contiguous()):
+            y = call(c)
+            dy = torch.linspace(-1, 1, y.numel(), device="cuda").view_as(y)
+            out.append([y, *torch.autograd.grad(y, (x, z, table, gate), dy, allow_unused=True)])
+        for a, b in zip(*out):
+            assert (a is None and b is None) or torch.equal(a, b), k
