@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import ops_model as m
+import xent_plan
 from paper_1911_13214_amd import ops
 
 pytestmark = pytest.mark.gpu
@@ -910,3 +911,15 @@ def test_cross_entropy_of_tokens_without_a_target_over_a_row_that_is_not_finite(
     assert not loss[(t == -100).cuda()].any()
     assert torch.equal(dh[none.cuda()], torch.zeros(int(none.sum()), cols, dtype=h.dtype, device="cuda"))
     assert dh[0].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,cols,ignored", xent_plan.CHECKED)
+def test_cross_entropy_through_every_product(dtype, n, rows, cols, ignored):
+    # each of the five products with large and with small tiles, over many
+    # steps, odd and even numbers of them, several tiles a workgroup (which
+    # sizes reach what is held in test_ops.py)
+    print("cross entropy products", dtype, n, rows, cols, ignored, flush=True)
+    h, w, t, gl = xent_case(n, rows, cols, dtype, ignored=0.0)
+    t[torch.randperm(n, generator=torch.Generator().manual_seed(n))[:round(n * ignored)]] = -100
+    check_xent(h, w, t, gl)

@@ -2,10 +2,12 @@
 return ROTOR_EINVAL before any device work, the binding raises ValueError."""
 import contextlib
 import ctypes
+import itertools
 
 import pytest
 import torch
 
+import xent_plan
 from paper_1911_13214_amd import ops, rotor
 
 FAKE = 0x10000
@@ -212,3 +214,39 @@ def test_more_workgroups_than_a_grid_holds_are_refused():
     assert rotor.lib().rotor_embedding_workspace_bytes(4, 10, 33553921, ctypes.byref(need)) == rotor.ROTOR_OK
     assert rotor.lib().rotor_embedding_backward(1, 4, 10, 33553921, FAKE, 8, FAKE, 33553921, 1.0, -1, FAKE, 33553921,
                                                 FAKE, need.value, None) == E
+
+
+def test_the_cross_entropys_plan_in_python_is_the_librarys():
+    need = ctypes.c_uint64()
+    sizes = [1, 3, 17, 33, 64, 65, 300, 2100, 9000, 70001], [1, 8, 63, 300, 1031, 4096, 65536], [1, 300, 24700, 128000]
+    for type, n, d, v, aligned in itertools.product(range(3), *sizes, (0, 1)):
+        for backward, plan in ((0, xent_plan.forward), (1, xent_plan.backward)):
+            assert rotor.lib().rotor_xent_workspace_bytes(type, n, d, v, aligned, backward, ctypes.byref(need)) == 0
+            assert plan(type, n, d, v, aligned)[0] == need.value, (type, n, d, v, aligned, backward)
+
+
+def test_checked_cross_entropies_reach_every_product():
+    # every product with both tiles, in every type; with the large ones an odd
+    # and an even number of steps past the pipeline's first, and more tiles than
+    # the 256 workgroups that run at once
+    seen = set()
+    for type, name in enumerate(("f32", "bf16", "f16")):
+        for n, rows, cols, ignored in xent_plan.CHECKED:
+            aligned = cols % 8 == 0
+            live = round(n * (1 - ignored))
+            runs = xent_plan.forward(type, n, cols, rows, aligned)[1] + \
+                xent_plan.backward(type, n, cols, rows, aligned, live)[1]
+            for what, side, steps, count in runs:
+                seen.add((type, what, side))
+                if side == 256 and steps > 8:
+                    seen |= {(type, what, "odd" if steps % 2 else "even")} | \
+                        ({(type, what, "several")} if count > 256 else set())
+        for what, want in (("stats", (128, 256, "several")), ("prob", (128, 256, "several")),
+                           ("dh", (128, 256, "several")), ("dw", (128, 256)), ("dw split", (128, 256))):
+            for w in want:
+                assert (type, what, w) in seen, (name, what, w)
+            assert (type, what, "even") in seen or (type, what, "odd") in seen, (name, what)
+        if type != xent_plan.F32:  # six products of as many steps each: an even number, where they are not split
+            for what in ("stats", "prob", "dh", "dw"):
+                assert {(type, what, "even"), (type, what, "odd")} <= seen, (name, what)
+    assert {(1, "dw", "several"), (2, "dw", "several")} <= seen
