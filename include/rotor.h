@@ -604,9 +604,12 @@ ROTOR_API int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64
  *                       and the gradient of each loss.
  *   d_dh, d_dw          DEVICE, written, shaped and typed as h and w; either
  *                       may be NULL (not wanted).
- * The probabilities are rounded once to 16 bits (32-bit tensors: kept to 24)
- * before they are multiplied with w and h; sums over the vocabulary and the
- * tokens are taken in an order that depends on the sizes alone. */
+ * The probabilities times a token's gradient are rounded once to 16 bits
+ * (32-bit tensors: kept to 24) before they are multiplied with w and h.  In
+ * float16, where that product is below 2^-40 of the largest gradient of a loss
+ * (2^-48 where the token's own is less than 2^-8 of it), it is lost.  Sums over
+ * the vocabulary and the tokens are taken in an order that depends on the sizes
+ * and on which tokens have a gradient. */
 ROTOR_API int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows, const void *d_h,
                                       int64_t h_pitch, const void *d_w, int64_t w_pitch, const int64_t *d_targets,
                                       int64_t ignore, const float *d_lse, const float *d_grad_loss, void *d_dh,

@@ -43,11 +43,13 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t rows, i
 
 // The tokens that count, in two layouts as operands: packed[r][c] = row
 // order[r] of src, and turned[c][r], which is 0 for r from their number up to
-// the next multiple of 8 (NULL: not wanted).  64 x 64 elements a workgroup
-// through LDS, eight adjacent ones a load and a store.  8192 x 4096 bf16: 23 us.
+// the next multiple of 8 (NULL: not wanted), and whose columns r are multiplied
+// by undo[r] (NULL: 1).  64 x 64 elements a workgroup through LDS, eight adjacent
+// ones a load and a store.  8192 x 4096 bf16: 23 us.
 template <typename P> struct TurnArgs {
     int64_t cols, pitch;
     const int *order, *live;
+    const float *undo;
     P *packed, *turned;
     int64_t packed_pitch, packed_seg, turned_pitch, turned_seg;
 };
@@ -68,9 +70,10 @@ __global__ __launch_bounds__(256) void turn_kernel(const T *src, TurnArgs<typena
         const bool some = r < live;
         const typename VecOf<T, 8>::V v =
             row_piece(src + (int64_t)(some ? a.order[r] : 0) * a.pitch, c0 + col, some ? a.cols : 0);
+        const float u = some && a.undo ? a.undo[r] : 1.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            tile[row][col + e] = (float)v[e];
+            tile[row][col + e] = (float)v[e] * u;
         if (some && c0 + col < a.cols) {
             typename Mfma<P>::Frag t[kParts];
             terms_of<T>(v, t);
@@ -358,19 +361,28 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2 *part, int64_t t
 }
 
 // Gradients of the losses, 0 without a target, divided by the largest and
-// multiplied by 2^12, so that P fits the range of 16-bit floats whatever the
+// multiplied by 2^15, so that P fits the range of 16-bit floats whatever the
 // loss was divided by; `scale` undoes it.  The gradient of a mean or a sum is
-// then 2^12 for every token, and what P holds at the targets, by far the largest
-// of its terms, is 2^12 (p - 1): rounded to 16 bits it is off by a third less on
+// then 2^15 for every token, and what P holds at the targets, by far the largest
+// of its terms, is 2^15 (p - 1): rounded to 16 bits it is off by a third less on
 // average than at gradients between two powers of two, and by p at most for a
 // small p (70 draws in bf16: errors of the gradients up to 1.5 times those of a
 // last rounding alone, with a power of two as the divisor up to twice).
+//
+// Of f16, whose range ends 2^40 below that, the smaller gradients are multiplied
+// by up to 2^8 more, a power of two for each token (undo: its inverse), and the
+// token's column of H^T is divided by it: the probabilities of a token with
+// 2^-20 of the largest gradient would vanish otherwise, and with them their part
+// of its row of dH (60000 x 64, off by a quarter).  2^8, since h in 16 bits stays
+// within its own rounding down to 2^-6.
 struct GradArgs {
     const float *grad_loss;
     const int64_t *targets;
     int64_t ignore, vocab, tokens;
-    float *grad, *scale;
+    int lift;  // the most by which a gradient is multiplied, as a power of two
+    float *grad, *scale, *undo;  // undo: NULL without lift
 };
+constexpr int kTop = 15;
 __device__ inline float grad_size(const GradArgs &a, int64_t j)
 {
     const int64_t t = a.targets[j];
@@ -381,8 +393,14 @@ __device__ inline float grad_unit(float most) { return fmaxf(most, 0x1p-100f); }
 __device__ inline float scaled_grad(const GradArgs &a, int64_t j, float unit)
 {
     const int64_t t = a.targets[j];
-    const float g = a.grad_loss[j] / unit * 0x1p12f;
+    const float g = a.grad_loss[j] / unit * 0x1p15f;
     return t == a.ignore ? 0.f : t >= 0 && t < a.vocab ? g : __builtin_nanf("");
+}
+__device__ inline int lift_of(const GradArgs &a, float scaled)
+{
+    int e = 0;
+    (void)frexpf(scaled, &e);
+    return e >= kTop ? 0 : kTop - e < a.lift ? kTop - e : a.lift;
 }
 __device__ inline float wave_max(float v)
 {
@@ -456,7 +474,10 @@ __global__ __launch_bounds__(1024) void grad_kernel(TokenArgs a)
         if (g[k] != 0.f) {
             const int64_t t = a.g.targets[j + k];
             a.order[at] = j + k;
-            a.g.grad[at] = g[k];
+            const int lift = lift_of(a.g, g[k]);
+            a.g.grad[at] = ldexpf(g[k], lift);
+            if (a.g.undo)
+                a.g.undo[at] = ldexpf(1.f, -lift);
             a.live_lse[at] = a.lse[j + k];
             a.live_target[at] = t >= 0 && t < a.g.vocab ? (int)t : -1;
             ++at;
@@ -465,7 +486,7 @@ __global__ __launch_bounds__(1024) void grad_kernel(TokenArgs a)
         }
     }
     if (threadIdx.x == 0 && blockIdx.x == 0)
-        *a.g.scale = unit * 0x1p-12f;
+        *a.g.scale = unit * 0x1p-15f;
     if (threadIdx.x == 0 && blockIdx.x == gridDim.x - 1)
         *a.live = live;
 }
@@ -492,11 +513,16 @@ template <typename T> __global__ __launch_bounds__(256) void few_prepare_kernel(
     const int tokens = (int)a.g.tokens;
     const float unit = grad_unit(wave_max(x < tokens ? grad_size(a.g, x) : 0.f));
     const float g = x < tokens ? scaled_grad(a.g, x, unit) : 0.f;
+    const int lift = lift_of(a.g, g);
+    const float undo = ldexpf(1.f, -lift);
     if (blockIdx.x == 0 && y == 0) {
-        if (x < tokens)
-            a.g.grad[x] = g;
+        if (x < tokens) {
+            a.g.grad[x] = ldexpf(g, lift);
+            if (a.g.undo)
+                a.g.undo[x] = undo;
+        }
         if (x == 0)
-            *a.g.scale = unit * 0x1p-12f;
+            *a.g.scale = unit * 0x1p-15f;
     }
     const int64_t c = (int64_t)blockIdx.x * 64 + x;
     for (int k = y; k < kFew; k += 4) {
@@ -508,7 +534,7 @@ template <typename T> __global__ __launch_bounds__(256) void few_prepare_kernel(
         for (int k = y; k < 64 && blockIdx.x * 64 + k < a.cols; k += 4) {
             P *at = a.turned + ((int64_t)blockIdx.x * 64 + k) * kParts * a.rows_to + x;
             if constexpr (kParts == 1) {
-                *at = (P)tile[x][k];
+                *at = (P)(tile[x][k] * undo);
             } else {
                 bf16 t[kTerms];
                 split(tile[x][k], t);
@@ -535,11 +561,12 @@ template <typename T> __global__ __launch_bounds__(256) void few_prepare_kernel(
 // A gradient from its parts' sums: four columns a thread, Y threads a share of the
 // parts each, the shares then in order.  Where rows are tokens (grad is their
 // losses' gradients), those without a gradient are 0 whatever their sums hold: 0
-// times a row of W that is not finite is NaN.
+// times a row of W that is not finite is NaN.  undo: factors of the rows, or NULL.
 template <typename T, int Y>
 __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t pitch, int64_t part, int parts,
                                                      int64_t rows, int64_t cols, const float *scale,
-                                                     const float *grad, T *out, int64_t out_pitch)
+                                                     const float *grad, const float *undo, T *out,
+                                                     int64_t out_pitch)
 {
     constexpr int X = 256 / Y;
     __shared__ f32x4 other[Y][X];
@@ -566,7 +593,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t p
         return;
     if (grad && grad[j] == 0.f)
         s = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float f = *scale;
+    const float f = *scale * (undo ? undo[j] : 1.f);
     const float v[4] = {s[0] * f, s[1] * f, s[2] * f, s[3] * f};
     store_some(out + j * out_pitch + i, cols - i < 4 ? (int)(cols - i) : 4, v);
 }
@@ -579,8 +606,8 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *sum, int64_t p
 template <typename T, int D>
 __global__ __launch_bounds__(256) void turn_finish_kernel(const float *sum, int64_t pitch, int64_t part, int parts,
                                                           int64_t rows, int64_t cols, const int *order,
-                                                          const int *count, const float *scale, T *out,
-                                                          int64_t out_pitch)
+                                                          const int *count, const float *scale,
+                                                          const float *undo, T *out, int64_t out_pitch)
 {
     __shared__ float tile[D][65];
     const int live = *count;
@@ -608,10 +635,11 @@ __global__ __launch_bounds__(256) void turn_finish_kernel(const float *sum, int6
         const int row = row0 + 1024 / D * k;
         if (r0 + row >= rows || c >= cols)
             continue;
+        const float u = undo && r0 + row < live ? f * undo[r0 + row] : f;
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            v[e] = r0 + row < live ? tile[col + e][row] * f : 0.f;
+            v[e] = r0 + row < live ? tile[col + e][row] * u : 0.f;
         store_some(out + order[r0 + row] * out_pitch + c, cols - c < 4 ? (int)(cols - c) : 4, v);
     }
 }
@@ -710,7 +738,7 @@ constexpr int64_t kSkew = 256;
 int64_t skewed(int64_t cols) { return cols + kSkew; }
 
 struct BackwardLayout {
-    uint64_t grad, scale, order, lse, target, live, h, w, ht, p, pt, sum, w_sum, total;
+    uint64_t grad, scale, undo, order, lse, target, live, h, w, ht, p, pt, sum, w_sum, total;
     int64_t dk, piece, nk, p_pitch, sum_pitch, w_pitch;
     int split, w_split;
 };
@@ -726,6 +754,7 @@ BackwardLayout backward_layout(int32_t type, int64_t n, int64_t d, int64_t v, bo
     l.sum_pitch = pad(d, 4);
     l.grad = b.take(4ull * (uint64_t)n);
     l.scale = b.take(4);
+    l.undo = b.take(type == ROTOR_F16 ? 4ull * (uint64_t)n : 0);
     if (few_tokens(type, n, v, pack, true)) {
         l.nk = n <= 32 ? 32 : 64;
         l.piece = pad(v, kFewRows);
@@ -834,12 +863,12 @@ void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e,
 // The parts' sums joined, into a gradient.
 template <typename T>
 void finish_rows(const float *sum, int64_t pitch, int64_t part, int parts, int64_t rows, int64_t cols,
-                 const float *scale, const float *grad, T *out, int64_t out_pitch, hipStream_t s)
+                 const float *scale, const float *grad, const float *undo, T *out, int64_t out_pitch, hipStream_t s)
 {
     const int share = parts >= 8 ? 16 : 1;
     const auto finish = share > 1 ? finish_kernel<T, 16> : finish_kernel<T, 1>;
     finish<<<dim3((uint32_t)ceil_div(rows * ceil_div(cols, 4), 256 / share)), 256, 0, s>>>(
-        sum, pitch, part, parts, rows, cols, scale, grad, out, out_pitch);
+        sum, pitch, part, parts, rows, cols, scale, grad, undo, out, out_pitch);
 }
 
 // H or rows of W as a product's operand, copied into `space` if need be.
@@ -1015,7 +1044,8 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
         float *const sum = (float *)(work + l.sum);
         int *const order = (int *)(work + l.order), *const live = (int *)(work + l.live);
         const T *h = (const T *)d_h, *w = (const T *)d_w;
-        const GradArgs ga{d_grad_loss, d_targets, ignore, n_rows, n_tokens, grad, scale};
+        float *const undo = type == ROTOR_F16 ? (float *)(work + l.undo) : nullptr;
+        const GradArgs ga{d_grad_loss, d_targets, ignore, n_rows, n_tokens, undo ? 8 : 0, grad, scale, undo};
         const bool few = few_tokens(type, n_tokens, n_rows, pack, true);
         Operand<P> hb{(const P *)d_h, n_tokens, cols, h_pitch, 0};
         if (few) {
@@ -1039,6 +1069,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             t.pitch = h_pitch;
             t.order = order;
             t.live = live;
+            t.undo = undo;
             t.packed = (P *)(work + l.h);
             t.packed_pitch = parts * l.dk;
             t.packed_seg = l.dk;
@@ -1144,7 +1175,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
                     we.rows = (int)rows;
                     we.add = 0;
                     run_product<true>(ha, pb, Extent{cols, rows, n_tokens, l.w_split}, we, s);
-                    finish_rows(we.c, l.w_pitch, we.part, l.w_split, rows, cols, scale, nullptr,
+                    finish_rows(we.c, l.w_pitch, we.part, l.w_split, rows, cols, scale, nullptr, nullptr,
                                 (T *)d_dw + v0 * dw_pitch, dw_pitch, s);
                 } else {
                     OutEpilogue<T> oe;
@@ -1162,11 +1193,11 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             const int side = l.split >= 4 ? 16 : 64;
             const auto finish = side == 16 ? turn_finish_kernel<T, 16> : turn_finish_kernel<T, 64>;
             finish<<<dim3((uint32_t)ceil_div(n_tokens, 64), (uint32_t)ceil_div(cols, side)), 256, 0, s>>>(
-                sum, l.sum_pitch, cols * l.sum_pitch, l.split, n_tokens, cols, order, live, scale, (T *)d_dh,
+                sum, l.sum_pitch, cols * l.sum_pitch, l.split, n_tokens, cols, order, live, scale, undo, (T *)d_dh,
                 dh_pitch);
         } else if (d_dh) {
-            finish_rows(sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, grad, (T *)d_dh,
-                        dh_pitch, s);
+            finish_rows(sum, l.sum_pitch, n_tokens * l.sum_pitch, l.split, n_tokens, cols, scale, grad, undo,
+                        (T *)d_dh, dh_pitch, s);
         }
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;

@@ -923,3 +923,36 @@ def test_cross_entropy_through_every_product(dtype, n, rows, cols, ignored):
     h, w, t, gl = xent_case(n, rows, cols, dtype, ignored=0.0)
     t[torch.randperm(n, generator=torch.Generator().manual_seed(n))[:round(n * ignored)]] = -100
     check_xent(h, w, t, gl)
+
+
+@pytest.mark.parametrize("n,rows,cols", [(24, 60000, 64), (24, 60000, 63), (40, 60000, 64), (300, 60000, 72)])
+def test_cross_entropy_in_f16_of_tokens_with_small_gradients(n, rows, cols):
+    # Losses weighted by 1 down to 2^-22, times a loss scale: a token's row of
+    # dh is as exact relative to its own gradient, although P of 16 bits is
+    # 2^-16 of that for most rows of w.  These have a part in common, which dh
+    # loses if such terms vanish.
+    print("cross entropy f16 weights", n, rows, cols, flush=True)
+    h, w, t, _ = xent_case(n, rows, cols, "f16", ignored=0.0)
+    w = (w.double() + m.normal(torch.Generator().manual_seed(1), cols, std=0.3)).half()
+    h = (h.double() / 4).half()
+    e = (torch.arange(n) * 5) % 23
+    gl = 2.0 ** (12 - e.double()).float()
+    loss, lse = ops.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    dh, dw = ops.linear_cross_entropy_backward(h.cuda(), w.cuda(), t.cuda(), lse, gl.cuda())
+    # as in check_xent, but what P loses below the range of 16-bit floats: half
+    # a subnormal's spacing, 2^-25, where the largest gradient is scaled to 2^15
+    # and a smaller one by up to 2^8 more, to half of that at least
+    p = m.cross_entropy_grad(h, w, t, gl, -100)
+    soft = torch.softmax(h.double() @ w.double().t(), 1)
+    a = h.double().abs() @ w.double().abs().t()
+    s = (cols + 32) * m.U32 * a
+    slack = s.max(1).values + 32 * m.U32 * (1 + m.cross_entropy(h, w, t, -100)[1].abs())
+    lift = (e - 1).clamp(0, 8).double()
+    dp = gl.double().unsqueeze(1) * soft * (2 * s + 2 * slack.unsqueeze(1) + 64 * m.U32) * 1.1 + \
+        p.abs() * (m.UNIT[torch.float16] + 8 * m.U32) + (2.0 ** (12 - 40 - lift)).unsqueeze(1)
+    aw, ah = w.double().abs(), h.double().abs()
+    pa = p.abs() + dp
+    m.close(dh, p @ w.double(), dp @ aw + (rows + 64) * m.U32 * (pa @ aw), "dh")
+    # h is divided by what its gradient was multiplied by, in 16 bits
+    dah = (2.0 ** (lift - 25)).unsqueeze(1).expand_as(ah)
+    m.close(dw, p.t() @ h.double(), dp.t() @ ah + pa.t() @ dah + (n + 64) * m.U32 * (pa.t() @ ah), "dw")

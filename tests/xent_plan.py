@@ -70,6 +70,7 @@ def backward(type, n, d, v, aligned, live=None):
     live = n if live is None else live
     b.take(4 * n)
     b.take(4)
+    b.take(4 * n if type == F16 else 0)
     if few_tokens(type, n, v, pack, True):
         nk, piece = 32 if n <= 32 else 64, up(v, 64)
         b.take(2 * parts * dk * n if pack else 0)
