@@ -565,7 +565,10 @@ ROTOR_API int32_t rotor_residual_norm_backward(const rotor_norm *how, const void
  *   logit[j][v] = h[j] . w[v],  lse[j] = log sum_v exp(logit[j][v]),
  *   loss[j] = lse[j] - logit[j][targets[j]].
  * Products of 16-bit tensors are exact and summed in 32 bits; 32-bit tensors
- * are multiplied as three bf16 terms each, which keeps their 24 bits.
+ * are multiplied as three bf16 terms each, which keeps their 24 bits.  An
+ * infinity or a lowest value of w counts as in the formula, so a column of ones
+ * in h and of biases in w masks rows (32-bit gradients that are infinite may
+ * come as NaN).
  *   d_h, d_w    DEVICE [n_tokens][cols] and [n_rows][cols], of one type.
  *   d_targets   DEVICE, n_tokens int64.  A token whose target is `ignore` has
  *               loss 0 and no gradient, whatever h and w hold; any other

@@ -103,7 +103,7 @@ template <typename T> struct FewArgs {
 // reading W: backward, one token, 50000 x 2048 bf16, 40 us (205 MB, 5.1 TB/s);
 // 32 tokens 57 us, H then costs half as many loads as W.
 template <typename T, int C, int KW, bool BACK>
-__global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
+__global__ __launch_bounds__(kFewThreads, sizeof(T) == 4 ? (C == 2 ? 3 : 2) : 1) void few_kernel(FewArgs<T> a)
 {
     typedef typename ProductOf<T>::P P;
     typedef typename Mfma<P>::Frag Frag;
@@ -128,6 +128,8 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
 #pragma unroll
         for (int c = 0; c < C; ++c)
             acc[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // of terms: the sums of all products but the last
+    [[maybe_unused]] f32x4 low_acc[kParts > 1 ? R : 1][kParts > 1 ? C : 1] = {};
     for (int64_t k0 = (wave % KW) * 32 * U; k0 < a.cols; k0 += 32 * U * KW) {
         typename VecOf<T, 8>::V raw[U][R];
         Frag hb[U][C][kParts];
@@ -154,9 +156,27 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(FewArgs<T> a)
                 Frag t[kParts];
                 terms_of<T>(raw[u][r], t);
 #pragma unroll
-                for (int c = 0; c < C; ++c)
-                    acc[r][c] = multiply_terms<P, kParts>(t, hb[u][c], acc[r][c]);
+                for (int c = 0; c < C; ++c) {
+                    if constexpr (kParts > 1) {
+                        constexpr int kLast = kTermProducts - 1;
+#pragma unroll
+                        for (int s = 0; s < kLast; ++s)
+                            low_acc[r][c] = Mfma<P>::run(t[term_a(s)], hb[u][c][term_b(s)], low_acc[r][c]);
+                        acc[r][c] = Mfma<P>::run(t[term_a(kLast)], hb[u][c][term_b(kLast)], acc[r][c]);
+                    } else {
+                        acc[r][c] = Mfma<P>::run(t[0], hb[u][c][0], acc[r][c]);
+                    }
+                }
             }
+    }
+    if constexpr (kParts > 1) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[r][c][e] += finite_or_0(low_acc[r][c][e]);
     }
     if constexpr (KW > 1) {
         if (wave > 0)

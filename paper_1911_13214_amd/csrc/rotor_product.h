@@ -50,20 +50,29 @@ template <typename T> struct Operand {
 // The products of terms (a, b) whose sum is the product of two 32-bit
 // matrices: all that are not below 2^-24 of the largest, the smallest first.
 // 16-bit operands take the last one alone.
+// An infinity times the other operand's terms is right in the last product
+// alone: the others hold 0 or the other sign, and make NaN.  Where a result with
+// an infinity among its factors counts (a logit: minus infinity masks a row of
+// W), what the first five give is therefore kept only if it is finite; it is
+// below 2^-7 of the last, so it is not finite for another reason unless the last
+// is not either. (1000 x 10007 x 1024 f32, forward: 147 us so, 143 without.)
 constexpr int kTerms = 3;
 constexpr int kTermProducts = 6;
 __device__ constexpr int term_a(int s) { return 0x124 >> (2 * s) & 3; }  // 0 1 2 0 1 0
 __device__ constexpr int term_b(int s) { return 0x046 >> (2 * s) & 3; }  // 2 1 0 1 0 0
 
 // The three bf16 terms of a 32-bit value.  Infinities and NaN stay in the
-// first.
+// first; finite values above the largest bf16 do not become one.
 __device__ inline void split(float v, bf16 (&t)[kTerms])
 {
-    t[0] = (bf16)v;
-    const float r = v - (float)t[0];
-    const bool finite = fabsf((float)t[0]) <= 3.3895314e38f;
-    t[1] = finite ? (bf16)r : (bf16)0.f;
-    t[2] = finite ? (bf16)(r - (float)t[1]) : (bf16)0.f;
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr float kMost = 3.3895314e38f;  // of bf16
+    const bool finite = fabsf(v) <= 3.4028235e38f;
+    t[0] = (bf16)(finite ? __builtin_amdgcn_fmed3f(v, -kMost, kMost) : v);
+    const float r = finite ? v - (float)t[0] : 0.f;
+    t[1] = (bf16)r;
+    t[2] = (bf16)(r - (float)t[1]);
+#endif
 }
 
 // Element type of the products of a call: bf16 terms for 32-bit tensors.
@@ -343,7 +352,8 @@ template <int WAIT> __device__ inline void phase_barrier()
 // buffers of 32 with counted waits 1066, 1183, 1247; two groups half a phase
 // apart (this one) 1101, 1267, 1372, and 1398, 1480, 1514 without the stores.
 // The library's product of 8192^3 reaches 1297 here, of 16384^3 1559.
-template <typename T, typename S, bool KB, typename E>
+// TERMS: of 32-bit operands, whose results may have infinite factors.
+template <typename T, typename S, bool KB, bool TERMS, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Operand<T> b, ProductArgs p, E epilogue)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -383,7 +393,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
     auto load = [&](char *lds, bool live) {
         la.load(a, lds, term_a(s) * a.seg, at, live);
         lb.load(b, lds + kB, term_b(s) * b.seg, at, live);
-        if (++at == per) {
+        if ((!TERMS || live) && ++at == per) {
             at = 0;
             ++s;
         }
@@ -412,6 +422,21 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
             for (int jj = 0; jj < S::NJ; ++jj)
                 res.acc[ii][jj] = Mfma<T>::run(fa[ii], fb[jj], res.acc[ii][jj]);
         __builtin_amdgcn_s_setprio(0);
+    };
+
+    // Where TERMS, the steps are those of all six products, in one part.  The
+    // last product starts at an even step: after an odd number of them comes
+    // one of zeros.
+    const int low = (kTermProducts - 1) * per, dead = TERMS && low % 2 ? low : -1, last = low + low % 2;
+    const int end = TERMS ? t1 + low % 2 : t1;
+    auto drop_infinite = [&]() {
+#pragma unroll
+        for (int ii = 0; ii < S::NI; ++ii)
+#pragma unroll
+            for (int jj = 0; jj < S::NJ; ++jj)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    res.acc[ii][jj][e] = finite_or_0(res.acc[ii][jj][e]);
     };
 
     // A workgroup takes every gridDim.x-th tile; the next one's first step is
@@ -452,10 +477,12 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
             phase_barrier<kWaitAll>();
             if (late)
                 phase_barrier<kWaitNone>();
-            for (int t = t0; t < t1; t += 2) {
-                phase(even, 0, odd, t + 1 < t1);
+            for (int t = t0; t < end; t += 2) {
+                if (TERMS && t == last)
+                    drop_infinite();
+                phase(even, 0, odd, t + 1 < end && t + 1 != dead);
                 phase(even, 1, nullptr, false);
-                phase(odd, 0, even, t + 2 < t1);
+                phase(odd, 0, even, t + 2 < end);
                 phase(odd, 1, nullptr, false);
             }
             if (!late)
@@ -470,14 +497,21 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Operand<T> a, Oper
                 }
             };
             __syncthreads();
-            for (int t = t0; t < t1; t += 2) {
-                load(odd, t + 1 < t1);
-                step(even);
-                __syncthreads();
-                if (t + 2 < t1)
-                    load(even, true);
-                step(odd);
-                __syncthreads();
+            // (two loops: inside of one, dropping costs 5 of 57 us in 300 x
+            // 8000 x 512 f32; of the large tiles it is the other way round)
+            for (int from = t0, to = TERMS ? last : end;; from = to, to = end) {
+                for (int t = from; t < to; t += 2) {
+                    load(odd, t + 1 < end && t + 1 != dead);
+                    step(even);
+                    __syncthreads();
+                    if (t + 2 < end)
+                        load(even, true);
+                    step(odd);
+                    __syncthreads();
+                }
+                if (!TERMS || to == end)
+                    break;
+                drop_infinite();
             }
         }
         res.tile_i = ti;

@@ -823,7 +823,7 @@ struct Extent {
     int split;
 };
 
-template <typename P, typename S, bool KB, typename E>
+template <typename P, typename S, bool KB, bool TERMS, typename E>
 void run_tiles(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, hipStream_t s)
 {
     ProductArgs p;
@@ -835,7 +835,7 @@ void run_tiles(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, h
     p.split_steps = (int)ceil_div(p.steps, x.split);
     // as many workgroups as the 256 CUs hold at once (by their LDS)
     const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j, most = 256 * ((160 << 10) / (2 * S::kBytes)) / x.split;
-    product_kernel<P, S, KB, E>
+    product_kernel<P, S, KB, TERMS, E>
         <<<dim3((uint32_t)(tiles < most || most < 8 ? tiles : most / 8 * 8), (uint32_t)x.split), S::kThreads, 0, s>>>(
             a, b, p, e);
 }
@@ -851,13 +851,13 @@ bool large_tiles(int64_t a, int64_t b, int split)
     return tiles(a, b, 256) * split >= 128 && a > 128 && b > 128;
 }
 
-template <bool KB, typename P, typename E>
+template <bool KB, bool TERMS = false, typename P, typename E>
 void run_product(const Operand<P> &a, const Operand<P> &b, const Extent &x, E e, hipStream_t s)
 {
     if (large_tiles(x.ni, x.nj, x.split))
-        run_tiles<P, Large, KB, E>(a, b, x, e, s);
+        run_tiles<P, Large, KB, TERMS, E>(a, b, x, e, s);
     else
-        run_tiles<P, Small, KB, E>(a, b, x, e, s);
+        run_tiles<P, Small, KB, TERMS, E>(a, b, x, e, s);
 }
 
 // The parts' sums joined, into a gradient.
@@ -994,7 +994,7 @@ int32_t rotor_xent(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
             ep.vocab = (int)rows;
             ep.tokens = (int)n_tokens;
             ep.v0 = v0;
-            run_product<false>(a, b, Extent{rows, n_tokens, cols, 1}, ep, s);
+            run_product<false, (ProductOf<T>::kParts > 1)>(a, b, Extent{rows, n_tokens, cols, 1}, ep, s);
             tiles_done += ceil_div(rows, large_tiles(rows, n_tokens, 1) ? 256 : 128);
         }
         run_loss(part, tiles_done, target, d_targets, ignore, n_rows, n_tokens, d_loss, d_lse, s);
@@ -1148,7 +1148,7 @@ int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t cols, int64_
             ep.targets = (const int *)(work + l.target);
             ep.v0 = (int)v0;
             ep.rows = (int)rows;
-            run_product<false>(wa, hb, Extent{rows, n_tokens, cols, 1}, ep, s);
+            run_product<false, (parts > 1)>(wa, hb, Extent{rows, n_tokens, cols, 1}, ep, s);
             const Operand<P> pb{(const P *)(work + l.p), n_tokens, pad(rows, 8), parts * l.p_pitch,
                                 parts > 1 ? l.p_pitch : 0};
             if (d_dh) {

@@ -956,3 +956,56 @@ def test_cross_entropy_in_f16_of_tokens_with_small_gradients(n, rows, cols):
     # h is divided by what its gradient was multiplied by, in 16 bits
     dah = (2.0 ** (lift - 25)).unsqueeze(1).expand_as(ah)
     m.close(dw, p.t() @ h.double(), dp.t() @ ah + pa.t() @ dah + (n + 64) * m.U32 * (pa.t() @ ah), "dw")
+
+
+def xent_bounds(h, w, t, gl):
+    """Reference values and bounds of loss, lse, dh and dw, as in check_xent."""
+    ref_loss, ref_lse = m.cross_entropy(h, w, t, -100)
+    n, cols, rows = *h.shape, w.shape[0]
+    a = h.double().abs() @ w.double().abs().t()
+    three = 2.0 ** -22 if h.dtype == torch.float32 else 0.0
+    s = ((cols + 32) * m.U32 + three) * a
+    top = s.max(1).values
+    slack = top + 32 * m.U32 * (1 + ref_lse.abs())
+    p = m.cross_entropy_grad(h, w, t, gl, -100)
+    some = (t != -100).double().unsqueeze(1)
+    size = gl.double().abs().unsqueeze(1) * some
+    unit = 2.0 ** -23 if h.dtype == torch.float32 else m.UNIT[h.dtype]
+    soft = torch.softmax(h.double() @ w.double().t(), 1)
+    dp = size * soft * (2 * s + 2 * slack.unsqueeze(1) + 64 * m.U32) * 1.1 + p.abs() * (unit + 8 * m.U32)
+    if h.dtype == torch.float16:
+        dp = dp + size.max() * 2.0 ** -36 * some
+    pa, aw, ah = p.abs() + dp, w.double().abs(), h.double().abs()
+    return (ref_loss, slack + top + 4 * m.U32 * a.max(1).values), (ref_lse, slack), \
+        (p @ w.double(), dp @ aw + ((rows + 64) * m.U32 + three) * (pa @ aw)), \
+        (p.t() @ h.double(), dp.t() @ ah + ((n + 64) * m.U32 + three) * (pa.t() @ ah))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,cols", [(3, 400, 64), (20, 400, 63), (64, 400, 72), (150, 700, 72), (150, 700, 71),
+                                         (1100, 9000, 136)])
+@pytest.mark.parametrize("mask", ["inf", "lowest"])
+def test_cross_entropy_of_rows_masked_by_a_bias(dtype, n, rows, cols, mask):
+    # a column of ones in h, a bias in w: rows whose bias is minus infinity, or
+    # the type's lowest value, are not there
+    print("cross entropy masked rows", dtype, n, rows, cols, mask, flush=True)
+    h, w, t, gl = xent_case(n, rows, cols, dtype, ignored=0.2)
+    h[:, -1] = 1.0
+    keep = torch.ones(rows, dtype=torch.bool)
+    keep[torch.randperm(rows, generator=torch.Generator().manual_seed(3))[:rows // 3]] = False
+    keep[0], keep[rows - 1] = True, False
+    place = torch.cumsum(keep, 0) - 1
+    t = torch.where((t != -100) & ~keep[t.clamp(min=0)], 0, t)
+    masked = w.clone()
+    masked[~keep, -1] = -float("inf") if mask == "inf" else torch.finfo(w.dtype).min
+    loss, lse = ops.linear_cross_entropy(h.cuda(), masked.cuda(), t.cuda())
+    dh, dw = ops.linear_cross_entropy_backward(h.cuda(), masked.cuda(), t.cuda(), lse, gl.cuda())
+    want = xent_bounds(h, w[keep], torch.where(t == -100, t, place[t.clamp(min=0)]), gl)
+    # the column of the bias is 0 times infinity in dh
+    got = (loss, lse, dh[:, :-1], dw[keep.cuda()])
+    for what, out, (ref, slack) in zip(("loss", "lse", "dh", "dw"), got, want):
+        ref, slack = (ref[:, :-1], slack[:, :-1]) if what == "dh" else (ref, slack)
+        m.close(out, ref, slack, what)
+    assert not dw[~keep.cuda()].any()
+    if mask == "lowest":
+        m.close(dh[:, -1:], want[2][0][:, -1:], want[2][1][:, -1:], "dh of the bias")
