@@ -546,7 +546,10 @@ typedef struct {
  *   d_dy     DEVICE or NULL (0);  d_dh  DEVICE; NULL if and only if pre is
  *            ROTOR_NORM_NONE (then d_dy is required).
  *   d_y, d_z, d_stats  what rotor_residual_norm wrote and read (d_y is not
- *            used, and may be NULL, without pre; d_z NULL as there).
+ *            used, and may be NULL, without pre; d_z NULL as there).  The normed
+ *            row of pre comes from y as it was rounded: in 16 bits that adds its
+ *            rounding to the gradient of pre_weight, which is then about 1.4
+ *            times as far off as by its own rounding alone.
  *   d_dx     DEVICE, written;  d_dz  DEVICE, written; NULL if d_z is.
  *   grads    HOST, the parameters' gradients.
  *   d_work   DEVICE scratch of rotor_residual_norm_workspace_bytes, 16-byte
@@ -589,11 +592,15 @@ ROTOR_API int32_t rotor_residual_norm_backward(const rotor_norm *how, const void
 #define ROTOR_XENT_MAX_ROWS (1 << 26)
 
 /* Device workspace of rotor_xent (backward 0) or rotor_xent_backward (1).
- * Forward: 8 bytes per token and 128 rows of w.  Backward: at most 128 MiB
+ * Forward: 8 bytes per token and 128 rows of w (16 for up to 64 tokens).
+ * Backward: at most 128 MiB
  * for a piece of the probabilities (256 rows of w at least; up to 64 tokens:
- * 256 MiB), two copies of h, 32-bit sums for dh, and for dw where that has few
- * tiles (64 MiB at most).  Where operands are copied, at most 128 MiB for a
- * piece of w as well.  Host only. */
+ * 256 MiB), two copies of h, 512 bytes per token and per column between the
+ * rows of these, 32-bit sums for dh and, where dh or dw have few tiles, 64 MiB
+ * for the parts' sums of each.  32-bit tensors: three times those 512 bytes, and
+ * three halves of h for each copy.  Where operands are copied, in either
+ * direction, at most 128 MiB for a piece of w (256 rows at least) and, forward,
+ * one copy of h.  Rows are padded to 64 columns.  Host only. */
 ROTOR_API int32_t rotor_xent_workspace_bytes(int32_t type, int64_t n_tokens, int64_t cols, int64_t n_rows,
                                              int32_t aligned, int32_t backward, uint64_t *bytes);
 

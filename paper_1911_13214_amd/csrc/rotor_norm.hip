@@ -374,9 +374,13 @@ __global__ __launch_bounds__(Team<TH>::kBlock) void back_kernel(const T *dy, con
 }
 
 // The gradients of wide rows, a workgroup a row.  With the sums over rows
-// beside them in one launch, registers spilled: 8192 x 5120 bf16 450 us, 3000 x
-// 12288 2243 us; the two launches 177 and 172 us (ten tensors moved instead of
-// six, 4.3 to 4.7 TB/s).
+// beside them in one launch of 512 to 1024 threads with 16 elements each,
+// registers spilled: 8192 x 5120 bf16 450 us, 3000 x 12288 2243 us; the two
+// launches 183 and 172 us (ten tensors moved instead of six, 4.3 to 4.7 TB/s).
+// In one launch with 8 elements a thread (the same two of bf16, then f32, in one
+// launch and in two): 8192 x 5120 147 and 183, 585 and 327 us; 4096 x 6144 88 and
+// 104, 415 and 203; 4096 x 8192, where every shape spills most, 369 and 138, 1011
+// and 263.
 template <typename T, int TH, int V, int N>
 __global__ __launch_bounds__(TH) void wide_row_kernel(const T *dy, const T *dh, const T *y, const T *z, T *dx, T *dz,
                                                       BackArgs a)

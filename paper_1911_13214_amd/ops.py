@@ -280,8 +280,9 @@ def residual_norm(x, z=None, *, post="none", post_weight=None, post_bias=None, g
     ``post``, ``pre``: "none", "rms" or "layer", each with an optional weight
     and bias [cols]; ``gate``: [cols], or [..., cols] of n rows where n divides
     the rows of x (one row of gates for each run of rows / n adjacent rows);
-    ``z`` None: no block, y = residual_scale * x.  ``stats``: keep what the
-    backward needs (16 bytes a row), or None is returned."""
+    ``z`` None: no block, y = residual_scale * x (``x`` itself if that is 1).
+    ``stats``: keep what the backward needs (16 bytes a row), or None is
+    returned."""
     if stream is not None:
         return _on(stream, residual_norm, x, z, post=post, post_weight=post_weight, post_bias=post_bias, gate=gate,
                    residual_scale=residual_scale, pre=pre, pre_weight=pre_weight, pre_bias=pre_bias, eps=eps,

@@ -250,3 +250,24 @@ def test_checked_cross_entropies_reach_every_product():
             for what in ("stats", "prob", "dh", "dw"):
                 assert {(type, what, "even"), (type, what, "odd")} <= seen, (name, what)
     assert {(1, "dw", "several"), (2, "dw", "several")} <= seen
+
+
+def test_cross_entropy_workspace_is_within_the_documented_sum():
+    need = ctypes.c_uint64()
+    mib = 1 << 20
+    sizes = [1, 17, 64, 65, 300, 2100, 8192, 65536, 262144, 1 << 20], [1, 63, 300, 1031, 4096, 65536], \
+        [1, 300, 24700, 128000, 1 << 22]
+    for type, n, d, v, aligned in itertools.product(range(3), *sizes, (0, 1)):
+        pack = type == 0 or not aligned
+        parts, dk = 3 if type == 0 else 1, -(-d // 64) * 64
+        copy_h = 2 * parts * n * dk
+        copy_w = max(128 * mib, 256 * 2 * parts * dk) if pack else 0
+        small = 64 * (n + 256)  # per-token figures, each array's rounding to 256 bytes
+        assert rotor.lib().rotor_xent_workspace_bytes(type, n, d, v, aligned, 0, ctypes.byref(need)) == 0
+        rows = 16 if n <= 64 else 128  # few tokens' waves take as few as 16 rows
+        assert need.value <= 8 * n * -(-v // rows) + small + (copy_h + copy_w if pack else 0), (type, n, d, v, aligned)
+        assert rotor.lib().rotor_xent_workspace_bytes(type, n, d, v, aligned, 1, ctypes.byref(need)) == 0
+        p = 256 * mib if n <= 64 else max(128 * mib, 256 * 2 * parts * n)
+        skew = 512 * parts * (n + d) + 2 * parts * 64 * (n + d)
+        assert need.value <= p + 2 * copy_h + skew + 4 * n * (d + 4) + 2 * 64 * mib + copy_w + small, \
+            (type, n, d, v, aligned, need.value)
