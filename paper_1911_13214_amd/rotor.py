@@ -340,18 +340,23 @@ def alloc_workspace(n_chains: int, L: int, M: int, device="cuda"):
 
 def solve(params: np.ndarray, M: int, device="cuda", stream=None, schedule: str = "auto"):
     """Upload, allocate and fill.  Returns (d_params, cost, dec) device
-    tensors; the fill is enqueued on ``stream`` (the workspace is released to
-    torch's caching allocator on that stream)."""
+    tensors; the fill is enqueued on ``stream``, where all of it is allocated
+    (the workspace is released to torch's caching allocator there; what is
+    returned may be freed where the caller works as well)."""
+    import torch
     p = np.asarray(params)
     if p.ndim == 2:
         p = p[None]
     n_chains, _, L = p.shape
-    d_params = upload_params(p, M, device)
-    cost, dec = alloc_tables(n_chains, L, M, device)
-    work = alloc_workspace(n_chains, L, M, device)
-    rotor_solve_schedule(d_params, n_chains, L, M, cost, dec, work, schedule, stream)
+    here = torch.cuda.current_stream(stream.device) if stream is not None else None
+    with torch.cuda.stream(stream):
+        d_params = upload_params(p, M, device)
+        cost, dec = alloc_tables(n_chains, L, M, device)
+        work = alloc_workspace(n_chains, L, M, device)
+        rotor_solve_schedule(d_params, n_chains, L, M, cost, dec, work, schedule, stream)
     if stream is not None:
-        work.record_stream(stream)
+        for t in (d_params, cost, dec):
+            t.record_stream(here)
     return d_params, cost, dec
 
 
@@ -360,13 +365,14 @@ def reconstruct(d_params, n_chains: int, L: int, M: int, d_dec, chain: int, budg
     None where no sequence fits.  Synchronises the stream."""
     import torch
     device = d_dec.device
-    budgets = torch.as_tensor(np.asarray(budgets, dtype=np.int64), device=device)
-    n = budgets.numel()
-    cap = L * (L + 1) // 2 + L
-    ops = torch.empty((n, cap, 2), dtype=torch.int32, device=device)
-    count = torch.empty(n, dtype=torch.int64, device=device)
-    status = torch.empty(n, dtype=torch.int32, device=device)
-    rotor_reconstruct(d_params, n_chains, L, M, d_dec, chain, budgets, cap, ops, count, status, stream)
+    with torch.cuda.stream(stream):
+        budgets = torch.as_tensor(np.asarray(budgets, dtype=np.int64), device=device)
+        n = budgets.numel()
+        cap = L * (L + 1) // 2 + L
+        ops = torch.empty((n, cap, 2), dtype=torch.int32, device=device)
+        count = torch.empty(n, dtype=torch.int64, device=device)
+        status = torch.empty(n, dtype=torch.int32, device=device)
+        rotor_reconstruct(d_params, n_chains, L, M, d_dec, chain, budgets, cap, ops, count, status, stream)
     if stream is None:
         torch.cuda.current_stream().synchronize()
     else:

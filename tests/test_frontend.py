@@ -186,3 +186,48 @@ def test_kernel_code_digest_ignores_comments_only(tmp_path):
     assert bench.kernel_code_digest(str(src)) == d0
     src.write_text("int f(int a) { return a + 2; }\n")
     assert bench.kernel_code_digest(str(src)) != d0
+
+
+def test_solve_and_reconstruct_allocate_on_the_stream_they_are_given(monkeypatch):
+    # tables, workspace and sequences are written there: blocks of another
+    # stream's pool may still be in use.  Kernels and streams are replaced.
+    import contextlib
+
+    import torch
+
+    now, seen, recorded = ["current"], [], []
+
+    class Stream:
+        device = torch.device("cpu")
+        cuda_stream = 7
+
+        def synchronize(self):
+            pass
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, now[0] = now[0], now[0] if stream is None else stream
+        yield
+        now[0] = before
+
+    def watch(f):
+        def alloc(*args, **kw):
+            seen.append(now[0])
+            return f(*args, **kw)
+        return alloc
+
+    given = Stream()
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[0])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: recorded.append(stream))
+    for name in ("alloc_tables", "alloc_workspace", "upload_params"):
+        monkeypatch.setattr(rotor, name, watch(getattr(rotor, name)))
+    monkeypatch.setattr(rotor, "rotor_solve_schedule", lambda *args: None)
+    monkeypatch.setattr(rotor, "rotor_reconstruct", lambda *args: [args[k].zero_() for k in (9, 10)])
+    params = chaingen.homogeneous_chain(6)
+    d_params, cost, dec = rotor.solve(params, 40, device="cpu", stream=given)
+    assert len(seen) == 3 and all(s is given for s in seen) and recorded.count("current") == 3
+    monkeypatch.setattr(torch, "empty", watch(torch.empty))
+    seen.clear()
+    assert rotor.reconstruct(d_params, 1, 6, 40, dec, 0, np.array([10, 20]), stream=given) == [[], []]
+    assert len(seen) == 3 and all(s is given for s in seen)
