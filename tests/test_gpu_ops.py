@@ -1009,3 +1009,50 @@ def test_cross_entropy_of_rows_masked_by_a_bias(dtype, n, rows, cols, mask):
     assert not dw[~keep.cuda()].any()
     if mask == "lowest":
         m.close(dh[:, -1:], want[2][0][:, -1:], want[2][1][:, -1:], "dh of the bias")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_operators_in_a_captured_graph(dtype):
+    # replays on new inputs, with eager calls and synchronizations between
+    # them, give what eager calls give, bit for bit
+    print("graph", dtype, flush=True)
+    g = torch.Generator().manual_seed(77)
+    t = m.DTYPES[dtype]
+    x, z, dy, dh = (m.normal(g, 300, 96, dtype=t).cuda() for _ in range(4))
+    w, gate = m.normal(g, 700, 96, dtype=t, std=0.1).cuda(), m.normal(g, 3, 96, dtype=t).cuda()
+    tokens = torch.randint(0, 700, (300,), generator=g).cuda()
+    many = torch.randint(0, 700, (40000,), generator=g).cuda()
+    rows = m.normal(g, 40000, 9, dtype=t).cuda()
+    few = x[:7].clone()
+    gl = torch.ones(300, device="cuda")
+
+    def step():
+        how = dict(post="rms", gate=gate, pre="layer", pre_weight=w[0].contiguous())
+        y, h, st = ops.residual_norm(x, z, **how)
+        out = [y, h, *ops.residual_norm_backward(dy, dh, y, z, st, **how).values()]
+        out += [ops.embedding(tokens, w, 2.0), ops.embedding_backward(tokens, dy, 700),
+                ops.embedding_backward(many, rows, 700)]
+        for a, n in ((h, 300), (few, 7)):
+            loss, lse = ops.linear_cross_entropy(a, w, tokens[:n])
+            out += [loss, *ops.linear_cross_entropy_backward(a, w, tokens[:n], lse, gl[:n])]
+        return out
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        for a in (x, z, dy, dh, w, few, rows):
+            a.copy_(m.normal(g, *a.shape, dtype=t, std=0.3 + k))
+        for a in (tokens, many):
+            a.copy_(torch.randint(0, 700, a.shape, generator=g))
+        tokens[k::5] = -100 if k % 2 else 3
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) for a, b in zip(out, want)), k
