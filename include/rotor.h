@@ -626,6 +626,140 @@ ROTOR_API int32_t rotor_xent_backward(int32_t type, int64_t n_tokens, int64_t co
                                       int64_t dh_pitch, void *d_dw, int64_t dw_pitch, int32_t aligned, void *d_work,
                                       uint64_t work_bytes, void *stream);
 
+/* ---- operators that mix the tokens of a chain ------------------------------
+ *
+ * Heads.  A tensor [batch][tokens][heads][width] with any strides, in elements
+ * (of dimensions of one element they do not matter); the columns of a head are
+ * adjacent. */
+typedef struct {
+    void *p;
+    int64_t batch, token, head;
+} rotor_heads;
+
+/* Norms of the query and key heads and their rotation by position, in one
+ * pass.  For a head's row u of a token at position p, n its normed row (as in
+ * rotor_norm), x = n * weight:
+ *   (x_a, x_b) -> (x_a cos t - x_b sin t, x_b cos t + x_a sin t),  t = p f_i
+ * for the pairs i = 0 .. rotary / 2 - 1 of the first `rotary` columns: a = i,
+ * b = i + rotary / 2, or, interleaved, a = 2 i, b = 2 i + 1.  The other columns
+ * stay as they are.  Angles are held as 64-bit fractions of a turn, whatever the
+ * position: within 2^-32 of a turn up to position 2^24. */
+typedef struct {
+    int32_t type, norm, interleaved;
+    int32_t position_bytes;            /* 4 or 8 */
+    int64_t batch, tokens;
+    int64_t heads, kv_heads;           /* of q and of k; kv_heads 0: there is no k */
+    int64_t width, rotary;             /* both even, 2 <= width <= ROTOR_ROTATE_MAX_WIDTH, 0 <= rotary <= width */
+    double eps;                        /* >= 0 */
+    const double *frequencies;         /* HOST, rotary / 2 finite numbers: f_i, radians a position */
+    const void *positions;             /* DEVICE, signed integers; NULL: 0 .. tokens - 1 */
+    int64_t position_batch;            /* elements from one sequence's positions to the next's; 0: shared */
+    const void *q_weight, *k_weight;   /* DEVICE [width] or NULL (1); NULL without a norm */
+} rotor_head_rotation;
+#define ROTOR_ROTATE_MAX_WIDTH 256
+
+/* q and k normed and rotated.  An output may be its input (with the same
+ * strides).  Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_head_norm_rotate(const rotor_head_rotation *how, const rotor_heads *q, const rotor_heads *k,
+                                         const rotor_heads *q_out, const rotor_heads *k_out, void *stream);
+
+/* Device workspace of rotor_head_norm_rotate_backward: partial sums of the
+ * weights' gradients.  Host only.  Returns ROTOR_OK or ROTOR_EINVAL. */
+ROTOR_API int32_t rotor_head_norm_rotate_workspace_bytes(const rotor_head_rotation *how, uint64_t *bytes);
+
+/* Gradients of q and k (those that the forward took, not its results) from
+ * those of its results, and of the weights (d_dq_weight, d_dk_weight: [width],
+ * of the call's type; NULL: not wanted).  dq may be dq_out, dk dk_out (with the
+ * same strides).  Sums over tokens and heads are taken in an order that depends
+ * on the sizes alone.
+ *   d_work  DEVICE scratch of rotor_head_norm_rotate_workspace_bytes, 16-byte
+ *           aligned.
+ * Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_head_norm_rotate_backward(const rotor_head_rotation *how, const rotor_heads *dq_out,
+                                                  const rotor_heads *dk_out, const rotor_heads *q,
+                                                  const rotor_heads *k, const rotor_heads *dq, const rotor_heads *dk,
+                                                  void *d_dq_weight, void *d_dk_weight, void *d_work,
+                                                  uint64_t work_bytes, void *stream);
+
+/* Causal attention under a window with first keys that stay visible.  Query row
+ * i of sequence b stands at position p_i = positions[b] + i and sees key j if
+ *   0 <= j <= p_i < lengths[b]  and  (p_i - j < window or j < sinks);
+ * out_i = sum over those of softmax(scale q_i . k_j) v_j.  A row that sees
+ * nothing (a place of padding) has out 0 and lse -inf, and no gradient; what q,
+ * k, v or the gradient of out hold in such places is never used: it may be
+ * infinite or NaN, and so may a key or value that a row does not see.
+ * `heads / kv_heads` adjacent query heads share a key head.
+ * 16-bit probabilities and gradients of scores are rounded once before they are
+ * multiplied (the latter, in float16, after scaling by a power of two for each
+ * row, or for 32 adjacent rows); scores, sums and statistics are 32 bits wide.
+ * Heads start 16-byte aligned (pointers and strides); width is a multiple of 8,
+ * at most ROTOR_ATTENTION_MAX_WIDTH.
+ * keys < 2^30, heads <= 2^15, tokens * heads / kv_heads <= 65535 * 128 (and, for
+ * the gradients, keys), batch * kv_heads <= 2^20; 66 rows of keys, and 66 tokens
+ * and the heads of a group of queries in the gradients, must lie within 2^31
+ * bytes. */
+typedef struct {
+    int32_t type;
+    int32_t position_bytes, length_bytes; /* 4 or 8 */
+    int32_t reserved;                     /* 0 */
+    int64_t batch, tokens, keys;
+    int64_t heads, kv_heads, width;
+    int64_t window;                       /* keys that a row sees with its own; 0: all up to it */
+    int64_t sinks;
+    double scale;                         /* > 0 */
+    const void *positions;                /* DEVICE [batch], signed; NULL: keys - tokens */
+    const void *lengths;                  /* DEVICE [batch], signed; NULL: keys */
+} rotor_attention;
+#define ROTOR_ATTENTION_MAX_WIDTH 128
+
+/* Device workspace of rotor_window_attention (step 0) and
+ * rotor_window_attention_step (1): where few rows meet many keys, the sums of
+ * each part of the keys, 4 bytes a column and 8 a row.  Host only. */
+ROTOR_API int32_t rotor_window_attention_workspace_bytes(const rotor_attention *how, int32_t step, uint64_t *bytes);
+
+/*   q, out  [batch][tokens][heads][width];  k, v  [batch][keys][kv_heads][width]
+ *   d_lse   DEVICE, written: [batch][tokens][heads] floats, log of the sum of
+ *           exp(scale q_i . k_j); NULL: not kept (no backward follows).
+ *   d_work  DEVICE scratch, 16-byte aligned (NULL if none is needed).
+ * Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_window_attention(const rotor_attention *how, const rotor_heads *q, const rotor_heads *k,
+                                         const rotor_heads *v, const rotor_heads *out, float *d_lse, void *d_work,
+                                         uint64_t work_bytes, void *stream);
+
+/* Device workspace of rotor_window_attention_backward: 12 bytes a query row
+ * and, where keys are few or some are seen by all rows, 32-bit sums of their
+ * gradients for each part of the rows.  Host only. */
+ROTOR_API int32_t rotor_window_attention_backward_workspace_bytes(const rotor_attention *how, uint64_t *bytes);
+
+/* Gradients of q, k and v from that of out (dout); out and d_lse are what
+ * rotor_window_attention wrote.  dq, dk, dv: written whole (0 where nothing
+ * reaches).  Every sum is taken in an order that depends on the sizes,
+ * positions and lengths alone.
+ * Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_window_attention_backward(const rotor_attention *how, const rotor_heads *dout,
+                                                  const rotor_heads *q, const rotor_heads *k, const rotor_heads *v,
+                                                  const rotor_heads *out, const float *d_lse, const rotor_heads *dq,
+                                                  const rotor_heads *dk, const rotor_heads *dv, void *d_work,
+                                                  uint64_t work_bytes, void *stream);
+
+/* One token of each sequence against a cache: its key and value (k, v:
+ * [batch][kv_heads][width], strides batch and head) are written into the
+ * caches [batch][keys][kv_heads][width] at the token's position, and its query
+ * attends to what it sees there.  how->tokens is 1, positions[b] the token's
+ * position, lengths NULL.
+ *   ring  0: position j lies in slot j.
+ *         1: in slot j below sinks, in slot sinks + (j - sinks) % (keys - sinks)
+ *         from there on, so that a bounded cache serves any length; window >= 1
+ *         and sinks + window <= keys are required, positions are below 2^30.
+ * A negative position is a place without a token: nothing is written to the
+ * caches, out is 0.  A position past the cache (or 2^30): out is NaN, nothing is
+ * written to the caches.  Slots that the token does not see are not used.
+ * Returns ROTOR_OK, ROTOR_EINVAL or ROTOR_EDEVICE. */
+ROTOR_API int32_t rotor_window_attention_step(const rotor_attention *how, const rotor_heads *q, const rotor_heads *k,
+                                              const rotor_heads *v, const rotor_heads *k_cache,
+                                              const rotor_heads *v_cache, int32_t ring, const rotor_heads *out,
+                                              void *d_work, uint64_t work_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

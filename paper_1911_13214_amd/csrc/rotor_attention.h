@@ -1,0 +1,487 @@
+// Attention of a chain's tokens: what its kernels share.
+//
+// Row i of a sequence's queries stands at position p_i = offset + i and sees
+// the keys j with 0 <= j <= p_i < length and (p_i - j < window or j < sinks):
+//   s_ij = scale q_i k_j,  P_ij = exp(s_ij - lse_i),  o_i = sum P_ij v_j
+//   delta_i = do_i o_i,  dS_ij = P_ij (do_i v_j - delta_i)
+//   dv_j = sum P_ij do_i,  dk_j = scale sum dS_ij q_i,  dq_i = scale sum dS_ij k_j
+//
+// The query heads of one key head are rows of one problem: row r is head
+// r % group of token r / group, so that a tile of keys serves them all and
+// their gradients' sums are one sum.
+//
+// Products are 32 x 32 tiles of the matrix units.  A result's columns are a
+// wave's lanes and its rows their registers, so that the probabilities of a
+// tile, rows the summed index, are the next product's operand as they are:
+// scores are computed transposed forward (keys x rows, then o^T = v^T P^T) and
+// straight for the keys' gradients (rows x keys, then dv^T = do^T P).
+#pragma once
+
+#include "rotor_ops.h"
+
+namespace rotor {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4, kThreads = kWaves * 64;
+constexpr int kTileRows = kWaves * 32;  // rows of a workgroup, 32 a wave
+constexpr int kTileKeys = 64;           // keys in LDS at a time
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr float kInf = __builtin_huge_valf();
+
+// A strided tensor of heads: element (batch, token, head, column).
+struct Heads {
+    char *p;
+    int64_t batch, token, head;  // bytes
+};
+
+struct Attention {
+    Heads q, k, v, out;
+    Heads dout, dq, dk, dv;  // backward
+    Heads k_new, v_new;      // a single token's, into the caches k and v
+    float *lse;              // [batch][tokens][heads]
+    const void *positions, *lengths;
+    int position_bytes, length_bytes;
+    int batch, kv, group, tokens, keys, width;
+    int rows;            // tokens * group
+    int window, sinks;   // window at most kFar
+    float scale, c;      // c = scale log2(e)
+    uint32_t magic;      // ceil(2^32 / group)
+    int parts;           // of the keys (forward) or of the rows (gradients of keys)
+    int ring;            // slots past the first ones, 0: the cache is linear
+    // workspace
+    float *part_out;     // [part][batch * kv][rows][width]
+    float2 *part_soft;   // [part][batch * kv][rows]: maximum (in powers of two) and sum
+    float *row_lse, *row_delta;  // [batch * kv][row_pitch]: lse log2(e) (+inf: sees nothing), delta
+    int *row_at;         // [batch * kv][row_pitch]: position, -1: sees nothing
+    int *row_exp;        // [batch * kv][row_pitch / 32]: exponent of the largest |do|
+    int row_pitch;
+    int tiles, sink_tiles, sink_parts;  // of 128 keys (gradients of keys)
+    float *part_dk, *part_dv;           // [item][batch * kv][128][width]
+};
+
+constexpr int kFar = 1 << 30;
+
+// 16 bytes of a row, as operands of a 32 x 32 tile: lane l holds row l % 32 and
+// of every 32 bytes of the summed index the half l / 32.
+template <typename T> struct Frag;
+template <> struct Frag<bf16> {
+    typedef bf16 F __attribute__((ext_vector_type(8)));
+    static constexpr int N = 8;
+    static __device__ f32x16 mma(F a, F b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Frag<f16> {
+    typedef f16 F __attribute__((ext_vector_type(8)));
+    static constexpr int N = 8;
+    static __device__ f32x16 mma(F a, F b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Frag<float> {
+    typedef float F __attribute__((ext_vector_type(4)));
+    static constexpr int N = 4;
+    static __device__ f32x16 mma(F a, F b, f32x16 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// Row of a result's register e for a lane of half h.
+__device__ constexpr int row_of(int e, int h) { return 8 * (e / 4) + 4 * h + e % 4; }
+
+// Tiles in LDS: rows of kRow bytes in pieces of 16, which change places by the
+// row: piece c of row r lies at c ^ turn(r).  turn is even, so that pairs of
+// pieces stay pairs; the eight rows that a quarter wave reads a piece of, and
+// the four rows that a transposing read takes 32 bytes of, lie in different
+// banks.
+// NB: blocks of 32 columns that the width fills.
+template <typename T, int NB> struct Shape {
+    static constexpr int kBlocks = NB == 3 ? 4 : NB;
+    static constexpr int kRow = kBlocks * 32 * (int)sizeof(T);
+    static constexpr int kPieces = kRow / 16;
+    static constexpr int kPerBanks = kRow >= 256 ? 1 : 256 / kRow;  // rows that fill the banks
+    static constexpr int NK = NB * (int)sizeof(T);                  // fragments of a row: 32 bytes each
+    static constexpr int kGroups = 32 / (2 * Frag<T>::N);           // fragments of 32 summed rows
+    static __device__ int turn(int row) { return 2 * (row / kPerBanks % (8 / kPerBanks)); }
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+
+typedef __attribute__((address_space(3))) void *lds_ptr;
+typedef short Turned __attribute__((ext_vector_type(4)));
+
+// The transposing read of four 16-bit elements: of the 16 lanes that address
+// four rows of 16 columns, lane i gets column i of the four rows.
+__device__ inline Turned turned(const char *lds)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Turned *)lds);
+}
+
+// Waits for this wave's loads into LDS and for all waves.
+__device__ inline void tile_barrier()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// A lane's places in a tile of LDS, from which fragments are read.
+template <typename T, int NB> struct Reader {
+    typedef Shape<T, NB> S;
+    typedef typename Frag<T>::F F;
+    int straight;  // row lane % 32, its half of the first 32 bytes
+    int cross[sizeof(T) == 4 ? 4 : 1];
+    __device__ void init(int lane)
+    {
+        const int row = lane % 32, h = lane / 32;
+        straight = row * S::kRow + (h ^ S::turn(row)) * 16;
+        if constexpr (sizeof(T) == 2) {
+            const int g = lane / 16, r = 4 * (g / 2) + lane % 16 / 4;
+            cross[0] = r * S::kRow + ((2 * (g % 2) + lane % 4 / 2) ^ S::turn(r)) * 16 + lane % 2 * 8;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * h + e;
+                cross[e] = r * S::kRow + ((lane % 32 / 4) ^ S::turn(r)) * 16 + lane % 4 * 4;
+            }
+        }
+    }
+    // Fragment k of 32 rows, the summed index along them.
+    __device__ F row(const char *tile, int k) const { return *(const F *)(tile + (straight ^ (k * 32))); }
+    // Fragment g of block b of columns, the summed index over the rows: lane l
+    // has column l % 32 and, of each 2 N rows, those that a result's registers
+    // hold for its half.
+    __device__ F column(const char *tile, int g, int b) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            const char *p = tile + (cross[0] ^ (b * 64)) + g * 16 * S::kRow;
+            return __builtin_bit_cast(F, __builtin_shufflevector(turned(p), turned(p + 8 * S::kRow), 0, 1, 2, 3, 4, 5,
+                                                                 6, 7));
+        } else {
+            F f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                f[e] = *(const float *)(tile + (cross[e] ^ (b * 128)) + g * 8 * S::kRow);
+            return f;
+        }
+    }
+};
+
+// A tile of ROWS rows from global memory to LDS without registers, by WAVES
+// waves; rows outside [first, end) and columns past the width come as 0.
+template <typename T, int NB, int ROWS, int WAVES> struct Loader {
+    typedef Shape<T, NB> S;
+    static constexpr int kAtOnce = 64 / S::kPieces, kLoads = ROWS / kAtOnce / WAVES;
+    uint32_t at[kLoads];  // rows one stride apart
+    int row0, first;
+    __device__ static int piece(int lane, int row) { return (lane % S::kPieces) ^ S::turn(row); }
+    __device__ void init(int wave, int lane, int width, int64_t stride)
+    {
+        row0 = wave * kLoads * kAtOnce + lane / S::kPieces;
+        first = wave * kLoads * 1024;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = row0 + i * kAtOnce, c = piece(lane, row);
+            at[i] = c * Frag<T>::N < width ? (uint32_t)row * (uint32_t)stride + c * 16 : 0x80000000u;
+        }
+    }
+    // `rows`: of the tile that exist
+    __device__ void load(char *lds, const char *p, int rows) const
+    {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, 0x7FFFFFFF, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + i * 1024), 16,
+                                                     row0 + i * kAtOnce < rows ? at[i] : 0x80000000u, 0, 0, 0);
+    }
+    // Rows of (token, head of the group): rows r0 + [from, to) of the tile exist.
+    __device__ void load_rows(char *lds, const char *p, const Attention &a, const Heads &h, int lane, int r0, int from,
+                              int to) const
+    {
+        const int t0 = r0 / a.group, g0 = r0 - t0 * a.group;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(p + t0 * h.token), 0, 0x7FFFFFFF, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = row0 + i * kAtOnce, c = piece(lane, row), x = g0 + row;
+            const int t = a.group == 1 ? x : (int)__umulhi((uint32_t)x, a.magic), g = x - t * a.group;
+            const uint32_t off = (uint32_t)t * (uint32_t)h.token + (uint32_t)g * (uint32_t)h.head + c * 16;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rsrc, (lds_ptr)(lds + first + i * 1024), 16,
+                row >= from && row < to && c * Frag<T>::N < a.width ? off : 0x80000000u, 0, 0, 0);
+        }
+    }
+};
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float other_half(float v) { return __shfl_xor(v, 32); }
+
+// Registers [g * 2N / 2 ...) of a 32 x 32 result as the fragment of its summed
+// rows, rounded to the type.
+template <typename T> __device__ inline typename Frag<T>::F packed(const f32x16 &s, int g)
+{
+    typename Frag<T>::F f;
+#pragma unroll
+    for (int e = 0; e < Frag<T>::N; ++e)
+        f[e] = (T)s[g * Frag<T>::N + e];
+    return f;
+}
+
+template <int NB> __device__ inline void clear(f32x16 (&acc)[NB])
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            acc[b][e] = 0.f;
+}
+
+// 32 rows of a tile times 32 of the operand in registers: a 32 x 32 result.
+template <typename T, int NB>
+__device__ inline f32x16 product(const char *tile, const Reader<T, NB> &rd,
+                                 const typename Frag<T>::F (&f)[Shape<T, NB>::NK])
+{
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        s[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < Shape<T, NB>::NK; ++k)
+        s = Frag<T>::mma(rd.row(tile, k), f[k], s);
+    return s;
+}
+
+// acc[column][lane] += sum over 32 rows of tile[row][column] * p[row][lane]
+template <typename T, int NB>
+__device__ inline void add_rows(f32x16 (&acc)[NB], const char *tile, const Reader<T, NB> &rd, const f32x16 &p)
+{
+#pragma unroll
+    for (int g = 0; g < Shape<T, NB>::kGroups; ++g) {
+        const typename Frag<T>::F f = packed<T>(p, g);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            acc[b] = Frag<T>::mma(rd.column(tile, g, b), f, acc[b]);
+    }
+}
+
+// The same row by row, for tiles that hold infinities or NaN: where a factor
+// is 0 (a row and a key that do not see each other), nothing is added.
+template <typename T, int NB>
+__device__ inline void add_rows_apart(f32x16 (&acc)[NB], const char *tile, int lane, const f32x16 &p)
+{
+    typedef Shape<T, NB> S;
+    const int h = lane / 32;
+#pragma unroll 1
+    for (int row = 0; row < 32; ++row) {
+        const int r = row / 8 * 4 + row % 4;
+        float w = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            w = e == r ? p[e] : w;
+        w = (float)(T)__shfl(w, lane % 32 + row / 4 % 2 * 32);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int at = (32 * b + row_of(e, h)) * (int)sizeof(T);
+                const float v =
+                    (float)*(const T *)(tile + row * S::kRow + ((at / 16) ^ S::turn(row)) * 16 + at % 16);
+                acc[b][e] = w != 0.f ? __builtin_fmaf(w, v, acc[b][e]) : acc[b][e];
+            }
+    }
+}
+
+template <int NB> __device__ inline bool finite(const f32x16 (&acc)[NB])
+{
+    float t = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            t += acc[b][e] * 0.f;
+    return t == 0.f;
+}
+
+// What a lane's row sees: positions [lo, hi], and those below sinks that are
+// not past hi.
+struct Sight {
+    int lo, hi, sinks;
+    __device__ bool operator()(int j) const { return j <= hi && (j >= lo || j < sinks); }
+};
+
+__device__ inline int64_t index_at(const void *p, int bytes, int i)
+{
+    return bytes == 8 ? ((const int64_t *)p)[i] : ((const int32_t *)p)[i];
+}
+
+// A sequence: position of its first query row, keys that it has.
+struct Span {
+    int offset, length;
+    __device__ Span(const Attention &a, int b)
+    {
+        int64_t o = a.keys - a.tokens, l = a.ring ? kFar : a.keys;
+        if (a.positions) {
+            o = index_at(a.positions, a.position_bytes, b);
+            o = o < -kFar ? -kFar : o > kFar ? kFar : o;
+        }
+        if (a.lengths) {
+            l = index_at(a.lengths, a.length_bytes, b);
+            l = l < 0 ? 0 : l > a.keys ? a.keys : l;
+        }
+        offset = (int)o;
+        length = (int)l;
+    }
+    // Tokens of [t0, t1] that see something, as positions [lo, hi].
+    __device__ bool positions(int t0, int t1, int &lo, int &hi) const
+    {
+        lo = offset + t0 < 0 ? 0 : offset + t0;
+        hi = offset + t1 < length - 1 ? offset + t1 : length - 1;
+        return lo <= hi;
+    }
+};
+
+__device__ inline char *rows_of(const Heads &h, int b, int head) { return h.p + b * h.batch + head * h.head; }
+
+// A row's 16 bytes as a fragment: `have` is whether the row exists.
+template <typename T> __device__ inline typename Frag<T>::F global_frag(const char *row, bool have, int piece, int width)
+{
+    typename Frag<T>::F f = {};
+    if (have && piece * Frag<T>::N < width)
+        f = *(const typename Frag<T>::F *)(row + piece * 16);
+    return f;
+}
+
+// A lane's results of a row: columns 32 b + row_of(e, h), times a factor, or 0.
+template <typename T, int NB>
+__device__ inline void put_row(char *row, int h, int width, const f32x16 (&v)[NB], float factor, bool some)
+{
+    typedef T V __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int col = 32 * b + 8 * r + 4 * h;
+            V x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] = (T)(some ? v[b][4 * r + e] * factor : 0.f);
+            if (col < width)
+                *(V *)(row + col * sizeof(T)) = x;
+        }
+}
+template <int NB> __device__ inline void put_sums(float *row, int h, int width, const f32x16 (&v)[NB])
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int col = 32 * b + 8 * r + 4 * h;
+            if (col < width)
+                *(f32x4 *)(row + col) = f32x4{v[b][4 * r], v[b][4 * r + 1], v[b][4 * r + 2], v[b][4 * r + 3]};
+        }
+}
+#endif
+
+}  // namespace
+}  // namespace rotor
+
+// ---- host ------------------------------------------------------------------
+
+namespace rotor {
+namespace {
+
+constexpr int64_t kMaxWidth = 128, kMaxRows = (int64_t)65535 * 128, kMaxHeads = 1 << 15, kMaxProblems = 1 << 20;
+
+inline bool index_ok(const void *p, int32_t bytes)
+{
+    return !p || ((bytes == 4 || bytes == 8) && (uintptr_t)p % (uintptr_t)bytes == 0);
+}
+
+inline bool attention_sizes_ok(const rotor_attention *n)
+{
+    if (!n || !type_ok(n->type) || n->batch < 0 || n->tokens < 0 || n->keys < 0 || n->heads < 1 || n->kv_heads < 1 ||
+        n->heads > kMaxHeads || n->kv_heads > n->heads || n->heads % n->kv_heads || n->width < 8 ||
+        n->width > kMaxWidth || n->width % 8 || n->window < 0 || n->sinks < 0 || !(n->scale > 0.) ||
+        !(n->scale <= 1e30))
+        return false;
+    return n->batch <= kMaxProblems / n->kv_heads && n->tokens <= kMaxRows / (n->heads / n->kv_heads) &&
+           n->keys < kFar;
+}
+
+// A tensor of heads as the kernels take it; strides of dimensions of one
+// element do not matter.
+inline bool heads_ok(const rotor_heads *h, int64_t batch, int64_t tokens, int64_t heads, int64_t es, Heads &out)
+{
+    out = Heads{nullptr, 0, 0, 0};
+    if (batch == 0 || tokens == 0)
+        return true;
+    if (!h || !h->p || (uintptr_t)h->p % 16)
+        return false;
+    const int64_t n[3] = {batch, tokens, heads}, s[3] = {h->batch, h->token, h->head};
+    int64_t by[3];
+    for (int i = 0; i < 3; ++i) {
+        by[i] = 0;
+        if (n[i] == 1)
+            continue;
+        if (s[i] < 0 || s[i] >= ((int64_t)1 << 58) / es || s[i] * es % 16)
+            return false;
+        by[i] = s[i] * es;
+        if ((unsigned __int128)by[i] * (unsigned __int128)n[i] >= ((unsigned __int128)1 << 61))
+            return false;
+    }
+    out = Heads{(char *)h->p, by[0], by[1], by[2]};
+    return true;
+}
+
+// Offsets in a tile are 32 bits wide: 64 rows of keys, or of (token, head).
+inline bool tiles_ok(const Heads &h, int64_t group)
+{
+    const __int128 most = (__int128)h.token * (64 / group + 2) + (__int128)h.head * group + 1024;
+    return most < ((__int128)1 << 31);
+}
+
+inline void fill(Attention &a, const rotor_attention *n)
+{
+    a = Attention{};
+    a.positions = n->positions;
+    a.lengths = n->lengths;
+    a.position_bytes = n->position_bytes;
+    a.length_bytes = n->length_bytes;
+    a.batch = (int)n->batch;
+    a.kv = (int)n->kv_heads;
+    a.group = (int)(n->heads / n->kv_heads);
+    a.tokens = (int)n->tokens;
+    a.keys = (int)n->keys;
+    a.width = (int)n->width;
+    a.rows = a.tokens * a.group;
+    a.window = n->window == 0 || n->window > kFar ? kFar : (int)n->window;
+    a.sinks = a.window >= a.keys ? 0 : n->sinks < n->keys ? (int)n->sinks : a.keys;
+    a.scale = (float)n->scale;
+    a.c = (float)(n->scale * 1.4426950408889634);
+    a.magic = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
+    a.parts = 1;
+}
+
+template <int N> struct Int {
+    static constexpr int v = N;
+};
+
+// Calls f with the element type's tag and the blocks of 32 columns.
+template <typename F> inline void with_shape(int32_t type, int64_t width, F f)
+{
+    with_type(type, [&](auto e) {
+        if (width <= 64)
+            f(e, Int<2>{});
+        else if (width <= 96)
+            f(e, Int<3>{});
+        else
+            f(e, Int<4>{});
+    });
+}
+
+}  // namespace
+}  // namespace rotor

@@ -1,0 +1,483 @@
+// rotor_window_attention_backward: the scores once more, twice, instead of kept:
+// with rows of queries in the registers for dq, with keys for dk and dv.  No sum
+// is shared between workgroups, so that none depends on their order.
+#include "rotor_attention.h"
+
+#include <type_traits>
+
+namespace rotor {
+namespace {
+
+constexpr int kKeys = 128;   // of a workgroup, gradients of keys
+constexpr int kStepRows = 64;
+
+#if defined(__HIP_DEVICE_COMPILE__)
+// float16 holds 40 bits of range, and dS is as small as the gradients that
+// arrive: it is multiplied by a power of two, so that the largest |do| of a row
+// (of 32 rows, where they are summed) comes to lie in [2^-6, 2^-5).  |dS| is at
+// most twice that times 128 |v|: in range for any v.
+template <typename T> struct Scaled {
+    static constexpr bool kOn = std::is_same<T, f16>::value;
+};
+__device__ inline int exponent_of(float most)
+{
+    return most > 0.f && most <= 3.4e38f ? __builtin_amdgcn_frexp_expf(most) - 1 : -30;
+}
+__device__ inline float power_of(int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
+#endif
+
+// dq: as the forward kernel, with rows in the registers.  It also leaves what
+// the gradients of keys need of each row: log-sum-exp, delta, position.
+template <typename T, int NB>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel(Attention a)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef Shape<T, NB> S;
+    typedef typename Frag<T>::F F;
+    constexpr int kBytes = kTileKeys * S::kRow;
+    __shared__ __attribute__((aligned(1024))) char tiles[2][2][kBytes];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
+    const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
+    const int r0 = (gridDim.y - 1 - blockIdx.y) * kTileRows, rw = r0 + wave * 32, row = rw + lane % 32;
+    const Span span(a, b);
+    const int last_row = min(a.rows - 1, r0 + kTileRows - 1);
+    const int t = row / a.group, p = span.offset + t, head = kv * a.group + row % a.group;
+    const bool seen = row < a.rows && p >= 0 && p < span.length;
+
+    F q[S::NK], d[S::NK];
+    float delta = 0.f, most = 0.f, lse = kInf;
+    {
+        const char *at[3] = {rows_of(a.q, b, head) + t * a.q.token, rows_of(a.dout, b, head) + t * a.dout.token,
+                             rows_of(a.out, b, head) + t * a.out.token};
+#pragma unroll
+        for (int k = 0; k < S::NK; ++k) {
+            q[k] = global_frag<T>(at[0], seen, 2 * k + h, a.width);
+            d[k] = global_frag<T>(at[1], seen, 2 * k + h, a.width);
+            const F o = global_frag<T>(at[2], seen, 2 * k + h, a.width);
+#pragma unroll
+            for (int e = 0; e < Frag<T>::N; ++e) {
+                delta += (float)d[k][e] * (float)o[e];
+                most = fmaxf(most, fabsf((float)d[k][e]));
+            }
+        }
+        if (seen)
+            lse = a.lse[((int64_t)b * a.tokens + t) * ((int64_t)a.kv * a.group) + head] * kLog2e;
+    }
+    delta += other_half(delta);
+    most = fmaxf(most, other_half(most));
+    int exponent = 0;
+    {
+        const int64_t at = (int64_t)blockIdx.x * a.row_pitch + row;  // the pitch covers the last tile
+        if (h == 0) {
+            a.row_lse[at] = lse;
+            a.row_delta[at] = delta;
+        } else {
+            a.row_at[at] = seen ? p : -1;
+        }
+        if constexpr (Scaled<T>::kOn) {
+            exponent = exponent_of(most) + 6;
+            float all = most;
+#pragma unroll
+            for (int off = 16; off >= 1; off /= 2)
+                all = fmaxf(all, __shfl_xor(all, off));
+            if (lane == 0)
+                a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + rw / 32] = exponent_of(all) + 6;
+        }
+    }
+    char *const to = rows_of(a.dq, b, head) + t * a.dq.token;
+    f32x16 acc[NB];
+    clear(acc);
+    int lo, hi;
+    if (!span.positions(r0 / a.group, last_row / a.group, lo, hi)) {
+        if (row < a.rows)
+            put_row<T>(to, h, a.width, acc, 0.f, false);
+        return;
+    }
+    const float factor = Scaled<T>::kOn ? power_of(-exponent) : 1.f;
+    const Sight sight{p - a.window + 1, p, a.sinks};
+    int wlo = 0, whi = -1;
+    const bool some = rw < a.rows && span.positions(rw / a.group, min(a.rows - 1, rw + 31) / a.group, wlo, whi);
+
+    const int from = max(0, lo - a.window + 1), ahead = min(a.sinks, from);
+    const int first = (ahead + kTileKeys - 1) / kTileKeys, begin = max(first, from / kTileKeys);
+    const int n = first + hi / kTileKeys - begin + 1;
+    Loader<T, NB, kTileKeys, kWaves> lk, lv;
+    lk.init(wave, lane, a.width, a.k.token);
+    lv.init(wave, lane, a.width, a.v.token);
+    Reader<T, NB> rd;
+    rd.init(lane);
+    const char *const k0 = rows_of(a.k, b, kv), *const v0 = rows_of(a.v, b, kv);
+    auto load = [&](int i) {
+        const int j = (i < first ? i : begin + i - first) * kTileKeys;
+        lk.load(tiles[i & 1][0], k0 + j * a.k.token, hi + 1 - j);
+        lv.load(tiles[i & 1][1], v0 + j * a.v.token, hi + 1 - j);
+    };
+    auto pass = [&](auto apart) {
+        constexpr bool kApart = decltype(apart)::value;
+        load(0);
+        for (int i = 0; i < n; ++i) {
+            tile_barrier();
+            if (i + 1 < n)
+                load(i + 1);
+            const int j = (i < first ? i : begin + i - first) * kTileKeys;
+#pragma unroll
+            for (int k = 0; k < kTileKeys / 32; ++k) {
+                const int jk = j + 32 * k, je = jk + 31;
+                if (!some || jk > whi || (jk >= a.sinks && je < wlo - a.window + 1))
+                    continue;
+                const char *keys = tiles[i & 1][0] + k * 32 * S::kRow, *vals = tiles[i & 1][1] + k * 32 * S::kRow;
+                f32x16 s = product<T, NB>(keys, rd, q), ds = product<T, NB>(vals, rd, d);
+                const bool all = je <= wlo && (je < a.sinks || jk >= whi - a.window + 1);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    ds[e] = exp2_of(__builtin_fmaf(s[e], a.c, -lse)) * ((ds[e] - delta) * factor);
+                if (!all) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        ds[e] = sight(jk + row_of(e, h)) ? ds[e] : 0.f;
+                }
+                if constexpr (kApart)
+                    add_rows_apart<T, NB>(acc, keys, lane, ds);
+                else
+                    add_rows<T, NB>(acc, keys, rd, ds);
+            }
+        }
+    };
+    pass(std::false_type{});
+    // infinities or NaN may have come from keys that a row does not see
+    if (__syncthreads_or(!finite(acc))) {
+        clear(acc);
+        pass(std::true_type{});
+    }
+    if (row < a.rows)
+        put_row<T>(to, h, a.width, acc, a.scale * (Scaled<T>::kOn ? power_of(exponent) : 1.f), seen);
+#endif
+}
+
+// dk and dv of 128 keys, 32 a wave: the rows that see any of them pass through
+// LDS, 64 at a time.  blockIdx.y: first the tiles with keys that every later row
+// sees, whose rows are split into sink_parts, then the others, in parts.
+template <typename T, int NB>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(Attention a)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef Shape<T, NB> S;
+    typedef typename Frag<T>::F F;
+    constexpr int kBytes = kStepRows * S::kRow;
+    __shared__ __attribute__((aligned(1024))) char tiles[2][2][kBytes];  // [which][q, do]
+    __shared__ __attribute__((aligned(16))) float stats[2][3][kStepRows];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
+    const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
+    int tile, part, parts;
+    {
+        const int item = blockIdx.y, ahead = a.sink_tiles * a.sink_parts;
+        if (item < ahead) {
+            parts = a.sink_parts;
+            tile = item / parts;
+            part = item - tile * parts;
+        } else {
+            parts = a.parts;
+            tile = (item - ahead) / parts;
+            part = item - ahead - tile * parts;
+            tile += a.sink_tiles;
+        }
+    }
+    const int j0 = tile * kKeys, jw = j0 + wave * 32, key = jw + lane % 32;
+    const Span span(a, b);
+    const bool have = key < span.length;
+    F kf[S::NK], vf[S::NK];
+    {
+        const char *k = rows_of(a.k, b, kv) + key * a.k.token, *v = rows_of(a.v, b, kv) + key * a.v.token;
+#pragma unroll
+        for (int i = 0; i < S::NK; ++i) {
+            kf[i] = global_frag<T>(k, have, 2 * i + h, a.width);
+            vf[i] = global_frag<T>(v, have, 2 * i + h, a.width);
+        }
+    }
+    f32x16 dk[NB], dv[NB];
+    clear(dk);
+    clear(dv);
+    int exponent = -1000;  // of what dk is multiplied with
+
+    // positions that see a key of the tile, as rows, in steps of 64
+    const int64_t far = j0 < a.sinks ? (int64_t)kFar * 2 : (int64_t)j0 + kKeys - 1 + a.window - 1;
+    const int plo = max(j0, 0), phi = (int)min((int64_t)span.length - 1, far);
+    const int t0 = max(0, plo - span.offset);
+    const int64_t t1 = min((int64_t)a.tokens - 1, (int64_t)phi - span.offset);
+    int n = 0, begin = 0;
+    if (t0 <= t1) {
+        begin = t0 * a.group / kStepRows;
+        n = (int)((t1 + 1) * a.group + kStepRows - 1) / kStepRows - begin;
+    }
+    const int i0 = begin + (int)((int64_t)n * part / parts), i1 = begin + (int)((int64_t)n * (part + 1) / parts);
+
+    Loader<T, NB, kStepRows, kWaves> ld;
+    ld.init(wave, lane, a.width, 0);
+    Reader<T, NB> rd;
+    rd.init(lane);
+    const char *const q0 = rows_of(a.q, b, kv * a.group), *const d0 = rows_of(a.dout, b, kv * a.group);
+    // rows without a place in the sequence are not read
+    const int64_t live0 = max((int64_t)0, -(int64_t)span.offset) * a.group;
+    const int64_t live1 = min((int64_t)a.tokens, max((int64_t)0, (int64_t)span.length - span.offset)) * a.group;
+    auto load = [&](int i) {
+        const int r = i * kStepRows;
+        const int from = (int)max((int64_t)0, min((int64_t)kStepRows, live0 - r));
+        const int to = (int)max((int64_t)0, min((int64_t)kStepRows, live1 - r));
+        ld.load_rows(tiles[i & 1][0], q0, a, a.q, lane, r, from, to);
+        ld.load_rows(tiles[i & 1][1], d0, a, a.dout, lane, r, from, to);
+        if (wave < 3) {
+            const void *const p = wave == 0 ? (const void *)a.row_lse : wave == 1 ? (const void *)a.row_delta : a.row_at;
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
+                (void *)((const char *)p + ((int64_t)blockIdx.x * a.row_pitch + r) * 4), 0, kStepRows * 4, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)stats[i & 1][wave], 4, lane * 4, 0, 0, 0);
+        }
+    };
+    auto pass = [&](auto apart) {
+        constexpr bool kApart = decltype(apart)::value;
+        if (i0 < i1)
+            load(i0);
+        for (int i = i0; i < i1; ++i) {
+            tile_barrier();
+            if (i + 1 < i1)
+                load(i + 1);
+#pragma unroll 1
+            for (int u = 0; u < kStepRows / 32; ++u) {
+                const int r = i * kStepRows + u * 32;
+                int lo, hi;
+                if (r >= a.rows || !span.positions(r / a.group, min(a.rows - 1, r + 31) / a.group, lo, hi) ||
+                    jw > hi || (jw >= a.sinks && jw + 31 < lo - a.window + 1))
+                    continue;
+                const bool all = r >= live0 && r + 32 <= live1 && jw + 31 <= lo &&
+                                 (jw + 31 < a.sinks || jw >= hi - a.window + 1);
+                const char *qt = tiles[i & 1][0] + u * 32 * S::kRow, *dt = tiles[i & 1][1] + u * 32 * S::kRow;
+                const float *st = &stats[i & 1][0][u * 32];
+                f32x16 s = product<T, NB>(qt, rd, kf), ds = product<T, NB>(dt, rd, vf);
+                float factor = 1.f;
+                if constexpr (Scaled<T>::kOn) {
+                    const int e = a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + r / 32];
+                    if (e > exponent) {
+                        const float by = power_of(max(exponent - e, -300));
+#pragma unroll
+                        for (int x = 0; x < NB; ++x)
+#pragma unroll
+                            for (int y = 0; y < 16; ++y)
+                                dk[x][y] *= by;
+                        exponent = e;
+                    }
+                    factor = power_of(-exponent);
+                }
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 l = *(const f32x4 *)(st + 8 * g + 4 * h);
+                    const f32x4 dl = *(const f32x4 *)(st + kStepRows + 8 * g + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[4 * g + e] = exp2_of(__builtin_fmaf(s[4 * g + e], a.c, -l[e]));
+                        ds[4 * g + e] = s[4 * g + e] * ((ds[4 * g + e] - dl[e]) * factor);
+                    }
+                }
+                if (!all) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        typedef int i32x4 __attribute__((ext_vector_type(4)));
+                        const i32x4 p = *(const i32x4 *)(st + 2 * kStepRows + 8 * g + 4 * h);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool in = key <= p[e] && (key > p[e] - a.window || key < a.sinks);
+                            s[4 * g + e] = in ? s[4 * g + e] : 0.f;
+                            ds[4 * g + e] = in ? ds[4 * g + e] : 0.f;
+                        }
+                    }
+                }
+                if constexpr (kApart) {
+                    add_rows_apart<T, NB>(dv, dt, lane, s);
+                    add_rows_apart<T, NB>(dk, qt, lane, ds);
+                } else {
+                    add_rows<T, NB>(dv, dt, rd, s);
+                    add_rows<T, NB>(dk, qt, rd, ds);
+                }
+            }
+        }
+    };
+    pass(std::false_type{});
+    // infinities or NaN may have come from rows that do not see a key
+    if (__syncthreads_or(!finite(dk) || !finite(dv))) {
+        clear(dk);
+        clear(dv);
+        exponent = -1000;
+        pass(std::true_type{});
+    }
+    const float by = a.scale * (Scaled<T>::kOn ? power_of(max(exponent, -300)) : 1.f);
+    if (parts > 1) {
+        const int64_t at = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kKeys + wave * 32 + lane % 32) * a.width;
+#pragma unroll
+        for (int x = 0; x < NB; ++x)
+#pragma unroll
+            for (int y = 0; y < 16; ++y)
+                dk[x][y] *= by;
+        put_sums(a.part_dk + at, h, a.width, dk);
+        put_sums(a.part_dv + at, h, a.width, dv);
+    } else if (key < a.keys) {
+        put_row<T>(rows_of(a.dk, b, kv) + key * a.dk.token, h, a.width, dk, by, have);
+        put_row<T>(rows_of(a.dv, b, kv) + key * a.dv.token, h, a.width, dv, 1.f, have);
+    }
+#endif
+}
+
+// The parts' sums of dk and dv joined, in their order: four columns a thread;
+// blockIdx.y: tile of keys (of those in parts), z: dk, dv.
+template <typename T> __global__ __launch_bounds__(256) void join_keys_kernel(Attention a)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int tile = blockIdx.y;
+    const bool sink = tile < a.sink_tiles;
+    const int parts = sink ? a.sink_parts : a.parts;
+    const int64_t item = sink ? (int64_t)tile * parts
+                              : (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(tile - a.sink_tiles) * parts;
+    const int per = a.width / 4, heads = a.batch * a.kv;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, line = i / per;
+    if (line >= (int64_t)heads * kKeys)
+        return;
+    const int col = (int)(i - line * per) * 4, bk = (int)(line / kKeys), key = tile * kKeys + (int)(line % kKeys);
+    if (key >= a.keys)
+        return;
+    const float *p = blockIdx.z ? a.part_dv : a.part_dk;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k)
+        v += *(const f32x4 *)(p + (((item + k) * heads + bk) * kKeys + line % kKeys) * a.width + col);
+    const Heads &h = blockIdx.z ? a.dv : a.dk;
+    const Span span(a, bk / a.kv);
+    typedef T V __attribute__((ext_vector_type(4)));
+    V x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        x[e] = (T)(key < span.length ? v[e] : 0.f);
+    *(V *)(rows_of(h, bk / a.kv, bk % a.kv) + key * h.token + col * sizeof(T)) = x;
+#endif
+}
+
+}  // namespace
+}  // namespace rotor
+
+namespace rotor {
+namespace {
+
+struct BackPlan {
+    int row_pitch, tiles, sink_tiles, sink_parts, parts;
+    int64_t items;  // whose sums go through the workspace
+    uint64_t row_bytes, exp_bytes, part_bytes;
+    uint64_t bytes() const { return 3 * row_bytes + exp_bytes + 2 * part_bytes; }
+};
+
+// Rows of a tile of keys are split where the tiles leave CUs without work, and
+// where a tile holds first keys, which all rows see, into parts about as long
+// as the other tiles'.
+bool back_plan(const rotor_attention *n, BackPlan &p)
+{
+    const int64_t group = n->heads / n->kv_heads, rows = n->tokens * group, bk = n->batch * n->kv_heads;
+    const int64_t pitch = ceil_div(rows, kTileRows) * kTileRows, tiles = ceil_div(n->keys, kKeys);
+    const bool windowed = n->window && n->window < n->keys;
+    const int64_t sinks = windowed ? (n->sinks < n->keys ? n->sinks : n->keys) : 0;
+    const int64_t sink_tiles = ceil_div(sinks, kKeys);
+    const int64_t seen = windowed && n->window + kKeys - 1 < n->tokens ? n->window + kKeys - 1 : n->tokens;
+    const int64_t steps = ceil_div(seen * group, kStepRows) + 1, sink_steps = ceil_div(rows, kStepRows);
+    const int64_t base = tiles * bk;
+    int64_t parts = 1;
+    if (base > 0 && base < 384) {
+        parts = ceil_div(512, base) < steps / 4 ? ceil_div(512, base) : steps / 4;
+        parts = parts < 1 ? 1 : parts > 16 ? 16 : parts;
+    }
+    const int64_t each = steps / parts > 4 ? steps / parts : 4;
+    int64_t sink_parts = ceil_div(sink_steps, each);
+    sink_parts = sink_parts > 64 ? 64 : sink_parts;
+    sink_parts = sink_parts < parts ? parts : sink_parts;
+    const int64_t all = sink_tiles * sink_parts + (tiles - sink_tiles) * parts;
+    if (all > 65535 || pitch > kMaxRows)
+        return false;
+    p.row_pitch = (int)pitch;
+    p.tiles = (int)tiles;
+    p.sink_tiles = (int)sink_tiles;
+    p.sink_parts = (int)sink_parts;
+    p.parts = (int)parts;
+    p.items = parts > 1 ? all : sink_parts > 1 ? sink_tiles * sink_parts : 0;
+    p.row_bytes = round256((uint64_t)bk * pitch * 4);
+    p.exp_bytes = n->type == ROTOR_F16 ? round256((uint64_t)bk * (pitch / 32) * 4) : 0;
+    p.part_bytes = round256((uint64_t)p.items * bk * kKeys * n->width * 4);
+    return true;
+}
+
+}  // namespace
+}  // namespace rotor
+
+using namespace rotor;
+
+extern "C" {
+
+int32_t rotor_window_attention_backward_workspace_bytes(const rotor_attention *how, uint64_t *bytes)
+{
+    BackPlan p;
+    if (!bytes || !attention_sizes_ok(how) || !back_plan(how, p))
+        return ROTOR_EINVAL;
+    *bytes = p.bytes();
+    return ROTOR_OK;
+}
+
+int32_t rotor_window_attention_backward(const rotor_attention *how, const rotor_heads *dout, const rotor_heads *q,
+                                        const rotor_heads *k, const rotor_heads *v, const rotor_heads *out,
+                                        const float *d_lse, const rotor_heads *dq, const rotor_heads *dk,
+                                        const rotor_heads *dv, void *d_work, uint64_t work_bytes, void *stream)
+{
+    BackPlan p;
+    if (!attention_sizes_ok(how) || !index_ok(how->positions, how->position_bytes) ||
+        !index_ok(how->lengths, how->length_bytes) || !back_plan(how, p))
+        return ROTOR_EINVAL;
+    const int64_t es = elem_bytes(how->type), b = how->batch, t = how->tokens, m = how->keys;
+    Attention a;
+    fill(a, how);
+    if (!heads_ok(q, b, t, how->heads, es, a.q) || !heads_ok(dout, b, t, how->heads, es, a.dout) ||
+        !heads_ok(out, b, t, how->heads, es, a.out) || !heads_ok(dq, b, t, how->heads, es, a.dq) ||
+        !heads_ok(k, b, m, how->kv_heads, es, a.k) || !heads_ok(v, b, m, how->kv_heads, es, a.v) ||
+        !heads_ok(dk, b, m, how->kv_heads, es, a.dk) || !heads_ok(dv, b, m, how->kv_heads, es, a.dv) ||
+        !tiles_ok(a.k, 1) || !tiles_ok(a.v, 1) || !tiles_ok(a.q, a.group) || !tiles_ok(a.dout, a.group) ||
+        (uintptr_t)d_lse % 4 || (b > 0 && t > 0 && !d_lse))
+        return ROTOR_EINVAL;
+    if (b == 0 || (t == 0 && m == 0))
+        return ROTOR_OK;
+    if (p.bytes() > 0 && (!d_work || (uintptr_t)d_work % 16 || work_bytes < p.bytes()))
+        return ROTOR_EINVAL;
+    char *w = (char *)d_work;
+    a.lse = (float *)d_lse;
+    a.row_lse = (float *)w;
+    a.row_delta = (float *)(w += p.row_bytes);
+    a.row_at = (int *)(w += p.row_bytes);
+    a.row_exp = (int *)(w += p.row_bytes);
+    a.part_dk = (float *)(w += p.exp_bytes);
+    a.part_dv = (float *)(w += p.part_bytes);
+    a.row_pitch = p.row_pitch;
+    a.tiles = p.tiles;
+    a.sink_tiles = p.sink_tiles;
+    a.sink_parts = p.sink_parts;
+    a.parts = p.parts;
+    const hipStream_t s = (hipStream_t)stream;
+    const uint32_t bk = (uint32_t)(a.batch * a.kv);
+    (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
+    with_shape(how->type, how->width, [&](auto e, auto nb) {
+        typedef typename decltype(e)::T T;
+        constexpr int NB = decltype(nb)::v;
+        if (t > 0)
+            query_kernel<T, NB><<<dim3(bk, (uint32_t)(p.row_pitch / kTileRows)), kThreads, 0, s>>>(a);
+        if (m == 0)
+            return;
+        const int items = p.sink_tiles * p.sink_parts + (p.tiles - p.sink_tiles) * p.parts;
+        key_kernel<T, NB><<<dim3(bk, (uint32_t)items), kThreads, 0, s>>>(a);
+        if (p.items > 0) {
+            const int joined = p.parts > 1 ? p.tiles : p.sink_tiles;
+            join_keys_kernel<T><<<dim3((uint32_t)ceil_div((int64_t)bk * kKeys * (a.width / 4), 256), (uint32_t)joined, 2),
+                                  256, 0, s>>>(a);
+        }
+    });
+    return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+}
+
+}  // extern "C"

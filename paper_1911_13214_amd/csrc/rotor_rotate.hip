@@ -1,0 +1,539 @@
+// rotor_head_norm_rotate: norms of query and key heads and their rotation by
+// position, one pass; and the gradients.
+//
+// A head's columns are width / 2 pairs: those that turn together and, past the
+// rotated columns, the rest in pairs of no meaning.  A lane holds V adjacent
+// pairs, a team of lanes (a power of two) a head, a wave 64 / team heads at a
+// time of one token, whose angles it computes once.
+//
+// Angles.  A frequency is a 64-bit fraction of a turn, so that position times
+// frequency, modulo 2^64, is the angle, exact but for the frequency's own last
+// bit; a quarter turn is taken off and the rest, at most pi / 4, goes through
+// the Taylor series of sine and cosine (to x^9 and x^10: within 2e-9).
+#include "rotor_ops.h"
+
+#include <math.h>
+
+namespace rotor {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMaxPairs = ROTOR_ROTATE_MAX_WIDTH / 2;
+constexpr int kBlocks = 1024;  // of the gradients: each leaves one row of sums
+
+struct HeadRows {
+    char *p;
+    int64_t batch, token, head;  // bytes
+};
+
+struct RotateArgs {
+    HeadRows in[2], out[2], grad[2];  // of q and k; gradients of the results
+    const void *weight[2];
+    const void *positions;
+    int64_t position_batch;
+    int position_bytes, norm;
+    int tokens, heads[2], width, rotary, team;
+    int64_t all;      // tokens of all sequences
+    int turns, split; // rounds of heads, and into how many waves a token's are split
+    float eps;
+    float *sums;      // [block][2][width]
+    uint64_t frequency[kMaxPairs];
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+
+__device__ inline float team_sum(float v, int team)
+{
+    for (int off = team / 2; off >= 1; off /= 2)
+        v += __shfl_xor(v, off);
+    return v;
+}
+
+__device__ inline void turn_of(uint64_t phase, float &c, float &s)
+{
+    const uint64_t quarter = (phase + ((uint64_t)1 << 61)) >> 62;
+    const int64_t rest = (int64_t)(phase - (quarter << 62));
+    const float x = (float)(int32_t)(rest >> 30) * 3.6572952e-10f;  // 2 pi / 2^34
+    const float y = x * x;
+    float sn = __builtin_fmaf(y, 2.7557319e-6f, -1.9841270e-4f);
+    sn = __builtin_fmaf(y, sn, 8.3333333e-3f);
+    sn = __builtin_fmaf(y, sn, -1.6666667e-1f);
+    sn = __builtin_fmaf(x * y, sn, x);
+    float cs = __builtin_fmaf(y, -2.7557319e-7f, 2.4801587e-5f);
+    cs = __builtin_fmaf(y, cs, -1.3888889e-3f);
+    cs = __builtin_fmaf(y, cs, 4.1666667e-2f);
+    cs = __builtin_fmaf(y, cs, -0.5f);
+    cs = __builtin_fmaf(y, cs, 1.f);
+    const bool odd = quarter & 1;
+    c = odd ? sn : cs;
+    s = odd ? cs : sn;
+    c = quarter == 1 || quarter == 2 ? -c : c;
+    s = quarter == 2 || quarter == 3 ? -s : s;
+}
+
+// A lane's pairs of a head.
+template <typename T, int V, int N, bool INTER> struct Pairs {
+    int first[N], col[N], apart[N];  // first pair; its columns
+    bool have[N];
+    __device__ void init(const RotateArgs &a, int lane)
+    {
+        const int half = a.rotary / 2;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int s = (n * 64 + lane % a.team) * V;
+            first[n] = s;
+            have[n] = s < a.width / 2;
+            if (INTER) {
+                col[n] = 2 * s;
+                apart[n] = 0;
+            } else {
+                col[n] = s < half ? s : s + half;
+                apart[n] = s < half ? half : a.width / 2 - half;
+            }
+        }
+    }
+    __device__ void load(const T *p, bool row, float (&x)[N][2][V]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                x[n][0][e] = x[n][1][e] = 0.f;
+            if (!row || !have[n])
+                continue;
+            if constexpr (INTER) {
+                float f[2 * V];
+                load_vec(p + col[n], f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    x[n][0][e] = f[2 * e];
+                    x[n][1][e] = f[2 * e + 1];
+                }
+            } else {
+                load_vec(p + col[n], x[n][0]);
+                load_vec(p + col[n] + apart[n], x[n][1]);
+            }
+        }
+    }
+    template <typename O> __device__ void store(O *p, bool row, const float (&x)[N][2][V]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (!row || !have[n])
+                continue;
+            if constexpr (INTER) {
+                float f[2 * V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    f[2 * e] = x[n][0][e];
+                    f[2 * e + 1] = x[n][1][e];
+                }
+                store_vec(p + col[n], f);
+            } else {
+                store_vec(p + col[n], x[n][0]);
+                store_vec(p + col[n] + apart[n], x[n][1]);
+            }
+        }
+    }
+    // The angles of a position.
+    __device__ void angles(const RotateArgs &a, uint64_t position, float (&c)[N][V], float (&s)[N][V]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const int i = first[n] + e;
+                c[n][e] = 1.f;
+                s[n][e] = 0.f;
+                if (i < a.rotary / 2)
+                    turn_of(position * a.frequency[i], c[n][e], s[n][e]);
+            }
+    }
+    // Rotates; what is not rotated is not touched (0 times infinity).
+    __device__ void rotate(const RotateArgs &a, float (&x)[N][2][V], const float (&c)[N][V], const float (&s)[N][V],
+                           float way) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const bool in = first[n] + e < a.rotary / 2;
+                const float u = x[n][0][e], v = x[n][1][e], t = s[n][e] * way;
+                x[n][0][e] = in ? u * c[n][e] - v * t : u;
+                x[n][1][e] = in ? v * c[n][e] + u * t : v;
+            }
+    }
+};
+
+template <int V, int N, typename F> __device__ inline void each(F f)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                f(n, z, e);
+}
+
+// u to its normed row (and 1 / deviation).
+template <int V, int N, typename P>
+__device__ inline float normed(const RotateArgs &a, const P &at, float (&u)[N][2][V])
+{
+    if (a.norm == ROTOR_NORM_LAYER) {
+        float sum = 0.f;
+        each<V, N>([&](int n, int z, int e) { sum += u[n][z][e]; });
+        const float mean = team_sum(sum, a.team) / (float)a.width;
+        each<V, N>([&](int n, int z, int e) { u[n][z][e] = at.have[n] ? u[n][z][e] - mean : 0.f; });
+    }
+    float sum = 0.f;
+    each<V, N>([&](int n, int z, int e) { sum += u[n][z][e] * u[n][z][e]; });
+    const float r = 1.f / sqrtf(team_sum(sum, a.team) / (float)a.width + a.eps);
+    each<V, N>([&](int n, int z, int e) { u[n][z][e] *= r; });
+    return r;
+}
+
+__device__ inline uint64_t position_of(const RotateArgs &a, int64_t b, int t)
+{
+    if (!a.positions)
+        return (uint64_t)t;
+    const int64_t i = b * a.position_batch + t;
+    return a.position_bytes == 8 ? (uint64_t)((const int64_t *)a.positions)[i]
+                                 : (uint64_t)(int64_t)((const int32_t *)a.positions)[i];
+}
+__device__ inline char *row_at(const HeadRows &h, int64_t b, int t, int head)
+{
+    return h.p + b * h.batch + t * h.token + head * h.head;
+}
+#endif
+
+template <typename T, int V, int N, bool INTER> __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int lane = threadIdx.x % 64;
+    const int64_t task = block_at() * kWaves + threadIdx.x / 64, n = task / a.split;
+    if (n >= a.all)
+        return;
+    const int part = (int)(task - n * a.split);
+    const int64_t b = n / a.tokens;
+    const int t = (int)(n - b * a.tokens), teams = 64 / a.team;
+    Pairs<T, V, N, INTER> at;
+    at.init(a, lane);
+    float c[N][V], s[N][V];
+    at.angles(a, position_of(a, b, t), c, s);
+    for (int i = part; i < a.turns; i += a.split) {
+        int head = i * teams + lane / a.team;
+        const bool row = head < a.heads[0] + a.heads[1];
+        const int z = head >= a.heads[0] ? 1 : 0;
+        head -= z ? a.heads[0] : 0;
+        float u[N][2][V], w[N][2][V];
+        at.load((const T *)row_at(a.in[z], b, t, head), row, u);
+        const T *weight = (const T *)a.weight[z];
+        if (weight)
+            at.load(weight, row, w);
+        if (a.norm != ROTOR_NORM_NONE) {
+            normed<V, N>(a, at, u);
+            if (weight)
+                each<V, N>([&](int p, int q, int e) { u[p][q][e] *= w[p][q][e]; });
+        }
+        at.rotate(a, u, c, s, 1.f);
+        at.store((T *)row_at(a.out[z], b, t, head), row, u);
+    }
+#endif
+}
+
+template <typename T, int V, int N, bool INTER>
+__global__ __launch_bounds__(kThreads) void rotate_back_kernel(RotateArgs a)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, teams = 64 / a.team;
+    Pairs<T, V, N, INTER> at;
+    at.init(a, lane);
+    float sums[2][N][2][V];
+    for (int z = 0; z < 2; ++z)
+        each<V, N>([&](int p, int q, int e) { sums[z][p][q][e] = 0.f; });
+    const int64_t stride = (int64_t)gridDim.x * kWaves;
+    for (int64_t task = (int64_t)blockIdx.x * kWaves + wave; task < a.all * a.split; task += stride) {
+        const int64_t n = task / a.split, b = n / a.tokens;
+        const int t = (int)(n - b * a.tokens), part = (int)(task - n * a.split);
+        float c[N][V], s[N][V];
+        at.angles(a, position_of(a, b, t), c, s);
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            float w[N][2][V];
+            const T *weight = (const T *)a.weight[z];
+            each<V, N>([&](int p, int q, int e) { w[p][q][e] = 1.f; });
+            if (weight)
+                at.load(weight, true, w);
+            for (int i = part * teams; i < a.heads[z]; i += a.split * teams) {
+                const int head = i + lane / a.team;
+                const bool row = head < a.heads[z];
+                float g[N][2][V], u[N][2][V];
+                at.load((const T *)row_at(a.grad[z], b, t, head), row, g);
+                if (a.norm != ROTOR_NORM_NONE)
+                    at.load((const T *)row_at(a.in[z], b, t, head), row, u);
+                at.rotate(a, g, c, s, -1.f);
+                if (a.norm != ROTOR_NORM_NONE) {
+                    const float r = normed<V, N>(a, at, u);
+                    float dot = 0.f, sum = 0.f;
+                    each<V, N>([&](int p, int q, int e) {
+                        sums[z][p][q][e] += row ? g[p][q][e] * u[p][q][e] : 0.f;
+                        g[p][q][e] *= w[p][q][e];
+                        dot += g[p][q][e] * u[p][q][e];
+                        sum += g[p][q][e];
+                    });
+                    dot = team_sum(dot, a.team) / (float)a.width;
+                    const float mean = a.norm == ROTOR_NORM_LAYER ? team_sum(sum, a.team) / (float)a.width : 0.f;
+                    each<V, N>([&](int p, int q, int e) { g[p][q][e] = r * (g[p][q][e] - mean - u[p][q][e] * dot); });
+                }
+                at.store((T *)row_at(a.out[z], b, t, head), row, g);
+            }
+        }
+    }
+    if (!a.sums)
+        return;
+    // over the teams, then over the waves in order
+    __shared__ float lines[kWaves][2][ROTOR_ROTATE_MAX_WIDTH];
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        each<V, N>([&](int p, int q, int e) {
+            for (int off = a.team; off < 64; off *= 2)
+                sums[z][p][q][e] += __shfl_xor(sums[z][p][q][e], off);
+        });
+        at.store(lines[wave][z], lane < a.team, sums[z]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.width; i += kThreads) {
+        const int z = i / a.width, col = i - z * a.width;
+        float v = lines[0][z][col];
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k)
+            v += lines[k][z][col];
+        a.sums[(int64_t)blockIdx.x * 2 * a.width + i] = v;
+    }
+#endif
+}
+
+// The blocks' sums joined in their order: 16 columns a workgroup, 16 strips of
+// blocks.
+template <typename T> __global__ __launch_bounds__(256) void join_kernel(const float *sums, int blocks, int width, T *dq, T *dk)
+{
+    __shared__ float strip[16][16];
+    const int col = blockIdx.x * 16 + threadIdx.x % 16, k = threadIdx.x / 16, z = blockIdx.y;
+    float v = 0.f;
+    if (col < width)
+#pragma unroll 8
+        for (int i = k; i < blocks; i += 16)
+            v += sums[((int64_t)i * 2 + z) * width + col];
+    strip[k][threadIdx.x % 16] = v;
+    __syncthreads();
+    T *const out = z ? dk : dq;
+    if (k == 0 && col < width && out) {
+        for (int i = 1; i < 16; ++i)
+            v += strip[i][threadIdx.x];
+        out[col] = (T)v;
+    }
+}
+
+bool rotation_ok(const rotor_head_rotation *n)
+{
+    return n && type_ok(n->type) && n->norm >= ROTOR_NORM_NONE && n->norm <= ROTOR_NORM_LAYER &&
+           (n->interleaved == 0 || n->interleaved == 1) && n->batch >= 0 && n->tokens >= 0 && n->heads >= 1 &&
+           n->kv_heads >= 0 && n->heads <= 1 << 20 && n->kv_heads <= 1 << 20 && n->width >= 2 &&
+           n->width <= ROTOR_ROTATE_MAX_WIDTH && n->width % 2 == 0 && n->rotary >= 0 && n->rotary <= n->width &&
+           n->rotary % 2 == 0 && n->eps >= 0. && n->tokens < ((int64_t)1 << 31) &&
+           (unsigned __int128)n->batch * (unsigned __int128)n->tokens < ((uint64_t)1 << 40);
+}
+
+bool head_rows_ok(const rotor_heads *h, const rotor_head_rotation *n, int64_t heads, HeadRows &out)
+{
+    out = HeadRows{nullptr, 0, 0, 0};
+    if (heads == 0 || n->batch == 0 || n->tokens == 0)
+        return true;
+    const int64_t es = elem_bytes(n->type);
+    if (!h || !h->p || (uintptr_t)h->p % (uintptr_t)es)
+        return false;
+    const int64_t count[3] = {n->batch, n->tokens, heads}, s[3] = {h->batch, h->token, h->head};
+    int64_t by[3];
+    for (int i = 0; i < 3; ++i) {
+        by[i] = count[i] == 1 ? 0 : s[i];
+        if (by[i] < 0 || (unsigned __int128)by[i] * (unsigned __int128)count[i] >= ((unsigned __int128)1 << 58))
+            return false;
+        by[i] *= es;
+    }
+    out = HeadRows{(char *)h->p, by[0], by[1], by[2]};
+    return true;
+}
+
+template <int N> struct Num {
+    static constexpr int v = N;
+};
+
+// Adjacent pairs of a lane: 16 bytes of columns where the halves allow it.
+int pairs_of(const rotor_head_rotation *n)
+{
+    const int most = n->interleaved || n->type == ROTOR_F32 ? 4 : 8;
+    for (int v = most; v > 1; v /= 2)
+        if (n->width / 2 % v == 0 && (n->interleaved || n->rotary / 2 % v == 0))
+            return v;
+    return 1;
+}
+
+template <typename F> void with_pairs(const rotor_head_rotation *n, F f)
+{
+    const int v = pairs_of(n);
+    if (n->interleaved) {
+        if (v == 4)
+            f(Num<4>{}, Num<1>{}, Num<1>{});
+        else if (v == 2)
+            f(Num<2>{}, Num<1>{}, Num<1>{});
+        else
+            f(Num<1>{}, Num<2>{}, Num<1>{});
+    } else {
+        if (v == 8)
+            f(Num<8>{}, Num<1>{}, Num<0>{});
+        else if (v == 4)
+            f(Num<4>{}, Num<1>{}, Num<0>{});
+        else if (v == 2)
+            f(Num<2>{}, Num<1>{}, Num<0>{});
+        else
+            f(Num<1>{}, Num<2>{}, Num<0>{});
+    }
+}
+
+int blocks_of(const rotor_head_rotation *n, int split)
+{
+    const int64_t want = ceil_div(n->batch * n->tokens * split, kWaves);
+    return (int)(want < kBlocks ? want : kBlocks);
+}
+
+bool fill(RotateArgs &a, const rotor_head_rotation *n)
+{
+    const int64_t es = elem_bytes(n->type);
+    if ((n->rotary > 0 && !n->frequencies) || (n->norm == ROTOR_NORM_NONE && (n->q_weight || n->k_weight)) ||
+        (uintptr_t)n->q_weight % (uintptr_t)es || (uintptr_t)n->k_weight % (uintptr_t)es || n->position_batch < 0 ||
+        (n->positions && ((n->position_bytes != 4 && n->position_bytes != 8) ||
+                          (uintptr_t)n->positions % (uintptr_t)n->position_bytes)))
+        return false;
+    for (int64_t i = 0; i < n->rotary / 2; ++i) {
+        if (!isfinite(n->frequencies[i]))
+            return false;
+        long double turn = (long double)n->frequencies[i] / 6.283185307179586476925286766559L;
+        turn -= floorl(turn);
+        const long double f = roundl(turn * 18446744073709551616.0L);
+        a.frequency[i] = f >= 18446744073709551616.0L ? 0 : (uint64_t)f;
+    }
+    a.weight[0] = n->q_weight;
+    a.weight[1] = n->k_weight;
+    a.positions = n->positions;
+    a.position_batch = n->position_batch;
+    a.position_bytes = n->position_bytes;
+    a.norm = n->norm;
+    a.tokens = (int)n->tokens;
+    a.heads[0] = (int)n->heads;
+    a.heads[1] = (int)n->kv_heads;
+    a.width = (int)n->width;
+    a.rotary = (int)n->rotary;
+    a.all = n->batch * n->tokens;
+    a.eps = (float)n->eps;
+    a.sums = nullptr;
+    const int lanes = (int)n->width / 2 / pairs_of(n);
+    a.team = 1;
+    while (a.team < lanes && a.team < 64)
+        a.team *= 2;
+    return true;
+}
+
+// Waves among which a token's heads are split: all of a token's in one wave
+// compute its angles once, but few tokens leave CUs without work.
+int split_of(int64_t all, int turns)
+{
+    const int64_t want = all > 0 ? 8192 / all : 1;
+    return (int)(want < 1 ? 1 : want > turns ? turns : want);
+}
+
+}  // namespace
+}  // namespace rotor
+
+using namespace rotor;
+
+extern "C" {
+
+int32_t rotor_head_norm_rotate(const rotor_head_rotation *how, const rotor_heads *q, const rotor_heads *k,
+                               const rotor_heads *q_out, const rotor_heads *k_out, void *stream)
+{
+    RotateArgs a;
+    if (!rotation_ok(how) || !fill(a, how) || !head_rows_ok(q, how, how->heads, a.in[0]) ||
+        !head_rows_ok(k, how, how->kv_heads, a.in[1]) || !head_rows_ok(q_out, how, how->heads, a.out[0]) ||
+        !head_rows_ok(k_out, how, how->kv_heads, a.out[1]))
+        return ROTOR_EINVAL;
+    a.grad[0] = a.grad[1] = HeadRows{nullptr, 0, 0, 0};
+    if (a.all == 0)
+        return ROTOR_OK;
+    a.turns = (int)ceil_div(a.heads[0] + a.heads[1], 64 / a.team);
+    a.split = split_of(a.all, a.turns);
+    const int64_t blocks = ceil_div(a.all * a.split, kWaves);
+    if (!grid_ok(blocks))
+        return ROTOR_EINVAL;
+    (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
+    with_type(how->type, [&](auto e) {
+        typedef typename decltype(e)::T T;
+        with_pairs(how, [&](auto v, auto n, auto inter) {
+            rotate_kernel<T, decltype(v)::v, decltype(n)::v, decltype(inter)::v == 1>
+                <<<grid_of(blocks), kThreads, 0, (hipStream_t)stream>>>(a);
+        });
+    });
+    return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+}
+
+int32_t rotor_head_norm_rotate_workspace_bytes(const rotor_head_rotation *how, uint64_t *bytes)
+{
+    if (!bytes || !rotation_ok(how))
+        return ROTOR_EINVAL;
+    *bytes = how->norm == ROTOR_NORM_NONE ? 0 : (uint64_t)kBlocks * 2 * how->width * 4;
+    return ROTOR_OK;
+}
+
+int32_t rotor_head_norm_rotate_backward(const rotor_head_rotation *how, const rotor_heads *dq_out,
+                                        const rotor_heads *dk_out, const rotor_heads *q, const rotor_heads *k,
+                                        const rotor_heads *dq, const rotor_heads *dk, void *d_dq_weight,
+                                        void *d_dk_weight, void *d_work, uint64_t work_bytes, void *stream)
+{
+    RotateArgs a;
+    uint64_t need = 0;
+    if (!rotation_ok(how) || !fill(a, how) ||
+        rotor_head_norm_rotate_workspace_bytes(how, &need) != ROTOR_OK)
+        return ROTOR_EINVAL;
+    const int64_t es = elem_bytes(how->type);
+    a.in[0] = a.in[1] = HeadRows{nullptr, 0, 0, 0};
+    if (!head_rows_ok(dq_out, how, how->heads, a.grad[0]) || !head_rows_ok(dk_out, how, how->kv_heads, a.grad[1]) ||
+        (how->norm != ROTOR_NORM_NONE &&
+         (!head_rows_ok(q, how, how->heads, a.in[0]) || !head_rows_ok(k, how, how->kv_heads, a.in[1]))) ||
+        !head_rows_ok(dq, how, how->heads, a.out[0]) || !head_rows_ok(dk, how, how->kv_heads, a.out[1]) ||
+        (uintptr_t)d_dq_weight % (uintptr_t)es || (uintptr_t)d_dk_weight % (uintptr_t)es ||
+        (how->norm == ROTOR_NORM_NONE && (d_dq_weight || d_dk_weight)))
+        return ROTOR_EINVAL;
+    const bool sums = d_dq_weight || d_dk_weight;
+    if (sums && (!d_work || (uintptr_t)d_work % 16 || work_bytes < need))
+        return ROTOR_EINVAL;
+    const int teams = 64 / a.team, most = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
+    a.turns = (int)ceil_div(most, teams);
+    a.split = split_of(a.all, a.turns);
+    a.sums = sums ? (float *)d_work : nullptr;
+    const int blocks = blocks_of(how, a.split);
+    (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
+    with_type(how->type, [&](auto e) {
+        typedef typename decltype(e)::T T;
+        if (blocks > 0)
+            with_pairs(how, [&](auto v, auto n, auto inter) {
+                rotate_back_kernel<T, decltype(v)::v, decltype(n)::v, decltype(inter)::v == 1>
+                    <<<dim3((uint32_t)blocks), kThreads, 0, (hipStream_t)stream>>>(a);
+            });
+        if (sums)
+            join_kernel<T><<<dim3((uint32_t)ceil_div(how->width, 16), 2), 256, 0, (hipStream_t)stream>>>(
+                a.sums, blocks, a.width, (T *)d_dq_weight, (T *)d_dk_weight);
+    });
+    return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
+}
+
+}  // extern "C"

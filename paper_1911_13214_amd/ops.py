@@ -1,12 +1,16 @@
 """Operators of a language-model chain's stages, on the C ABI in
 include/rotor.h: counter-based dropout, embedding lookup, the residual seam
 between two blocks (norms, gate, residual scale), the cross entropy over a
-vocabulary without its logits, and their gradients.
+vocabulary without its logits, norms of query and key heads with their rotation
+by position, attention under a window, and their gradients; and that attention
+for one token against a cache.
 
 Argument checks, allocation and marshalling only: every operator runs in the
 library's HIP kernels.  Tensors are CUDA tensors of one device and, where
 floating-point, of one type (float32, bfloat16 or float16); a matrix may have
-any row pitch, its last dimension is dense.  Calls enqueue on ``stream``
+any row pitch, its last dimension is dense, and a tensor of heads ([tokens,
+heads, width] or [batch, tokens, heads, width]) any strides before it.  Calls
+enqueue on ``stream``
 (default: the current one) and return at once; a tensor that was made on
 another stream is the caller's to order and to keep (``record_stream``), and
 so is the order of a result's use on another one.  What a call allocates,
@@ -27,6 +31,8 @@ from . import rotor
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 NORM_MAX_COLS = 16384
+ROTATE_MAX_WIDTH = 256
+ATTENTION_MAX_WIDTH = 128
 
 
 class _Norm(ctypes.Structure):
@@ -406,3 +412,315 @@ def linear_cross_entropy_backward(h, w, targets, lse, grad_loss, ignore=-100, *,
           targets.data_ptr(), ignore, lse, grad_loss, _ptr(dh), cols, _ptr(dw), cols, aligned, work.data_ptr(),
           work.numel())
     return dh, dw
+
+
+# ---- heads: norms and rotation -------------------------------------------------------------
+
+def _heads(t, what, like=None, dims=(3, 4)):
+    """A tensor of heads, checked, as the C ABI takes it: strides in elements
+    of [batch, tokens, heads, width], 0 where there is one of something."""
+    _cuda(t, what)
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{what} must be {like.dtype} on {like.device}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) not in dims:
+        raise ValueError(f"{what} must be [tokens, heads, width] or [batch, tokens, heads, width]" if 4 in dims else
+                         f"{what} must be [batch, heads, width]")
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError(f"{what} must have a dense last dimension")
+    return rotor.Heads(t.data_ptr(), *((0,) * (4 - len(shape)) + tuple(0 if n == 1 else s for n, s in
+                                                                   zip(shape[:-1], stride[:-1]))))
+
+
+def _no_overlap(t, what):
+    """A result's elements must lie in places of their own."""
+    at = 1
+    for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda x: x[1]):
+        if s < at:
+            raise ValueError(f"{what} has elements that overlap")
+        at = n * s
+    return t
+
+
+@functools.lru_cache(maxsize=256)
+def _frequencies(rotary, base, given):
+    f = given if given is not None else tuple(base ** (-2.0 * i / rotary) for i in range(rotary // 2))
+    if len(f) != rotary // 2:
+        raise ValueError(f"{rotary // 2} frequencies are needed for {rotary} rotated columns, not {len(f)}")
+    if not all(-float("inf") < x < float("inf") for x in f):
+        raise ValueError("frequencies must be finite")
+    return (ctypes.c_double * max(1, len(f)))(*f)
+
+
+def _index(t, what, device):
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int64, torch.int32) or t.device != device:
+        raise ValueError(f"{what} must be int64 or int32 on {device}")
+    return t.element_size()
+
+
+def _rotation(q, k, norm, q_weight, k_weight, eps, positions, rotary, base, frequencies, interleaved):
+    """The C ABI's description of a rotation, checked against q and k."""
+    code = _typed(q, "q")
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {tuple(NORMS)}")
+    if q.dim() not in (3, 4):
+        raise ValueError("q must be [tokens, heads, width] or [batch, tokens, heads, width]")
+    shape = q.shape
+    width = shape[-1]
+    if not (2 <= width <= ROTATE_MAX_WIDTH and width % 2 == 0):
+        raise ValueError(f"the width must be even, from 2 to {ROTATE_MAX_WIDTH}")
+    if shape[-2] < 1:
+        raise ValueError("q has no heads")
+    rotary = width if rotary is None else rotary
+    if not (0 <= rotary <= width and rotary % 2 == 0):
+        raise ValueError(f"rotary must be even, from 0 to {width}")
+    if not eps >= 0.0:
+        raise ValueError("eps must not be negative")
+    if not base > 0.0:
+        raise ValueError("base must be positive")
+    if k is not None and (_cuda(k, "k").dim() != len(shape) or k.shape[:-2] != shape[:-2] or k.shape[-1] != width or
+                          k.dtype != q.dtype or k.device != q.device):
+        raise ValueError(f"k must be {q.dtype} on {q.device}, shaped as q but for its heads")
+    if k is None and k_weight is not None:
+        raise ValueError("k_weight without k")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if norm == "none":
+            raise ValueError(f"{name} without a norm")
+        if not _like(w, q, name, (width,)).is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    batch, tokens = shape[0] if len(shape) == 4 else 1, shape[-3]
+    n = rotor.Rotation(code, NORMS[norm], bool(interleaved), 8, batch, tokens, shape[-2], 0 if k is None else k.shape[-2],
+                  width, rotary, eps, None, None, 0, _ptr(q_weight), _ptr(k_weight))
+    # (kept alive by the cache, and by this frame's caller through n)
+    n.keep = _frequencies(rotary, base, None if frequencies is None else tuple(map(float, frequencies)))
+    n.frequencies = ctypes.addressof(n.keep)
+    if positions is not None:
+        n.position_bytes = _index(positions, "positions", q.device)
+        if positions.shape != shape[:-2] and positions.shape != shape[-3:-2]:
+            raise ValueError(f"positions must have shape {tuple(shape[:-2])} or ({tokens},)")
+        if tokens > 1 and positions.stride(-1) != 1:
+            raise ValueError("positions must have a dense last dimension")
+        n.positions = positions.data_ptr()
+        n.position_batch = positions.stride(0) if positions.dim() == 2 and batch > 1 else 0
+    return n
+
+
+def head_norm_rotate(q, k=None, *, norm="rms", q_weight=None, k_weight=None, eps=1e-5, positions=None, rotary=None,
+                     base=10000.0, frequencies=None, interleaved=False, out=None, stream=None):
+    """Query and key heads, each normed ("rms", "layer" or "none") and
+    multiplied by a weight [width] or nothing, then rotated by their position:
+    returns (q', k'), k' None without ``k``.
+
+    ``q`` and ``k``: [tokens, heads, width] or [batch, tokens, heads, width], any
+    strides, each with its number of heads.  ``positions``: int64 or int32,
+    shaped as the leading dimensions or [tokens] (default 0, 1, ...), negative
+    ones turn the other way.  The first ``rotary`` columns (default all) turn in
+    pairs (i, i + rotary / 2), or (2i, 2i + 1) if ``interleaved``, by
+    position * frequency; ``frequencies``: rotary / 2 numbers, radians a position
+    (default base ** (-2i / rotary)).  ``out``: (q', k') to write into, which may
+    be (q, k)."""
+    if stream is not None:
+        return _on(stream, head_norm_rotate, q, k, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps,
+                   positions=positions, rotary=rotary, base=base, frequencies=frequencies, interleaved=interleaved,
+                   out=out)
+    n = _rotation(q, k, norm, q_weight, k_weight, eps, positions, rotary, base, frequencies, interleaved)
+    if out is None:
+        y, z = _empty(q), None if k is None else _empty(k)
+    else:
+        y, z = out
+        if (z is None) != (k is None):
+            raise ValueError("out must have a place for each of q and k")
+        _no_overlap(_like(y, q, "out"), "out")
+        if z is not None:
+            _no_overlap(_like(z, k, "out"), "out")
+    _call("rotor_head_norm_rotate", q.device, n, _heads(q, "q"), k if k is None else _heads(k, "k"), _heads(y, "out"),
+          k if k is None else _heads(z, "out"))
+    return y, z
+
+
+def head_norm_rotate_backward(dq, dk, q, k=None, *, norm="rms", q_weight=None, k_weight=None, eps=1e-5, positions=None,
+                              rotary=None, base=10000.0, frequencies=None, interleaved=False, stream=None):
+    """Gradients of head_norm_rotate's arguments from those of its results, as
+    a dict: "q", "k" and the weights that are given.  ``q`` and ``k`` are what
+    the forward took; without a norm only their shapes count."""
+    if stream is not None:
+        return _on(stream, head_norm_rotate_backward, dq, dk, q, k, norm=norm, q_weight=q_weight, k_weight=k_weight,
+                   eps=eps, positions=positions, rotary=rotary, base=base, frequencies=frequencies,
+                   interleaved=interleaved)
+    n = _rotation(q, k, norm, q_weight, k_weight, eps, positions, rotary, base, frequencies, interleaved)
+    if (dk is None) != (k is None):
+        raise ValueError("dk goes with k")
+    _like(dq, q, "dq")
+    g = {"q": _empty(q)}
+    if k is not None:
+        _like(dk, k, "dk")
+        g["k"] = _empty(k)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            g[name] = _empty(w)
+    need = ctypes.c_uint64()
+    rotor._check(_entry("rotor_head_norm_rotate_workspace_bytes")(ctypes.byref(n), ctypes.byref(need)),
+                 "rotor_head_norm_rotate_workspace_bytes")
+    work = _scratch(need.value, q)
+    _call("rotor_head_norm_rotate_backward", q.device, n, _heads(dq, "dq"), k if k is None else _heads(dk, "dk"),
+          _heads(q, "q"), k if k is None else _heads(k, "k"), _heads(g["q"], "dq"),
+          k if k is None else _heads(g["k"], "dk"), _ptr(g.get("q_weight")), _ptr(g.get("k_weight")), work.data_ptr(),
+          work.numel())
+    return g
+
+
+# ---- attention -------------------------------------------------------------------------------
+
+def _attention(q, k, v, window, sinks, scale, positions, lengths, shape):
+    """The C ABI's description of an attention, checked: ``shape`` is (batch,
+    tokens, heads, width) of q."""
+    code = _typed(q, "q")
+    batch, tokens, heads, width = shape
+    if width % 8 or not 8 <= width <= ATTENTION_MAX_WIDTH:
+        raise ValueError(f"the width must be a multiple of 8, from 8 to {ATTENTION_MAX_WIDTH}")
+    if _cuda(k, "k").dim() != 4 or k.shape[0] != batch or k.shape[3] != width or k.shape[2] < 1 or \
+            heads % k.shape[2] or heads < 1:
+        raise ValueError(f"k must be [{batch}, keys, heads, {width}], its heads dividing the {heads} of q")
+    _like(k, q, "k", k.shape)
+    _like(v, q, "v", k.shape)
+    if window is not None and window < 1:
+        raise ValueError("window must be at least 1, or None")
+    if sinks < 0:
+        raise ValueError("sinks must not be negative")
+    scale = width ** -0.5 if scale is None else scale
+    if not 0.0 < scale <= 1e30:
+        raise ValueError("scale must be positive")
+    n = rotor.Attention(code, 8, 8, 0, batch, tokens, k.shape[1], heads, k.shape[2], width, window or 0, sinks, scale,
+                   None, None)
+    for name, t in (("positions", positions), ("lengths", lengths)):
+        if t is None:
+            continue
+        size = _index(t, name, q.device)
+        if t.shape != (batch,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous, of shape ({batch},)")
+        if name == "positions":
+            n.position_bytes, n.positions = size, t.data_ptr()
+        else:
+            n.length_bytes, n.lengths = size, t.data_ptr()
+    return n
+
+
+def _batched(t, what):
+    """[batch, tokens, heads, width], of which the batch may be left out."""
+    if _cuda(t, what).dim() not in (3, 4):
+        raise ValueError(f"{what} must be [tokens, heads, width] or [batch, tokens, heads, width]")
+    return t if t.dim() == 4 else t.unsqueeze(0)
+
+
+def _aligned(t, what, like=None, dims=(3, 4)):
+    """Heads that start 16-byte aligned."""
+    h, es = _heads(t, what, like, dims), t.element_size()
+    if t.numel() and (h.p % 16 or (h.batch | h.token | h.head) * es % 16):
+        raise ValueError(f"the heads of {what} must start 16-byte aligned")
+    return h
+
+
+def window_attention(q, k, v, *, window=None, sinks=0, scale=None, positions=None, lengths=None, stats=True,
+                     stream=None):
+    """Causal attention of the last ``window`` keys (its own with them; None:
+    all) and of the first ``sinks`` ones: returns (out, lse), out shaped as q,
+    lse float32 [..., tokens, heads] (None unless ``stats``; the backward needs
+    it).
+
+    ``q``: [batch, tokens, heads, width], ``k``, ``v``: [batch, keys, kv_heads,
+    width] (all without the batch if there is one sequence), any strides of 16
+    bytes; heads / kv_heads adjacent query heads share a key head.  Row i of a
+    sequence stands at positions[b] + i (int32 or int64 [batch]; default
+    keys - tokens) and sees the keys up to its position and below lengths[b]
+    (default: keys).  Rows at negative positions or past the length see nothing:
+    out is 0, lse -inf, and nothing that q, k or v hold there is used.
+    ``scale``: default width ** -0.5."""
+    if stream is not None:
+        return _on(stream, window_attention, q, k, v, window=window, sinks=sinks, scale=scale, positions=positions,
+                   lengths=lengths, stats=stats)
+    flat = q
+    q, k, v = _batched(q, "q"), _batched(k, "k"), _batched(v, "v")
+    n = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
+    out = _empty(flat)
+    lse = q.new_empty(flat.shape[:-1], dtype=torch.float32) if stats else None
+    need = ctypes.c_uint64()
+    rotor._check(_entry("rotor_window_attention_workspace_bytes")(ctypes.byref(n), 0, ctypes.byref(need)),
+                 "rotor_window_attention_workspace_bytes")
+    work = _scratch(need.value, q) if need.value else None
+    _call("rotor_window_attention", q.device, n, _aligned(q, "q"), _aligned(k, "k"), _aligned(v, "v"),
+          _heads(out, "out"), _ptr(lse), _ptr(work), need.value)
+    return out, lse
+
+
+def window_attention_backward(dout, q, k, v, out, lse, *, window=None, sinks=0, scale=None, positions=None,
+                              lengths=None, stream=None):
+    """Gradients (dq, dk, dv) from that of out; ``out`` and ``lse`` are what the
+    forward returned.  Bit for bit the same on every call."""
+    if stream is not None:
+        return _on(stream, window_attention_backward, dout, q, k, v, out, lse, window=window, sinks=sinks, scale=scale,
+                   positions=positions, lengths=lengths)
+    dq, dk, dv = _empty(q), _empty(k), _empty(v)
+    _like(dout, q, "dout")
+    _like(out, q, "out")
+    if not isinstance(lse, torch.Tensor) or lse.dtype != torch.float32 or lse.device != q.device or \
+            lse.shape != q.shape[:-1] or not lse.is_contiguous():
+        raise ValueError("lse must be what window_attention returned")
+    q, k, v = _batched(q, "q"), _batched(k, "k"), _batched(v, "v")
+    n = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
+    need = ctypes.c_uint64()
+    rotor._check(_entry("rotor_window_attention_backward_workspace_bytes")(ctypes.byref(n), ctypes.byref(need)),
+                 "rotor_window_attention_backward_workspace_bytes")
+    work = _scratch(need.value, q)
+    _call("rotor_window_attention_backward", q.device, n, _aligned(dout, "dout"), _aligned(q, "q"),
+          _aligned(k, "k"), _aligned(v, "v"), _aligned(out, "out"), lse.data_ptr(), _heads(dq, "dq"),
+          _heads(dk, "dk"), _heads(dv, "dv"), work.data_ptr(), work.numel())
+    return dq, dk, dv
+
+
+def window_attention_step(q, k, v, k_cache, v_cache, positions, *, window=None, sinks=0, scale=None, ring=False,
+                          out=None, stream=None):
+    """One token of each sequence: writes its key and value, ``k`` and ``v``
+    [batch, kv_heads, width], into the caches [batch, slots, kv_heads, width] at
+    positions[b] (int32 or int64), and returns its query's attention [batch,
+    heads, width], as window_attention's with that position.
+
+    ``ring``: the first ``sinks`` positions keep their slots and later ones go
+    round the others, slot sinks + (position - sinks) % (slots - sinks), at least
+    ``window`` of them.  A negative position is a place without a token: its
+    result is 0; one past the cache gives NaN; neither writes to the caches.
+    Slots that a token does not see may hold anything."""
+    if stream is not None:
+        return _on(stream, window_attention_step, q, k, v, k_cache, v_cache, positions, window=window, sinks=sinks,
+                   scale=scale, ring=ring, out=out)
+    if _cuda(q, "q").dim() != 3:
+        raise ValueError("q must be [batch, heads, width]")
+    batch, heads, width = q.shape
+    n = _attention(q, k_cache, v_cache, window, sinks, scale, positions, None, (batch, 1, heads, width))
+    slots = k_cache.shape[1]
+    if positions is None or slots < 1:
+        raise ValueError("a position for each sequence and at least one slot are needed")
+    if ring and (window is None or sinks + window > slots):
+        raise ValueError(f"a ring of {slots} slots must hold its sinks and a window")
+    shape = (batch, k_cache.shape[2], width)
+    _like(k, q, "k", shape)
+    _like(v, q, "v", shape)
+    _no_overlap(k_cache, "k_cache")
+    _no_overlap(v_cache, "v_cache")
+    y = _out(out, q, "out")
+    if out is not None:
+        _no_overlap(y, "out")
+    need = ctypes.c_uint64()
+    rotor._check(_entry("rotor_window_attention_workspace_bytes")(ctypes.byref(n), 1, ctypes.byref(need)),
+                 "rotor_window_attention_workspace_bytes")
+    work = _scratch(need.value, q) if need.value else None
+
+    def one(t, what):  # [batch, heads, width]: strides of batch and head
+        h = _aligned(t, what, q, (3,))
+        return rotor.Heads(h.p, h.token, 0, h.head)
+
+    _call("rotor_window_attention_step", q.device, n, one(q, "q"), one(k, "k"), one(v, "v"),
+          _aligned(k_cache, "k_cache"), _aligned(v_cache, "v_cache"), bool(ring), one(y, "out"), _ptr(work),
+          need.value)
+    return y

@@ -28,9 +28,28 @@ N_ROWS = 6
 MAX_L = 32767
 MAX_L_RECONSTRUCT = 8191
 
-# name -> (restype, argtypes) of every function include/rotor.h declares
 _i32, _i64, _u64, _vp, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_double
 _P = ctypes.POINTER
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("p", _vp), ("batch", _i64), ("token", _i64), ("head", _i64)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("type", _i32), ("norm", _i32), ("interleaved", _i32), ("position_bytes", _i32), ("batch", _i64),
+                ("tokens", _i64), ("heads", _i64), ("kv_heads", _i64), ("width", _i64), ("rotary", _i64),
+                ("eps", _f64), ("frequencies", _vp), ("positions", _vp), ("position_batch", _i64), ("q_weight", _vp),
+                ("k_weight", _vp)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [("type", _i32), ("position_bytes", _i32), ("length_bytes", _i32), ("reserved", _i32), ("batch", _i64),
+                ("tokens", _i64), ("keys", _i64), ("heads", _i64), ("kv_heads", _i64), ("width", _i64),
+                ("window", _i64), ("sinks", _i64), ("scale", _f64), ("positions", _vp), ("lengths", _vp)]
+
+
+# name -> (restype, argtypes) of every function include/rotor.h declares
 SIGNATURES = {
     "rotor_version": (_i32, []),
     "rotor_status_string": (ctypes.c_char_p, [_i32]),
@@ -62,6 +81,16 @@ SIGNATURES = {
     "rotor_xent": (_i32, [_i32, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _u64, _vp]),
     "rotor_xent_backward": (_i32, [_i32, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp,
                                    _i64, _i32, _vp, _u64, _vp]),
+    # (structures of a binding, which passes them by reference)
+    "rotor_head_norm_rotate": (_i32, [_P(Rotation)] + [_P(Heads)] * 4 + [_vp]),
+    "rotor_head_norm_rotate_workspace_bytes": (_i32, [_P(Rotation), _P(_u64)]),
+    "rotor_head_norm_rotate_backward": (_i32, [_P(Rotation)] + [_P(Heads)] * 6 + [_vp, _vp, _vp, _u64, _vp]),
+    "rotor_window_attention_workspace_bytes": (_i32, [_P(Attention), _i32, _P(_u64)]),
+    "rotor_window_attention": (_i32, [_P(Attention)] + [_P(Heads)] * 4 + [_vp, _vp, _u64, _vp]),
+    "rotor_window_attention_backward_workspace_bytes": (_i32, [_P(Attention), _P(_u64)]),
+    "rotor_window_attention_backward": (_i32, [_P(Attention)] + [_P(Heads)] * 5 + [_vp] + [_P(Heads)] * 3 +
+                                        [_vp, _u64, _vp]),
+    "rotor_window_attention_step": (_i32, [_P(Attention)] + [_P(Heads)] * 5 + [_i32, _P(Heads), _vp, _u64, _vp]),
 }
 
 KERNEL_CLASSES = ("leaf", "diag", "middle", "edge", "prep")
