@@ -50,7 +50,7 @@ struct Attention {
     int rows;            // tokens * group
     int window, sinks;   // window at most kFar
     float scale, c;      // c = scale log2(e)
-    uint32_t magic;      // ceil(2^32 / group)
+    uint64_t magic40;    // ceil(2^40 / group)
     int parts;           // of the keys (forward) or of the rows (gradients of keys)
     int ring;            // slots past the first ones, 0: the cache is linear
     // workspace
@@ -90,6 +90,10 @@ template <> struct Frag<float> {
         return c;
     }
 };
+
+// row / group without a division: exact for rows below 2^23 and groups up to
+// 2^15.
+__device__ inline int token_of(const Attention &a, int row) { return (int)((uint64_t)(uint32_t)row * a.magic40 >> 40); }
 
 // Row of a result's register e for a lane of half h.
 __device__ constexpr int row_of(int e, int h) { return 8 * (e / 4) + 4 * h + e % 4; }
@@ -203,16 +207,16 @@ template <typename T, int NB, int ROWS, int WAVES> struct Loader {
     __device__ void load_rows(char *lds, const char *p, const Attention &a, const Heads &h, int lane, int r0, int from,
                               int to) const
     {
-        const int t0 = r0 / a.group, g0 = r0 - t0 * a.group;
+        const int t0 = token_of(a, r0), g0 = r0 - t0 * a.group;
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(p + t0 * h.token), 0, 0x7FFFFFFF, 0x00020000);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int row = row0 + i * kAtOnce, c = piece(lane, row), x = g0 + row;
-            const int t = a.group == 1 ? x : (int)__umulhi((uint32_t)x, a.magic), g = x - t * a.group;
+            const int t = token_of(a, x), g = x - t * a.group;
             const uint32_t off = (uint32_t)t * (uint32_t)h.token + (uint32_t)g * (uint32_t)h.head + c * 16;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rsrc, (lds_ptr)(lds + first + i * 1024), 16,
-                row >= from && row < to && c * Frag<T>::N < a.width ? off : 0x80000000u, 0, 0, 0);
+            const bool in = (row >= from) & (row < to) & (c * Frag<T>::N < a.width);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + i * 1024), 16,
+                                                     in ? off : 0x80000000u, 0, 0, 0);
         }
     }
 };
@@ -462,7 +466,7 @@ inline void fill(Attention &a, const rotor_attention *n)
     a.sinks = a.window >= a.keys ? 0 : n->sinks < n->keys ? (int)n->sinks : a.keys;
     a.scale = (float)n->scale;
     a.c = (float)(n->scale * 1.4426950408889634);
-    a.magic = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
+    a.magic40 = (((uint64_t)1 << 40) + a.group - 1) / a.group;
     a.parts = 1;
 }
 

@@ -232,6 +232,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)stats[i & 1][wave], 4, lane * 4, 0, 0, 0);
         }
     };
+    // rows that see any of the wave's keys, and those that see all of them
+    const int64_t gw = a.group, off = span.offset;
+    const bool first = jw + 31 < a.sinks;
+    const int some0 = (int)max(live0, (jw - off) * gw);
+    const int some1 = (int)(jw < a.sinks ? live1 : min(live1, (jw + 31 + (int64_t)a.window - off) * gw));
+    const int all0 = (int)max(live0, (jw + 31 - off) * gw);
+    const int all1 = (int)(first ? live1 : min(live1, max((int64_t)0, (jw + (int64_t)a.window - off) * gw)));
     auto pass = [&](auto apart) {
         constexpr bool kApart = decltype(apart)::value;
         if (i0 < i1)
@@ -243,12 +250,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
 #pragma unroll 1
             for (int u = 0; u < kStepRows / 32; ++u) {
                 const int r = i * kStepRows + u * 32;
-                int lo, hi;
-                if (r >= a.rows || !span.positions(r / a.group, min(a.rows - 1, r + 31) / a.group, lo, hi) ||
-                    jw > hi || (jw >= a.sinks && jw + 31 < lo - a.window + 1))
+                if (r + 32 <= some0 || r >= some1)
                     continue;
-                const bool all = r >= live0 && r + 32 <= live1 && jw + 31 <= lo &&
-                                 (jw + 31 < a.sinks || jw >= hi - a.window + 1);
+                const bool all = r >= all0 && r + 32 <= all1;
                 const char *qt = tiles[i & 1][0] + u * 32 * S::kRow, *dt = tiles[i & 1][1] + u * 32 * S::kRow;
                 const float *st = &stats[i & 1][0][u * 32];
                 f32x16 s = product<T, NB>(qt, rd, kf), ds = product<T, NB>(dt, rd, vf);
@@ -277,6 +281,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
                     }
                 }
                 if (!all) {
+                    asm volatile("");  // a branch: few tiles need it
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         typedef int i32x4 __attribute__((ext_vector_type(4)));
