@@ -99,19 +99,26 @@ __device__ inline int token_of(const Attention &a, int row) { return (int)((uint
 __device__ constexpr int row_of(int e, int h) { return 8 * (e / 4) + 4 * h + e % 4; }
 
 // Tiles in LDS: rows of kRow bytes in pieces of 16, which change places by the
-// row: piece c of row r lies at c ^ turn(r).  turn is even, so that pairs of
-// pieces stay pairs; the eight rows that a quarter wave reads a piece of, and
-// the four rows that a transposing read takes 32 bytes of, lie in different
-// banks.
+// row: piece c of row r lies at c ^ turn(r), so that what is read at once, 256
+// bytes, lies in different banks: a piece of 16 rows, 64 bytes of four rows (the
+// transposing reads), or in 32 bits 128 bytes of rows four apart.  (attention of
+// 16384 tokens, 32 heads on 8, 128 wide, bf16: 2.15 ms with half the turns, two
+// rows to a bank.)
 // NB: blocks of 32 columns that the width fills.
 template <typename T, int NB> struct Shape {
     static constexpr int kBlocks = NB == 3 ? 4 : NB;
     static constexpr int kRow = kBlocks * 32 * (int)sizeof(T);
     static constexpr int kPieces = kRow / 16;
-    static constexpr int kPerBanks = kRow >= 256 ? 1 : 256 / kRow;  // rows that fill the banks
     static constexpr int NK = NB * (int)sizeof(T);                  // fragments of a row: 32 bytes each
     static constexpr int kGroups = 32 / (2 * Frag<T>::N);           // fragments of 32 summed rows
-    static __device__ int turn(int row) { return 2 * (row / kPerBanks % (8 / kPerBanks)); }
+    static __device__ int turn(int row)
+    {
+        if (sizeof(T) == 4)
+            return (row / 4 % 2) << 3 | (row % 4) << 1 | row / 8 % 2;
+        if (kRow == 128)
+            return (row / 2 % 2) << 2 | row / 4 % 4;
+        return (row % 4) << 2 | row / 4 % 4;
+    }
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -163,14 +170,16 @@ template <typename T, int NB> struct Reader {
     __device__ F column(const char *tile, int g, int b) const
     {
         if constexpr (sizeof(T) == 2) {
-            const char *p = tile + (cross[0] ^ (b * 64)) + g * 16 * S::kRow;
-            return __builtin_bit_cast(F, __builtin_shufflevector(turned(p), turned(p + 8 * S::kRow), 0, 1, 2, 3, 4, 5,
+            // (eight rows on, a piece's place differs by 2)
+            const char *const p = tile + (cross[0] ^ (b * 64)), *const q = tile + (cross[0] ^ (b * 64) ^ 32);
+            return __builtin_bit_cast(F, __builtin_shufflevector(turned(p + g * 16 * S::kRow),
+                                                                 turned(q + (g * 16 + 8) * S::kRow), 0, 1, 2, 3, 4, 5,
                                                                  6, 7));
         } else {
             F f;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                f[e] = *(const float *)(tile + (cross[e] ^ (b * 128)) + g * 8 * S::kRow);
+                f[e] = *(const float *)(tile + (cross[e] ^ (b * 128) ^ (g % 2 * 16)) + g * 8 * S::kRow);
             return f;
         }
     }
