@@ -27,7 +27,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kTileRows = kWaves * 32;  // rows of a workgroup, 32 a wave
-constexpr int kTileKeys = 64;           // keys in LDS at a time
+constexpr int kTileKeys = 32;           // keys of a step
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.69314718055994531f;
@@ -133,6 +133,30 @@ __device__ inline Turned turned(const char *lds)
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Turned *)lds);
 }
 
+// Orders what follows in its basic block: N times a matrix instruction with
+// VALU others and EXP exponentials beside it.
+template <int N, int VALU, int EXP> __device__ inline void beside()
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        if (VALU)
+            __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
+        if (EXP)
+            __builtin_amdgcn_sched_group_barrier(0x400, EXP, 0);
+    }
+}
+template <int N> __device__ inline void reads() { __builtin_amdgcn_sched_group_barrier(0x100, N, 0); }
+
+// Waits until at most LEFT of this wave's loads into LDS are on their way, and
+// for all waves.
+template <int LEFT> __device__ inline void step_barrier()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // Waits for this wave's loads into LDS and for all waves.
 __device__ inline void tile_barrier()
 {
@@ -203,14 +227,15 @@ template <typename T, int NB, int ROWS, int WAVES> struct Loader {
             at[i] = c * Frag<T>::N < width ? (uint32_t)row * (uint32_t)stride + c * 16 : 0x80000000u;
         }
     }
-    // `rows`: of the tile that exist
-    __device__ void load(char *lds, const char *p, int rows) const
+    // `rows`: of the tile that exist, `row`: bytes of one.  What lies past them is
+    // past the buffer's end (rows one place apart are all the same: they all exist).
+    __device__ void load(char *lds, const char *p, int rows, uint32_t stride, int row) const
     {
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, 0x7FFFFFFF, 0x00020000);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)p, 0, rows <= 0 ? 0 : (rows < ROWS ? rows - 1 : ROWS - 1) * stride + row, 0x00020000);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + i * 1024), 16,
-                                                     row0 + i * kAtOnce < rows ? at[i] : 0x80000000u, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + i * 1024), 16, at[i], 0, 0, 0);
     }
     // Rows of (token, head of the group): rows r0 + [from, to) of the tile exist.
     __device__ void load_rows(char *lds, const char *p, const Attention &a, const Heads &h, int lane, int r0, int from,
@@ -231,7 +256,27 @@ template <typename T, int NB, int ROWS, int WAVES> struct Loader {
 };
 
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ inline float other_half(float v) { return __shfl_xor(v, 32); }
+// Over a lane and the one 32 away: the maximum, the sum.
+struct Both {
+    float low, high;
+};
+__device__ inline Both halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v),
+                                                    false, false);
+    const uint32_t low = r[0], high = r[1];
+    return Both{__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+__device__ inline float halves_max(float v)
+{
+    const Both b = halves(v);
+    return fmaxf(b.low, b.high);
+}
+__device__ inline float halves_sum(float v)
+{
+    const Both b = halves(v);
+    return b.low + b.high;
+}
 
 // Registers [g * 2N / 2 ...) of a 32 x 32 result as the fragment of its summed
 // rows, rounded to the type.
@@ -268,17 +313,58 @@ __device__ inline f32x16 product(const char *tile, const Reader<T, NB> &rd,
     return s;
 }
 
-// acc[column][lane] += sum over 32 rows of tile[row][column] * p[row][lane]
+// The same in two parts: fragments out of LDS, whose way takes longer than four
+// products, and the products.
 template <typename T, int NB>
-__device__ inline void add_rows(f32x16 (&acc)[NB], const char *tile, const Reader<T, NB> &rd, const f32x16 &p)
+__device__ inline void fetch_rows(const char *tile, const Reader<T, NB> &rd, typename Frag<T>::F (&f)[Shape<T, NB>::NK])
 {
 #pragma unroll
-    for (int g = 0; g < Shape<T, NB>::kGroups; ++g) {
-        const typename Frag<T>::F f = packed<T>(p, g);
+    for (int k = 0; k < Shape<T, NB>::NK; ++k)
+        f[k] = rd.row(tile, k);
+}
+template <typename T, int NK>
+__device__ inline void multiply(f32x16 &s, const typename Frag<T>::F (&a)[NK], const typename Frag<T>::F (&b)[NK])
+{
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        s[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k)
+        s = Frag<T>::mma(a[k], b[k], s);
+}
+
+// 32 rows of a result as the operand of the next product, rounded.
+template <typename T, int NB> struct Packed {
+    typename Frag<T>::F f[Shape<T, NB>::kGroups];
+    __device__ Packed() = default;
+    __device__ Packed(const f32x16 &p)
+    {
+#pragma unroll
+        for (int g = 0; g < Shape<T, NB>::kGroups; ++g)
+            f[g] = packed<T>(p, g);
+    }
+    // Has them computed here, not where they are used.
+    __device__ void pin()
+    {
+#pragma unroll
+        for (int g = 0; g < Shape<T, NB>::kGroups; ++g) {
+            typedef int I __attribute__((ext_vector_type(4)));
+            I x = __builtin_bit_cast(I, f[g]);
+            asm volatile("" : "+v"(x));
+            f[g] = __builtin_bit_cast(typename Frag<T>::F, x);
+        }
+    }
+};
+
+// acc[column][lane] += sum over 32 rows of tile[row][column] * p[row][lane]
+template <typename T, int NB>
+__device__ inline void add_rows(f32x16 (&acc)[NB], const char *tile, const Reader<T, NB> &rd, const Packed<T, NB> &p)
+{
+#pragma unroll
+    for (int g = 0; g < Shape<T, NB>::kGroups; ++g)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-            acc[b] = Frag<T>::mma(rd.column(tile, g, b), f, acc[b]);
-    }
+            acc[b] = Frag<T>::mma(rd.column(tile, g, b), p.f[g], acc[b]);
 }
 
 // The same row by row, for tiles that hold infinities or NaN: where a factor
@@ -356,6 +442,28 @@ struct Span {
         return lo <= hi;
     }
 };
+
+// The keys of a pass, a step after the other: first ones, then those of the
+// window.
+template <int STEP> struct Steps {
+    int first, begin, n;  // steps of first keys, step of the first other, all
+    int turn, to;         // the last step of first keys (its key), and what follows it
+    __device__ Steps(const Attention &a, int lo, int hi)
+    {
+        const int from = max(0, lo - a.window + 1), ahead = min(a.sinks, from);
+        first = (ahead + STEP - 1) / STEP;
+        begin = max(first, from / STEP);
+        n = first + hi / STEP - begin + 1;
+        turn = first > 0 ? (first - 1) * STEP : -1;
+        to = begin * STEP;
+    }
+    __device__ int key(int step) const { return (step < first ? step : begin + step - first) * STEP; }
+    __device__ int next(int j) const { return j == turn ? to : j + STEP; }
+};
+__device__ inline const char *row_at(const char *p, int j, uint32_t stride)
+{
+    return p + (uint64_t)(uint32_t)j * stride;
+}
 
 __device__ inline char *rows_of(const Heads &h, int b, int head) { return h.p + b * h.batch + head * h.head; }
 

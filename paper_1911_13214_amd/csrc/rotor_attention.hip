@@ -28,35 +28,43 @@ template <typename T, int NB> struct Rows {
         sum = 0.f;
     }
 
-    // KB blocks of 32 keys: masked scores to probabilities.
-    template <int KB> __device__ void soften(f32x16 (&s)[KB], float c)
+    // 32 keys: masked scores to probabilities.  First the maximum: `by` is the
+    // factor by which what acc holds falls behind, if any row's is raised.
+    __device__ bool raise(const f32x16 &s, float c, float &by)
     {
-        float most = s[0][0];
+        float most = s[0];
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                most = fmaxf(most, s[b][e]);
-        most = fmaxf(most, other_half(most));
-        if (__any((most - top) * c > kSlack)) {  // (-inf - -inf is NaN: no)
-            const float next = fmaxf(top, most), by = next > top ? exp2_of((top - next) * c) : 1.f;
+        for (int e = 1; e < 16; ++e)
+            most = fmaxf(most, s[e]);
+        most = halves_max(most);
+        const bool any = __any((most - top) * c > kSlack);  // (-inf - -inf is NaN: no)
+        if (any) {
+            const float next = fmaxf(top, most);
+            by = next > top ? exp2_of((top - next) * c) : 1.f;
             sum *= by;
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    acc[b][e] *= by;
             top = next;
         }
+        return any;
+    }
+    __device__ void soften(f32x16 &s, float c)
+    {
         // a row that has seen nothing yet: exp2(-inf - 0) = 0
         const float base = top == -kInf ? 0.f : top * c;
+        float add = 0.f;
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int e = 0; e < 16; ++e) {
+            s[e] = exp2_of(__builtin_fmaf(s[e], c, -base));
+            add += s[e];
+        }
+        sum += add;
+    }
+    __device__ void scale(float by)
+    {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[b][e] = exp2_of(__builtin_fmaf(s[b][e], c, -base));
-                sum += s[b][e];
-            }
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                acc[b][e] *= by;
     }
 };
 
@@ -65,7 +73,7 @@ template <typename T, int NB>
 __device__ inline void put_rows(const Attention &a, const Rows<T, NB> &w, int b, int kv, int part, int row, bool seen,
                                 int h)
 {
-    const float sum = w.sum + other_half(w.sum);
+    const float sum = halves_sum(w.sum);
     if (row >= a.rows)
         return;
     if (a.parts > 1) {
@@ -83,8 +91,11 @@ __device__ inline void put_rows(const Attention &a, const Rows<T, NB> &w, int b,
 }
 #endif
 
-// A workgroup takes 128 rows of one key head and goes over the tiles of 64 keys
-// that any of them sees; the next tile arrives in LDS while one is used.
+// A workgroup takes 128 rows of one key head and goes over the keys that any of
+// them sees, 32 a step.  The steps overlap: while the exponentials of one are
+// computed, the matrix units work on the scores of the next and on the values
+// of the one before, in one stream of independent instructions.  Three places
+// in LDS for keys and for values: one is read, two are on their way.
 // blockIdx.x: key head and sequence (so that an XCD keeps to few of them),
 // y: rows, the last (with the most keys) first, z: part of the keys.
 template <typename T, int NB>
@@ -92,8 +103,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef Shape<T, NB> S;
-    constexpr int kBytes = kTileKeys * S::kRow, KB = kTileKeys / 32;
-    __shared__ __attribute__((aligned(1024))) char tiles[2][2][kBytes];  // [which][keys, values]
+    typedef typename Frag<T>::F F;
+    constexpr int kBytes = kTileKeys * S::kRow;
+    // one array a place: a read waits for the loads into its own array alone
+    __shared__ __attribute__((aligned(1024))) char keys0[kBytes], keys1[kBytes], keys2[kBytes];
+    __shared__ __attribute__((aligned(1024))) char vals0[kBytes], vals1[kBytes], vals2[kBytes];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
     const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
     const int r0 = (gridDim.y - 1 - blockIdx.y) * kTileRows, rw = r0 + wave * 32, row = rw + lane % 32;
@@ -120,63 +134,114 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
     int wlo = 0, whi = -1;
     const bool some = rw < a.rows && span.positions(rw / a.group, min(a.rows - 1, rw + 31) / a.group, wlo, whi);
 
-    // tiles of first keys, then those of the window
-    const int from = max(0, lo - a.window + 1), ahead = min(a.sinks, from);
-    const int first = (ahead + kTileKeys - 1) / kTileKeys, begin = max(first, from / kTileKeys);
-    const int n = first + hi / kTileKeys - begin + 1;
-    const int i0 = (int)((int64_t)n * blockIdx.z / a.parts), i1 = (int)((int64_t)n * (blockIdx.z + 1) / a.parts);
+    const Steps<kTileKeys> steps(a, lo, hi);
+    const int i0 = (int)((int64_t)steps.n * blockIdx.z / a.parts);
+    const int i1 = (int)((int64_t)steps.n * (blockIdx.z + 1) / a.parts);
 
-    Loader<T, NB, kTileKeys, kWaves> lk, lv;
+    typedef Loader<T, NB, kTileKeys, kWaves> Load;
+    Load lk, lv;
     lk.init(wave, lane, a.width, a.k.token);
     lv.init(wave, lane, a.width, a.v.token);
     Reader<T, NB> rd;
     rd.init(lane);
     const char *const k0 = rows_of(a.k, b, kv), *const v0 = rows_of(a.v, b, kv);
-
-    auto load = [&](int i) {
-        const int j = (i < first ? i : begin + i - first) * kTileKeys;
-        lk.load(tiles[i & 1][0], k0 + j * a.k.token, hi + 1 - j);
-        lv.load(tiles[i & 1][1], v0 + j * a.v.token, hi + 1 - j);
+    const uint32_t k_stride = (uint32_t)a.k.token, v_stride = (uint32_t)a.v.token;
+    const int row_bytes = a.width * (int)sizeof(T);
+    auto load_keys = [&](char *place, int j) {
+        lk.load(place, row_at(k0, j, k_stride), hi + 1 - j, k_stride, row_bytes);
     };
-    auto pass = [&](auto apart) {
-        constexpr bool kApart = decltype(apart)::value;
-        if (i0 < i1)
-            load(i0);
-        for (int i = i0; i < i1; ++i) {
-            tile_barrier();
-            if (i + 1 < i1)
-                load(i + 1);
-            const int j = (i < first ? i : begin + i - first) * kTileKeys, je = j + kTileKeys - 1;
-            if (!some || j > whi || (j >= a.sinks && je < wlo - a.window + 1))
-                continue;
-            const char *keys = tiles[i & 1][0], *vals = tiles[i & 1][1];
-            f32x16 s[KB];
+    auto load_values = [&](char *place, int j) {
+        lv.load(place, row_at(v0, j, v_stride), hi + 1 - j, v_stride, row_bytes);
+    };
+    const int all_from = whi - a.window + 1;
+    auto mask = [&](f32x16 &s, int j) {
+        const int je = j + kTileKeys - 1;
+        if (!some || je > wlo || (je >= a.sinks && j < all_from)) {
+            asm volatile("");  // a branch: few steps need it
 #pragma unroll
-            for (int k = 0; k < KB; ++k)
-                s[k] = product<T, NB>(keys + k * 32 * S::kRow, rd, w.q);
-            if (je > wlo || (je >= a.sinks && j < whi - a.window + 1)) {
-#pragma unroll
-                for (int k = 0; k < KB; ++k)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        s[k][e] = sight(j + 32 * k + row_of(e, h)) ? s[k][e] : -kInf;
-            }
-            w.soften(s, a.c);
-#pragma unroll
-            for (int k = 0; k < KB; ++k) {
-                if constexpr (kApart)
-                    add_rows_apart<T, NB>(w.acc, vals + k * 32 * S::kRow, lane, s[k]);
-                else
-                    add_rows<T, NB>(w.acc, vals + k * 32 * S::kRow, rd, s[k]);
-            }
+            for (int e = 0; e < 16; ++e)
+                s[e] = sight(j + row_of(e, h)) ? s[e] : -kInf;
         }
     };
-    pass(std::false_type{});
+
+    // keys of this step and of the next three
+    int j = steps.key(i0), j1 = steps.next(j), j2 = steps.next(j1);
+    load_keys(keys0, j);
+    load_keys(keys1, j1);
+    load_values(vals2, hi + 1);  // zeros: there is no step before
+    load_keys(keys2, j2);
+    load_values(vals0, j);
+    step_barrier<4 * Load::kLoads>();
+    f32x16 s = product<T, NB>(keys0, rd, w.q);
+    Packed<T, NB> before{};
+    auto step = [&](char *free, char *next_keys, char *next_vals, char *last_vals) {
+        step_barrier<2 * Load::kLoads>();
+        const int j3 = steps.next(j2);
+        F kf[S::NK];
+        fetch_rows<T, NB>(next_keys, rd, kf);
+        load_keys(free, j3);
+        load_values(next_vals, j1);
+        mask(s, j);
+        float by;
+        const bool raised = w.raise(s, a.c, by);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 ahead;
+        multiply<T>(ahead, kf, w.q);
+        w.soften(s, a.c);
+        add_rows<T, NB>(w.acc, last_vals, rd, before);
+        before = Packed<T, NB>(s);
+        before.pin();
+        if constexpr (sizeof(T) == 2) {
+            reads<2 * NB>();
+            beside<S::NK / 2, 4, 0>();
+            reads<2 * NB>();
+            beside<S::NK / 2, 4, 0>();
+            beside<2 * NB, 2, 16 / (2 * NB)>();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (raised)
+            w.scale(by);
+        s = ahead;
+        j = j1;
+        j1 = j2;
+        j2 = j3;
+    };
+    int left = i1 - i0;
+    for (; left >= 3; left -= 3) {
+        step(keys0, keys1, vals1, vals2);
+        step(keys1, keys2, vals2, vals0);
+        step(keys2, keys0, vals0, vals1);
+    }
+    if (left > 0)
+        step(keys0, keys1, vals1, vals2);
+    if (left > 1)
+        step(keys1, keys2, vals2, vals0);
+    tile_barrier();
+    if (left == 0)
+        add_rows<T, NB>(w.acc, vals2, rd, before);
+    else if (left == 1)
+        add_rows<T, NB>(w.acc, vals0, rd, before);
+    else
+        add_rows<T, NB>(w.acc, vals1, rd, before);
+
     // Infinities or NaN: they may have come from keys that a row does not see,
     // as 0 times their values.
     if (__syncthreads_or(!finite(w.acc))) {
         w.reset();
-        pass(std::true_type{});
+        j = steps.key(i0);
+        for (int i = i0; i < i1; ++i, j = steps.next(j)) {
+            load_keys(keys0, j);
+            load_values(vals0, j);
+            tile_barrier();
+            s = product<T, NB>(keys0, rd, w.q);
+            mask(s, j);
+            float by;
+            if (w.raise(s, a.c, by))
+                w.scale(by);
+            w.soften(s, a.c);
+            add_rows_apart<T, NB>(w.acc, vals0, lane, s);
+            tile_barrier();
+        }
     }
     put_rows(a, w, b, kv, blockIdx.z, row, seen, h);
 #endif
@@ -290,32 +355,35 @@ __global__ __launch_bounds__(256, 1) void few_kernel(Attention a)
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
             }
-            f32x16 s[1];
+            f32x16 s;
             if (whole) {
-                s[0] = product<T, NB>(keys, rd, w.q);
+                s = product<T, NB>(keys, rd, w.q);
             } else {
                 // columns past the width hold others again: they count as 0
 #pragma unroll
                 for (int x = 0; x < 16; ++x)
-                    s[0][x] = 0.f;
+                    s[x] = 0.f;
 #pragma unroll
                 for (int k = 0; k < S::NK; ++k) {
                     F f = rd.row(keys, k);
                     if ((2 * k + h) * Frag<T>::N >= a.width)
                         f = F{};
-                    s[0] = Frag<T>::mma(f, w.q[k], s[0]);
+                    s = Frag<T>::mma(f, w.q[k], s);
                 }
             }
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
                 const int at = e + row_of(x, h);
-                s[0][x] = at < e1 && sight(position(at)) ? s[0][x] : -kInf;
+                s[x] = at < e1 && sight(position(at)) ? s[x] : -kInf;
             }
+            float by;
+            if (w.raise(s, a.c, by))
+                w.scale(by);
             w.soften(s, a.c);
             if constexpr (kApart)
-                add_rows_apart<T, NB>(w.acc, vals, lane, s[0]);
+                add_rows_apart<T, NB>(w.acc, vals, lane, s);
             else
-                add_rows<T, NB>(w.acc, vals, rd, s[0]);
+                add_rows<T, NB>(w.acc, vals, rd, Packed<T, NB>(s));
         }
     };
     pass(std::false_type{});
@@ -327,7 +395,7 @@ __global__ __launch_bounds__(256, 1) void few_kernel(Attention a)
 
     // the waves' sums: relative to the highest maximum, added in order
     if (wave < W)
-        w.sum += other_half(w.sum);
+        w.sum = halves_sum(w.sum);
     if (wave < W && h == 0)
         soft[wave][lane] = make_float2(w.top, w.sum);
     __syncthreads();
@@ -477,7 +545,7 @@ ForwardPlan forward_plan(const rotor_attention *n, bool step)
                 break;
         }
     } else {
-        const int64_t base = bk * ceil_div(rows, kTileRows), tiles = most / kTileKeys;
+        const int64_t base = bk * ceil_div(rows, kTileRows), tiles = most / 64;
         if (base < 256 && tiles >= 16)
             parts = ceil_div(512, base) < tiles / 8 ? ceil_div(512, base) : tiles / 8;
     }

@@ -8,6 +8,7 @@
 namespace rotor {
 namespace {
 
+constexpr int kPairKeys = 64;
 constexpr int kKeys = 128;   // of a workgroup, gradients of keys
 constexpr int kStepRows = 64;
 
@@ -34,7 +35,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef Shape<T, NB> S;
     typedef typename Frag<T>::F F;
-    constexpr int kBytes = kTileKeys * S::kRow;
+    constexpr int kBytes = kPairKeys * S::kRow;
     __shared__ __attribute__((aligned(1024))) char tiles[2][2][kBytes];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
     const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
@@ -63,8 +64,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
         if (seen)
             lse = a.lse[((int64_t)b * a.tokens + t) * ((int64_t)a.kv * a.group) + head] * kLog2e;
     }
-    delta += other_half(delta);
-    most = fmaxf(most, other_half(most));
+    delta = halves_sum(delta);
+    most = halves_max(most);
     int exponent = 0;
     {
         const int64_t at = (int64_t)blockIdx.x * a.row_pitch + row;  // the pitch covers the last tile
@@ -99,18 +100,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     const bool some = rw < a.rows && span.positions(rw / a.group, min(a.rows - 1, rw + 31) / a.group, wlo, whi);
 
     const int from = max(0, lo - a.window + 1), ahead = min(a.sinks, from);
-    const int first = (ahead + kTileKeys - 1) / kTileKeys, begin = max(first, from / kTileKeys);
-    const int n = first + hi / kTileKeys - begin + 1;
-    Loader<T, NB, kTileKeys, kWaves> lk, lv;
+    const int first = (ahead + kPairKeys - 1) / kPairKeys, begin = max(first, from / kPairKeys);
+    const int n = first + hi / kPairKeys - begin + 1;
+    Loader<T, NB, kPairKeys, kWaves> lk, lv;
     lk.init(wave, lane, a.width, a.k.token);
     lv.init(wave, lane, a.width, a.v.token);
     Reader<T, NB> rd;
     rd.init(lane);
     const char *const k0 = rows_of(a.k, b, kv), *const v0 = rows_of(a.v, b, kv);
     auto load = [&](int i) {
-        const int j = (i < first ? i : begin + i - first) * kTileKeys;
-        lk.load(tiles[i & 1][0], k0 + j * a.k.token, hi + 1 - j);
-        lv.load(tiles[i & 1][1], v0 + j * a.v.token, hi + 1 - j);
+        const int j = (i < first ? i : begin + i - first) * kPairKeys;
+        lk.load(tiles[i & 1][0], k0 + j * a.k.token, hi + 1 - j, a.k.token, a.width * (int)sizeof(T));
+        lv.load(tiles[i & 1][1], v0 + j * a.v.token, hi + 1 - j, a.v.token, a.width * (int)sizeof(T));
     };
     auto pass = [&](auto apart) {
         constexpr bool kApart = decltype(apart)::value;
@@ -119,9 +120,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
             tile_barrier();
             if (i + 1 < n)
                 load(i + 1);
-            const int j = (i < first ? i : begin + i - first) * kTileKeys;
+            const int j = (i < first ? i : begin + i - first) * kPairKeys;
 #pragma unroll
-            for (int k = 0; k < kTileKeys / 32; ++k) {
+            for (int k = 0; k < kPairKeys / 32; ++k) {
                 const int jk = j + 32 * k, je = jk + 31;
                 if (!some || jk > whi || (jk >= a.sinks && je < wlo - a.window + 1))
                     continue;
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
                 if constexpr (kApart)
                     add_rows_apart<T, NB>(acc, keys, lane, ds);
                 else
-                    add_rows<T, NB>(acc, keys, rd, ds);
+                    add_rows<T, NB>(acc, keys, rd, Packed<T, NB>(ds));
             }
         }
     };
@@ -298,8 +299,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
                     add_rows_apart<T, NB>(dv, dt, lane, s);
                     add_rows_apart<T, NB>(dk, qt, lane, ds);
                 } else {
-                    add_rows<T, NB>(dv, dt, rd, s);
-                    add_rows<T, NB>(dk, qt, rd, ds);
+                    add_rows<T, NB>(dv, dt, rd, Packed<T, NB>(s));
+                    add_rows<T, NB>(dk, qt, rd, Packed<T, NB>(ds));
                 }
             }
         }
