@@ -50,6 +50,7 @@ struct Attention {
     int rows;            // tokens * group
     int window, sinks;   // window at most kFar
     float scale, c;      // c = scale log2(e)
+    uint32_t magic;      // ceil(2^32 / group), 0 for a group of one: x / group for x below 2^16
     uint64_t magic40;    // ceil(2^40 / group)
     int parts;           // of the keys (forward) or of the rows (gradients of keys)
     int ring;            // slots past the first ones, 0: the cache is linear
@@ -237,20 +238,25 @@ template <typename T, int NB, int ROWS, int WAVES> struct Loader {
         for (int i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + i * 1024), 16, at[i], 0, 0, 0);
     }
-    // Rows of (token, head of the group): rows r0 + [from, to) of the tile exist.
-    __device__ void load_rows(char *lds, const char *p, const Attention &a, const Heads &h, int lane, int r0, int from,
-                              int to) const
+    // Rows of (token, head of the group), of two tensors: rows r0 + [from, to) of
+    // the tile exist.
+    __device__ void load_rows(char *lds_x, char *lds_y, const char *x, const char *y, const Attention &a,
+                              const Heads &hx, const Heads &hy, int lane, int r0, int from, int to) const
     {
         const int t0 = token_of(a, r0), g0 = r0 - t0 * a.group;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(p + t0 * h.token), 0, 0x7FFFFFFF, 0x00020000);
+        const auto rx = __builtin_amdgcn_make_buffer_rsrc((void *)(x + t0 * hx.token), 0, 0x7FFFFFFF, 0x00020000);
+        const auto ry = __builtin_amdgcn_make_buffer_rsrc((void *)(y + t0 * hy.token), 0, 0x7FFFFFFF, 0x00020000);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int row = row0 + i * kAtOnce, c = piece(lane, row), x = g0 + row;
-            const int t = token_of(a, x), g = x - t * a.group;
-            const uint32_t off = (uint32_t)t * (uint32_t)h.token + (uint32_t)g * (uint32_t)h.head + c * 16;
+            const int row = row0 + i * kAtOnce, c = piece(lane, row);
+            const uint32_t n = g0 + row, t = a.magic ? __umulhi(n, a.magic) : n, g = n - t * a.group;
             const bool in = (row >= from) & (row < to) & (c * Frag<T>::N < a.width);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + first + i * 1024), 16,
-                                                     in ? off : 0x80000000u, 0, 0, 0);
+            const uint32_t off_x = t * (uint32_t)hx.token + g * (uint32_t)hx.head + c * 16;
+            const uint32_t off_y = t * (uint32_t)hy.token + g * (uint32_t)hy.head + c * 16;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_ptr)(lds_x + first + i * 1024), 16,
+                                                     in ? off_x : 0x80000000u, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (lds_ptr)(lds_y + first + i * 1024), 16,
+                                                     in ? off_y : 0x80000000u, 0, 0, 0);
         }
     }
 };
@@ -583,6 +589,7 @@ inline void fill(Attention &a, const rotor_attention *n)
     a.sinks = a.window >= a.keys ? 0 : n->sinks < n->keys ? (int)n->sinks : a.keys;
     a.scale = (float)n->scale;
     a.c = (float)(n->scale * 1.4426950408889634);
+    a.magic = a.group == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
     a.magic40 = (((uint64_t)1 << 40) + a.group - 1) / a.group;
     a.parts = 1;
 }

@@ -8,9 +8,8 @@
 namespace rotor {
 namespace {
 
-constexpr int kPairKeys = 64;
 constexpr int kKeys = 128;   // of a workgroup, gradients of keys
-constexpr int kStepRows = 64;
+constexpr int kStepRows = 64;  // the most at a time
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // float16 holds 40 bits of range, and dS is as small as the gradients that
@@ -27,16 +26,21 @@ __device__ inline int exponent_of(float most)
 __device__ inline float power_of(int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 #endif
 
-// dq: as the forward kernel, with rows in the registers.  It also leaves what
-// the gradients of keys need of each row: log-sum-exp, delta, position.
+// dq: as the forward kernel, with rows in the registers.  While the matrix units
+// multiply do with the values, the exponentials of the scores are computed, and
+// while they work on the next step's scores, the gradients of this one's.  It
+// also leaves what the gradients of keys need of each row: log-sum-exp, delta,
+// position.
 template <typename T, int NB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel(Attention a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef Shape<T, NB> S;
     typedef typename Frag<T>::F F;
-    constexpr int kBytes = kPairKeys * S::kRow;
-    __shared__ __attribute__((aligned(1024))) char tiles[2][2][kBytes];
+    constexpr int kBytes = kTileKeys * S::kRow;
+    // one array a place: a read waits for the loads into its own array alone
+    __shared__ __attribute__((aligned(1024))) char keys0[kBytes], keys1[kBytes], keys2[kBytes];
+    __shared__ __attribute__((aligned(1024))) char vals0[kBytes], vals1[kBytes], vals2[kBytes];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
     const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
     const int r0 = (gridDim.y - 1 - blockIdx.y) * kTileRows, rw = r0 + wave * 32, row = rw + lane % 32;
@@ -99,56 +103,93 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     int wlo = 0, whi = -1;
     const bool some = rw < a.rows && span.positions(rw / a.group, min(a.rows - 1, rw + 31) / a.group, wlo, whi);
 
-    const int from = max(0, lo - a.window + 1), ahead = min(a.sinks, from);
-    const int first = (ahead + kPairKeys - 1) / kPairKeys, begin = max(first, from / kPairKeys);
-    const int n = first + hi / kPairKeys - begin + 1;
-    Loader<T, NB, kPairKeys, kWaves> lk, lv;
+    const Steps<kTileKeys> steps(a, lo, hi);
+    typedef Loader<T, NB, kTileKeys, kWaves> Load;
+    Load lk, lv;
     lk.init(wave, lane, a.width, a.k.token);
     lv.init(wave, lane, a.width, a.v.token);
     Reader<T, NB> rd;
     rd.init(lane);
     const char *const k0 = rows_of(a.k, b, kv), *const v0 = rows_of(a.v, b, kv);
-    auto load = [&](int i) {
-        const int j = (i < first ? i : begin + i - first) * kPairKeys;
-        lk.load(tiles[i & 1][0], k0 + j * a.k.token, hi + 1 - j, a.k.token, a.width * (int)sizeof(T));
-        lv.load(tiles[i & 1][1], v0 + j * a.v.token, hi + 1 - j, a.v.token, a.width * (int)sizeof(T));
+    const uint32_t k_stride = (uint32_t)a.k.token, v_stride = (uint32_t)a.v.token;
+    const int row_bytes = a.width * (int)sizeof(T), all_from = whi - a.window + 1;
+    auto load = [&](char *keys, char *vals, int j) {
+        lk.load(keys, row_at(k0, j, k_stride), hi + 1 - j, k_stride, row_bytes);
+        lv.load(vals, row_at(v0, j, v_stride), hi + 1 - j, v_stride, row_bytes);
     };
-    auto pass = [&](auto apart) {
-        constexpr bool kApart = decltype(apart)::value;
-        load(0);
-        for (int i = 0; i < n; ++i) {
-            tile_barrier();
-            if (i + 1 < n)
-                load(i + 1);
-            const int j = (i < first ? i : begin + i - first) * kPairKeys;
+    // from scores and do v to gradients of scores
+    auto slope = [&](f32x16 &s, const f32x16 &dp) {
 #pragma unroll
-            for (int k = 0; k < kPairKeys / 32; ++k) {
-                const int jk = j + 32 * k, je = jk + 31;
-                if (!some || jk > whi || (jk >= a.sinks && je < wlo - a.window + 1))
-                    continue;
-                const char *keys = tiles[i & 1][0] + k * 32 * S::kRow, *vals = tiles[i & 1][1] + k * 32 * S::kRow;
-                f32x16 s = product<T, NB>(keys, rd, q), ds = product<T, NB>(vals, rd, d);
-                const bool all = je <= wlo && (je < a.sinks || jk >= whi - a.window + 1);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    ds[e] = exp2_of(__builtin_fmaf(s[e], a.c, -lse)) * ((ds[e] - delta) * factor);
-                if (!all) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        ds[e] = sight(jk + row_of(e, h)) ? ds[e] : 0.f;
-                }
-                if constexpr (kApart)
-                    add_rows_apart<T, NB>(acc, keys, lane, ds);
-                else
-                    add_rows<T, NB>(acc, keys, rd, Packed<T, NB>(ds));
-            }
+        for (int e = 0; e < 16; ++e) {
+            const float x = dp[e] - delta;
+            s[e] *= Scaled<T>::kOn ? x * factor : x;
         }
     };
-    pass(std::false_type{});
+    auto mask = [&](f32x16 &s, int j) {
+        const int je = j + kTileKeys - 1;
+        if (!some || je > wlo || (je >= a.sinks && j < all_from)) {
+            asm volatile("");  // a branch: few steps need it
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                s[e] = sight(j + row_of(e, h)) ? s[e] : 0.f;
+        }
+    };
+
+    int j = steps.key(0), j1 = steps.next(j);
+    load(keys0, vals0, j);
+    load(keys1, vals1, j1);
+    step_barrier<2 * Load::kLoads>();
+    f32x16 s = product<T, NB>(keys0, rd, q);
+    auto step = [&](const char *keys, const char *vals, const char *next_keys, char *free_keys, char *free_vals) {
+        step_barrier<Load::kLoads>();
+        const int j2 = steps.next(j1);
+        F f[S::NK];
+        fetch_rows<T, NB>(vals, rd, f);
+        load(free_keys, free_vals, j2);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 dp, ahead;
+        multiply<T>(dp, f, d);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            s[e] = exp2_of(__builtin_fmaf(s[e], a.c, -lse));
+        fetch_rows<T, NB>(next_keys, rd, f);
+        multiply<T>(ahead, f, q);
+        slope(s, dp);
+        mask(s, j);
+        add_rows<T, NB>(acc, keys, rd, Packed<T, NB>(s));
+        s = ahead;
+        j = j1;
+        j1 = j2;
+    };
+    int left = steps.n;
+    for (; left >= 3; left -= 3) {
+        step(keys0, vals0, keys1, keys2, vals2);
+        step(keys1, vals1, keys2, keys0, vals0);
+        step(keys2, vals2, keys0, keys1, vals1);
+    }
+    if (left > 0)
+        step(keys0, vals0, keys1, keys2, vals2);
+    if (left > 1)
+        step(keys1, vals1, keys2, keys0, vals0);
+    tile_barrier();
+
     // infinities or NaN may have come from keys that a row does not see
     if (__syncthreads_or(!finite(acc))) {
         clear(acc);
-        pass(std::true_type{});
+        j = steps.key(0);
+        for (int i = 0; i < steps.n; ++i, j = steps.next(j)) {
+            load(keys0, vals0, j);
+            tile_barrier();
+            s = product<T, NB>(keys0, rd, q);
+            const f32x16 dp = product<T, NB>(vals0, rd, d);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                s[e] = exp2_of(__builtin_fmaf(s[e], a.c, -lse));
+            slope(s, dp);
+            mask(s, j);
+            add_rows_apart<T, NB>(acc, keys0, lane, s);
+            tile_barrier();
+        }
     }
     if (row < a.rows)
         put_row<T>(to, h, a.width, acc, a.scale * (Scaled<T>::kOn ? power_of(exponent) : 1.f), seen);
@@ -156,7 +197,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
 }
 
 // dk and dv of 128 keys, 32 a wave: the rows that see any of them pass through
-// LDS, 64 at a time.  blockIdx.y: first the tiles with keys that every later row
+// LDS, 64 at a time.  Past 96 columns sums and keys fill the registers: the
+// values are read from LDS, and rows come 32 at a time.  blockIdx.y: first the tiles with keys that every later row
 // sees, whose rows are split into sink_parts, then the others, in parts.
 template <typename T, int NB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(Attention a)
@@ -164,9 +206,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef Shape<T, NB> S;
     typedef typename Frag<T>::F F;
-    constexpr int kBytes = kStepRows * S::kRow;
-    __shared__ __attribute__((aligned(1024))) char tiles[2][2][kBytes];  // [which][q, do]
-    __shared__ __attribute__((aligned(16))) float stats[2][3][kStepRows];
+    constexpr bool kHeld = NB < 4;  // values in registers
+    constexpr int kStep = kHeld ? kStepRows : kStepRows / 2, kBytes = kStep * S::kRow;
+    // one array a place: a read waits for the loads into its own array alone
+    __shared__ __attribute__((aligned(1024))) char q_even[kBytes], q_odd[kBytes], d_even[kBytes], d_odd[kBytes];
+    __shared__ __attribute__((aligned(1024))) char values[kHeld ? 16 : kKeys * S::kRow];
+    __shared__ __attribute__((aligned(16))) float stats_even[3 * 64], stats_odd[3 * 64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
     const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
     int tile, part, parts;
@@ -186,13 +231,25 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
     const int j0 = tile * kKeys, jw = j0 + wave * 32, key = jw + lane % 32;
     const Span span(a, b);
     const bool have = key < span.length;
-    F kf[S::NK], vf[S::NK];
+    Reader<T, NB> rd;
+    rd.init(lane);
+    F kf[S::NK], vf[kHeld ? S::NK : 1];
     {
-        const char *k = rows_of(a.k, b, kv) + key * a.k.token, *v = rows_of(a.v, b, kv) + key * a.v.token;
+        const char *k = rows_of(a.k, b, kv) + key * a.k.token, *v = rows_of(a.v, b, kv);
 #pragma unroll
         for (int i = 0; i < S::NK; ++i) {
             kf[i] = global_frag<T>(k, have, 2 * i + h, a.width);
-            vf[i] = global_frag<T>(v, have, 2 * i + h, a.width);
+            if constexpr (kHeld)
+                vf[i] = global_frag<T>(v + key * a.v.token, have, 2 * i + h, a.width);
+        }
+        if constexpr (!kHeld) {
+            // (tiles of 64 rows keep their offsets below 2^31 bytes)
+            Loader<T, NB, 64, kWaves> lv;
+            lv.init(wave, lane, a.width, a.v.token);
+#pragma unroll
+            for (int i = 0; i < kKeys / 64; ++i)
+                lv.load(values + i * 64 * S::kRow, v + (j0 + i * 64) * a.v.token, span.length - j0 - i * 64,
+                        (uint32_t)a.v.token, a.width * (int)sizeof(T));
         }
     }
     f32x16 dk[NB], dv[NB];
@@ -200,110 +257,124 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
     clear(dv);
     int exponent = -1000;  // of what dk is multiplied with
 
-    // positions that see a key of the tile, as rows, in steps of 64
+    // positions that see a key of the tile, as rows, in steps
     const int64_t far = j0 < a.sinks ? (int64_t)kFar * 2 : (int64_t)j0 + kKeys - 1 + a.window - 1;
     const int plo = max(j0, 0), phi = (int)min((int64_t)span.length - 1, far);
     const int t0 = max(0, plo - span.offset);
     const int64_t t1 = min((int64_t)a.tokens - 1, (int64_t)phi - span.offset);
     int n = 0, begin = 0;
     if (t0 <= t1) {
-        begin = t0 * a.group / kStepRows;
-        n = (int)((t1 + 1) * a.group + kStepRows - 1) / kStepRows - begin;
+        begin = t0 * a.group / kStep;
+        n = (int)((t1 + 1) * a.group + kStep - 1) / kStep - begin;
     }
     const int i0 = begin + (int)((int64_t)n * part / parts), i1 = begin + (int)((int64_t)n * (part + 1) / parts);
 
-    Loader<T, NB, kStepRows, kWaves> ld;
+    Loader<T, NB, kStep, kWaves> ld;
     ld.init(wave, lane, a.width, 0);
-    Reader<T, NB> rd;
-    rd.init(lane);
     const char *const q0 = rows_of(a.q, b, kv * a.group), *const d0 = rows_of(a.dout, b, kv * a.group);
     // rows without a place in the sequence are not read
-    const int64_t live0 = max((int64_t)0, -(int64_t)span.offset) * a.group;
-    const int64_t live1 = min((int64_t)a.tokens, max((int64_t)0, (int64_t)span.length - span.offset)) * a.group;
-    auto load = [&](int i) {
-        const int r = i * kStepRows;
-        const int from = (int)max((int64_t)0, min((int64_t)kStepRows, live0 - r));
-        const int to = (int)max((int64_t)0, min((int64_t)kStepRows, live1 - r));
-        ld.load_rows(tiles[i & 1][0], q0, a, a.q, lane, r, from, to);
-        ld.load_rows(tiles[i & 1][1], d0, a, a.dout, lane, r, from, to);
-        if (wave < 3) {
-            const void *const p = wave == 0 ? (const void *)a.row_lse : wave == 1 ? (const void *)a.row_delta : a.row_at;
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
-                (void *)((const char *)p + ((int64_t)blockIdx.x * a.row_pitch + r) * 4), 0, kStepRows * 4, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)stats[i & 1][wave], 4, lane * 4, 0, 0, 0);
-        }
+    const int64_t gw = a.group, off = span.offset;
+    const int live0 = (int)(min((int64_t)a.tokens, max((int64_t)0, -off)) * gw);
+    const int live1 = (int)(min((int64_t)a.tokens, max((int64_t)0, span.length - off)) * gw);
+    const char *const stats_of = (const char *)(wave == 0 ? (const void *)a.row_lse
+                                                : wave == 1 ? (const void *)a.row_delta
+                                                            : a.row_at) +
+                                 (int64_t)blockIdx.x * a.row_pitch * 4;
+    auto load = [&](int i, char *qs, char *ds, float *stats) {
+        const int r = i * kStep;
+        ld.load_rows(qs, ds, q0, d0, a, a.q, a.dout, lane, r, live0 - r, live1 - r);
+        if (wave < 3)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                __builtin_amdgcn_make_buffer_rsrc((void *)(stats_of + r * 4), 0, kStep * 4, 0x00020000),
+                (lds_ptr)(stats + wave * 64), 4, lane * 4, 0, 0, 0);
     };
     // rows that see any of the wave's keys, and those that see all of them
-    const int64_t gw = a.group, off = span.offset;
-    const bool first = jw + 31 < a.sinks;
-    const int some0 = (int)max(live0, (jw - off) * gw);
-    const int some1 = (int)(jw < a.sinks ? live1 : min(live1, (jw + 31 + (int64_t)a.window - off) * gw));
-    const int all0 = (int)max(live0, (jw + 31 - off) * gw);
-    const int all1 = (int)(first ? live1 : min(live1, max((int64_t)0, (jw + (int64_t)a.window - off) * gw)));
+    auto row_at_key = [&](int64_t j) { return (int)min((int64_t)live1, max((int64_t)live0, (j - off) * gw)); };
+    const int some0 = row_at_key(jw), some1 = jw < a.sinks ? live1 : row_at_key(jw + 31 + (int64_t)a.window);
+    const int all0 = row_at_key(jw + 31), all1 = jw + 31 < a.sinks ? live1 : row_at_key(jw + (int64_t)a.window);
     auto pass = [&](auto apart) {
         constexpr bool kApart = decltype(apart)::value;
-        if (i0 < i1)
-            load(i0);
-        for (int i = i0; i < i1; ++i) {
-            tile_barrier();
-            if (i + 1 < i1)
-                load(i + 1);
-#pragma unroll 1
-            for (int u = 0; u < kStepRows / 32; ++u) {
-                const int r = i * kStepRows + u * 32;
-                if (r + 32 <= some0 || r >= some1)
-                    continue;
-                const bool all = r >= all0 && r + 32 <= all1;
-                const char *qt = tiles[i & 1][0] + u * 32 * S::kRow, *dt = tiles[i & 1][1] + u * 32 * S::kRow;
-                const float *st = &stats[i & 1][0][u * 32];
-                f32x16 s = product<T, NB>(qt, rd, kf), ds = product<T, NB>(dt, rd, vf);
-                float factor = 1.f;
-                if constexpr (Scaled<T>::kOn) {
-                    const int e = a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + r / 32];
-                    if (e > exponent) {
-                        const float by = power_of(max(exponent - e, -300));
+        auto half = [&](int r, const char *qt, const char *dt, const float *st) {
+            if (r + 32 <= some0 || r >= some1)
+                return;
+            const bool all = r >= all0 && r + 32 <= all1;
+            f32x16 s = product<T, NB>(qt, rd, kf), ds;
+            if constexpr (kHeld) {
+                ds = product<T, NB>(dt, rd, vf);
+            } else {
 #pragma unroll
-                        for (int x = 0; x < NB; ++x)
+                for (int e = 0; e < 16; ++e)
+                    ds[e] = 0.f;
 #pragma unroll
-                            for (int y = 0; y < 16; ++y)
-                                dk[x][y] *= by;
-                        exponent = e;
-                    }
-                    factor = power_of(-exponent);
+                for (int k = 0; k < S::NK; ++k)
+                    ds = Frag<T>::mma(rd.row(dt, k), rd.row(values + wave * 32 * S::kRow, k), ds);
+            }
+            float factor = 1.f;
+            if constexpr (Scaled<T>::kOn) {
+                const int e = a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + r / 32];
+                if (e > exponent) {
+                    const float by = power_of(max(exponent - e, -300));
+#pragma unroll
+                    for (int x = 0; x < NB; ++x)
+#pragma unroll
+                        for (int y = 0; y < 16; ++y)
+                            dk[x][y] *= by;
+                    exponent = e;
                 }
+                factor = power_of(-exponent);
+            }
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 l = *(const f32x4 *)(st + 8 * g + 4 * h);
-                    const f32x4 dl = *(const f32x4 *)(st + kStepRows + 8 * g + 4 * h);
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 l = *(const f32x4 *)(st + 8 * g + 4 * h), dl = *(const f32x4 *)(st + 64 + 8 * g + 4 * h);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[4 * g + e] = exp2_of(__builtin_fmaf(s[4 * g + e], a.c, -l[e]));
-                        ds[4 * g + e] = s[4 * g + e] * ((ds[4 * g + e] - dl[e]) * factor);
-                    }
-                }
-                if (!all) {
-                    asm volatile("");  // a branch: few tiles need it
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        typedef int i32x4 __attribute__((ext_vector_type(4)));
-                        const i32x4 p = *(const i32x4 *)(st + 2 * kStepRows + 8 * g + 4 * h);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const bool in = key <= p[e] && (key > p[e] - a.window || key < a.sinks);
-                            s[4 * g + e] = in ? s[4 * g + e] : 0.f;
-                            ds[4 * g + e] = in ? ds[4 * g + e] : 0.f;
-                        }
-                    }
-                }
-                if constexpr (kApart) {
-                    add_rows_apart<T, NB>(dv, dt, lane, s);
-                    add_rows_apart<T, NB>(dk, qt, lane, ds);
-                } else {
-                    add_rows<T, NB>(dv, dt, rd, Packed<T, NB>(s));
-                    add_rows<T, NB>(dk, qt, rd, Packed<T, NB>(ds));
+                for (int e = 0; e < 4; ++e) {
+                    s[4 * g + e] = exp2_of(__builtin_fmaf(s[4 * g + e], a.c, -l[e]));
+                    const float x = ds[4 * g + e] - dl[e];
+                    ds[4 * g + e] = s[4 * g + e] * (Scaled<T>::kOn ? x * factor : x);
                 }
             }
+            if (!all) {
+                asm volatile("");  // a branch: few tiles need it
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    typedef int i32x4 __attribute__((ext_vector_type(4)));
+                    const i32x4 p = *(const i32x4 *)(st + 128 + 8 * g + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool in = key <= p[e] && (key > p[e] - a.window || key < a.sinks);
+                        s[4 * g + e] = in ? s[4 * g + e] : 0.f;
+                        ds[4 * g + e] = in ? ds[4 * g + e] : 0.f;
+                    }
+                }
+            }
+            if constexpr (kApart) {
+                add_rows_apart<T, NB>(dv, dt, lane, s);
+                add_rows_apart<T, NB>(dk, qt, lane, ds);
+            } else {
+                add_rows<T, NB>(dv, dt, rd, Packed<T, NB>(s));
+                add_rows<T, NB>(dk, qt, rd, Packed<T, NB>(ds));
+            }
+        };
+        auto use = [&](int i, const char *qt, const char *dt, const float *st) {
+#pragma unroll 1
+            for (int u = 0; u < kStep / 32; ++u)
+                half(i * kStep + u * 32, qt + u * 32 * S::kRow, dt + u * 32 * S::kRow, st + u * 32);
+        };
+        if (i0 < i1)
+            load(i0, q_even, d_even, stats_even);
+        for (int i = i0; i < i1; i += 2) {
+            tile_barrier();
+            if (i + 1 < i1)
+                load(i + 1, q_odd, d_odd, stats_odd);
+            use(i, q_even, d_even, stats_even);
+            if (i + 1 == i1)
+                break;
+            tile_barrier();
+            if (i + 2 < i1)
+                load(i + 2, q_even, d_even, stats_even);
+            use(i + 1, q_odd, d_odd, stats_odd);
         }
+        tile_barrier();
     };
     pass(std::false_type{});
     // infinities or NaN may have come from rows that do not see a key
