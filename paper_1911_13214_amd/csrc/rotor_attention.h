@@ -112,6 +112,7 @@ template <typename T, int NB> struct Shape {
     static constexpr int kPieces = kRow / 16;
     static constexpr int NK = NB * (int)sizeof(T);                  // fragments of a row: 32 bytes each
     static constexpr int kGroups = 32 / (2 * Frag<T>::N);           // fragments of 32 summed rows
+    static constexpr int kTurned = sizeof(T) == 4 ? 4 : 2;          // reads of a fragment of columns
     static __device__ int turn(int row)
     {
         if (sizeof(T) == 4)
@@ -134,13 +135,16 @@ __device__ inline Turned turned(const char *lds)
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Turned *)lds);
 }
 
-// Orders what follows in its basic block: N times a matrix instruction with
-// VALU others and EXP exponentials beside it.
-template <int N, int VALU, int EXP> __device__ inline void beside()
+// Orders what follows in its basic block, N times: the matrix instructions of one
+// fragment, and beside them READ reads of LDS, VALU others and EXP exponentials.
+// Without it every product waits for the read of its own operand.
+template <typename T, int N, int READ, int VALU, int EXP> __device__ inline void beside()
 {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, sizeof(T) == 4 ? 4 : 1, 0);
+        if (READ)
+            __builtin_amdgcn_sched_group_barrier(0x100, READ, 0);
         if (VALU)
             __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
         if (EXP)

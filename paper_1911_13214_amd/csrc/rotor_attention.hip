@@ -191,13 +191,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
         add_rows<T, NB>(w.acc, last_vals, rd, before);
         before = Packed<T, NB>(s);
         before.pin();
-        if constexpr (sizeof(T) == 2) {
-            reads<2 * NB>();
-            beside<S::NK / 2, 4, 0>();
-            reads<2 * NB>();
-            beside<S::NK / 2, 4, 0>();
-            beside<2 * NB, 2, 16 / (2 * NB)>();
-        }
+        constexpr int kColumns = S::kGroups * NB, kReads = S::kTurned * kColumns;
+        beside<T, S::NK, kReads / S::NK, 32 / S::NK, 0>();
+        beside<T, kColumns, 0, 2, 16 / kColumns>();
         __builtin_amdgcn_sched_barrier(0);
         if (raised)
             w.scale(by);

@@ -117,21 +117,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
         lk.load(keys, row_at(k0, j, k_stride), hi + 1 - j, k_stride, row_bytes);
         lv.load(vals, row_at(v0, j, v_stride), hi + 1 - j, v_stride, row_bytes);
     };
-    // from scores and do v to gradients of scores
-    auto slope = [&](f32x16 &s, const f32x16 &dp) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float x = dp[e] - delta;
-            s[e] *= Scaled<T>::kOn ? x * factor : x;
-        }
-    };
-    auto mask = [&](f32x16 &s, int j) {
+    auto mask = [&](f32x16 &s, int j, float none) {
         const int je = j + kTileKeys - 1;
         if (!some || je > wlo || (je >= a.sinks && j < all_from)) {
             asm volatile("");  // a branch: few steps need it
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                s[e] = sight(j + row_of(e, h)) ? s[e] : 0.f;
+                s[e] = sight(j + row_of(e, h)) ? s[e] : none;
+        }
+    };
+    // scores and do v to gradients of scores
+    auto slope = [&](f32x16 &s, const f32x16 &dp) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float x = dp[e] - delta;
+            s[e] *= Scaled<T>::kOn ? x * factor : x;
         }
     };
 
@@ -146,6 +146,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
         F f[S::NK];
         fetch_rows<T, NB>(vals, rd, f);
         load(free_keys, free_vals, j2);
+        mask(s, j, -kInf);  // before the exponentials: their gradients are 0 times what is finite
         __builtin_amdgcn_sched_barrier(0);
         f32x16 dp, ahead;
         multiply<T>(dp, f, d);
@@ -155,8 +156,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
         fetch_rows<T, NB>(next_keys, rd, f);
         multiply<T>(ahead, f, q);
         slope(s, dp);
-        mask(s, j);
         add_rows<T, NB>(acc, keys, rd, Packed<T, NB>(s));
+        constexpr int kColumns = S::kGroups * NB, kReads = S::kTurned * kColumns;
+        beside<T, S::NK, 1, 16 / S::NK, 16 / S::NK>();
+        beside<T, S::NK, kReads / S::NK, 40 / S::NK, 0>();
+        beside<T, kColumns, 0, 1, 0>();
+        __builtin_amdgcn_sched_barrier(0);
         s = ahead;
         j = j1;
         j1 = j2;
@@ -186,7 +191,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
             for (int e = 0; e < 16; ++e)
                 s[e] = exp2_of(__builtin_fmaf(s[e], a.c, -lse));
             slope(s, dp);
-            mask(s, j);
+            mask(s, j, 0.f);
             add_rows_apart<T, NB>(acc, keys0, lane, s);
             tile_barrier();
         }
@@ -298,16 +303,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
             if (r + 32 <= some0 || r >= some1)
                 return;
             const bool all = r >= all0 && r + 32 <= all1;
-            f32x16 s = product<T, NB>(qt, rd, kf), ds;
+            constexpr int kColumns = S::kGroups * NB, kReads = S::kTurned * kColumns;
+            F g[kHeld ? S::NK : 1];
+            f32x16 s, ds;
+            s = product<T, NB>(qt, rd, kf);
             if constexpr (kHeld) {
-                ds = product<T, NB>(dt, rd, vf);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    ds[e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < S::NK; ++k)
-                    ds = Frag<T>::mma(rd.row(dt, k), rd.row(values + wave * 32 * S::kRow, k), ds);
+                fetch_rows<T, NB>(dt, rd, g);
+                reads<S::NK>();
+                beside<T, S::NK, 1, 0, 0>();
+                __builtin_amdgcn_sched_barrier(0);
             }
             float factor = 1.f;
             if constexpr (Scaled<T>::kOn) {
@@ -323,36 +327,67 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
                 }
                 factor = power_of(-exponent);
             }
+            // (a row's place, -1 for none, is below every key it does not see)
+            auto mask = [&](f32x16 &x, float none) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *(const f32x4 *)(st + 8 * g + 4 * h), dl = *(const f32x4 *)(st + 64 + 8 * g + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[4 * g + e] = exp2_of(__builtin_fmaf(s[4 * g + e], a.c, -l[e]));
-                    const float x = ds[4 * g + e] - dl[e];
-                    ds[4 * g + e] = s[4 * g + e] * (Scaled<T>::kOn ? x * factor : x);
-                }
-            }
-            if (!all) {
-                asm volatile("");  // a branch: few tiles need it
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
+                for (int i = 0; i < 4; ++i) {
                     typedef int i32x4 __attribute__((ext_vector_type(4)));
-                    const i32x4 p = *(const i32x4 *)(st + 128 + 8 * g + 4 * h);
+                    const i32x4 p = *(const i32x4 *)(st + 128 + 8 * i + 4 * h);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const bool in = key <= p[e] && (key > p[e] - a.window || key < a.sinks);
-                        s[4 * g + e] = in ? s[4 * g + e] : 0.f;
-                        ds[4 * g + e] = in ? ds[4 * g + e] : 0.f;
+                        const bool in = (key <= p[e]) & ((key > p[e] - a.window) | (key < a.sinks));
+                        x[4 * i + e] = in ? x[4 * i + e] : none;
                     }
                 }
+            };
+            if (kHeld && !all) {
+                asm volatile("");  // a branch: few tiles need it
+                mask(s, -kInf);  // before the exponentials: their gradients are 0 times what is finite
+            }
+            if constexpr (kHeld) {
+                __builtin_amdgcn_sched_barrier(0);
+                multiply<T>(ds, g, vf);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    ds[e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < S::NK; ++k)
+                    ds = Frag<T>::mma(rd.row(dt, k), rd.row(values + wave * 32 * S::kRow, k), ds);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 l = *(const f32x4 *)(st + 8 * i + 4 * h), dl = *(const f32x4 *)(st + 64 + 8 * i + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[4 * i + e] = exp2_of(__builtin_fmaf(s[4 * i + e], a.c, -l[e]));
+                    const float x = ds[4 * i + e] - dl[e];
+                    ds[4 * i + e] = s[4 * i + e] * (Scaled<T>::kOn ? x * factor : x);
+                }
+            }
+            if (!kHeld && !all) {
+                asm volatile("");
+                mask(s, 0.f);
+                mask(ds, 0.f);
             }
             if constexpr (kApart) {
+                if (kHeld && !all)
+                    mask(ds, 0.f);
                 add_rows_apart<T, NB>(dv, dt, lane, s);
                 add_rows_apart<T, NB>(dk, qt, lane, ds);
             } else {
                 add_rows<T, NB>(dv, dt, rd, Packed<T, NB>(s));
                 add_rows<T, NB>(dk, qt, rd, Packed<T, NB>(ds));
+                // (past 96 columns no registers are left for reads ahead: so ordered,
+                // 16384 tokens, 32 heads on 8, 128 wide take 6.3 ms instead of 4.5)
+                if constexpr (kHeld) {
+                    reads<4>();
+                    beside<T, S::NK, 1, 16 / S::NK, 16 / S::NK>();
+                    reads<S::kTurned>();
+                    beside<T, kColumns, S::kTurned, 40 / kColumns, 0>();
+                    beside<T, kColumns, S::kTurned, 1, 0>();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         };
         auto use = [&](int i, const char *qt, const char *dt, const float *st) {
