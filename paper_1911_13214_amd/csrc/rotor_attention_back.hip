@@ -303,15 +303,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
             if (r + 32 <= some0 || r >= some1)
                 return;
             const bool all = r >= all0 && r + 32 <= all1;
-            constexpr int kColumns = S::kGroups * NB, kReads = S::kTurned * kColumns;
-            F g[kHeld ? S::NK : 1];
-            f32x16 s, ds;
-            s = product<T, NB>(qt, rd, kf);
+            f32x16 s = product<T, NB>(qt, rd, kf), ds;
             if constexpr (kHeld) {
-                fetch_rows<T, NB>(dt, rd, g);
-                reads<S::NK>();
-                beside<T, S::NK, 1, 0, 0>();
-                __builtin_amdgcn_sched_barrier(0);
+                ds = product<T, NB>(dt, rd, vf);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    ds[e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < S::NK; ++k)
+                    ds = Frag<T>::mma(rd.row(dt, k), rd.row(values + wave * 32 * S::kRow, k), ds);
             }
             float factor = 1.f;
             if constexpr (Scaled<T>::kOn) {
@@ -328,7 +329,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
                 factor = power_of(-exponent);
             }
             // (a row's place, -1 for none, is below every key it does not see)
-            auto mask = [&](f32x16 &x, float none) {
+            auto mask = [&](f32x16 &x) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -336,25 +337,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const bool in = (key <= p[e]) & ((key > p[e] - a.window) | (key < a.sinks));
-                        x[4 * i + e] = in ? x[4 * i + e] : none;
+                        x[4 * i + e] = in ? x[4 * i + e] : 0.f;
                     }
                 }
             };
-            if (kHeld && !all) {
-                asm volatile("");  // a branch: few tiles need it
-                mask(s, -kInf);  // before the exponentials: their gradients are 0 times what is finite
-            }
-            if constexpr (kHeld) {
-                __builtin_amdgcn_sched_barrier(0);
-                multiply<T>(ds, g, vf);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    ds[e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < S::NK; ++k)
-                    ds = Frag<T>::mma(rd.row(dt, k), rd.row(values + wave * 32 * S::kRow, k), ds);
-            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x4 l = *(const f32x4 *)(st + 8 * i + 4 * h), dl = *(const f32x4 *)(st + 64 + 8 * i + 4 * h);
@@ -365,29 +351,17 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
                     ds[4 * i + e] = s[4 * i + e] * (Scaled<T>::kOn ? x * factor : x);
                 }
             }
-            if (!kHeld && !all) {
-                asm volatile("");
-                mask(s, 0.f);
-                mask(ds, 0.f);
+            if (!all) {
+                asm volatile("");  // a branch: few tiles need it
+                mask(s);
+                mask(ds);
             }
             if constexpr (kApart) {
-                if (kHeld && !all)
-                    mask(ds, 0.f);
                 add_rows_apart<T, NB>(dv, dt, lane, s);
                 add_rows_apart<T, NB>(dk, qt, lane, ds);
             } else {
                 add_rows<T, NB>(dv, dt, rd, Packed<T, NB>(s));
                 add_rows<T, NB>(dk, qt, rd, Packed<T, NB>(ds));
-                // (past 96 columns no registers are left for reads ahead: so ordered,
-                // 16384 tokens, 32 heads on 8, 128 wide take 6.3 ms instead of 4.5)
-                if constexpr (kHeld) {
-                    reads<4>();
-                    beside<T, S::NK, 1, 16 / S::NK, 16 / S::NK>();
-                    reads<S::kTurned>();
-                    beside<T, kColumns, S::kTurned, 40 / kColumns, 0>();
-                    beside<T, kColumns, S::kTurned, 1, 0>();
-                    __builtin_amdgcn_sched_barrier(0);
-                }
             }
         };
         auto use = [&](int i, const char *qt, const char *dt, const float *st) {
