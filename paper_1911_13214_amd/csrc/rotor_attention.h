@@ -170,6 +170,14 @@ __device__ inline void tile_barrier()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// Waits until at most LEFT of this wave's loads into LDS are on their way.
+template <int LEFT> __device__ inline void arrived()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // A lane's places in a tile of LDS, from which fragments are read.
 template <typename T, int NB> struct Reader {
     typedef Shape<T, NB> S;

@@ -7,7 +7,7 @@
 namespace rotor {
 namespace {
 
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 32;  // the most that few_kernel takes at a time, and that it is chosen for
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
@@ -243,42 +243,96 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
 #endif
 }
 
-// Up to 32 rows of a key head: the waves share the rows and split the keys.
-// Each has tiles of 32 keys of its own in LDS, the next on its way while one is
+// Products of few rows: 16 x 16 tiles, so that no more of them is empty than
+// need be.  A lane holds row lane % 16; of a result's registers, key
+// 4 (lane / 16) + e.
+template <typename T> struct Mfma16;
+template <> struct Mfma16<bf16> {
+    static __device__ f32x4 run(Frag<bf16>::F a, Frag<bf16>::F b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mfma16<f16> {
+    static __device__ f32x4 run(Frag<f16>::F a, Frag<f16>::F b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mfma16<float> {
+    static __device__ f32x4 run(Frag<float>::F a, Frag<float>::F b, f32x4 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// Over the four lanes that hold a row.
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ inline Both quarters(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v),
+                                                    false, false);
+    const uint32_t low = r[0], high = r[1];
+    return Both{__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+__device__ inline float row_max(float v)
+{
+    const Both b = quarters(halves_max(v));
+    return fmaxf(b.low, b.high);
+}
+__device__ inline float row_sum(float v)
+{
+    const Both b = quarters(halves_sum(v));
+    return b.low + b.high;
+}
+#endif
+
+// A few rows of a key head: the waves share R * 16 of them and split the keys.
+// Each has tiles of keys of its own in LDS, the next on its way while one is
 // used, and waits for no other before the end, when the waves' sums are joined.
 // The keys that any row sees are a list: the first ones, then the window's.
 // STEP: one token, whose key and value are new: they are in the place of the
 // last key of the list, and go into the cache.
-template <typename T, int NB, bool STEP>
-__global__ __launch_bounds__(256, 1) void few_kernel(Attention a)
+template <typename T, int NB, int R, bool STEP>
+__global__ __launch_bounds__(kThreads, 1) void few_kernel(Attention a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef Shape<T, NB> S;
-    constexpr int W = sizeof(T) == 4 ? 2 : 4;  // waves that have tiles
-    constexpr int kBytes = 32 * S::kRow, kAtOnce = 64 / S::kPieces, kLoads = 32 / kAtOnce;
-    __shared__ __attribute__((aligned(1024))) char tiles[W][2][2][kBytes];
-    __shared__ float2 soft[W][32];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
+    typedef typename Frag<T>::F F;
+    constexpr int kKeys = sizeof(T) == 4 ? 16 : 32, KT = kKeys / 16;  // of a tile
+    constexpr int kBytes = kKeys * S::kRow, kAtOnce = 64 / S::kPieces, kLoads = kKeys / kAtOnce;
+    constexpr int NK = NB * 32 * (int)sizeof(T) / 64, ND = NB * 2;  // fragments of a row, blocks of 16 columns
+    // one array a place: a read waits for the loads into its own array alone
+    __shared__ __attribute__((aligned(1024))) char keys_even[kWaves * kBytes], keys_odd[kWaves * kBytes];
+    __shared__ __attribute__((aligned(1024))) char vals_even[kWaves * kBytes], vals_odd[kWaves * kBytes];
+    __shared__ float2 soft[kWaves][R * 16];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
     const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
-    const int r0 = blockIdx.y * kFewRows, row = r0 + lane % 32;
+    const int r0 = blockIdx.y * (R * 16);
     const Span span(a, b);
-    const int t = row / a.group, p = span.offset + t;
-    const bool seen = row < a.rows && p >= 0 && p < span.length;
-    Rows<T, NB> w;
-    w.reset();
-    {
-        const char *q = rows_of(a.q, b, kv * a.group + row % a.group) + t * a.q.token;
+    F q[R][NK];
+    f32x4 acc[R][ND];
+    float top[R], sum[R];
+    Sight sight[R];
 #pragma unroll
-        for (int k = 0; k < S::NK; ++k)
-            w.q[k] = global_frag<T>(q, seen, 2 * k + h, a.width);
+    for (int x = 0; x < R; ++x) {
+        const int row = r0 + x * 16 + lane % 16, t = row / a.group, p = span.offset + t;
+        const bool seen = row < a.rows && p >= 0 && p < span.length;
+        const char *at = rows_of(a.q, b, kv * a.group + row % a.group) + t * a.q.token;
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+            q[x][k] = global_frag<T>(at, seen, 4 * k + h, a.width);
+        sight[x] = Sight{p - a.window + 1, p, a.sinks};
     }
     int lo = 0, hi = -1;
-    const bool some = span.positions(r0 / a.group, min(a.rows - 1, r0 + kFewRows - 1) / a.group, lo, hi);
+    const bool some = span.positions(r0 / a.group, min(a.rows - 1, r0 + R * 16 - 1) / a.group, lo, hi);
     const int from = max(0, lo - a.window + 1), ahead = min(a.sinks, from);
     const int n = some ? ahead + hi - from + 1 : 0;
     const int share = (n + a.parts - 1) / a.parts;
     const int e0 = min(n, (int)blockIdx.z * share), e1 = min(n, e0 + share);
-    const Sight sight{p - a.window + 1, p, a.sinks};
     // position of the list's element e
     auto position = [&](int e) { return e < ahead ? e : from + e - ahead; };
     // rounds that the ring has made before the window's first key
@@ -292,11 +346,10 @@ __global__ __launch_bounds__(256, 1) void few_kernel(Attention a)
         return a.sinks + x;
     };
     const char *const k0 = rows_of(a.k, b, kv), *const v0 = rows_of(a.v, b, kv);
-    const bool whole = a.width == NB * 32;
 
     // Rows past the end are the last one again: their probabilities are 0, and
     // what they hold is what the rows see anyway.
-    auto load = [&](char (&to)[2][kBytes], int e) {
+    auto load = [&](char *keys, char *vals, int e) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r = i * kAtOnce + lane / S::kPieces;
@@ -304,13 +357,12 @@ __global__ __launch_bounds__(256, 1) void few_kernel(Attention a)
             c = c * Frag<T>::N < a.width ? c : 0;
             const int j = slot(position(min(e + r, e1 - 1)));
             __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(k0 + j * a.k.token + c * 16),
-                                             (lds_ptr)(to[0] + i * 1024), 16, 0, 0);
+                                             (lds_ptr)(keys + i * 1024), 16, 0, 0);
             __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(v0 + j * a.v.token + c * 16),
-                                             (lds_ptr)(to[1] + i * 1024), 16, 0, 0);
+                                             (lds_ptr)(vals + i * 1024), 16, 0, 0);
         }
     };
     // the new key and value: a piece a lane
-    typedef typename Frag<T>::F F;
     F fresh[2] = {{}, {}};
     const int piece = lane % S::kPieces;
     const bool mine = STEP && e0 < e1 && e1 == n;  // this part has the last key
@@ -323,178 +375,293 @@ __global__ __launch_bounds__(256, 1) void few_kernel(Attention a)
             *(F *)(rows_of(a.v, b, kv) + j * a.v.token + piece * 16) = fresh[1];
         }
     }
-    Reader<T, NB> rd;
-    rd.init(lane);
-    auto pass = [&](auto apart) {
+    // places of a lane in a tile: fragments of rows, and of columns
+    const int straight = lane % 16 * S::kRow + (h ^ S::turn(lane % 16)) * 16;
+    const int across = 4 * h + (sizeof(T) == 4 ? 0 : lane % 16 / 4);
+    auto column = [&](const char *vals, int m) __attribute__((always_inline)) {  // block m of 16 columns, keys as a result's registers have them
+        if constexpr (sizeof(T) == 2) {
+            const int at = across * S::kRow + ((2 * m + lane % 4 / 2) ^ S::turn(across)) * 16 + lane % 2 * 8;
+            return __builtin_bit_cast(F, __builtin_shufflevector(turned(vals + at), turned(vals + at + 16 * S::kRow), 0,
+                                                                 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            F f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                f[e] = *(const float *)(vals + (across + e) * S::kRow +
+                                        ((4 * m + lane % 16 / 4) ^ S::turn(across + e)) * 16 + lane % 4 * 4);
+            return f;
+        }
+    };
+
+    auto use = [&](auto apart, char *keys, char *vals, int e) __attribute__((always_inline)) {
         constexpr bool kApart = decltype(apart)::value;
-        int e = e0 + wave * 32, which = 0;
-        if (wave < W && e < e1)
-            load(tiles[wave][0], e);
-        for (; wave < W && e < e1; e += 32 * W, which ^= 1) {
-            const bool more = e + 32 * W < e1;
-            __builtin_amdgcn_sched_barrier(0);
-            if (more) {
-                // what read this place is done: its results were used
-                load(tiles[wave][which ^ 1], e + 32 * W);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
-            } else {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (mine && e + kKeys >= n) {
+            // in the place of the last key, and of what follows it there
+            for (int r = n - 1 - e + lane / S::kPieces; r < kKeys; r += kAtOnce) {
+                *(F *)(keys + r * S::kRow + (piece ^ S::turn(r)) * 16) = fresh[0];
+                *(F *)(vals + r * S::kRow + (piece ^ S::turn(r)) * 16) = fresh[1];
             }
-            __builtin_amdgcn_sched_barrier(0);
-            char *keys = tiles[wave][which][0], *vals = tiles[wave][which][1];
-            if (mine && e + 32 >= n) {
-                // in the place of the last key, and of what follows it there
-                for (int r = n - 1 - e + lane / S::kPieces; r < 32; r += kAtOnce) {
-                    *(F *)(keys + r * S::kRow + (piece ^ S::turn(r)) * 16) = fresh[0];
-                    *(F *)(vals + r * S::kRow + (piece ^ S::turn(r)) * 16) = fresh[1];
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
-            f32x16 s;
-            if (whole) {
-                s = product<T, NB>(keys, rd, w.q);
-            } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        f32x4 s[R][KT];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+            for (int x = 0; x < R; ++x)
+                s[x][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                F f = *(const F *)(keys + t * 16 * S::kRow + (straight ^ (k * 64)));
                 // columns past the width hold others again: they count as 0
+                if ((4 * k + h) * Frag<T>::N >= a.width)
+                    f = F{};
 #pragma unroll
-                for (int x = 0; x < 16; ++x)
-                    s[x] = 0.f;
+                for (int x = 0; x < R; ++x)
+                    s[x][t] = Mfma16<T>::run(f, q[x][k], s[x][t]);
+            }
+        }
 #pragma unroll
-                for (int k = 0; k < S::NK; ++k) {
-                    F f = rd.row(keys, k);
-                    if ((2 * k + h) * Frag<T>::N >= a.width)
-                        f = F{};
-                    s = Frag<T>::mma(f, w.q[k], s);
+        for (int x = 0; x < R; ++x) {
+            float most = -kInf;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = e + 16 * t + 4 * h + i;
+                    s[x][t][i] = (at < e1) & sight[x](position(at)) ? s[x][t][i] : -kInf;
+                    most = fmaxf(most, s[x][t][i]);
                 }
-            }
+            most = row_max(most);
+            if (__any((most - top[x]) * a.c > kSlack)) {  // (-inf - -inf is NaN: no)
+                const float next = fmaxf(top[x], most), by = next > top[x] ? exp2_of((top[x] - next) * a.c) : 1.f;
+                sum[x] *= by;
+                top[x] = next;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                const int at = e + row_of(x, h);
-                s[x] = at < e1 && sight(position(at)) ? s[x] : -kInf;
+                for (int m = 0; m < ND; ++m)
+                    acc[x][m] *= by;
             }
-            float by;
-            if (w.raise(s, a.c, by))
-                w.scale(by);
-            w.soften(s, a.c);
-            if constexpr (kApart)
-                add_rows_apart<T, NB>(w.acc, vals, lane, s);
-            else
-                add_rows<T, NB>(w.acc, vals, rd, Packed<T, NB>(s));
+            const float base = top[x] == -kInf ? 0.f : top[x] * a.c;
+            F p[sizeof(T) == 4 ? KT : 1];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[x][t][i] = exp2_of(__builtin_fmaf(s[x][t][i], a.c, -base));
+                    sum[x] += s[x][t][i];
+                    p[sizeof(T) == 4 ? t : 0][sizeof(T) == 4 ? i : 4 * t + i] = (T)s[x][t][i];
+                }
+            if constexpr (kApart) {
+                // key by key, for infinities or NaN among the values: a row that does
+                // not see a key takes nothing from it
+#pragma unroll 1
+                for (int key = 0; key < kKeys; ++key) {
+                    float w = 0.f;
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            w = key / 16 == t && key % 4 == i ? s[x][t][i] : w;
+                    w = (float)(T)__shfl(w, lane % 16 + key % 16 / 4 * 16);
+#pragma unroll
+                    for (int m = 0; m < ND; ++m)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int at = (16 * m + 4 * h + i) * (int)sizeof(T);
+                            const float v =
+                                (float)*(const T *)(vals + key * S::kRow + ((at / 16) ^ S::turn(key)) * 16 + at % 16);
+                            acc[x][m][i] = w != 0.f ? __builtin_fmaf(w, v, acc[x][m][i]) : acc[x][m][i];
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int m = 0; m < ND; ++m)
+                    acc[x][m] = Mfma16<T>::run(column(vals, m), p[0], acc[x][m]);
+            }
+        }
+    };
+    auto pass = [&](auto apart) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < R; ++x) {
+            top[x] = -kInf;
+            sum[x] = 0.f;
+#pragma unroll
+            for (int m = 0; m < ND; ++m)
+                acc[x][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        constexpr int kStride = kKeys * kWaves;
+        char *const ke = keys_even + wave * kBytes, *const ko = keys_odd + wave * kBytes;
+        char *const ve = vals_even + wave * kBytes, *const vo = vals_odd + wave * kBytes;
+        int e = e0 + wave * kKeys;
+        if (e < e1)
+            load(ke, ve, e);
+        for (; e < e1; e += 2 * kStride) {
+            // (what read the other place is done: its results were used)
+            const int e2 = e + kStride, e3 = e + 2 * kStride;
+            if (e2 < e1) {
+                load(ko, vo, e2);
+                arrived<2 * kLoads>();
+            } else {
+                arrived<0>();
+            }
+            use(apart, ke, ve, e);
+            if (e2 >= e1)
+                break;
+            if (e3 < e1) {
+                load(ke, ve, e3);
+                arrived<2 * kLoads>();
+            } else {
+                arrived<0>();
+            }
+            use(apart, ko, vo, e2);
         }
     };
     pass(std::false_type{});
-    if (__syncthreads_or(!finite(w.acc))) {
-        w.reset();
-        pass(std::true_type{});
-        __syncthreads();
+    bool clean = true;
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+        float t = 0.f;
+#pragma unroll
+        for (int m = 0; m < ND; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                t += acc[x][m][i] * 0.f;
+        clean &= t == 0.f;
     }
+    if (__syncthreads_or(!clean))
+        pass(std::true_type{});
 
     // the waves' sums: relative to the highest maximum, added in order
-    if (wave < W)
-        w.sum = halves_sum(w.sum);
-    if (wave < W && h == 0)
-        soft[wave][lane] = make_float2(w.top, w.sum);
-    __syncthreads();
-    float top = -kInf, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < W; ++i)
-        top = fmaxf(top, soft[i][lane % 32].x);
-    const float base = top == -kInf ? 0.f : top;
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-        sum += soft[i][lane % 32].y * exp2_of((soft[i][lane % 32].x - base) * a.c);
-    // a wave's 32 rows of sums, skewed by 16 bytes for the banks' sake
-    constexpr int kLine = NB * 32 + 4;
-    float *const lines = (float *)tiles;
-    static_assert(W * 32 * kLine * 4 <= (int)sizeof(tiles), "all waves' sums");
-    if (wave < W) {
-        const float by = exp2_of((w.top - base) * a.c);
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *(f32x4 *)(lines + (wave * 32 + lane % 32) * kLine + 32 * i + 8 * r + 4 * h) =
-                    f32x4{w.acc[i][4 * r], w.acc[i][4 * r + 1], w.acc[i][4 * r + 2], w.acc[i][4 * r + 3]} * by;
+    for (int x = 0; x < R; ++x) {
+        sum[x] = row_sum(sum[x]);
+        if (h == 0)
+            soft[wave][x * 16 + lane] = make_float2(top[x], sum[x]);
     }
-    __shared__ float2 joined[32];
-    if (wave == 0 && h == 0)
-        joined[lane] = make_float2(top, sum);
-    __syncthreads();
-    // 8 lanes a row, four columns at a time
-    const int line = threadIdx.x / 8, rr = r0 + line;
-    if (rr >= a.rows)
-        return;
-    const float2 j = joined[line];
-    const int tt = rr / a.group, head = kv * a.group + rr % a.group, pp = span.offset + tt;
-    const bool sees = pp >= 0 && pp < span.length;
-    const int64_t part = ((int64_t)blockIdx.z * a.batch * a.kv + (int64_t)b * a.kv + kv) * a.rows + rr;
-    // a position past the cache of a single token has no result
-    const float none = STEP && span.offset >= 0 ? __builtin_nanf("") : 0.f;
-    for (int col = threadIdx.x % 8 * 4; col < a.width; col += 32) {
-        f32x4 v = *(const f32x4 *)(lines + line * kLine + col);
+    // a wave's 16 rows of sums, in pieces of 16 bytes that change places by the row
+    constexpr int kLine = S::kBlocks * 32;
+    static_assert(kWaves * 16 * kLine * 4 <= (int)sizeof(keys_even), "the waves' sums");
+    float *const lines = (float *)keys_even;
 #pragma unroll
-        for (int i = 1; i < W; ++i)
-            v += *(const f32x4 *)(lines + (i * 32 + line) * kLine + col);
-        if (a.parts > 1) {
-            *(f32x4 *)(a.part_out + part * a.width + col) = v;
-        } else {
-            typedef T V __attribute__((ext_vector_type(4)));
-            V x;
+    for (int x = 0; x < R; ++x) {
+        __syncthreads();
+        float most = -kInf;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                x[e] = (T)(sees ? v[e] / j.y : none);
-            *(V *)(rows_of(a.out, b, head) + tt * a.out.token + col * sizeof(T)) = x;
+        for (int i = 0; i < kWaves; ++i)
+            most = fmaxf(most, soft[i][x * 16 + lane % 16].x);
+        const float base = most == -kInf ? 0.f : most, by = exp2_of((top[x] - base) * a.c);
+#pragma unroll
+        for (int m = 0; m < ND; ++m)
+            *(f32x4 *)(lines + (wave * 16 + lane % 16) * kLine + ((4 * m + h) ^ (lane % 16)) * 4) = acc[x][m] * by;
+        __syncthreads();
+        // 16 threads a row, four columns at a time
+        const int line = threadIdx.x / 16, row = r0 + x * 16 + line;
+        if (row >= a.rows)
+            continue;
+        float all = -kInf, total = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i)
+            all = fmaxf(all, soft[i][x * 16 + line].x);
+        const float floor = all == -kInf ? 0.f : all;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i)
+            total += soft[i][x * 16 + line].y * exp2_of((soft[i][x * 16 + line].x - floor) * a.c);
+        const int t = row / a.group, head = kv * a.group + row % a.group, p = span.offset + t;
+        const bool seen = p >= 0 && p < span.length;
+        const int64_t part = ((int64_t)blockIdx.z * a.batch * a.kv + (int64_t)b * a.kv + kv) * a.rows + row;
+        // a position past the cache of a single token has no result
+        const float none = STEP && span.offset >= 0 ? __builtin_nanf("") : 0.f;
+        for (int c = threadIdx.x % 16; c * 4 < a.width; c += 16) {
+            f32x4 v = *(const f32x4 *)(lines + line * kLine + (c ^ line) * 4);
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i)
+                v += *(const f32x4 *)(lines + (i * 16 + line) * kLine + (c ^ line) * 4);
+            if (a.parts > 1) {
+                *(f32x4 *)(a.part_out + part * a.width + c * 4) = v;
+            } else {
+                typedef T V __attribute__((ext_vector_type(4)));
+                V o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    o[i] = (T)(seen ? v[i] / total : none);
+                *(V *)(rows_of(a.out, b, head) + t * a.out.token + c * 4 * sizeof(T)) = o;
+            }
         }
-    }
-    if (threadIdx.x % 8 == 0) {
-        if (a.parts > 1)
-            a.part_soft[part] = make_float2(j.x * a.c, j.y);
-        else if (a.lse)
-            a.lse[((int64_t)b * a.tokens + tt) * ((int64_t)a.kv * a.group) + head] =
-                sees ? (j.x * a.c + __builtin_amdgcn_logf(j.y)) * kLn2 : -kInf;
+        if (threadIdx.x % 16 == 0) {
+            if (a.parts > 1)
+                a.part_soft[part] = make_float2(all * a.c, total);
+            else if (a.lse)
+                a.lse[((int64_t)b * a.tokens + t) * ((int64_t)a.kv * a.group) + head] =
+                    seen ? (all * a.c + __builtin_amdgcn_logf(total)) * kLn2 : -kInf;
+        }
     }
 #endif
 }
 
-// The parts' sums of a row joined, in their order: four columns a thread.
+// The parts' sums of a row joined: a workgroup a row; four columns a thread and
+// 256 / 32 groups of threads for the parts, whose sums are added in order.
 template <typename T, bool STEP> __global__ __launch_bounds__(256) void join_kernel(Attention a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    const int per = (a.width + 3) / 4;
-    const int64_t heads = (int64_t)a.batch * a.kv, all = heads * a.rows;
-    const int64_t i = block_at() * 256 + threadIdx.x, at = i / per;
+    constexpr int kGroups = 8;
+    __shared__ f32x4 lines[kGroups][32];
+    __shared__ float2 whole[4];
+    const int64_t at = block_at(), all = (int64_t)a.batch * a.kv * a.rows;
     if (at >= all)
         return;
-    const int col = (int)(i - at * per) * 4, row = (int)(at % a.rows), bk = (int)(at / a.rows);
+    const int row = (int)(at % a.rows), bk = (int)(at / a.rows);
     const int b = bk / a.kv, kv = bk % a.kv, t = row / a.group, head = kv * a.group + row % a.group;
     const Span span(a, b);
     const int p = span.offset + t;
     const bool seen = p >= 0 && p < span.length;
-    float top = -kInf;
-    for (int k = 0; k < a.parts; ++k)
-        top = fmaxf(top, a.part_soft[k * all + at].x);
+    // every thread's part, its maximum and sum (there are at most 256)
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    float2 soft = make_float2(-kInf, 0.f);
+    if ((int)threadIdx.x < a.parts)
+        soft = a.part_soft[threadIdx.x * all + at];
+    float top = soft.x;
+#pragma unroll
+    for (int off = 32; off >= 1; off /= 2)
+        top = fmaxf(top, __shfl_xor(top, off));
     const float base = top == -kInf ? 0.f : top;
+    const float sum = wave_sum(soft.y * exp2_of(soft.x - base));
+    if (lane == 0)
+        whole[wave] = make_float2(top, sum);
+    __syncthreads();
+    float most = -kInf, total = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        most = fmaxf(most, whole[i].x);
+    const float floor = most == -kInf ? 0.f : most;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        total += whole[i].y * exp2_of(whole[i].x - floor);
+    const int group = threadIdx.x / 32, col = threadIdx.x % 32 * 4;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
+    if (col < a.width)
 #pragma unroll 4
-    for (int k = 0; k < a.parts; ++k) {
-        const float2 s = a.part_soft[k * all + at];
-        const float by = exp2_of(s.x - base);
-        sum += s.y * by;
-        const f32x4 o = *(const f32x4 *)(a.part_out + (k * all + at) * a.width + col);
-        // a part without keys has nothing to scale, whatever its factor
-        v += s.y != 0.f || s.x != -kInf ? o * by : f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+        for (int k = group; k < a.parts; k += kGroups) {
+            const float by = exp2_of(a.part_soft[k * all + at].x - floor);
+            v += *(const f32x4 *)(a.part_out + (k * all + at) * a.width + col) * by;
+        }
+    lines[group][threadIdx.x % 32] = v;
+    __syncthreads();
+    if (group > 0 || col >= a.width)
+        return;
+#pragma unroll
+    for (int i = 1; i < kGroups; ++i)
+        v += lines[i][threadIdx.x];
+    // a position past the cache of a single token has no result
     const float none = STEP && span.offset >= 0 ? __builtin_nanf("") : 0.f;
     typedef T V __attribute__((ext_vector_type(4)));
     V x;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        x[e] = (T)(seen ? v[e] / sum : none);
+        x[e] = (T)(seen ? v[e] / total : none);
     *(V *)(rows_of(a.out, b, head) + t * a.out.token + col * sizeof(T)) = x;
     if (col == 0 && a.lse)
         a.lse[((int64_t)b * a.tokens + t) * ((int64_t)a.kv * a.group) + head] =
-            seen ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -kInf;
+            seen ? (most + __builtin_amdgcn_logf(total)) * kLn2 : -kInf;
 #endif
 }
 
@@ -570,14 +737,19 @@ int32_t launch_forward(const rotor_attention *n, Attention &a, bool step, void *
         typedef typename decltype(e)::T T;
         constexpr int NB = decltype(nb)::v;
         const dim3 few(bk, (uint32_t)ceil_div(a.rows, kFewRows), z);
-        if (step)
-            few_kernel<T, NB, true><<<few, 256, 0, s>>>(a);
+        const bool one = a.rows <= 16;
+        if (step && one)
+            few_kernel<T, NB, 1, true><<<few, kThreads, 0, s>>>(a);
+        else if (step)
+            few_kernel<T, NB, 2, true><<<few, kThreads, 0, s>>>(a);
+        else if (p.few && one)
+            few_kernel<T, NB, 1, false><<<few, kThreads, 0, s>>>(a);
         else if (p.few)
-            few_kernel<T, NB, false><<<few, 256, 0, s>>>(a);
+            few_kernel<T, NB, 2, false><<<few, kThreads, 0, s>>>(a);
         else
             attention_kernel<T, NB><<<dim3(bk, (uint32_t)ceil_div(a.rows, kTileRows), z), kThreads, 0, s>>>(a);
         if (a.parts > 1) {
-            const dim3 grid = grid_of(ceil_div((int64_t)bk * a.rows * (a.width / 4), 256));
+            const dim3 grid = grid_of((int64_t)bk * a.rows);
             if (step)
                 join_kernel<T, true><<<grid, 256, 0, s>>>(a);
             else
