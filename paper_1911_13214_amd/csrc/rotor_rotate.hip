@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxPairs = ROTOR_ROTATE_MAX_WIDTH / 2;
-constexpr int kBlocks = 1024;  // of the gradients: each leaves one row of sums
+constexpr int kBlocks = 2048;  // of the gradients: each leaves one row of sums
 
 struct HeadRows {
     char *p;
@@ -35,18 +35,51 @@ struct RotateArgs {
     int tokens, heads[2], width, rotary, team;
     int64_t all;      // tokens of all sequences
     int turns, split; // rounds of heads, and into how many waves a token's are split
-    float eps;
-    float *sums;      // [block][2][width]
+    int splits[2], blocks_q;  // gradients: the same of q and k, workgroups that take q
+    float eps, by_width;  // by_width = 1 / width
+    float *sums;      // [block][width]
     uint64_t frequency[kMaxPairs];
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
-__device__ inline float team_sum(float v, int team)
+// Sums over teams of lanes, in registers: within four and eight lanes by their
+// neighbours, then by mirrors (the lanes of a half hold the same by then), past
+// 16 by swapped rows.
+template <int CTRL> __device__ inline float moved(float v)
 {
-    for (int off = team / 2; off >= 1; off /= 2)
-        v += __shfl_xor(v, off);
-    return v;
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <typename R> __device__ inline float both(const R &r)
+{
+    const uint32_t x = r[0], y = r[1];
+    return __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+}
+template <int N> __device__ inline void team_sum(float (&v)[N], int team)
+{
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = f(v[i]);
+    };
+    if (team >= 2)
+        each([](float x) { return x + moved<0xB1>(x); });
+    if (team >= 4)
+        each([](float x) { return x + moved<0x4E>(x); });
+    if (team >= 8)
+        each([](float x) { return x + moved<0x141>(x); });
+    if (team >= 16)
+        each([](float x) { return x + moved<0x140>(x); });
+    if (team >= 32)
+        each([](float x) {
+            const uint32_t b = __builtin_bit_cast(uint32_t, x);
+            return both(__builtin_amdgcn_permlane16_swap(b, b, false, false));
+        });
+    if (team >= 64)
+        each([](float x) {
+            const uint32_t b = __builtin_bit_cast(uint32_t, x);
+            return both(__builtin_amdgcn_permlane32_swap(b, b, false, false));
+        });
 }
 
 __device__ inline void turn_of(uint64_t phase, float &c, float &s)
@@ -74,7 +107,7 @@ __device__ inline void turn_of(uint64_t phase, float &c, float &s)
 // A lane's pairs of a head.
 template <typename T, int V, int N, bool INTER> struct Pairs {
     int first[N], col[N], apart[N];  // first pair; its columns
-    bool have[N];
+    bool have[N], turns[N];          // V divides the pairs that turn: all of them or none
     __device__ void init(const RotateArgs &a, int lane)
     {
         const int half = a.rotary / 2;
@@ -83,6 +116,7 @@ template <typename T, int V, int N, bool INTER> struct Pairs {
             const int s = (n * 64 + lane % a.team) * V;
             first[n] = s;
             have[n] = s < a.width / 2;
+            turns[n] = s < half;
             if (INTER) {
                 col[n] = 2 * s;
                 apart[n] = 0;
@@ -92,28 +126,44 @@ template <typename T, int V, int N, bool INTER> struct Pairs {
             }
         }
     }
-    __device__ void load(const T *p, bool row, float (&x)[N][2][V]) const
+    // Loads as they are, and their conversion: what is on its way takes half the
+    // registers, and nothing waits for it.
+    typedef typename VecOf<T, V>::V Half;
+    struct Raw {
+        Half x[N][2];
+    };
+    __device__ void fetch(const T *p, bool row, Raw &r) const
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                x[n][0][e] = x[n][1][e] = 0.f;
-            if (!row || !have[n])
-                continue;
-            if constexpr (INTER) {
-                float f[2 * V];
-                load_vec(p + col[n], f);
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    x[n][0][e] = f[2 * e];
-                    x[n][1][e] = f[2 * e + 1];
-                }
-            } else {
-                load_vec(p + col[n], x[n][0]);
-                load_vec(p + col[n] + apart[n], x[n][1]);
+            r.x[n][0] = r.x[n][1] = Half{};
+            if (row && have[n]) {
+                // (interleaved: the second half lies next to the first)
+                r.x[n][0] = *(const Half *)(p + col[n]);
+                r.x[n][1] = *(const Half *)(p + col[n] + (INTER ? V : apart[n]));
             }
         }
+    }
+    __device__ void unpack(const Raw &r, float (&x)[N][2][V]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if constexpr (INTER) {
+                    x[n][0][e] = (float)(2 * e < V ? r.x[n][0][2 * e % V] : r.x[n][1][2 * e % V]);
+                    x[n][1][e] = (float)(2 * e + 1 < V ? r.x[n][0][(2 * e + 1) % V] : r.x[n][1][(2 * e + 1) % V]);
+                } else {
+                    x[n][0][e] = (float)r.x[n][0][e];
+                    x[n][1][e] = (float)r.x[n][1][e];
+                }
+            }
+    }
+    __device__ void load(const T *p, bool row, float (&x)[N][2][V]) const
+    {
+        Raw r;
+        fetch(p, row, r);
+        unpack(r, x);
     }
     template <typename O> __device__ void store(O *p, bool row, const float (&x)[N][2][V]) const
     {
@@ -142,25 +192,24 @@ template <typename T, int V, int N, bool INTER> struct Pairs {
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const int i = first[n] + e;
                 c[n][e] = 1.f;
                 s[n][e] = 0.f;
-                if (i < a.rotary / 2)
-                    turn_of(position * a.frequency[i], c[n][e], s[n][e]);
+                if (turns[n])
+                    turn_of(position * a.frequency[first[n] + e], c[n][e], s[n][e]);
             }
     }
     // Rotates; what is not rotated is not touched (0 times infinity).
-    __device__ void rotate(const RotateArgs &a, float (&x)[N][2][V], const float (&c)[N][V], const float (&s)[N][V],
-                           float way) const
+    __device__ void rotate(float (&x)[N][2][V], const float (&c)[N][V], const float (&s)[N][V], float way) const
     {
 #pragma unroll
         for (int n = 0; n < N; ++n)
+            if (turns[n]) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const bool in = first[n] + e < a.rotary / 2;
-                const float u = x[n][0][e], v = x[n][1][e], t = s[n][e] * way;
-                x[n][0][e] = in ? u * c[n][e] - v * t : u;
-                x[n][1][e] = in ? v * c[n][e] + u * t : v;
+                for (int e = 0; e < V; ++e) {
+                    const float u = x[n][0][e], v = x[n][1][e], t = s[n][e] * way;
+                    x[n][0][e] = u * c[n][e] - v * t;
+                    x[n][1][e] = v * c[n][e] + u * t;
+                }
             }
     }
 };
@@ -176,21 +225,16 @@ template <int V, int N, typename F> __device__ inline void each(F f)
                 f(n, z, e);
 }
 
-// u to its normed row (and 1 / deviation).
-template <int V, int N, typename P>
-__device__ inline float normed(const RotateArgs &a, const P &at, float (&u)[N][2][V])
+// u less its mean, for layer norms.
+template <int V, int N, typename P> __device__ inline void centre(const RotateArgs &a, const P &at, float (&u)[N][2][V])
 {
-    if (a.norm == ROTOR_NORM_LAYER) {
-        float sum = 0.f;
-        each<V, N>([&](int n, int z, int e) { sum += u[n][z][e]; });
-        const float mean = team_sum(sum, a.team) / (float)a.width;
-        each<V, N>([&](int n, int z, int e) { u[n][z][e] = at.have[n] ? u[n][z][e] - mean : 0.f; });
-    }
-    float sum = 0.f;
-    each<V, N>([&](int n, int z, int e) { sum += u[n][z][e] * u[n][z][e]; });
-    const float r = 1.f / sqrtf(team_sum(sum, a.team) / (float)a.width + a.eps);
-    each<V, N>([&](int n, int z, int e) { u[n][z][e] *= r; });
-    return r;
+    if (a.norm != ROTOR_NORM_LAYER)
+        return;
+    float sum[1] = {0.f};
+    each<V, N>([&](int n, int z, int e) { sum[0] += u[n][z][e]; });
+    team_sum(sum, a.team);
+    const float mean = sum[0] * a.by_width;
+    each<V, N>([&](int n, int z, int e) { u[n][z][e] = at.have[n] ? u[n][z][e] - mean : 0.f; });
 }
 
 __device__ inline uint64_t position_of(const RotateArgs &a, int64_t b, int t)
@@ -201,10 +245,7 @@ __device__ inline uint64_t position_of(const RotateArgs &a, int64_t b, int t)
     return a.position_bytes == 8 ? (uint64_t)((const int64_t *)a.positions)[i]
                                  : (uint64_t)(int64_t)((const int32_t *)a.positions)[i];
 }
-__device__ inline char *row_at(const HeadRows &h, int64_t b, int t, int head)
-{
-    return h.p + b * h.batch + t * h.token + head * h.head;
-}
+__device__ inline char *token_at(const HeadRows &h, int64_t b, int t) { return h.p + b * h.batch + t * h.token; }
 #endif
 
 template <typename T, int V, int N, bool INTER> __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a)
@@ -219,112 +260,140 @@ template <typename T, int V, int N, bool INTER> __global__ __launch_bounds__(kTh
     const int t = (int)(n - b * a.tokens), teams = 64 / a.team;
     Pairs<T, V, N, INTER> at;
     at.init(a, lane);
+    const char *const in[2] = {token_at(a.in[0], b, t), token_at(a.in[1], b, t)};
+    char *const out[2] = {token_at(a.out[0], b, t), token_at(a.out[1], b, t)};
     float c[N][V], s[N][V];
     at.angles(a, position_of(a, b, t), c, s);
     for (int i = part; i < a.turns; i += a.split) {
         int head = i * teams + lane / a.team;
-        const bool row = head < a.heads[0] + a.heads[1];
-        const int z = head >= a.heads[0] ? 1 : 0;
+        const bool row = head < a.heads[0] + a.heads[1], z = head >= a.heads[0];
         head -= z ? a.heads[0] : 0;
-        float u[N][2][V], w[N][2][V];
-        at.load((const T *)row_at(a.in[z], b, t, head), row, u);
-        const T *weight = (const T *)a.weight[z];
-        if (weight)
-            at.load(weight, row, w);
+        const T *const x = (const T *)((z ? in[1] : in[0]) + head * (z ? a.in[1].head : a.in[0].head));
+        T *const y = (T *)((z ? out[1] : out[0]) + head * (z ? a.out[1].head : a.out[0].head));
+        float u[N][2][V];
+        at.load(x, row, u);
         if (a.norm != ROTOR_NORM_NONE) {
-            normed<V, N>(a, at, u);
+            const T *weight = (const T *)(z ? a.weight[1] : a.weight[0]);
+            float w[N][2][V];
+            each<V, N>([&](int n, int q, int e) { w[n][q][e] = 1.f; });
             if (weight)
-                each<V, N>([&](int p, int q, int e) { u[p][q][e] *= w[p][q][e]; });
+                at.load(weight, true, w);
+            centre<V, N>(a, at, u);
+            float sum[1] = {0.f};
+            each<V, N>([&](int n, int q, int e) { sum[0] += u[n][q][e] * u[n][q][e]; });
+            team_sum(sum, a.team);
+            const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], a.by_width, a.eps));
+            each<V, N>([&](int n, int q, int e) { u[n][q][e] *= r * w[n][q][e]; });
         }
-        at.rotate(a, u, c, s, 1.f);
-        at.store((T *)row_at(a.out[z], b, t, head), row, u);
+        at.rotate(u, c, s, 1.f);
+        at.store(y, row, u);
     }
 #endif
 }
 
+// The first `blocks_q` workgroups take the heads of q, the others those of k:
+// the sums of one weight's gradient fit the registers.
 template <typename T, int V, int N, bool INTER>
 __global__ __launch_bounds__(kThreads) void rotate_back_kernel(RotateArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, teams = 64 / a.team;
+    const int z = (int)blockIdx.x >= a.blocks_q ? 1 : 0, block = blockIdx.x - (z ? a.blocks_q : 0);
+    const int heads = a.heads[z], split = a.splits[z];
+    const int64_t stride = (int64_t)(z ? gridDim.x - a.blocks_q : a.blocks_q) * kWaves;
+    const T *weight = (const T *)a.weight[z];
+    const HeadRows in = a.in[z], out = a.out[z], grad = a.grad[z];
     Pairs<T, V, N, INTER> at;
     at.init(a, lane);
-    float sums[2][N][2][V];
-    for (int z = 0; z < 2; ++z)
-        each<V, N>([&](int p, int q, int e) { sums[z][p][q][e] = 0.f; });
-    const int64_t stride = (int64_t)gridDim.x * kWaves;
-    for (int64_t task = (int64_t)blockIdx.x * kWaves + wave; task < a.all * a.split; task += stride) {
-        const int64_t n = task / a.split, b = n / a.tokens;
-        const int t = (int)(n - b * a.tokens), part = (int)(task - n * a.split);
+    float sums[N][2][V];
+    each<V, N>([&](int p, int q, int e) { sums[p][q][e] = 0.f; });
+    for (int64_t task = (int64_t)block * kWaves + wave; task < a.all * split; task += stride) {
+        const int64_t n = task / split, b = n / a.tokens;
+        const int t = (int)(n - b * a.tokens), part = (int)(task - n * split);
+        const char *const grad_at = token_at(grad, b, t), *const in_at = token_at(in, b, t);
+        char *const out_at = token_at(out, b, t);
+        typename Pairs<T, V, N, INTER>::Raw next_g, next_u;
+        auto fetch = [&](int i) {
+            const int head = i + lane / a.team;
+            at.fetch((const T *)(grad_at + head * grad.head), head < heads, next_g);
+            if (a.norm != ROTOR_NORM_NONE)
+                at.fetch((const T *)(in_at + head * in.head), head < heads, next_u);
+        };
+        fetch(part * teams);
         float c[N][V], s[N][V];
         at.angles(a, position_of(a, b, t), c, s);
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-            float w[N][2][V];
-            const T *weight = (const T *)a.weight[z];
-            each<V, N>([&](int p, int q, int e) { w[p][q][e] = 1.f; });
-            if (weight)
-                at.load(weight, true, w);
-            for (int i = part * teams; i < a.heads[z]; i += a.split * teams) {
-                const int head = i + lane / a.team;
-                const bool row = head < a.heads[z];
-                float g[N][2][V], u[N][2][V];
-                at.load((const T *)row_at(a.grad[z], b, t, head), row, g);
-                if (a.norm != ROTOR_NORM_NONE)
-                    at.load((const T *)row_at(a.in[z], b, t, head), row, u);
-                at.rotate(a, g, c, s, -1.f);
-                if (a.norm != ROTOR_NORM_NONE) {
-                    const float r = normed<V, N>(a, at, u);
-                    float dot = 0.f, sum = 0.f;
-                    each<V, N>([&](int p, int q, int e) {
-                        sums[z][p][q][e] += row ? g[p][q][e] * u[p][q][e] : 0.f;
-                        g[p][q][e] *= w[p][q][e];
-                        dot += g[p][q][e] * u[p][q][e];
-                        sum += g[p][q][e];
-                    });
-                    dot = team_sum(dot, a.team) / (float)a.width;
-                    const float mean = a.norm == ROTOR_NORM_LAYER ? team_sum(sum, a.team) / (float)a.width : 0.f;
-                    each<V, N>([&](int p, int q, int e) { g[p][q][e] = r * (g[p][q][e] - mean - u[p][q][e] * dot); });
-                }
-                at.store((T *)row_at(a.out[z], b, t, head), row, g);
+        for (int i = part * teams; i < heads; i += split * teams) {
+            const int head = i + lane / a.team;
+            const bool row = head < heads;
+            float g[N][2][V], u[N][2][V];
+            at.unpack(next_g, g);
+            if (a.norm != ROTOR_NORM_NONE)
+                at.unpack(next_u, u);
+            if (i + split * teams < heads)
+                fetch(i + split * teams);
+            if (a.norm != ROTOR_NORM_NONE) {
+                float w[N][2][V];
+                each<V, N>([&](int p, int q, int e) { w[p][q][e] = 1.f; });
+                if (weight)
+                    at.load(weight, true, w);
+                at.rotate(g, c, s, -1.f);
+                centre<V, N>(a, at, u);
+                // of u^2, of the weighted gradient times u, and of it alone
+                float sum[3] = {0.f, 0.f, 0.f};
+                each<V, N>([&](int p, int q, int e) {
+                    const float y = g[p][q][e] * w[p][q][e];
+                    sum[0] += u[p][q][e] * u[p][q][e];
+                    sum[1] += y * u[p][q][e];
+                    sum[2] += y;
+                });
+                team_sum(sum, a.team);
+                const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], a.by_width, a.eps));
+                const float dot = sum[1] * r * a.by_width;
+                const float mean = a.norm == ROTOR_NORM_LAYER ? sum[2] * a.by_width : 0.f;
+                each<V, N>([&](int p, int q, int e) {
+                    const float v = u[p][q][e] * r;  // (0 where there is no head)
+                    sums[p][q][e] += row ? g[p][q][e] * v : 0.f;
+                    g[p][q][e] = r * (g[p][q][e] * w[p][q][e] - mean - v * dot);
+                });
+            } else {
+                at.rotate(g, c, s, -1.f);
             }
+            at.store((T *)(out_at + head * out.head), row, g);
         }
     }
     if (!a.sums)
         return;
     // over the teams, then over the waves in order
-    __shared__ float lines[kWaves][2][ROTOR_ROTATE_MAX_WIDTH];
-#pragma unroll
-    for (int z = 0; z < 2; ++z) {
-        each<V, N>([&](int p, int q, int e) {
-            for (int off = a.team; off < 64; off *= 2)
-                sums[z][p][q][e] += __shfl_xor(sums[z][p][q][e], off);
-        });
-        at.store(lines[wave][z], lane < a.team, sums[z]);
-    }
+    __shared__ float lines[kWaves][ROTOR_ROTATE_MAX_WIDTH];
+    each<V, N>([&](int p, int q, int e) {
+        for (int off = a.team; off < 64; off *= 2)
+            sums[p][q][e] += __shfl_xor(sums[p][q][e], off);
+    });
+    at.store(lines[wave], lane < a.team, sums);
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.width; i += kThreads) {
-        const int z = i / a.width, col = i - z * a.width;
-        float v = lines[0][z][col];
+    for (int col = threadIdx.x; col < a.width; col += kThreads) {
+        float v = lines[0][col];
 #pragma unroll
         for (int k = 1; k < kWaves; ++k)
-            v += lines[k][z][col];
-        a.sums[(int64_t)blockIdx.x * 2 * a.width + i] = v;
+            v += lines[k][col];
+        a.sums[(int64_t)blockIdx.x * a.width + col] = v;
     }
 #endif
 }
 
 // The blocks' sums joined in their order: 16 columns a workgroup, 16 strips of
-// blocks.
-template <typename T> __global__ __launch_bounds__(256) void join_kernel(const float *sums, int blocks, int width, T *dq, T *dk)
+// blocks; blockIdx.y: q, k.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const float *sums, int blocks_q, int blocks, int width, T *dq, T *dk)
 {
     __shared__ float strip[16][16];
     const int col = blockIdx.x * 16 + threadIdx.x % 16, k = threadIdx.x / 16, z = blockIdx.y;
+    const int end = z ? blocks : blocks_q;
     float v = 0.f;
     if (col < width)
 #pragma unroll 8
-        for (int i = k; i < blocks; i += 16)
-            v += sums[((int64_t)i * 2 + z) * width + col];
+        for (int i = (z ? blocks_q : 0) + k; i < end; i += 16)
+            v += sums[(int64_t)i * width + col];
     strip[k][threadIdx.x % 16] = v;
     __syncthreads();
     T *const out = z ? dk : dq;
@@ -369,12 +438,13 @@ template <int N> struct Num {
     static constexpr int v = N;
 };
 
-// Adjacent pairs of a lane: 16 bytes of columns where the halves allow it.
+// Adjacent pairs of a lane: four where they divide both parts of a head (with
+// eight, whole 16 bytes of 16-bit columns, the registers leave fewer waves: 4 x
+// 4096 tokens of 32 + 8 heads, 128 wide, bf16, gradients: 205 us, with four 157).
 int pairs_of(const rotor_head_rotation *n)
 {
-    const int most = n->interleaved || n->type == ROTOR_F32 ? 4 : 8;
-    for (int v = most; v > 1; v /= 2)
-        if (n->width / 2 % v == 0 && (n->interleaved || n->rotary / 2 % v == 0))
+    for (int v = 4; v > 1; v /= 2)
+        if (n->width / 2 % v == 0 && n->rotary / 2 % v == 0)
             return v;
     return 1;
 }
@@ -390,21 +460,13 @@ template <typename F> void with_pairs(const rotor_head_rotation *n, F f)
         else
             f(Num<1>{}, Num<2>{}, Num<1>{});
     } else {
-        if (v == 8)
-            f(Num<8>{}, Num<1>{}, Num<0>{});
-        else if (v == 4)
+        if (v == 4)
             f(Num<4>{}, Num<1>{}, Num<0>{});
         else if (v == 2)
             f(Num<2>{}, Num<1>{}, Num<0>{});
         else
             f(Num<1>{}, Num<2>{}, Num<0>{});
     }
-}
-
-int blocks_of(const rotor_head_rotation *n, int split)
-{
-    const int64_t want = ceil_div(n->batch * n->tokens * split, kWaves);
-    return (int)(want < kBlocks ? want : kBlocks);
 }
 
 bool fill(RotateArgs &a, const rotor_head_rotation *n)
@@ -436,6 +498,7 @@ bool fill(RotateArgs &a, const rotor_head_rotation *n)
     a.rotary = (int)n->rotary;
     a.all = n->batch * n->tokens;
     a.eps = (float)n->eps;
+    a.by_width = 1.f / (float)n->width;
     a.sums = nullptr;
     const int lanes = (int)n->width / 2 / pairs_of(n);
     a.team = 1;
@@ -449,7 +512,7 @@ bool fill(RotateArgs &a, const rotor_head_rotation *n)
 int split_of(int64_t all, int turns)
 {
     const int64_t want = all > 0 ? 8192 / all : 1;
-    return (int)(want < 1 ? 1 : want > turns ? turns : want);
+    return (int)(want < 1 || turns < 1 ? 1 : want > turns ? turns : want);
 }
 
 }  // namespace
@@ -490,7 +553,7 @@ int32_t rotor_head_norm_rotate_workspace_bytes(const rotor_head_rotation *how, u
 {
     if (!bytes || !rotation_ok(how))
         return ROTOR_EINVAL;
-    *bytes = how->norm == ROTOR_NORM_NONE ? 0 : (uint64_t)kBlocks * 2 * how->width * 4;
+    *bytes = how->norm == ROTOR_NORM_NONE ? 0 : (uint64_t)kBlocks * how->width * 4;
     return ROTOR_OK;
 }
 
@@ -516,11 +579,18 @@ int32_t rotor_head_norm_rotate_backward(const rotor_head_rotation *how, const ro
     const bool sums = d_dq_weight || d_dk_weight;
     if (sums && (!d_work || (uintptr_t)d_work % 16 || work_bytes < need))
         return ROTOR_EINVAL;
-    const int teams = 64 / a.team, most = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
-    a.turns = (int)ceil_div(most, teams);
-    a.split = split_of(a.all, a.turns);
+    // workgroups by the heads of each, one at least
+    const int teams = 64 / a.team;
+    int64_t want[2];
+    for (int z = 0; z < 2; ++z) {
+        a.splits[z] = split_of(a.all, (int)ceil_div(a.heads[z], teams));
+        want[z] = ceil_div(a.all * (a.heads[z] ? a.splits[z] : 0), kWaves);
+        const int64_t most = (int64_t)kBlocks * a.heads[z] / (a.heads[0] + a.heads[1]);
+        want[z] = want[z] > 0 && want[z] > most ? (most > 1 ? most : 1) : want[z];
+    }
+    a.blocks_q = (int)want[0];
+    const int blocks = (int)(want[0] + want[1]);
     a.sums = sums ? (float *)d_work : nullptr;
-    const int blocks = blocks_of(how, a.split);
     (void)hipGetLastError();  // an error the caller's earlier calls left behind is not this launch's
     with_type(how->type, [&](auto e) {
         typedef typename decltype(e)::T T;
@@ -531,7 +601,7 @@ int32_t rotor_head_norm_rotate_backward(const rotor_head_rotation *how, const ro
             });
         if (sums)
             join_kernel<T><<<dim3((uint32_t)ceil_div(how->width, 16), 2), 256, 0, (hipStream_t)stream>>>(
-                a.sums, blocks, a.width, (T *)d_dq_weight, (T *)d_dk_weight);
+                a.sums, a.blocks_q, blocks, a.width, (T *)d_dq_weight, (T *)d_dk_weight);
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
 }
