@@ -478,12 +478,16 @@ bool fill(RotateArgs &a, const rotor_head_rotation *n)
                           (uintptr_t)n->positions % (uintptr_t)n->position_bytes)))
         return false;
     for (int64_t i = 0; i < n->rotary / 2; ++i) {
-        if (!isfinite(n->frequencies[i]))
+        const double f = n->frequencies[i];
+        if (!isfinite(f))
             return false;
-        long double turn = (long double)n->frequencies[i] / 6.283185307179586476925286766559L;
-        turn -= floorl(turn);
-        const long double f = roundl(turn * 18446744073709551616.0L);
-        a.frequency[i] = f >= 18446744073709551616.0L ? 0 : (uint64_t)f;
+        // as a fraction of a turn; of less than half a turn it is one product
+        long double turn = (long double)f * 0.15915494309189533576888376337251436L;
+        if (!(fabs(f) < 3.14)) {
+            turn -= floorl(turn);
+            turn -= turn >= 0.5L ? 1.L : 0.L;
+        }
+        a.frequency[i] = (uint64_t)(int64_t)(turn * 18446744073709551616.0L);
     }
     a.weight[0] = n->q_weight;
     a.weight[1] = n->k_weight;

@@ -416,24 +416,23 @@ def linear_cross_entropy_backward(h, w, targets, lse, grad_loss, ignore=-100, *,
 
 # ---- heads: norms and rotation -------------------------------------------------------------
 
-def _heads(t, what, like=None, dims=(3, 4)):
-    """A tensor of heads, checked, as the C ABI takes it: strides in elements
-    of [batch, tokens, heads, width], 0 where there is one of something."""
-    _cuda(t, what)
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{what} must be {like.dtype} on {like.device}")
-    shape, stride = t.shape, t.stride()
-    if len(shape) not in dims:
-        raise ValueError(f"{what} must be [tokens, heads, width] or [batch, tokens, heads, width]" if 4 in dims else
-                         f"{what} must be [batch, heads, width]")
-    if shape[-1] > 1 and stride[-1] != 1:
+def _heads(t, what):
+    """A tensor of heads as the C ABI takes it: strides in elements of [batch,
+    tokens, heads, width], 0 for a batch that is left out."""
+    stride = t.stride()
+    if stride[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{what} must have a dense last dimension")
-    return rotor.Heads(t.data_ptr(), *((0,) * (4 - len(shape)) + tuple(0 if n == 1 else s for n, s in
-                                                                   zip(shape[:-1], stride[:-1]))))
+    if len(stride) == 4:
+        return rotor.Heads(t.data_ptr(), stride[0], stride[1], stride[2])
+    if len(stride) != 3:
+        raise ValueError(f"{what} must be [tokens, heads, width] or [batch, tokens, heads, width]")
+    return rotor.Heads(t.data_ptr(), 0, stride[0], stride[1])
 
 
 def _no_overlap(t, what):
     """A result's elements must lie in places of their own."""
+    if t.is_contiguous():
+        return t
     at = 1
     for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda x: x[1]):
         if s < at:
@@ -561,7 +560,7 @@ def head_norm_rotate_backward(dq, dk, q, k=None, *, norm="rms", q_weight=None, k
         if w is not None:
             g[name] = _empty(w)
     need = ctypes.c_uint64()
-    rotor._check(_entry("rotor_head_norm_rotate_workspace_bytes")(ctypes.byref(n), ctypes.byref(need)),
+    rotor._check(_entry("rotor_head_norm_rotate_workspace_bytes")(n, ctypes.byref(need)),
                  "rotor_head_norm_rotate_workspace_bytes")
     work = _scratch(need.value, q)
     _call("rotor_head_norm_rotate_backward", q.device, n, _heads(dq, "dq"), k if k is None else _heads(dk, "dk"),
@@ -614,12 +613,27 @@ def _batched(t, what):
     return t if t.dim() == 4 else t.unsqueeze(0)
 
 
-def _aligned(t, what, like=None, dims=(3, 4)):
-    """Heads that start 16-byte aligned."""
-    h, es = _heads(t, what, like, dims), t.element_size()
-    if t.numel() and (h.p % 16 or (h.batch | h.token | h.head) * es % 16):
-        raise ValueError(f"the heads of {what} must start 16-byte aligned")
+def _aligned(t, what):
+    """Heads that start 16-byte aligned (strides of one of something aside)."""
+    h = _heads(t, what)
+    if ((h.batch | h.token | h.head) * t.element_size() | h.p) % 16 and t.numel():
+        wrong = h.p % 16 or any(n > 1 and s * t.element_size() % 16 for n, s in zip(t.shape[:-1], t.stride()))
+        if wrong:
+            raise ValueError(f"the heads of {what} must start 16-byte aligned")
     return h
+
+
+@functools.lru_cache(maxsize=4096)
+def _attention_bytes(name, *sizes):
+    """Workspace of an attention's entry point for these sizes."""
+    keys = ("type", "batch", "tokens", "keys", "heads", "kv_heads", "width", "window", "sinks")
+    n, need = rotor.Attention(scale=1.0, **dict(zip(keys, sizes))), ctypes.c_uint64()
+    rotor._check(_entry(name)(n, *sizes[len(keys):], ctypes.byref(need)), name)
+    return need.value
+
+
+def _sizes(n):
+    return n.type, n.batch, n.tokens, n.keys, n.heads, n.kv_heads, n.width, n.window, n.sinks
 
 
 def window_attention(q, k, v, *, window=None, sinks=0, scale=None, positions=None, lengths=None, stats=True,
@@ -645,12 +659,10 @@ def window_attention(q, k, v, *, window=None, sinks=0, scale=None, positions=Non
     n = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
     out = _empty(flat)
     lse = q.new_empty(flat.shape[:-1], dtype=torch.float32) if stats else None
-    need = ctypes.c_uint64()
-    rotor._check(_entry("rotor_window_attention_workspace_bytes")(ctypes.byref(n), 0, ctypes.byref(need)),
-                 "rotor_window_attention_workspace_bytes")
-    work = _scratch(need.value, q) if need.value else None
+    need = _attention_bytes("rotor_window_attention_workspace_bytes", *_sizes(n), 0)
+    work = _scratch(need, q) if need else None
     _call("rotor_window_attention", q.device, n, _aligned(q, "q"), _aligned(k, "k"), _aligned(v, "v"),
-          _heads(out, "out"), _ptr(lse), _ptr(work), need.value)
+          _heads(out, "out"), _ptr(lse), _ptr(work), need)
     return out, lse
 
 
@@ -669,10 +681,7 @@ def window_attention_backward(dout, q, k, v, out, lse, *, window=None, sinks=0, 
         raise ValueError("lse must be what window_attention returned")
     q, k, v = _batched(q, "q"), _batched(k, "k"), _batched(v, "v")
     n = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
-    need = ctypes.c_uint64()
-    rotor._check(_entry("rotor_window_attention_backward_workspace_bytes")(ctypes.byref(n), ctypes.byref(need)),
-                 "rotor_window_attention_backward_workspace_bytes")
-    work = _scratch(need.value, q)
+    work = _scratch(_attention_bytes("rotor_window_attention_backward_workspace_bytes", *_sizes(n)), q)
     _call("rotor_window_attention_backward", q.device, n, _aligned(dout, "dout"), _aligned(q, "q"),
           _aligned(k, "k"), _aligned(v, "v"), _aligned(out, "out"), lse.data_ptr(), _heads(dq, "dq"),
           _heads(dk, "dk"), _heads(dv, "dv"), work.data_ptr(), work.numel())
@@ -711,16 +720,14 @@ def window_attention_step(q, k, v, k_cache, v_cache, positions, *, window=None, 
     y = _out(out, q, "out")
     if out is not None:
         _no_overlap(y, "out")
-    need = ctypes.c_uint64()
-    rotor._check(_entry("rotor_window_attention_workspace_bytes")(ctypes.byref(n), 1, ctypes.byref(need)),
-                 "rotor_window_attention_workspace_bytes")
-    work = _scratch(need.value, q) if need.value else None
+    need = _attention_bytes("rotor_window_attention_workspace_bytes", *_sizes(n), 1)
+    work = _scratch(need, q) if need else None
 
     def one(t, what):  # [batch, heads, width]: strides of batch and head
-        h = _aligned(t, what, q, (3,))
-        return rotor.Heads(h.p, h.token, 0, h.head)
+        h = _aligned(t, what)
+        h.batch = h.token
+        return h
 
     _call("rotor_window_attention_step", q.device, n, one(q, "q"), one(k, "k"), one(v, "v"),
-          _aligned(k_cache, "k_cache"), _aligned(v_cache, "v_cache"), bool(ring), one(y, "out"), _ptr(work),
-          need.value)
+          _aligned(k_cache, "k_cache"), _aligned(v_cache, "v_cache"), bool(ring), one(y, "out"), _ptr(work), need)
     return y
