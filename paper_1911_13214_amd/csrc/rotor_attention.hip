@@ -793,7 +793,7 @@ int32_t rotor_window_attention_step(const rotor_attention *how, const rotor_head
                                     int32_t ring, const rotor_heads *out, void *d_work, uint64_t work_bytes,
                                     void *stream)
 {
-    if (!attention_sizes_ok(how) || how->tokens != 1 || how->keys < 1 || !how->positions || how->lengths ||
+    if (!attention_sizes_ok(how) || how->tokens != 1 || how->keys < 1 || (!how->positions && how->batch > 0) || how->lengths ||
         !index_ok(how->positions, how->position_bytes) || (ring != 0 && ring != 1))
         return ROTOR_EINVAL;
     // a ring holds the first keys and then at least a window

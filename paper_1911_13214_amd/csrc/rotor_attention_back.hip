@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
         }
         if constexpr (Scaled<T>::kOn) {
             exponent = exponent_of(most) + 6;
-            float all = most;
+            float all = most <= 3.4e38f ? most : 0.f;  // (a row of infinities has no gradients to keep)
 #pragma unroll
             for (int off = 16; off >= 1; off /= 2)
                 all = fmaxf(all, __shfl_xor(all, off));

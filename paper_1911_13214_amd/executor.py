@@ -221,11 +221,13 @@ def synthetic_chain(L, seed, width=1024, device="cpu", dtype=None):
     return stages, dims
 
 
-def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repeats=3, chain="mlp", rows=32000):
+def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repeats=3, chain="mlp", rows=32000,
+             attention=None):
     """The paper's check of the model (Sections 5.3-5.4) on a synthetic chain
     on cuda:0 (``chain`` "mlp": synthetic_chain in 32 bits; "language": token
     lookup, L - 2 residual blocks with dropout and the loss over ``rows``
-    tokens, stages.language_chain, in bf16): estimate the parameters, fill the table with the library at
+    tokens, stages.language_chain, in bf16, its ``batch`` tokens one sequence
+    where ``attention``, that function's, is given): estimate the parameters, fill the table with the library at
     ``slots`` slots of the store-everything memory, rebuild the sequences of
     ``n_budgets`` equally spaced budgets in one call, run each, and compare
     the measured time and peak memory with what the model predicts for that
@@ -243,7 +245,8 @@ def validate(L=24, seed=1, width=1024, batch=4096, slots=500, n_budgets=10, repe
         from . import stages as lm
         if L < 2:
             raise ValueError("a language chain has a lookup and a loss: L >= 2")
-        stages, dims = lm.language_chain(L - 2, seed, rows=rows, width=width, device=dev), [width] * (L + 1)
+        stages = lm.language_chain(L - 2, seed, rows=rows, width=width, device=dev, attention=attention)
+        dims = [width] * (L + 1)
         lm.set_step(stages, seed)
         tokens = torch.randint(0, rows, (batch + 1,), device=dev)
         x, stages[-1].targets = tokens[:-1].contiguous(), tokens[1:].contiguous()
@@ -311,5 +314,15 @@ if __name__ == "__main__":
     ap.add_argument("--budgets", type=int, default=10)
     ap.add_argument("--chain", choices=("mlp", "language"), default="mlp")
     ap.add_argument("--rows", type=int, default=32000, help="tokens of a language chain")
+    ap.add_argument("--heads", type=int, help="a language chain with attention: query heads")
+    ap.add_argument("--kv-heads", type=int, help="key heads (default: as many)")
+    ap.add_argument("--window", type=int, help="keys that a token sees (default: all up to it)")
+    ap.add_argument("--sinks", type=int, default=0, help="first keys that every token sees")
     a = ap.parse_args()
-    print(json.dumps(validate(a.L, a.seed, a.width, a.batch, a.slots, a.budgets, chain=a.chain, rows=a.rows)))
+    how = None
+    if a.heads is not None:
+        if a.chain != "language":
+            ap.error("--heads goes with --chain language")
+        how = dict(heads=a.heads, kv_heads=a.kv_heads, window=a.window, sinks=a.sinks)
+    print(json.dumps(validate(a.L, a.seed, a.width, a.batch, a.slots, a.budgets, chain=a.chain, rows=a.rows,
+                              attention=how)))

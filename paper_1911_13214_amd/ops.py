@@ -615,9 +615,9 @@ def _batched(t, what):
 
 def _aligned(t, what):
     """Heads that start 16-byte aligned (strides of one of something aside)."""
-    h = _heads(t, what)
-    if ((h.batch | h.token | h.head) * t.element_size() | h.p) % 16 and t.numel():
-        wrong = h.p % 16 or any(n > 1 and s * t.element_size() % 16 for n, s in zip(t.shape[:-1], t.stride()))
+    h, at = _heads(t, what), t.data_ptr()
+    if ((h.batch | h.token | h.head) * t.element_size() | at) % 16 and t.numel():
+        wrong = at % 16 or any(n > 1 and s * t.element_size() % 16 for n, s in zip(t.shape[:-1], t.stride()))
         if wrong:
             raise ValueError(f"the heads of {what} must start 16-byte aligned")
     return h

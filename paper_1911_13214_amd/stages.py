@@ -5,14 +5,16 @@ A stage that runs again under a schedule has to compute what it computed the
 first time, and what it keeps for its backward (w_abar) is what the schedule
 budgets.  So the dropout here draws its mask from (seed, step) and keeps
 nothing, the residual seam keeps its block's output, its sum and 16 bytes a
-row, the loss keeps 4 bytes a token and no logits, and every gradient is the
-same bit for bit on every call.  Inputs of any layout are taken, as in
+row, attention keeps its inputs, its output and 4 bytes a head and token and no
+scores, the norms of its heads keep their inputs alone, the loss keeps 4 bytes a
+token and no logits, and every gradient is the same bit for bit on every call.  Inputs of any layout are taken, as in
 ``linear_cross_entropy(x[:, :-1], w, tokens[:, 1:])``: those that the operators
 refuse are copied (and the copy is what is kept).  Second derivatives exist for the dropout
 alone; the others raise where one is taken.
 
-``language_chain`` builds a chain of them: token lookup, residual blocks and
-the loss over the vocabulary, ready for ``executor.run_sequence``."""
+``language_chain`` builds a chain of them: token lookup, residual blocks, with
+attention or without, and the loss over the vocabulary, ready for
+``executor.run_sequence``."""
 from __future__ import annotations
 
 import functools
@@ -171,6 +173,73 @@ def linear_cross_entropy(h, w, targets, ignore=-100):
     return _CrossEntropy.apply(h, w, targets, ignore)
 
 
+def _heads(t, aligned=False):
+    """A tensor of heads as the operators take them: one with a strided last
+    dimension is copied, and, for attention, one whose heads are not 16-byte
+    aligned."""
+    if t is None:
+        return t
+    if (t.shape[-1] > 1 and t.stride(-1) != 1) or (
+            aligned and (t.data_ptr() % 16 or any(n > 1 and s * t.element_size() % 16
+                                                  for n, s in zip(t.shape[:-1], t.stride())))):
+        return t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+class _HeadNormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, how):
+        q, k = _heads(q), _heads(k)
+        q_weight, k_weight = (None if w is None else w.contiguous() for w in (q_weight, k_weight))
+        positions = None if positions is None else positions.contiguous()
+        y, z = ops.head_norm_rotate(q, k, q_weight=q_weight, k_weight=k_weight, positions=positions, **how)
+        # without a norm the gradients need no inputs; their shapes are the results'
+        kept = (q, k) if how["norm"] != "none" else (None, None)
+        ctx.save_for_backward(*kept, q_weight, k_weight, positions)
+        ctx.how = how
+        return y, z
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dy, dz):
+        q, k, q_weight, k_weight, positions = ctx.saved_tensors
+        dy, dz = _heads(dy), _heads(dz)
+        g = ops.head_norm_rotate_backward(dy, dz, dy if q is None else q, dz if k is None else k, q_weight=q_weight,
+                                          k_weight=k_weight, positions=positions, **ctx.how)
+        return g["q"], g.get("k"), g.get("q_weight"), g.get("k_weight"), None, None
+
+
+def head_norm_rotate(q, k=None, *, norm="rms", q_weight=None, k_weight=None, eps=1e-5, positions=None, rotary=None,
+                     base=10000.0, frequencies=None, interleaved=False):
+    """ops.head_norm_rotate with gradients: (q', k')."""
+    how = dict(norm=norm, eps=eps, rotary=rotary, base=base, interleaved=interleaved,
+               frequencies=None if frequencies is None else tuple(map(float, frequencies)))
+    return _HeadNormRotate.apply(q, k, q_weight, k_weight, positions, how)
+
+
+class _WindowAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, positions, lengths, how):
+        q, k, v = (_heads(t, True) for t in (q, k, v))
+        positions, lengths = (None if t is None else t.contiguous() for t in (positions, lengths))
+        out, lse = ops.window_attention(q, k, v, positions=positions, lengths=lengths, **how)
+        ctx.save_for_backward(q, k, v, out, lse, positions, lengths)
+        ctx.how = how
+        return out
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dout):
+        q, k, v, out, lse, positions, lengths = ctx.saved_tensors
+        return (*ops.window_attention_backward(_heads(dout, True), q, k, v, out, lse, positions=positions,
+                                               lengths=lengths, **ctx.how), None, None, None)
+
+
+def window_attention(q, k, v, *, window=None, sinks=0, scale=None, positions=None, lengths=None):
+    """ops.window_attention with gradients: its output."""
+    return _WindowAttention.apply(q, k, v, positions, lengths, dict(window=window, sinks=sinks, scale=scale))
+
+
 # ---- modules -----------------------------------------------------------------------
 
 class Dropout(nn.Module):
@@ -254,6 +323,67 @@ class Block(nn.Module):
         return self.leave(y, self.drops[1](self.second(h)))[0]
 
 
+class Attention(nn.Module):
+    """Queries, keys and values of a token from one projection, norms of the
+    query and key heads and their rotation, attention under a window, and the
+    projection back.  Takes [tokens, width] (one sequence) or [batch, tokens,
+    width]; ``lengths`` is the stage's own, set before a step: int32 or int64
+    [batch], for a padded batch."""
+
+    def __init__(self, width, heads, kv_heads=None, head_width=None, window=None, sinks=0, norm="rms", base=10000.0):
+        super().__init__()
+        kv_heads = heads if kv_heads is None else kv_heads
+        head_width = width // heads if head_width is None else head_width
+        self.heads, self.kv_heads, self.head_width = heads, kv_heads, head_width
+        self.window, self.sinks, self.norm, self.base, self.lengths = window, sinks, norm, base, None
+        self.enter = nn.Linear(width, (heads + 2 * kv_heads) * head_width, bias=False)
+        self.leave = nn.Linear(heads * head_width, width, bias=False)
+        self.q_weight, self.k_weight = (nn.Parameter(torch.ones(head_width)) if norm != "none" else None
+                                        for _ in range(2))
+
+    def _split(self, x):
+        h, k = self.heads, self.kv_heads
+        x = self.enter(x).unflatten(-1, (h + 2 * k, self.head_width))
+        return x[..., :h, :], x[..., h:h + k, :], x[..., h + k:, :]
+
+    def forward(self, x):
+        q, k, v = self._split(x)
+        q, k = head_norm_rotate(q, k, norm=self.norm, q_weight=self.q_weight, k_weight=self.k_weight, base=self.base)
+        y = window_attention(q, k, v, window=self.window, sinks=self.sinks, lengths=self.lengths)
+        return self.leave(y.flatten(-2))
+
+    @torch.no_grad()
+    def step(self, x, k_cache, v_cache, positions, ring=False):
+        """The same for one token of each sequence, x [batch, width] at
+        positions [batch], whose keys and values go into the caches [batch,
+        slots, kv_heads, head_width]."""
+        q, k, v = self._split(x)
+        q, k = ops.head_norm_rotate(q, k, norm=self.norm, q_weight=self.q_weight, k_weight=self.k_weight,
+                                    base=self.base, positions=positions)
+        y = ops.window_attention_step(q, k, _heads(v, True), k_cache, v_cache, positions, window=self.window,
+                                      sinks=self.sinks, ring=ring)
+        return self.leave(y.flatten(-2))
+
+
+class AttentionBlock(nn.Module):
+    """A stage: an attention branch and a branch of Linear, GELU, Linear, each
+    with dropout, with the seams before, between and after them."""
+
+    def __init__(self, width, inner, p, seed, residual_scale=1.0, **attention):
+        super().__init__()
+        self.enter = Seam(width, post="none", gate=False)
+        self.between = Seam(width, residual_scale=residual_scale)
+        self.leave = Seam(width, pre="none", residual_scale=residual_scale)
+        self.first = Attention(width, **attention)
+        self.second = nn.Sequential(nn.Linear(width, inner), nn.GELU(), nn.Linear(inner, width))
+        self.drops = nn.ModuleList(Dropout(p, 2 * seed + k) for k in range(2))
+
+    def forward(self, x):
+        _, h = self.enter(x)
+        y, h = self.between(x, self.drops[0](self.first(h)))
+        return self.leave(y, self.drops[1](self.second(h)))[0]
+
+
 class Loss(nn.Module):
     """The last stage: a norm, the projection onto the vocabulary and the mean
     cross entropy over the tokens that have a target.  The targets are the
@@ -271,16 +401,34 @@ class Loss(nn.Module):
         return loss.sum() / (self.targets != self.ignore).sum().clamp(min=1)
 
 
-def language_chain(blocks, seed, rows=32000, width=1024, p=0.1, device="cuda", dtype=torch.bfloat16):
+def set_lengths(stages, lengths):
+    """Sets the lengths of a padded batch's sequences (None: no padding) in
+    every Attention of a list of stages."""
+    for s in stages:
+        for mod in s.modules():
+            if isinstance(mod, Attention):
+                mod.lengths = lengths
+
+
+def language_chain(blocks, seed, rows=32000, width=1024, p=0.1, device="cuda", dtype=torch.bfloat16, attention=None):
     """Stages of a chain: token lookup, ``blocks`` residual blocks whose inner
-    widths are drawn from {width, 2 width, 4 width}, the loss.  Seeded
-    weights."""
+    widths are drawn from {width, 2 width, 4 width}, the loss.  Seeded weights.
+    ``attention``: arguments of Attention (heads, kv_heads, window, ...), for
+    blocks whose first branch is one; without it tokens do not see each
+    other."""
     from . import chaingen
 
     rng = chaingen.SplitMix64(seed)
+
+    def block(k):
+        inner = width << rng.uniform(0, 2)
+        if attention is None:
+            return Block(width, inner, p, seed * 1000 + k)
+        return AttentionBlock(width, inner, p, seed * 1000 + k, **attention)
+
     with torch.random.fork_rng(devices=[]):
         torch.manual_seed(seed)
         stages = [Embedding(rows, width, scale=math.sqrt(width))]
-        stages += [Block(width, width << rng.uniform(0, 2), p, seed * 1000 + k) for k in range(blocks)]
+        stages += [block(k) for k in range(blocks)]
         stages.append(Loss(rows, width))
     return [s.to(device=device, dtype=dtype) for s in stages]

@@ -261,3 +261,19 @@ def test_the_plain_rotation_keeps_lengths_and_distances(interleaved):
     assert torch.allclose(turn(x, 77).norm(), x.norm()) and torch.equal(turn(x, 5)[..., 12:], x[..., 12:])
     a = (turn(x, 19) * turn(y, 12)).sum()
     assert torch.allclose((turn(x, 1007) * turn(y, 1000)).sum(), a) and torch.allclose(turn(turn(x, 4), -4), x)
+
+
+def test_a_chain_with_attention_is_made_of_its_blocks():
+    from paper_1911_13214_amd import stages as lm
+    how = dict(heads=4, kv_heads=2, head_width=16, window=9, sinks=2)
+    chain = lm.language_chain(3, 7, rows=11, width=32, device="cpu", attention=how)
+    assert [type(f) for f in chain] == [lm.Embedding] + [lm.AttentionBlock] * 3 + [lm.Loss]
+    a = chain[1].first
+    assert a.enter.weight.shape == ((4 + 4) * 16, 32) and a.leave.weight.shape == (32, 64) and a.window == 9
+    lm.set_lengths(chain, 5)
+    assert all(f.first.lengths == 5 for f in chain[1:4])
+    # seeded: the same again, and widths that do not depend on attention
+    again = lm.language_chain(3, 7, rows=11, width=32, device="cpu", attention=how)
+    assert all(torch.equal(x, y) for f, g in zip(chain, again) for x, y in zip(f.parameters(), g.parameters()))
+    plain = lm.language_chain(3, 7, rows=11, width=32, device="cpu")
+    assert [f.second[0].out_features for f in chain[1:4]] == [f.second[0].out_features for f in plain[1:4]]
