@@ -9,13 +9,17 @@ namespace rotor {
 namespace {
 
 constexpr int kKeys = 128;   // of a workgroup, gradients of keys
+constexpr int kFewSteps = 8;  // of keys, up to which delta is summed from its terms
 constexpr int kStepRows = 64;  // the most at a time
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // float16 holds 40 bits of range, and dS is as small as the gradients that
-// arrive: it is multiplied by a power of two, so that the largest |do| of a row
-// (of 32 rows, where they are summed) comes to lie in [2^-6, 2^-5).  |dS| is at
-// most twice that times 128 |v|: in range for any v.
+// arrive, times a probability: it is multiplied by a power of two, so that the
+// largest |do| of a row (of 32 rows, where they are summed) comes to lie in
+// [2^3, 2^4): probabilities down to 2^-14 keep all bits.  Where that overflows
+// (do v past 2^16), the sums are not finite, and are computed again with the
+// largest in [2^-6, 2^-5): |dS| is then at most 8 |v|, in range for any v.
+constexpr int kWide = -3, kSafe = 6;
 template <typename T> struct Scaled {
     static constexpr bool kOn = std::is_same<T, f16>::value;
 };
@@ -71,34 +75,32 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     delta = halves_sum(delta);
     most = halves_max(most);
     int exponent = 0;
-    {
-        const int64_t at = (int64_t)blockIdx.x * a.row_pitch + row;  // the pitch covers the last tile
-        if (h == 0) {
-            a.row_lse[at] = lse;
-            a.row_delta[at] = delta;
-        } else {
-            a.row_at[at] = seen ? p : -1;
-        }
-        if constexpr (Scaled<T>::kOn) {
-            exponent = exponent_of(most) + 6;
-            float all = most <= 3.4e38f ? most : 0.f;  // (a row of infinities has no gradients to keep)
+    const int64_t stats_at = (int64_t)blockIdx.x * a.row_pitch + row;  // the pitch covers the last tile
+    if (h == 0)
+        a.row_lse[stats_at] = lse;
+    else
+        a.row_at[stats_at] = seen ? p : -1;
+    if constexpr (Scaled<T>::kOn) {
+        exponent = exponent_of(most) + kWide;
+        float all = most <= 3.4e38f ? most : 0.f;  // (a row of infinities has no gradients to keep)
 #pragma unroll
-            for (int off = 16; off >= 1; off /= 2)
-                all = fmaxf(all, __shfl_xor(all, off));
-            if (lane == 0)
-                a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + rw / 32] = exponent_of(all) + 6;
-        }
+        for (int off = 16; off >= 1; off /= 2)
+            all = fmaxf(all, __shfl_xor(all, off));
+        if (lane == 0)
+            a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + rw / 32] = exponent_of(all);
     }
     char *const to = rows_of(a.dq, b, head) + t * a.dq.token;
     f32x16 acc[NB];
     clear(acc);
     int lo, hi;
     if (!span.positions(r0 / a.group, last_row / a.group, lo, hi)) {
+        if (h == 0)
+            a.row_delta[stats_at] = 0.f;
         if (row < a.rows)
             put_row<T>(to, h, a.width, acc, 0.f, false);
         return;
     }
-    const float factor = Scaled<T>::kOn ? power_of(-exponent) : 1.f;
+    float factor = Scaled<T>::kOn ? power_of(-exponent) : 1.f;
     const Sight sight{p - a.window + 1, p, a.sinks};
     int wlo = 0, whi = -1;
     const bool some = rw < a.rows && span.positions(rw / a.group, min(a.rows - 1, rw + 31) / a.group, wlo, whi);
@@ -136,6 +138,28 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     };
 
     int j = steps.key(0), j1 = steps.next(j);
+    if (sizeof(T) == 2 && steps.n <= kFewSteps) {
+        // delta as the sum of P times do v: of few keys the output is not small
+        // against them, and its rounding would be in every gradient
+        delta = 0.f;
+        for (int i = 0; i < steps.n; ++i, j = steps.next(j)) {
+            load(keys0, vals0, j);
+            tile_barrier();
+            f32x16 u = product<T, NB>(keys0, rd, q);
+            const f32x16 dp = product<T, NB>(vals0, rd, d);
+            mask(u, j, -kInf);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                u[e] = exp2_of(__builtin_fmaf(u[e], a.c, -lse));
+                delta += u[e] != 0.f ? u[e] * dp[e] : 0.f;
+            }
+            tile_barrier();
+        }
+        delta = halves_sum(delta);
+        j = steps.key(0);
+    }
+    if (h == 0)
+        a.row_delta[stats_at] = delta;
     load(keys0, vals0, j);
     load(keys1, vals1, j1);
     step_barrier<2 * Load::kLoads>();
@@ -181,6 +205,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     // infinities or NaN may have come from keys that a row does not see
     if (__syncthreads_or(!finite(acc))) {
         clear(acc);
+        exponent += kSafe - kWide;
+        factor = Scaled<T>::kOn ? power_of(-exponent) : 1.f;
         j = steps.key(0);
         for (int i = 0; i < steps.n; ++i, j = steps.next(j)) {
             load(keys0, vals0, j);
@@ -316,7 +342,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
             }
             float factor = 1.f;
             if constexpr (Scaled<T>::kOn) {
-                const int e = a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + r / 32];
+                const int e = a.row_exp[(int64_t)blockIdx.x * (a.row_pitch / 32) + r / 32] + (kApart ? kSafe : kWide);
                 if (e > exponent) {
                     const float by = power_of(max(exponent - e, -300));
 #pragma unroll

@@ -458,3 +458,20 @@ def test_optimal_sequences_of_a_chain_with_attention_run_within_their_budgets():
     for r in ok:
         # the allocator rounds blocks to 512 bytes
         assert r["measured_bytes"] <= r["budget_bytes"] * 1.02 + (8 << 20), r
+
+
+def test_float16_gradients_of_large_values_and_small_probabilities():
+    """Scores' gradients that leave float16's range at the scale that keeps
+    small probabilities exact: values of 2000 all of one sign, times gradients
+    of one sign; and long rows, whose probabilities are small."""
+    from test_gpu_attention import check
+    n, d = 80, 64
+    g = torch.Generator().manual_seed(3)
+    q, k = (m.normal(g, 1, n, 2, d, dtype=torch.float16) for _ in range(2))
+    v = (m.normal(g, 1, n, 2, d, std=1.0).abs() * 1000 + 1000).half()
+    dout = (m.normal(g, 1, n, 2, d).abs() + 1.0).half()
+    val, err = mix_model.attention(q, k, v, dout=dout)
+    got = attend(*(x.cuda() for x in (q, k, v, dout)))
+    for x, name in zip((got[0], *got[2:]), ("out", "dq", "dk", "dv")):
+        m.close(x, val[name], err[name], name)
+    check("f16", 1, 1400, 1400, 1, 1, 64)
