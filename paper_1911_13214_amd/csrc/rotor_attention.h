@@ -52,6 +52,7 @@ struct Attention {
     float scale, c;      // c = scale log2(e)
     uint32_t magic;      // ceil(2^32 / group), 0 for a group of one: x / group for x below 2^16
     uint64_t magic40;    // ceil(2^40 / group)
+    uint64_t kv_magic;   // ceil(2^40 / kv)
     int parts;           // of the keys (forward) or of the rows (gradients of keys)
     int ring;            // slots past the first ones, 0: the cache is linear
     // workspace
@@ -95,6 +96,16 @@ template <> struct Frag<float> {
 // row / group without a division: exact for rows below 2^23 and groups up to
 // 2^15.
 __device__ inline int token_of(const Attention &a, int row) { return (int)((uint64_t)(uint32_t)row * a.magic40 >> 40); }
+
+// Sequence and key head of a workgroup (fewer than 2^20 of them).
+struct Problem {
+    int b, kv;
+    __device__ Problem(const Attention &a, int i)
+    {
+        b = (int)((uint64_t)(uint32_t)i * a.kv_magic >> 40);
+        kv = i - b * a.kv;
+    }
+};
 
 // Row of a result's register e for a lane of half h.
 __device__ constexpr int row_of(int e, int h) { return 8 * (e / 4) + 4 * h + e % 4; }
@@ -603,6 +614,7 @@ inline void fill(Attention &a, const rotor_attention *n)
     a.c = (float)(n->scale * 1.4426950408889634);
     a.magic = a.group == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
     a.magic40 = (((uint64_t)1 << 40) + a.group - 1) / a.group;
+    a.kv_magic = (((uint64_t)1 << 40) + a.kv - 1) / a.kv;
     a.parts = 1;
 }
 

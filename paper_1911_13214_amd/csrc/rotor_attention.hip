@@ -83,7 +83,7 @@ __device__ inline void put_rows(const Attention &a, const Rows<T, NB> &w, int b,
         put_sums(a.part_out + at * a.width, h, a.width, w.acc);
         return;
     }
-    const int t = row / a.group, head = kv * a.group + row % a.group;
+    const int t = token_of(a, row), head = kv * a.group + row - t * a.group;
     put_row<T>(rows_of(a.out, b, head) + t * a.out.token, h, a.width, w.acc, 1.f / sum, seen);
     if (h == 0 && a.lse)
         a.lse[((int64_t)b * a.tokens + t) * ((int64_t)a.kv * a.group) + head] =
@@ -109,22 +109,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
     __shared__ __attribute__((aligned(1024))) char keys0[kBytes], keys1[kBytes], keys2[kBytes];
     __shared__ __attribute__((aligned(1024))) char vals0[kBytes], vals1[kBytes], vals2[kBytes];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
-    const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
+    const Problem at_head(a, blockIdx.x);
+    const int b = at_head.b, kv = at_head.kv;
     const int r0 = (gridDim.y - 1 - blockIdx.y) * kTileRows, rw = r0 + wave * 32, row = rw + lane % 32;
     const Span span(a, b);
     const int last_row = min(a.rows - 1, r0 + kTileRows - 1);
 
-    const int t = row / a.group, p = span.offset + t;
+    const int t = token_of(a, row), p = span.offset + t;
     const bool seen = row < a.rows && p >= 0 && p < span.length;
     Rows<T, NB> w;
     w.reset();
     int lo, hi;
-    if (!span.positions(r0 / a.group, last_row / a.group, lo, hi)) {
+    if (!span.positions(token_of(a, r0), token_of(a, last_row), lo, hi)) {
         put_rows(a, w, b, kv, blockIdx.z, row, false, h);
         return;
     }
     {
-        const char *q = rows_of(a.q, b, kv * a.group + row % a.group) + t * a.q.token;
+        const char *q = rows_of(a.q, b, kv * a.group + row - t * a.group) + t * a.q.token;
 #pragma unroll
         for (int k = 0; k < S::NK; ++k)
             w.q[k] = global_frag<T>(q, seen, 2 * k + h, a.width);
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
     const Sight sight{p - a.window + 1, p, a.sinks};
     // what all rows of the wave see, and what any of them does
     int wlo = 0, whi = -1;
-    const bool some = rw < a.rows && span.positions(rw / a.group, min(a.rows - 1, rw + 31) / a.group, wlo, whi);
+    const bool some = rw < a.rows && span.positions(token_of(a, rw), token_of(a, min(a.rows - 1, rw + 31)), wlo, whi);
 
     const Steps<kTileKeys> steps(a, lo, hi);
     const int i0 = (int)((int64_t)steps.n * blockIdx.z / a.parts);
@@ -310,7 +311,8 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(Attention a)
     __shared__ __attribute__((aligned(1024))) char vals_even[kWaves * kBytes], vals_odd[kWaves * kBytes];
     __shared__ float2 soft[kWaves][R * 16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16;
-    const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
+    const Problem at_head(a, blockIdx.x);
+    const int b = at_head.b, kv = at_head.kv;
     const int r0 = blockIdx.y * (R * 16);
     const Span span(a, b);
     F q[R][NK];
@@ -319,16 +321,16 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(Attention a)
     Sight sight[R];
 #pragma unroll
     for (int x = 0; x < R; ++x) {
-        const int row = r0 + x * 16 + lane % 16, t = row / a.group, p = span.offset + t;
+        const int row = r0 + x * 16 + lane % 16, t = token_of(a, row), p = span.offset + t;
         const bool seen = row < a.rows && p >= 0 && p < span.length;
-        const char *at = rows_of(a.q, b, kv * a.group + row % a.group) + t * a.q.token;
+        const char *at = rows_of(a.q, b, kv * a.group + row - t * a.group) + t * a.q.token;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
             q[x][k] = global_frag<T>(at, seen, 4 * k + h, a.width);
         sight[x] = Sight{p - a.window + 1, p, a.sinks};
     }
     int lo = 0, hi = -1;
-    const bool some = span.positions(r0 / a.group, min(a.rows - 1, r0 + R * 16 - 1) / a.group, lo, hi);
+    const bool some = span.positions(token_of(a, r0), token_of(a, min(a.rows - 1, r0 + R * 16 - 1)), lo, hi);
     const int from = max(0, lo - a.window + 1), ahead = min(a.sinks, from);
     const int n = some ? ahead + hi - from + 1 : 0;
     const int share = (n + a.parts - 1) / a.parts;
@@ -566,7 +568,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(Attention a)
 #pragma unroll
         for (int i = 0; i < kWaves; ++i)
             total += soft[i][x * 16 + line].y * exp2_of((soft[i][x * 16 + line].x - floor) * a.c);
-        const int t = row / a.group, head = kv * a.group + row % a.group, p = span.offset + t;
+        const int t = token_of(a, row), head = kv * a.group + row - t * a.group, p = span.offset + t;
         const bool seen = p >= 0 && p < span.length;
         const int64_t part = ((int64_t)blockIdx.z * a.batch * a.kv + (int64_t)b * a.kv + kv) * a.rows + row;
         // a position past the cache of a single token has no result

@@ -20,6 +20,9 @@ constexpr int kStepRows = 64;  // the most at a time
 // (do v past 2^16), the sums are not finite, and are computed again with the
 // largest in [2^-6, 2^-5): |dS| is then at most 8 |v|, in range for any v.
 constexpr int kWide = -3, kSafe = 6;
+// Its probabilities, as factors of do in dv, are multiplied by 2^10: those of rows
+// with many keys would lose bits below 2^-14.
+constexpr int kUp = 10;
 template <typename T> struct Scaled {
     static constexpr bool kOn = std::is_same<T, f16>::value;
 };
@@ -46,11 +49,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     __shared__ __attribute__((aligned(1024))) char keys0[kBytes], keys1[kBytes], keys2[kBytes];
     __shared__ __attribute__((aligned(1024))) char vals0[kBytes], vals1[kBytes], vals2[kBytes];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
-    const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
+    const Problem at_head(a, blockIdx.x);
+    const int b = at_head.b, kv = at_head.kv;
     const int r0 = (gridDim.y - 1 - blockIdx.y) * kTileRows, rw = r0 + wave * 32, row = rw + lane % 32;
     const Span span(a, b);
     const int last_row = min(a.rows - 1, r0 + kTileRows - 1);
-    const int t = row / a.group, p = span.offset + t, head = kv * a.group + row % a.group;
+    const int t = token_of(a, row), p = span.offset + t, head = kv * a.group + row - t * a.group;
     const bool seen = row < a.rows && p >= 0 && p < span.length;
 
     F q[S::NK], d[S::NK];
@@ -77,7 +81,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     int exponent = 0;
     const int64_t stats_at = (int64_t)blockIdx.x * a.row_pitch + row;  // the pitch covers the last tile
     if (h == 0)
-        a.row_lse[stats_at] = lse;
+        a.row_lse[stats_at] = Scaled<T>::kOn ? lse - (float)kUp : lse;
     else
         a.row_at[stats_at] = seen ? p : -1;
     if constexpr (Scaled<T>::kOn) {
@@ -93,7 +97,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     f32x16 acc[NB];
     clear(acc);
     int lo, hi;
-    if (!span.positions(r0 / a.group, last_row / a.group, lo, hi)) {
+    if (!span.positions(token_of(a, r0), token_of(a, last_row), lo, hi)) {
         if (h == 0)
             a.row_delta[stats_at] = 0.f;
         if (row < a.rows)
@@ -103,7 +107,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     float factor = Scaled<T>::kOn ? power_of(-exponent) : 1.f;
     const Sight sight{p - a.window + 1, p, a.sinks};
     int wlo = 0, whi = -1;
-    const bool some = rw < a.rows && span.positions(rw / a.group, min(a.rows - 1, rw + 31) / a.group, wlo, whi);
+    const bool some = rw < a.rows && span.positions(token_of(a, rw), token_of(a, min(a.rows - 1, rw + 31)), wlo, whi);
 
     const Steps<kTileKeys> steps(a, lo, hi);
     typedef Loader<T, NB, kTileKeys, kWaves> Load;
@@ -244,7 +248,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
     __shared__ __attribute__((aligned(1024))) char values[kHeld ? 16 : kKeys * S::kRow];
     __shared__ __attribute__((aligned(16))) float stats_even[3 * 64], stats_odd[3 * 64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
-    const int b = blockIdx.x / a.kv, kv = blockIdx.x % a.kv;
+    const Problem at_head(a, blockIdx.x);
+    const int b = at_head.b, kv = at_head.kv;
     int tile, part, parts;
     {
         const int item = blockIdx.y, ahead = a.sink_tiles * a.sink_parts;
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
                             dk[x][y] *= by;
                     exponent = e;
                 }
-                factor = power_of(-exponent);
+                factor = power_of(-exponent - kUp);
             }
             // (a row's place, -1 for none, is below every key it does not see)
             auto mask = [&](f32x16 &x) {
@@ -420,18 +425,22 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
         pass(std::true_type{});
     }
     const float by = a.scale * (Scaled<T>::kOn ? power_of(max(exponent, -300)) : 1.f);
+    const float up = Scaled<T>::kOn ? power_of(-kUp) : 1.f;
     if (parts > 1) {
         const int64_t at = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kKeys + wave * 32 + lane % 32) * a.width;
 #pragma unroll
         for (int x = 0; x < NB; ++x)
 #pragma unroll
             for (int y = 0; y < 16; ++y)
+            {
                 dk[x][y] *= by;
+                dv[x][y] *= up;
+            }
         put_sums(a.part_dk + at, h, a.width, dk);
         put_sums(a.part_dv + at, h, a.width, dv);
     } else if (key < a.keys) {
         put_row<T>(rows_of(a.dk, b, kv) + key * a.dk.token, h, a.width, dk, by, have);
-        put_row<T>(rows_of(a.dv, b, kv) + key * a.dv.token, h, a.width, dv, 1.f, have);
+        put_row<T>(rows_of(a.dv, b, kv) + key * a.dv.token, h, a.width, dv, up, have);
     }
 #endif
 }
