@@ -7,6 +7,7 @@
 namespace rotor {
 namespace {
 
+constexpr int kMostParts = 256;  // of the keys: a thread each where they are joined
 constexpr int kFewRows = 32;  // the most that few_kernel takes at a time, and that it is chosen for
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -616,7 +617,7 @@ template <typename T, bool STEP> __global__ __launch_bounds__(256) void join_ker
     const Span span(a, b);
     const int p = span.offset + t;
     const bool seen = p >= 0 && p < span.length;
-    // every thread's part, its maximum and sum (there are at most 256)
+    // every thread's part, its maximum and sum
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     float2 soft = make_float2(-kInf, 0.f);
     if ((int)threadIdx.x < a.parts)
@@ -699,7 +700,7 @@ ForwardPlan forward_plan(const rotor_attention *n, bool step)
         const int64_t at_once = 256 * (n->width <= 64 ? 2 : 1), base = bk * ceil_div(rows, kFewRows);
         const int64_t limit = most / 512;  // 4 tiles of 32 keys for each of 4 waves
         double best = 0.;
-        for (int64_t k = 1; base && k <= limit && k <= 256; ++k) {
+        for (int64_t k = 1; base && k <= limit && k <= kMostParts; ++k) {
             const int64_t rounds = ceil_div(base * k, at_once);
             const double full = (double)(base * k) / (double)(rounds * at_once);
             if (full > best + 0.02) {
@@ -711,10 +712,10 @@ ForwardPlan forward_plan(const rotor_attention *n, bool step)
         }
     } else {
         const int64_t base = bk * ceil_div(rows, kTileRows), tiles = most / 64;
-        if (base < 256 && tiles >= 16)
+        if (base > 0 && base < 256 && tiles >= 16)
             parts = ceil_div(512, base) < tiles / 8 ? ceil_div(512, base) : tiles / 8;
     }
-    p.parts = (int)(parts < 1 ? 1 : parts);
+    p.parts = (int)(parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts);
     p.out_bytes = p.soft_bytes = 0;
     if (p.parts > 1) {
         p.out_bytes = round256((uint64_t)p.parts * bk * rows * n->width * 4);

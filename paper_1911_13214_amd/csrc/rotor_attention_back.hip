@@ -492,8 +492,10 @@ struct BackPlan {
 };
 
 // Rows of a tile of keys are split where the tiles leave CUs without work, and
-// where a tile holds first keys, which all rows see, into parts about as long
-// as the other tiles'.
+// where a tile holds first keys, which all rows see, into parts about as long as
+// the other tiles', or as half of what a workgroup's place gets to do in all (two
+// sequences of 8192, 8 key heads, window 1024: 4 first keys in one part would
+// take 7 times as long as other tiles).
 bool back_plan(const rotor_attention *n, BackPlan &p)
 {
     const int64_t group = n->heads / n->kv_heads, rows = n->tokens * group, bk = n->batch * n->kv_heads;
@@ -509,7 +511,9 @@ bool back_plan(const rotor_attention *n, BackPlan &p)
         parts = ceil_div(512, base) < steps / 4 ? ceil_div(512, base) : steps / 4;
         parts = parts < 1 ? 1 : parts > 16 ? 16 : parts;
     }
-    const int64_t each = steps / parts > 4 ? steps / parts : 4;
+    const int64_t half = bk * (tiles * steps + sink_tiles * sink_steps) / 1024;
+    int64_t each = steps / parts > 4 ? steps / parts : 4;
+    each = each > half ? each : half;
     int64_t sink_parts = ceil_div(sink_steps, each);
     sink_parts = sink_parts > 64 ? 64 : sink_parts;
     sink_parts = sink_parts < parts ? parts : sink_parts;

@@ -717,6 +717,8 @@ def window_attention_step(q, k, v, k_cache, v_cache, positions, *, window=None, 
     _like(v, q, "v", shape)
     _no_overlap(k_cache, "k_cache")
     _no_overlap(v_cache, "v_cache")
+    if batch and k_cache.data_ptr() == v_cache.data_ptr():
+        raise ValueError("k_cache and v_cache must be two tensors")
     y = _out(out, q, "out")
     if out is not None:
         _no_overlap(y, "out")

@@ -162,6 +162,19 @@ def test_parts_of_the_keys_and_of_the_rows(dtype):
     check(dtype, 1, 1, 1500, 40, 1, 128)
 
 
+def test_more_parts_than_a_workgroup_joins():
+    """One tile of rows against keys for more than 256 parts: values that are
+    the keys' own numbers, so that a part left out shows, uniform scores."""
+    n, keys = 40, 300000
+    q, k = torch.zeros(1, n, 1, 8, device="cuda"), torch.zeros(1, keys, 1, 8, device="cuda")
+    v = (torch.arange(keys, device="cuda", dtype=torch.float32) / keys)[None, :, None, None].expand(1, keys, 1, 8)
+    out, lse = ops.window_attention(q, k, v.contiguous())
+    seen = torch.arange(keys - n + 1, keys + 1, dtype=torch.float64)
+    # sums of 300000 terms in parts of 1200, in lanes of 600: 600 + 256 roundings
+    m.close(out[0, :, 0], ((seen - 1) / 2 / keys)[:, None].expand(n, 8), 900 * m.U32)
+    m.close(lse[0, :, 0], torch.log(seen), 900 * m.U32)
+
+
 def test_a_cache_past_32_bits():
     """A cache whose slots lie more than 2^31 elements and 2^32 bytes apart."""
     slots, hk, d = 2 ** 20 + 64, 16, 128  # 4.3 GB each
@@ -198,7 +211,7 @@ def test_without_elements():
 def test_refusals():
     x, w = torch.zeros(2, 8, 4, 64, device="cuda"), torch.ones(64, device="cuda")
     at = torch.zeros(2, dtype=torch.int32, device="cuda")
-    cache, one = torch.zeros(2, 16, 4, 64, device="cuda"), x[:, 0]
+    cache, other, one = torch.zeros(2, 16, 4, 64, device="cuda"), torch.zeros(2, 16, 4, 64, device="cuda"), x[:, 0]
     odd = torch.zeros(2, 8, 4, 66, device="cuda")[..., 1:65]
     half, double = x.half(), x.double()
     lse = torch.zeros(2, 8, 4, device="cuda")
@@ -223,13 +236,14 @@ def test_refusals():
         lambda: ops.window_attention(x.transpose(-1, -2), x, x),
         lambda: ops.window_attention_backward(x, x, x, x, x, lse[:1]), lambda: ops.window_attention_backward(x, x, x, x, half, lse),
         lambda: ops.window_attention_backward(x[:1], x, x, x, x, lse),
-        lambda: ops.window_attention_step(x, one, one, cache, cache, at), lambda: ops.window_attention_step(one, one, one, cache, cache, None),
-        lambda: ops.window_attention_step(one, one, one, cache, cache, at, ring=True),
-        lambda: ops.window_attention_step(one, one, one, cache, cache, at, ring=True, window=15, sinks=2),
-        lambda: ops.window_attention_step(one, one[:1], one, cache, cache, at),
-        lambda: ops.window_attention_step(one, one, one, cache, cache[:, :8], at),
-        lambda: ops.window_attention_step(one, one, one, cache[:1].expand(2, 16, 4, 64), cache, at),
-        lambda: ops.window_attention_step(one, one, one, cache[:, :0], cache[:, :0], at),
+        lambda: ops.window_attention_step(x, one, one, cache, other, at), lambda: ops.window_attention_step(one, one, one, cache, other, None),
+        lambda: ops.window_attention_step(one, one, one, cache, other, at, ring=True),
+        lambda: ops.window_attention_step(one, one, one, cache, other, at, ring=True, window=15, sinks=2),
+        lambda: ops.window_attention_step(one, one[:1], one, cache, other, at),
+        lambda: ops.window_attention_step(one, one, one, cache, cache, at),
+        lambda: ops.window_attention_step(one, one, one, cache, other[:, :8], at),
+        lambda: ops.window_attention_step(one, one, one, cache[:1].expand(2, 16, 4, 64), other, at),
+        lambda: ops.window_attention_step(one, one, one, cache[:, :0], other[:, :0], at),
     ]
     for i, f in enumerate(bad):
         with pytest.raises(ValueError):
