@@ -573,17 +573,18 @@ def head_norm_rotate_backward(dq, dk, q, k=None, *, norm="rms", q_weight=None, k
 # ---- attention -------------------------------------------------------------------------------
 
 def _attention(q, k, v, window, sinks, scale, positions, lengths, shape):
-    """The C ABI's description of an attention, checked: ``shape`` is (batch,
-    tokens, heads, width) of q."""
+    """The C ABI's description of an attention, checked, and the sizes that its
+    workspace follows from: ``shape`` is (batch, tokens, heads, width) of q."""
     code = _typed(q, "q")
     batch, tokens, heads, width = shape
     if width % 8 or not 8 <= width <= ATTENTION_MAX_WIDTH:
         raise ValueError(f"the width must be a multiple of 8, from 8 to {ATTENTION_MAX_WIDTH}")
-    if _cuda(k, "k").dim() != 4 or k.shape[0] != batch or k.shape[3] != width or k.shape[2] < 1 or \
-            heads % k.shape[2] or heads < 1:
+    cache = _cuda(k, "k").shape
+    if len(cache) != 4 or cache[0] != batch or cache[3] != width or cache[2] < 1 or heads < 1 or heads % cache[2]:
         raise ValueError(f"k must be [{batch}, keys, heads, {width}], its heads dividing the {heads} of q")
-    _like(k, q, "k", k.shape)
-    _like(v, q, "v", k.shape)
+    if k.dtype != q.dtype or k.device != q.device:
+        raise ValueError(f"k must be {q.dtype} on {q.device}")
+    _like(v, q, "v", cache)
     if window is not None and window < 1:
         raise ValueError("window must be at least 1, or None")
     if sinks < 0:
@@ -591,49 +592,53 @@ def _attention(q, k, v, window, sinks, scale, positions, lengths, shape):
     scale = width ** -0.5 if scale is None else scale
     if not 0.0 < scale <= 1e30:
         raise ValueError("scale must be positive")
-    n = rotor.Attention(code, 8, 8, 0, batch, tokens, k.shape[1], heads, k.shape[2], width, window or 0, sinks, scale,
-                   None, None)
-    for name, t in (("positions", positions), ("lengths", lengths)):
-        if t is None:
-            continue
-        size = _index(t, name, q.device)
-        if t.shape != (batch,) or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous, of shape ({batch},)")
-        if name == "positions":
-            n.position_bytes, n.positions = size, t.data_ptr()
-        else:
-            n.length_bytes, n.lengths = size, t.data_ptr()
-    return n
+    sizes = (batch, tokens, cache[1], heads, cache[2], width, window or 0, sinks)
+    n = rotor.Attention(code, 8, 8, 0, *sizes, scale)
+    if positions is not None:
+        n.position_bytes, n.positions = _per_sequence(positions, "positions", q.device, batch)
+    if lengths is not None:
+        n.length_bytes, n.lengths = _per_sequence(lengths, "lengths", q.device, batch)
+    return n, (code,) + sizes
+
+
+def _per_sequence(t, what, device, batch):
+    size = _index(t, what, device)
+    if t.shape != (batch,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous, of shape ({batch},)")
+    return size, t.data_ptr()
 
 
 def _batched(t, what):
     """[batch, tokens, heads, width], of which the batch may be left out."""
-    if _cuda(t, what).dim() not in (3, 4):
+    dims = _cuda(t, what).dim()
+    if dims == 4:
+        return t
+    if dims != 3:
         raise ValueError(f"{what} must be [tokens, heads, width] or [batch, tokens, heads, width]")
-    return t if t.dim() == 4 else t.unsqueeze(0)
+    return t.unsqueeze(0)
 
 
-def _aligned(t, what):
-    """Heads that start 16-byte aligned (strides of one of something aside)."""
-    h, at = _heads(t, what), t.data_ptr()
-    if ((h.batch | h.token | h.head) * t.element_size() | at) % 16 and t.numel():
-        wrong = at % 16 or any(n > 1 and s * t.element_size() % 16 for n, s in zip(t.shape[:-1], t.stride()))
-        if wrong:
-            raise ValueError(f"the heads of {what} must start 16-byte aligned")
-    return h
+def _call_aligned(name, device, heads, *args):
+    """An entry point whose heads have to start 16-byte aligned: the library
+    looks, what it refused is named here."""
+    try:
+        _call(name, device, *args)
+    except rotor.RotorError:
+        for what, t in heads.items():
+            size = t.element_size()
+            if t.numel() and (t.data_ptr() % 16 or any(n > 1 and s * size % 16
+                                                       for n, s in zip(t.shape[:-1], t.stride()))):
+                raise ValueError(f"the heads of {what} must start 16-byte aligned") from None
+        raise
 
 
 @functools.lru_cache(maxsize=4096)
-def _attention_bytes(name, *sizes):
+def _attention_bytes(name, sizes, *more):
     """Workspace of an attention's entry point for these sizes."""
     keys = ("type", "batch", "tokens", "keys", "heads", "kv_heads", "width", "window", "sinks")
     n, need = rotor.Attention(scale=1.0, **dict(zip(keys, sizes))), ctypes.c_uint64()
-    rotor._check(_entry(name)(n, *sizes[len(keys):], ctypes.byref(need)), name)
+    rotor._check(_entry(name)(n, *more, ctypes.byref(need)), name)
     return need.value
-
-
-def _sizes(n):
-    return n.type, n.batch, n.tokens, n.keys, n.heads, n.kv_heads, n.width, n.window, n.sinks
 
 
 def window_attention(q, k, v, *, window=None, sinks=0, scale=None, positions=None, lengths=None, stats=True,
@@ -656,13 +661,13 @@ def window_attention(q, k, v, *, window=None, sinks=0, scale=None, positions=Non
                    lengths=lengths, stats=stats)
     flat = q
     q, k, v = _batched(q, "q"), _batched(k, "k"), _batched(v, "v")
-    n = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
+    n, sizes = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
     out = _empty(flat)
     lse = q.new_empty(flat.shape[:-1], dtype=torch.float32) if stats else None
-    need = _attention_bytes("rotor_window_attention_workspace_bytes", *_sizes(n), 0)
+    need = _attention_bytes("rotor_window_attention_workspace_bytes", sizes, 0)
     work = _scratch(need, q) if need else None
-    _call("rotor_window_attention", q.device, n, _aligned(q, "q"), _aligned(k, "k"), _aligned(v, "v"),
-          _heads(out, "out"), _ptr(lse), _ptr(work), need)
+    _call_aligned("rotor_window_attention", q.device, dict(q=q, k=k, v=v), n, _heads(q, "q"), _heads(k, "k"),
+                  _heads(v, "v"), _heads(out, "out"), _ptr(lse), _ptr(work), need)
     return out, lse
 
 
@@ -680,11 +685,11 @@ def window_attention_backward(dout, q, k, v, out, lse, *, window=None, sinks=0, 
             lse.shape != q.shape[:-1] or not lse.is_contiguous():
         raise ValueError("lse must be what window_attention returned")
     q, k, v = _batched(q, "q"), _batched(k, "k"), _batched(v, "v")
-    n = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
-    work = _scratch(_attention_bytes("rotor_window_attention_backward_workspace_bytes", *_sizes(n)), q)
-    _call("rotor_window_attention_backward", q.device, n, _aligned(dout, "dout"), _aligned(q, "q"),
-          _aligned(k, "k"), _aligned(v, "v"), _aligned(out, "out"), lse.data_ptr(), _heads(dq, "dq"),
-          _heads(dk, "dk"), _heads(dv, "dv"), work.data_ptr(), work.numel())
+    n, sizes = _attention(q, k, v, window, sinks, scale, positions, lengths, q.shape)
+    work = _scratch(_attention_bytes("rotor_window_attention_backward_workspace_bytes", sizes), q)
+    _call_aligned("rotor_window_attention_backward", q.device, dict(dout=dout, q=q, k=k, v=v, out=out), n,
+                  _heads(dout, "dout"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"),
+                  lse.data_ptr(), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"), work.data_ptr(), work.numel())
     return dq, dk, dv
 
 
@@ -706,7 +711,7 @@ def window_attention_step(q, k, v, k_cache, v_cache, positions, *, window=None, 
     if _cuda(q, "q").dim() != 3:
         raise ValueError("q must be [batch, heads, width]")
     batch, heads, width = q.shape
-    n = _attention(q, k_cache, v_cache, window, sinks, scale, positions, None, (batch, 1, heads, width))
+    n, sizes = _attention(q, k_cache, v_cache, window, sinks, scale, positions, None, (batch, 1, heads, width))
     slots = k_cache.shape[1]
     if positions is None or slots < 1:
         raise ValueError("a position for each sequence and at least one slot are needed")
@@ -722,14 +727,15 @@ def window_attention_step(q, k, v, k_cache, v_cache, positions, *, window=None, 
     y = _out(out, q, "out")
     if out is not None:
         _no_overlap(y, "out")
-    need = _attention_bytes("rotor_window_attention_workspace_bytes", *_sizes(n), 1)
+    need = _attention_bytes("rotor_window_attention_workspace_bytes", sizes, 1)
     work = _scratch(need, q) if need else None
 
     def one(t, what):  # [batch, heads, width]: strides of batch and head
-        h = _aligned(t, what)
+        h = _heads(t, what)
         h.batch = h.token
         return h
 
-    _call("rotor_window_attention_step", q.device, n, one(q, "q"), one(k, "k"), one(v, "v"),
-          _aligned(k_cache, "k_cache"), _aligned(v_cache, "v_cache"), bool(ring), one(y, "out"), _ptr(work), need)
+    _call_aligned("rotor_window_attention_step", q.device, dict(q=q, k=k, v=v, k_cache=k_cache, v_cache=v_cache, out=y),
+                  n, one(q, "q"), one(k, "k"), one(v, "v"), _heads(k_cache, "k_cache"), _heads(v_cache, "v_cache"),
+                  bool(ring), one(y, "out"), _ptr(work), need)
     return y
