@@ -297,7 +297,7 @@ template <typename T, int V, int N, bool INTER>
 __global__ __launch_bounds__(kThreads) void rotate_back_kernel(RotateArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, teams = 64 / a.team;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), teams = 64 / a.team;
     const int z = (int)blockIdx.x >= a.blocks_q ? 1 : 0, block = blockIdx.x - (z ? a.blocks_q : 0);
     const int heads = a.heads[z], split = a.splits[z];
     const int64_t stride = (int64_t)(z ? gridDim.x - a.blocks_q : a.blocks_q) * kWaves;
@@ -305,6 +305,8 @@ __global__ __launch_bounds__(kThreads) void rotate_back_kernel(RotateArgs a)
     const HeadRows in = a.in[z], out = a.out[z], grad = a.grad[z];
     Pairs<T, V, N, INTER> at;
     at.init(a, lane);
+    typename Pairs<T, V, N, INTER>::Raw weights;
+    at.fetch(weight, weight != nullptr, weights);
     float sums[N][2][V];
     each<V, N>([&](int p, int q, int e) { sums[p][q][e] = 0.f; });
     for (int64_t task = (int64_t)block * kWaves + wave; task < a.all * split; task += stride) {
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(kThreads) void rotate_back_kernel(RotateArgs a)
                 float w[N][2][V];
                 each<V, N>([&](int p, int q, int e) { w[p][q][e] = 1.f; });
                 if (weight)
-                    at.load(weight, true, w);
+                    at.unpack(weights, w);
                 at.rotate(g, c, s, -1.f);
                 centre<V, N>(a, at, u);
                 // of u^2, of the weighted gradient times u, and of it alone
@@ -381,25 +383,37 @@ __global__ __launch_bounds__(kThreads) void rotate_back_kernel(RotateArgs a)
 #endif
 }
 
-// The blocks' sums joined in their order: 16 columns a workgroup, 16 strips of
-// blocks; blockIdx.y: q, k.
+// The blocks' sums joined in their order: 16 columns a workgroup, 64 strips of
+// blocks, joined by eights; blockIdx.y: q, k.
+constexpr int kStrips = 64, kEights = kStrips / 8;
+
 template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(const float *sums, int blocks_q, int blocks, int width, T *dq, T *dk)
+__global__ __launch_bounds__(16 * kStrips) void join_kernel(const float *sums, int blocks_q, int blocks, int width,
+                                                            T *dq, T *dk)
 {
-    __shared__ float strip[16][16];
-    const int col = blockIdx.x * 16 + threadIdx.x % 16, k = threadIdx.x / 16, z = blockIdx.y;
+    __shared__ float strip[kStrips][16], eights[kEights][16];
+    const int lane = threadIdx.x % 16, col = blockIdx.x * 16 + lane, k = threadIdx.x / 16, z = blockIdx.y;
     const int end = z ? blocks : blocks_q;
     float v = 0.f;
     if (col < width)
 #pragma unroll 8
-        for (int i = (z ? blocks_q : 0) + k; i < end; i += 16)
+        for (int i = (z ? blocks_q : 0) + k; i < end; i += kStrips)
             v += sums[(int64_t)i * width + col];
-    strip[k][threadIdx.x % 16] = v;
+    strip[k][lane] = v;
+    __syncthreads();
+    if (k < kEights) {
+        v = strip[8 * k][lane];
+#pragma unroll
+        for (int i = 1; i < 8; ++i)
+            v += strip[8 * k + i][lane];
+        eights[k][lane] = v;
+    }
     __syncthreads();
     T *const out = z ? dk : dq;
     if (k == 0 && col < width && out) {
-        for (int i = 1; i < 16; ++i)
-            v += strip[i][threadIdx.x];
+#pragma unroll
+        for (int i = 1; i < kEights; ++i)
+            v += eights[i][lane];
         out[col] = (T)v;
     }
 }
@@ -604,7 +618,7 @@ int32_t rotor_head_norm_rotate_backward(const rotor_head_rotation *how, const ro
                     <<<dim3((uint32_t)blocks), kThreads, 0, (hipStream_t)stream>>>(a);
             });
         if (sums)
-            join_kernel<T><<<dim3((uint32_t)ceil_div(how->width, 16), 2), 256, 0, (hipStream_t)stream>>>(
+            join_kernel<T><<<dim3((uint32_t)ceil_div(how->width, 16), 2), 16 * kStrips, 0, (hipStream_t)stream>>>(
                 a.sums, a.blocks_q, blocks, a.width, (T *)d_dq_weight, (T *)d_dk_weight);
     });
     return hipGetLastError() == hipSuccess ? ROTOR_OK : ROTOR_EDEVICE;
