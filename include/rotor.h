@@ -691,7 +691,8 @@ ROTOR_API int32_t rotor_head_norm_rotate_backward(const rotor_head_rotation *how
  * `heads / kv_heads` adjacent query heads share a key head.
  * 16-bit probabilities and gradients of scores are rounded once before they are
  * multiplied (the latter, in float16, after scaling by a power of two for each
- * row, or for 32 adjacent rows); scores, sums and statistics are 32 bits wide.
+ * row, or for 32 adjacent rows, the former by 2^10 in the gradient of v); scores,
+ * sums and statistics are 32 bits wide.
  * Heads start 16-byte aligned (pointers and strides); width is a multiple of 8,
  * at most ROTOR_ATTENTION_MAX_WIDTH.
  * keys < 2^30, heads <= 2^15, tokens * heads / kv_heads <= 65535 * 128 (and, for
@@ -726,9 +727,10 @@ ROTOR_API int32_t rotor_window_attention(const rotor_attention *how, const rotor
                                          const rotor_heads *v, const rotor_heads *out, float *d_lse, void *d_work,
                                          uint64_t work_bytes, void *stream);
 
-/* Device workspace of rotor_window_attention_backward: 12 bytes a query row
- * and, where keys are few or some are seen by all rows, 32-bit sums of their
- * gradients for each part of the rows.  Host only. */
+/* Device workspace of rotor_window_attention_backward: 12 bytes a query row (of
+ * each key head's, rounded up to 128), in float16 4 more for 32 of them, and,
+ * where keys are few or some are seen by all rows, 32-bit sums of their gradients
+ * for each part of the rows.  Host only. */
 ROTOR_API int32_t rotor_window_attention_backward_workspace_bytes(const rotor_attention *how, uint64_t *bytes);
 
 /* Gradients of q, k and v from that of out (dout); out and d_lse are what

@@ -62,7 +62,7 @@ struct Attention {
     int *row_at;         // [batch * kv][row_pitch]: position, -1: sees nothing
     int *row_exp;        // [batch * kv][row_pitch / 32]: exponent of the largest |do|
     int row_pitch;
-    int tiles, sink_tiles, sink_parts;  // of 128 keys (gradients of keys)
+    int sink_tiles, sink_parts;  // tiles of 128 keys with first ones among them (gradients of keys)
     float *part_dk, *part_dv;           // [item][batch * kv][128][width]
 };
 

@@ -9,10 +9,11 @@ namespace rotor {
 namespace {
 
 constexpr int kKeys = 128;   // of a workgroup, gradients of keys
-constexpr int kFewSteps = 8;  // of keys, up to which delta is summed from its terms
 constexpr int kStepRows = 64;  // the most at a time
 
 #if defined(__HIP_DEVICE_COMPILE__)
+constexpr int kFewSteps = 8;  // of keys, up to which delta is summed from its terms
+
 // float16 holds 40 bits of range, and dS is as small as the gradients that
 // arrive, times a probability: it is multiplied by a power of two, so that the
 // largest |do| of a row (of 32 rows, where they are summed) comes to lie in
@@ -37,7 +38,8 @@ __device__ inline float power_of(int e) { return __builtin_amdgcn_ldexpf(1.f, e)
 // multiply do with the values, the exponentials of the scores are computed, and
 // while they work on the next step's scores, the gradients of this one's.  It
 // also leaves what the gradients of keys need of each row: log-sum-exp, delta,
-// position.
+// position.  Bound as the forward kernel; 16384 tokens, 32 heads on 8, 128 wide,
+// bf16: 2.68 ms (3.3 TF, 1.23 PF/s).
 template <typename T, int NB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel(Attention a)
 {
@@ -233,8 +235,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
 
 // dk and dv of 128 keys, 32 a wave: the rows that see any of them pass through
 // LDS, 64 at a time.  Past 96 columns sums and keys fill the registers: the
-// values are read from LDS, and rows come 32 at a time.  blockIdx.y: first the tiles with keys that every later row
-// sees, whose rows are split into sink_parts, then the others, in parts.
+// values are read from LDS, and rows come 32 at a time.  blockIdx.y: first the
+// tiles with keys that every later row sees, whose rows are split into
+// sink_parts, then the others, in parts.
+// Bound by its registers: two waves a SIMD, and no room to read operands ahead.
+// 16384 tokens, 32 heads on 8, 128 wide, bf16: 4.06 ms (4.4 TF, 1.08 PF/s); with
+// dk and dv in waves of their own that hand each other the probabilities, which
+// leaves that room, the same within 2%, and 64 columns (4 x 4096 tokens, 16 heads,
+// f16) 496 us instead of 382.
 template <typename T, int NB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(Attention a)
 {
@@ -446,7 +454,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
 }
 
 // The parts' sums of dk and dv joined, in their order: four columns a thread;
-// blockIdx.y: tile of keys (of those in parts), z: dk, dv.
+// blockIdx.y: tile of keys (of those in parts), z: dk, dv.  (1001 keys of 80
+// columns in f32, 3 x 4 heads, 4 to 12 parts: 39 MB in 8.5 us.)
 template <typename T> __global__ __launch_bounds__(256) void join_keys_kernel(Attention a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -580,7 +589,6 @@ int32_t rotor_window_attention_backward(const rotor_attention *how, const rotor_
     a.part_dk = (float *)(w += p.exp_bytes);
     a.part_dv = (float *)(w += p.part_bytes);
     a.row_pitch = p.row_pitch;
-    a.tiles = p.tiles;
     a.sink_tiles = p.sink_tiles;
     a.sink_parts = p.sink_parts;
     a.parts = p.parts;
