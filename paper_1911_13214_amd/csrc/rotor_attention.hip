@@ -98,7 +98,7 @@ __device__ inline void put_rows(const Attention &a, const Rows<T, NB> &w, int b,
 // of the one before, in one stream of independent instructions.  Three places
 // in LDS for keys and for values: one is read, two are on their way.
 // Bound by the matrix units, the exponentials beside them and the barrier of a
-// step: 16384 tokens, 32 heads on 8, 128 wide, bf16, take 1.93 ms (2.2 TF, 1.14
+// step: 16384 tokens, 32 heads on 8, 128 wide, bf16, take 1.97 ms (2.2 TF, 1.12
 // PF/s, the library's product of 8192 reaches 1.39); two rows of tiles a wave
 // spill.
 // blockIdx.x: key head and sequence (so that an XCD keeps to few of them),
@@ -301,7 +301,7 @@ __device__ inline float row_sum(float v)
 // used, and waits for no other before the end, when the waves' sums are joined.
 // The keys that any row sees are a list: the first ones, then the window's.
 // Bound by reading them: 64 sequences, a window of 4096, 8 key heads, 128 wide,
-// bf16: 1.08 GB in 187 us (5.7 TB/s).
+// bf16: 1.08 GB in 188 us (5.7 TB/s).
 // STEP: one token, whose key and value are new: they are in the place of the
 // last key of the list, and go into the cache.
 template <typename T, int NB, int R, bool STEP>

@@ -39,7 +39,7 @@ __device__ inline float power_of(int e) { return __builtin_amdgcn_ldexpf(1.f, e)
 // while they work on the next step's scores, the gradients of this one's.  It
 // also leaves what the gradients of keys need of each row: log-sum-exp, delta,
 // position.  Bound as the forward kernel; 16384 tokens, 32 heads on 8, 128 wide,
-// bf16: 2.68 ms (3.3 TF, 1.23 PF/s).
+// bf16: 2.75 ms (3.3 TF, 1.20 PF/s).
 template <typename T, int NB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel(Attention a)
 {
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
 // tiles with keys that every later row sees, whose rows are split into
 // sink_parts, then the others, in parts.
 // Bound by its registers: two waves a SIMD, and no room to read operands ahead.
-// 16384 tokens, 32 heads on 8, 128 wide, bf16: 4.06 ms (4.4 TF, 1.08 PF/s); with
+// 16384 tokens, 32 heads on 8, 128 wide, bf16: 4.34 ms (4.4 TF, 1.01 PF/s); with
 // dk and dv in waves of their own that hand each other the probabilities, which
 // leaves that room, the same within 2%, and 64 columns (4 x 4096 tokens, 16 heads,
 // f16) 496 us instead of 382.
