@@ -504,7 +504,12 @@ struct BackPlan {
 // where a tile holds first keys, which all rows see, into parts about as long as
 // the other tiles', or as half of what a workgroup's place gets to do in all (two
 // sequences of 8192, 8 key heads, window 1024: 4 first keys in one part would
-// take 7 times as long as other tiles).
+// take 7 times as long as other tiles).  Under a window tiles have about the same
+// to do, and the parts are those with the fewest steps on all places, one more
+// counted for each part (3001 tokens, 16 heads on 4, 96 wide, window 500, bf16:
+// 120 us with two workgroups a CU at least, 111 so); without one the last keys'
+// tiles are short, and more parts even it out (4 x 1000 tokens, 16 heads on 4, 64
+// wide, f32: 443 us, counted as under a window 552).
 bool back_plan(const rotor_attention *n, BackPlan &p)
 {
     const int64_t group = n->heads / n->kv_heads, rows = n->tokens * group, bk = n->batch * n->kv_heads;
@@ -514,19 +519,30 @@ bool back_plan(const rotor_attention *n, BackPlan &p)
     const int64_t sink_tiles = ceil_div(sinks, kKeys);
     const int64_t seen = windowed && n->window + kKeys - 1 < n->tokens ? n->window + kKeys - 1 : n->tokens;
     const int64_t steps = ceil_div(seen * group, kStepRows) + 1, sink_steps = ceil_div(rows, kStepRows);
-    const int64_t base = tiles * bk;
+    const int64_t base = tiles * bk, places = n->type == ROTOR_F32 ? 256 : 512;
+    const int64_t half = bk * (tiles * steps + sink_tiles * sink_steps) / (2 * places);
+    auto sink_parts_of = [&](int64_t k) {
+        int64_t each = steps / k > 4 ? steps / k : 4;
+        each = each > half ? each : half;
+        const int64_t s = ceil_div(sink_steps, each) > 64 ? 64 : ceil_div(sink_steps, each);
+        return s < k ? k : s;
+    };
+    auto items_of = [&](int64_t k) { return sink_tiles * sink_parts_of(k) + (tiles - sink_tiles) * k; };
     int64_t parts = 1;
-    if (base > 0 && base < 384) {
+    if (base > 0 && base < 384 && seen < n->tokens) {
+        int64_t least = 0;
+        for (int64_t k = 1; k <= 16 && (k == 1 || 4 * k <= steps); ++k) {
+            const int64_t cost = ceil_div(items_of(k) * bk, places) * (ceil_div(steps, k) + 1);
+            if (k == 1 || cost < least) {
+                parts = k;
+                least = cost;
+            }
+        }
+    } else if (base > 0 && base < 384) {
         parts = ceil_div(512, base) < steps / 4 ? ceil_div(512, base) : steps / 4;
         parts = parts < 1 ? 1 : parts > 16 ? 16 : parts;
     }
-    const int64_t half = bk * (tiles * steps + sink_tiles * sink_steps) / 1024;
-    int64_t each = steps / parts > 4 ? steps / parts : 4;
-    each = each > half ? each : half;
-    int64_t sink_parts = ceil_div(sink_steps, each);
-    sink_parts = sink_parts > 64 ? 64 : sink_parts;
-    sink_parts = sink_parts < parts ? parts : sink_parts;
-    const int64_t all = sink_tiles * sink_parts + (tiles - sink_tiles) * parts;
+    const int64_t sink_parts = sink_parts_of(parts), all = items_of(parts);
     if (all > 65535 || pitch > kMaxRows)
         return false;
     p.row_pitch = (int)pitch;
