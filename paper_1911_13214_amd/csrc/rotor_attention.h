@@ -122,6 +122,11 @@ template <typename T, int NB> struct Shape {
     static constexpr int kRow = kBlocks * 32 * (int)sizeof(T);
     static constexpr int kPieces = kRow / 16;
     static constexpr int NK = NB * (int)sizeof(T);                  // fragments of a row: 32 bytes each
+    // Fragments that every width of these blocks fills.  In 32 bits with three
+    // blocks the last 16 columns are left to a branch: 1001 tokens, 12 heads on 4, 80
+    // wide, window 257, take 243 us instead of 254.  With two and four blocks it
+    // would cost widths 64 and 128 2%.
+    static constexpr int kFilled = sizeof(T) == 4 && NB == 3 ? NK - 2 : NK;
     static constexpr int kGroups = 32 / (2 * Frag<T>::N);           // fragments of 32 summed rows
     static constexpr int kTurned = sizeof(T) == 4 ? 4 : 2;          // reads of a fragment of columns
     static __device__ int turn(int row)
@@ -195,8 +200,10 @@ template <typename T, int NB> struct Reader {
     typedef typename Frag<T>::F F;
     int straight;  // row lane % 32, its half of the first 32 bytes
     int cross[sizeof(T) == 4 ? 4 : 1];
-    __device__ void init(int lane)
+    bool full;  // the width reaches into the last 16 columns of the blocks
+    __device__ void init(int lane, int width)
     {
+        full = width > NB * 32 - 16;
         const int row = lane % 32, h = lane / 32;
         straight = row * S::kRow + (h ^ S::turn(row)) * 16;
         if constexpr (sizeof(T) == 2) {
@@ -336,8 +343,13 @@ __device__ inline f32x16 product(const char *tile, const Reader<T, NB> &rd,
 #pragma unroll
     for (int e = 0; e < 16; ++e)
         s[e] = 0.f;
+    typedef Shape<T, NB> S;
+    if (S::kFilled < S::NK && rd.full)
 #pragma unroll
-    for (int k = 0; k < Shape<T, NB>::NK; ++k)
+        for (int k = S::kFilled; k < S::NK; ++k)
+            s = Frag<T>::mma(rd.row(tile, k), f[k], s);
+#pragma unroll
+    for (int k = 0; k < S::kFilled; ++k)
         s = Frag<T>::mma(rd.row(tile, k), f[k], s);
     return s;
 }
@@ -351,14 +363,20 @@ __device__ inline void fetch_rows(const char *tile, const Reader<T, NB> &rd, typ
     for (int k = 0; k < Shape<T, NB>::NK; ++k)
         f[k] = rd.row(tile, k);
 }
-template <typename T, int NK>
-__device__ inline void multiply(f32x16 &s, const typename Frag<T>::F (&a)[NK], const typename Frag<T>::F (&b)[NK])
+template <typename T, int NB>
+__device__ inline void multiply(f32x16 &s, const typename Frag<T>::F (&a)[Shape<T, NB>::NK],
+                                const typename Frag<T>::F (&b)[Shape<T, NB>::NK], const Reader<T, NB> &rd)
 {
+    typedef Shape<T, NB> S;
 #pragma unroll
     for (int e = 0; e < 16; ++e)
         s[e] = 0.f;
+    if (S::kFilled < S::NK && rd.full)
 #pragma unroll
-    for (int k = 0; k < NK; ++k)
+        for (int k = S::kFilled; k < S::NK; ++k)
+            s = Frag<T>::mma(a[k], b[k], s);
+#pragma unroll
+    for (int k = 0; k < S::kFilled; ++k)
         s = Frag<T>::mma(a[k], b[k], s);
 }
 

@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
     lk.init(wave, lane, a.width, a.k.token);
     lv.init(wave, lane, a.width, a.v.token);
     Reader<T, NB> rd;
-    rd.init(lane);
+    rd.init(lane, a.width);
     const char *const k0 = rows_of(a.k, b, kv), *const v0 = rows_of(a.v, b, kv);
     const uint32_t k_stride = (uint32_t)a.k.token, v_stride = (uint32_t)a.v.token;
     const int row_bytes = a.width * (int)sizeof(T);
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void attention_ke
         const bool raised = w.raise(s, a.c, by);
         __builtin_amdgcn_sched_barrier(0);
         f32x16 ahead;
-        multiply<T>(ahead, kf, w.q);
+        multiply<T, NB>(ahead, kf, w.q, rd);
         w.soften(s, a.c);
         add_rows<T, NB>(w.acc, last_vals, rd, before);
         before = Packed<T, NB>(s);

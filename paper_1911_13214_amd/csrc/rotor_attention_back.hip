@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
     lk.init(wave, lane, a.width, a.k.token);
     lv.init(wave, lane, a.width, a.v.token);
     Reader<T, NB> rd;
-    rd.init(lane);
+    rd.init(lane, a.width);
     const char *const k0 = rows_of(a.k, b, kv), *const v0 = rows_of(a.v, b, kv);
     const uint32_t k_stride = (uint32_t)a.k.token, v_stride = (uint32_t)a.v.token;
     const int row_bytes = a.width * (int)sizeof(T), all_from = whi - a.window + 1;
@@ -179,12 +179,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void query_kernel
         mask(s, j, -kInf);  // before the exponentials: their gradients are 0 times what is finite
         __builtin_amdgcn_sched_barrier(0);
         f32x16 dp, ahead;
-        multiply<T>(dp, f, d);
+        multiply<T, NB>(dp, f, d, rd);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             s[e] = exp2_of(__builtin_fmaf(s[e], a.c, -lse));
         fetch_rows<T, NB>(next_keys, rd, f);
-        multiply<T>(ahead, f, q);
+        multiply<T, NB>(ahead, f, q, rd);
         slope(s, dp);
         add_rows<T, NB>(acc, keys, rd, Packed<T, NB>(s));
         constexpr int kColumns = S::kGroups * NB, kReads = S::kTurned * kColumns;
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void key_kernel(A
     const Span span(a, b);
     const bool have = key < span.length;
     Reader<T, NB> rd;
-    rd.init(lane);
+    rd.init(lane, a.width);
     F kf[S::NK], vf[kHeld ? S::NK : 1];
     {
         const char *k = rows_of(a.k, b, kv) + key * a.k.token, *v = rows_of(a.v, b, kv);
