@@ -414,6 +414,21 @@ __device__ inline void add_rows(f32x16 (&acc)[NB], const char *tile, const Reade
             acc[b] = Frag<T>::mma(rd.column(tile, g, b), p.f[g], acc[b]);
 }
 
+// The same for two operands, whose sums take each fragment once.
+template <typename T, int NB>
+__device__ inline void add_rows_twice(f32x16 (&x)[NB], f32x16 (&y)[NB], const char *tile, const Reader<T, NB> &rd,
+                                      const Packed<T, NB> &p, const Packed<T, NB> &q)
+{
+#pragma unroll
+    for (int g = 0; g < Shape<T, NB>::kGroups; ++g)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const typename Frag<T>::F f = rd.column(tile, g, b);
+            x[b] = Frag<T>::mma(f, p.f[g], x[b]);
+            y[b] = Frag<T>::mma(f, q.f[g], y[b]);
+        }
+}
+
 // The same row by row, for tiles that hold infinities or NaN: where a factor
 // is 0 (a row and a key that do not see each other), nothing is added.
 template <typename T, int NB>

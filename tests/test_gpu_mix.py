@@ -489,3 +489,46 @@ def test_float16_gradients_of_large_values_and_small_probabilities():
     for x, name in zip((got[0], *got[2:]), ("out", "dq", "dk", "dv")):
         m.close(x, val[name], err[name], name)
     check("f16", 1, 1400, 1400, 1, 1, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [8, 32, 64])
+def test_the_rounding_of_the_output_stays_out_of_the_queries_gradients(dtype, d):
+    """Keys that are all the same: the gradients of a row's scores sum to 0, and
+    with them dq and, over the rows, what dk takes from each.  Values next to 8,
+    so that do times the rounded output misses that sum by far more than the
+    roundings of the single gradients."""
+    n, t = 700, m.DTYPES[dtype]
+    unit, scale = m.UNIT[t], d ** -0.5
+    g = torch.Generator().manual_seed(d)
+    q, dout = m.normal(g, 1, n, 1, d, dtype=t), m.normal(g, 1, n, 1, d, dtype=t)
+    k = torch.full((1, n, 1, d), 0.5, dtype=t)
+    step = 2.0 ** -4 if dtype == "bf16" else 2.0 ** -7  # between numbers from 8 on
+    v = (8 + step * torch.randint(0, 2, (1, n, 1, d), generator=g)).to(t)
+    out, lse = ops.window_attention(q.cuda(), k.cuda(), v.cuda())
+    dq, dk, _ = ops.window_attention_backward(dout.cuda(), q.cuda(), k.cuda(), v.cuda(), out, lse)
+    do, vv, o, qq = (x[0, :, 0].double().cpu() for x in (dout, v, out, q))
+    see = torch.ones(n, n, dtype=torch.float64).tril()
+    p = see / see.sum(1, keepdim=True)
+    dp, rough = do @ vv.T, (do * o).sum(1, keepdim=True)
+    missing = (p * (dp - rough)).sum(1, keepdim=True)
+    # roundings of P (dP - delta) and, for what is put right, of P; sums of n
+    # terms in 32 bits of the size of do v; float16's P below 2^-14 lose 2^-25
+    size = m.U32 * (n + d + 32) * do.abs() @ vv.abs().T.amax(1, keepdim=True)
+    least = 2.0 ** -25 * see.sum(1, keepdim=True) if dtype == "f16" else 0.0
+    off = unit * (p * (dp - rough).abs()).sum(1, keepdim=True) + (unit + least) * missing.abs() + size
+    if dtype == "f16":
+        # dS times 2^(3 - e) and more: what is below 2^-14 loses 2^-25 of it
+        off += 2.0 ** -25 * 2.0 ** -2 * do.abs().amax(1, keepdim=True) * see.sum(1, keepdim=True)
+    # (a result below float16's normal numbers is off by 2^-25, half its least step)
+    bound = scale * 0.5 * off * (1 + unit) + m.TINY[t]
+    assert (dq[0, :, 0].double().cpu().abs() <= bound).all()
+    # what the test can tell: rows that would miss 4 times their bound (in float16 a
+    # share of them: o misses 2^-9 on average, sqrt(d) of that in delta, and 4 times
+    # the bound of the 32-bit sums is 4 * 2^-24 * (700 + d) * 8 * sqrt(d), the same)
+    assert (scale * 0.5 * missing.abs() > 4 * bound)[300:].any()
+    want = scale * (p * (dp - (p * dp).sum(1, keepdim=True))).T @ qq
+    err = scale * (p * (unit * (dp - rough).abs() + unit * missing.abs() + size)).T @ qq.abs() + unit * want.abs()
+    if dtype == "f16":
+        err += scale * 2.0 ** -27 * (see.T @ (do.abs().amax() * qq.abs()))
+    assert ((dk[0, :, 0].double().cpu() - want).abs() <= err * (1 + unit) + m.TINY[t]).all()
