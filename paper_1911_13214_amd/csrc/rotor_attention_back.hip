@@ -558,9 +558,12 @@ bool back_plan(const rotor_attention *n, BackPlan &p)
     const int64_t seen = windowed && n->window + kKeys - 1 < n->tokens ? n->window + kKeys - 1 : n->tokens;
     const int64_t steps = ceil_div(seen * group, kStepRows) + 1, sink_steps = ceil_div(rows, kStepRows);
     const int64_t base = tiles * bk, places = n->type == ROTOR_F32 ? 256 : 512;
+    // steps of a part: in 32 bits one takes longer than the join (97 tokens, 21 heads
+    // on 3, 128 wide: 149 us with four at least, 98 with one), in 16 a quarter of it
+    const int64_t shortest = n->type == ROTOR_F32 ? 1 : 4;
     const int64_t half = bk * (tiles * steps + sink_tiles * sink_steps) / (2 * places);
     auto sink_parts_of = [&](int64_t k) {
-        int64_t each = steps / k > 4 ? steps / k : 4;
+        int64_t each = steps / k > shortest ? steps / k : shortest;
         each = each > half ? each : half;
         const int64_t s = ceil_div(sink_steps, each) > 64 ? 64 : ceil_div(sink_steps, each);
         return s < k ? k : s;
@@ -569,7 +572,7 @@ bool back_plan(const rotor_attention *n, BackPlan &p)
     int64_t parts = 1;
     if (base > 0 && base < 384 && seen < n->tokens) {
         int64_t least = 0;
-        for (int64_t k = 1; k <= 16 && (k == 1 || 4 * k <= steps); ++k) {
+        for (int64_t k = 1; k <= 16 && (k == 1 || shortest * k <= steps); ++k) {
             const int64_t cost = ceil_div(items_of(k) * bk, places) * (ceil_div(steps, k) + 1);
             if (k == 1 || cost < least) {
                 parts = k;
@@ -577,7 +580,7 @@ bool back_plan(const rotor_attention *n, BackPlan &p)
             }
         }
     } else if (base > 0 && base < 384) {
-        parts = ceil_div(512, base) < steps / 4 ? ceil_div(512, base) : steps / 4;
+        parts = ceil_div(512, base) < steps / shortest ? ceil_div(512, base) : steps / shortest;
         parts = parts < 1 ? 1 : parts > 16 ? 16 : parts;
     }
     const int64_t sink_parts = sink_parts_of(parts), all = items_of(parts);
